@@ -310,6 +310,96 @@ gkv_status gkv_evict_launch_plan(const gkv_config* cfg, int32_t n_layers_in_laun
 typedef struct { int32_t tensor_core, grid, items, rows_per_item, stages, query_buffers, smem_bytes; } gkv_score_plan_t;
 gkv_status gkv_score_launch_plan(const gkv_config* cfg, int32_t n_layers_in_launch, int32_t sm_count, gkv_score_plan_t* out);
 
+/* ---- Key/value stores: caches of one layer in 16, 8 or 4 bits, and shared prefixes -------------------------------------
+ * (No counterpart in the paper, which stores its compressed cache in 16 bits and gives every sampled answer its own copy of
+ * the question.) A store is a plain description of caller-owned device buffers; the calls below keep no state between them,
+ * allocate nothing and run on the caller's stream and the current device. Sequence lengths are device arrays that the caller
+ * keeps (int32[batch]); no call changes them, so a call can be captured once and replayed while they grow.
+ *
+ * Layouts (d = 128)
+ *   k, v             [batch][n_kv_heads][capacity][row]     row = 128 bf16, 128 codes of 8 bits, or 64 bytes of 4-bit codes
+ *   k_scale, v_scale [batch][n_kv_heads][capacity][scales]  bf16; 1 scale a row in 8 bits, 4 a row (32 elements each) in 4 bits
+ * A code c of a group with scale s stands for c * s. With a = max |x| over the group:
+ *   E4M3  8-bit floats (4 exponent, 3 mantissa bits); s = 2^e, the smallest e >= -126 with a / 2^e <= 448
+ *   INT8  whole numbers -127..127, two's complement;  s = max(bf16(a / 127), 2^-126)
+ *   INT4  whole numbers -7..7, stored + 8 in a nibble; s = max(bf16(a / 7), 2^-126)
+ * and c = x / s rounded to nearest, ties to even. INT4 rows: elements 32g + 4q .. 32g + 4q + 3 are the nibbles, lowest first,
+ * of the row's 16-bit word 4q + g (g = 0..3, q = 0..7). A group that holds a NaN or an infinity gets s = NaN: it reads back as
+ * NaN and makes the attention over it NaN. */
+typedef enum { GKV_STORE_BF16 = 0, GKV_STORE_E4M3 = 1, GKV_STORE_INT8 = 2, GKV_STORE_INT4 = 3 } gkv_store_format;
+typedef struct {
+    int32_t format;                                                   /* gkv_store_format                                  */
+    int32_t batch, n_q_heads, n_kv_heads, head_dim;                   /* head_dim 128; n_q_heads / n_kv_heads <= 8          */
+    int32_t capacity;                                                 /* rows per head                                     */
+    void *k, *v;                                                      /* 16-byte aligned                                   */
+    void *k_scale, *v_scale;                                          /* 8-byte aligned; NULL for GKV_STORE_BF16            */
+} gkv_store;
+typedef struct { uint64_t k, v, k_scale, v_scale; } gkv_store_sizes;  /* bytes                                             */
+
+/* Bytes of the four buffers of a store (its pointers are not looked at).
+ * Errors: INVALID_ARG (NULL, sizes <= 0, unknown format, n_q_heads not a multiple of n_kv_heads), UNSUPPORTED (head_dim !=
+ * 128, more than 8 query heads per KV head, batch > 65535, capacity > 2^24, batch * n_q_heads >= 2^30). */
+gkv_status gkv_store_query_sizes(const gkv_store* store, gkv_store_sizes* out);
+
+/* Quantise as it is written: row first[i] + t of every head of sequence i becomes token t of k and v, for t < count[i].
+ * k, v: device, bf16, element (i, t, h, x) at i * seq_stride + t * token_stride + h * head_stride + x (strides in elements,
+ * multiples of 8; 16-byte aligned). first, count: device int32[batch]; NULL = 0 and n_tokens. n_tokens is the most tokens
+ * a sequence has (count[i] above it counts as n_tokens, below 0 as 0). Rows outside 0..capacity-1 are not written; rows
+ * that no token goes to are left as they were. The source may not overlap the store. n_tokens = 0 does nothing (k, v may be NULL).
+ * Errors: as gkv_store_query_sizes; INVALID_ARG (NULL or misaligned pointer, n_tokens < 0, a stride that is negative or not
+ * a multiple of 8), UNSUPPORTED (n_tokens * n_kv_heads >= 2^30), CUDA. */
+gkv_status gkv_store_write(const gkv_store* store, const void* k, const void* v, int64_t seq_stride, int64_t token_stride,
+                           int64_t head_stride, const int32_t* first, const int32_t* count, int32_t n_tokens, void* stream);
+
+/* Read back: token t of k and v of sequence i becomes bf16(c * s) of row first[i] + t, for t < count[i]; arguments as
+ * gkv_store_write with k, v written (two (i, t, h) may not share an address). Tokens from count[i] on, and those whose row
+ * is outside the store, are left as they were. Errors: as gkv_store_write. */
+gkv_status gkv_store_read(const gkv_store* store, void* k, void* v, int64_t seq_stride, int64_t token_stride,
+                          int64_t head_stride, const int32_t* first, const int32_t* count, int32_t n_tokens, void* stream);
+
+/* Prefixes shared by the sequences of a batch: sequence i attends to all rows of prefix i / (batch / n_prefix) besides its
+ * own. k, v: device, bf16 [n_prefix][n_kv_heads][rows][128], 16-byte aligned, of which prefix p has its first len[p] rows in
+ * use (len: HOST int32[n_prefix], 0..rows; what lies behind them is not used). */
+typedef struct {
+    int32_t n_prefix; /* 1..64, divides batch */
+    int32_t rows;
+    const int32_t* len;
+    const void *k, *v;
+} gkv_prefix;
+
+/* Bytes of workspace that gkv_store_attn needs for a store of this shape, at any lengths, with up to n_prefix prefixes of up
+ * to prefix_rows rows (0, 0: without a prefix). The workspace needs no initial contents and holds nothing between calls; calls
+ * that share one must not overlap on the GPU. Errors: as gkv_store_query_sizes; INVALID_ARG (negative, n_prefix > 64 or not
+ * a divisor of batch). */
+gkv_status gkv_store_attn_workspace(const gkv_store* store, int32_t n_prefix, int32_t prefix_rows, uint64_t* bytes);
+
+/* Decode attention over a store: one query token per sequence, standard GQA attention with scale 1 / sqrt(d) over rows
+ * 0..len[i]-1 of sequence i, the new token if there is one, and the rows of its prefix if there is one.
+ *   len      device int32[batch]. len[i] < 0: the sequence is left out (its out, lse and rows stay as they were). A length
+ *            that does not fit the store (above capacity, or capacity with a new token) gives NaN in out and lse, and nothing
+ *            is written to the store.
+ *   max_len  the longest length, for spreading the work (0: capacity). Results do not depend on it beyond rounding.
+ *   q, out   device, bf16 [batch][n_q_heads][128], 16-byte aligned
+ *   k_new, v_new  device, bf16 [batch][n_kv_heads][128], 16-byte aligned, or both NULL. The new row is quantised into row
+ *            len[i] and attended to as it stands there. The caller then counts len[i] up.
+ *   prefix   NULL: none
+ *   lse      device, fp32 [batch][n_q_heads], or NULL: the natural logarithm of the sum of exp(scaled logits)
+ * A sequence with nothing to attend to gets out = 0 and lse = -infinity.
+ * Errors: as gkv_store_query_sizes; INVALID_ARG (NULL or misaligned pointer, only one of k_new and v_new, max_len outside
+ * 0..capacity, n_prefix outside 1..64 or not a divisor of batch, a prefix length outside 0..rows, workspace_bytes too small),
+ * UNSUPPORTED (2^31 prefix rows or more over all prefixes and heads), CUDA. */
+gkv_status gkv_store_attn(const gkv_store* store, const int32_t* len, int32_t max_len, const void* q, const void* k_new,
+                          const void* v_new, const gkv_prefix* prefix, void* out, float* lse, void* workspace,
+                          uint64_t workspace_bytes, void* stream);
+
+/* gkv_decode_attn of one layer with a shared prefix in front of the compressed cache: append, attention over the prefix and
+ * the cache, len += 1. The prefix is not part of the cache and is never evicted. Window scores are not accumulated: a
+ * compression is scored from q_window, over the cached keys alone. Workspace: gkv_store_attn_workspace of a GKV_STORE_BF16
+ * store with this context's batch, heads and C as capacity (16-byte aligned, as there).
+ * Errors: as gkv_decode_attn and gkv_store_attn; INVALID_ARG (layer = -1, prefix == NULL), STATE (fuse_window_scores is on). */
+gkv_status gkv_decode_attn_prefix(gkv_ctx* ctx, int32_t layer, const void* q, const void* k_new, const void* v_new,
+                                  const gkv_prefix* prefix, void* out, void* workspace, uint64_t workspace_bytes, void* stream);
+
 /* Memory model of the paper's appendix "Memory Analysis": bytes of the full KV cache at
  * seq_len tokens, of the compressed cache ((b + s) rows instead of seq_len), and of the score
  * cache F (b - w entries per head), for `elem_bytes`-wide elements, over all layers and the

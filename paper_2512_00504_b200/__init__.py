@@ -22,13 +22,15 @@ _ROOT = _PKG.parent
 _CHECKED = os.environ.get("GKV_LIB_VARIANT", "") == "check"
 LIB_PATH = _PKG / ("libgkv_check.so" if _CHECKED else "libgkv.so")
 _SOURCES = ["gkv_api.cu", "gkv_decode.cu", "gkv_evict.cu", "gkv_score.cu", "gkv_score_tc.cu", "gkv_redundancy.cu",
-            "gkv_static_scratch.cu"]
+            "gkv_static_scratch.cu", "gkv_store.cu", "gkv_store_attn.cu", "gkv_prefix.cu", "gkv_store_api.cu"]
 
 GKV_OK, GKV_ERR_INVALID_ARG, GKV_ERR_STATE, GKV_ERR_CAPACITY, GKV_ERR_CUDA, GKV_ERR_TIMEOUT, GKV_ERR_UNSUPPORTED, \
     GKV_ERR_SCRATCH_LIMIT, GKV_ERR_INTERNAL = range(9)
 GKV_MODE_MAX, GKV_MODE_MEAN, GKV_MODE_SUM, GKV_MODE_LOCAL = range(4)
 GKV_STAGE_SCORE, GKV_STAGE_MERGE, GKV_STAGE_SELECT, GKV_STAGE_COMPACT, GKV_STAGE_REDUNDANCY = range(5)
 GKV_POLICY_SCORE, GKV_POLICY_STREAMING = range(2)
+GKV_STORE_BF16, GKV_STORE_E4M3, GKV_STORE_INT8, GKV_STORE_INT4 = range(4)
+STORE_FORMATS = {"bf16": GKV_STORE_BF16, "e4m3": GKV_STORE_E4M3, "int8": GKV_STORE_INT8, "int4": GKV_STORE_INT4}
 
 
 class GKVError(RuntimeError):
@@ -67,6 +69,20 @@ class gkv_evict_plan_t(ctypes.Structure):
 class gkv_score_plan_t(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("tensor_core", "grid", "items", "rows_per_item", "stages", "query_buffers",
                                               "smem_bytes")]
+
+
+class gkv_store(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("format", "batch", "n_q_heads", "n_kv_heads", "head_dim", "capacity")] + \
+               [(n, ctypes.c_void_p) for n in ("k", "v", "k_scale", "v_scale")]
+
+
+class gkv_store_sizes(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_uint64) for n in ("k", "v", "k_scale", "v_scale")]
+
+
+class gkv_prefix(ctypes.Structure):
+    _fields_ = [("n_prefix", ctypes.c_int32), ("rows", ctypes.c_int32), ("len", ctypes.POINTER(ctypes.c_int32)),
+                ("k", ctypes.c_void_p), ("v", ctypes.c_void_p)]
 
 
 class gkv_memory_model_t(ctypes.Structure):
@@ -132,6 +148,16 @@ def lib() -> ctypes.CDLL:
         L.gkv_evict_launch_plan.restype = ctypes.c_int
         L.gkv_score_launch_plan.argtypes = [P(gkv_config), i32, i32, P(gkv_score_plan_t)]
         L.gkv_score_launch_plan.restype = ctypes.c_int
+        u64 = ctypes.c_uint64
+        L.gkv_store_query_sizes.argtypes = [P(gkv_store), P(gkv_store_sizes)]
+        L.gkv_store_write.argtypes = [P(gkv_store), vp, vp, i64, i64, i64, vp, vp, i32, vp]
+        L.gkv_store_read.argtypes = [P(gkv_store), vp, vp, i64, i64, i64, vp, vp, i32, vp]
+        L.gkv_store_attn_workspace.argtypes = [P(gkv_store), i32, i32, P(u64)]
+        L.gkv_store_attn.argtypes = [P(gkv_store), vp, i32, vp, vp, vp, P(gkv_prefix), vp, vp, vp, u64, vp]
+        L.gkv_decode_attn_prefix.argtypes = [vp, i32, vp, vp, vp, P(gkv_prefix), vp, vp, u64, vp]
+        for name in ("gkv_store_query_sizes", "gkv_store_write", "gkv_store_read", "gkv_store_attn_workspace",
+                     "gkv_store_attn", "gkv_decode_attn_prefix"):
+            getattr(L, name).restype = ctypes.c_int
         L.gkv_strerror.argtypes = [ctypes.c_int]
         L.gkv_strerror.restype = ctypes.c_char_p
         L.gkv_destroy.argtypes = [vp]
@@ -292,6 +318,26 @@ def gkv_destroy(ctx):
     lib().gkv_destroy(ctx)
 
 
+# The tensor arguments of the calls on a store are checked by the holders below; these only marshal.
+def gkv_store_query_sizes(store: gkv_store) -> gkv_store_sizes:
+    out = gkv_store_sizes()
+    _check(lib().gkv_store_query_sizes(ctypes.byref(store), ctypes.byref(out)), "gkv_store_query_sizes")
+    return out
+
+
+def gkv_store_attn_workspace(store: gkv_store, n_prefix: int = 0, prefix_rows: int = 0) -> int:
+    out = ctypes.c_uint64()
+    _check(lib().gkv_store_attn_workspace(ctypes.byref(store), int(n_prefix), int(prefix_rows), ctypes.byref(out)),
+           "gkv_store_attn_workspace")
+    return out.value
+
+
+def gkv_decode_attn_prefix(ctx, layer, q, k_new, v_new, prefix, out, workspace):
+    """prefix: a Prefix; workspace: a uint8 tensor of gkv_store_attn_workspace bytes (GKVCache.prefix_workspace)."""
+    _check(lib().gkv_decode_attn_prefix(ctx, layer, _ptr(q), _ptr(k_new), _ptr(v_new), ctypes.byref(prefix.desc), _ptr(out),
+                                        _ptr(workspace), workspace.numel(), _stream()), "gkv_decode_attn_prefix")
+
+
 # ------------------------------------------------------------------ buffer holder
 class GKVCache:
     """Allocates the caller-owned buffers with torch and owns the context."""
@@ -365,5 +411,127 @@ class GKVCache:
         gkv_get_redundancy(self.ctx, layer, out)
         return out
 
+    def prefix_workspace(self, n_prefix, prefix_rows):
+        """Workspace of decode_attn_prefix for up to n_prefix prefixes of up to prefix_rows rows."""
+        import torch
+        c = self.cfg
+        shape = gkv_store(GKV_STORE_BF16, c.batch, c.n_q_heads, c.n_kv_heads, c.head_dim, self.C)
+        return torch.empty(gkv_store_attn_workspace(shape, n_prefix, prefix_rows), dtype=torch.uint8, device=self.device)
+
+    def decode_attn_prefix(self, layer, q, k_new, v_new, prefix, out, workspace):
+        gkv_decode_attn_prefix(self.ctx, layer, q, k_new, v_new, prefix, out, workspace)
+
     def poll(self):
         gkv_poll_device_status(self.ctx)
+
+
+def _stream_of(device):
+    """The current stream of `device`, which has to be the current device: the library launches on that one."""
+    import torch
+    if torch.cuda.current_device() != device.index:
+        raise ValueError(f"the store is on {device}, the current device is cuda:{torch.cuda.current_device()}")
+    return torch.cuda.current_stream(device).cuda_stream
+
+
+def _tensor(t, what, dtype, shape, device):
+    """Data pointer of a contiguous tensor of this type, shape and device."""
+    if t.dtype != dtype or t.shape != shape or t.device != device or not t.is_contiguous():
+        raise ValueError(f"{what}: a contiguous {dtype} tensor of shape {tuple(shape)} on {device} is needed, "
+                         f"got {t.dtype} {tuple(t.shape)} on {t.device}" + ("" if t.is_contiguous() else ", not contiguous"))
+    return t.data_ptr()
+
+
+class Prefix:
+    """Rows that the sequences of a batch share: k, v [n_prefix][kv heads][rows][128] bf16 on the device, of which prefix p
+    has its first lengths[p] in use. Sequence i of a batch belongs to prefix i // (batch // n_prefix)."""
+
+    def __init__(self, k, v, lengths):
+        import torch
+        if k.dim() != 4 or k.shape[3] != 128 or k.device.type != "cuda":
+            raise ValueError("k, v: bf16 device tensors [n_prefix][kv heads][rows][128]")
+        pk, pv = (_tensor(t, n, torch.bfloat16, k.shape, k.device) for t, n in ((k, "k"), (v, "v")))
+        lengths = [int(n) for n in lengths]
+        if len(lengths) != k.shape[0]:
+            raise ValueError(f"{len(lengths)} lengths for {k.shape[0]} prefixes")
+        self.k, self.v, self.h_kv = k, v, k.shape[1]
+        self._len = (ctypes.c_int32 * len(lengths))(*lengths)
+        self.desc = gkv_prefix(k.shape[0], k.shape[2], self._len, pk, pv)
+
+
+class KVStore:
+    """K and V rows of one layer in 16, 8 or 4 bits (layouts in gkv.h), with the workspace of its attention.
+
+    fmt: "bf16", "e4m3", "int8" or "int4". The buffers are allocated here (uninitialised: rows are written before they are
+    read) or given: (k, v, k_scale, v_scale), for bf16 (k, v). max_prefix and n_prefix: the longest prefix and the most
+    prefixes that attn will be given. Calls of one store must not overlap on the GPU (they share the workspace)."""
+
+    def __init__(self, fmt, *, batch, h_q, h_kv, capacity, device=None, buffers=None, max_prefix=0, n_prefix=0):
+        import torch
+        self.fmt, self.batch, self.h_q, self.h_kv, self.capacity = fmt, batch, h_q, h_kv, capacity
+        if fmt not in STORE_FORMATS:
+            raise ValueError(f"format {fmt!r}: one of {sorted(STORE_FORMATS)} is needed")
+        self.desc = gkv_store(STORE_FORMATS[fmt], batch, h_q, h_kv, 128, capacity)
+        self.sizes = gkv_store_query_sizes(self.desc)
+        code = {"bf16": torch.bfloat16, "e4m3": torch.float8_e4m3fn, "int8": torch.int8, "int4": torch.uint8}[fmt]
+        scales = {"bf16": 0, "e4m3": 1, "int8": 1, "int4": 4}[fmt]
+        shape, s_shape = torch.Size((batch, h_kv, capacity, 64 if fmt == "int4" else 128)), torch.Size((batch, h_kv, capacity, scales))
+        if buffers is None:
+            device = torch.device(device or "cuda")
+            buffers = [torch.empty(shape, dtype=code, device=device) for _ in range(2)]
+            if scales:
+                buffers += [torch.empty(s_shape, dtype=torch.bfloat16, device=device) for _ in range(2)]
+        if len(buffers) != (4 if scales else 2):
+            raise ValueError(f"{len(buffers)} buffers for format {fmt}")
+        self.device = buffers[0].device
+        for t, n in zip(buffers, ("k", "v")):
+            setattr(self.desc, n, _tensor(t, n, code, shape, self.device))
+        for t, n in zip(buffers[2:], ("k_scale", "v_scale")):
+            setattr(self.desc, n, _tensor(t, n, torch.bfloat16, s_shape, self.device))
+        self.k, self.v = buffers[0], buffers[1]
+        self.k_scale, self.v_scale = (buffers[2], buffers[3]) if scales else (None, None)
+        self.workspace = torch.empty(gkv_store_attn_workspace(self.desc, n_prefix, max_prefix), dtype=torch.uint8, device=self.device)
+        self._desc = ctypes.byref(self.desc)
+        self._ws = (self.workspace.data_ptr(), self.workspace.numel())
+        self._q_shape, self._kv_shape = torch.Size((batch, h_q, 128)), torch.Size((batch, h_kv, 128))
+        self._lse_shape, self._len_shape = torch.Size((batch, h_q)), torch.Size((batch,))
+        self._bf16, self._f32, self._i32 = torch.bfloat16, torch.float32, torch.int32
+
+    def _copy_args(self, k, v, first, count):
+        """k, v [batch][tokens][kv heads][128] with any strides whose last one is 1; the same ones for both."""
+        for t, n in ((k, "k"), (v, "v")):
+            if t.dtype != self._bf16 or t.dim() != 4 or t.shape[0] != self.batch or t.shape[2] != self.h_kv or t.shape[3] != 128 or \
+                    t.shape != k.shape or t.device != self.device:
+                raise ValueError(f"{n}: a bf16 tensor [{self.batch}][tokens][{self.h_kv}][128] on {self.device} is needed, "
+                                 f"got {t.dtype} {tuple(t.shape)} on {t.device}")
+        strides = [tuple(0 if n == 1 else st for n, st in zip(t.shape, t.stride())) for t in (k, v)]   # of steps that are taken
+        if strides[0] != strides[1] or strides[0][3] != 1:
+            raise ValueError(f"k, v: strides {k.stride()}, {v.stride()}: the last one has to be 1, and the two have to agree")
+        p_first = None if first is None else _tensor(first, "first", self._i32, self._len_shape, self.device)
+        p_count = None if count is None else _tensor(count, "count", self._i32, self._len_shape, self.device)
+        ss, ts, hs, _ = strides[0]
+        return k.data_ptr(), v.data_ptr(), ss, ts, hs, p_first, p_count, k.shape[1], _stream_of(self.device)
+
+    def write(self, k, v, first=None, count=None):
+        """Quantise tokens into rows first[i] .. first[i] + count[i] - 1 of every sequence i (first, count: int32 on the
+        device; None: 0 and all tokens)."""
+        _check(lib().gkv_store_write(self._desc, *self._copy_args(k, v, first, count)), "gkv_store_write")
+
+    def read(self, k, v, first=None, count=None):
+        """Read the same rows back as bf16 into k and v; tokens from count[i] on are left as they were."""
+        _check(lib().gkv_store_read(self._desc, *self._copy_args(k, v, first, count)), "gkv_store_read")
+
+    def attn(self, length, q, out, k_new=None, v_new=None, prefix=None, lse=None, max_len=0):
+        """Decode attention over rows 0 .. length[i] - 1 (int32 on the device), the new token (appended at row length[i]) and
+        the sequence's prefix. The caller counts length up. max_len: the longest length (0: the capacity)."""
+        dev = self.device
+        if prefix is not None and (prefix.k.device != dev or prefix.h_kv != self.h_kv):
+            raise ValueError(f"the prefix has {prefix.h_kv} KV heads on {prefix.k.device}, the store {self.h_kv} on {dev}")
+        ws, ws_bytes = self._ws
+        _check(lib().gkv_store_attn(
+            self._desc, _tensor(length, "length", self._i32, self._len_shape, dev), max_len,
+            _tensor(q, "q", self._bf16, self._q_shape, dev),
+            None if k_new is None else _tensor(k_new, "k_new", self._bf16, self._kv_shape, dev),
+            None if v_new is None else _tensor(v_new, "v_new", self._bf16, self._kv_shape, dev),
+            None if prefix is None else ctypes.byref(prefix.desc), _tensor(out, "out", self._bf16, self._q_shape, dev),
+            None if lse is None else _tensor(lse, "lse", self._f32, self._lse_shape, dev), ws, ws_bytes, _stream_of(dev)),
+            "gkv_store_attn")

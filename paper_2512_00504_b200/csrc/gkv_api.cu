@@ -115,9 +115,12 @@ EncodeTiledFn encode_tiled_fn() {
     return fn;
 }
 
+}  // namespace
+
+namespace gkv {
 // 2-D view of a buffer of 128-element bf16 rows: [rows][128], boxes of box_rows rows x 64 elements,
 // 128-byte swizzle (K and V: 64-row boxes; 16-row and 128-row boxes for the kernels that want them).
-gkv_status encode_map(CUtensorMap* map, void* base, uint64_t rows, uint32_t box_rows = kTileKeys) {
+gkv_status encode_map(CUtensorMap* map, void* base, uint64_t rows, uint32_t box_rows) {
     const EncodeTiledFn fn = encode_tiled_fn();
     if (!fn) return GKV_ERR_CUDA;
     const cuuint64_t dims[2] = {(cuuint64_t)kHeadDim, (cuuint64_t)rows};
@@ -129,6 +132,9 @@ gkv_status encode_map(CUtensorMap* map, void* base, uint64_t rows, uint32_t box_
                           CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS ? GKV_OK : GKV_ERR_CUDA;
 }
+}  // namespace gkv
+
+namespace {
 
 // 3-D view of the window queries [heads][w][128] bf16 for the tensor-core scoring kernel: one box = box_rows
 // consecutive window rows of `g` consecutive heads x 64 elements (128-byte swizzle), so a block of window rows of all
@@ -359,7 +365,7 @@ gkv_status gkv_init(gkv_ctx** out, const gkv_config* cfg, const gkv_buffers* b, 
                  redundancy_kernel_setup() == cudaSuccess;
     if (ok) {
         const uint64_t rows = (uint64_t)cfg->n_layers * ctx->units_per_layer * ctx->C;
-        ok = encode_map(&ctx->tm_k, b->k, rows) == GKV_OK && encode_map(&ctx->tm_v, b->v, rows) == GKV_OK &&
+        ok = encode_map(&ctx->tm_k, b->k, rows, kTileKeys) == GKV_OK && encode_map(&ctx->tm_v, b->v, rows, kTileKeys) == GKV_OK &&
              encode_map(&ctx->tm_k128, b->k, rows, kScoreTcKeyBoxRows) == GKV_OK && encode_map(&ctx->tm_k16, b->k, rows, 16) == GKV_OK && encode_map(&ctx->tm_v16, b->v, rows, 16) == GKV_OK;
     }
     if (!ok) {
@@ -641,7 +647,7 @@ gkv_status gkv_compress_prompt(gkv_ctx* ctx, int32_t layer, const void* k_prompt
     if (any_long && scored) {
         CUtensorMap tm_kp, tm_kp128;
         const uint64_t rows = (uint64_t)c.batch * c.n_kv_heads * c.max_prompt;
-        if (encode_map(&tm_kp, const_cast<void*>(k_prompt), rows) != GKV_OK ||
+        if (encode_map(&tm_kp, const_cast<void*>(k_prompt), rows, kTileKeys) != GKV_OK ||
             encode_map(&tm_kp128, const_cast<void*>(k_prompt), rows, kScoreTcKeyBoxRows) != GKV_OK)
             return GKV_ERR_CUDA;
         ScoreLaunch sp;

@@ -13,6 +13,8 @@
 
 namespace gkv {
 
+constexpr int kHeadDimHost = 128;   // d
+
 // Offsets (bytes) of the regions of the caller-allocated workspace.
 struct WorkspaceLayout {
     uint64_t status;      // int32[64]   latched device status + diagnostics
@@ -125,6 +127,45 @@ struct ScoreLaunch {
     float scale_log2;
 };
 
+// ---- key/value stores and shared prefixes
+constexpr int kMaxPrefixes = 64;
+constexpr int kOwnRecFloats = 32 + kHeadDimHost * 8;            // partial result of one unit's split: M[8], L[8], Mv[8], pad, O[128][8]
+constexpr int kPrefixRows = 256;                                // query rows of a prefix work item
+constexpr int kPrefixRecFloats = kPrefixRows * (2 + kHeadDimHost);   // M[256], L[256], O[128][256]
+
+struct StoreCopyLaunch {       // write / read
+    uint8_t* data[2];          // the store's k, v
+    __nv_bfloat16* scale[2];
+    __nv_bfloat16* x[2];       // the bf16 side (not written by a write)
+    int64_t seq_stride, token_stride, head_stride;
+    const int32_t* first;      // may be NULL
+    const int32_t* count;      // may be NULL
+    int batch, h_kv, capacity, n_tokens, format;
+};
+
+struct StoreAttnLaunch {
+    uint8_t *k, *v;
+    __nv_bfloat16 *k_scale, *v_scale;
+    const int32_t* len;
+    int32_t* len_out;          // may be NULL: receives len + 1 (gkv_decode_attn_prefix)
+    const __nv_bfloat16 *q, *k_new, *v_new;
+    __nv_bfloat16* out;
+    float* lse;                // may be NULL
+    float* own_part;           // [units][splits][kOwnRecFloats]
+    float* prefix_part;        // [prefix items][kPrefixRecFloats], or NULL without a prefix
+    int format, batch, h_q, h_kv, g, capacity;
+    int splits, split_tiles;   // pieces of a unit and 16-key tiles of a piece (the last piece takes what is left)
+    float scale_log2;
+    // shared prefixes
+    const __nv_bfloat16 *k_prefix, *v_prefix;
+    int n_prefix, prefix_rows, seqs_per_prefix;
+    int seqs_per_block, n_blocks;   // sequences of a row block; row blocks of a (prefix, KV head)
+    int two_tiles;                  // a block has more than 128 rows: two query tiles that see every key tile
+    int chunk;                      // 128-key tiles of a prefix item
+    int prefix_items;
+    int32_t prefix_len[kMaxPrefixes];
+};
+
 }  // namespace gkv
 
 struct gkv_ctx {
@@ -167,5 +208,12 @@ cudaError_t launch_redundancy(const RedundancyLaunch& p, const CUtensorMap& tm_k
 cudaError_t redundancy_kernel_setup();
 cudaError_t decode_kernel_setup();
 cudaError_t score_kernel_setup();
+cudaError_t launch_store_write(const StoreCopyLaunch& p, cudaStream_t s);
+cudaError_t launch_store_read(const StoreCopyLaunch& p, cudaStream_t s);
+cudaError_t launch_store_attn(const StoreAttnLaunch& p, cudaStream_t s);                    // a unit's own rows
+cudaError_t launch_prefix_attn(const StoreAttnLaunch& p, const CUtensorMap& tm_k, const CUtensorMap& tm_v, cudaStream_t s);
+cudaError_t launch_store_merge(const StoreAttnLaunch& p, cudaStream_t s);
+void store_plan(StoreAttnLaunch* p, int max_len, int sm_count);                             // splits, row blocks, chunk, items
+gkv_status encode_map(CUtensorMap* map, void* base, uint64_t rows, uint32_t box_rows);      // [rows][128] bf16, 64-element boxes
 
 }  // namespace gkv

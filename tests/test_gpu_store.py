@@ -1,0 +1,519 @@
+"""Key/value stores on the GPU against the fp64 reference: quantised write and read back (bit-exact), decode attention over a
+store with the new row appended, shared prefixes, and the prefix in front of a context's compressed cache."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2512_00504_b200 as gkv
+import store_reference as ref
+
+pytestmark = pytest.mark.gpu
+DEV = torch.device("cuda:0")
+FORMATS = ["bf16", "e4m3", "int8", "int4"]
+
+
+@pytest.fixture(scope="module", autouse=True)
+def built():
+    gkv.build_library()
+
+
+def gen(seed):
+    return torch.Generator(device=DEV).manual_seed(seed)
+
+
+def randn(g, *shape):
+    return torch.randn(*shape, generator=g, device=DEV).to(torch.bfloat16)
+
+
+def f64(t):
+    return t.detach().double().cpu().numpy()
+
+
+def ints(x):
+    return torch.tensor(x, dtype=torch.int32, device=DEV)
+
+
+def raw(t):
+    return t.contiguous().view(torch.uint8).cpu().numpy()
+
+
+def wide_rows(seed, n):
+    """Rows that go wrong easily: all magnitudes bf16 has, ties, zeros, single large elements, values at the scales' borders."""
+    rng = np.random.RandomState(seed)
+    x = rng.randn(n, 128) * np.exp2(rng.randint(-133, 120, (n, 1)).astype(float))
+    x[0] = 0
+    x[1] = rng.randint(-254, 255, 128) / 2.0
+    x[1, 0] = 127                                        # int8 scale 1: halves are ties
+    x[2] = rng.randint(-14, 15, 128) / 2.0
+    x[2, ::32] = 7                                       # int4 scale 1: ties
+    x[3] = 448 * rng.choice([-1, 1, 0.5, 0.25], 128)
+    x[4] = 450 * rng.choice([-1, 1, 0.5, 0.25], 128)     # just above 448 (bf16 450)
+    x[5] = 2.0 ** -133 * rng.randint(-3, 4, 128)         # subnormals
+    x[6] = rng.randn(128) * 1e-3
+    x[6, 77] = 3e38
+    x[7] = np.exp2(rng.randint(-30, 1, 128))
+    x[8, 64:96] = 0                                      # a zero group among others
+    x[9] = 17 * 2.0 ** -4 * rng.choice([1, 3, 5, 7], 128)
+    x[9, 0] = 256                                        # e4m3: ties between neighbouring codes
+    return torch.from_numpy(np.clip(x, -3.3e38, 3.3e38)).to(torch.bfloat16).to(DEV)
+
+
+def expect_codes(x, fmt):
+    """bytes [..., row], scales fp64 [..., groups] of rows x."""
+    if fmt == "bf16":
+        return raw(x).reshape(x.shape[:-1] + (256,)), np.zeros(x.shape[:-1] + (0,))
+    c, s = ref.encode(f64(x), fmt)
+    return ref.pack(c, fmt), s
+
+
+def dequantised(store):
+    """The store's rows as fp64, by the reference's reading of its bytes."""
+    got = []
+    for codes, scale in ((store.k, store.k_scale), (store.v, store.v_scale)):
+        if store.fmt == "bf16":
+            got.append(f64(codes))
+        elif store.fmt == "int4":
+            b = codes.cpu().numpy().astype(np.int64)
+            c = np.zeros(b.shape[:-1] + (128,))
+            for e in range(128):
+                w, i = 4 * (e % 32 // 4) + e // 32, e % 4
+                c[..., e] = ((b[..., 2 * w + i // 2] >> (4 * (i % 2))) & 15) - 8
+            got.append(ref.values(c, f64(scale), "int4"))
+        else:
+            got.append(ref.values(f64(codes.float()), f64(scale), store.fmt))
+    return got
+
+
+# ---------------------------------------------------------------------------------------------- write, read
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_codes_of_all_magnitudes(fmt):
+    n = 480
+    k, v = wide_rows(1, n), wide_rows(2, n)
+    st = gkv.KVStore(fmt, batch=1, h_q=6, h_kv=3, capacity=n // 3, device=DEV)
+    st.write(k.view(1, n // 3, 3, 128), v.view(1, n // 3, 3, 128))
+    for x, codes, scale in ((k, st.k, st.k_scale), (v, st.v, st.v_scale)):
+        want, s = expect_codes(x.view(n // 3, 3, 128).transpose(0, 1).contiguous(), fmt)
+        assert (raw(codes[0]).reshape(want.shape) == want).all()
+        if fmt != "bf16":
+            assert (f64(scale[0]) == s).all()
+    back = torch.empty((2, 1, n // 3, 3, 128), dtype=torch.bfloat16, device=DEV)
+    st.read(back[0], back[1])
+    if fmt == "bf16":
+        assert torch.equal(back[0].view(n, 128), k) and torch.equal(back[1].view(n, 128), v)
+    else:
+        for x, got in ((k, back[0]), (v, back[1])):
+            want = ref.round_bf16(ref.values(*ref.encode(f64(x), fmt), fmt))
+            assert (f64(got).reshape(n, 128) == want).all()
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_ragged_rows_from_a_strided_source(fmt):
+    B, T, H, Hq, C = 5, 37, 2, 6, 64
+    g = gen(3)
+    qkv = randn(g, B, T, Hq + 2 * H, 128)
+    k, v = qkv[:, :, Hq:Hq + H], qkv[:, :, Hq + H:]
+    first, count = [0, 27, 60, 3, -2], [37, 37, 37, 0, 9]     # the last ones reach past both ends of the store
+    st = gkv.KVStore(fmt, batch=B, h_q=Hq, h_kv=H, capacity=C, device=DEV)
+    bufs = [t for t in (st.k, st.v, st.k_scale, st.v_scale) if t is not None]
+    for t in bufs:
+        t.view(torch.uint8).fill_(0x3A)
+    st.write(k, v, first=ints(first), count=ints(count))
+    written = np.zeros((B, C), bool)
+    for b in range(B):
+        for t in range(count[b]):
+            r = first[b] + t
+            if 0 <= r < C:
+                written[b, r] = True
+                for x, codes, scale in ((k, st.k, st.k_scale), (v, st.v, st.v_scale)):
+                    want, s = expect_codes(x[b, t], fmt)
+                    assert (raw(codes[b, :, r]).reshape(want.shape) == want).all(), (b, t)
+                    if scale is not None:
+                        assert (f64(scale[b, :, r]) == s).all()
+    for t in bufs:                                             # everything else is as it was
+        assert (raw(t).reshape(B, H, C, -1).transpose(0, 2, 1, 3)[~written] == 0x3A).all()
+    wide = torch.full((2, B, T + 3, H + 1, 128), 7.0, dtype=torch.bfloat16, device=DEV)
+    out = wide[:, :, :T, :H]
+    st.read(out[0], out[1], first=ints(first), count=ints(count))
+    vals = dequantised(st)
+    keep = np.ones((B, T + 3, H + 1), bool)
+    for b in range(B):
+        for t in range(count[b]):
+            if 0 <= first[b] + t < C:
+                keep[b, t, :H] = False
+                for i in range(2):
+                    assert (f64(out[i, b, t]) == ref.round_bf16(vals[i][b, :, first[b] + t])).all()
+    assert (f64(wide)[:, keep] == 7.0).all()
+
+
+@pytest.mark.parametrize("fmt", FORMATS[1:])
+def test_what_is_not_finite_reads_back_as_nan(fmt):
+    x = randn(gen(4), 1, 4, 1, 128)
+    x[0, 0, 0, 40] = float("inf")
+    x[0, 1, 0, 41] = float("nan")
+    x[0, 2, 0, 42] = float("-inf")
+    st = gkv.KVStore(fmt, batch=1, h_q=4, h_kv=1, capacity=4, device=DEV)
+    st.write(x, x)
+    out = torch.zeros((2, 1, 4, 1, 128), dtype=torch.bfloat16, device=DEV)
+    st.read(out[0], out[1])
+    bad = torch.isnan(out[0, 0, :, 0])
+    group = slice(32, 64) if fmt == "int4" else slice(0, 128)
+    assert bad[:3, group].all() and not bad[3].any() and int(bad.sum()) == 3 * (group.stop - group.start)
+    if fmt == "int4":
+        assert torch.equal(torch.isfinite(out[1, 0, :3, 0]).sum(-1).cpu(), torch.tensor([96, 96, 96]))
+
+
+def test_no_tokens_and_one_token():
+    st = gkv.KVStore("int8", batch=2, h_q=2, h_kv=2, capacity=3, device=DEV)
+    st.k.fill_(5)
+    st.write(torch.empty((2, 0, 2, 128), dtype=torch.bfloat16, device=DEV), torch.empty((2, 0, 2, 128), dtype=torch.bfloat16, device=DEV))
+    assert (st.k == 5).all()
+    x = randn(gen(5), 2, 1, 2, 128)
+    st.write(x, x, first=ints([2, 0]))
+    want, _ = expect_codes(x[:, 0], "int8")
+    assert (raw(st.k[0, :, 2]) == want[0]).all() and (raw(st.k[1, :, 0]) == want[1]).all() and (st.k[0, :, :2] == 5).all()
+
+
+# ---------------------------------------------------------------------------------------------- attention
+def filled(fmt, B, Hq, H, C, lens, seed, **kw):
+    """A store with lens[b] rows of every sequence written and all other bytes such that using them shows (NaN, or 0xFF)."""
+    g = gen(seed)
+    st = gkv.KVStore(fmt, batch=B, h_q=Hq, h_kv=H, capacity=C, device=DEV, **kw)
+    for t in (st.k, st.v, st.k_scale, st.v_scale):
+        if t is not None:
+            t.view(torch.uint8).fill_(0xFF)          # NaN as bf16 rows, as scales and as 8-bit floats
+    n = max(max(lens), 1)
+    k, v = randn(g, B, n, H, 128), randn(g, B, n, H, 128)
+    k *= torch.exp2(torch.randint(-3, 3, (B, n, H, 1), generator=g, device=DEV).float()).to(torch.bfloat16)
+    v *= torch.exp2(torch.randint(-12, 4, (B, n, H, 1), generator=g, device=DEV).float()).to(torch.bfloat16)
+    st.write(k, v, count=ints([max(x, 0) for x in lens]))
+    return st, g
+
+
+def check(st, lens, q, out, lse, appended=False, prefix=None, seqs=None, skip=()):
+    """out and lse against the reference on the rows the store holds now."""
+    vals = dequantised(st)
+    B, g = st.batch, st.h_q // st.h_kv
+    o, l = f64(out), f64(lse)
+    for b in (range(B) if seqs is None else seqs):
+        if b in skip:
+            continue
+        n = lens[b] + int(appended)
+        for h in range(st.h_kv):
+            kp = vp = None
+            if prefix is not None:
+                i = b // (B // prefix[0].shape[0])
+                kp, vp = f64(prefix[0][i, h, :prefix[2][i]]), f64(prefix[1][i, h, :prefix[2][i]])
+            hs = slice(h * g, (h + 1) * g)
+            want, wl, tol, ltol = ref.attend(f64(q[b, hs]), vals[0][b, h, :n], vals[1][b, h, :n], kp, vp,
+                                             ref.U_BF16 if st.fmt == "bf16" else ref.U_F16)
+            err = np.abs(o[b, hs] - want)
+            assert (err <= tol).all(), (b, h, n, float((err / tol).max()))
+            if np.isinf(wl).any():
+                assert (l[b, hs] == wl).all()
+            else:
+                assert (np.abs(l[b, hs] - wl) <= ltol).all(), (b, h, n, float((np.abs(l[b, hs] - wl) / ltol).max()))
+
+
+def attn_case(fmt, B, Hq, H, C, lens, seed, append, max_len=0, prefix=None, n_prefix=0, max_prefix=0, seqs=None):
+    st, g = filled(fmt, B, Hq, H, C, lens, seed, n_prefix=n_prefix, max_prefix=max_prefix)
+    q = randn(g, B, Hq, 128) * 1.5
+    kn, vn = (randn(g, B, H, 128), randn(g, B, H, 128)) if append else (None, None)
+    out = torch.full((B, Hq, 128), 7.0, dtype=torch.bfloat16, device=DEV)
+    lse = torch.full((B, Hq), 7.0, device=DEV)
+    before = [raw(t).copy() for t in (st.k, st.v)]
+    pre = None if prefix is None else gkv.Prefix(*prefix)
+    st.attn(ints(lens), q, out, k_new=kn, v_new=vn, prefix=pre, lse=lse, max_len=max_len)
+    torch.cuda.synchronize()
+    after = [raw(t) for t in (st.k, st.v)]
+    for x, y, new in zip(before, after, (kn, vn)):
+        x, y = (t.reshape(B, H, C, -1) for t in (x, y))
+        if append:
+            want, _ = expect_codes(new, fmt)
+            for b in range(B):
+                if lens[b] >= 0:
+                    assert (y[b, :, lens[b]] == want[b]).all()
+                    x[b, :, lens[b]] = y[b, :, lens[b]]
+        assert (x == y).all()                         # nothing but the new rows was written
+    check(st, lens, q, out, lse, append, prefix, seqs, skip=[b for b in range(B) if lens[b] < 0])
+    for b in range(B):
+        if lens[b] < 0:
+            assert (out[b] == 7).all() and (lse[b] == 7).all()
+    return st
+
+
+@pytest.mark.parametrize("append", [False, True])
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_attention_at_every_small_length(fmt, append):
+    lens = list(range(0, 36)) + [47, 48, 49, 63, 64, 65, 127, 128, 129, 200, 255, 256, 257]
+    attn_case(fmt, len(lens), 14, 2, 260, lens, 11, append)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("h_q,h_kv", [(1, 1), (6, 3), (4, 1), (5, 1), (28, 4), (16, 2)])
+def test_attention_head_layouts(fmt, h_q, h_kv):
+    attn_case(fmt, 3, h_q, h_kv, 300, [299, 5, 130], 12, True)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("B,C,lens,max_len", [
+    (1, 640, [639], 639), (1, 2000, [1999], 0), (2, 5000, [4999, 17], 4999), (3, 777, [776, 0, 400], 100),    # a max_len that is too small
+    (2, 1024, [1024, 1000], 1024),
+])
+def test_attention_with_few_units_is_split(fmt, B, C, lens, max_len):
+    attn_case(fmt, B, 8, 2, C, lens, 13, append=max(lens) < C, max_len=max_len)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_attention_of_a_large_batch_with_sequences_left_out(fmt):
+    rng = np.random.RandomState(14)
+    B = 130
+    lens = rng.randint(0, 150, B)
+    lens[rng.choice(B, 30, replace=False)] = -1
+    attn_case(fmt, B, 16, 4, 151, [int(x) for x in lens], 14, True, seqs=range(0, B, 3))
+
+
+@pytest.mark.parametrize("append", [False, True])
+@pytest.mark.parametrize("batch", [2, 300])     # split and whole units
+def test_lengths_that_do_not_fit_give_nan_and_write_nothing(append, batch):
+    C = 40
+    lens = [10] * batch
+    lens[0] = C + 1
+    lens[1] = C if append else C + 7
+    st, g = filled("int8", batch, 8, 2, C, [10] * batch, 15)
+    q, kn = randn(g, batch, 8, 128), randn(g, batch, 2, 128)
+    out, lse = torch.zeros((batch, 8, 128), dtype=torch.bfloat16, device=DEV), torch.zeros((batch, 8), device=DEV)
+    before = raw(st.k)[0:2].copy()
+    st.attn(ints(lens), q, out, k_new=kn if append else None, v_new=kn if append else None, lse=lse)
+    assert torch.isnan(out[:2]).all() and torch.isnan(lse[:2]).all() and torch.isfinite(out[2:]).all()
+    assert (raw(st.k)[0:2] == before).all()
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_extreme_logits_and_scales(fmt):
+    """Logits of +-10^4 (all weight on one key, later and earlier), V rows from 2^-100 to 2^100, zero rows."""
+    B, H, n = 4, 1, 200
+    st = gkv.KVStore(fmt, batch=B, h_q=3, h_kv=H, capacity=n, device=DEV)
+    g = gen(16)
+    k, v, q = randn(g, B, n, H, 128), randn(g, B, n, H, 128), randn(g, B, 3, 128)
+    ramp = torch.linspace(-300, 300, n, device=DEV)
+    k[0] = (q[0, 0] * ramp[:, None]).to(torch.bfloat16).view(n, 1, 128)
+    k[1] = (q[1, 0] * ramp.flip(0)[:, None]).to(torch.bfloat16).view(n, 1, 128)
+    v[2] = (v[2].float() * torch.exp2(torch.linspace(-100, 100, n, device=DEV))[:, None, None]).to(torch.bfloat16)
+    v[3, ::2] = 0
+    k[3, 1::3] = 0
+    st.write(k, v)
+    out, lse = torch.empty((B, 3, 128), dtype=torch.bfloat16, device=DEV), torch.empty((B, 3), device=DEV)
+    st.attn(ints([n] * B), q, out, lse=lse)
+    check(st, [n] * B, q, out, lse)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_nan_rows_show_in_the_output(fmt):
+    st, g = filled(fmt, 3, 4, 1, 64, [50, 50, 50], 17)
+    x = randn(g, 3, 1, 1, 128)
+    y = x.clone()
+    y[1] = float("nan")
+    st.write(y, x, first=ints([20] * 3))              # K of sequence 1
+    z = x.clone()
+    z[2, :, :, 100] = float("inf")
+    st.write(x, z, first=ints([20] * 3), count=ints([0, 0, 1]))
+    out, lse = torch.empty((3, 4, 128), dtype=torch.bfloat16, device=DEV), torch.empty((3, 4), device=DEV)
+    st.attn(ints([50] * 3), randn(g, 3, 4, 128), out, lse=lse)
+    assert torch.isfinite(out[0]).all() and torch.isnan(out[1]).all() and torch.isnan(lse[1]).all() and torch.isfinite(lse[2]).all()
+    bad = ~torch.isfinite(out[2])
+    group = slice(96, 128) if fmt == "int4" else slice(100, 101) if fmt == "bf16" else slice(0, 128)
+    assert bad[:, group].all() and int(bad.sum()) == 4 * (group.stop - group.start)
+
+
+def test_rows_beyond_4_gb():
+    C = 1 << 23                                       # 3 heads x 2^23 rows x 256 bytes: 6 GB of K
+    st = gkv.KVStore("bf16", batch=1, h_q=3, h_kv=3, capacity=C, device=DEV)
+    g = gen(18)
+    first = C - 40
+    k, v = randn(g, 1, 30, 3, 128), randn(g, 1, 30, 3, 128)
+    st.write(k, v, first=ints([first]))
+    back = torch.zeros((2, 1, 30, 3, 128), dtype=torch.bfloat16, device=DEV)
+    st.read(back[0], back[1], first=ints([first]))
+    assert torch.equal(back[0], k) and torch.equal(back[1], v)
+    assert torch.equal(st.k[0, 2, first:first + 30], k[0, :, 2])
+    del st
+    # attention: head 1 of a store whose second head starts beyond 2 GB and ends beyond 4
+    C = 1 << 24
+    st = gkv.KVStore("int8", batch=1, h_q=3, h_kv=3, capacity=C, device=DEV)
+    st.k_scale.fill_(2.0 ** -7); st.v_scale.fill_(2.0 ** -7)
+    st.k.zero_()
+    st.v.fill_(64)
+    st.v[0, 2, -1000:] = -64
+    q = randn(g, 1, 3, 128)
+    out, lse = torch.empty((1, 3, 128), dtype=torch.bfloat16, device=DEV), torch.empty((1, 3), device=DEV)
+    st.attn(ints([C]), q, out, lse=lse)
+    # all logits are 0: the mean of V, and log C; fp32 sums of 2^24 equal weights over many lanes are exact to 2^-12
+    assert torch.allclose(lse, torch.full_like(lse, float(np.log(C))), rtol=2.0 ** -12, atol=0)
+    assert torch.allclose(out.float(), torch.full((1, 3, 128), 0.5, device=DEV), rtol=2.0 ** -8 + 2000.0 / C, atol=0)
+
+
+# ---------------------------------------------------------------------------------------------- shared prefixes
+def prefix_rows(g, n, H, rows, lens):
+    k, v = randn(g, n, H, rows, 128), randn(g, n, H, rows, 128)
+    for i, m in enumerate(lens):                      # what lies behind a prefix must not matter
+        k[i, :, m:] = float("nan")
+        v[i, :, m:] = float("inf")
+    return k, v, lens
+
+
+@pytest.mark.parametrize("m", [0, 1, 2, 63, 127, 128, 129, 255, 256, 257, 400, 1000])
+def test_prefix_lengths(m):
+    g = gen(100 + m)
+    attn_case("e4m3", 3, 14, 2, 40, [39, 0, 17], 21, False, prefix=prefix_rows(g, 1, 2, max(m, 1) + 3, [m]), n_prefix=1, max_prefix=m + 3)
+
+
+@pytest.mark.parametrize("B,h_q,h_kv", [(1, 1, 1), (1, 8, 1), (15, 8, 1), (16, 8, 1), (17, 8, 1), (18, 7, 1), (19, 14, 2), (32, 16, 2),
+                                        (33, 8, 1), (36, 7, 1), (37, 7, 1), (64, 8, 1), (130, 4, 1), (300, 1, 1)])
+def test_prefix_row_blocks(B, h_q, h_kv):
+    """Row counts around one tile (128), one block (256) and several blocks."""
+    g = gen(200 + B)
+    lens = [int(x) for x in np.random.RandomState(B).randint(0, 30, B)]
+    attn_case("bf16", B, h_q, h_kv, 31, lens, 22, True, prefix=prefix_rows(g, 1, h_kv, 300, [291]), n_prefix=1, max_prefix=300,
+              seqs=sorted({0, B // 3, B // 2, B - 1, 15 % B, 16 % B, 31 % B, 32 % B}))
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_several_prefixes_of_different_lengths(fmt):
+    g = gen(23)
+    lens = [int(x) for x in np.random.RandomState(23).randint(-1, 90, 4 * 9)]
+    attn_case(fmt, 36, 12, 3, 91, lens, 23, True, prefix=prefix_rows(g, 4, 3, 700, [700, 0, 129, 512]), n_prefix=4, max_prefix=700)
+
+
+def test_only_a_prefix_and_nothing_at_all():
+    g = gen(24)
+    attn_case("int4", 6, 4, 1, 16, [0] * 6, 24, False, prefix=prefix_rows(g, 2, 1, 200, [0, 200]), n_prefix=2, max_prefix=200)
+    attn_case("int8", 2, 4, 1, 16, [0, 0], 25, False, prefix=prefix_rows(g, 2, 1, 1, [0, 0]), n_prefix=2, max_prefix=1)
+
+
+def test_a_long_prefix_with_logits_that_keep_rising():
+    """Every key tile raises the running maximum (accumulators are rescaled each time), or none does."""
+    for two_tiles, sign in ((False, 1), (True, 1), (True, -1)):
+        B = 36 if two_tiles else 4
+        g = gen(26)
+        q = randn(g, B, 7, 128)
+        m = 1500
+        k, v = randn(g, 1, 1, m, 128), randn(g, 1, 1, m, 128)
+        u = q.float().mean((0, 1)) + 0.3
+        k += (sign * u[None, :] * torch.linspace(-60, 60, m, device=DEV)[:, None]).to(torch.bfloat16)
+        st, _ = filled("bf16", B, 7, 1, 20, [9] * B, 27, n_prefix=1, max_prefix=m)
+        out, lse = torch.empty((B, 7, 128), dtype=torch.bfloat16, device=DEV), torch.empty((B, 7), device=DEV)
+        st.attn(ints([9] * B), q, out, lse=lse, prefix=gkv.Prefix(k, v, [m]))
+        check(st, [9] * B, q, out, lse, prefix=(k, v, [m]), seqs=[0, 1, B - 1])
+
+
+def test_nan_in_a_prefix_and_in_one_query():
+    g = gen(28)
+    k, v, lens = prefix_rows(g, 1, 1, 300, [300])
+    st, _ = filled("e4m3", 5, 4, 1, 20, [9] * 5, 28, n_prefix=1, max_prefix=300)
+    q = randn(g, 5, 4, 128)
+    q[3, 2, 5] = float("nan")
+    out = torch.empty((5, 4, 128), dtype=torch.bfloat16, device=DEV)
+    st.attn(ints([9] * 5), q, out, prefix=gkv.Prefix(k, v, lens))
+    bad = torch.isnan(out).all(-1)
+    assert bad[3, 2] and int(bad.sum()) == 1 and int(torch.isnan(out).any(-1).sum()) == 1
+    v[0, 0, 77, 64] = float("nan")
+    st.attn(ints([9] * 5), q, out, prefix=gkv.Prefix(k, v, lens))
+    assert torch.isnan(out[:, :, 64]).all() and torch.isfinite(out[0, :, :64]).all()
+
+
+# ---------------------------------------------------------------------------------------------- as they are used
+@pytest.mark.parametrize("fmt", ["e4m3", "int4"])
+def test_prompt_write_then_decode_in_a_replayed_graph(fmt):
+    """A prompt is quantised into the store, then tokens are decoded by replaying one captured step whose lengths grow on the
+    device, on a stream of its own; the store is read back at the end."""
+    B, Hq, H, C, T, steps, m = 3, 8, 2, 96, 61, 30, 140
+    g = gen(31)
+    k, v, lens = prefix_rows(g, 1, H, m, [m])
+    prefix = gkv.Prefix(k, v, lens)
+    st = gkv.KVStore(fmt, batch=B, h_q=Hq, h_kv=H, capacity=C, device=DEV, n_prefix=1, max_prefix=m)
+    counts = [61, 40, 1]
+    kp, vp = randn(g, B, T, H, 128), randn(g, B, T, H, 128)
+    length = ints(counts)
+    q, kn, vn = randn(g, B, Hq, 128), randn(g, B, H, 128), randn(g, B, H, 128)
+    out, lse = torch.empty((B, Hq, 128), dtype=torch.bfloat16, device=DEV), torch.empty((B, Hq), device=DEV)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        st.write(kp, vp, count=length)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=s):
+            st.attn(length, q, out, k_new=kn, v_new=vn, prefix=prefix, lse=lse, max_len=C - 1)
+            length += 1
+        for t in range(steps):
+            q.copy_(randn(g, B, Hq, 128)); kn.copy_(randn(g, B, H, 128)); vn.copy_(randn(g, B, H, 128))
+            graph.replay()
+            if t % 7 == 0 or t == steps - 1:
+                s.synchronize()
+                check(st, [c + t for c in counts], q, out, lse, True, (k, v, lens))
+        n = [c + steps for c in counts]
+        back = torch.zeros((2, B, C, H, 128), dtype=torch.bfloat16, device=DEV)
+        st.read(back[0], back[1], count=length)
+    s.synchronize()
+    assert length.tolist() == n
+    for i, val in enumerate(dequantised(st)):
+        for b in range(B):
+            assert (f64(back[i, b, :n[b]]) == ref.round_bf16(val[b, :, :n[b]].transpose(1, 0, 2))).all()
+
+
+def test_results_repeat_bit_for_bit_and_do_not_depend_on_the_workspace():
+    g = gen(32)
+    k, v, lens = prefix_rows(g, 1, 2, 600, [555])
+    st, _ = filled("int8", 9, 14, 2, 700, [600 + i for i in range(9)], 33, n_prefix=1, max_prefix=600)
+    q = randn(g, 9, 14, 128)
+    length = ints([600 + i for i in range(9)])
+    got = []
+    for fill in (0, 0xFF, 0x7F):
+        st.workspace.fill_(fill)
+        out = torch.empty((9, 14, 128), dtype=torch.bfloat16, device=DEV)
+        st.attn(length, q, out, prefix=gkv.Prefix(k, v, lens))
+        got.append(out)
+    assert torch.equal(got[0], got[1]) and torch.equal(got[0], got[2])
+
+
+def test_context_with_a_prefix_decodes_and_evicts():
+    """gkv_decode_attn_prefix over a compressed cache: lengths advance, compressions are scored from window queries, and every
+    step's output is attention over prefix and cache as they stand."""
+    L, B, Hq, H, b, s, w = 2, 3, 8, 2, 48, 16, 16
+    cfg = gkv.make_config(n_layers=L, batch=B, h_q=Hq, h_kv=H, b=b, buffer=24, w=w, s=s, fuse_window_scores=False)
+    cache = gkv.GKVCache(cfg, DEV)
+    g = gen(41)
+    m = 333
+    kp, vp, lens = prefix_rows(g, 1, H, m, [m])
+    prefix, ws = gkv.Prefix(kp, vp, lens), cache.prefix_workspace(1, m)
+    qs = [[] for _ in range(L)]
+    n = 0
+    for t in range(b + 3 * s):
+        for layer in range(L):
+            q, kn, vn = randn(g, B, Hq, 128), randn(g, B, H, 128), randn(g, B, H, 128)
+            out = torch.empty((B, Hq, 128), dtype=torch.bfloat16, device=DEV)
+            cache.decode_attn_prefix(layer, q, kn, vn, prefix, out, ws)
+            qs[layer].append(q)
+            if t % 9 == 0 or t > b:
+                view = gkv.KVStore("bf16", batch=B, h_q=Hq, h_kv=H, capacity=cache.C, buffers=(cache.k[layer], cache.v[layer]))
+                lse = torch.full((B, Hq), 0.0, device=DEV)
+                again = torch.empty_like(out)
+                view2 = gkv.KVStore("bf16", batch=B, h_q=Hq, h_kv=H, capacity=cache.C, buffers=(cache.k[layer], cache.v[layer]),
+                                    n_prefix=1, max_prefix=m)
+                view2.attn(cache.len[0, layer], q, again, prefix=prefix, lse=lse)   # the row is in the cache now
+                check(view, [n + 1] * B, q, out, lse, False, (kp, vp, lens), seqs=[t % B])
+        n += 1
+        assert cache.state(0)[0] == n and cache.len[0].unique().tolist() == [n]
+        if (t + 1) % s == 0:
+            for layer in range(L):
+                cache.evict(layer, torch.stack(qs[layer][-w:], 2).contiguous())
+            n = min(n, b)
+            assert cache.state(L - 1)[0] == n and cache.len[0].unique().tolist() == [n]
+    cache.poll()
+    with pytest.raises(gkv.GKVError) as e:            # the ordinary calls still work on it, and a full cache is refused
+        for _ in range(40):
+            cache.decode_attn_prefix(0, q, kn, vn, prefix, out, ws)
+    assert e.value.status == gkv.GKV_ERR_CAPACITY and cache.state(0)[0] == cache.C
+    fused = gkv.GKVCache(gkv.make_config(n_layers=1, batch=B, h_q=Hq, h_kv=H, b=b, buffer=24, w=w, s=s), DEV)
+    with pytest.raises(gkv.GKVError) as e:
+        fused.decode_attn_prefix(0, q, kn, vn, prefix, out, fused.prefix_workspace(1, m))
+    assert e.value.status == gkv.GKV_ERR_STATE
