@@ -2,66 +2,99 @@
 //
 // Both directions only move rows: 256 bytes of bf16 on one side, 130 (8 bits) or 72 (4 bits) of codes and scales on the other,
 // against a few dozen instructions for every 8 elements, so the kernels are bound by HBM and what matters is that enough rows
-// are in flight: half a warp handles a row (16 lanes x 16 bytes), takes kRowsPerLane rows at once and loads all of them before
-// it works on the first.
+// are in flight and that they go in whole sectors. Half a warp takes kRun consecutive tokens of one head: all of their loads
+// start before the first is worked on, the codes are one contiguous stretch of the store, and so are the scales, which are
+// gathered in the lanes and go with one access (2 bytes at a time they cost a 32-byte sector each). Neighbouring half warps
+// have the neighbouring heads of the same tokens, which lie next to each other on the bf16 side.
 #include "gkv_store_codes.cuh"
 
 namespace gkv {
 
 constexpr int kCopyThreads = 256;
-constexpr int kRowsPerLane = 4;
-constexpr int kRowsPerBlock = kCopyThreads / 16 * kRowsPerLane;
+constexpr int kRun = 8;
 
-// Row j = t * h_kv + h of sequence blockIdx.y; blockIdx.z = K or V. Rows of consecutive j lie next to each other in a
-// contiguous source, and a block's rows of one head next to each other in the store.
+// Work item i of sequence blockIdx.y: head i % h_kv, tokens kRun * (i / h_kv) and on; blockIdx.z = K or V.
 template <int F, bool READ>
 __global__ void __launch_bounds__(kCopyThreads) gkv_store_copy_kernel(const StoreCopyLaunch p) {
     using Fm = StoreFormat<F>;
-    const int b = blockIdx.y, which = blockIdx.z;
-    const int l = threadIdx.x & 15, hw = threadIdx.x >> 4;
-    const int count = p.count ? min(max(p.count[b], 0), p.n_tokens) : p.n_tokens;
-    const int first = p.first ? p.first[b] : 0;
-    const int total = count * p.h_kv;
-    const int j0 = blockIdx.x * kRowsPerBlock + hw;
-    if (blockIdx.x * kRowsPerBlock >= total) return;
+    const int b = blockIdx.y;
+    const bool is_v = blockIdx.z != 0;
+    const int l = threadIdx.x & 15;
+    const int item = blockIdx.x * (kCopyThreads / 16) + (threadIdx.x >> 4);
+    const int h = item % p.h_kv, t0 = item / p.h_kv * kRun;
+    const int count = p.count ? min(p.count[b], p.n_tokens) : p.n_tokens;
+    const int64_t first = p.first ? p.first[b] : 0;
+    // tokens lo .. hi - 1 of the run have a row (none: lo >= hi); the whole warp stays for the shuffles
+    const int hi = (int)min((int64_t)min(count - t0, kRun), p.capacity - first - t0);
+    const int lo = (int)max((int64_t)0, min((int64_t)kRun, -(first + t0)));
+    const int64_t row0 = ((int64_t)b * p.h_kv + h) * p.capacity + first + t0;
+    uint8_t* data = (is_v ? p.data[1] : p.data[0]) + row0 * Fm::kRow;
+    __nv_bfloat16* scale = (is_v ? p.scale[1] : p.scale[0]) + row0 * Fm::kScales;
+    __nv_bfloat16* x = (is_v ? p.x[1] : p.x[0]) + (int64_t)b * p.seq_stride + (int64_t)t0 * p.token_stride + (int64_t)h * p.head_stride;
 
-    uint8_t* data = p.data[which];
-    __nv_bfloat16* scale = p.scale[which];
-    __nv_bfloat16* xs = p.x[which] + (int64_t)b * p.seq_stride;
-    __nv_bfloat16* x[kRowsPerLane];
-    int64_t row[kRowsPerLane];      // row of the store, or -1: nothing to do
-    uint4 v[kRowsPerLane];
-    StoreRaw<F> raw[kRowsPerLane];
+    // Scales are held and moved by lane 2i + j: in 4 bits those of groups 2j, 2j + 1 of token i, in 8 bits that of token i (the
+    // odd lane has a copy).
+    const int st = l >> 1;
+    const bool has_scale = Fm::kScales != 0 && st >= lo && st < min(hi, kRun) && (F == GKV_STORE_INT4 || (l & 1) == 0);
+    uint32_t* scale4 = reinterpret_cast<uint32_t*>(scale) + l;
+    uint16_t* scale2 = reinterpret_cast<uint16_t*>(scale) + st;
+    uint4 v[kRun];
 #pragma unroll
-    for (int i = 0; i < kRowsPerLane; ++i) {
-        const int j = j0 + i * (kCopyThreads / 16);
-        const int t = j / p.h_kv, h = j - t * p.h_kv;
-        const int64_t r = (int64_t)first + t;
-        row[i] = (j < total && r >= 0 && r < p.capacity) ? ((int64_t)b * p.h_kv + h) * p.capacity + r : -1;
-        x[i] = xs + (int64_t)t * p.token_stride + (int64_t)h * p.head_stride;
+    for (int i = 0; i < kRun; ++i) {
         v[i] = make_uint4(0u, 0u, 0u, 0u);
-        raw[i].c = v[i];
-        raw[i].s = 0u;
-        if (row[i] >= 0) {
-            if (READ) raw[i] = store_get_raw<F>(data + row[i] * Fm::kRow, scale + row[i] * Fm::kScales, l);
-            else v[i] = store_load_source<F>(x[i], l);
+        if (i >= lo && i < hi) {
+            if (READ) v[i] = store_get_codes<F>(data + (int64_t)i * Fm::kRow, l);
+            else v[i] = store_load_source<F>(x + (int64_t)i * p.token_stride, l);
         }
     }
+    if (READ) {
+        uint32_t sc = 0u;
+        if (has_scale) sc = F == GKV_STORE_INT4 ? *scale4 : *scale2;
 #pragma unroll
-    for (int i = 0; i < kRowsPerLane; ++i) {
-        if (READ) {
-            if (row[i] >= 0) store_put_target<F>(x[i], l, store_decode_raw<F>(raw[i]));
-        } else {
-            const int64_t r = max(row[i], (int64_t)0);
-            store_put_row<F>(data + r * Fm::kRow, scale + r * Fm::kScales, l, v[i], row[i] >= 0);
+        for (int i = 0; i < kRun; ++i) {
+            const uint32_t s = __shfl_sync(0xffffffffu, sc, 2 * i + (F == GKV_STORE_INT4 ? l & 1 : 0), 16);
+            if (i >= lo && i < hi) store_put_target<F>(x + (int64_t)i * p.token_stride, l, store_decode<F>(v[i], s));
+        }
+    } else {
+        float inv0 = 1.f, inv1 = 1.f;
+        if (Fm::kScales != 0) {
+            // Maxima of the 8 tokens, reduced and handed out at once: a lane gives away half of what it holds at every step
+            // (7 exchanges for 8 tokens instead of 3 or 4 for each), until it has the token of its scale.
+            uint32_t a[kRun];
+#pragma unroll
+            for (int i = 0; i < kRun; ++i) a[i] = store_lane_max<F>(v[i]);
+#pragma unroll
+            for (int o = 8, n = kRun / 2; o >= 2; o >>= 1, n >>= 1) {
+                const bool upper = (l & o) != 0;
+#pragma unroll
+                for (int i = 0; i < kRun / 2; ++i)
+                    if (i < n) {
+                        const uint32_t keep = upper ? a[i + n] : a[i], give = upper ? a[i] : a[i + n];
+                        a[i] = __vmaxu2(keep, __shfl_xor_sync(0xffffffffu, give, o));
+                    }
+            }
+            if (F != GKV_STORE_INT4) a[0] = __vmaxu2(a[0], __shfl_xor_sync(0xffffffffu, a[0], 1));
+            const uint32_t sc = store_scale<F>(a[0], &inv0, &inv1);
+            if (has_scale) {
+                if (F == GKV_STORE_INT4) *scale4 = sc;
+                else *scale2 = (uint16_t)sc;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kRun; ++i) {
+            const int from = 2 * i + (F == GKV_STORE_INT4 ? l & 1 : 0);
+            float f0 = 1.f, f1 = 1.f;
+            if (Fm::kScales != 0) f0 = f1 = __shfl_sync(0xffffffffu, inv0, from, 16);
+            if (F == GKV_STORE_INT4) f1 = __shfl_sync(0xffffffffu, inv1, from, 16);
+            if (i >= lo && i < hi) store_put_codes<F>(data + (int64_t)i * Fm::kRow, l, store_codes<F>(v[i], f0, f1));
         }
     }
 }
 
 template <bool READ>
 static cudaError_t launch_copy(const StoreCopyLaunch& p, cudaStream_t s) {
-    const int64_t rows = (int64_t)p.n_tokens * p.h_kv;
-    const dim3 grid((unsigned)((rows + kRowsPerBlock - 1) / kRowsPerBlock), (unsigned)p.batch, 2);
+    const int items = (p.n_tokens + kRun - 1) / kRun * p.h_kv;
+    const dim3 grid((unsigned)((items + kCopyThreads / 16 - 1) / (kCopyThreads / 16)), (unsigned)p.batch, 2);
     switch (p.format) {
         case GKV_STORE_BF16: gkv_store_copy_kernel<GKV_STORE_BF16, READ><<<grid, kCopyThreads, 0, s>>>(p); break;
         case GKV_STORE_E4M3: gkv_store_copy_kernel<GKV_STORE_E4M3, READ><<<grid, kCopyThreads, 0, s>>>(p); break;

@@ -301,7 +301,7 @@ __global__ void __launch_bounds__(kThreads, F == GKV_STORE_BF16 ? 3 : 3) gkv_sto
         const __nv_bfloat16* src = (lane < 16 ? p.k_new : p.v_new) + (size_t)unit * kHeadDim;
         const uint4 x = store_load_source<F>(src, l);
         store_put_row<F>((lane < 16 ? kb : vb) + (size_t)len * StoreFormat<F>::kRow,
-                         (lane < 16 ? ksb : vsb) + (size_t)len * StoreFormat<F>::kScales, l, x, true);
+                         (lane < 16 ? ksb : vsb) + (size_t)len * StoreFormat<F>::kScales, l, x);
         __threadfence_block();
         __syncwarp();
     }

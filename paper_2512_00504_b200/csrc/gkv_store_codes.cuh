@@ -52,28 +52,30 @@ __device__ __forceinline__ uint32_t bf16_absmax(uint32_t a, uint32_t b) {
     return max(x & 0xffffu, x >> 16);
 }
 
-// bf16 bits of the scale of a group whose largest magnitude has the bf16 bits `a`, and what elements are multiplied by.
-__device__ __forceinline__ uint16_t e4m3_scale(uint32_t a, float* inv) {
-    if (a >= 0x7f80u) { *inv = 0.f; return 0x7fc0u; }
+// bf16 bits of the scale of a group whose largest magnitude has the bf16 bits `a`, and what elements are multiplied by (0 where
+// the group is not finite: its codes do not matter, its scale is NaN).
+__device__ __forceinline__ uint32_t e4m3_scale(uint32_t a, float* inv) {
     // a = m 2^E, 1 <= m < 2, against 448 = 1.75 * 2^8: e = E - 8, one more above 1.75 (mantissa bits 1.1100000b = 0x60)
-    int e = (int)(a >> 7) - 127 - 8 + ((a & 0x7fu) > 0x60u ? 1 : 0);
-    e = max(e, -126);
-    *inv = __uint_as_float((uint32_t)(127 - e) << 23);        // exact: e is in -126 .. 120
-    return (uint16_t)((e + 127) << 7);
+    const int e = max((int)(a >> 7) - 127 - 8 + ((a & 0x7fu) > 0x60u ? 1 : 0), -126);
+    const bool fine = a < 0x7f80u;
+    *inv = fine ? __uint_as_float((uint32_t)(127 - e) << 23) : 0.f;        // exact: e is in -126 .. 120
+    return fine ? (uint32_t)(e + 127) << 7 : 0x7fc0u;
 }
-__device__ __forceinline__ uint16_t int_scale(uint32_t a, float levels, float* inv) {
-    if (a >= 0x7f80u) { *inv = 0.f; return 0x7fc0u; }
-    const float s = fmaxf(__bfloat162float(__float2bfloat16_rn(__fdiv_rn(__uint_as_float(a << 16), levels))), 0x1p-126f);
-    *inv = __frcp_rn(s);
-    return (uint16_t)(__float_as_uint(s) >> 16);
+// a / levels rounded to bf16, by a multiplication: with 8 significant bits in a and 3 or 7 in `levels` the quotient is at least
+// 2^-16 of itself away from where the rounding changes, and the product is within 2^-23.
+__device__ __forceinline__ uint32_t int_scale(uint32_t a, float one_over_levels, float* inv) {
+    const float s = fmaxf(__bfloat162float(__float2bfloat16_rn(__uint_as_float(a << 16) * one_over_levels)), 0x1p-126f);
+    const bool fine = a < 0x7f80u;
+    *inv = fine ? __frcp_rn(s) : 0.f;
+    return fine ? __float_as_uint(s) >> 16 : 0x7fc0u;
 }
-// x / s rounded to a whole number, ties to even, as exact arithmetic gives it. x has 8 significant bits and s has 8, so a
-// quotient below 128 that is not half-way between whole numbers is at least 2^-10 away from half-way, and x * (1 / s) is within
-// 2^-16 of the quotient: rounding it to a multiple of 2^-13 first (adding and taking off 1.5 * 2^10) puts the half-way cases
-// exactly on half-way and moves none of the others across.
-__device__ __forceinline__ float round_quotient(float x, float inv) {
-    const float y = __fadd_rn(__fadd_rn(__fmul_rn(x, inv), 1536.f), -1536.f);
-    return rintf(y);
+// x / s rounded to a whole number, ties to even, as exact arithmetic gives it, in the low bits of the result (two's complement,
+// plus `add`). x has 8 significant bits and s has 8, so a quotient below 128 that is not half-way between whole numbers is at
+// least 2^-10 away from half-way, and x * (1 / s) is within 2^-16 of the quotient. Adding 1.5 * 2^10 rounds it to a multiple of
+// 2^-13, which puts the half-way cases exactly on half-way and moves none of the others across; going on to 1.5 * 2^23 rounds
+// that to a whole number.
+__device__ __forceinline__ uint32_t round_quotient(float x, float inv, float add) {
+    return __float_as_uint(__fadd_rn(__fmaf_rn(x, inv, 1536.f), 12582912.f - 1536.f + add));
 }
 
 __device__ __forceinline__ uint32_t e4m3_pack4(float a, float b, float c, float d) {
@@ -88,100 +90,102 @@ __device__ __forceinline__ uint32_t e4m3x2_to_f16x2(uint16_t x) {
     return d;
 }
 
-template <int L>   // over the 16 lanes of a half warp (L = 16) or over those with the same lowest bit (L = 8)
-__device__ __forceinline__ uint32_t half_warp_max(uint32_t a) {
-#pragma unroll
-    for (int o = 8; o >= (L == 16 ? 1 : 2); o >>= 1) a = max(a, __shfl_xor_sync(0xffffffffu, a, o));
-    return a;
-}
-
-// Lane l of a half warp quantises its 8 elements of a row into `data` (the row's codes) and the row's scales. All 32 lanes
-// call it (both half warps, each with its own row); `write` = 0 computes without storing.
+// The largest magnitudes among a lane's 8 elements, two 16-bit numbers still to be reduced: in 4 bits those of groups 2p (low)
+// and 2p + 1 over the lanes of the same p, else two of the row over all lanes.
 template <int F>
-__device__ __forceinline__ void store_put_row(uint8_t* data, __nv_bfloat16* scale, int l, uint4 x, bool write) {
-    if (F == GKV_STORE_BF16) {
-        if (write) *reinterpret_cast<uint4*>(data + 16 * l) = x;
-        return;
-    }
-    float v[8] = {bf16_lo(x.x), bf16_hi(x.x), bf16_lo(x.y), bf16_hi(x.y), bf16_lo(x.z), bf16_hi(x.z), bf16_lo(x.w), bf16_hi(x.w)};
-    uint16_t* sc = reinterpret_cast<uint16_t*>(scale);
-    float inv;
+__device__ __forceinline__ uint32_t store_lane_max(uint4 x) {
+    const uint32_t m = 0x7fff7fffu;
+    const uint32_t a = __vmaxu2(x.x & m, x.y & m), b = __vmaxu2(x.z & m, x.w & m);
+    if (F == GKV_STORE_INT4)   // low: groups 2p of both halves, high: 2p + 1
+        return __vmaxu2(__byte_perm(a, b, 0x5410), __byte_perm(a, b, 0x7632));
+    return __vmaxu2(a, b);
+}
+// bf16 bits of the scale(s) for reduced maxima (both groups' in 4 bits), and the factors of the lane's first and last 4 elements.
+template <int F>
+__device__ __forceinline__ uint32_t store_scale(uint32_t a, float* inv0, float* inv1) {
     if (F == GKV_STORE_INT4) {
-        const uint32_t a0 = half_warp_max<8>(bf16_absmax(x.x, x.y)), a1 = half_warp_max<8>(bf16_absmax(x.z, x.w));
-        float inv1;
-        const uint16_t s0 = int_scale(a0, 7.f, &inv), s1 = int_scale(a1, 7.f, &inv1);
-        uint32_t c = 0;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float f = i < 4 ? inv : inv1;
-            const float q = f == 0.f ? 0.f : round_quotient(v[i], f);
-            c |= (uint32_t)((int)q + 8) << (4 * i);
-        }
-        if (write) {
-            *reinterpret_cast<uint32_t*>(data + 4 * l) = c;
-            if (l < 2) *reinterpret_cast<uint32_t*>(sc + 2 * l) = (uint32_t)s0 | ((uint32_t)s1 << 16);
-        }
-        return;
+        const uint32_t s0 = int_scale(a & 0xffffu, 1.f / 7.f, inv0), s1 = int_scale(a >> 16, 1.f / 7.f, inv1);
+        return s0 | (s1 << 16);
     }
-    const uint32_t a = half_warp_max<16>(max(bf16_absmax(x.x, x.y), bf16_absmax(x.z, x.w)));
-    const uint16_t s = F == GKV_STORE_E4M3 ? e4m3_scale(a, &inv) : int_scale(a, 127.f, &inv);
-    uint2 c;
-    if (F == GKV_STORE_E4M3) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = inv == 0.f ? 0.f : v[i] * inv;
-        c.x = e4m3_pack4(v[0], v[1], v[2], v[3]);
-        c.y = e4m3_pack4(v[4], v[5], v[6], v[7]);
+    a = max(a & 0xffffu, a >> 16);
+    const uint32_t s = F == GKV_STORE_E4M3 ? e4m3_scale(a, inv0) : int_scale(a, 1.f / 127.f, inv0);
+    *inv1 = *inv0;
+    return s;
+}
+// Codes of a lane's 8 elements (for bf16 the elements themselves, else in .x and, in 8 bits, .y).
+template <int F>
+__device__ __forceinline__ uint4 store_codes(uint4 x, float inv0, float inv1) {
+    if constexpr (F == GKV_STORE_BF16) return x;
+    const float v[8] = {bf16_lo(x.x), bf16_hi(x.x), bf16_lo(x.y), bf16_hi(x.y), bf16_lo(x.z), bf16_hi(x.z), bf16_lo(x.w), bf16_hi(x.w)};
+    uint4 c = make_uint4(0u, 0u, 0u, 0u);
+    if constexpr (F == GKV_STORE_E4M3) {
+        c.x = e4m3_pack4(v[0] * inv0, v[1] * inv0, v[2] * inv0, v[3] * inv0);
+        c.y = e4m3_pack4(v[4] * inv0, v[5] * inv0, v[6] * inv0, v[7] * inv0);
     } else {
         uint32_t b[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) b[i] = (uint32_t)(int)(inv == 0.f ? 0.f : round_quotient(v[i], inv));
+        for (int i = 0; i < 8; ++i) b[i] = round_quotient(v[i], i < 4 ? inv0 : inv1, F == GKV_STORE_INT4 ? 8.f : 0.f);
+        if constexpr (F == GKV_STORE_INT4) {   // the low 20 bits of the numbers are the codes alone
+#pragma unroll
+            for (int i = 0; i < 4; ++i) b[i] = b[2 * i] + (b[2 * i + 1] << 4);
+        } else {
+            c.y = __byte_perm(__byte_perm(b[4], b[5], 0x0040), __byte_perm(b[6], b[7], 0x0040), 0x5410);
+        }
         c.x = __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
-        c.y = __byte_perm(__byte_perm(b[4], b[5], 0x0040), __byte_perm(b[6], b[7], 0x0040), 0x5410);
     }
-    if (write) {
-        *reinterpret_cast<uint2*>(data + 8 * l) = c;
-        if (l == 0) sc[0] = s;
+    return c;
+}
+template <int F>
+__device__ __forceinline__ void store_put_codes(uint8_t* row, int l, uint4 c) {
+    if (F == GKV_STORE_BF16) *reinterpret_cast<uint4*>(row + 16 * l) = c;
+    else if (F == GKV_STORE_INT4) *reinterpret_cast<uint32_t*>(row + 4 * l) = c.x;
+    else *reinterpret_cast<uint2*>(row + 8 * l) = make_uint2(c.x, c.y);
+}
+// Quantise and store one row (the copy kernel does several at once). All 32 lanes, both half warps with a row of their own.
+template <int F>
+__device__ __forceinline__ void store_put_row(uint8_t* row, __nv_bfloat16* scale, int l, uint4 x) {
+    float inv0 = 1.f, inv1 = 1.f;
+    if (F != GKV_STORE_BF16) {
+        uint32_t a = store_lane_max<F>(x);
+#pragma unroll
+        for (int o = 8; o >= (F == GKV_STORE_INT4 ? 2 : 1); o >>= 1) a = __vmaxu2(a, __shfl_xor_sync(0xffffffffu, a, o));
+        const uint32_t s = store_scale<F>(a, &inv0, &inv1);
+        if (F == GKV_STORE_INT4) { if (l < 2) reinterpret_cast<uint32_t*>(scale)[l] = s; }
+        else if (l == 0) *reinterpret_cast<uint16_t*>(scale) = (uint16_t)s;
     }
+    store_put_codes<F>(row, l, store_codes<F>(x, inv0, inv1));
 }
 
-// The raw codes and scales lane l needs of a row, and the 8 bf16 elements they stand for.
-template <int F> struct StoreRaw { uint4 c; uint32_t s; };
 template <int F>
-__device__ __forceinline__ StoreRaw<F> store_get_raw(const uint8_t* data, const __nv_bfloat16* scale, int l) {
-    StoreRaw<F> r;
-    r.s = 0;
-    if (F == GKV_STORE_BF16) r.c = *reinterpret_cast<const uint4*>(data + 16 * l);
-    else if (F == GKV_STORE_INT4) {
-        r.c.x = *reinterpret_cast<const uint32_t*>(data + 4 * l);
-        r.s = *reinterpret_cast<const uint32_t*>(scale + 2 * (l & 1));
-    } else {
-        const uint2 c = *reinterpret_cast<const uint2*>(data + 8 * l);
-        r.c.x = c.x; r.c.y = c.y;
-        r.s = *reinterpret_cast<const uint16_t*>(scale);
-    }
-    return r;
+__device__ __forceinline__ uint4 store_get_codes(const uint8_t* row, int l) {
+    if (F == GKV_STORE_BF16) return *reinterpret_cast<const uint4*>(row + 16 * l);
+    uint4 c = make_uint4(0u, 0u, 0u, 0u);
+    if (F == GKV_STORE_INT4) c.x = *reinterpret_cast<const uint32_t*>(row + 4 * l);
+    else { const uint2 d = *reinterpret_cast<const uint2*>(row + 8 * l); c.x = d.x; c.y = d.y; }
+    return c;
 }
+// The 8 bf16 elements that a lane's codes and scale(s) stand for.
 template <int F>
-__device__ __forceinline__ uint4 store_decode_raw(const StoreRaw<F>& r) {
-    if (F == GKV_STORE_BF16) return r.c;
+__device__ __forceinline__ uint4 store_decode(uint4 c, uint32_t sc) {
+    if (F == GKV_STORE_BF16) return c;
     float v[8];
     if (F == GKV_STORE_INT4) {
-        const float s0 = bf16_lo(r.s), s1 = bf16_hi(r.s);
+        const float s0 = bf16_lo(sc), s1 = bf16_hi(sc);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = (float)((int)((r.c.x >> (4 * i)) & 15u) - 8) * (i < 4 ? s0 : s1);
+        for (int i = 0; i < 8; ++i) v[i] = (float)((int)((c.x >> (4 * i)) & 15u) - 8) * (i < 4 ? s0 : s1);
     } else {
-        const float s = bf16_lo(r.s);
+        const float s = bf16_lo(sc);
         if (F == GKV_STORE_E4M3) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const uint32_t w = i < 2 ? r.c.x : r.c.y;
+                const uint32_t w = i < 2 ? c.x : c.y;
                 const uint32_t h = e4m3x2_to_f16x2((uint16_t)(w >> (16 * (i & 1))));
                 const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h));
                 v[2 * i] = f.x * s; v[2 * i + 1] = f.y * s;
             }
         } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = (float)(int8_t)((i < 4 ? r.c.x : r.c.y) >> (8 * (i & 3))) * s;
+            for (int i = 0; i < 8; ++i) v[i] = (float)(int8_t)((i < 4 ? c.x : c.y) >> (8 * (i & 3))) * s;
         }
     }
     return make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
