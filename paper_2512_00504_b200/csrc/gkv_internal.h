@@ -129,9 +129,9 @@ struct ScoreLaunch {
 
 // ---- key/value stores and shared prefixes
 constexpr int kMaxPrefixes = 64;
-constexpr int kOwnRecFloats = 32 + kHeadDimHost * 8;            // partial result of one unit's split: M[8], L[8], Mv[8], pad, O[128][8]
+constexpr int kOwnRecFloats = 32 + kHeadDimHost * 8;            // partial result of one unit's split: M[8], L[8], Mv[8], pad, O[32][8][4]
 constexpr int kPrefixRows = 256;                                // query rows of a prefix work item
-constexpr int kPrefixRecFloats = kPrefixRows * (2 + kHeadDimHost);   // M[256], L[256], O[128][256]
+constexpr int kPrefixRecFloats = kPrefixRows * (2 + kHeadDimHost);   // M[256], L[256], O[32][256][4]
 
 struct StoreCopyLaunch {       // write / read
     uint8_t* data[2];          // the store's k, v
@@ -212,6 +212,8 @@ cudaError_t launch_store_write(const StoreCopyLaunch& p, cudaStream_t s);
 cudaError_t launch_store_read(const StoreCopyLaunch& p, cudaStream_t s);
 cudaError_t launch_store_attn(const StoreAttnLaunch& p, cudaStream_t s);                    // a unit's own rows
 cudaError_t launch_prefix_attn(const StoreAttnLaunch& p, const CUtensorMap& tm_k, const CUtensorMap& tm_v, cudaStream_t s);
+int store_attn_ctas_per_sm(int format);                                                      // of launch_store_attn
+bool store_needs_merge(const StoreAttnLaunch& p);                                           // partial results go through the workspace
 cudaError_t launch_store_merge(const StoreAttnLaunch& p, cudaStream_t s);
 void store_plan(StoreAttnLaunch* p, int max_len, int sm_count);                             // splits, row blocks, chunk, items
 gkv_status encode_map(CUtensorMap* map, void* base, uint64_t rows, uint32_t box_rows);      // [rows][128] bf16, 64-element boxes

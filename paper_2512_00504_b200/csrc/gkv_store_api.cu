@@ -13,6 +13,8 @@ constexpr int kMaxStoreCapacity = 1 << 24;
 constexpr int kMaxStoreBatch = 65535;      // a grid dimension
 constexpr int kTileKeysOwn = 16;           // keys of a tile of the attention over own rows
 constexpr int64_t kSplitUnits = 2048;      // pieces beyond one per unit are at most this many (sizes the workspace)
+constexpr int kMaxSplits = 128;            // pieces of a unit
+constexpr int kMaxRuns = 160;              // runs of a prefix
 constexpr int kPrefixSplitItems = 296;     // prefix items beyond one per row block are at most this many
 
 uint64_t align_up(uint64_t x) { return (x + 255) / 256 * 256; }
@@ -117,7 +119,7 @@ gkv_status run_attn(StoreAttnLaunch& p, const gkv_store* shape, const gkv_prefix
     }
     if (launch_store_attn(p, s) != cudaSuccess) { (void)cudaGetLastError(); return GKV_ERR_CUDA; }
     ++*launches;
-    if (p.splits > 1 || p.prefix_part || p.len_out) {
+    if (store_needs_merge(p)) {
         if (launch_store_merge(p, s) != cudaSuccess) { (void)cudaGetLastError(); return GKV_ERR_CUDA; }
         ++*launches;
     }
@@ -145,15 +147,18 @@ gkv_status copy_args(const gkv_store* store, const void* k, const void* v, int64
 
 namespace gkv {
 
-// Own rows: as many pieces per unit as give every SM its resident CTAs (3), but no piece below 4 tiles per warp's turn.
+// Own rows: as many pieces per unit as fill the places of resident CTAs, none below 8 tiles (two turns of the four warps). (With
+// more units than half the places units go whole: cutting 1024 units into thirds, to fill the last round of CTAs better, took 157
+// us as clusters and 105 us by way of the workspace where whole units take 110 us.)
 // Prefixes: runs of key tiles such that the items fill whole rounds of one CTA per SM.
 void store_plan(StoreAttnLaunch* p, int max_len, int sm_count) {
-    const int64_t units = (int64_t)p->batch * p->h_kv;
+    const int64_t units = (int64_t)p->batch * p->h_kv, places = (int64_t)store_attn_ctas_per_sm(p->format) * sm_count;
     const int n = max_len + (p->k_new ? 1 : 0);
     const int tiles = n > 0 ? (n + kTileKeysOwn - 1) / kTileKeysOwn : 1;
-    int64_t splits = units >= 3 * sm_count ? 1 : (3 * sm_count) / units;
+    int64_t splits = places / units;
     const int64_t most = (tiles + 7) / 8;
     if (splits > most) splits = most;
+    if (splits > kMaxSplits) splits = kMaxSplits;
     if (splits < 1) splits = 1;
     p->split_tiles = (int)((tiles + splits - 1) / splits);
     p->splits = (tiles + p->split_tiles - 1) / p->split_tiles;
@@ -166,7 +171,7 @@ void store_plan(StoreAttnLaunch* p, int max_len, int sm_count) {
     // the cheapest of the possible run lengths: rounds x (tiles of a run + a fixed cost of about 3 tiles per item)
     const int64_t base = prefix_items(*p, key_tiles);
     int64_t best_cost = -1;
-    for (int runs = 1; runs <= key_tiles; ++runs) {
+    for (int runs = 1; runs <= key_tiles && runs <= kMaxRuns; ++runs) {
         const int chunk = (key_tiles + runs - 1) / runs;
         const int64_t items = prefix_items(*p, chunk);
         if (runs > 1 && items > base + kPrefixSplitItems) break;

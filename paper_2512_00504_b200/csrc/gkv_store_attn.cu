@@ -11,12 +11,17 @@
 //
 // 8- and 4-bit codes become fp16 exactly (their scales stay outside the products), q becomes fp16 after division by a power
 // of two (an element is exact down to 2^-17 of its row's largest; below, the error is at most 2^-25 of the largest), weights
-// are rounded to fp16 (11 bits). The scale of a K row multiplies its logit. The scale s of a V row goes into the weight by way
-// of the exponent, w = exp2(z + log2 s - m'), with a running maximum m' of its own over z + log2 s: the weights handed to the
-// product then lie in fp16's range whatever the scales are. Sums and accumulators are fp32.
+// are rounded to fp16 (11 bits). The scale of a K row multiplies its logit. The scale s of a V row goes into the weight:
+// w = p s c with p = exp2(z - m) as it enters the sum of the softmax, and c = exp2(m - v) with a running maximum v over
+// z + log2 s, so that the weights handed to the product lie in fp16's range whatever the scales are. (v is kept at least at
+// m - 112: c stays finite, and where all of V is below 2^-112 the outputs are numbers of that size.) Sums and accumulators are
+// fp32.
 //
-// The running maxima are allowed to lag: a tile raises them (which costs a reduction over the warp and a rescaling of the
-// accumulators) only when some logit is more than 2^kLag above them.
+// The running maxima are allowed to lag: a step raises them (which costs a reduction over the warp and a rescaling of the
+// accumulators) only when its weights have grown large.
+//
+// The pieces of a unit are joined by the CTAs of a cluster reading one another's shared memory (up to 8 pieces, no prefix), or
+// leave partial results in the workspace for the merge kernel.
 #include "gkv_store_codes.cuh"
 
 namespace gkv {
@@ -24,10 +29,16 @@ namespace gkv {
 constexpr int kWarps = 4;
 constexpr int kThreads = kWarps * 32;
 constexpr int kTile = 16;            // keys of a tile
-constexpr float kLag = 8.f;
+constexpr int kMaxCluster = 8;
+constexpr int kMergeHops = 4;
+// How far weights (relative to the running maximum, summed over a warp's lane and step) may go before the maximum is raised:
+// scaled rows by the range of fp16, bf16 ones by what keeps the smaller weights in range as well.
+template <int F> struct LagLimit { static constexpr float value = F == GKV_STORE_BF16 ? 0x1p60f : 256.f; };
 // state word of a unit's first partial result
 constexpr float kPieceOk = 0.f, kPieceNoFit = 1.f, kPieceLeftOut = 2.f;
 constexpr float kLift = 6.f;         // the weights of scaled rows are lifted by 2^6: at most 2^14, subnormal below 2^-20
+constexpr float kLiftFactor = 64.f;
+constexpr float kScaleSpan = 112.f;
 
 // ---- loads of codes. The store may have been written earlier in the same kernel (the new row): no read-only path.
 __device__ __forceinline__ uint4 ld16(const void* a) {
@@ -73,6 +84,11 @@ __device__ __forceinline__ uint32_t hfma2(uint32_t a, uint32_t b, uint32_t c) {
     asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
     return d;
 }
+__device__ __forceinline__ float fast_log2(float x) {   // absolute error 2^-22; only places a reference
+    float y;
+    asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
 // Four 8-bit codes -> two fp16 pairs (codes 0, 1 and 2, 3).
 template <int F>
 __device__ __forceinline__ void unpack8(uint32_t w, uint32_t& lo, uint32_t& hi) {
@@ -85,14 +101,18 @@ __device__ __forceinline__ void unpack8(uint32_t w, uint32_t& lo, uint32_t& hi) 
         hi = hsub2(__byte_perm(w, 0x64646464u, 0x4342), 0x64806480u);
     }
 }
-// Two 16-bit words of nibbles (one in each half of w) -> four fp16 pairs (nibble e of both words): 1024 + u - 1032 for the
-// nibbles in the low places, (1024 + 16 u) / 16 - 72 for those in the high ones, u = c + 8.
+// Two 16-bit words of nibbles (one in each half of w) -> four fp16 pairs (nibble e of both words), exactly. A byte u0 + 16 u1
+// (u = c + 8) under the exponent of 1024 is x = 1024 + u0 + 16 u1; without its low nibble y = 1024 + 16 u1, so c1 = y / 16 - 72
+// and c0 = (x - 16 c1) - 1160. The logic unit, which has half the rate of the floating-point pipe here, gets 4 instructions of
+// 10. (Leaving the offset 8 in and taking it off the sums would save more, but costs precision: as 1024 + u in the fp32 sums,
+// as subnormals u 2^-24 where the products are aligned.)
 __device__ __forceinline__ void unpack4(uint32_t w, uint32_t (&e)[4]) {
-    const uint32_t w8 = w >> 8;
-    e[0] = hsub2((w & 0x000f000fu) | 0x64006400u, 0x64086408u);
-    e[1] = hfma2((w & 0x00f000f0u) | 0x64006400u, 0x2c002c00u, 0xd480d480u);
-    e[2] = hsub2((w8 & 0x000f000fu) | 0x64006400u, 0x64086408u);
-    e[3] = hfma2((w8 & 0x00f000f0u) | 0x64006400u, 0x2c002c00u, 0xd480d480u);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const uint32_t x = __byte_perm(w, 0x64646464u, i == 0 ? 0x4240 : 0x4341);
+        e[2 * i + 1] = hfma2(x & 0xfff0fff0u, 0x2c002c00u, 0xd480d480u);
+        e[2 * i] = hsub2(hfma2(e[2 * i + 1], 0xcc00cc00u, x), 0x64886488u);
+    }
 }
 
 // Registers of one 16-key tile. K: this lane's pieces of rows r = lane / 4 and r + 8. V: its pieces of keys 2j, 2j + 1, 2j + 8,
@@ -108,43 +128,83 @@ template <> struct TileV<GKV_STORE_E4M3> { uint4 d[4]; uint32_t s[2]; };
 template <> struct TileV<GKV_STORE_INT8> { uint4 d[4]; uint32_t s[2]; };
 template <> struct TileV<GKV_STORE_INT4> { uint2 d[4]; uint2 s[2]; };
 
-// Rows from `end` on are not loaded: zeros stand for them, so that whatever lies there cannot reach the sums.
+// Where a lane's pieces of a tile begin: offsets from the unit's rows (below 2^32: a unit has at most 2^24 rows of 256 bytes);
+// everything of a tile and of the others of a step is at constant distances.
 template <int F>
-__device__ __forceinline__ void load_k(TileK<F>& t, const uint8_t* k, const __nv_bfloat16* sc, int key0, int end, int lane) {
+struct TilePtrs {
+    using Fm = StoreFormat<F>;
+    const uint8_t *kb, *vb;
+    const uint8_t *ksb, *vsb;
+    uint32_t k, v, s;
+    __device__ __forceinline__ void set(int key0, int lane) {
+        const int q = lane >> 2, j = lane & 3;
+        k = (uint32_t)(key0 + q) * Fm::kRow + j * 16;
+        v = (uint32_t)(key0 + 2 * j) * Fm::kRow + q * (F == GKV_STORE_INT4 ? 8 : 16);
+        s = (uint32_t)(key0 + q) * (2 * Fm::kScales);
+    }
+    __device__ __forceinline__ void advance(int keys) { k += keys * Fm::kRow; v += keys * Fm::kRow; s += keys * (2 * Fm::kScales); }
+};
+// Rows from `left` on (counted from the tile's first) are not loaded: zeros stand for them, so that whatever lies there cannot
+// reach the sums. WHOLE: all 16 exist.
+template <int F, bool WHOLE>
+__device__ __forceinline__ void load_k(TileK<F>& t, const TilePtrs<F>& p, int u, int left, int lane) {
     constexpr int kPieces = F == GKV_STORE_BF16 ? 4 : F == GKV_STORE_INT4 ? 1 : 2;
 #pragma unroll
     for (int hf = 0; hf < 2; ++hf) {
-        const int key = key0 + (lane >> 2) + 8 * hf;
-        const uint8_t* row = k + (size_t)key * StoreFormat<F>::kRow + (lane & 3) * 16;
+        const bool in = WHOLE || (lane >> 2) + 8 * hf < left;
+        const uint8_t* row = p.kb + p.k + (u * kTile + 8 * hf) * StoreFormat<F>::kRow;
+        const uint8_t* sc = p.ksb + p.s + (u * kTile + 8 * hf) * (2 * StoreFormat<F>::kScales);
 #pragma unroll
-        for (int c = 0; c < kPieces; ++c) t.d[hf][c] = key < end ? ld16(row + c * 64) : make_uint4(0u, 0u, 0u, 0u);
-        if constexpr (F == GKV_STORE_INT4) t.s[hf] = key < end ? ld8(sc + (size_t)key * 4) : make_uint2(0u, 0u);
-        else if constexpr (F != GKV_STORE_BF16) t.s[hf] = key < end ? ld2(sc + key) : 0u;
+        for (int c = 0; c < kPieces; ++c) t.d[hf][c] = in ? ld16(row + c * 64) : make_uint4(0u, 0u, 0u, 0u);
+        if constexpr (F == GKV_STORE_INT4) t.s[hf] = in ? ld8(sc) : make_uint2(0u, 0u);
+        else if constexpr (F != GKV_STORE_BF16) t.s[hf] = in ? ld2(sc) : 0u;
     }
 }
-template <int F>
-__device__ __forceinline__ void load_v(TileV<F>& t, const uint8_t* v, const __nv_bfloat16* sc, int key0, int end, int lane) {
-    const int q = lane >> 2, j = lane & 3;
+template <int F, bool WHOLE>
+__device__ __forceinline__ void load_v(TileV<F>& t, const TilePtrs<F>& p, int u, int left, int lane) {
+    const int j = lane & 3;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const int key = key0 + 2 * j + (i & 1) + 8 * (i >> 1);
-        const uint8_t* row = v + (size_t)key * StoreFormat<F>::kRow;
-        const bool in = key < end;
+        const int key = (i & 1) + 8 * (i >> 1);
+        const bool in = WHOLE || 2 * j + key < left;
+        const uint8_t* row = p.vb + p.v + (u * kTile + key) * StoreFormat<F>::kRow;
         if constexpr (F == GKV_STORE_BF16) {
-            t.d[i][0] = in ? ld16(row + q * 16) : make_uint4(0u, 0u, 0u, 0u);
-            t.d[i][1] = in ? ld16(row + 128 + q * 16) : make_uint4(0u, 0u, 0u, 0u);
+            t.d[i][0] = in ? ld16(row) : make_uint4(0u, 0u, 0u, 0u);
+            t.d[i][1] = in ? ld16(row + 128) : make_uint4(0u, 0u, 0u, 0u);
         } else if constexpr (F == GKV_STORE_INT4) {
-            t.d[i] = in ? ld8(row + q * 8) : make_uint2(0u, 0u);
+            t.d[i] = in ? ld8(row) : make_uint2(0u, 0u);
         } else {
-            t.d[i] = in ? ld16(row + q * 16) : make_uint4(0u, 0u, 0u, 0u);
+            t.d[i] = in ? ld16(row) : make_uint4(0u, 0u, 0u, 0u);
         }
     }
     // scales by key as the logits are held: rows r, r + 8
 #pragma unroll
     for (int hf = 0; hf < 2; ++hf) {
-        const int key = key0 + (lane >> 2) + 8 * hf;
-        if constexpr (F == GKV_STORE_INT4) t.s[hf] = key < end ? ld8(sc + (size_t)key * 4) : make_uint2(0u, 0u);
-        else if constexpr (F != GKV_STORE_BF16) t.s[hf] = key < end ? ld2(sc + key) : 0u;
+        const bool in = WHOLE || (lane >> 2) + 8 * hf < left;
+        const uint8_t* sc = p.vsb + p.s + (u * kTile + 8 * hf) * (2 * StoreFormat<F>::kScales);
+        if constexpr (F == GKV_STORE_INT4) t.s[hf] = in ? ld8(sc) : make_uint2(0u, 0u);
+        else if constexpr (F != GKV_STORE_BF16) t.s[hf] = in ? ld2(sc) : 0u;
+    }
+}
+// `left` keys of the step's U tiles exist (the same number for the whole warp; none or fewer: no loads).
+template <int F, int U>
+__device__ __forceinline__ void load_step_k(TileK<F> (&t)[U], const TilePtrs<F>& p, int left, int lane) {
+    if (left >= U * kTile) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) load_k<F, true>(t[u], p, u, 0, lane);
+    } else {
+#pragma unroll
+        for (int u = 0; u < U; ++u) load_k<F, false>(t[u], p, u, left - u * kTile, lane);
+    }
+}
+template <int F, int U>
+__device__ __forceinline__ void load_step_v(TileV<F> (&t)[U], const TilePtrs<F>& p, int left, int lane) {
+    if (left >= U * kTile) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) load_v<F, true>(t[u], p, u, 0, lane);
+    } else {
+#pragma unroll
+        for (int u = 0; u < U; ++u) load_v<F, false>(t[u], p, u, left - u * kTile, lane);
     }
 }
 
@@ -264,13 +324,30 @@ __device__ __forceinline__ void load_query(const __nv_bfloat16* row, int ks, int
 __device__ __forceinline__ uint32_t bf16x2_to_f16x2(uint32_t x, float f) { return pack_f16x2(bf16_lo(x) * f, bf16_hi(x) * f); }
 
 __device__ __forceinline__ float finite_ref(float m) { return m == -INFINITY ? 0.f : m; }
+// Output and log-sum-exp from sums relative to 2^v (values) and 2^m (weights); m = -infinity and no weight: nothing to attend to.
+__device__ __forceinline__ float final_value(float o, float m, float l, float v, bool fits) {
+    return !fits ? NAN : m == -INFINITY && l == 0.f ? 0.f : o * (fast_exp2(v - m) / l);
+}
+__device__ __forceinline__ float final_lse(float m, float l, bool fits) {
+    return !fits ? NAN : m == -INFINITY && l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+}
 
-// Own rows of the units. Grid: units x splits, split fastest. PART: write a partial result instead of the output.
-template <int F, int U, bool PART>
-__global__ void __launch_bounds__(kThreads, F == GKV_STORE_BF16 ? 3 : 3) gkv_store_attn_kernel(const StoreAttnLaunch p) {
+// Resident CTAs per SM. 8-bit rows: one 16-key tile per warp and step and 128 registers, 16 warps (the 32B batch of the
+// benchmark shapes: 97 us; two tiles, 168 registers and 12 warps: 110 us). bf16 rows need twice the registers for a tile, 4-bit
+// ones want two tiles in flight.
+__host__ __device__ constexpr int store_ctas(int format) { return format == GKV_STORE_BF16 || format == GKV_STORE_INT4 ? 3 : 4; }
+int store_attn_ctas_per_sm(int format) { return store_ctas(format); }
+
+// What becomes of a CTA's result: it is the unit's; it goes to the workspace; it is joined with those of the cluster's other CTAs.
+enum { kWhole = 0, kPart = 1, kCluster = 2 };
+
+// Own rows of the units. Grid: units x splits, split fastest.
+template <int F, int U, int MODE>
+__global__ void __launch_bounds__(kThreads, store_ctas(F)) gkv_store_attn_kernel(const StoreAttnLaunch p) {
     constexpr int NG = F == GKV_STORE_INT4 ? 4 : 1;
     constexpr bool kScaled = F != GKV_STORE_BF16;
     __shared__ float s_m[kWarps][8], s_l[kWarps][8], s_v[kWarps][8], s_wgt[kWarps][8], s_fin[3][8];
+    __shared__ float s_cl[kMaxCluster][8], s_norm[3][8];
     __shared__ __align__(16) float s_o[kWarps][kHeadDim * 8];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int unit = blockIdx.x / p.splits, split = blockIdx.x - unit * p.splits;
@@ -279,9 +356,13 @@ __global__ void __launch_bounds__(kThreads, F == GKV_STORE_BF16 ? 3 : 3) gkv_sto
     const bool append = p.k_new != nullptr;
     const bool fits = append ? len < p.capacity : len <= p.capacity;
     // The merge goes by this word and not by the length, which it may count up itself.
-    if (PART && split == 0 && threadIdx.x == 0)
+    if (MODE == kPart) grid_launch_dependents();
+    if (MODE == kPart && split == 0 && threadIdx.x == 0)
         p.own_part[(size_t)blockIdx.x * kOwnRecFloats + 24] = len < 0 ? kPieceLeftOut : fits ? kPieceOk : kPieceNoFit;
-    if (len < 0) return;
+    if (len < 0) {
+        if (MODE == kPart && p.prefix_part && blockIdx.x == 0) grid_wait_previous();   // see the end of the partial form
+        return;
+    }
     const int n = fits ? len + (append ? 1 : 0) : 0;
     const int tiles = (n + kTile - 1) / kTile;
     const int t_begin = min(split * p.split_tiles, tiles);
@@ -335,58 +416,84 @@ __global__ void __launch_bounds__(kThreads, F == GKV_STORE_BF16 ? 3 : 3) gkv_sto
 
     float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;       // running maxima (they may lag) and sums, heads h0, h0 + 1
     float v0 = -INFINITY, v1 = -INFINITY;                           // the same maxima of z + log2(scale of V)
+    float n0 = -INFINITY, n1 = -INFINITY;                           // m, or 0 where every logit was -infinity; at first: -infinity
+    float c0 = 1.f, c1 = 1.f;                                       // 2^(m - v + kLift), with finite m and v
     float acc[8][4];
 #pragma unroll
     for (int i = 0; i < 8; ++i) acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.f;
 
     TileK<F> tk[U];
     TileV<F> tv[U];
-    int step = warp;
-    int key0 = (t_begin + step * U) * kTile;
+    constexpr int kStepKeys = U * kTile;
     const int end = min(t_end * kTile, n);
-#pragma unroll
-    for (int u = 0; u < U; ++u) load_k<F>(tk[u], kb, ksb, key0 + u * kTile, step < steps ? end : 0, lane);
-#pragma unroll
-    for (int u = 0; u < U; ++u) load_v<F>(tv[u], vb, vsb, key0 + u * kTile, step < steps ? end : 0, lane);
-    for (; step < steps; step += kWarps) {
-        const int next0 = key0 + kWarps * U * kTile;
-        const int next_end = step + kWarps < steps ? end : 0;
+    const int key0 = (t_begin + warp * U) * kTile;
+    int left = warp < steps ? end - key0 : 0;                       // keys from this step's first on
+    TilePtrs<F> at;
+    at.kb = kb; at.vb = vb;
+    at.ksb = reinterpret_cast<const uint8_t*>(ksb); at.vsb = reinterpret_cast<const uint8_t*>(vsb);
+    at.set(key0, lane);
+    load_step_k<F, U>(tk, at, left, lane);
+    load_step_v<F, U>(tv, at, left, lane);
+    while (left > 0) {
+        at.advance(kWarps * kStepKeys);
+        const int left_next = left - kWarps * kStepKeys;
         float z[U][4];
 #pragma unroll
         for (int u = 0; u < U; ++u) tile_logits<F>(tk[u], qf, f0, f1, z[u]);
+        load_step_k<F, U>(tk, at, left_next, lane);
+        if (left < kStepKeys) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) load_k<F>(tk[u], kb, ksb, next0 + u * kTile, next_end, lane);
-        // log2 of the V scales of this lane's two keys, and their largest (the groups of a 4-bit row)
-        float lv[U][2][NG], lmax[U][2];
-        bool raise = false;
+            for (int u = 0; u < U; ++u)
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
+                for (int hf = 0; hf < 2; ++hf)
+                    if (u * kTile + hq + 8 * hf >= left) z[u][2 * hf] = z[u][2 * hf + 1] = -INFINITY;
+        }
+        // V scales of this lane's two keys (0 behind the end), and the sum of a key's: the largest, up to a factor of 4
+        float sc[U][2][NG], top[U][2];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
 #pragma unroll
             for (int hf = 0; hf < 2; ++hf) {
-                lmax[u][hf] = 0.f;
                 if constexpr (F == GKV_STORE_INT4) {
                     const uint2 s = tv[u].s[hf];
-                    lv[u][hf][0] = __log2f(bf16_lo(s.x)); lv[u][hf][1] = __log2f(bf16_hi(s.x));
-                    lv[u][hf][2] = __log2f(bf16_lo(s.y)); lv[u][hf][3] = __log2f(bf16_hi(s.y));
-                    lmax[u][hf] = fmaxf(fmaxf(lv[u][hf][0], lv[u][hf][1]), fmaxf(lv[u][hf][2], lv[u][hf][3]));
+                    sc[u][hf][0] = bf16_lo(s.x); sc[u][hf][1] = bf16_hi(s.x);
+                    sc[u][hf][2] = bf16_lo(s.y); sc[u][hf][3] = bf16_hi(s.y);
+                    top[u][hf] = (sc[u][hf][0] + sc[u][hf][1]) + (sc[u][hf][2] + sc[u][hf][3]);
                 } else if constexpr (kScaled) {
-                    lmax[u][hf] = lv[u][hf][0] = __log2f(bf16_lo(tv[u].s[hf]));
+                    top[u][hf] = sc[u][hf][0] = bf16_lo(tv[u].s[hf]);
+                } else {
+                    sc[u][hf][0] = top[u][hf] = 1.f;
                 }
-                const int key = key0 + u * kTile + hq + 8 * hf;
-                if (key >= end) { z[u][2 * hf] = z[u][2 * hf + 1] = -INFINITY; if (kScaled) lmax[u][hf] = 0.f; }
-                raise |= z[u][2 * hf] > m0 + kLag || z[u][2 * hf + 1] > m1 + kLag;
-                if (kScaled) raise |= z[u][2 * hf] + lmax[u][hf] > v0 + kLag || z[u][2 * hf + 1] + lmax[u][hf] > v1 + kLag;
             }
-        }
-        if (__any_sync(0xffffffffu, raise)) {
-            float a0 = m0, a1 = m1, c0 = v0, c1 = v1;
+        float e[U][4];                  // exp2(z - m)
+        // A z that is far above m, or a z + log2(scale) far above v, shows in the results: they are sums of non-negative numbers
+        // (at most the limit then), infinite or NaN, also at the first step, where m is -infinity.
+        float total = 0.f;
+        auto weigh = [&]() {
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                e[u][0] = fast_exp2(z[u][0] - n0); e[u][1] = fast_exp2(z[u][1] - n1);
+                e[u][2] = fast_exp2(z[u][2] - n0); e[u][3] = fast_exp2(z[u][3] - n1);
+                total += (e[u][0] + e[u][2]) + (e[u][1] + e[u][3]);
+                if (kScaled)
+                    total += ((e[u][0] * c0 + e[u][1] * c1) * top[u][0] + (e[u][2] * c0 + e[u][3] * c1) * top[u][1]) * (1.f / kLiftFactor);
+            }
+        };
+        weigh();
+        const bool over = !(total <= LagLimit<F>::value);
+        if (__any_sync(0xffffffffu, over)) {
+            float a0 = m0, a1 = m1, b0 = v0, b1 = v1;
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 a0 = fmaxf(a0, fmaxf(z[u][0], z[u][2]));
                 a1 = fmaxf(a1, fmaxf(z[u][1], z[u][3]));
                 if (kScaled) {
-                    c0 = fmaxf(c0, fmaxf(z[u][0] + lmax[u][0], z[u][2] + lmax[u][1]));
-                    c1 = fmaxf(c1, fmaxf(z[u][1] + lmax[u][0], z[u][3] + lmax[u][1]));
+                    float t0 = sc[u][0][0], t1 = sc[u][1][0];     // fmaxf leaves out a NaN
+#pragma unroll
+                    for (int g = 1; g < NG; ++g) { t0 = fmaxf(t0, sc[u][0][g]); t1 = fmaxf(t1, sc[u][1][g]); }
+                    const float x0 = fast_log2(t0), x1 = fast_log2(t1);
+                    b0 = fmaxf(b0, fmaxf(z[u][0] + x0, z[u][2] + x1));
+                    b1 = fmaxf(b1, fmaxf(z[u][1] + x0, z[u][3] + x1));
                 }
             }
 #pragma unroll
@@ -394,45 +501,48 @@ __global__ void __launch_bounds__(kThreads, F == GKV_STORE_BF16 ? 3 : 3) gkv_sto
                 a0 = fmaxf(a0, __shfl_xor_sync(0xffffffffu, a0, o));
                 a1 = fmaxf(a1, __shfl_xor_sync(0xffffffffu, a1, o));
                 if (kScaled) {
-                    c0 = fmaxf(c0, __shfl_xor_sync(0xffffffffu, c0, o));
-                    c1 = fmaxf(c1, __shfl_xor_sync(0xffffffffu, c1, o));
+                    b0 = fmaxf(b0, __shfl_xor_sync(0xffffffffu, b0, o));
+                    b1 = fmaxf(b1, __shfl_xor_sync(0xffffffffu, b1, o));
                 }
             }
-            l0 *= fast_exp2(m0 - finite_ref(a0));
-            l1 *= fast_exp2(m1 - finite_ref(a1));
-            float r0, r1;
-            if (kScaled) { r0 = fast_exp2(v0 - finite_ref(c0)); r1 = fast_exp2(v1 - finite_ref(c1)); }
-            else { r0 = fast_exp2(m0 - finite_ref(a0)); r1 = fast_exp2(m1 - finite_ref(a1)); }
-            m0 = a0; m1 = a1; v0 = c0; v1 = c1;
+            float r0 = fast_exp2(m0 - finite_ref(a0)), r1 = fast_exp2(m1 - finite_ref(a1));
+            l0 *= r0;
+            l1 *= r1;
+            m0 = a0; m1 = a1;
+            n0 = finite_ref(m0); n1 = finite_ref(m1);
+            if (kScaled) {
+                b0 = fmaxf(b0, a0 - kScaleSpan);
+                b1 = fmaxf(b1, a1 - kScaleSpan);
+                r0 = fast_exp2(v0 - finite_ref(b0));
+                r1 = fast_exp2(v1 - finite_ref(b1));
+                v0 = b0; v1 = b1;
+                c0 = fast_exp2(n0 - finite_ref(v0) + kLift);
+                c1 = fast_exp2(n1 - finite_ref(v1) + kLift);
+            }
 #pragma unroll
             for (int i = 0; i < 8; ++i) { acc[i][0] *= r0; acc[i][1] *= r1; acc[i][2] *= r0; acc[i][3] *= r1; }
+            weigh();
         }
-        const float n0 = finite_ref(m0), n1 = finite_ref(m1);
-        const float w0 = finite_ref(v0) - kLift, w1 = finite_ref(v1) - kLift;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const float p0 = fast_exp2(z[u][0] - n0), p1 = fast_exp2(z[u][1] - n1);
-            const float p2 = fast_exp2(z[u][2] - n0), p3 = fast_exp2(z[u][3] - n1);
-            l0 += p0 + p2;
-            l1 += p1 + p3;
+            l0 += e[u][0] + e[u][2];
+            l1 += e[u][1] + e[u][3];
             uint32_t b[NG][2];
             if constexpr (!kScaled) {
-                b[0][0] = movmatrix_trans(pack_weights<F>(p0, p1));
-                b[0][1] = movmatrix_trans(pack_weights<F>(p2, p3));
+                b[0][0] = movmatrix_trans(pack_weights<F>(e[u][0], e[u][1]));
+                b[0][1] = movmatrix_trans(pack_weights<F>(e[u][2], e[u][3]));
             } else {
-                const bool in0 = key0 + u * kTile + hq < end, in1 = key0 + u * kTile + hq + 8 < end;
+                const float p0 = e[u][0] * c0, p1 = e[u][1] * c1, p2 = e[u][2] * c0, p3 = e[u][3] * c1;
 #pragma unroll
                 for (int g = 0; g < NG; ++g) {
-                    const float e0 = in0 ? lv[u][0][g] : 0.f, e1 = in1 ? lv[u][1][g] : 0.f;   // z = -inf there: no weight
-                    b[g][0] = movmatrix_trans(pack_weights<F>(fast_exp2(z[u][0] + e0 - w0), fast_exp2(z[u][1] + e0 - w1)));
-                    b[g][1] = movmatrix_trans(pack_weights<F>(fast_exp2(z[u][2] + e1 - w0), fast_exp2(z[u][3] + e1 - w1)));
+                    b[g][0] = movmatrix_trans(pack_weights<F>(p0 * sc[u][0][g], p1 * sc[u][0][g]));
+                    b[g][1] = movmatrix_trans(pack_weights<F>(p2 * sc[u][1][g], p3 * sc[u][1][g]));
                 }
             }
             tile_values<F, NG>(tv[u], b, acc);
         }
-#pragma unroll
-        for (int u = 0; u < U; ++u) load_v<F>(tv[u], vb, vsb, next0 + u * kTile, next_end, lane);
-        key0 = next0;
+        load_step_v<F, U>(tv, at, left_next, lane);
+        left = left_next;
     }
 
     // ---- the warps' results: statistics, then the accumulators weighted to a common maximum
@@ -474,119 +584,244 @@ __global__ void __launch_bounds__(kThreads, F == GKV_STORE_BF16 ? 3 : 3) gkv_sto
         o[0] = fmaf(a.x, s_wgt[w][0], o[0]); o[1] = fmaf(a.y, s_wgt[w][1], o[1]); o[2] = fmaf(a.z, s_wgt[w][2], o[2]); o[3] = fmaf(a.w, s_wgt[w][3], o[3]);
         o[4] = fmaf(b.x, s_wgt[w][4], o[4]); o[5] = fmaf(b.y, s_wgt[w][5], o[5]); o[6] = fmaf(b.z, s_wgt[w][6], o[6]); o[7] = fmaf(b.w, s_wgt[w][7], o[7]);
     }
-    if (PART) {
+    if (MODE == kPart) {
         float* rec = p.own_part + (size_t)blockIdx.x * kOwnRecFloats;
         if (d < 8) { rec[d] = s_fin[0][d]; rec[8 + d] = s_fin[1][d]; rec[16 + d] = s_fin[2][d]; }
-        float4* ro = reinterpret_cast<float4*>(rec + 32 + d * 8);
-        ro[0] = make_float4(o[0], o[1], o[2], o[3]);
-        ro[1] = make_float4(o[4], o[5], o[6], o[7]);
-    } else {
-        __nv_bfloat16* orow = p.out + ((size_t)seq * p.h_q + (size_t)head * p.g) * kHeadDim + d;
+        // [dim / 4][head][4], by way of shared memory
+        __syncthreads();                              // the warps' accumulators have been read
+        float* mine = &s_o[0][0];
 #pragma unroll
-        for (int h = 0; h < 8; ++h) {
-            if (h >= p.g) break;
-            // (values) * 2^(v - m) / l; nothing to attend to: 0
-            const float f = fast_exp2(s_fin[2][h] - s_fin[0][h]) / s_fin[1][h];
-            const bool none = s_fin[0][h] == -INFINITY && s_fin[1][h] == 0.f;
-            const float x = !fits ? NAN : none ? 0.f : o[h] * f;
-            orow[(size_t)h * kHeadDim] = __float2bfloat16_rn(x);
-        }
-        if (p.lse && d < p.g) {
-            const bool none = s_fin[0][d] == -INFINITY && s_fin[1][d] == 0.f;
-            const float x = !fits ? NAN : none ? -INFINITY : (s_fin[0][d] + log2f(s_fin[1][d])) * 0.6931471805599453f;
-            p.lse[(size_t)seq * p.h_q + (size_t)head * p.g + d] = x;
-        }
+        for (int h = 0; h < 8; ++h) mine[((d >> 2) * 8 + h) * 4 + (d & 3)] = o[h];
+        __syncthreads();
+        float4* ro = reinterpret_cast<float4*>(rec + 32);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) ro[i * kThreads + d] = *reinterpret_cast<const float4*>(mine + (i * kThreads + d) * 4);
+        // The merge waits for this kernel only, so this kernel may not end before the prefixes' does.
+        if (p.prefix_part && blockIdx.x == 0) grid_wait_previous();
+        return;
     }
+    if (MODE == kCluster) {
+        // The CTAs leave their results [head][dim] in their own shared memory, and each then puts together a share of the
+        // outputs from all of them. Nobody leaves before everybody has read.
+        __syncthreads();                              // the warps' accumulators have been read
+        float* mine = &s_o[0][0];
+#pragma unroll
+        for (int h = 0; h < 8; ++h) mine[h * kHeadDim + d] = o[h];
+        cluster_sync_all();
+        if (d < 8) {
+            float m = -INFINITY, v = -INFINITY, l = 0.f;
+            float pm[kMaxCluster], pl[kMaxCluster], pv[kMaxCluster];
+#pragma unroll
+            for (int r = 0; r < kMaxCluster; ++r) {
+                const bool in = r < p.splits;
+                const uint32_t at = cluster_map_shared(smem_u32(&s_fin[0][d]), in ? r : 0);
+                pm[r] = in ? ld_cluster_f32(at) : -INFINITY;
+                pl[r] = in ? ld_cluster_f32(at + 32) : 0.f;
+                pv[r] = in ? ld_cluster_f32(at + 64) : -INFINITY;
+                m = fmaxf(m, pm[r]);
+                v = fmaxf(v, pv[r]);
+            }
+#pragma unroll
+            for (int r = 0; r < kMaxCluster; ++r) {
+                l += pl[r] * fast_exp2(pm[r] - finite_ref(m));
+                s_cl[r][d] = fast_exp2(pv[r] - finite_ref(v));
+            }
+            s_norm[0][d] = m; s_norm[1][d] = l; s_norm[2][d] = v;
+        }
+        __syncthreads();
+        for (int i = split * kThreads + d; i < p.g * kHeadDim; i += p.splits * kThreads) {
+            const int h = i / kHeadDim;
+            float x = 0.f;
+            for (int r = 0; r < p.splits; ++r)
+                x = fmaf(ld_cluster_f32(cluster_map_shared(smem_u32(&mine[i]), r)), s_cl[r][h], x);
+            p.out[((size_t)seq * p.h_q + (size_t)head * p.g) * kHeadDim + i] =
+                __float2bfloat16_rn(final_value(x, s_norm[0][h], s_norm[1][h], s_norm[2][h], fits));
+        }
+        if (p.lse && split == 0 && d < p.g)
+            p.lse[(size_t)seq * p.h_q + (size_t)head * p.g + d] = final_lse(s_norm[0][d], s_norm[1][d], fits);
+        cluster_sync_all();
+        return;
+    }
+    __nv_bfloat16* orow = p.out + ((size_t)seq * p.h_q + (size_t)head * p.g) * kHeadDim + d;
+#pragma unroll
+    for (int h = 0; h < 8; ++h)
+        if (h < p.g) orow[(size_t)h * kHeadDim] = __float2bfloat16_rn(final_value(o[h], s_fin[0][h], s_fin[1][h], s_fin[2][h], fits));
+    if (p.lse && d < p.g) p.lse[(size_t)seq * p.h_q + (size_t)head * p.g + d] = final_lse(s_fin[0][d], s_fin[1][d], fits);
 }
 
 // Joins the partial results of a unit: those of its own pieces and, with a prefix, those of the prefix items that hold its
-// query rows. One CTA per unit; thread t holds head t & 7 of dimensions t / 8 + 32 k, so that 8 lanes read 32 contiguous bytes
-// of a record.
-__global__ void __launch_bounds__(256) gkv_store_merge_kernel(const StoreAttnLaunch p) {
-    __shared__ __align__(16) __nv_bfloat16 s_out[8 * kHeadDim];
+// query rows. One CTA per unit; thread t holds head t & 7 of four dimensions over every (blockDim / 256)th of the parts, so that
+// 8 lanes read 128 contiguous bytes of a record. The statistics of all parts are loaded at once, the values of 8 parts at a
+// time: the kernel is a few trips to L2.
+__global__ void __launch_bounds__(1024) gkv_store_merge_kernel(const StoreAttnLaunch p) {
+    extern __shared__ float s_part[];                // [parts][8] factors
+    __shared__ __align__(16) float s_red[4 * 1024];
+    __shared__ float s_fin[3][8];
     const int unit = blockIdx.x, seq = unit / p.h_kv, head = unit - seq * p.h_kv;
-    const float* own = p.own_part + (size_t)unit * p.splits * kOwnRecFloats;
+    const int t = threadIdx.x, slices = blockDim.x >> 8, slice = t >> 8, h = t & 7, d4 = (t >> 3) & 31;
+    const int hc = min(h, p.g - 1), warps = blockDim.x >> 5;
+
+    // records: own ones, then those of the prefix items (two results each where the item's streams share the rows)
+    int items = 0;
+    int row0 = 0;
+    size_t step = 0;
+    const float *own = p.own_part + (size_t)unit * p.splits * kOwnRecFloats, *pre_rec = nullptr;
+    if (p.prefix_part) {
+        const int pre = seq / p.seqs_per_prefix, sl = seq - pre * p.seqs_per_prefix, blk = sl / p.seqs_per_block;
+        int base = head * p.n_blocks + blk;
+        for (int i = 0; i < pre; ++i) base += ((p.prefix_len[i] + 127) / 128 + p.chunk - 1) / p.chunk * p.h_kv * p.n_blocks;
+        items = ((p.prefix_len[pre] + 127) / 128 + p.chunk - 1) / p.chunk;
+        step = (size_t)p.h_kv * p.n_blocks * kPrefixRecFloats;
+        pre_rec = p.prefix_part + (size_t)base * kPrefixRecFloats;
+        row0 = (sl - blk * p.seqs_per_block) * p.g;
+    }
+    const int twice = p.two_tiles ? 0 : 1, parts = p.splits + (items << twice);
+    // statistics and values of prefix part j at the unit's first row
+    auto pre_stats = [&](int j) { return pre_rec + (size_t)(j >> twice) * step + row0 + (j & twice) * 128; };
+    auto pre_values = [&](int j) {
+        return reinterpret_cast<const float4*>(pre_rec + (size_t)(j >> twice) * step + 2 * kPrefixRows) + row0 + (j & twice) * 128;
+    };
+    grid_wait_previous();
     const float state = own[24];
     if (state == kPieceLeftOut) return;
     const bool fits = state == kPieceOk;
-    const int h = threadIdx.x & 7, d0 = threadIdx.x >> 3;
 
-    // prefix records of this unit
-    int items = 0, base = 0, step = 0, slot = 0;
-    const int sub = p.two_tiles ? 1 : 2;             // results per record that belong to the unit
-    if (p.prefix_part) {
-        const int pre = seq / p.seqs_per_prefix, sl = seq - pre * p.seqs_per_prefix;
-        for (int i = 0; i < pre; ++i) base += ((p.prefix_len[i] + 127) / 128 + p.chunk - 1) / p.chunk * p.h_kv * p.n_blocks;
-        items = ((p.prefix_len[pre] + 127) / 128 + p.chunk - 1) / p.chunk;
-        const int blk = sl / p.seqs_per_block;
-        base += head * p.n_blocks + blk;
-        step = p.h_kv * p.n_blocks;
-        slot = (sl - blk * p.seqs_per_block) * p.g + min(h, p.g - 1);
-    }
-    float m = -INFINITY, v = -INFINITY;
-    for (int i = 0; i < p.splits; ++i) {
-        m = fmaxf(m, own[(size_t)i * kOwnRecFloats + h]);
-        v = fmaxf(v, own[(size_t)i * kOwnRecFloats + 16 + h]);
-    }
-    for (int i = 0; i < items * sub; ++i) {
-        const float* rec = p.prefix_part + (size_t)(base + (i / sub) * step) * kPrefixRecFloats;
-        const float x = rec[slot + (i % sub) * 128];
-        m = fmaxf(m, x);
-        v = fmaxf(v, x);
-    }
-    const float mr = finite_ref(m), vr = finite_ref(v);
-    float l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int i = 0; i < p.splits; ++i) {
-        const float* rec = own + (size_t)i * kOwnRecFloats;
-        l += rec[8 + h] * fast_exp2(rec[h] - mr);
-        const float w = fast_exp2(rec[16 + h] - vr);
+    // ---- statistics: factors of all parts. Thread t has head t & 7 of parts t / 8, t / 8 + blockDim / 8, ...
+    const int hops = (parts * 8 + (int)blockDim.x - 1) / (int)blockDim.x;
+    float m = -INFINITY, v = -INFINITY, l = 0.f, x[kMergeHops], y[kMergeHops], z[kMergeHops];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) o[k] = fmaf(rec[32 + (d0 + 32 * k) * 8 + h], w, o[k]);
+    for (int k = 0; k < kMergeHops; ++k) {
+        x[k] = y[k] = -INFINITY;
+        z[k] = 0.f;
+        const int part = (t + k * (int)blockDim.x) >> 3;
+        if (k < hops && part < parts) {
+            if (part < p.splits) {
+                const float* r = own + (size_t)part * kOwnRecFloats + hc;
+                x[k] = r[0]; z[k] = r[8]; y[k] = r[16];
+            } else {
+                const float* r = pre_stats(part - p.splits) + hc;
+                x[k] = y[k] = r[0]; z[k] = r[kPrefixRows];
+            }
+        }
+        m = fmaxf(m, x[k]);
+        v = fmaxf(v, y[k]);
     }
-    for (int i = 0; i < items * sub; ++i) {
-        const float* rec = p.prefix_part + (size_t)(base + (i / sub) * step) * kPrefixRecFloats;
-        const int sl = slot + (i % sub) * 128;
-        const float x = rec[sl];
-        if (x == -INFINITY) continue;   // no key: its values were not written
-        l += rec[kPrefixRows + sl] * fast_exp2(x - mr);
-        const float w = fast_exp2(x - vr);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) o[k] = fmaf(rec[2 * kPrefixRows + (d0 + 32 * k) * kPrefixRows + sl], w, o[k]);
-    }
-    const bool none = m == -INFINITY && l == 0.f;    // nothing to attend to
-    const float f = none ? 0.f : fast_exp2(v - m) / l;
-#pragma unroll
-    for (int k = 0; k < 4; ++k)
-        s_out[h * kHeadDim + d0 + 32 * k] = __float2bfloat16_rn(!fits ? NAN : none ? 0.f : o[k] * f);
+    for (int o = 8; o < 32; o <<= 1) { m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o)); v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o)); }
+    if ((t & 31) < 8) { s_red[(t >> 5) * 16 + h] = m; s_red[(t >> 5) * 16 + 8 + h] = v; }
     __syncthreads();
-    if (threadIdx.x < p.g * 16) {
-        uint4* orow = reinterpret_cast<uint4*>(p.out + ((size_t)seq * p.h_q + (size_t)head * p.g) * kHeadDim);
-        orow[threadIdx.x] = reinterpret_cast<const uint4*>(s_out)[threadIdx.x];
+    for (int i = 0; i < warps; ++i) { m = fmaxf(m, s_red[i * 16 + h]); v = fmaxf(v, s_red[i * 16 + 8 + h]); }
+    const float mr = finite_ref(m), vr = finite_ref(v);
+#pragma unroll
+    for (int k = 0; k < kMergeHops; ++k) {
+        const int i = t + k * (int)blockDim.x;
+        l += z[k] * fast_exp2(x[k] - mr);            // (a NaN sum comes with a maximum of -infinity)
+        if (k < hops && i < parts * 8) s_part[i] = x[k] == -INFINITY ? 0.f : fast_exp2(y[k] - vr);   // 0: no key, values may be missing
     }
-    if (p.lse && d0 == 0 && h < p.g)
-        p.lse[(size_t)seq * p.h_q + (size_t)head * p.g + h] = !fits ? NAN : none ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
-    if (p.len_out && head == 0 && threadIdx.x == 0 && fits) p.len_out[seq] += 1;
+#pragma unroll
+    for (int o = 8; o < 32; o <<= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+    if ((t & 31) < 8) s_red[1024 + (t >> 5) * 8 + h] = l;
+    __syncthreads();
+    if (t < 8) {
+        float sum = 0.f;
+        for (int i = 0; i < warps; ++i) sum += s_red[1024 + i * 8 + h];
+        s_fin[0][h] = m; s_fin[1][h] = sum; s_fin[2][h] = v;
+    }
+
+    // ---- values
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    auto add = [&](float w, const float4& a) {
+        if (w != 0.f) { o.x = fmaf(a.x, w, o.x); o.y = fmaf(a.y, w, o.y); o.z = fmaf(a.z, w, o.z); o.w = fmaf(a.w, w, o.w); }
+    };
+    const float4* ov = reinterpret_cast<const float4*>(own + 32) + d4 * 8 + h;
+#pragma unroll 4
+    for (int i = slice; i < p.splits; i += slices) {
+        const float4 a = ov[(size_t)i * (kOwnRecFloats / 4)];
+        add(s_part[i * 8 + h], a);
+    }
+    const int n_pre = items << twice;
+    for (int i0 = slice; i0 < n_pre; i0 += 8 * slices) {
+        float4 a[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) a[k] = pre_values(min(i0 + k * slices, n_pre - 1))[d4 * kPrefixRows + hc];
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            if (i0 + k * slices < n_pre) add(s_part[(p.splits + i0 + k * slices) * 8 + h], a[k]);
+    }
+    if (slices > 1) {
+        __syncthreads();
+        reinterpret_cast<float4*>(s_red)[t] = o;
+        __syncthreads();
+        if (slice == 0)
+            for (int i = 1; i < slices; ++i) {
+                const float4 a = reinterpret_cast<const float4*>(s_red)[i * 256 + t];
+                o.x += a.x; o.y += a.y; o.z += a.z; o.w += a.w;
+            }
+    } else {
+        __syncthreads();
+    }
+    if (slice == 0 && h < p.g) {
+        const float fm = s_fin[0][h], fl = s_fin[1][h], fv = s_fin[2][h];
+        *reinterpret_cast<uint2*>(p.out + ((size_t)seq * p.h_q + (size_t)head * p.g + h) * kHeadDim + 4 * d4) =
+            make_uint2(pack_bf16x2(final_value(o.x, fm, fl, fv, fits), final_value(o.y, fm, fl, fv, fits)),
+                       pack_bf16x2(final_value(o.z, fm, fl, fv, fits), final_value(o.w, fm, fl, fv, fits)));
+    }
+    if (t < p.g) {
+        if (p.lse) p.lse[(size_t)seq * p.h_q + (size_t)head * p.g + t] = final_lse(s_fin[0][t], s_fin[1][t], fits);
+        if (p.len_out && head == 0 && t == 0 && fits) p.len_out[seq] += 1;
+    }
 }
 
-template <int F, int U>
-static void launch_own(const StoreAttnLaunch& p, bool part, cudaStream_t s) {
-    const unsigned grid = (unsigned)(p.batch * p.h_kv * p.splits);
-    if (part) gkv_store_attn_kernel<F, U, true><<<grid, kThreads, 0, s>>>(p);
-    else gkv_store_attn_kernel<F, U, false><<<grid, kThreads, 0, s>>>(p);
-}
-cudaError_t launch_store_attn(const StoreAttnLaunch& p, cudaStream_t s) {
-    const bool part = p.splits > 1 || p.prefix_part != nullptr || p.len_out != nullptr;
-    switch (p.format) {
-        case GKV_STORE_BF16: launch_own<GKV_STORE_BF16, 1>(p, part, s); break;
-        case GKV_STORE_E4M3: launch_own<GKV_STORE_E4M3, 2>(p, part, s); break;
-        case GKV_STORE_INT8: launch_own<GKV_STORE_INT8, 2>(p, part, s); break;
-        default:             launch_own<GKV_STORE_INT4, 2>(p, part, s); break;
+// cluster > 1: clusters of that many CTAs; dependent: the kernel may start while the one before it drains.
+static cudaError_t launch_ex(void (*kernel)(StoreAttnLaunch), const StoreAttnLaunch& p, unsigned grid, unsigned threads, size_t smem, int cluster,
+                             bool dependent, cudaStream_t s) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[2];
+    int n = 0;
+    if (cluster > 1) {
+        attr[n].id = cudaLaunchAttributeClusterDimension;
+        attr[n].val.clusterDim.x = (unsigned)cluster;
+        attr[n].val.clusterDim.y = attr[n].val.clusterDim.z = 1;
+        ++n;
     }
+    if (dependent) {
+        attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[n].val.programmaticStreamSerializationAllowed = 1;
+        ++n;
+    }
+    cfg.attrs = attr;
+    cfg.numAttrs = (unsigned)n;
+    return cudaLaunchKernelEx(&cfg, kernel, p);
+}
+template <int F, int U>
+static cudaError_t launch_own(const StoreAttnLaunch& p, cudaStream_t s) {
+    const unsigned grid = (unsigned)(p.batch * p.h_kv * p.splits);
+    if (store_needs_merge(p)) return launch_ex(gkv_store_attn_kernel<F, U, kPart>, p, grid, kThreads, 0, 1, p.prefix_part != nullptr, s);
+    if (p.splits > 1) return launch_ex(gkv_store_attn_kernel<F, U, kCluster>, p, grid, kThreads, 0, p.splits, false, s);
+    gkv_store_attn_kernel<F, U, kWhole><<<grid, kThreads, 0, s>>>(p);
     return cudaGetLastError();
 }
+bool store_needs_merge(const StoreAttnLaunch& p) { return p.splits > kMaxCluster || p.prefix_part != nullptr || p.len_out != nullptr; }
+cudaError_t launch_store_attn(const StoreAttnLaunch& p, cudaStream_t s) {
+    switch (p.format) {
+        case GKV_STORE_BF16: return launch_own<GKV_STORE_BF16, 1>(p, s);
+        case GKV_STORE_E4M3: return launch_own<GKV_STORE_E4M3, 1>(p, s);
+        case GKV_STORE_INT8: return launch_own<GKV_STORE_INT8, 1>(p, s);
+        default:             return launch_own<GKV_STORE_INT4, 2>(p, s);
+    }
+}
+// 256 threads per 8 parts or so, up to 1024. (The plan bounds the parts of a unit: kMaxSplits + 2 kMaxRuns = 448, 8 numbers each are 3.5 per thread.)
 cudaError_t launch_store_merge(const StoreAttnLaunch& p, cudaStream_t s) {
-    gkv_store_merge_kernel<<<(unsigned)(p.batch * p.h_kv), 256, 0, s>>>(p);
-    return cudaGetLastError();
+    int longest = 0;
+    for (int i = 0; i < p.n_prefix; ++i) longest = p.prefix_len[i] > longest ? p.prefix_len[i] : longest;
+    const int items = p.prefix_part ? ((longest + 127) / 128 + p.chunk - 1) / p.chunk * (p.two_tiles ? 1 : 2) : 0;
+    const int parts = p.splits + items;
+    const int slices = parts <= 8 ? 1 : parts <= 16 ? 2 : 4;
+    return launch_ex(gkv_store_merge_kernel, p, (unsigned)(p.batch * p.h_kv), 256u * slices, (size_t)parts * 8 * sizeof(float), 1, true, s);
 }
 
 }  // namespace gkv
