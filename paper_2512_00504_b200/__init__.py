@@ -110,7 +110,27 @@ def build_library(force: bool = False, verbose: bool = False, check_bounds: bool
     return out
 
 
+def build_binding(force: bool = False) -> Path:
+    """Compile csrc/gkv_torch.cpp (the Python module through which KVStore makes its calls) against this torch."""
+    import sysconfig
+
+    import torch
+    src, out = _PKG / "csrc" / "gkv_torch.cpp", _PKG / "_gkv_torch.so"
+    if not force and out.exists() and all(out.stat().st_mtime >= d.stat().st_mtime for d in (src, _ROOT / "include" / "gkv.h")):
+        return out
+    t = Path(torch.__file__).resolve().parent
+    cuda = Path(os.environ.get("CUDA_HOME", "/usr/local/cuda"))
+    tmp = out.with_suffix(f".so.tmp{os.getpid()}")
+    subprocess.check_call(["g++", "-O2", "-std=c++17", "-shared", "-fPIC", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+                           "-I", str(_ROOT / "include"), "-I", str(t / "include"), "-I", str(t / "include/torch/csrc/api/include"),
+                           "-I", str(cuda / "include"), "-I", sysconfig.get_paths()["include"], "-o", str(tmp), str(src),
+                           "-L", str(t / "lib"), "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_python"])
+    os.replace(tmp, out)
+    return out
+
+
 _lib = None
+_binding = None
 
 
 def lib() -> ctypes.CDLL:
@@ -168,6 +188,25 @@ def lib() -> ctypes.CDLL:
             getattr(L, name).restype = ctypes.c_int
         _lib = L
     return _lib
+
+
+def _torch_binding():
+    """The module that takes torch tensors to the store calls, bound to the loaded library. Raises if it has not been built."""
+    global _binding
+    if _binding is None:
+        import importlib.util
+
+        import torch  # noqa: F401  (its libraries have to be loaded first)
+        path = _PKG / "_gkv_torch.so"
+        if not path.exists():
+            raise RuntimeError(f"{path} is missing: run __graft_entry__.build() first")
+        spec = importlib.util.spec_from_file_location("_gkv_torch", path)
+        module = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(module)
+        L = lib()
+        module.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (L.gkv_store_write, L.gkv_store_read, L.gkv_store_attn)))
+        _binding = module
+    return _binding
 
 
 def _check(status: int, what: str) -> None:
@@ -318,7 +357,7 @@ def gkv_destroy(ctx):
     lib().gkv_destroy(ctx)
 
 
-# The tensor arguments of the calls on a store are checked by the holders below; these only marshal.
+# The calls on a store that take tensors are made by KVStore (below), through csrc/gkv_torch.cpp.
 def gkv_store_query_sizes(store: gkv_store) -> gkv_store_sizes:
     out = gkv_store_sizes()
     _check(lib().gkv_store_query_sizes(ctypes.byref(store), ctypes.byref(out)), "gkv_store_query_sizes")
@@ -425,14 +464,6 @@ class GKVCache:
         gkv_poll_device_status(self.ctx)
 
 
-def _stream_of(device):
-    """The current stream of `device`, which has to be the current device: the library launches on that one."""
-    import torch
-    if torch.cuda.current_device() != device.index:
-        raise ValueError(f"the store is on {device}, the current device is cuda:{torch.cuda.current_device()}")
-    return torch.cuda.current_stream(device).cuda_stream
-
-
 def _tensor(t, what, dtype, shape, device):
     """Data pointer of a contiguous tensor of this type, shape and device."""
     if t.dtype != dtype or t.shape != shape or t.device != device or not t.is_contiguous():
@@ -456,6 +487,7 @@ class Prefix:
         self.k, self.v, self.h_kv = k, v, k.shape[1]
         self._len = (ctypes.c_int32 * len(lengths))(*lengths)
         self.desc = gkv_prefix(k.shape[0], k.shape[2], self._len, pk, pv)
+        self.at = ctypes.addressof(self.desc)
 
 
 class KVStore:
@@ -490,48 +522,32 @@ class KVStore:
         self.k, self.v = buffers[0], buffers[1]
         self.k_scale, self.v_scale = (buffers[2], buffers[3]) if scales else (None, None)
         self.workspace = torch.empty(gkv_store_attn_workspace(self.desc, n_prefix, max_prefix), dtype=torch.uint8, device=self.device)
-        self._desc = ctypes.byref(self.desc)
+        if self.device.type != "cuda":
+            raise ValueError(f"the buffers are on {self.device}")
+        self._call = _torch_binding()
+        self._at = (ctypes.addressof(self.desc), self.device.index)
         self._ws = (self.workspace.data_ptr(), self.workspace.numel())
-        self._q_shape, self._kv_shape = torch.Size((batch, h_q, 128)), torch.Size((batch, h_kv, 128))
-        self._lse_shape, self._len_shape = torch.Size((batch, h_q)), torch.Size((batch,))
-        self._bf16, self._f32, self._i32 = torch.bfloat16, torch.float32, torch.int32
-
-    def _copy_args(self, k, v, first, count):
-        """k, v [batch][tokens][kv heads][128] with any strides whose last one is 1; the same ones for both."""
-        for t, n in ((k, "k"), (v, "v")):
-            if t.dtype != self._bf16 or t.dim() != 4 or t.shape[0] != self.batch or t.shape[2] != self.h_kv or t.shape[3] != 128 or \
-                    t.shape != k.shape or t.device != self.device:
-                raise ValueError(f"{n}: a bf16 tensor [{self.batch}][tokens][{self.h_kv}][128] on {self.device} is needed, "
-                                 f"got {t.dtype} {tuple(t.shape)} on {t.device}")
-        strides = [tuple(0 if n == 1 else st for n, st in zip(t.shape, t.stride())) for t in (k, v)]   # of steps that are taken
-        if strides[0] != strides[1] or strides[0][3] != 1:
-            raise ValueError(f"k, v: strides {k.stride()}, {v.stride()}: the last one has to be 1, and the two have to agree")
-        p_first = None if first is None else _tensor(first, "first", self._i32, self._len_shape, self.device)
-        p_count = None if count is None else _tensor(count, "count", self._i32, self._len_shape, self.device)
-        ss, ts, hs, _ = strides[0]
-        return k.data_ptr(), v.data_ptr(), ss, ts, hs, p_first, p_count, k.shape[1], _stream_of(self.device)
 
     def write(self, k, v, first=None, count=None):
-        """Quantise tokens into rows first[i] .. first[i] + count[i] - 1 of every sequence i (first, count: int32 on the
-        device; None: 0 and all tokens)."""
-        _check(lib().gkv_store_write(self._desc, *self._copy_args(k, v, first, count)), "gkv_store_write")
+        """Quantise tokens into rows first[i] .. first[i] + count[i] - 1 of every sequence i. k, v: bf16 [batch][tokens][kv
+        heads][128] with any strides whose last one is 1, the same ones for both; first, count: int32 on the device (None: 0
+        and all tokens)."""
+        at, dev = self._at
+        _check(self._call.copy(False, at, dev, k, v, first, count), "gkv_store_write")
 
     def read(self, k, v, first=None, count=None):
         """Read the same rows back as bf16 into k and v; tokens from count[i] on are left as they were."""
-        _check(lib().gkv_store_read(self._desc, *self._copy_args(k, v, first, count)), "gkv_store_read")
+        at, dev = self._at
+        _check(self._call.copy(True, at, dev, k, v, first, count), "gkv_store_read")
 
     def attn(self, length, q, out, k_new=None, v_new=None, prefix=None, lse=None, max_len=0):
         """Decode attention over rows 0 .. length[i] - 1 (int32 on the device), the new token (appended at row length[i]) and
         the sequence's prefix. The caller counts length up. max_len: the longest length (0: the capacity)."""
-        dev = self.device
-        if prefix is not None and (prefix.k.device != dev or prefix.h_kv != self.h_kv):
-            raise ValueError(f"the prefix has {prefix.h_kv} KV heads on {prefix.k.device}, the store {self.h_kv} on {dev}")
+        at, dev = self._at
         ws, ws_bytes = self._ws
-        _check(lib().gkv_store_attn(
-            self._desc, _tensor(length, "length", self._i32, self._len_shape, dev), max_len,
-            _tensor(q, "q", self._bf16, self._q_shape, dev),
-            None if k_new is None else _tensor(k_new, "k_new", self._bf16, self._kv_shape, dev),
-            None if v_new is None else _tensor(v_new, "v_new", self._bf16, self._kv_shape, dev),
-            None if prefix is None else ctypes.byref(prefix.desc), _tensor(out, "out", self._bf16, self._q_shape, dev),
-            None if lse is None else _tensor(lse, "lse", self._f32, self._lse_shape, dev), ws, ws_bytes, _stream_of(dev)),
-            "gkv_store_attn")
+        pre = 0
+        if prefix is not None:
+            if prefix.k.device != self.device or prefix.h_kv != self.h_kv:
+                raise ValueError(f"the prefix has {prefix.h_kv} KV heads on {prefix.k.device}, the store {self.h_kv} on {self.device}")
+            pre = prefix.at
+        _check(self._call.attn(at, dev, length, max_len, q, k_new, v_new, pre, out, lse, ws, ws_bytes), "gkv_store_attn")

@@ -15,6 +15,7 @@ FORMATS = ["bf16", "e4m3", "int8", "int4"]
 @pytest.fixture(scope="module", autouse=True)
 def built():
     gkv.build_library()
+    gkv.build_binding()
 
 
 def gen(seed):

@@ -15,6 +15,7 @@ A = 1 << 20     # an aligned address that is never looked at
 @pytest.fixture(scope="module", autouse=True)
 def built():
     gkv.build_library()
+    gkv.build_binding()
 
 
 def store(**over):
