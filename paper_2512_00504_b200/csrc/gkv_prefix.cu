@@ -5,20 +5,28 @@
 // (running maximum, sum, unscaled output of every row) goes to the workspace and is joined with the other runs' and with the
 // sequences' own rows by the merge kernel.
 //
-// One CTA (one per SM: 226 KB of shared memory, all 512 TMEM columns) holds two streams, A and B, each with 128 query rows: with more than 128 rows in the item A and B have a row tile each and both see every key tile; with fewer they
-// have the same rows and take the even and the odd key tiles. Per stream and key tile
+// One CTA (one per SM: 226 KB of shared memory, all 512 TMEM columns) holds two streams, A and B, each with 128 query rows: with
+// more than 128 rows in the item A and B have a row tile each and both see every key tile; with fewer they have the same rows
+// and take the even and the odd key tiles. Per stream and key tile
 //     S = Q K^T          128 x 128 x 128, operands in shared memory, S in 128 TMEM columns
-//     softmax            eight warps: TMEM lane = query row, two threads per row with 64 keys each, whose maximum and sum are
-//                        loops in the thread; P as bf16 goes back over the first 64 of S's columns
+//     softmax            four warps, thread = TMEM lane = query row, so that the sum over the keys is a loop in one thread; P as
+//                        bf16 goes back over S columns that have been read, one half of the keys after the other
 //     O += P V           P is read from TMEM as the A operand, V from shared memory with the head dimension contiguous (as it
-//                        lies in memory: no transpose), O in 128 TMEM columns
-// While one stream is in its softmax the tensor cores work for the other. A stream's steps follow one another (S, softmax, P V,
-// the next S), so what counts is how long each takes: with one thread per row and 128 exponentials in a row the chain was 6200
-// cycles a tile. The running maximum is the first tile's and is raised
-// only when the weights of a tile sum up to more than 2^60: bf16 and fp32 have the range for it and the relative precision of
-// all sums is the same, so there is no pass for the maximum and no rescaling of O (a trip of 128 columns through registers)
-// but in the first tile and in extreme ones. K and V tiles come by TMA through a ring of five 32 KB slots in the order in which
-// the products want them.
+//                        lies in memory: no transpose), O in 128 TMEM columns; the first half of the keys while the softmax is
+//                        at the second
+// The steps of a stream follow one another (S, softmax, P V, the next S); while one stream is in its softmax the tensor cores
+// work for the other. One warp issues the products of both in turn, which keeps them out of step (with an issuer each they fall
+// into step, both in the softmax and then both waiting for products: 5300 cycles a tile of 256 rows).
+//
+// Weights are relative to the maximum of the row's first tile, and stay so: bf16 and fp32 have the range for weights of 2^60 and
+// the relative precision of all sums is the same. There is no pass for the maximum and no rescaling of O. If half a tile's
+// weights do sum up to more than 2^60 in some row, the item is done again, once to find the rows' maxima and once with them.
+//
+// K and V tiles come by TMA through a ring of three 32 KB slots in the order in which the products want them.
+//
+// The kernel is a chain of waits that leaves HBM and most issue slots idle, and the attention over the sequences' own rows, which
+// runs next to it, is bound by HBM: 80 registers a thread and 162 KB of shared memory leave room for two CTAs of that kernel on
+// the same SM.
 //
 // Bound: for 256 rows a key tile costs 64 KB of HBM traffic (1.5 us of an SM's share), 2048 cycles of the tensor core and 2048
 // cycles of the exponential unit: all three are level.
@@ -27,28 +35,36 @@
 
 namespace gkv {
 
-constexpr int kPxSoftmax = 512;              // warps 0-7: stream A, 8-15: stream B (warp / 4 & 1: keys 0-63 or 64-127 of a tile)
-constexpr int kPxThreads = kPxSoftmax + 64;  // warp 16: TMA, 17: MMA
+constexpr int kPxSoftmax = 256;              // warps 0-3: stream A, 4-7: stream B
+constexpr int kPxThreads = kPxSoftmax + 64;  // warp 8: TMA, 9: MMA
 constexpr int kPxTmaWarp = kPxSoftmax / 32, kPxMmaWarp = kPxTmaWarp + 1;
 constexpr int kPxKeys = 128;                 // keys of a tile
 constexpr int kPxHalf = 128 * 128;           // bytes of 128 rows x 64 elements
 constexpr int kPxSlotBytes = 2 * kPxHalf;    // one K or V tile, or one row tile of q
-constexpr int kPxSlots = 5;
-constexpr float kPxLimit = 0x1p60f;          // a row's weights of one tile may sum up to this before the maximum is raised
+constexpr int kPxSlots = 3;
+constexpr float kPxLimit = 0x1p60f;          // a row's weights of half a tile may sum up to this
 
 struct __align__(16) PrefixTail {
     uint64_t q_full;
     uint64_t full[kPxSlots], empty[kPxSlots];
-    uint64_t s_full[2], p_ready[2];
+    uint64_t s_full[2], p_ready[2][2];       // per stream (and half of the keys)
     uint64_t o_full;
-    float row[2][128];   // [stream][row]: what the two threads of a row tell each other (a maximum, at the end a sum)
     uint32_t tmem_base;
     int abort_flag;
+    int overflow;      // weights left their range: once more
     int issued;        // ring slots filled so far
 };
 constexpr size_t kPxSmem = 1024 + 2 * kPxSlotBytes + kPxSlots * kPxSlotBytes + sizeof(PrefixTail);
 static_assert(kPxSmem <= 227 * 1024, "shared memory of a CTA");
 
+// One lane of the warp, chosen by the hardware: the branch that it takes leaves the rest of the code uniform for the warp, which
+// keeps descriptors in uniform registers. (The same products issued under `lane == 0` took 1580 cycles for a P V and a Q K^T of
+// half a tile, more than the tensor cores need.)
+__device__ __forceinline__ bool elect_one() {
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+    return r != 0;
+}
 // A operand in tensor memory (lane = row, one 32-bit column = two bf16 of the inner index), B in shared memory.
 __device__ __forceinline__ void umma_bf16_ta(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
     asm volatile(
@@ -94,27 +110,15 @@ __device__ __forceinline__ void tmem_ld_wait(float (&r)[32]) {
           "+f"(r[27]), "+f"(r[28]), "+f"(r[29]), "+f"(r[30]), "+f"(r[31])
         :: "memory");
 }
-// The two warps that share 32 query rows: wait for each other; and whether a predicate holds anywhere among them.
-__device__ __forceinline__ void pair_sync(int id) {
-    __syncwarp();
-    asm volatile("bar.sync %0, 64;" ::"r"(id) : "memory");
-}
-__device__ __forceinline__ bool pair_any(int id, bool x) {
-    uint32_t r;
-    __syncwarp();
-    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %2, 0;\n\tbar.red.or.pred q, %1, 64, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
-                 : "=r"(r) : "r"(id), "r"((uint32_t)x) : "memory");
-    return r != 0;
-}
-// Keys from `valid` on (32 c is the block's first) do not exist.
-__device__ __forceinline__ void mask_block(float (&z)[32], int c, int valid) {
-    if (32 * c + 32 > valid) {
+// Keys from `valid` on (`key0` is the block's first) do not exist.
+__device__ __forceinline__ void mask_block(float (&z)[32], int key0, int valid) {
+    if (key0 + 32 > valid) {
 #pragma unroll
-        for (int k = 0; k < 32; ++k) if (32 * c + k >= valid) z[k] = -INFINITY;
+        for (int k = 0; k < 32; ++k) if (key0 + k >= valid) z[k] = -INFINITY;
     }
 }
 
-__global__ void __launch_bounds__(kPxThreads, 1)
+__global__ void __maxnreg__(80)
 gkv_prefix_attn_kernel(const StoreAttnLaunch p, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v) {
     grid_launch_dependents();   // the attention over own rows takes the SMs as they fall free
     extern __shared__ uint8_t smem_raw[];
@@ -122,7 +126,8 @@ gkv_prefix_attn_kernel(const StoreAttnLaunch p, const __grid_constant__ CUtensor
     uint8_t* q_smem = smem;                              // two row tiles
     uint8_t* ring = smem + 2 * kPxSlotBytes;
     PrefixTail* tail = reinterpret_cast<PrefixTail*>(ring + kPxSlots * kPxSlotBytes);
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    // (numbers that are the same for a warp by a shuffle, which lets the compiler keep what hangs on them in uniform registers)
+    const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
 
     // ---- the work item
     int item = blockIdx.x, pre = 0, runs = 0;
@@ -144,9 +149,11 @@ gkv_prefix_attn_kernel(const StoreAttnLaunch p, const __grid_constant__ CUtensor
     if (tid == 0) {
         mbar_init(smem_u32(&tail->q_full), kPxSoftmax);
         for (int s = 0; s < kPxSlots; ++s) { mbar_init(smem_u32(&tail->full[s]), 1); mbar_init(smem_u32(&tail->empty[s]), 1); }
-        for (int s = 0; s < 2; ++s) { mbar_init(smem_u32(&tail->s_full[s]), 1); mbar_init(smem_u32(&tail->p_ready[s]), kPxSoftmax / 2); }
+        for (int s = 0; s < 2; ++s) mbar_init(smem_u32(&tail->s_full[s]), 1);
+        for (int s = 0; s < 4; ++s) mbar_init(smem_u32(&tail->p_ready[s >> 1][s & 1]), kPxSoftmax / 2);
         mbar_init(smem_u32(&tail->o_full), 1);
         tail->abort_flag = 0;
+        tail->overflow = 0;
         tail->issued = 0;
         fence_mbar_init();
     }
@@ -157,227 +164,222 @@ gkv_prefix_attn_kernel(const StoreAttnLaunch p, const __grid_constant__ CUtensor
     }
     __syncthreads();
     tmem_fence_after_sync();
-    const uint32_t tmem = *(volatile uint32_t*)&tail->tmem_base;
+    const uint32_t tmem = __shfl_sync(0xffffffffu, *(volatile uint32_t*)&tail->tmem_base, 0);
     const int* abort_flag = &tail->abort_flag;
     // ring position of key tile t's V tile and K tile: K_0 [K_1] then V_t, K_(t + ahead) in turn, while there are such tiles
     auto v_pos = [&](int t) { return min(ahead, n_tiles) + t + min(t, max(n_tiles - ahead, 0)); };
     auto k_pos = [&](int t) { return t < ahead ? t : v_pos(t - ahead) + 1; };
     auto wait_full = [&](int pos) { return tc_wait(smem_u32(&tail->full[pos % kPxSlots]), (pos / kPxSlots) & 1, abort_flag); };
 
+    // A stream's key tiles: first(x), first(x) + stride, ...
+    const int stride = two ? 1 : 2;
+    auto first = [&](int x) { return two ? 0 : x; };
+    auto count = [&](int x) { return two ? n_tiles : (n_tiles - x + 1) / 2; };
     bool ok = true;
-    if (warp == kPxTmaWarp) {
-        // ------------------------------------------------------------------ TMA
-        if (lane == 0) {
-            prefetch_tensormap(&tm_k);
-            prefetch_tensormap(&tm_v);
-            const int row0 = (pre * p.h_kv + head) * p.prefix_rows;
-            const int total = 2 * n_tiles;
-            int kt = 0, vt = 0;
-            for (int pos = 0; pos < total && ok; ++pos) {
-                const bool is_k = kt < n_tiles && k_pos(kt) == pos;
-                const int t = is_k ? kt++ : vt++;
-                const int s = pos % kPxSlots;
-                if (pos >= kPxSlots) ok = tc_wait(smem_u32(&tail->empty[s]), (pos / kPxSlots - 1) & 1, abort_flag);
-                if (!ok) { tail->abort_flag = 1; break; }
-                const uint32_t bar = smem_u32(&tail->full[s]), dst = smem_u32(ring + s * kPxSlotBytes);
-                const CUtensorMap* m = is_k ? &tm_k : &tm_v;
-                const int y = row0 + (t0 + t) * kPxKeys;
-                mbar_arrive_expect_tx(bar, kPxSlotBytes);
-                tma_load_2d(dst, m, 0, y, bar);
-                tma_load_2d(dst + kPxHalf, m, 64, y, bar);
-                *(volatile int*)&tail->issued = pos + 1;
+    float m = -INFINITY, l = 0.f;                        // softmax: in log2 units
+    const int x = warp >> 2;                             // softmax: stream
+    const int row = tid & 127;                           // TMEM lane = query row of the stream's tile
+    const uint32_t t_lane = (uint32_t)((warp & 3) * 32) << 16;
+    const uint32_t s_addr = tmem + t_lane + 128 * x, o_addr = tmem + t_lane + 256 + 128 * x;
+
+    // One pass over the item, or three: weights relative to the first tile's maxima; the maxima; weights relative to them. (In
+    // the second pass the products run as in the others, on whatever is in P's place; the third starts O anew.)
+    int pass = 0;
+    for (;; ++pass) {
+        const int pos0 = pass * 2 * n_tiles;             // ring positions used so far
+        if (warp == kPxTmaWarp) {
+            // -------------------------------------------------------------- TMA
+            if (elect_one()) {
+                const int row0 = (pre * p.h_kv + head) * p.prefix_rows;
+                int kt = 0, vt = 0;
+                for (int pos = 0; pos < 2 * n_tiles && ok; ++pos) {
+                    const bool is_k = kt < n_tiles && k_pos(kt) == pos;
+                    const int t = is_k ? kt++ : vt++;
+                    const int at = pos0 + pos, s = at % kPxSlots;
+                    if (at >= kPxSlots) ok = tc_wait(smem_u32(&tail->empty[s]), (at / kPxSlots - 1) & 1, abort_flag);
+                    if (!ok) { tail->abort_flag = 1; break; }
+                    const uint32_t bar = smem_u32(&tail->full[s]), dst = smem_u32(ring + s * kPxSlotBytes);
+                    const CUtensorMap* mp = is_k ? &tm_k : &tm_v;
+                    const int y = row0 + (t0 + t) * kPxKeys;
+                    mbar_arrive_expect_tx(bar, kPxSlotBytes);
+                    tma_load_2d(dst, mp, 0, y, bar);
+                    tma_load_2d(dst + kPxHalf, mp, 64, y, bar);
+                    *(volatile int*)&tail->issued = at + 1;
+                }
             }
-        }
-    } else if (warp == kPxMmaWarp) {
-        // ------------------------------------------------------------------ MMA
-        if (lane == 0) {
+        } else if (warp == kPxMmaWarp) {
+            // -------------------------------------------------------------- MMA (the whole warp; one lane issues)
+            // What stands between two products costs the tensor cores time (they hold few products in advance): slots and
+            // parities are worked out once per tile.
             const uint32_t idesc_s = umma_idesc_bf16_m128(128);
-            const uint32_t idesc_o = idesc_s | (1u << 16);           // B's contiguous direction is its outer index
-            const uint32_t qa[2] = {umma_desc_lo(smem_u32(q_smem)), umma_desc_lo(smem_u32(q_smem + (two ? kPxSlotBytes : 0)))};
-            auto scores = [&](int x, int t) {                        // S_x = Q_x K_t^T
-                const int pos = k_pos(t);
-                if (!wait_full(pos)) return false;
-                tmem_fence_after_sync();
-                const uint32_t kb = umma_desc_lo(smem_u32(ring + (pos % kPxSlots) * kPxSlotBytes));
-#pragma unroll
-                for (int ks = 0; ks < 8; ++ks)
-                    umma_bf16(tmem + 128 * x, umma_desc(qa[x] + umma_kstep(ks, kPxHalf)), umma_desc(kb + umma_kstep(ks, kPxHalf)), idesc_s, ks > 0);
-                umma_commit(smem_u32(&tail->s_full[x]));
-                return true;
+            const uint32_t idesc_o = idesc_s | (1u << 16);               // B's contiguous direction is its outer index
+            const uint32_t qd0 = umma_desc_lo(smem_u32(q_smem)), qd1 = two ? umma_desc_lo(smem_u32(q_smem + kPxSlotBytes)) : qd0;
+            struct Tile { uint32_t addr, full, empty, parity; };
+            auto tile_at = [&](int pos) {
+                const uint32_t at = (uint32_t)(pos0 + pos), s = at % kPxSlots;
+                return Tile{smem_u32(ring) + s * kPxSlotBytes, smem_u32(&tail->full[s]), smem_u32(&tail->empty[s]), (at / kPxSlots) & 1};
             };
-            auto values = [&](int x, int t, int nth) {               // O_x += P_x V_t, the nth of the stream
-                if (!tc_wait(smem_u32(&tail->p_ready[x]), nth & 1, abort_flag)) return false;
-                const int pos = v_pos(t);
-                if (!wait_full(pos)) return false;
-                tmem_fence_after_sync();
-                const uint32_t vb = umma_desc_lo_outer(smem_u32(ring + (pos % kPxSlots) * kPxSlotBytes));
+            auto wait = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, tc_wait(bar, parity, abort_flag)); };
+            // S = Q K^T; O += P V. Commits arrive once all that has been issued is done; `last`: nobody reads the tile after this.
+            auto scores = [&](int st, const Tile& k, bool last) {
+                if (elect_one()) {
+                    const uint32_t kb = umma_desc_lo(k.addr), qd = st ? qd1 : qd0;
 #pragma unroll
-                for (int ks = 0; ks < 8; ++ks)                       // 16 keys: 2048 bytes of V, 8 columns of P
-                    umma_bf16_ta(tmem + 256 + 128 * x, tmem + 128 * x + 8 * ks, umma_desc(vb + ks * 128), idesc_o, nth > 0 || ks > 0);
-                return true;
+                    for (int ks = 0; ks < 8; ++ks)
+                        umma_bf16(tmem + 128 * st, umma_desc(qd + umma_kstep(ks, kPxHalf)), umma_desc(kb + umma_kstep(ks, kPxHalf)), idesc_s, ks > 0);
+                    umma_commit(smem_u32(&tail->s_full[st]));
+                    if (last) umma_commit(k.empty);
+                }
+                __syncwarp();
             };
-            ok = tc_wait(smem_u32(&tail->q_full), 0, abort_flag);
-            if (two) {
-                for (int x = 0; x < 2 && ok; ++x) ok = scores(x, 0);
-                if (ok) umma_commit(smem_u32(&tail->empty[k_pos(0) % kPxSlots]));
-                for (int t = 0; t < n_tiles && ok; ++t) {
-                    for (int x = 0; x < 2 && ok; ++x) {
-                        ok = values(x, t, t);
-                        if (ok && x == 1) umma_commit(smem_u32(&tail->empty[v_pos(t) % kPxSlots]));
-                        if (ok && t + 1 < n_tiles) ok = scores(x, t + 1);
+            auto values = [&](int st, int hf, const Tile& v, uint32_t more, bool last) {    // for half of the keys
+                if (elect_one()) {
+                    const uint32_t vb = umma_desc_lo_outer(v.addr);
+#pragma unroll
+                    for (int ks = 4 * hf; ks < 4 * hf + 4; ++ks)         // 16 keys: 2048 bytes of V, 8 columns of P
+                        umma_bf16_ta(tmem + 256 + 128 * st, tmem + 128 * st + 64 * hf + 8 * (ks & 3), umma_desc(vb + ks * 128), idesc_o,
+                                     ks > 0 ? 1u : more);
+                    if (last) umma_commit(v.empty);
+                }
+                __syncwarp();
+            };
+            if (pass == 0) ok = wait(smem_u32(&tail->q_full), 0);
+            for (int st = 0; st < 2 && ok; ++st)
+                if (count(st) > 0) {
+                    const Tile k = tile_at(k_pos(first(st)));
+                    ok = wait(k.full, k.parity);
+                    tmem_fence_after_sync();
+                    if (ok) scores(st, k, !two || st == 1);
+                }
+            for (int nth = 0; nth < count(0) && ok; ++nth) {
+#pragma unroll
+                for (int st = 0; st < 2; ++st) {
+                    const int n = count(st), t = first(st) + nth * stride;
+                    if (nth >= n) break;
+                    const bool more = nth + 1 < n, last = !two || st == 1;
+                    const Tile v = tile_at(v_pos(t)), k = tile_at(more ? k_pos(t + stride) : 0);
+                    ok = wait(v.full, v.parity);
+#pragma unroll
+                    for (int hf = 0; hf < 2; ++hf) {
+                        ok = ok && wait(smem_u32(&tail->p_ready[st][hf]), (pass * n + nth) & 1);
+                        if (!ok) break;
+                        tmem_fence_after_sync();
+                        values(st, hf, v, nth > 0, hf == 1 && last);
                     }
-                    if (ok && t + 1 < n_tiles) umma_commit(smem_u32(&tail->empty[k_pos(t + 1) % kPxSlots]));
-                }
-            } else {
-                for (int t = 0; t < min(2, n_tiles) && ok; ++t) {
-                    ok = scores(t, t);
-                    if (ok) umma_commit(smem_u32(&tail->empty[k_pos(t) % kPxSlots]));
-                }
-                for (int t = 0; t < n_tiles && ok; ++t) {
-                    ok = values(t & 1, t, t >> 1);
-                    if (ok) umma_commit(smem_u32(&tail->empty[v_pos(t) % kPxSlots]));
-                    if (ok && t + 2 < n_tiles) {
-                        ok = scores(t & 1, t + 2);
-                        if (ok) umma_commit(smem_u32(&tail->empty[k_pos(t + 2) % kPxSlots]));
+                    if (!ok) break;
+                    if (more) {
+                        ok = wait(k.full, k.parity);
+                        if (!ok) break;
+                        tmem_fence_after_sync();
+                        scores(st, k, last);
                     }
                 }
             }
             if (!ok) tail->abort_flag = 1;
-            umma_commit(smem_u32(&tail->o_full));    // also after a wait that expired: what was issued has to end
-        }
-    } else {
-        // ------------------------------------------------------------------ softmax
-        const int x = warp >> 3, half = (warp >> 2) & 1;    // stream, half of a tile's keys
-        const int row = tid & 127;                          // TMEM lane = query row of the stream's tile
-        const int pair = 1 + (x << 2) + (warp & 3);         // named barrier of the two warps of these rows
-        const uint32_t t_lane = (uint32_t)((warp & 3) * 32) << 16;
-        const uint32_t s_addr = tmem + t_lane + 128 * x, o_addr = tmem + t_lane + 256 + 128 * x + 64 * half;
-        {   // query rows into shared memory in the layout TMA would give them; rows that do not exist are zeros
-            uint4 v[8];                                  // all loads first; two ? 8 : 4 of them count
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                const int i = tid + k * kPxSoftmax, r = i >> 4, c = i & 15;
-                v[k] = make_uint4(0u, 0u, 0u, 0u);
-                if (r < rows) {
-                    const int s = r / p.g;
-                    v[k] = *reinterpret_cast<const uint4*>(p.q + ((size_t)(seq0 + s) * p.h_q + (size_t)head * p.g + (r - s * p.g)) * kHeadDim + c * 8);
+            if (elect_one()) umma_commit(smem_u32(&tail->o_full));    // also after a wait that expired: what was issued has to end
+            __syncwarp();
+        } else {
+            // -------------------------------------------------------------- softmax
+            if (pass == 0) {
+                // query rows into shared memory in the layout TMA would give them; rows that do not exist are zeros
+                for (int k = 0; k < (two ? 16 : 8); ++k) {
+                    const int i = tid + k * kPxSoftmax, r = i >> 4, c = i & 15, rr = min(r, rows - 1), sq = rr / p.g;
+                    cp_async_16_or_zeros(smem_u32(q_smem + (r >> 7) * kPxSlotBytes + (c >> 3) * kPxHalf + (r & 127) * 128 + (((c & 7) ^ (r & 7)) << 4)),
+                                         p.q + ((size_t)(seq0 + sq) * p.h_q + (size_t)head * p.g + (rr - sq * p.g)) * kHeadDim + c * 8, r < rows);
                 }
-            }
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                const int i = tid + k * kPxSoftmax, r = i >> 4, c = i & 15;
-                if (k < 4 || two)
-                    *reinterpret_cast<uint4*>(q_smem + (r >> 7) * kPxSlotBytes + (c >> 3) * kPxHalf + (r & 127) * 128 + (((c & 7) ^ (r & 7)) << 4)) = v[k];
-            }
-            fence_proxy_async_smem();
-            mbar_arrive(smem_u32(&tail->q_full));
-        }
-        float m = -INFINITY, l = 0.f;                   // in log2 units; l: this thread's half of the keys
-        const int mine = two ? n_tiles : (n_tiles - x + 1) / 2;
-        for (int i = 0; i < mine; ++i) {
-            const int t = two ? i : 2 * i + x;
-            const int valid = n_keys - (t0 + t) * kPxKeys;      // keys of this tile that exist (128 or more: all)
-            bool come = tc_wait(smem_u32(&tail->s_full[x]), i & 1, abort_flag);
-            if (valid < kPxKeys && (x == 0 || !two)) {
-                // V rows behind the prefix's end hold whatever the caller has there (0 * NaN): zeros instead. In the
-                // two-tile form stream B's product comes after stream A's, which waits for this.
-                const int pos = v_pos(t);
-                come = come && wait_full(pos);
-                uint8_t* v = ring + (pos % kPxSlots) * kPxSlotBytes;
-                if (come)
-                    for (int e = (half << 7) + row; e < (kPxKeys - valid) * 16; e += 256)
-                        *reinterpret_cast<uint4*>(v + (e & 8 ? kPxHalf : 0) + (valid + (e >> 4)) * 128 + (e & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+                cp_async_commit();
+                cp_async_wait_all();
                 fence_proxy_async_smem();
+                mbar_arrive(smem_u32(&tail->q_full));
             }
-            // the two warps go on or give up together
-            if (pair_any(pair, !come)) { ok = false; break; }
-            tmem_fence_after_sync();
-            uint32_t w[32];                                     // this thread's weights of the tile, bf16 pairs
-            float total;
-            bool fresh = i == 0;                                // no maximum yet
-            for (;;) {
-                if (fresh) {
-                    float top = -INFINITY;
-#pragma unroll
-                    for (int c = 0; c < 2; ++c) {
+            const int mine = count(x);
+            float top = -INFINITY;                       // second pass
+            l = 0.f;
+            for (int i = 0; i < mine; ++i) {
+                const int t = first(x) + i * stride;
+                const int valid = n_keys - (t0 + t) * kPxKeys;      // keys of this tile that exist (128 or more: all)
+                ok = tc_wait(smem_u32(&tail->s_full[x]), (pass * mine + i) & 1, abort_flag);
+                if (valid < kPxKeys) {
+                    // V rows behind the prefix's end hold whatever the caller has there (0 * NaN): zeros instead
+                    const int pos = pos0 + v_pos(t);
+                    ok = ok && wait_full(pos);
+                    uint8_t* v = ring + (pos % kPxSlots) * kPxSlotBytes;
+                    if (ok)
+                        for (int e = row; e < (kPxKeys - valid) * 16; e += 128)
+                            *reinterpret_cast<uint4*>(v + (e & 8 ? kPxHalf : 0) + (valid + (e >> 4)) * 128 + (e & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+                    fence_proxy_async_smem();
+                }
+                ok = __all_sync(0xffffffffu, ok);                   // a warp gives up as a whole
+                if (!ok) break;
+                tmem_fence_after_sync();
+                if (pass == 1 || (pass == 0 && i == 0)) {
+                    for (int c = 0; c < 4; ++c) {
                         float z[32];
-                        tmem_ld32_start(s_addr + 64 * half + 32 * c, z);
+                        tmem_ld32_start(s_addr + 32 * c, z);
                         tmem_ld_wait(z);
-                        mask_block(z, 2 * half + c, valid);
+                        mask_block(z, 32 * c, valid);
 #pragma unroll
                         for (int k = 0; k < 32; ++k) top = fmaxf(top, z[k]);
                     }
-                    if (half == 0) tail->row[x][row] = top;
-                    pair_sync(pair);
-                    if (half == 1) tail->row[x][row] = top = fmaxf(top, tail->row[x][row]);
-                    pair_sync(pair);
-                    top = tail->row[x][row];
-                    const float m_new = fmaxf(m, top * p.scale_log2);
-                    const float f = m_new == -INFINITY ? 1.f : fast_exp2(m - m_new);
-                    m = m_new;
-                    l *= f;
-                    if (i > 0) {                        // O of the tiles before is complete: S was issued after it
-#pragma unroll
-                        for (int c = 0; c < 2; ++c) {
-                            float o[32];
-                            tmem_ld32_start(o_addr + 32 * c, o);
-                            tmem_ld_wait(o);
-#pragma unroll
-                            for (int k = 0; k < 32; ++k) w[k] = __float_as_uint(o[k] * f);
-                            tmem_st32(o_addr + 32 * c, w);
-                        }
-                    }
+                    if (pass == 0) m = top * p.scale_log2;
                 }
                 const float ref = m == -INFINITY ? 0.f : -m;
                 const float2 scale2 = make_float2(p.scale_log2, p.scale_log2), ref2 = make_float2(ref, ref);
-                float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+#pragma unroll 1
+                for (int half = 0; half < 2; ++half) {
+                    if (pass != 1) {
+                        float2 sum = make_float2(0.f, 0.f);
+                        uint32_t w[32];                             // the weights of 64 keys, bf16 pairs
 #pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    float z[32];
-                    tmem_ld32_start(s_addr + 64 * half + 32 * c, z);
-                    tmem_ld_wait(z);
-                    mask_block(z, 2 * half + c, valid);
+                        for (int c = 0; c < 2; ++c) {
+                            float z[32];
+                            tmem_ld32_start(s_addr + 64 * half + 32 * c, z);
+                            tmem_ld_wait(z);
+                            mask_block(z, 64 * half + 32 * c, valid);
 #pragma unroll
-                    for (int k = 0; k < 32; k += 2) {
-                        const float2 y = fma_f32x2(make_float2(z[k], z[k + 1]), scale2, ref2);
-                        const float2 e = make_float2(fast_exp2(y.x), fast_exp2(y.y));
-                        sum[(k >> 1) & 1] = add_f32x2(sum[(k >> 1) & 1], e);
-                        w[16 * c + (k >> 1)] = pack_bf16x2(e.x, e.y);
+                            for (int k = 0; k < 32; k += 2) {
+                                const float2 y = fma_f32x2(make_float2(z[k], z[k + 1]), scale2, ref2);
+                                const float2 e = make_float2(fast_exp2(y.x), fast_exp2(y.y));
+                                sum = add_f32x2(sum, e);
+                                w[16 * c + (k >> 1)] = pack_bf16x2(e.x, e.y);
+                            }
+                        }
+                        const float total = sum.x + sum.y;
+                        if (pass == 0 && !(total <= kPxLimit)) *(volatile int*)&tail->overflow = 1;  // (NaN too: it comes out again)
+                        l += total;
+                        tmem_st32(s_addr + 64 * half, w);
+                        tmem_wait_st();
                     }
+                    tmem_fence_before_sync();
+                    mbar_arrive(smem_u32(&tail->p_ready[x][half]));
                 }
-                total = (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
-                // Both warps have read S when they get past this; weights of a fresh maximum are at most 1.
-                const bool over = pair_any(pair, !fresh && !(total <= kPxLimit));
-                if (!over) break;
-                fresh = true;
             }
-            l += total;
-            tmem_st32(s_addr + 32 * half, w);
-            tmem_wait_st();
-            tmem_fence_before_sync();
-            mbar_arrive(smem_u32(&tail->p_ready[x]));
+            if (!ok) tail->abort_flag = 1;
+            if (pass == 1) m = top * p.scale_log2;
+            if (!tc_wait(smem_u32(&tail->o_full), pass & 1, abort_flag)) ok = false;
         }
-        if (!ok) tail->abort_flag = 1;
-        if (!tc_wait(smem_u32(&tail->o_full), 0, abort_flag)) ok = false;
-        if (half == 1) tail->row[x][row] = l;
-        ok = !pair_any(pair, !ok || *(volatile int*)abort_flag != 0);
+        __syncthreads();
+        if (pass == 2 || *(volatile int*)&tail->overflow == 0) break;    // (written in the first pass only)
+    }
+    if (warp < kPxTmaWarp) {
         // ---- the row's partial result; a wait that expired shows as NaN in the output
+        ok = *(volatile int*)abort_flag == 0;
         float* rec = p.prefix_part + (size_t)blockIdx.x * kPrefixRecFloats;
         const int slot = 128 * x + row;
         const bool real = (two ? slot : row) < rows;
-        if (real && half == 0) {
+        if (real) {
             rec[slot] = ok ? m : 0.f;
-            rec[kPrefixRows + slot] = ok ? l + tail->row[x][row] : NAN;
+            rec[kPrefixRows + slot] = ok ? l : NAN;
         }
         tmem_fence_after_sync();
-        if (mine > 0 && ok && __any_sync(0xffffffffu, real)) {
+        if (count(x) > 0 && ok && __any_sync(0xffffffffu, real)) {
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
+            for (int c = 0; c < 4; ++c) {
                 float o[32];
                 __syncwarp();
                 tmem_ld32_start(o_addr + 32 * c, o);
                 tmem_ld_wait(o);
-                float4* dst = reinterpret_cast<float4*>(rec + 2 * kPrefixRows) + (16 * half + 8 * c) * kPrefixRows + slot;
+                float4* dst = reinterpret_cast<float4*>(rec + 2 * kPrefixRows) + 8 * c * kPrefixRows + slot;
                 if (real)
 #pragma unroll
                     for (int k = 0; k < 8; ++k) dst[k * kPrefixRows] = make_float4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
@@ -391,7 +393,7 @@ gkv_prefix_attn_kernel(const StoreAttnLaunch p, const __grid_constant__ CUtensor
         const int issued = *(volatile int*)&tail->issued;
         for (int pos = max(0, issued - kPxSlots); pos < issued; ++pos)
             mbar_wait_bounded(smem_u32(&tail->full[pos % kPxSlots]), (pos / kPxSlots) & 1);
-        mbar_wait_bounded(smem_u32(&tail->o_full), 0);
+        mbar_wait_bounded(smem_u32(&tail->o_full), pass & 1);
     }
     __syncthreads();
     if (warp == kPxMmaWarp) {
@@ -402,7 +404,9 @@ gkv_prefix_attn_kernel(const StoreAttnLaunch p, const __grid_constant__ CUtensor
 
 cudaError_t launch_prefix_attn(const StoreAttnLaunch& p, const CUtensorMap& tm_k, const CUtensorMap& tm_v, cudaStream_t s) {
     // a property of the function on the current device; setting it again costs less than finding out whether it is set
-    const cudaError_t e = cudaFuncSetAttribute(gkv_prefix_attn_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kPxSmem);
+    // (All of the SM's memory as shared memory, so that CTAs of the next kernel find room beside this one's.)
+    cudaError_t e = cudaFuncSetAttribute(gkv_prefix_attn_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kPxSmem);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(gkv_prefix_attn_kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
     if (e != cudaSuccess) return e;
     gkv_prefix_attn_kernel<<<(unsigned)p.prefix_items, kPxThreads, kPxSmem, s>>>(p, tm_k, tm_v);
     return cudaGetLastError();

@@ -150,7 +150,11 @@ namespace gkv {
 // Own rows: as many pieces per unit as fill the places of resident CTAs, none below 8 tiles (two turns of the four warps). (With
 // more units than half the places units go whole: cutting 1024 units into thirds, to fill the last round of CTAs better, took 157
 // us as clusters and 105 us by way of the workspace where whole units take 110 us.)
-// Prefixes: runs of key tiles such that the items fill whole rounds of one CTA per SM.
+// Prefixes: the length of the runs that the prefixes' key tiles are cut into. An item occupies an SM for about 8 us + 1.05 us a
+// tile (2.1 with more than 128 query rows); the attention over own rows (at 5.5 TB/s, with sequences three quarters of the
+// longest on average) takes the SMs that are left and, in part, the same ones; every run leaves a partial result that is written
+// and read again (3.4 TB/s). Short runs end soon, long ones waste less. (32 answers on 8192 shared rows, 64 tiles, by tiles of a
+// run: 1: 53 us, 2: 44, 4: 33, 6: 31, 8: 36, 16: 53; 128 answers on 4 documents of up to 128 tiles: 26: 161 us, 43: 145, 64: 177.)
 void store_plan(StoreAttnLaunch* p, int max_len, int sm_count) {
     const int64_t units = (int64_t)p->batch * p->h_kv, places = (int64_t)store_attn_ctas_per_sm(p->format) * sm_count;
     const int n = max_len + (p->k_new ? 1 : 0);
@@ -168,15 +172,18 @@ void store_plan(StoreAttnLaunch* p, int max_len, int sm_count) {
     int longest = 0;
     for (int i = 0; i < p->n_prefix; ++i) longest = p->prefix_len[i] > longest ? p->prefix_len[i] : longest;
     const int key_tiles = (longest + 127) / 128;
-    // the cheapest of the possible run lengths: rounds x (tiles of a run + a fixed cost of about 3 tiles per item)
     const int64_t base = prefix_items(*p, key_tiles);
-    int64_t best_cost = -1;
+    const double row = row_bytes(p->format) + 2 * scales_per_row(p->format);
+    const double own_us = 4 + 0.75 * n * row * 2 * units / 5.5e6, part_us = (double)p->batch * p->h_q * kHeadDim * 8 / 3.4e6;
+    double best = -1;
     for (int runs = 1; runs <= key_tiles && runs <= kMaxRuns; ++runs) {
         const int chunk = (key_tiles + runs - 1) / runs;
-        const int64_t items = prefix_items(*p, chunk);
+        const int64_t items = prefix_items(*p, chunk), rounds = (items + sm_count - 1) / sm_count;
         if (runs > 1 && items > base + kPrefixSplitItems) break;
-        const int64_t cost = ((items + sm_count - 1) / sm_count) * (chunk + 3);
-        if (best_cost < 0 || cost < best_cost) { best_cost = cost; p->chunk = chunk; p->prefix_items = (int)items; }
+        const double item_us = 8 + (p->two_tiles ? 2.1 : 1.05) * chunk;
+        const double alone = rounds * item_us, together = own_us + items * item_us / sm_count;
+        const double cost = (alone > together ? alone : together) + part_us * ((key_tiles + chunk - 1) / chunk);
+        if (best < 0 || cost < best) { best = cost; p->chunk = chunk; p->prefix_items = (int)items; }
     }
 }
 
