@@ -101,18 +101,14 @@ __device__ __forceinline__ void unpack8(uint32_t w, uint32_t& lo, uint32_t& hi) 
         hi = hsub2(__byte_perm(w, 0x64646464u, 0x4342), 0x64806480u);
     }
 }
-// Two 16-bit words of nibbles (one in each half of w) -> four fp16 pairs (nibble e of both words), exactly. A byte u0 + 16 u1
-// (u = c + 8) under the exponent of 1024 is x = 1024 + u0 + 16 u1; without its low nibble y = 1024 + 16 u1, so c1 = y / 16 - 72
-// and c0 = (x - 16 c1) - 1160. The logic unit, which has half the rate of the floating-point pipe here, gets 4 instructions of
-// 10. (Leaving the offset 8 in and taking it off the sums would save more, but costs precision: as 1024 + u in the fp32 sums,
-// as subnormals u 2^-24 where the products are aligned.)
-__device__ __forceinline__ void unpack4(uint32_t w, uint32_t (&e)[4]) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const uint32_t x = __byte_perm(w, 0x64646464u, i == 0 ? 0x4240 : 0x4341);
-        e[2 * i + 1] = hfma2(x & 0xfff0fff0u, 0x2c002c00u, 0xd480d480u);
-        e[2 * i] = hsub2(hfma2(e[2 * i + 1], 0xcc00cc00u, x), 0x64886488u);
-    }
+// Two bytes of nibbles under the exponent of 1024, x = 1024 + u0 + 16 u1 in both halves (u = c + 8) -> the fp16 pairs c0 and c1,
+// exactly: without its low nibble x is y = 1024 + 16 u1, so c1 = y / 16 - 72 and c0 = (x - 16 c1) - 1160. One instruction for
+// the logic unit, which these kernels keep busiest, and three for the half-precision pipe. (Leaving the offset 8 in and taking it
+// off the sums would save the latter, but costs precision: as 1024 + u in the fp32 sums, as subnormals u 2^-24 where the
+// products are aligned.)
+__device__ __forceinline__ void unpack4(uint32_t x, uint32_t& c0, uint32_t& c1) {
+    c1 = hfma2(x & 0xfff0fff0u, 0x2c002c00u, 0xd480d480u);
+    c0 = hsub2(hfma2(c1, 0xcc00cc00u, x), 0x64886488u);
 }
 
 // Registers of one 16-key tile. K: this lane's pieces of rows r = lane / 4 and r + 8. V: its pieces of keys 2j, 2j + 1, 2j + 8,
@@ -129,7 +125,7 @@ template <> struct TileV<GKV_STORE_INT8> { uint4 d[4]; uint32_t s[2]; };
 template <> struct TileV<GKV_STORE_INT4> { uint2 d[4]; uint2 s[2]; };
 
 // Where a lane's pieces of a tile begin: offsets from the unit's rows (below 2^32: a unit has at most 2^24 rows of 256 bytes);
-// everything of a tile and of the others of a step is at constant distances.
+// everything of a tile is at constant distances.
 template <int F>
 struct TilePtrs {
     using Fm = StoreFormat<F>;
@@ -147,13 +143,13 @@ struct TilePtrs {
 // Rows from `left` on (counted from the tile's first) are not loaded: zeros stand for them, so that whatever lies there cannot
 // reach the sums. WHOLE: all 16 exist.
 template <int F, bool WHOLE>
-__device__ __forceinline__ void load_k(TileK<F>& t, const TilePtrs<F>& p, int u, int left, int lane) {
+__device__ __forceinline__ void load_k(TileK<F>& t, const TilePtrs<F>& p, int left, int lane) {
     constexpr int kPieces = F == GKV_STORE_BF16 ? 4 : F == GKV_STORE_INT4 ? 1 : 2;
 #pragma unroll
     for (int hf = 0; hf < 2; ++hf) {
         const bool in = WHOLE || (lane >> 2) + 8 * hf < left;
-        const uint8_t* row = p.kb + p.k + (u * kTile + 8 * hf) * StoreFormat<F>::kRow;
-        const uint8_t* sc = p.ksb + p.s + (u * kTile + 8 * hf) * (2 * StoreFormat<F>::kScales);
+        const uint8_t* row = p.kb + p.k + 8 * hf * StoreFormat<F>::kRow;
+        const uint8_t* sc = p.ksb + p.s + 8 * hf * (2 * StoreFormat<F>::kScales);
 #pragma unroll
         for (int c = 0; c < kPieces; ++c) t.d[hf][c] = in ? ld16(row + c * 64) : make_uint4(0u, 0u, 0u, 0u);
         if constexpr (F == GKV_STORE_INT4) t.s[hf] = in ? ld8(sc) : make_uint2(0u, 0u);
@@ -161,13 +157,13 @@ __device__ __forceinline__ void load_k(TileK<F>& t, const TilePtrs<F>& p, int u,
     }
 }
 template <int F, bool WHOLE>
-__device__ __forceinline__ void load_v(TileV<F>& t, const TilePtrs<F>& p, int u, int left, int lane) {
+__device__ __forceinline__ void load_v(TileV<F>& t, const TilePtrs<F>& p, int left, int lane) {
     const int j = lane & 3;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int key = (i & 1) + 8 * (i >> 1);
         const bool in = WHOLE || 2 * j + key < left;
-        const uint8_t* row = p.vb + p.v + (u * kTile + key) * StoreFormat<F>::kRow;
+        const uint8_t* row = p.vb + p.v + key * StoreFormat<F>::kRow;
         if constexpr (F == GKV_STORE_BF16) {
             t.d[i][0] = in ? ld16(row) : make_uint4(0u, 0u, 0u, 0u);
             t.d[i][1] = in ? ld16(row + 128) : make_uint4(0u, 0u, 0u, 0u);
@@ -181,31 +177,21 @@ __device__ __forceinline__ void load_v(TileV<F>& t, const TilePtrs<F>& p, int u,
 #pragma unroll
     for (int hf = 0; hf < 2; ++hf) {
         const bool in = WHOLE || (lane >> 2) + 8 * hf < left;
-        const uint8_t* sc = p.vsb + p.s + (u * kTile + 8 * hf) * (2 * StoreFormat<F>::kScales);
+        const uint8_t* sc = p.vsb + p.s + 8 * hf * (2 * StoreFormat<F>::kScales);
         if constexpr (F == GKV_STORE_INT4) t.s[hf] = in ? ld8(sc) : make_uint2(0u, 0u);
         else if constexpr (F != GKV_STORE_BF16) t.s[hf] = in ? ld2(sc) : 0u;
     }
 }
-// `left` keys of the step's U tiles exist (the same number for the whole warp; none or fewer: no loads).
-template <int F, int U>
-__device__ __forceinline__ void load_step_k(TileK<F> (&t)[U], const TilePtrs<F>& p, int left, int lane) {
-    if (left >= U * kTile) {
-#pragma unroll
-        for (int u = 0; u < U; ++u) load_k<F, true>(t[u], p, u, 0, lane);
-    } else {
-#pragma unroll
-        for (int u = 0; u < U; ++u) load_k<F, false>(t[u], p, u, left - u * kTile, lane);
-    }
+// `left` of a tile's keys exist (the same number for the whole warp; none or fewer: no loads).
+template <int F>
+__device__ __forceinline__ void load_tile_k(TileK<F>& t, const TilePtrs<F>& p, int left, int lane) {
+    if (left >= kTile) load_k<F, true>(t, p, 0, lane);
+    else load_k<F, false>(t, p, left, lane);
 }
-template <int F, int U>
-__device__ __forceinline__ void load_step_v(TileV<F> (&t)[U], const TilePtrs<F>& p, int left, int lane) {
-    if (left >= U * kTile) {
-#pragma unroll
-        for (int u = 0; u < U; ++u) load_v<F, true>(t[u], p, u, 0, lane);
-    } else {
-#pragma unroll
-        for (int u = 0; u < U; ++u) load_v<F, false>(t[u], p, u, left - u * kTile, lane);
-    }
+template <int F>
+__device__ __forceinline__ void load_tile_v(TileV<F>& t, const TilePtrs<F>& p, int left, int lane) {
+    if (left >= kTile) load_v<F, true>(t, p, 0, lane);
+    else load_v<F, false>(t, p, left, lane);
 }
 
 // Logits of a tile in log2 units: z[0], z[1] = key r and heads h0, h0 + 1; z[2], z[3] = key r + 8. f0, f1: factors of the heads.
@@ -215,16 +201,18 @@ __device__ __forceinline__ void tile_logits(const TileK<F>& t, const uint32_t (&
         z[0] = z[1] = z[2] = z[3] = 0.f;
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
-            uint32_t a[2][4];   // [row r / r + 8][element pair]
-#pragma unroll
-            for (int hf = 0; hf < 2; ++hf) {
-                const uint4 d = t.d[hf][0];
-                unpack4(__byte_perm(g < 2 ? d.x : d.y, g < 2 ? d.z : d.w, (g & 1) ? 0x7632 : 0x5410), a[hf]);
-            }
             float acc[4] = {0.f, 0.f, 0.f, 0.f};
-            const uint32_t a0[4] = {a[0][0], a[1][0], a[0][1], a[1][1]}, a1[4] = {a[0][2], a[1][2], a[0][3], a[1][3]};
-            mma_row<F>(acc, a0, qf[2 * g][0], qf[2 * g][1]);
-            mma_row<F>(acc, a1, qf[2 * g + 1][0], qf[2 * g + 1][1]);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {       // the 16-bit words 2j and 2j + 1 of the group: elements 0, 2 and 1, 3 of each
+                uint32_t a[4];
+#pragma unroll
+                for (int hf = 0; hf < 2; ++hf) {
+                    const uint4 d = t.d[hf][0];
+                    const uint32_t w = k == 0 ? (g < 2 ? d.x : d.y) : (g < 2 ? d.z : d.w);
+                    unpack4(__byte_perm(w, 0x64646464u, (g & 1) ? 0x4342 : 0x4140), a[hf], a[hf + 2]);
+                }
+                mma_row<F>(acc, a, qf[2 * g + k][0], qf[2 * g + k][1]);
+            }
             const uint32_t w0 = g < 2 ? t.s[0].x : t.s[0].y, w1 = g < 2 ? t.s[1].x : t.s[1].y;
             const float s0 = (g & 1) ? bf16_hi(w0) : bf16_lo(w0), s1 = (g & 1) ? bf16_hi(w1) : bf16_lo(w1);
             z[0] = fmaf(acc[0], s0, z[0]); z[1] = fmaf(acc[1], s0, z[1]);
@@ -275,12 +263,14 @@ __device__ __forceinline__ void tile_values(const TileV<F>& t, const uint32_t (&
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
             auto word = [&](int key) { return g < 2 ? t.d[key].x : t.d[key].y; };
-            uint32_t x[4], y[4];
-            unpack4(__byte_perm(word(0), word(1), (g & 1) ? 0x7632 : 0x5410), x);
-            unpack4(__byte_perm(word(2), word(3), (g & 1) ? 0x7632 : 0x5410), y);
-            const uint32_t a0[4] = {x[0], x[1], y[0], y[1]}, a1[4] = {x[2], x[3], y[2], y[3]};
-            mma_row<F>(acc[2 * g], a0, b[g][0], b[g][1]);
-            mma_row<F>(acc[2 * g + 1], a1, b[g][0], b[g][1]);
+            const uint32_t x = __byte_perm(word(0), word(1), (g & 1) ? 0x7632 : 0x5410), y = __byte_perm(word(2), word(3), (g & 1) ? 0x7632 : 0x5410);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {       // the group's bytes: dimensions 2k (rows q) and 2k + 1 (rows q + 8)
+                uint32_t a[4];
+                unpack4(__byte_perm(x, 0x64646464u, k == 0 ? 0x4240 : 0x4341), a[0], a[1]);
+                unpack4(__byte_perm(y, 0x64646464u, k == 0 ? 0x4240 : 0x4341), a[2], a[3]);
+                mma_row<F>(acc[2 * g + k], a, b[g][0], b[g][1]);
+            }
         }
     } else {
 #pragma unroll
@@ -304,8 +294,7 @@ __device__ __forceinline__ int out_dim(int i, int q) {
     if (F == GKV_STORE_INT4) return 32 * (i >> 1) + 4 * q + 2 * (i & 1);
     return 16 * q + 2 * i;
 }
-// First of the two element pairs of q that lane j multiplies at step ks; the second pair is at +step2, the pair's second
-// element at +next.
+// The two pairs of elements of q that lane j has at step ks.
 template <int F>
 __device__ __forceinline__ void load_query(const __nv_bfloat16* row, int ks, int j, uint32_t& b0, uint32_t& b1) {
     const uint16_t* q = reinterpret_cast<const uint16_t*>(row);
@@ -313,9 +302,8 @@ __device__ __forceinline__ void load_query(const __nv_bfloat16* row, int ks, int
         const uint2 x = *reinterpret_cast<const uint2*>(q + 32 * (ks >> 1) + 8 * j + 4 * (ks & 1));
         b0 = x.x; b1 = x.y;
     } else if (F == GKV_STORE_INT4) {
-        const uint16_t* x = q + 32 * (ks >> 1) + 8 * j + 2 * (ks & 1);
-        const uint32_t a = *reinterpret_cast<const uint32_t*>(x), b = *reinterpret_cast<const uint32_t*>(x + 4);
-        b0 = __byte_perm(a, b, 0x5410); b1 = __byte_perm(a, b, 0x7632);
+        const uint2 x = *reinterpret_cast<const uint2*>(q + 32 * (ks >> 1) + 8 * j + 4 * (ks & 1));
+        b0 = __byte_perm(x.x, x.y, 0x5410); b1 = __byte_perm(x.x, x.y, 0x7632);
     } else {
         const uint2 x = *reinterpret_cast<const uint2*>(q + 64 * (ks >> 2) + 16 * j + 4 * (ks & 3));
         b0 = x.x; b1 = x.y;
@@ -332,9 +320,9 @@ __device__ __forceinline__ float final_lse(float m, float l, bool fits) {
     return !fits ? NAN : m == -INFINITY && l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
 }
 
-// Resident CTAs per SM. 8-bit rows: one 16-key tile per warp and step and 128 registers, 16 warps (the 32B batch of the
-// benchmark shapes: 97 us; two tiles, 168 registers and 12 warps: 110 us). bf16 rows need twice the registers for a tile, 4-bit
-// ones want two tiles in flight.
+// Resident CTAs per SM. 8-bit rows: 128 registers, 16 warps (the 32B batch of the benchmark shapes: 97 us; two tiles per step, 168
+// registers and 12 warps: 110 us). bf16 rows need twice the registers for a tile; 4-bit ones are slower at 128 registers (131071
+// keys: 83 us against 81, with two tiles per step 85).
 __host__ __device__ constexpr int store_ctas(int format) { return format == GKV_STORE_BF16 || format == GKV_STORE_INT4 ? 3 : 4; }
 int store_attn_ctas_per_sm(int format) { return store_ctas(format); }
 
@@ -342,7 +330,7 @@ int store_attn_ctas_per_sm(int format) { return store_ctas(format); }
 enum { kWhole = 0, kPart = 1, kCluster = 2 };
 
 // Own rows of the units. Grid: units x splits, split fastest.
-template <int F, int U, int MODE>
+template <int F, int MODE>
 __global__ void __launch_bounds__(kThreads, store_ctas(F)) gkv_store_attn_kernel(const StoreAttnLaunch p) {
     constexpr int NG = F == GKV_STORE_INT4 ? 4 : 1;
     constexpr bool kScaled = F != GKV_STORE_BF16;
@@ -354,6 +342,8 @@ __global__ void __launch_bounds__(kThreads, store_ctas(F)) gkv_store_attn_kernel
     const int seq = unit / p.h_kv, head = unit - seq * p.h_kv;
     const int len = p.len[seq];
     const bool append = p.k_new != nullptr;
+    uint4 new_row = make_uint4(0u, 0u, 0u, 0u);           // on its way while the length is (lanes 0-15: K, 16-31: V)
+    if (append) new_row = store_load_source<F>((lane < 16 ? p.k_new : p.v_new) + (size_t)unit * kHeadDim, lane & 15);
     const bool fits = append ? len < p.capacity : len <= p.capacity;
     // The merge goes by this word and not by the length, which it may count up itself.
     if (MODE == kPart) grid_launch_dependents();
@@ -373,16 +363,12 @@ __global__ void __launch_bounds__(kThreads, store_ctas(F)) gkv_store_attn_kernel
     __nv_bfloat16* ksb = p.k_scale + (size_t)unit * p.capacity * StoreFormat<F>::kScales;
     __nv_bfloat16* vsb = p.v_scale + (size_t)unit * p.capacity * StoreFormat<F>::kScales;
 
-    // Steps of U tiles go round the warps.
-    const int steps = (t_end - t_begin + U - 1) / U;
     // The warp that comes to the new row's tile puts the row into the store, before it loads anything of that tile (its own
     // writes are ordered before its later reads; no other warp reads the row).
-    if (append && fits && steps > 0 && t_end == tiles && warp == (steps - 1) % kWarps) {
-        const int l = lane & 15;
-        const __nv_bfloat16* src = (lane < 16 ? p.k_new : p.v_new) + (size_t)unit * kHeadDim;
-        const uint4 x = store_load_source<F>(src, l);
+    const int own_tiles = t_end - t_begin;               // tile i of the piece is warp i % kWarps'
+    if (append && fits && own_tiles > 0 && t_end == tiles && warp == (own_tiles - 1) % kWarps) {
         store_put_row<F>((lane < 16 ? kb : vb) + (size_t)len * StoreFormat<F>::kRow,
-                         (lane < 16 ? ksb : vsb) + (size_t)len * StoreFormat<F>::kScales, l, x);
+                         (lane < 16 ? ksb : vsb) + (size_t)len * StoreFormat<F>::kScales, lane & 15, new_row);
         __threadfence_block();
         __syncwarp();
     }
@@ -422,79 +408,67 @@ __global__ void __launch_bounds__(kThreads, store_ctas(F)) gkv_store_attn_kernel
 #pragma unroll
     for (int i = 0; i < 8; ++i) acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.f;
 
-    TileK<F> tk[U];
-    TileV<F> tv[U];
-    constexpr int kStepKeys = U * kTile;
+    TileK<F> tk;
+    TileV<F> tv;
     const int end = min(t_end * kTile, n);
-    const int key0 = (t_begin + warp * U) * kTile;
-    int left = warp < steps ? end - key0 : 0;                       // keys from this step's first on
+    const int key0 = (t_begin + warp) * kTile;
+    int left = warp < own_tiles ? end - key0 : 0;        // keys from this tile's first on
     TilePtrs<F> at;
     at.kb = kb; at.vb = vb;
     at.ksb = reinterpret_cast<const uint8_t*>(ksb); at.vsb = reinterpret_cast<const uint8_t*>(vsb);
     at.set(key0, lane);
-    load_step_k<F, U>(tk, at, left, lane);
-    load_step_v<F, U>(tv, at, left, lane);
+    load_tile_k<F>(tk, at, left, lane);
+    load_tile_v<F>(tv, at, left, lane);
     while (left > 0) {
-        at.advance(kWarps * kStepKeys);
-        const int left_next = left - kWarps * kStepKeys;
-        float z[U][4];
+        at.advance(kWarps * kTile);
+        const int left_next = left - kWarps * kTile;
+        float z[4];
+        tile_logits<F>(tk, qf, f0, f1, z);
+        load_tile_k<F>(tk, at, left_next, lane);
+        if (left < kTile) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) tile_logits<F>(tk[u], qf, f0, f1, z[u]);
-        load_step_k<F, U>(tk, at, left_next, lane);
-        if (left < kStepKeys) {
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-#pragma unroll
-                for (int hf = 0; hf < 2; ++hf)
-                    if (u * kTile + hq + 8 * hf >= left) z[u][2 * hf] = z[u][2 * hf + 1] = -INFINITY;
+            for (int hf = 0; hf < 2; ++hf)
+                if (hq + 8 * hf >= left) z[2 * hf] = z[2 * hf + 1] = -INFINITY;
         }
         // V scales of this lane's two keys (0 behind the end), and the sum of a key's: the largest, up to a factor of 4
-        float sc[U][2][NG], top[U][2];
+        float sc[2][NG], top[2];
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-#pragma unroll
-            for (int hf = 0; hf < 2; ++hf) {
-                if constexpr (F == GKV_STORE_INT4) {
-                    const uint2 s = tv[u].s[hf];
-                    sc[u][hf][0] = bf16_lo(s.x); sc[u][hf][1] = bf16_hi(s.x);
-                    sc[u][hf][2] = bf16_lo(s.y); sc[u][hf][3] = bf16_hi(s.y);
-                    top[u][hf] = (sc[u][hf][0] + sc[u][hf][1]) + (sc[u][hf][2] + sc[u][hf][3]);
-                } else if constexpr (kScaled) {
-                    top[u][hf] = sc[u][hf][0] = bf16_lo(tv[u].s[hf]);
-                } else {
-                    sc[u][hf][0] = top[u][hf] = 1.f;
-                }
+        for (int hf = 0; hf < 2; ++hf) {
+            if constexpr (F == GKV_STORE_INT4) {
+                const uint2 s = tv.s[hf];
+                sc[hf][0] = bf16_lo(s.x); sc[hf][1] = bf16_hi(s.x);
+                sc[hf][2] = bf16_lo(s.y); sc[hf][3] = bf16_hi(s.y);
+                top[hf] = (sc[hf][0] + sc[hf][1]) + (sc[hf][2] + sc[hf][3]);
+            } else if constexpr (kScaled) {
+                top[hf] = sc[hf][0] = bf16_lo(tv.s[hf]);
+            } else {
+                sc[hf][0] = top[hf] = 1.f;
             }
-        float e[U][4];                  // exp2(z - m)
+        }
+        float e[4];                     // exp2(z - m)
         // A z that is far above m, or a z + log2(scale) far above v, shows in the results: they are sums of non-negative numbers
         // (at most the limit then), infinite or NaN, also at the first step, where m is -infinity.
         float total = 0.f;
         auto weigh = [&]() {
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                e[u][0] = fast_exp2(z[u][0] - n0); e[u][1] = fast_exp2(z[u][1] - n1);
-                e[u][2] = fast_exp2(z[u][2] - n0); e[u][3] = fast_exp2(z[u][3] - n1);
-                total += (e[u][0] + e[u][2]) + (e[u][1] + e[u][3]);
-                if (kScaled)
-                    total += ((e[u][0] * c0 + e[u][1] * c1) * top[u][0] + (e[u][2] * c0 + e[u][3] * c1) * top[u][1]) * (1.f / kLiftFactor);
-            }
+            e[0] = fast_exp2(z[0] - n0); e[1] = fast_exp2(z[1] - n1);
+            e[2] = fast_exp2(z[2] - n0); e[3] = fast_exp2(z[3] - n1);
+            total += (e[0] + e[2]) + (e[1] + e[3]);
+            if (kScaled)
+                total += ((e[0] * c0 + e[1] * c1) * top[0] + (e[2] * c0 + e[3] * c1) * top[1]) * (1.f / kLiftFactor);
         };
         weigh();
         const bool over = !(total <= LagLimit<F>::value);
         if (__any_sync(0xffffffffu, over)) {
             float a0 = m0, a1 = m1, b0 = v0, b1 = v1;
+            a0 = fmaxf(a0, fmaxf(z[0], z[2]));
+            a1 = fmaxf(a1, fmaxf(z[1], z[3]));
+            if (kScaled) {
+                float t0 = sc[0][0], t1 = sc[1][0];     // fmaxf leaves out a NaN
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                a0 = fmaxf(a0, fmaxf(z[u][0], z[u][2]));
-                a1 = fmaxf(a1, fmaxf(z[u][1], z[u][3]));
-                if (kScaled) {
-                    float t0 = sc[u][0][0], t1 = sc[u][1][0];     // fmaxf leaves out a NaN
-#pragma unroll
-                    for (int g = 1; g < NG; ++g) { t0 = fmaxf(t0, sc[u][0][g]); t1 = fmaxf(t1, sc[u][1][g]); }
-                    const float x0 = fast_log2(t0), x1 = fast_log2(t1);
-                    b0 = fmaxf(b0, fmaxf(z[u][0] + x0, z[u][2] + x1));
-                    b1 = fmaxf(b1, fmaxf(z[u][1] + x0, z[u][3] + x1));
-                }
+                for (int g = 1; g < NG; ++g) { t0 = fmaxf(t0, sc[0][g]); t1 = fmaxf(t1, sc[1][g]); }
+                const float x0 = fast_log2(t0), x1 = fast_log2(t1);
+                b0 = fmaxf(b0, fmaxf(z[0] + x0, z[2] + x1));
+                b1 = fmaxf(b1, fmaxf(z[1] + x0, z[3] + x1));
             }
 #pragma unroll
             for (int o = 4; o < 32; o <<= 1) {
@@ -523,25 +497,22 @@ __global__ void __launch_bounds__(kThreads, store_ctas(F)) gkv_store_attn_kernel
             for (int i = 0; i < 8; ++i) { acc[i][0] *= r0; acc[i][1] *= r1; acc[i][2] *= r0; acc[i][3] *= r1; }
             weigh();
         }
+        l0 += e[0] + e[2];
+        l1 += e[1] + e[3];
+        uint32_t b[NG][2];
+        if constexpr (!kScaled) {
+            b[0][0] = movmatrix_trans(pack_weights<F>(e[0], e[1]));
+            b[0][1] = movmatrix_trans(pack_weights<F>(e[2], e[3]));
+        } else {
+            const float p0 = e[0] * c0, p1 = e[1] * c1, p2 = e[2] * c0, p3 = e[3] * c1;
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            l0 += e[u][0] + e[u][2];
-            l1 += e[u][1] + e[u][3];
-            uint32_t b[NG][2];
-            if constexpr (!kScaled) {
-                b[0][0] = movmatrix_trans(pack_weights<F>(e[u][0], e[u][1]));
-                b[0][1] = movmatrix_trans(pack_weights<F>(e[u][2], e[u][3]));
-            } else {
-                const float p0 = e[u][0] * c0, p1 = e[u][1] * c1, p2 = e[u][2] * c0, p3 = e[u][3] * c1;
-#pragma unroll
-                for (int g = 0; g < NG; ++g) {
-                    b[g][0] = movmatrix_trans(pack_weights<F>(p0 * sc[u][0][g], p1 * sc[u][0][g]));
-                    b[g][1] = movmatrix_trans(pack_weights<F>(p2 * sc[u][1][g], p3 * sc[u][1][g]));
-                }
+            for (int g = 0; g < NG; ++g) {
+                b[g][0] = movmatrix_trans(pack_weights<F>(p0 * sc[0][g], p1 * sc[0][g]));
+                b[g][1] = movmatrix_trans(pack_weights<F>(p2 * sc[1][g], p3 * sc[1][g]));
             }
-            tile_values<F, NG>(tv[u], b, acc);
         }
-        load_step_v<F, U>(tv, at, left_next, lane);
+        tile_values<F, NG>(tv, b, acc);
+        load_tile_v<F>(tv, at, left_next, lane);
         left = left_next;
     }
 
@@ -650,15 +621,16 @@ __global__ void __launch_bounds__(kThreads, store_ctas(F)) gkv_store_attn_kernel
 }
 
 // Joins the partial results of a unit: those of its own pieces and, with a prefix, those of the prefix items that hold its
-// query rows. One CTA per unit; thread t holds head t & 7 of four dimensions over every (blockDim / 256)th of the parts, so that
-// 8 lanes read 128 contiguous bytes of a record. The statistics of all parts are loaded at once, the values of 8 parts at a
-// time: the kernel is a few trips to L2.
-__global__ void __launch_bounds__(1024) gkv_store_merge_kernel(const StoreAttnLaunch p) {
+// query rows. 2^ds CTAs per unit, each with a share of the dimensions; thread t holds head t & 7 of four dimensions over every
+// (slices)th of the parts, so that 8 lanes read 128 contiguous bytes of a record. The statistics of all parts are loaded at once,
+// the values of 8 parts at a time: the kernel is a few trips to L2.
+__global__ void __launch_bounds__(1024) gkv_store_merge_kernel(const StoreAttnLaunch p, const int ds) {
     extern __shared__ float s_part[];                // [parts][8] factors
     __shared__ __align__(16) float s_red[4 * 1024];
     __shared__ float s_fin[3][8];
-    const int unit = blockIdx.x, seq = unit / p.h_kv, head = unit - seq * p.h_kv;
-    const int t = threadIdx.x, slices = blockDim.x >> 8, slice = t >> 8, h = t & 7, d4 = (t >> 3) & 31;
+    const int unit = blockIdx.x >> ds, share = blockIdx.x & ((1 << ds) - 1), seq = unit / p.h_kv, head = unit - seq * p.h_kv;
+    const int t = threadIdx.x, slices = blockDim.x >> (8 - ds), slice = t >> (8 - ds), h = t & 7;
+    const int d4 = ((t >> 3) & ((32 >> ds) - 1)) + share * (32 >> ds);
     const int hc = min(h, p.g - 1), warps = blockDim.x >> 5;
 
     // records: own ones, then those of the prefix items (two results each where the item's streams share the rows)
@@ -754,7 +726,7 @@ __global__ void __launch_bounds__(1024) gkv_store_merge_kernel(const StoreAttnLa
         __syncthreads();
         if (slice == 0)
             for (int i = 1; i < slices; ++i) {
-                const float4 a = reinterpret_cast<const float4*>(s_red)[i * 256 + t];
+                const float4 a = reinterpret_cast<const float4*>(s_red)[(i << (8 - ds)) + t];
                 o.x += a.x; o.y += a.y; o.z += a.z; o.w += a.w;
             }
     } else {
@@ -766,15 +738,16 @@ __global__ void __launch_bounds__(1024) gkv_store_merge_kernel(const StoreAttnLa
             make_uint2(pack_bf16x2(final_value(o.x, fm, fl, fv, fits), final_value(o.y, fm, fl, fv, fits)),
                        pack_bf16x2(final_value(o.z, fm, fl, fv, fits), final_value(o.w, fm, fl, fv, fits)));
     }
-    if (t < p.g) {
+    if (share == 0 && t < p.g) {
         if (p.lse) p.lse[(size_t)seq * p.h_q + (size_t)head * p.g + t] = final_lse(s_fin[0][t], s_fin[1][t], fits);
         if (p.len_out && head == 0 && t == 0 && fits) p.len_out[seq] += 1;
     }
 }
 
 // cluster > 1: clusters of that many CTAs; dependent: the kernel may start while the one before it drains.
-static cudaError_t launch_ex(void (*kernel)(StoreAttnLaunch), const StoreAttnLaunch& p, unsigned grid, unsigned threads, size_t smem, int cluster,
-                             bool dependent, cudaStream_t s) {
+template <typename... A>
+static cudaError_t launch_ex(void (*kernel)(A...), unsigned grid, unsigned threads, size_t smem, int cluster, bool dependent, cudaStream_t s,
+                             const A&... args) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(grid);
     cfg.blockDim = dim3(threads);
@@ -795,33 +768,34 @@ static cudaError_t launch_ex(void (*kernel)(StoreAttnLaunch), const StoreAttnLau
     }
     cfg.attrs = attr;
     cfg.numAttrs = (unsigned)n;
-    return cudaLaunchKernelEx(&cfg, kernel, p);
+    return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
-template <int F, int U>
+template <int F>
 static cudaError_t launch_own(const StoreAttnLaunch& p, cudaStream_t s) {
     const unsigned grid = (unsigned)(p.batch * p.h_kv * p.splits);
-    if (store_needs_merge(p)) return launch_ex(gkv_store_attn_kernel<F, U, kPart>, p, grid, kThreads, 0, 1, p.prefix_part != nullptr, s);
-    if (p.splits > 1) return launch_ex(gkv_store_attn_kernel<F, U, kCluster>, p, grid, kThreads, 0, p.splits, false, s);
-    gkv_store_attn_kernel<F, U, kWhole><<<grid, kThreads, 0, s>>>(p);
+    if (store_needs_merge(p)) return launch_ex(gkv_store_attn_kernel<F, kPart>, grid, kThreads, 0, 1, p.prefix_part != nullptr, s, p);
+    if (p.splits > 1) return launch_ex(gkv_store_attn_kernel<F, kCluster>, grid, kThreads, 0, p.splits, false, s, p);
+    gkv_store_attn_kernel<F, kWhole><<<grid, kThreads, 0, s>>>(p);
     return cudaGetLastError();
 }
 bool store_needs_merge(const StoreAttnLaunch& p) { return p.splits > kMaxCluster || p.prefix_part != nullptr || p.len_out != nullptr; }
 cudaError_t launch_store_attn(const StoreAttnLaunch& p, cudaStream_t s) {
     switch (p.format) {
-        case GKV_STORE_BF16: return launch_own<GKV_STORE_BF16, 1>(p, s);
-        case GKV_STORE_E4M3: return launch_own<GKV_STORE_E4M3, 1>(p, s);
-        case GKV_STORE_INT8: return launch_own<GKV_STORE_INT8, 1>(p, s);
-        default:             return launch_own<GKV_STORE_INT4, 2>(p, s);
+        case GKV_STORE_BF16: return launch_own<GKV_STORE_BF16>(p, s);
+        case GKV_STORE_E4M3: return launch_own<GKV_STORE_E4M3>(p, s);
+        case GKV_STORE_INT8: return launch_own<GKV_STORE_INT8>(p, s);
+        default:             return launch_own<GKV_STORE_INT4>(p, s);
     }
 }
-// 256 threads per 8 parts or so, up to 1024. (The plan bounds the parts of a unit: kMaxSplits + 2 kMaxRuns = 448, 8 numbers each are 3.5 per thread.)
+// The fewer units, the more CTAs per unit. 256 threads for up to 8 parts, 512 for up to 16, else 1024. (The plan bounds the parts
+// of a unit: kMaxSplits + 2 kMaxRuns = 448, 8 numbers each are 3.5 per thread.)
 cudaError_t launch_store_merge(const StoreAttnLaunch& p, cudaStream_t s) {
     int longest = 0;
     for (int i = 0; i < p.n_prefix; ++i) longest = p.prefix_len[i] > longest ? p.prefix_len[i] : longest;
     const int items = p.prefix_part ? ((longest + 127) / 128 + p.chunk - 1) / p.chunk * (p.two_tiles ? 1 : 2) : 0;
-    const int parts = p.splits + items;
-    const int slices = parts <= 8 ? 1 : parts <= 16 ? 2 : 4;
-    return launch_ex(gkv_store_merge_kernel, p, (unsigned)(p.batch * p.h_kv), 256u * slices, (size_t)parts * 8 * sizeof(float), 1, true, s);
+    const int parts = p.splits + items, units = p.batch * p.h_kv, ds = units <= 40 ? 2 : units <= 80 ? 1 : 0;
+    return launch_ex(gkv_store_merge_kernel, (unsigned)units << ds, parts <= 8 ? 256u : parts <= 16 ? 512u : 1024u, (size_t)parts * 8 * sizeof(float), 1,
+                     true, s, p, ds);
 }
 
 }  // namespace gkv
