@@ -146,6 +146,21 @@ gkv_prefix_attn_kernel(const StoreAttnLaunch p, const __grid_constant__ CUtensor
     const bool two = p.two_tiles != 0;
     const int ahead = two ? 1 : 2;                       // key tiles whose S is asked for before their turn
 
+    if (warp < kPxTmaWarp) {
+        // Query rows into shared memory, in the layout TMA would give them and before anything else, since they take longest to
+        // come; rows that do not exist are zeros. (r / g by a multiplication: exact for r < 256, g <= 8.)
+        const int inv_g = (65536 + p.g - 1) / p.g;
+        const __nv_bfloat16* q0 = p.q + ((size_t)seq0 * p.h_q + (size_t)head * p.g) * kHeadDim + (tid & 15) * 8;
+        for (int k = 0; k < (two ? 16 : 8); ++k) {
+            const int r = (tid >> 4) + k * (kPxSoftmax / 16), c = tid & 15, rr = min(r, rows - 1), sq = rr * inv_g >> 16;
+            cp_async_16_or_zeros(smem_u32(q_smem + (r >> 7) * kPxSlotBytes + (c >> 3) * kPxHalf + (r & 127) * 128 + (((c & 7) ^ (r & 7)) << 4)),
+                                 q0 + ((size_t)sq * p.h_q + (rr - sq * p.g)) * kHeadDim, r < rows);
+        }
+        cp_async_commit();
+    } else if (warp == kPxTmaWarp && elect_one()) {
+        prefetch_tensormap(&tm_k);
+        prefetch_tensormap(&tm_v);
+    }
     if (tid == 0) {
         mbar_init(smem_u32(&tail->q_full), kPxSoftmax);
         for (int s = 0; s < kPxSlots; ++s) { mbar_init(smem_u32(&tail->full[s]), 1); mbar_init(smem_u32(&tail->empty[s]), 1); }
@@ -281,14 +296,7 @@ gkv_prefix_attn_kernel(const StoreAttnLaunch p, const __grid_constant__ CUtensor
         } else {
             // -------------------------------------------------------------- softmax
             if (pass == 0) {
-                // query rows into shared memory in the layout TMA would give them; rows that do not exist are zeros
-                for (int k = 0; k < (two ? 16 : 8); ++k) {
-                    const int i = tid + k * kPxSoftmax, r = i >> 4, c = i & 15, rr = min(r, rows - 1), sq = rr / p.g;
-                    cp_async_16_or_zeros(smem_u32(q_smem + (r >> 7) * kPxSlotBytes + (c >> 3) * kPxHalf + (r & 127) * 128 + (((c & 7) ^ (r & 7)) << 4)),
-                                         p.q + ((size_t)(seq0 + sq) * p.h_q + (size_t)head * p.g + (rr - sq * p.g)) * kHeadDim + c * 8, r < rows);
-                }
-                cp_async_commit();
-                cp_async_wait_all();
+                cp_async_wait_all();                     // this thread's share of the query rows
                 fence_proxy_async_smem();
                 mbar_arrive(smem_u32(&tail->q_full));
             }

@@ -12,7 +12,7 @@ namespace {
 constexpr int kMaxStoreCapacity = 1 << 24;
 constexpr int kMaxStoreBatch = 65535;      // a grid dimension
 constexpr int kTileKeysOwn = 16;           // keys of a tile of the attention over own rows
-constexpr int64_t kSplitUnits = 2048;      // pieces beyond one per unit are at most this many (sizes the workspace)
+constexpr int64_t kSplitUnits = 2048;      // a launch that cuts units into pieces has at most this many (sizes the workspace)
 constexpr int kMaxSplits = 128;            // pieces of a unit
 constexpr int kMaxRuns = 160;              // runs of a prefix
 constexpr int kPrefixSplitItems = 296;     // prefix items beyond one per row block are at most this many
@@ -54,8 +54,13 @@ int64_t prefix_items(const StoreAttnLaunch& p, int chunk) {
     return items * p.h_kv * p.n_blocks;
 }
 
-// Upper bound over all lengths, without a device.
-uint64_t own_part_bytes(const gkv_store* s) { return align_up(((uint64_t)s->batch * s->n_kv_heads + kSplitUnits) * kOwnRecFloats * 4); }
+// Upper bounds over all lengths, without a device. Partial results of own rows: of every unit when they are merged with
+// something else, and of the pieces of cut units.
+uint64_t own_part_bytes(const gkv_store* s, bool merged) {
+    const uint64_t units = (uint64_t)s->batch * s->n_kv_heads;
+    const uint64_t pieces = units * kMaxSplits < (uint64_t)kSplitUnits ? units * kMaxSplits : (uint64_t)kSplitUnits;
+    return align_up((pieces > units || !merged ? pieces : units) * kOwnRecFloats * 4);
+}
 uint64_t prefix_part_bytes(const gkv_store* s, int n_prefix, int rows) {
     if (n_prefix == 0 || rows == 0) return 0;
     int per_block, blocks, two;
@@ -101,7 +106,7 @@ gkv_status run_attn(StoreAttnLaunch& p, const gkv_store* shape, const gkv_prefix
             longest = prefix->len[i] > longest ? prefix->len[i] : longest;
         }
     }
-    const uint64_t own = own_part_bytes(shape);
+    const uint64_t own = own_part_bytes(shape, longest > 0 || p.len_out);
     const uint64_t need = own + (longest > 0 ? prefix_part_bytes(shape, p.n_prefix, longest) : 0);
     if (!workspace || misaligned(workspace, 16) || workspace_bytes < need) return GKV_ERR_INVALID_ARG;
     p.own_part = static_cast<float*>(workspace);
@@ -163,6 +168,7 @@ void store_plan(StoreAttnLaunch* p, int max_len, int sm_count) {
     const int64_t most = (tiles + 7) / 8;
     if (splits > most) splits = most;
     if (splits > kMaxSplits) splits = kMaxSplits;
+    if (units * splits > kSplitUnits) splits = kSplitUnits / units;
     if (splits < 1) splits = 1;
     p->split_tiles = (int)((tiles + splits - 1) / splits);
     p->splits = (tiles + p->split_tiles - 1) / p->split_tiles;
@@ -230,7 +236,7 @@ gkv_status gkv_store_attn_workspace(const gkv_store* store, int32_t n_prefix, in
         const uint64_t b = prefix_part_bytes(store, i, prefix_rows);
         most = b > most ? b : most;
     }
-    *bytes = own_part_bytes(store) + most;
+    *bytes = own_part_bytes(store, n_prefix > 0) + most;
     return GKV_OK;
 }
 

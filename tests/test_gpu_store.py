@@ -420,6 +420,11 @@ def test_nan_in_a_prefix_and_in_one_query():
     v[0, 0, 77, 64] = float("nan")
     st.attn(ints([9] * 5), q, out, prefix=gkv.Prefix(k, v, lens))
     assert torch.isnan(out[:, :, 64]).all() and torch.isfinite(out[0, :, :64]).all()
+    v[0, 0, 77, 64] = 0
+    k[0, 0, 200, 3] = float("nan")                    # a key: every row that sees it
+    lse = torch.zeros((5, 4), device=DEV)
+    st.attn(ints([9] * 5), q, out, prefix=gkv.Prefix(k, v, lens), lse=lse)
+    assert torch.isnan(out).all() and torch.isnan(lse).all()
 
 
 # ---------------------------------------------------------------------------------------------- as they are used
@@ -518,3 +523,106 @@ def test_context_with_a_prefix_decodes_and_evicts():
     with pytest.raises(gkv.GKVError) as e:
         fused.decode_attn_prefix(0, q, kn, vn, prefix, out, fused.prefix_workspace(1, m))
     assert e.value.status == gkv.GKV_ERR_STATE
+
+
+@pytest.mark.parametrize("seed", range(24))
+def test_shapes_drawn_at_random(seed):
+    rng = np.random.RandomState(900 + seed)
+    fmt = FORMATS[seed % 4]
+    h_kv = int(rng.choice([1, 2, 3, 8]))
+    g_heads = int(rng.randint(1, 9))
+    n_prefix = int(rng.choice([0, 1, 1, 2, 5]))
+    B = max(1, n_prefix) * int(2 ** rng.uniform(0, 6.5 if n_prefix < 2 else 4))
+    C = int(2 ** rng.uniform(2, 11))
+    append = bool(rng.randint(2))
+    lens = [int(x) for x in rng.randint(-1, C + (0 if append else 1), B)]
+    prefix, rows = None, int(2 ** rng.uniform(0, 11))
+    if n_prefix:
+        plens = [int(x) for x in rng.randint(0, rows + 1, n_prefix)]
+        prefix = prefix_rows(gen(950 + seed), n_prefix, h_kv, rows, plens)
+    seqs = sorted(set(int(x) for x in rng.randint(0, B, 6)) | {0, B - 1})
+    attn_case(fmt, B, h_kv * g_heads, h_kv, C, lens, 990 + seed, append, max_len=int(rng.choice([0, C, max(1, C // 3)])), prefix=prefix,
+              n_prefix=n_prefix, max_prefix=rows, seqs=seqs)
+
+
+def test_two_stores_on_two_streams_at_once():
+    """Stores with workspaces of their own share nothing: what they give together is what each gives alone."""
+    g = gen(51)
+    k, v, lens = prefix_rows(g, 1, 2, 3000, [2900])
+    prefix = gkv.Prefix(k, v, lens)
+    cases = []
+    for i, fmt in enumerate(("int4", "e4m3")):
+        st, _ = filled(fmt, 24, 16, 2, 2000, [1990] * 24, 60 + i, n_prefix=1, max_prefix=3000)
+        cases.append((st, randn(g, 24, 16, 128), torch.empty((24, 16, 128), dtype=torch.bfloat16, device=DEV), torch.cuda.Stream()))
+    length = ints([1990] * 24)
+    alone = []
+    for st, q, out, _ in cases:
+        st.attn(length, q, out, prefix=prefix)
+        alone.append(out.clone())
+        out.zero_()
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for st, q, out, s in cases:
+            with torch.cuda.stream(s):
+                st.attn(length, q, out, prefix=prefix)
+    torch.cuda.synchronize()
+    for (_, _, out, _), want in zip(cases, alone):
+        assert torch.equal(out, want)
+
+
+def test_two_captured_graphs_share_a_workspace():
+    g = gen(52)
+    k, v, lens = prefix_rows(g, 1, 1, 700, [700])
+    st, _ = filled("int8", 6, 8, 1, 900, [800] * 6, 53, n_prefix=1, max_prefix=700)
+    q = randn(g, 6, 8, 128)
+    short, long = ints([7, 0, 100, 3, 50, 1]), ints([800] * 6)
+    outs = [torch.empty((6, 8, 128), dtype=torch.bfloat16, device=DEV) for _ in range(2)]
+    calls = [lambda: st.attn(short, q, outs[0], prefix=gkv.Prefix(k, v, lens)), lambda: st.attn(long, q, outs[1], max_len=800)]
+    want, graphs = [], []
+    for call, out in zip(calls, outs):
+        call()
+        want.append(out.clone())
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            call()
+        graphs.append(graph)
+    for order in ((0, 1), (1, 0), (0, 0, 1, 1, 0)):
+        for out in outs:
+            out.zero_()
+        for i in order:
+            graphs[i].replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(o, w) for o, w in zip(outs, want))
+
+
+def test_calls_refuse_tensors_that_do_not_fit():
+    st = gkv.KVStore("int8", batch=2, h_q=8, h_kv=2, capacity=16, device=DEV)
+    x = torch.zeros((2, 3, 2, 128), dtype=torch.bfloat16, device=DEV)
+    q, out, length = torch.zeros((2, 8, 128), dtype=torch.bfloat16, device=DEV), torch.zeros((2, 8, 128), dtype=torch.bfloat16, device=DEV), ints([3, 3])
+    bad_copies = [
+        lambda: st.write(x.float(), x.float()), lambda: st.write(x[:1], x[:1]), lambda: st.write(x, x[:, :2]), lambda: st.write(x.cpu(), x.cpu()),
+        lambda: st.write(x, x.permute(0, 1, 3, 2).contiguous().permute(0, 1, 3, 2)),                        # elements not next to each other
+        lambda: st.write(x, torch.zeros((2, 2, 3, 128), dtype=torch.bfloat16, device=DEV).transpose(1, 2)),   # strides that differ
+        lambda: st.read(x, x, first=ints([0])), lambda: st.read(x, x, count=torch.zeros(2, device=DEV)), lambda: st.write(None, x),
+    ]
+    kn = torch.zeros((2, 2, 128), dtype=torch.bfloat16, device=DEV)
+    bad_attn = [
+        lambda: st.attn(length.long(), q, out), lambda: st.attn(length.cpu(), q, out), lambda: st.attn(length, q[:, :4], out),
+        lambda: st.attn(length, q.transpose(0, 1).contiguous().transpose(0, 1), out), lambda: st.attn(length, q, out.float()),
+        lambda: st.attn(length, q, out, k_new=kn[:, :1], v_new=kn), lambda: st.attn(length, q, out, lse=torch.zeros((2, 4), device=DEV)),
+        lambda: st.attn(length, q, out, prefix=gkv.Prefix(torch.zeros((1, 3, 8, 128), dtype=torch.bfloat16, device=DEV),
+                                                          torch.zeros((1, 3, 8, 128), dtype=torch.bfloat16, device=DEV), [8])),   # heads
+    ]
+    for call in bad_copies + bad_attn:
+        with pytest.raises(ValueError):
+            call()
+    for call in (lambda: st.attn(length, q, out, k_new=kn), lambda: st.attn(length, q, out, max_len=17), lambda: st.attn(length, q, out, max_len=-1),
+                 lambda: st.write(torch.zeros((2, 3, 2, 132), dtype=torch.bfloat16, device=DEV)[..., :128], torch.zeros((2, 3, 2, 132), dtype=torch.bfloat16, device=DEV)[..., :128]),
+                 lambda: st.attn(length, q, out, prefix=gkv.Prefix(torch.zeros((1, 2, 8, 128), dtype=torch.bfloat16, device=DEV),
+                                                                   torch.zeros((1, 2, 8, 128), dtype=torch.bfloat16, device=DEV), [8]))):   # no workspace for it
+        with pytest.raises(gkv.GKVError) as e:
+            call()
+        assert e.value.status == gkv.GKV_ERR_INVALID_ARG
+    torch.cuda.synchronize()
+    assert (out == 0).all()

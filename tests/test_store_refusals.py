@@ -127,6 +127,19 @@ def test_holder_refuses_tensors_that_do_not_fit():
         gkv.KVStore("int8", batch=1, h_q=9, h_kv=1, capacity=16)
 
 
+def test_the_torch_module_refuses_what_is_not_on_the_device():
+    call, s = gkv._torch_binding(), store()
+    at = ctypes.addressof(s)
+    kv, q, n = torch.zeros((6, 3, 2, 128), dtype=torch.bfloat16), torch.zeros((6, 8, 128), dtype=torch.bfloat16), torch.zeros(6, dtype=torch.int32)
+    for bad in (lambda: call.copy(False, at, 0, kv, kv, None, None), lambda: call.copy(True, at, 0, "k", kv, None, None),
+                lambda: call.attn(at, 0, n, 0, q, None, None, 0, q, None, A, 1 << 40)):
+        with pytest.raises(ValueError):
+            bad()
+    for bad in (lambda: call.copy(False, at), lambda: call.attn(at, 0), lambda: call.bind(1)):
+        with pytest.raises(TypeError):
+            bad()
+
+
 # ------------------------------------------------------------------ the reference itself
 def test_reference_codes_against_torch_and_by_hand():
     rng = np.random.RandomState(5)
