@@ -20,7 +20,8 @@
 //
 // Weights are relative to the maximum of the row's first tile, and stay so: bf16 and fp32 have the range for weights of 2^60 and
 // the relative precision of all sums is the same. There is no pass for the maximum and no rescaling of O. If half a tile's
-// weights do sum up to more than 2^60 in some row, the item is done again, once to find the rows' maxima and once with them.
+// weights do sum up to more than 2^60 in some row, or large weights make a sum of values overflow, or the first tile has no
+// maximum (every logit -infinity), the item is done again, once to find the rows' maxima and once with them.
 //
 // K and V tiles come by TMA through a ring of three 32 KB slots in the order in which the products want them.
 //
@@ -43,6 +44,7 @@ constexpr int kPxHalf = 128 * 128;           // bytes of 128 rows x 64 elements
 constexpr int kPxSlotBytes = 2 * kPxHalf;    // one K or V tile, or one row tile of q
 constexpr int kPxSlots = 3;
 constexpr float kPxLimit = 0x1p60f;          // a row's weights of half a tile may sum up to this
+constexpr float kPxCheck = 0x1p16f;          // from here on (in all) the row's values are looked at
 
 struct __align__(16) PrefixTail {
     uint64_t q_full;
@@ -330,6 +332,7 @@ gkv_prefix_attn_kernel(const StoreAttnLaunch p, const __grid_constant__ CUtensor
                         for (int k = 0; k < 32; ++k) top = fmaxf(top, z[k]);
                     }
                     if (pass == 0) m = top * p.scale_log2;
+                    if (pass == 0 && top == -INFINITY && mine > 1) *(volatile int*)&tail->overflow = 1;   // nothing to be relative to
                 }
                 const float ref = m == -INFINITY ? 0.f : -m;
                 const float2 scale2 = make_float2(p.scale_log2, p.scale_log2), ref2 = make_float2(ref, ref);
@@ -365,6 +368,20 @@ gkv_prefix_attn_kernel(const StoreAttnLaunch p, const __grid_constant__ CUtensor
             if (!ok) tail->abort_flag = 1;
             if (pass == 1) m = top * p.scale_log2;
             if (!tc_wait(smem_u32(&tail->o_full), pass & 1, abort_flag)) ok = false;
+            if (pass == 0 && __any_sync(0xffffffffu, l > kPxCheck)) {
+                // large weights of a row may have carried its values out of fp32's range
+                tmem_fence_after_sync();
+                float bad = 0.f;
+                for (int c = 0; c < 4; ++c) {
+                    float o[32];
+                    tmem_ld32_start(o_addr + 32 * c, o);
+                    tmem_ld_wait(o);
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) bad = fmaf(o[k], 0.f, bad);
+                }
+                if (!(bad == 0.f)) *(volatile int*)&tail->overflow = 1;
+                tmem_fence_before_sync();
+            }
         }
         __syncthreads();
         if (pass == 2 || *(volatile int*)&tail->overflow == 0) break;    // (written in the first pass only)

@@ -31,9 +31,10 @@ constexpr int kThreads = kWarps * 32;
 constexpr int kTile = 16;            // keys of a tile
 constexpr int kMaxCluster = 8;
 constexpr int kMergeHops = 4;
-// How far weights (relative to the running maximum, summed over a warp's lane and step) may go before the maximum is raised:
-// scaled rows by the range of fp16, bf16 ones by what keeps the smaller weights in range as well.
-template <int F> struct LagLimit { static constexpr float value = F == GKV_STORE_BF16 ? 0x1p60f : 256.f; };
+// How far weights (relative to the running maximum, summed over a warp's lane and step) may go before the maximum is raised: the
+// range of fp16 allows no more for scaled rows, and with bf16 ones a larger limit (2^60) would gain nothing and let the sums of
+// values near the end of the range overflow.
+constexpr float kLagLimit = 256.f;
 // state word of a unit's first partial result
 constexpr float kPieceOk = 0.f, kPieceNoFit = 1.f, kPieceLeftOut = 2.f;
 constexpr float kLift = 6.f;         // the weights of scaled rows are lifted by 2^6: at most 2^14, subnormal below 2^-20
@@ -402,7 +403,7 @@ __global__ void __launch_bounds__(kThreads, store_ctas(F)) gkv_store_attn_kernel
 
     float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;       // running maxima (they may lag) and sums, heads h0, h0 + 1
     float v0 = -INFINITY, v1 = -INFINITY;                           // the same maxima of z + log2(scale of V)
-    float n0 = -INFINITY, n1 = -INFINITY;                           // m, or 0 where every logit was -infinity; at first: -infinity
+    float n0 = -INFINITY, n1 = -INFINITY;                           // what logits are taken relative to: m, once that is finite
     float c0 = 1.f, c1 = 1.f;                                       // 2^(m - v + kLift), with finite m and v
     float acc[8][4];
 #pragma unroll
@@ -457,7 +458,7 @@ __global__ void __launch_bounds__(kThreads, store_ctas(F)) gkv_store_attn_kernel
                 total += ((e[0] * c0 + e[1] * c1) * top[0] + (e[2] * c0 + e[3] * c1) * top[1]) * (1.f / kLiftFactor);
         };
         weigh();
-        const bool over = !(total <= LagLimit<F>::value);
+        const bool over = !(total <= kLagLimit);
         if (__any_sync(0xffffffffu, over)) {
             float a0 = m0, a1 = m1, b0 = v0, b1 = v1;
             a0 = fmaxf(a0, fmaxf(z[0], z[2]));
@@ -496,6 +497,7 @@ __global__ void __launch_bounds__(kThreads, store_ctas(F)) gkv_store_attn_kernel
 #pragma unroll
             for (int i = 0; i < 8; ++i) { acc[i][0] *= r0; acc[i][1] *= r1; acc[i][2] *= r0; acc[i][3] *= r1; }
             weigh();
+            n0 = m0; n1 = m1;           // as long as every logit was -infinity, the next step comes here again
         }
         l0 += e[0] + e[2];
         l1 += e[1] + e[3];

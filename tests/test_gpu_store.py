@@ -626,3 +626,110 @@ def test_calls_refuse_tensors_that_do_not_fit():
         assert e.value.status == gkv.GKV_ERR_INVALID_ARG
     torch.cuda.synchronize()
     assert (out == 0).all()
+
+
+def masked_keys(g, q, n, H, spans):
+    """K, V [B][n][H][128] where the keys of a sequence's span have a logit of -infinity (q is made positive in element 0)."""
+    q[..., 0] = q[..., 0].abs() + 0.5
+    k, v = randn(g, len(spans), n, H, 128), randn(g, len(spans), n, H, 128)
+    for i, (a, b) in enumerate(spans):
+        k[i, a:b, :, 0] = float("-inf")
+    return k, v
+
+
+def check_masked(q, out, lse, own, prefix):
+    """own, prefix: per sequence K, V [n][H][128], span (or None). A key of weight 0 is a key that is not there."""
+    g = q.shape[1] // own[0][0].shape[1]
+    for b, (k, v, (x, y)) in enumerate(own):
+        for h in range(k.shape[1]):
+            keep = [i for i in range(len(k)) if not x <= i < y]
+            kp = vp = None
+            if prefix is not None:
+                pk, pv, (s, e) = prefix[b]
+                there = [i for i in range(len(pk)) if not s <= i < e]
+                kp, vp = f64(pk[there, h]), f64(pv[there, h])
+            hs = slice(h * g, (h + 1) * g)
+            want, wl, tol, ltol = ref.attend(f64(q[b, hs]), f64(k[keep, h]), f64(v[keep, h]), kp, vp, ref.U_BF16)
+            assert (np.abs(f64(out[b, hs]) - want) <= tol).all(), (b, h)
+            if np.isinf(wl).any():
+                assert (f64(lse[b, hs]) == wl).all()
+            else:
+                assert (np.abs(f64(lse[b, hs]) - wl) <= ltol).all(), (b, h)
+
+
+@pytest.mark.parametrize("batch", [5, 200])      # units cut into pieces and whole ones
+def test_own_keys_with_a_logit_of_minus_infinity(batch):
+    n, H = 200, 2
+    g = gen(61)
+    q = randn(g, batch, 8, 128)
+    spans = [(0, 100), (30, 150), (100, 200), (0, 200), (0, 199)] + [(0, 0)] * (batch - 5)
+    k, v = masked_keys(g, q, n, H, spans)
+    st = gkv.KVStore("bf16", batch=batch, h_q=8, h_kv=H, capacity=n, device=DEV)
+    st.write(k, v)
+    out, lse = torch.empty((batch, 8, 128), dtype=torch.bfloat16, device=DEV), torch.empty((batch, 8), device=DEV)
+    st.attn(ints([n] * batch), q, out, lse=lse)
+    check_masked(q[:5], out[:5], lse[:5], [(k[i], v[i], spans[i]) for i in range(5)], None)
+
+
+@pytest.mark.parametrize("seqs", [3, 16, 32])    # rows of a tile that do not exist; the streams of an item share their rows; or not
+@pytest.mark.parametrize("m,H,span", [(700, 1, (0, 130)), (700, 1, (0, 300)), (700, 1, (0, 699)), (700, 1, (0, 700)), (700, 1, (200, 500)),
+                                      (5000, 16, (0, 700)), (5000, 16, (600, 3333)), (5000, 16, (0, 4999))])   # runs of several tiles
+def test_prefix_keys_with_a_logit_of_minus_infinity(seqs, m, H, span):
+    g = gen(62)
+    q = randn(g, seqs, 8 * H, 128)
+    pk, pv = masked_keys(g, q, m, H, [span])
+    own = randn(g, 2, seqs, 3, H, 128)
+    st = gkv.KVStore("bf16", batch=seqs, h_q=8 * H, h_kv=H, capacity=3, device=DEV, n_prefix=1, max_prefix=m)
+    st.write(own[0], own[1])
+    some = [0, seqs - 1]
+    for n in (3, 0):                             # with rows of their own and without
+        out, lse = torch.empty((seqs, 8 * H, 128), dtype=torch.bfloat16, device=DEV), torch.empty((seqs, 8 * H), device=DEV)
+        prefix = gkv.Prefix(pk.transpose(1, 2).contiguous(), pv.transpose(1, 2).contiguous(), [m])
+        st.attn(ints([n] * seqs), q, out, prefix=prefix, lse=lse)
+        check_masked(q[some], out[some], lse[some], [(own[0, i, :n], own[1, i, :n], (0, 0)) for i in some], [(pk[0], pv[0], span)] * 2)
+
+
+@pytest.mark.parametrize("where", ["own", "prefix"])
+@pytest.mark.parametrize("seqs", [16, 32])
+def test_values_near_the_end_of_the_range_under_rising_logits(where, seqs):
+    """V of 2^90 and logits that go from -18 to 18 (52 in log2 units) and back every other tile of 128: outputs are finite, so all
+    sums have to be."""
+    m, H = (5000, 16) if where == "prefix" else (700, 1)
+    g = gen(63)
+    q = randn(g, 1, 1, 128).expand(seqs, 8 * H, 128).contiguous()
+    unit = q[0, 0].float() / q[0, 0].float().square().sum() * 128 ** 0.5
+    k = (unit * (torch.arange(m, device=DEV) // 256 % 2 * 36 - 18)[:, None]).to(torch.bfloat16).view(1, m, 1, 128).expand(1, m, H, 128)
+    v = (randn(g, 1, m, H, 128).float() * 2.0 ** 90).to(torch.bfloat16)
+    out, lse = torch.empty((seqs, 8 * H, 128), dtype=torch.bfloat16, device=DEV), torch.empty((seqs, 8 * H), device=DEV)
+    st = gkv.KVStore("bf16", batch=seqs, h_q=8 * H, h_kv=H, capacity=m, device=DEV, n_prefix=1, max_prefix=m)
+    if where == "own":
+        seqs, out, lse = 16 * seqs, out.repeat(16, 1, 1), lse.repeat(16, 1)      # units whole
+        q = q.repeat(16, 1, 1)
+        st = gkv.KVStore("bf16", batch=seqs, h_q=8, h_kv=1, capacity=m, device=DEV)
+        k, v = (t.expand(seqs, m, H, 128).contiguous() for t in (k, v))
+        st.write(k, v)
+        st.attn(ints([m] * seqs), q, out, lse=lse)
+        check(st, [m] * seqs, q, out, lse, seqs=[0, seqs - 1])
+    else:
+        prefix = (k.transpose(1, 2).contiguous(), v.transpose(1, 2).contiguous(), [m])
+        st.attn(ints([0] * seqs), q, out, prefix=gkv.Prefix(*prefix), lse=lse)
+        check(st, [0] * seqs, q, out, lse, prefix=prefix, seqs=[0])
+    assert torch.isfinite(out).all()
+
+
+def test_as_many_prefixes_as_there_may_be():
+    B, H, rows = 128, 1, 140
+    g = gen(64)
+    lens = [(37 * i) % (rows + 1) for i in range(64)]
+    prefix = prefix_rows(g, 64, H, rows, lens)
+    attn_case("e4m3", B, 4, H, 9, [i % 9 for i in range(B)], 65, True, prefix=prefix, n_prefix=64, max_prefix=rows)
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "int4"])
+def test_the_largest_batch(fmt):
+    B = 65535
+    g = gen(66)
+    lens = [i % 5 for i in range(B)]
+    prefix = prefix_rows(g, 1, 1, 130, [130])
+    attn_case(fmt, B, 1, 1, 5, lens, 67, True, seqs=[0, 1, 4, 255, 256, 32767, 32768, 65533, 65534])
+    attn_case(fmt, B, 1, 1, 5, lens, 67, True, prefix=prefix, n_prefix=1, max_prefix=130, seqs=[0, 1, 4, 255, 256, 32767, 32768, 65533, 65534])
