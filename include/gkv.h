@@ -352,8 +352,10 @@ gkv_status gkv_store_write(const gkv_store* store, const void* k, const void* v,
                            int64_t head_stride, const int32_t* first, const int32_t* count, int32_t n_tokens, void* stream);
 
 /* Read back: token t of k and v of sequence i becomes bf16(c * s) of row first[i] + t, for t < count[i]; arguments as
- * gkv_store_write with k, v written (two (i, t, h) may not share an address). Tokens from count[i] on, and those whose row
- * is outside the store, are left as they were. Errors: as gkv_store_write. */
+ * gkv_store_write with k, v written. Tokens from count[i] on, and those whose row is outside the store, are left as they
+ * were. Errors: as gkv_store_write; INVALID_ARG also for k = v and for strides with which rows overlap or interleave: in
+ * rising order (those of sizes of 1 left out), the first must be >= 128 and each other one >= the one before times its
+ * size. */
 gkv_status gkv_store_read(const gkv_store* store, void* k, void* v, int64_t seq_stride, int64_t token_stride,
                           int64_t head_stride, const int32_t* first, const int32_t* count, int32_t n_tokens, void* stream);
 

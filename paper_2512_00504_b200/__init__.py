@@ -536,7 +536,7 @@ class KVStore:
         _check(self._call.copy(False, at, dev, k, v, first, count), "gkv_store_write")
 
     def read(self, k, v, first=None, count=None):
-        """Read the same rows back as bf16 into k and v; tokens from count[i] on are left as they were."""
+        """Read the same rows back as bf16 into k and v, whose rows may not overlap; tokens from count[i] on are left as they were."""
         at, dev = self._at
         _check(self._call.copy(True, at, dev, k, v, first, count), "gkv_store_read")
 

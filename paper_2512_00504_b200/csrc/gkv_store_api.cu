@@ -1,6 +1,7 @@
 // C-ABI entry points of the key/value stores and shared prefixes: argument checks, the plan of an attention launch and the
 // launches themselves. Nothing here keeps state between calls.
 #include <math.h>
+#include <stdint.h>
 
 #include "gkv_common.cuh"
 #include "gkv_internal.h"
@@ -83,6 +84,22 @@ gkv_status check_prefix(const gkv_prefix* x, int batch, int h_kv) {
     return GKV_OK;
 }
 
+// Whether elements of an array of rows of 128 share an address (or may, with strides that no slice of an array has).
+bool rows_overlap(int64_t n0, int64_t s0, int64_t n1, int64_t s1, int64_t n2, int64_t s2) {
+    int64_t n[3] = {n0, n1, n2}, s[3] = {s0, s1, s2};
+    int64_t least = kHeadDim;                  // the next larger stride has to step over what the smaller ones span
+    for (int k = 0; k < 3; ++k) {
+        int next = -1;
+        for (int i = 0; i < 3; ++i)
+            if (n[i] > 1 && (next < 0 || s[i] < s[next])) next = i;
+        if (next < 0) break;
+        if (s[next] < least || s[next] > INT64_MAX / n[next]) return true;
+        least = s[next] * n[next];
+        n[next] = 1;
+    }
+    return false;
+}
+
 int device_sm_count() {
     int dev = 0, sm = 0;
     if (cudaGetDevice(&dev) == cudaSuccess) cudaDeviceGetAttribute(&sm, cudaDevAttrMultiProcessorCount, dev);
@@ -132,13 +149,15 @@ gkv_status run_attn(StoreAttnLaunch& p, const gkv_store* shape, const gkv_prefix
 }
 
 gkv_status copy_args(const gkv_store* store, const void* k, const void* v, int64_t seq_stride, int64_t token_stride, int64_t head_stride,
-                     const int32_t* first, const int32_t* count, int32_t n_tokens, StoreCopyLaunch* p) {
+                     const int32_t* first, const int32_t* count, int32_t n_tokens, bool read, StoreCopyLaunch* p) {
     const gkv_status st = check_store(store);
     if (st != GKV_OK) return st;
     if (n_tokens < 0 || (n_tokens > 0 && (!k || !v)) || misaligned(k, 16) || misaligned(v, 16)) return GKV_ERR_INVALID_ARG;
     if (misaligned(first, 4) || misaligned(count, 4)) return GKV_ERR_INVALID_ARG;
     if (seq_stride < 0 || token_stride < 0 || head_stride < 0 || ((seq_stride | token_stride | head_stride) & 7) != 0) return GKV_ERR_INVALID_ARG;
     if ((int64_t)n_tokens * store->n_kv_heads >= (1ll << 30)) return GKV_ERR_UNSUPPORTED;
+    if (read && n_tokens > 0 && k == v) return GKV_ERR_INVALID_ARG;
+    if (read && rows_overlap(store->batch, seq_stride, n_tokens, token_stride, store->n_kv_heads, head_stride)) return GKV_ERR_INVALID_ARG;
     p->data[0] = static_cast<uint8_t*>(store->k); p->data[1] = static_cast<uint8_t*>(store->v);
     p->scale[0] = static_cast<__nv_bfloat16*>(store->k_scale); p->scale[1] = static_cast<__nv_bfloat16*>(store->v_scale);
     p->x[0] = static_cast<__nv_bfloat16*>(const_cast<void*>(k)); p->x[1] = static_cast<__nv_bfloat16*>(const_cast<void*>(v));
@@ -210,7 +229,7 @@ gkv_status gkv_store_query_sizes(const gkv_store* store, gkv_store_sizes* out) {
 gkv_status gkv_store_write(const gkv_store* store, const void* k, const void* v, int64_t seq_stride, int64_t token_stride,
                            int64_t head_stride, const int32_t* first, const int32_t* count, int32_t n_tokens, void* stream) {
     StoreCopyLaunch p;
-    const gkv_status st = copy_args(store, k, v, seq_stride, token_stride, head_stride, first, count, n_tokens, &p);
+    const gkv_status st = copy_args(store, k, v, seq_stride, token_stride, head_stride, first, count, n_tokens, false, &p);
     if (st != GKV_OK || n_tokens == 0) return st;
     if (launch_store_write(p, static_cast<cudaStream_t>(stream)) != cudaSuccess) { (void)cudaGetLastError(); return GKV_ERR_CUDA; }
     return GKV_OK;
@@ -219,7 +238,7 @@ gkv_status gkv_store_write(const gkv_store* store, const void* k, const void* v,
 gkv_status gkv_store_read(const gkv_store* store, void* k, void* v, int64_t seq_stride, int64_t token_stride, int64_t head_stride,
                           const int32_t* first, const int32_t* count, int32_t n_tokens, void* stream) {
     StoreCopyLaunch p;
-    const gkv_status st = copy_args(store, k, v, seq_stride, token_stride, head_stride, first, count, n_tokens, &p);
+    const gkv_status st = copy_args(store, k, v, seq_stride, token_stride, head_stride, first, count, n_tokens, true, &p);
     if (st != GKV_OK || n_tokens == 0) return st;
     if (launch_store_read(p, static_cast<cudaStream_t>(stream)) != cudaSuccess) { (void)cudaGetLastError(); return GKV_ERR_CUDA; }
     return GKV_OK;

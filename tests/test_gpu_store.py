@@ -733,3 +733,26 @@ def test_the_largest_batch(fmt):
     prefix = prefix_rows(g, 1, 1, 130, [130])
     attn_case(fmt, B, 1, 1, 5, lens, 67, True, seqs=[0, 1, 4, 255, 256, 32767, 32768, 65533, 65534])
     attn_case(fmt, B, 1, 1, 5, lens, 67, True, prefix=prefix, n_prefix=1, max_prefix=130, seqs=[0, 1, 4, 255, 256, 32767, 32768, 65533, 65534])
+
+
+@pytest.mark.parametrize("view", ["heads first", "tokens last", "every other token", "one token", "one head"])
+def test_read_into_views(view):
+    B, T, H = (3, 1, 2) if view == "one token" else (3, 10, 1) if view == "one head" else (3, 10, 2)
+    st, _ = filled("int8", B, 4, H, 12, [T] * B, 68)
+    want = dequantised(st)
+    def target():
+        if view == "heads first":
+            return torch.zeros((B, H, T, 128), dtype=torch.bfloat16, device=DEV).transpose(1, 2)
+        if view == "tokens last":
+            return torch.zeros((T, H, B, 128), dtype=torch.bfloat16, device=DEV).permute(2, 0, 1, 3)
+        if view == "every other token":
+            return torch.zeros((B, 2 * T, H, 128), dtype=torch.bfloat16, device=DEV)[:, ::2]
+        return torch.zeros((B, T, H, 128), dtype=torch.bfloat16, device=DEV)
+    k, v = target(), target()
+    st.read(k, v)
+    for x, y in zip((k, v), want):
+        assert (f64(x) == ref.round_bf16(y[:, :, :T].transpose(0, 2, 1, 3))).all()
+    if T > 1:
+        one = torch.zeros((B, 1, H, 128), dtype=torch.bfloat16, device=DEV)
+        with pytest.raises(gkv.GKVError):
+            st.read(one.expand(B, T, H, 128), one.expand(B, T, H, 128))

@@ -83,6 +83,19 @@ def test_write_and_read_arguments(read, kw, status):
     assert call_write(store(), read=read, **kw) == status
 
 
+@pytest.mark.parametrize("shape,n,strides", [
+    (dict(), 4, (0, 256, 128)), (dict(), 4, (4096, 0, 128)), (dict(), 4, (4096, 256, 0)), (dict(), 4, (4096, 256, 120)),
+    (dict(), 4, (4096, 248, 128)), (dict(), 4, (1016, 256, 128)), (dict(), 4, (256, 256, 128)), (dict(), 4, (2 ** 62, 2 ** 61, 128)),
+    (dict(batch=1), 2, (0, 128, 128)), (dict(batch=1, n_kv_heads=1, n_q_heads=1), 2, (0, 0, 0)),
+])
+def test_read_refuses_a_target_whose_rows_overlap(shape, n, strides):
+    assert call_write(store(**shape), v=2 * A, strides=strides, n=n, read=True) == BAD
+
+
+def test_read_refuses_one_target_for_both():
+    assert call_write(store(), n=1, read=True) == BAD
+
+
 @pytest.mark.parametrize("kw,status", [
     (dict(length=0), BAD), (dict(q=0), BAD), (dict(out=0), BAD), (dict(q=A + 8), BAD), (dict(out=A + 8), BAD), (dict(length=A + 2), BAD),
     (dict(lse=A + 2), BAD), (dict(k_new=A), BAD), (dict(v_new=A), BAD), (dict(k_new=A + 8, v_new=A), BAD), (dict(k_new=A, v_new=A + 8), BAD),
