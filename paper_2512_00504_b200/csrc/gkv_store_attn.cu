@@ -22,6 +22,12 @@
 //
 // The pieces of a unit are joined by the CTAs of a cluster reading one another's shared memory (up to 8 pieces, no prefix), or
 // leave partial results in the workspace for the merge kernel.
+//
+// Bound by HBM for 8-bit rows in a large batch (128 sequences x 8 heads of about 2200 keys, 585 MB: 97 us, 6.0 TB/s). 4-bit rows
+// bring twice the elements per byte to unpack: 2 x 8 heads of about 120000 keys, 274 MB in 77 us, 3.6 TB/s, with the schedulers
+// issuing 6 cycles out of 10, the logic and fp32 pipes 4 to 5 (without the products and what feeds them the same loads take 55
+// us). A single sequence of 640 keys takes 6.7 us: the launch, three trips to memory (length, rows, the others' results), 3 tiles
+// per warp.
 #include "gkv_store_codes.cuh"
 
 namespace gkv {
@@ -61,6 +67,16 @@ __device__ __forceinline__ uint32_t ld2(const void* a) {
 __device__ __forceinline__ void mma_f16_16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// The same with zeros for C, which takes no registers and no moves.
+template <int F>
+__device__ __forceinline__ void mma_row_first(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    if (F == GKV_STORE_BF16)
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+                     : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
+    else
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+                     : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
 }
 template <int F>
 __device__ __forceinline__ void mma_row(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
@@ -103,13 +119,14 @@ __device__ __forceinline__ void unpack8(uint32_t w, uint32_t& lo, uint32_t& hi) 
     }
 }
 // Two bytes of nibbles under the exponent of 1024, x = 1024 + u0 + 16 u1 in both halves (u = c + 8) -> the fp16 pairs c0 and c1,
-// exactly: without its low nibble x is y = 1024 + 16 u1, so c1 = y / 16 - 72 and c0 = (x - 16 c1) - 1160. One instruction for
-// the logic unit, which these kernels keep busiest, and three for the half-precision pipe. (Leaving the offset 8 in and taking it
+// exactly: without its low nibble x is y = 1024 + 16 u1, so c1 = y / 16 - 72; without the high one it is 1024 + u0. Two
+// instructions for the logic unit and two for the fp32 and half-precision pipe, which are about equally busy then (c0 as
+// (x - 16 c1) - 1160 puts three on the latter: 131071 keys take 80 us instead of 78). (Leaving the offset 8 in and taking it
 // off the sums would save the latter, but costs precision: as 1024 + u in the fp32 sums, as subnormals u 2^-24 where the
 // products are aligned.)
 __device__ __forceinline__ void unpack4(uint32_t x, uint32_t& c0, uint32_t& c1) {
     c1 = hfma2(x & 0xfff0fff0u, 0x2c002c00u, 0xd480d480u);
-    c0 = hsub2(hfma2(c1, 0xcc00cc00u, x), 0x64886488u);
+    c0 = hsub2(x & 0xff0fff0fu, 0x64086408u);
 }
 
 // Registers of one 16-key tile. K: this lane's pieces of rows r = lane / 4 and r + 8. V: its pieces of keys 2j, 2j + 1, 2j + 8,
@@ -199,10 +216,9 @@ __device__ __forceinline__ void load_tile_v(TileV<F>& t, const TilePtrs<F>& p, i
 template <int F>
 __device__ __forceinline__ void tile_logits(const TileK<F>& t, const uint32_t (&qf)[8][2], float f0, float f1, float (&z)[4]) {
     if constexpr (F == GKV_STORE_INT4) {
-        z[0] = z[1] = z[2] = z[3] = 0.f;
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
-            float acc[4] = {0.f, 0.f, 0.f, 0.f};
+            float acc[4];
 #pragma unroll
             for (int k = 0; k < 2; ++k) {       // the 16-bit words 2j and 2j + 1 of the group: elements 0, 2 and 1, 3 of each
                 uint32_t a[4];
@@ -212,16 +228,17 @@ __device__ __forceinline__ void tile_logits(const TileK<F>& t, const uint32_t (&
                     const uint32_t w = k == 0 ? (g < 2 ? d.x : d.y) : (g < 2 ? d.z : d.w);
                     unpack4(__byte_perm(w, 0x64646464u, (g & 1) ? 0x4342 : 0x4140), a[hf], a[hf + 2]);
                 }
-                mma_row<F>(acc, a, qf[2 * g + k][0], qf[2 * g + k][1]);
+                if (k == 0) mma_row_first<F>(acc, a, qf[2 * g + k][0], qf[2 * g + k][1]);
+                else mma_row<F>(acc, a, qf[2 * g + k][0], qf[2 * g + k][1]);
             }
             const uint32_t w0 = g < 2 ? t.s[0].x : t.s[0].y, w1 = g < 2 ? t.s[1].x : t.s[1].y;
             const float s0 = (g & 1) ? bf16_hi(w0) : bf16_lo(w0), s1 = (g & 1) ? bf16_hi(w1) : bf16_lo(w1);
-            z[0] = fmaf(acc[0], s0, z[0]); z[1] = fmaf(acc[1], s0, z[1]);
-            z[2] = fmaf(acc[2], s1, z[2]); z[3] = fmaf(acc[3], s1, z[3]);
+            z[0] = g == 0 ? acc[0] * s0 : fmaf(acc[0], s0, z[0]); z[1] = g == 0 ? acc[1] * s0 : fmaf(acc[1], s0, z[1]);
+            z[2] = g == 0 ? acc[2] * s1 : fmaf(acc[2], s1, z[2]); z[3] = g == 0 ? acc[3] * s1 : fmaf(acc[3], s1, z[3]);
         }
         z[0] *= f0; z[1] *= f1; z[2] *= f0; z[3] *= f1;
     } else {
-        float sa[4] = {0.f, 0.f, 0.f, 0.f}, sb[4] = {0.f, 0.f, 0.f, 0.f};   // two accumulators: half the dependent chain
+        float sa[4], sb[4];   // two accumulators: half the dependent chain
 #pragma unroll
         for (int ks = 0; ks < 8; ++ks) {
             uint32_t a[4];
@@ -235,7 +252,8 @@ __device__ __forceinline__ void tile_logits(const TileK<F>& t, const uint32_t (&
                 unpack8<F>(i == 0 ? u.x : i == 1 ? u.y : i == 2 ? u.z : u.w, a[0], a[2]);
                 unpack8<F>(i == 0 ? w.x : i == 1 ? w.y : i == 2 ? w.z : w.w, a[1], a[3]);
             }
-            mma_row<F>((ks & 1) ? sb : sa, a, qf[ks][0], qf[ks][1]);
+            if (ks < 2) mma_row_first<F>((ks & 1) ? sb : sa, a, qf[ks][0], qf[ks][1]);
+            else mma_row<F>((ks & 1) ? sb : sa, a, qf[ks][0], qf[ks][1]);
         }
         float e0 = f0, e1 = f1, e2 = f0, e3 = f1;
         if constexpr (F != GKV_STORE_BF16) {
@@ -321,10 +339,10 @@ __device__ __forceinline__ float final_lse(float m, float l, bool fits) {
     return !fits ? NAN : m == -INFINITY && l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
 }
 
-// Resident CTAs per SM. 8-bit rows: 128 registers, 16 warps (the 32B batch of the benchmark shapes: 97 us; two tiles per step, 168
-// registers and 12 warps: 110 us). bf16 rows need twice the registers for a tile; 4-bit ones are slower at 128 registers (131071
-// keys: 83 us against 81, with two tiles per step 85).
-__host__ __device__ constexpr int store_ctas(int format) { return format == GKV_STORE_BF16 || format == GKV_STORE_INT4 ? 3 : 4; }
+// Resident CTAs per SM. 8- and 4-bit rows: 128 registers, 16 warps (128 sequences x 8 heads of about 2200 keys in 8 bits: 97 us;
+// two tiles per step, 168 registers and 12 warps: 110 us. 2 x 8 heads of up to 131071 keys in 4 bits: 77 us; 12 warps: 78, with
+// two tiles per step 85). bf16 rows need twice the registers for a tile.
+__host__ __device__ constexpr int store_ctas(int format) { return format == GKV_STORE_BF16 ? 3 : 4; }
 int store_attn_ctas_per_sm(int format) { return store_ctas(format); }
 
 // What becomes of a CTA's result: it is the unit's; it goes to the workspace; it is joined with those of the cluster's other CTAs.
