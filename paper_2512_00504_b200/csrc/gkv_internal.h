@@ -128,6 +128,8 @@ struct ScoreLaunch {
 };
 
 // ---- key/value stores and shared prefixes
+constexpr int kMaxCluster = 8;            // pieces of a unit that are joined in a cluster
+constexpr int kMaxPieces = 128;           // pieces of a unit of the attention over own rows
 constexpr int kMaxPrefixes = 64;
 constexpr int kOwnRecFloats = 32 + kHeadDimHost * 8;            // partial result of one unit's split: M[8], L[8], Mv[8], pad, O[32][8][4]
 constexpr int kPrefixRows = 256;                                // query rows of a prefix work item
@@ -155,6 +157,7 @@ struct StoreAttnLaunch {
     float* prefix_part;        // [prefix items][kPrefixRecFloats], or NULL without a prefix
     int format, batch, h_q, h_kv, g, capacity;
     int splits, split_tiles;   // pieces of a unit and 16-key tiles of a piece (the last piece takes what is left)
+    int dealt;               // the pieces are dealt out by the lengths instead: batch * splits per head over all sequences
     float scale_log2;
     // shared prefixes
     const __nv_bfloat16 *k_prefix, *v_prefix;

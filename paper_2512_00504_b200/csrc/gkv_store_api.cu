@@ -13,8 +13,8 @@ namespace {
 constexpr int kMaxStoreCapacity = 1 << 24;
 constexpr int kMaxStoreBatch = 65535;      // a grid dimension
 constexpr int kTileKeysOwn = 16;           // keys of a tile of the attention over own rows
+constexpr int kDealPiece = 128, kDealUnit = 512;   // tiles from which on pieces, and whole units, are dealt out by the lengths
 constexpr int64_t kSplitUnits = 2048;      // a launch that cuts units into pieces has at most this many (sizes the workspace)
-constexpr int kMaxSplits = 128;            // pieces of a unit
 constexpr int kMaxRuns = 160;              // runs of a prefix
 constexpr int kPrefixSplitItems = 296;     // prefix items beyond one per row block are at most this many
 
@@ -59,7 +59,7 @@ int64_t prefix_items(const StoreAttnLaunch& p, int chunk) {
 // something else, and of the pieces of cut units.
 uint64_t own_part_bytes(const gkv_store* s, bool merged) {
     const uint64_t units = (uint64_t)s->batch * s->n_kv_heads;
-    const uint64_t pieces = units * kMaxSplits < (uint64_t)kSplitUnits ? units * kMaxSplits : (uint64_t)kSplitUnits;
+    const uint64_t pieces = units * kMaxPieces < (uint64_t)kSplitUnits ? units * kMaxPieces : (uint64_t)kSplitUnits;
     return align_up((pieces > units || !merged ? pieces : units) * kOwnRecFloats * 4);
 }
 uint64_t prefix_part_bytes(const gkv_store* s, int n_prefix, int rows) {
@@ -173,7 +173,11 @@ namespace gkv {
 
 // Own rows: as many pieces per unit as fill the places of resident CTAs, none below 8 tiles (two turns of the four warps). (With
 // more units than half the places units go whole: cutting 1024 units into thirds, to fill the last round of CTAs better, took 157
-// us as clusters and 105 us by way of the workspace where whole units take 110 us.)
+// us as clusters and 105 us by way of the workspace where whole units take 110 us.) With long
+// rows the pieces are dealt out by the lengths that the sequences really have (store_piece_tiles), by way of the workspace, which
+// costs a merge of 4 us when all are equally long and saves more the more they differ (32 sequences x 4 heads of 8192 keys in 8
+// bits: 49 us as clusters, 53 dealt out; of 256 to 8192 keys: 43, 36; one of 8192 and 31 of 512: 36, 20. 128 x 8 heads, one of
+// 65536 and 127 of 2048 keys: 963 us as whole units, 168; all of 8192 keys: 352, 378).
 // Prefixes: the length of the runs that the prefixes' key tiles are cut into. An item occupies an SM for about 8 us + 1.05 us a
 // tile (2.1 with more than 128 query rows); the attention over own rows (at 5.5 TB/s, with sequences three quarters of the
 // longest on average) takes the SMs that are left and, in part, the same ones; every run leaves a partial result that is written
@@ -186,9 +190,17 @@ void store_plan(StoreAttnLaunch* p, int max_len, int sm_count) {
     int64_t splits = places / units;
     const int64_t most = (tiles + 7) / 8;
     if (splits > most) splits = most;
-    if (splits > kMaxSplits) splits = kMaxSplits;
+    if (splits > kMaxPieces) splits = kMaxPieces;
     if (units * splits > kSplitUnits) splits = kSplitUnits / units;
     if (splits < 1) splits = 1;
+    p->dealt = 0;
+    if (p->batch > 1 && !p->prefix_part && !p->len_out) {
+        if (tiles / splits >= (splits > 1 ? kDealPiece : kDealUnit) && units * 2 <= kSplitUnits) {
+            p->dealt = 1;
+            if (splits < 2) splits = 2;
+        }
+        if (splits > kMaxCluster) p->dealt = 1;
+    }
     p->split_tiles = (int)((tiles + splits - 1) / splits);
     p->splits = (tiles + p->split_tiles - 1) / p->split_tiles;
     if (!p->prefix_part) return;

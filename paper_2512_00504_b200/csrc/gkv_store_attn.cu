@@ -35,7 +35,6 @@ namespace gkv {
 constexpr int kWarps = 4;
 constexpr int kThreads = kWarps * 32;
 constexpr int kTile = 16;            // keys of a tile
-constexpr int kMaxCluster = 8;
 constexpr int kMergeHops = 4;
 // How far weights (relative to the running maximum, summed over a warp's lane and step) may go before the maximum is raised: the
 // range of fp16 allows no more for scaled rows, and with bf16 ones a larger limit (2^60) would gain nothing and let the sums of
@@ -345,10 +344,43 @@ __device__ __forceinline__ float final_lse(float m, float l, bool fits) {
 __host__ __device__ constexpr int store_ctas(int format) { return format == GKV_STORE_BF16 ? 3 : 4; }
 int store_attn_ctas_per_sm(int format) { return store_ctas(format); }
 
-// What becomes of a CTA's result: it is the unit's; it goes to the workspace; it is joined with those of the cluster's other CTAs.
-enum { kWhole = 0, kPart = 1, kCluster = 2 };
+// What becomes of a CTA's result: it is the unit's; it goes to the workspace (kDealt: pieces go by the lengths); it is joined with
+// those of the cluster's other CTAs.
+enum { kWhole = 0, kPart = 1, kCluster = 2, kDealt = 3 };
 
-// Own rows of the units. Grid: units x splits, split fastest.
+// ---- pieces by length: the batch * splits places of a head go to the sequences one after the other, as many to each
+// as its tiles need. Every warp works it out for itself; the merge does so again.
+__device__ __forceinline__ int own_tiles_of(const StoreAttnLaunch& p, int seq) {
+    if (seq >= p.batch) return 0;
+    const int len = p.len[seq], n = p.k_new ? 1 : 0;
+    return len < 0 || len > p.capacity - n ? 0 : (len + n + kTile - 1) / kTile;
+}
+__device__ __forceinline__ int pieces_of(int tiles, int per) { return (int)(((unsigned)tiles + (unsigned)per - 1) / (unsigned)per); }
+// Pieces of sequences 0 .. seqs - 1, `per` tiles each. t0: tiles of sequence `lane`.
+__device__ __forceinline__ int pieces_before(const StoreAttnLaunch& p, int seqs, int per, int lane, int t0) {
+    int c = lane < seqs ? pieces_of(t0, per) : 0;
+    for (int b = lane + 32; b < seqs; b += 32) c += pieces_of(own_tiles_of(p, b), per);
+    return (int)__reduce_add_sync(0xffffffffu, (unsigned)c);
+}
+// Tiles of a piece: 8 (two turns of the four warps) or more, no unit in more than kMaxPieces pieces, and all pieces in their
+// places: the mean, or a little more until roundings fit (with (splits - 1) / splits of the places they always do).
+__device__ __forceinline__ int store_piece_tiles(const StoreAttnLaunch& p, int lane, int t0) {
+    int sum = t0, most = t0;
+    for (int b = lane + 32; b < p.batch; b += 32) {
+        const int t = own_tiles_of(p, b);
+        sum += t;
+        most = max(most, t);
+    }
+    sum = (int)__reduce_add_sync(0xffffffffu, (unsigned)sum);
+    most = (int)__reduce_max_sync(0xffffffffu, (unsigned)most);
+    const int places = p.batch * p.splits;
+    int per = max(max(8, pieces_of(sum, places)), pieces_of(most, kMaxPieces));
+    for (int k = 0; pieces_before(p, p.batch, per, lane, t0) > places; ++k)
+        per = k < 4 ? per + per / 32 + 1 : max(per, pieces_of(sum, places - p.batch));
+    return per;
+}
+
+// Own rows of the units. Grid: units x splits, split fastest; dealt out: a head's places, head slowest.
 template <int F, int MODE>
 __global__ void __launch_bounds__(kThreads, store_ctas(F)) gkv_store_attn_kernel(const StoreAttnLaunch p) {
     constexpr int NG = F == GKV_STORE_INT4 ? 4 : 1;
@@ -357,15 +389,43 @@ __global__ void __launch_bounds__(kThreads, store_ctas(F)) gkv_store_attn_kernel
     __shared__ float s_cl[kMaxCluster][8], s_norm[3][8];
     __shared__ __align__(16) float s_o[kWarps][kHeadDim * 8];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int unit = blockIdx.x / p.splits, split = blockIdx.x - unit * p.splits;
-    const int seq = unit / p.h_kv, head = unit - seq * p.h_kv;
+    int unit = blockIdx.x / p.splits, split = blockIdx.x - unit * p.splits, splits = p.splits, split_tiles = p.split_tiles;
+    int seq = unit / p.h_kv, head = unit - seq * p.h_kv;
+    if (MODE == kPart || MODE == kDealt) grid_launch_dependents();
+    if (MODE == kDealt) {
+        const int places = p.batch * p.splits;
+        head = blockIdx.x / places;
+        split = blockIdx.x - head * places;
+        const int t0 = own_tiles_of(p, lane);
+        split_tiles = store_piece_tiles(p, lane, t0);
+        for (seq = -1; seq < p.batch;) {                 // the sequence whose places these are: 32 at a time
+            const int c = pieces_of(seq < 0 ? t0 : own_tiles_of(p, seq + 1 + lane), split_tiles);
+            int upto = c;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int x = __shfl_up_sync(0xffffffffu, upto, o);
+                if (lane >= o) upto += x;
+            }
+            const unsigned past = __ballot_sync(0xffffffffu, upto > split);
+            if (past) {
+                const int at = __ffs(past) - 1;
+                seq += 1 + at;
+                split -= __shfl_sync(0xffffffffu, upto - c, at);
+                splits = __shfl_sync(0xffffffffu, c, at);
+                break;
+            }
+            split -= __shfl_sync(0xffffffffu, upto, 31);
+            seq += 32;
+        }
+        if (seq >= p.batch) return;                      // a place that nobody needs
+        unit = seq * p.h_kv + head;
+    }
     const int len = p.len[seq];
     const bool append = p.k_new != nullptr;
     uint4 new_row = make_uint4(0u, 0u, 0u, 0u);           // on its way while the length is (lanes 0-15: K, 16-31: V)
     if (append) new_row = store_load_source<F>((lane < 16 ? p.k_new : p.v_new) + (size_t)unit * kHeadDim, lane & 15);
     const bool fits = append ? len < p.capacity : len <= p.capacity;
     // The merge goes by this word and not by the length, which it may count up itself.
-    if (MODE == kPart) grid_launch_dependents();
     if (MODE == kPart && split == 0 && threadIdx.x == 0)
         p.own_part[(size_t)blockIdx.x * kOwnRecFloats + 24] = len < 0 ? kPieceLeftOut : fits ? kPieceOk : kPieceNoFit;
     if (len < 0) {
@@ -374,8 +434,8 @@ __global__ void __launch_bounds__(kThreads, store_ctas(F)) gkv_store_attn_kernel
     }
     const int n = fits ? len + (append ? 1 : 0) : 0;
     const int tiles = (n + kTile - 1) / kTile;
-    const int t_begin = min(split * p.split_tiles, tiles);
-    const int t_end = split == p.splits - 1 ? tiles : min(t_begin + p.split_tiles, tiles);
+    const int t_begin = min(split * split_tiles, tiles);
+    const int t_end = split == splits - 1 ? tiles : min(t_begin + split_tiles, tiles);
 
     uint8_t* kb = p.k + (size_t)unit * p.capacity * StoreFormat<F>::kRow;
     uint8_t* vb = p.v + (size_t)unit * p.capacity * StoreFormat<F>::kRow;
@@ -575,7 +635,7 @@ __global__ void __launch_bounds__(kThreads, store_ctas(F)) gkv_store_attn_kernel
         o[0] = fmaf(a.x, s_wgt[w][0], o[0]); o[1] = fmaf(a.y, s_wgt[w][1], o[1]); o[2] = fmaf(a.z, s_wgt[w][2], o[2]); o[3] = fmaf(a.w, s_wgt[w][3], o[3]);
         o[4] = fmaf(b.x, s_wgt[w][4], o[4]); o[5] = fmaf(b.y, s_wgt[w][5], o[5]); o[6] = fmaf(b.z, s_wgt[w][6], o[6]); o[7] = fmaf(b.w, s_wgt[w][7], o[7]);
     }
-    if (MODE == kPart) {
+    if (MODE == kPart || MODE == kDealt) {
         float* rec = p.own_part + (size_t)blockIdx.x * kOwnRecFloats;
         if (d < 8) { rec[d] = s_fin[0][d]; rec[8 + d] = s_fin[1][d]; rec[16 + d] = s_fin[2][d]; }
         // [dim / 4][head][4], by way of shared memory
@@ -588,7 +648,7 @@ __global__ void __launch_bounds__(kThreads, store_ctas(F)) gkv_store_attn_kernel
 #pragma unroll
         for (int i = 0; i < 2; ++i) ro[i * kThreads + d] = *reinterpret_cast<const float4*>(mine + (i * kThreads + d) * 4);
         // The merge waits for this kernel only, so this kernel may not end before the prefixes' does.
-        if (p.prefix_part && blockIdx.x == 0) grid_wait_previous();
+        if (MODE == kPart && p.prefix_part && blockIdx.x == 0) grid_wait_previous();
         return;
     }
     if (MODE == kCluster) {
@@ -644,6 +704,7 @@ __global__ void __launch_bounds__(kThreads, store_ctas(F)) gkv_store_attn_kernel
 // query rows. 2^ds CTAs per unit, each with a share of the dimensions; thread t holds head t & 7 of four dimensions over every
 // (slices)th of the parts, so that 8 lanes read 128 contiguous bytes of a record. The statistics of all parts are loaded at once,
 // the values of 8 parts at a time: the kernel is a few trips to L2.
+template <bool DEALT>
 __global__ void __launch_bounds__(1024) gkv_store_merge_kernel(const StoreAttnLaunch p, const int ds) {
     extern __shared__ float s_part[];                // [parts][8] factors
     __shared__ __align__(16) float s_red[4 * 1024];
@@ -658,6 +719,12 @@ __global__ void __launch_bounds__(1024) gkv_store_merge_kernel(const StoreAttnLa
     int row0 = 0;
     size_t step = 0;
     const float *own = p.own_part + (size_t)unit * p.splits * kOwnRecFloats, *pre_rec = nullptr;
+    int n_own = p.splits;
+    if (DEALT) {
+        const int t0 = own_tiles_of(p, t & 31), per = store_piece_tiles(p, t & 31, t0);
+        own = p.own_part + ((size_t)head * p.batch * p.splits + pieces_before(p, seq, per, t & 31, t0)) * kOwnRecFloats;
+        n_own = pieces_of(own_tiles_of(p, seq), per);
+    }
     if (p.prefix_part) {
         const int pre = seq / p.seqs_per_prefix, sl = seq - pre * p.seqs_per_prefix, blk = sl / p.seqs_per_block;
         int base = head * p.n_blocks + blk;
@@ -667,16 +734,23 @@ __global__ void __launch_bounds__(1024) gkv_store_merge_kernel(const StoreAttnLa
         pre_rec = p.prefix_part + (size_t)base * kPrefixRecFloats;
         row0 = (sl - blk * p.seqs_per_block) * p.g;
     }
-    const int twice = p.two_tiles ? 0 : 1, parts = p.splits + (items << twice);
+    const int twice = p.two_tiles ? 0 : 1, parts = n_own + (items << twice);
     // statistics and values of prefix part j at the unit's first row
     auto pre_stats = [&](int j) { return pre_rec + (size_t)(j >> twice) * step + row0 + (j & twice) * 128; };
     auto pre_values = [&](int j) {
         return reinterpret_cast<const float4*>(pre_rec + (size_t)(j >> twice) * step + 2 * kPrefixRows) + row0 + (j & twice) * 128;
     };
     grid_wait_previous();
-    const float state = own[24];
-    if (state == kPieceLeftOut) return;
-    const bool fits = state == kPieceOk;
+    bool fits;
+    if (DEALT) {                                     // (a sequence without keys has no piece)
+        const int len = p.len[seq];
+        if (len < 0) return;
+        fits = p.k_new ? len < p.capacity : len <= p.capacity;
+    } else {
+        const float state = own[24];
+        if (state == kPieceLeftOut) return;
+        fits = state == kPieceOk;
+    }
 
     // ---- statistics: factors of all parts. Thread t has head t & 7 of parts t / 8, t / 8 + blockDim / 8, ...
     const int hops = (parts * 8 + (int)blockDim.x - 1) / (int)blockDim.x;
@@ -687,11 +761,11 @@ __global__ void __launch_bounds__(1024) gkv_store_merge_kernel(const StoreAttnLa
         z[k] = 0.f;
         const int part = (t + k * (int)blockDim.x) >> 3;
         if (k < hops && part < parts) {
-            if (part < p.splits) {
+            if (part < n_own) {
                 const float* r = own + (size_t)part * kOwnRecFloats + hc;
                 x[k] = r[0]; z[k] = r[8]; y[k] = r[16];
             } else {
-                const float* r = pre_stats(part - p.splits) + hc;
+                const float* r = pre_stats(part - n_own) + hc;
                 x[k] = y[k] = r[0]; z[k] = r[kPrefixRows];
             }
         }
@@ -727,7 +801,7 @@ __global__ void __launch_bounds__(1024) gkv_store_merge_kernel(const StoreAttnLa
     };
     const float4* ov = reinterpret_cast<const float4*>(own + 32) + d4 * 8 + h;
 #pragma unroll 4
-    for (int i = slice; i < p.splits; i += slices) {
+    for (int i = slice; i < n_own; i += slices) {
         const float4 a = ov[(size_t)i * (kOwnRecFloats / 4)];
         add(s_part[i * 8 + h], a);
     }
@@ -738,7 +812,7 @@ __global__ void __launch_bounds__(1024) gkv_store_merge_kernel(const StoreAttnLa
         for (int k = 0; k < 8; ++k) a[k] = pre_values(min(i0 + k * slices, n_pre - 1))[d4 * kPrefixRows + hc];
 #pragma unroll
         for (int k = 0; k < 8; ++k)
-            if (i0 + k * slices < n_pre) add(s_part[(p.splits + i0 + k * slices) * 8 + h], a[k]);
+            if (i0 + k * slices < n_pre) add(s_part[(n_own + i0 + k * slices) * 8 + h], a[k]);
     }
     if (slices > 1) {
         __syncthreads();
@@ -793,12 +867,13 @@ static cudaError_t launch_ex(void (*kernel)(A...), unsigned grid, unsigned threa
 template <int F>
 static cudaError_t launch_own(const StoreAttnLaunch& p, cudaStream_t s) {
     const unsigned grid = (unsigned)(p.batch * p.h_kv * p.splits);
+    if (p.dealt) return launch_ex(gkv_store_attn_kernel<F, kDealt>, grid, kThreads, 0, 1, false, s, p);
     if (store_needs_merge(p)) return launch_ex(gkv_store_attn_kernel<F, kPart>, grid, kThreads, 0, 1, p.prefix_part != nullptr, s, p);
     if (p.splits > 1) return launch_ex(gkv_store_attn_kernel<F, kCluster>, grid, kThreads, 0, p.splits, false, s, p);
     gkv_store_attn_kernel<F, kWhole><<<grid, kThreads, 0, s>>>(p);
     return cudaGetLastError();
 }
-bool store_needs_merge(const StoreAttnLaunch& p) { return p.splits > kMaxCluster || p.prefix_part != nullptr || p.len_out != nullptr; }
+bool store_needs_merge(const StoreAttnLaunch& p) { return p.dealt || p.splits > kMaxCluster || p.prefix_part != nullptr || p.len_out != nullptr; }
 cudaError_t launch_store_attn(const StoreAttnLaunch& p, cudaStream_t s) {
     switch (p.format) {
         case GKV_STORE_BF16: return launch_own<GKV_STORE_BF16>(p, s);
@@ -808,13 +883,16 @@ cudaError_t launch_store_attn(const StoreAttnLaunch& p, cudaStream_t s) {
     }
 }
 // The fewer units, the more CTAs per unit. 256 threads for up to 8 parts, 512 for up to 16, else 1024. (The plan bounds the parts
-// of a unit: kMaxSplits + 2 kMaxRuns = 448, 8 numbers each are 3.5 per thread.)
+// of a unit: kMaxPieces + 2 kMaxRuns = 448, 8 numbers each are 3.5 per thread.) Dealt out, units have few parts or up to
+// kMaxPieces, which the host does not know: threads by the number of units (256 units of 2 parts each with 1024, 512, 256 threads,
+// attention included: 102, 96, 96 us; one of them with most of the rows: 63, 61, 65; 1024 units: -, 378, 370 and -, 167, 153).
 cudaError_t launch_store_merge(const StoreAttnLaunch& p, cudaStream_t s) {
     int longest = 0;
     for (int i = 0; i < p.n_prefix; ++i) longest = p.prefix_len[i] > longest ? p.prefix_len[i] : longest;
     const int items = p.prefix_part ? ((longest + 127) / 128 + p.chunk - 1) / p.chunk * (p.two_tiles ? 1 : 2) : 0;
-    const int parts = p.splits + items, units = p.batch * p.h_kv, ds = units <= 40 ? 2 : units <= 80 ? 1 : 0;
-    return launch_ex(gkv_store_merge_kernel, (unsigned)units << ds, parts <= 8 ? 256u : parts <= 16 ? 512u : 1024u, (size_t)parts * 8 * sizeof(float), 1,
+    const int parts = (p.dealt ? min(p.batch * p.splits, kMaxPieces) : p.splits) + items, units = p.batch * p.h_kv, ds = units <= 40 ? 2 : units <= 80 ? 1 : 0;
+    const unsigned threads = p.dealt ? (units <= 148 ? 1024u : units <= 296 ? 512u : 256u) : parts <= 8 ? 256u : parts <= 16 ? 512u : 1024u;
+    return launch_ex(p.dealt ? gkv_store_merge_kernel<true> : gkv_store_merge_kernel<false>, (unsigned)units << ds, threads, (size_t)parts * 8 * sizeof(float), 1,
                      true, s, p, ds);
 }
 

@@ -756,3 +756,59 @@ def test_read_into_views(view):
         one = torch.zeros((B, 1, H, 128), dtype=torch.bfloat16, device=DEV)
         with pytest.raises(gkv.GKVError):
             st.read(one.expand(B, T, H, 128), one.expand(B, T, H, 128))
+
+
+@pytest.mark.parametrize("append", [False, True])
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("h_q,h_kv,lens", [
+    (4, 1, [9999, 0, -1, 5, 20000, 700]), (7, 1, [0, 0, -1, 0, 0, 0]), (4, 2, [1, 9000] + [0] * 18 + [-1, 33, 3000]), (8, 1, [130] * 45 + [8000]),
+    (2, 1, [15, 16, 17, 9999]), (1, 1, [9990, 9991]),
+])
+def test_pieces_go_by_the_lengths(fmt, append, h_q, h_kv, lens):
+    """Few units and a long capacity: very uneven lengths, sequences without keys, left out and not fitting."""
+    C = 10000
+    fits = [min(x, C - 1) for x in lens]
+    st, g = filled(fmt, len(lens), h_q, h_kv, C, fits, 71)
+    q = randn(g, len(lens), h_q, 128)
+    kn, vn = (randn(g, len(lens), h_kv, 128), randn(g, len(lens), h_kv, 128)) if append else (None, None)
+    out, lse = torch.full((len(lens), h_q, 128), 7.0, dtype=torch.bfloat16, device=DEV), torch.full((len(lens), h_q), 7.0, device=DEV)
+    st.attn(ints(lens), q, out, k_new=kn, v_new=vn, lse=lse)
+    skip = [b for b, x in enumerate(lens) if x < 0 or x > C]
+    check(st, lens, q, out, lse, append, skip=skip)
+    for b in skip:
+        assert (out[b] == 7).all() if lens[b] < 0 else torch.isnan(out[b]).all() and torch.isnan(lse[b]).all()
+    again = torch.empty_like(out)
+    if not append:
+        st.attn(ints(lens), q, again, max_len=C)
+        keep = [b for b in range(len(lens)) if b not in skip]
+        assert torch.equal(out[keep], again[keep])
+
+
+class Some:
+    """A few sequences of a store, for the reference."""
+    def __init__(self, st, seqs):
+        self.fmt, self.h_q, self.h_kv, self.batch = st.fmt, st.h_q, st.h_kv, len(seqs)
+        self.k, self.v, self.k_scale, self.v_scale = (None if t is None else t[seqs] for t in (st.k, st.v, st.k_scale, st.v_scale))
+
+
+@pytest.mark.parametrize("append", [False, True])
+@pytest.mark.parametrize("fmt,B,h_kv,C,long", [
+    ("int8", 150, 2, 8300, {3: 8299, 149: 5000}),     # more units than there are places
+    ("int4", 330, 1, 8300, {40: 8299, 41: 8000}),     # more sequences than two turns of a warp
+    ("e4m3", 40, 2, 17000, {0: 16999, 33: 4001}), ("bf16", 20, 4, 15000, {19: 14999}), ("int4", 37, 3, 16400, {36: 16399}),
+])
+def test_long_sequences_among_short_ones(fmt, append, B, h_kv, C, long):
+    rng = np.random.RandomState(B)
+    lens = [int(x) for x in rng.randint(-1, 60, B)]
+    for b, n in long.items():
+        lens[b] = n
+    st, g = filled(fmt, B, 4 * h_kv, h_kv, C, lens, 72)
+    q = randn(g, B, 4 * h_kv, 128)
+    kn, vn = (randn(g, B, h_kv, 128), randn(g, B, h_kv, 128)) if append else (None, None)
+    out, lse = torch.full((B, 4 * h_kv, 128), 7.0, dtype=torch.bfloat16, device=DEV), torch.full((B, 4 * h_kv), 7.0, device=DEV)
+    st.attn(ints(lens), q, out, k_new=kn, v_new=vn, lse=lse)
+    seqs = sorted(set(long) | set(range(0, B, 9)))
+    seqs = [b for b in seqs if lens[b] >= 0]
+    check(Some(st, seqs), [lens[b] for b in seqs], q[seqs], out[seqs], lse[seqs], append)
+    for b in range(B):
+        assert (out[b] == 7).all() if lens[b] < 0 else torch.isfinite(out[b]).all()
