@@ -5,7 +5,7 @@
 // (running maximum, sum, unscaled output of every row) goes to the workspace and is joined with the other runs' and with the
 // sequences' own rows by the merge kernel.
 //
-// One CTA (one per SM: 226 KB of shared memory, all 512 TMEM columns) holds two streams, A and B, each with 128 query rows: with
+// One CTA (one per SM: all 512 TMEM columns) holds two streams, A and B, each with 128 query rows: with
 // more than 128 rows in the item A and B have a row tile each and both see every key tile; with fewer they have the same rows
 // and take the even and the odd key tiles. Per stream and key tile
 //     S = Q K^T          128 x 128 x 128, operands in shared memory, S in 128 TMEM columns
@@ -30,7 +30,9 @@
 // the same SM.
 //
 // Bound: for 256 rows a key tile costs 64 KB of HBM traffic (1.5 us of an SM's share), 2048 cycles of the tensor core and 2048
-// cycles of the exponential unit: all three are level.
+// cycles of the exponential unit: all three are level. Measured: 3900 cycles a tile of 256 rows (2.1 us), tensor cores and
+// exponentials half busy, the rest being the hand-overs between the two streams' steps; 4 prefixes of up to 16384 keys x 8 heads
+// with 256 query rows each 80 us alone, 145 us with the own rows of 128 sequences (450 MB of e4m3, which alone take 75).
 #include "gkv_tcgen05.cuh"
 #include "gkv_internal.h"
 

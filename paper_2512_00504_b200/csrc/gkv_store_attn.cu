@@ -21,10 +21,11 @@
 // accumulators) only when its weights have grown large.
 //
 // The pieces of a unit are joined by the CTAs of a cluster reading one another's shared memory (up to 8 pieces, no prefix), or
-// leave partial results in the workspace for the merge kernel.
+// leave partial results in the workspace for the merge kernel. Long rows are dealt out by the lengths that the sequences have, so
+// that one long sequence among short ones gets the places that they do not need.
 //
 // Bound by HBM for 8-bit rows in a large batch (128 sequences x 8 heads of about 2200 keys, 585 MB: 97 us, 6.0 TB/s). 4-bit rows
-// bring twice the elements per byte to unpack: 2 x 8 heads of about 120000 keys, 274 MB in 77 us, 3.6 TB/s, with the schedulers
+// bring twice the elements per byte to unpack: 2 x 8 heads of about 120000 keys, 274 MB in 76 us, 3.6 TB/s, with the schedulers
 // issuing 6 cycles out of 10, the logic and fp32 pipes 4 to 5 (without the products and what feeds them the same loads take 55
 // us). A single sequence of 640 keys takes 6.7 us: the launch, three trips to memory (length, rows, the others' results), 3 tiles
 // per warp.

@@ -812,3 +812,26 @@ def test_long_sequences_among_short_ones(fmt, append, B, h_kv, C, long):
     check(Some(st, seqs), [lens[b] for b in seqs], q[seqs], out[seqs], lse[seqs], append)
     for b in range(B):
         assert (out[b] == 7).all() if lens[b] < 0 else torch.isfinite(out[b]).all()
+
+
+def test_a_captured_graph_deals_out_by_the_lengths_it_finds():
+    B, C = 12, 12000
+    st, g = filled("int8", B, 4, 1, C, [C - 3] * B, 73)
+    q, kn, vn = randn(g, B, 4, 128), randn(g, B, 1, 128), randn(g, B, 1, 128)
+    out, lse = torch.zeros((B, 4, 128), dtype=torch.bfloat16, device=DEV), torch.zeros((B, 4), device=DEV)
+    length = ints([100] * B)
+    st.attn(length, q, out, k_new=kn, v_new=vn, lse=lse)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        st.attn(length, q, out, k_new=kn, v_new=vn, lse=lse)
+        length += 1
+    for lens in ([100] * B, [11990] + [3] * (B - 1), [-2, 0] + [6000] * (B - 2)):
+        out.fill_(7)
+        length.copy_(ints(lens))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert length.tolist() == [x + 1 for x in lens]
+        check(st, lens, q, out, lse, True, skip=[b for b in range(B) if lens[b] < 0])
+        for b in range(B):
+            assert (out[b] == 7).all() if lens[b] < 0 else torch.isfinite(out[b]).all()
