@@ -380,7 +380,9 @@ gkv_status gkv_store_attn_workspace(const gkv_store* store, int32_t n_prefix, in
  *   len      device int32[batch]. len[i] < 0: the sequence is left out (its out, lse and rows stay as they were). A length
  *            that does not fit the store (above capacity, or capacity with a new token) gives NaN in out and lse, and nothing
  *            is written to the store.
- *   max_len  the longest length, for spreading the work (0: capacity). Results do not depend on it beyond rounding.
+ *   max_len  the longest length, for spreading the work (0: capacity). Results do not depend on it beyond rounding. (How
+ *            the work is spread, and with it the rounding of sums, may also depend on the other sequences' lengths; the same
+ *            call gives the same bits.)
  *   q, out   device, bf16 [batch][n_q_heads][128], 16-byte aligned
  *   k_new, v_new  device, bf16 [batch][n_kv_heads][128], 16-byte aligned, or both NULL. The new row is quantised into row
  *            len[i] and attended to as it stands there. The caller then counts len[i] up.
