@@ -10,13 +10,13 @@
 // Measured (bytes of both sides): 4 x 32768 tokens x 8 heads into 4 bits, 688 MB in 113 us: 6.1 TB/s; 64 x about 1900 tokens x 8
 // heads back from e4m3, 738 MB in 113 us: 6.5 TB/s; one token of 32 sequences x 4 heads: 2 us, which is a launch.
 #include "gkv_store_codes.cuh"
+#include "gkv_store_rows.h"
 
 namespace gkv {
 
 // Small blocks: a run of a few sequences is one round of them, and 128 threads end with a shorter tail than 256 (2048 tokens x 8
 // heads with ragged counts, write and read back: 26.4 us against 28.2; one sequence: 2.5 against 2.7; 64 threads: 26.8, 2.5).
 constexpr int kCopyThreads = 128;
-constexpr int kRun = 8;
 
 // Work item i of sequence blockIdx.y: head i % h_kv, tokens kRun * (i / h_kv) and on; blockIdx.z = K or V.
 template <int F, bool READ>
@@ -27,11 +27,10 @@ __global__ void __launch_bounds__(kCopyThreads) gkv_store_copy_kernel(const Stor
     const int l = threadIdx.x & 15;
     const int item = blockIdx.x * (kCopyThreads / 16) + (threadIdx.x >> 4);
     const int h = item % p.h_kv, t0 = item / p.h_kv * kRun;
-    const int count = p.count ? min(p.count[b], p.n_tokens) : p.n_tokens;
-    const int64_t first = p.first ? p.first[b] : 0;
-    // tokens lo .. hi - 1 of the run have a row (none: lo >= hi); the whole warp stays for the shuffles
-    const int hi = (int)min((int64_t)min(count - t0, kRun), p.capacity - first - t0);
-    const int lo = (int)max((int64_t)0, min((int64_t)kRun, -(first + t0)));
+    const int32_t first = p.first ? p.first[b] : 0;
+    // the whole warp stays for the shuffles, whatever the run has
+    const RunRows rows = run_rows(first, p.count ? p.count[b] : p.n_tokens, p.n_tokens, p.capacity, t0);
+    const int lo = rows.lo, hi = rows.hi;
     const int64_t row0 = ((int64_t)b * p.h_kv + h) * p.capacity + first + t0;
     uint8_t* data = (is_v ? p.data[1] : p.data[0]) + row0 * Fm::kRow;
     __nv_bfloat16* scale = (is_v ? p.scale[1] : p.scale[0]) + row0 * Fm::kScales;
@@ -40,7 +39,7 @@ __global__ void __launch_bounds__(kCopyThreads) gkv_store_copy_kernel(const Stor
     // Scales are held and moved by lane 2i + j: in 4 bits those of groups 2j, 2j + 1 of token i, in 8 bits that of token i (the
     // odd lane has a copy).
     const int st = l >> 1;
-    const bool has_scale = Fm::kScales != 0 && st >= lo && st < min(hi, kRun) && (F == GKV_STORE_INT4 || (l & 1) == 0);
+    const bool has_scale = Fm::kScales != 0 && st >= lo && st < hi && (F == GKV_STORE_INT4 || (l & 1) == 0);
     uint32_t* scale4 = reinterpret_cast<uint32_t*>(scale) + l;
     uint16_t* scale2 = reinterpret_cast<uint16_t*>(scale) + st;
     uint4 v[kRun];
