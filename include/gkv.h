@@ -361,7 +361,8 @@ gkv_status gkv_store_read(const gkv_store* store, void* k, void* v, int64_t seq_
 
 /* Prefixes shared by the sequences of a batch: sequence i attends to all rows of prefix i / (batch / n_prefix) besides its
  * own. k, v: device, bf16 [n_prefix][n_kv_heads][rows][128], 16-byte aligned, of which prefix p has its first len[p] rows in
- * use (len: HOST int32[n_prefix], 0..rows; what lies behind them is not used). */
+ * use (len: HOST int32[n_prefix], 0..rows; what lies behind them is not used). n_kv_heads is that of the store or the context:
+ * the caller sees to it that the rows have as many heads. */
 typedef struct {
     int32_t n_prefix; /* 1..64, divides batch */
     int32_t rows;

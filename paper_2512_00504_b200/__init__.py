@@ -372,7 +372,8 @@ def gkv_store_attn_workspace(store: gkv_store, n_prefix: int = 0, prefix_rows: i
 
 
 def gkv_decode_attn_prefix(ctx, layer, q, k_new, v_new, prefix, out, workspace):
-    """prefix: a Prefix; workspace: a uint8 tensor of gkv_store_attn_workspace bytes (GKVCache.prefix_workspace)."""
+    """prefix: a Prefix with the context's KV heads (a context does not say how many: GKVCache.decode_attn_prefix checks);
+    workspace: a uint8 tensor of gkv_store_attn_workspace bytes (GKVCache.prefix_workspace)."""
     _check(lib().gkv_decode_attn_prefix(ctx, layer, _ptr(q), _ptr(k_new), _ptr(v_new), ctypes.byref(prefix.desc), _ptr(out),
                                         _ptr(workspace), workspace.numel(), _stream()), "gkv_decode_attn_prefix")
 
@@ -458,6 +459,7 @@ class GKVCache:
         return torch.empty(gkv_store_attn_workspace(shape, n_prefix, prefix_rows), dtype=torch.uint8, device=self.device)
 
     def decode_attn_prefix(self, layer, q, k_new, v_new, prefix, out, workspace):
+        _fitting(prefix, self.cfg.n_kv_heads, self.k.device, "cache")
         gkv_decode_attn_prefix(self.ctx, layer, q, k_new, v_new, prefix, out, workspace)
 
     def poll(self):
@@ -470,6 +472,12 @@ def _tensor(t, what, dtype, shape, device):
         raise ValueError(f"{what}: a contiguous {dtype} tensor of shape {tuple(shape)} on {device} is needed, "
                          f"got {t.dtype} {tuple(t.shape)} on {t.device}" + ("" if t.is_contiguous() else ", not contiguous"))
     return t.data_ptr()
+
+
+def _fitting(prefix, h_kv, device, what):
+    """The C calls take the head count of a prefix's rows from the store or the context: others would be read out of place."""
+    if prefix.h_kv != h_kv or prefix.k.device != device:
+        raise ValueError(f"the prefix has {prefix.h_kv} KV heads on {prefix.k.device}, the {what} {h_kv} on {device}")
 
 
 class Prefix:
@@ -547,7 +555,6 @@ class KVStore:
         ws, ws_bytes = self._ws
         pre = 0
         if prefix is not None:
-            if prefix.k.device != self.device or prefix.h_kv != self.h_kv:
-                raise ValueError(f"the prefix has {prefix.h_kv} KV heads on {prefix.k.device}, the store {self.h_kv} on {self.device}")
+            _fitting(prefix, self.h_kv, self.device, "store")
             pre = prefix.at
         _check(self._call.attn(at, dev, length, max_len, q, k_new, v_new, pre, out, lse, ws, ws_bytes), "gkv_store_attn")
