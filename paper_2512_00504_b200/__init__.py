@@ -454,7 +454,7 @@ class GKVCache:
     def prefix_workspace(self, n_prefix, prefix_rows):
         """Workspace of decode_attn_prefix for up to n_prefix prefixes of up to prefix_rows rows."""
         import torch
-        c = self.cfg
+        c, n_prefix, prefix_rows = self.cfg, _int32(n_prefix, "n_prefix"), _int32(prefix_rows, "prefix_rows")
         shape = gkv_store(GKV_STORE_BF16, c.batch, c.n_q_heads, c.n_kv_heads, c.head_dim, self.C)
         return torch.empty(gkv_store_attn_workspace(shape, n_prefix, prefix_rows), dtype=torch.uint8, device=self.device)
 
@@ -474,6 +474,14 @@ def _tensor(t, what, dtype, shape, device):
     return t.data_ptr()
 
 
+def _int32(n, what):
+    """n as an int that the C calls' 32-bit arguments hold (ctypes cuts the rest off without a word)."""
+    n = int(n)
+    if not -2 ** 31 <= n < 2 ** 31:
+        raise ValueError(f"{what} {n} does not fit 32 bits")
+    return n
+
+
 def _fitting(prefix, h_kv, device, what):
     """The C calls take the head count of a prefix's rows from the store or the context: others would be read out of place."""
     if prefix.h_kv != h_kv or prefix.k.device != device:
@@ -489,7 +497,7 @@ class Prefix:
         if k.dim() != 4 or k.shape[3] != 128 or k.device.type != "cuda":
             raise ValueError("k, v: bf16 device tensors [n_prefix][kv heads][rows][128]")
         pk, pv = (_tensor(t, n, torch.bfloat16, k.shape, k.device) for t, n in ((k, "k"), (v, "v")))
-        lengths = [int(n) for n in lengths]
+        lengths = [_int32(n, "length") for n in lengths]
         if len(lengths) != k.shape[0]:
             raise ValueError(f"{len(lengths)} lengths for {k.shape[0]} prefixes")
         self.k, self.v, self.h_kv = k, v, k.shape[1]
@@ -510,6 +518,8 @@ class KVStore:
         self.fmt, self.batch, self.h_q, self.h_kv, self.capacity = fmt, batch, h_q, h_kv, capacity
         if fmt not in STORE_FORMATS:
             raise ValueError(f"format {fmt!r}: one of {sorted(STORE_FORMATS)} is needed")
+        for n, what in ((batch, "batch"), (h_q, "h_q"), (h_kv, "h_kv"), (capacity, "capacity"), (n_prefix, "n_prefix"), (max_prefix, "max_prefix")):
+            _int32(n, what)
         self.desc = gkv_store(STORE_FORMATS[fmt], batch, h_q, h_kv, 128, capacity)
         self.sizes = gkv_store_query_sizes(self.desc)
         code = {"bf16": torch.bfloat16, "e4m3": torch.float8_e4m3fn, "int8": torch.int8, "int4": torch.uint8}[fmt]
