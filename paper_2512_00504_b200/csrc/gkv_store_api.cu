@@ -157,7 +157,7 @@ gkv_status copy_args(const gkv_store* store, const void* k, const void* v, int64
     if (seq_stride < 0 || token_stride < 0 || head_stride < 0 || ((seq_stride | token_stride | head_stride) & 7) != 0) return GKV_ERR_INVALID_ARG;
     if ((int64_t)n_tokens * store->n_kv_heads >= (1ll << 30)) return GKV_ERR_UNSUPPORTED;
     if (read && n_tokens > 0 && k == v) return GKV_ERR_INVALID_ARG;
-    if (read && rows_overlap(store->batch, seq_stride, n_tokens, token_stride, store->n_kv_heads, head_stride)) return GKV_ERR_INVALID_ARG;
+    if (read && n_tokens > 0 && rows_overlap(store->batch, seq_stride, n_tokens, token_stride, store->n_kv_heads, head_stride)) return GKV_ERR_INVALID_ARG;
     p->data[0] = static_cast<uint8_t*>(store->k); p->data[1] = static_cast<uint8_t*>(store->v);
     p->scale[0] = static_cast<__nv_bfloat16*>(store->k_scale); p->scale[1] = static_cast<__nv_bfloat16*>(store->v_scale);
     p->x[0] = static_cast<__nv_bfloat16*>(const_cast<void*>(k)); p->x[1] = static_cast<__nv_bfloat16*>(const_cast<void*>(v));
