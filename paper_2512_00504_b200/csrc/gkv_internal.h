@@ -131,7 +131,9 @@ struct ScoreLaunch {
 constexpr int kMaxCluster = 8;            // pieces of a unit that are joined in a cluster
 constexpr int kMaxPieces = 128;           // pieces of a unit of the attention over own rows
 constexpr int kMaxPrefixes = 64;
-constexpr int kOwnRecFloats = 32 + kHeadDimHost * 8;            // partial result of one unit's split: M[8], L[8], Mv[8], pad, O[32][8][4]
+// Partial result of a piece of a unit: M[8], L[8], Mv[groups][8] (4 groups with 4-bit rows, else 1), at kOwnRecState a word that says
+// what the unit is (its first piece's), O[32][8][4].
+constexpr int kOwnRecState = 48, kOwnRecHead = 56, kOwnRecFloats = kOwnRecHead + kHeadDimHost * 8;
 constexpr int kPrefixRows = 256;                                // query rows of a prefix work item
 constexpr int kPrefixRecFloats = kPrefixRows * (2 + kHeadDimHost);   // M[256], L[256], O[32][256][4]
 

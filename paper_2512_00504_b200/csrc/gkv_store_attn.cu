@@ -13,9 +13,10 @@
 // of two (an element is exact down to 2^-17 of its row's largest; below, the error is at most 2^-25 of the largest), weights
 // are rounded to fp16 (11 bits). The scale of a K row multiplies its logit. The scale s of a V row goes into the weight:
 // w = p s c with p = exp2(z - m) as it enters the sum of the softmax, and c = exp2(m - v) with a running maximum v over
-// z + log2 s, so that the weights handed to the product lie in fp16's range whatever the scales are. (v is kept at least at
-// m - 112: c stays finite, and where all of V is below 2^-112 the outputs are numbers of that size.) Sums and accumulators are
-// fp32.
+// z + log2 s, so that the weights handed to the product lie in fp16's range whatever the scales are. A 4-bit row has a scale
+// for each 32 head dimensions, and every group of dimensions has its own v and c: groups of very different size do not share a
+// range. (v is kept at least at m - 112: c stays finite, and where all of a group's V is below 2^-112 its outputs are numbers of
+// that size.) Sums and accumulators are fp32.
 //
 // The running maxima are allowed to lag: a step raises them (which costs a reduction over the warp and a rescaling of the
 // accumulators) only when its weights have grown large.
@@ -25,9 +26,9 @@
 // that one long sequence among short ones gets the places that they do not need.
 //
 // Bound by HBM for 8-bit rows in a large batch (128 sequences x 8 heads of about 2200 keys, 585 MB: 97 us, 6.0 TB/s). 4-bit rows
-// bring twice the elements per byte to unpack: 2 x 8 heads of about 120000 keys, 274 MB in 76 us, 3.6 TB/s, with the schedulers
+// bring twice the elements per byte to unpack: 2 x 8 heads of about 120000 keys, 274 MB in 77 us, 3.6 TB/s, with the schedulers
 // issuing 6 cycles out of 10, the logic and fp32 pipes 4 to 5 (without the products and what feeds them the same loads take 55
-// us). A single sequence of 640 keys takes 6.7 us: the launch, three trips to memory (length, rows, the others' results), 3 tiles
+// us; one reference for all groups of a head instead of one for each: 75.7 against 76.8). A single sequence of 640 keys takes 6.7 us: the launch, three trips to memory (length, rows, the others' results), 3 tiles
 // per warp.
 #include "gkv_store_codes.cuh"
 
@@ -345,6 +346,9 @@ __device__ __forceinline__ float final_lse(float m, float l, bool fits) {
 __host__ __device__ constexpr int store_ctas(int format) { return format == GKV_STORE_BF16 ? 3 : 4; }
 int store_attn_ctas_per_sm(int format) { return store_ctas(format); }
 
+// Groups of head dimensions whose V rows have a scale of their own.
+__host__ __device__ constexpr int value_groups(int format) { return format == GKV_STORE_INT4 ? 4 : 1; }
+
 // What becomes of a CTA's result: it is the unit's; it goes to the workspace (kDealt: pieces go by the lengths); it is joined with
 // those of the cluster's other CTAs.
 enum { kWhole = 0, kPart = 1, kCluster = 2, kDealt = 3 };
@@ -384,10 +388,10 @@ __device__ __forceinline__ int store_piece_tiles(const StoreAttnLaunch& p, int l
 // Own rows of the units. Grid: units x splits, split fastest; dealt out: a head's places, head slowest.
 template <int F, int MODE>
 __global__ void __launch_bounds__(kThreads, store_ctas(F)) gkv_store_attn_kernel(const StoreAttnLaunch p) {
-    constexpr int NG = F == GKV_STORE_INT4 ? 4 : 1;
+    constexpr int NG = value_groups(F);
     constexpr bool kScaled = F != GKV_STORE_BF16;
-    __shared__ float s_m[kWarps][8], s_l[kWarps][8], s_v[kWarps][8], s_wgt[kWarps][8], s_fin[3][8];
-    __shared__ float s_cl[kMaxCluster][8], s_norm[3][8];
+    __shared__ float s_m[kWarps][8], s_l[kWarps][8], s_v[kWarps][NG][8], s_wgt[kWarps][NG][8], s_fin[2 + NG][8];
+    __shared__ float s_cl[kMaxCluster][NG][8], s_norm[2 + NG][8];
     __shared__ __align__(16) float s_o[kWarps][kHeadDim * 8];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     int unit = blockIdx.x / p.splits, split = blockIdx.x - unit * p.splits, splits = p.splits, split_tiles = p.split_tiles;
@@ -428,7 +432,7 @@ __global__ void __launch_bounds__(kThreads, store_ctas(F)) gkv_store_attn_kernel
     const bool fits = append ? len < p.capacity : len <= p.capacity;
     // The merge goes by this word and not by the length, which it may count up itself.
     if (MODE == kPart && split == 0 && threadIdx.x == 0)
-        p.own_part[(size_t)blockIdx.x * kOwnRecFloats + 24] = len < 0 ? kPieceLeftOut : fits ? kPieceOk : kPieceNoFit;
+        p.own_part[(size_t)blockIdx.x * kOwnRecFloats + kOwnRecState] = len < 0 ? kPieceLeftOut : fits ? kPieceOk : kPieceNoFit;
     if (len < 0) {
         if (MODE == kPart && p.prefix_part && blockIdx.x == 0) grid_wait_previous();   // see the end of the partial form
         return;
@@ -481,9 +485,19 @@ __global__ void __launch_bounds__(kThreads, store_ctas(F)) gkv_store_attn_kernel
     }
 
     float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;       // running maxima (they may lag) and sums, heads h0, h0 + 1
-    float v0 = -INFINITY, v1 = -INFINITY;                           // the same maxima of z + log2(scale of V)
+    // The same maxima of z + log2(scale of V): with one scale a row in registers, with several, by group, in the warp's part of
+    // s_v (they are looked at when maxima are raised, and registers are what limits the CTAs of an SM).
+    float v0 = -INFINITY, v1 = -INFINITY;
+    if constexpr (NG > 1) {
+        if (hq == 0)
+#pragma unroll
+            for (int g = 0; g < NG; ++g) s_v[warp][g][h0] = s_v[warp][g][h0 + 1] = -INFINITY;
+        __syncwarp();
+    }
     float n0 = -INFINITY, n1 = -INFINITY;                           // what logits are taken relative to: m, once that is finite
-    float c0 = 1.f, c1 = 1.f;                                       // 2^(m - v + kLift), with finite m and v
+    float c0[NG], c1[NG];                                           // 2^(m - v + kLift), with finite m and v
+#pragma unroll
+    for (int g = 0; g < NG; ++g) c0[g] = c1[g] = 1.f;
     float acc[8][4];
 #pragma unroll
     for (int i = 0; i < 8; ++i) acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.f;
@@ -510,22 +524,22 @@ __global__ void __launch_bounds__(kThreads, store_ctas(F)) gkv_store_attn_kernel
             for (int hf = 0; hf < 2; ++hf)
                 if (hq + 8 * hf >= left) z[2 * hf] = z[2 * hf + 1] = -INFINITY;
         }
-        // V scales of this lane's two keys (0 behind the end), and the sum of a key's: the largest, up to a factor of 4
-        float sc[2][NG], top[2];
+        // V scales of this lane's two keys (0 behind the end)
+        float sc[2][NG];
 #pragma unroll
         for (int hf = 0; hf < 2; ++hf) {
             if constexpr (F == GKV_STORE_INT4) {
                 const uint2 s = tv.s[hf];
                 sc[hf][0] = bf16_lo(s.x); sc[hf][1] = bf16_hi(s.x);
                 sc[hf][2] = bf16_lo(s.y); sc[hf][3] = bf16_hi(s.y);
-                top[hf] = (sc[hf][0] + sc[hf][1]) + (sc[hf][2] + sc[hf][3]);
             } else if constexpr (kScaled) {
-                top[hf] = sc[hf][0] = bf16_lo(tv.s[hf]);
+                sc[hf][0] = bf16_lo(tv.s[hf]);
             } else {
-                sc[hf][0] = top[hf] = 1.f;
+                sc[hf][0] = 1.f;
             }
         }
         float e[4];                     // exp2(z - m)
+        uint32_t b[NG][2];              // the weights, of several scales as soon as they are known
         // A z that is far above m, or a z + log2(scale) far above v, shows in the results: they are sums of non-negative numbers
         // (at most the limit then), infinite or NaN, also at the first step, where m is -infinity.
         float total = 0.f;
@@ -533,30 +547,45 @@ __global__ void __launch_bounds__(kThreads, store_ctas(F)) gkv_store_attn_kernel
             e[0] = fast_exp2(z[0] - n0); e[1] = fast_exp2(z[1] - n1);
             e[2] = fast_exp2(z[2] - n0); e[3] = fast_exp2(z[3] - n1);
             total += (e[0] + e[2]) + (e[1] + e[3]);
-            if (kScaled)
-                total += ((e[0] * c0 + e[1] * c1) * top[0] + (e[2] * c0 + e[3] * c1) * top[1]) * (1.f / kLiftFactor);
+            if constexpr (NG > 1) {
+                float sum = 0.f;
+#pragma unroll
+                for (int g = 0; g < NG; ++g)
+#pragma unroll
+                    for (int hf = 0; hf < 2; ++hf) {      // (e c is finite, c s need not be)
+                        const float x = e[2 * hf] * c0[g] * sc[hf][g], y = e[2 * hf + 1] * c1[g] * sc[hf][g];
+                        sum += x + y;
+                        b[g][hf] = pack_weights<F>(x, y);
+                    }
+                total += sum * (1.f / kLiftFactor);
+            } else if constexpr (kScaled) {
+                total += ((e[0] * c0[0] + e[1] * c1[0]) * sc[0][0] + (e[2] * c0[0] + e[3] * c1[0]) * sc[1][0]) * (1.f / kLiftFactor);
+            }
         };
         weigh();
         const bool over = !(total <= kLagLimit);
         if (__any_sync(0xffffffffu, over)) {
-            float a0 = m0, a1 = m1, b0 = v0, b1 = v1;
+            float a0 = m0, a1 = m1, b0[NG], b1[NG];
             a0 = fmaxf(a0, fmaxf(z[0], z[2]));
             a1 = fmaxf(a1, fmaxf(z[1], z[3]));
-            if (kScaled) {
-                float t0 = sc[0][0], t1 = sc[1][0];     // fmaxf leaves out a NaN
+            if constexpr (kScaled) {
 #pragma unroll
-                for (int g = 1; g < NG; ++g) { t0 = fmaxf(t0, sc[0][g]); t1 = fmaxf(t1, sc[1][g]); }
-                const float x0 = fast_log2(t0), x1 = fast_log2(t1);
-                b0 = fmaxf(b0, fmaxf(z[0] + x0, z[2] + x1));
-                b1 = fmaxf(b1, fmaxf(z[1] + x0, z[3] + x1));
+                for (int g = 0; g < NG; ++g) {          // fmaxf leaves out a NaN
+                    const float x0 = fast_log2(sc[0][g]), x1 = fast_log2(sc[1][g]);
+                    b0[g] = fmaxf(NG > 1 ? s_v[warp][g][h0] : v0, fmaxf(z[0] + x0, z[2] + x1));
+                    b1[g] = fmaxf(NG > 1 ? s_v[warp][g][h0 + 1] : v1, fmaxf(z[1] + x0, z[3] + x1));
+                }
             }
 #pragma unroll
             for (int o = 4; o < 32; o <<= 1) {
                 a0 = fmaxf(a0, __shfl_xor_sync(0xffffffffu, a0, o));
                 a1 = fmaxf(a1, __shfl_xor_sync(0xffffffffu, a1, o));
-                if (kScaled) {
-                    b0 = fmaxf(b0, __shfl_xor_sync(0xffffffffu, b0, o));
-                    b1 = fmaxf(b1, __shfl_xor_sync(0xffffffffu, b1, o));
+                if constexpr (kScaled) {
+#pragma unroll
+                    for (int g = 0; g < NG; ++g) {
+                        b0[g] = fmaxf(b0[g], __shfl_xor_sync(0xffffffffu, b0[g], o));
+                        b1[g] = fmaxf(b1[g], __shfl_xor_sync(0xffffffffu, b1[g], o));
+                    }
                 }
             }
             float r0 = fast_exp2(m0 - finite_ref(a0)), r1 = fast_exp2(m1 - finite_ref(a1));
@@ -564,34 +593,42 @@ __global__ void __launch_bounds__(kThreads, store_ctas(F)) gkv_store_attn_kernel
             l1 *= r1;
             m0 = a0; m1 = a1;
             n0 = finite_ref(m0); n1 = finite_ref(m1);
-            if (kScaled) {
-                b0 = fmaxf(b0, a0 - kScaleSpan);
-                b1 = fmaxf(b1, a1 - kScaleSpan);
-                r0 = fast_exp2(v0 - finite_ref(b0));
-                r1 = fast_exp2(v1 - finite_ref(b1));
-                v0 = b0; v1 = b1;
-                c0 = fast_exp2(n0 - finite_ref(v0) + kLift);
-                c1 = fast_exp2(n1 - finite_ref(v1) + kLift);
-            }
 #pragma unroll
-            for (int i = 0; i < 8; ++i) { acc[i][0] *= r0; acc[i][1] *= r1; acc[i][2] *= r0; acc[i][3] *= r1; }
+            for (int g = 0; g < NG; ++g) {
+                if constexpr (kScaled) {
+                    b0[g] = fmaxf(b0[g], a0 - kScaleSpan);
+                    b1[g] = fmaxf(b1[g], a1 - kScaleSpan);
+                    r0 = fast_exp2((NG > 1 ? s_v[warp][g][h0] : v0) - finite_ref(b0[g]));
+                    r1 = fast_exp2((NG > 1 ? s_v[warp][g][h0 + 1] : v1) - finite_ref(b1[g]));
+                    c0[g] = fast_exp2(n0 - finite_ref(b0[g]) + kLift);
+                    c1[g] = fast_exp2(n1 - finite_ref(b1[g]) + kLift);
+                }
+#pragma unroll
+                for (int i = g * (8 / NG); i < (g + 1) * (8 / NG); ++i) { acc[i][0] *= r0; acc[i][1] *= r1; acc[i][2] *= r0; acc[i][3] *= r1; }
+            }
+            if constexpr (NG > 1) {
+                __syncwarp();           // all lanes have read them
+                if (hq == 0)
+#pragma unroll
+                    for (int g = 0; g < NG; ++g) { s_v[warp][g][h0] = b0[g]; s_v[warp][g][h0 + 1] = b1[g]; }
+                __syncwarp();
+            } else if constexpr (kScaled) {
+                v0 = b0[0]; v1 = b1[0];
+            }
             weigh();
             n0 = m0; n1 = m1;           // as long as every logit was -infinity, the next step comes here again
         }
         l0 += e[0] + e[2];
         l1 += e[1] + e[3];
-        uint32_t b[NG][2];
         if constexpr (!kScaled) {
-            b[0][0] = movmatrix_trans(pack_weights<F>(e[0], e[1]));
-            b[0][1] = movmatrix_trans(pack_weights<F>(e[2], e[3]));
-        } else {
-            const float p0 = e[0] * c0, p1 = e[1] * c1, p2 = e[2] * c0, p3 = e[3] * c1;
-#pragma unroll
-            for (int g = 0; g < NG; ++g) {
-                b[g][0] = movmatrix_trans(pack_weights<F>(p0 * sc[0][g], p1 * sc[0][g]));
-                b[g][1] = movmatrix_trans(pack_weights<F>(p2 * sc[1][g], p3 * sc[1][g]));
-            }
+            b[0][0] = pack_weights<F>(e[0], e[1]);
+            b[0][1] = pack_weights<F>(e[2], e[3]);
+        } else if constexpr (NG == 1) {
+            b[0][0] = pack_weights<F>(e[0] * c0[0] * sc[0][0], e[1] * c1[0] * sc[0][0]);
+            b[0][1] = pack_weights<F>(e[2] * c0[0] * sc[1][0], e[3] * c1[0] * sc[1][0]);
         }
+#pragma unroll
+        for (int g = 0; g < NG; ++g) { b[g][0] = movmatrix_trans(b[g][0]); b[g][1] = movmatrix_trans(b[g][1]); }
         tile_values<F, NG>(tv, b, acc);
         load_tile_v<F>(tv, at, left_next, lane);
         left = left_next;
@@ -606,7 +643,12 @@ __global__ void __launch_bounds__(kThreads, store_ctas(F)) gkv_store_attn_kernel
     if (hq == 0) {
         s_m[warp][h0] = m0; s_m[warp][h0 + 1] = m1;
         s_l[warp][h0] = l0; s_l[warp][h0 + 1] = l1;
-        s_v[warp][h0] = kScaled ? v0 - kLift : m0; s_v[warp][h0 + 1] = kScaled ? v1 - kLift : m1;
+        if constexpr (NG > 1) {
+#pragma unroll
+            for (int g = 0; g < NG; ++g) { s_v[warp][g][h0] -= kLift; s_v[warp][g][h0 + 1] -= kLift; }
+        } else {
+            s_v[warp][0][h0] = kScaled ? v0 - kLift : m0; s_v[warp][0][h0 + 1] = kScaled ? v1 - kLift : m1;
+        }
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -615,37 +657,39 @@ __global__ void __launch_bounds__(kThreads, store_ctas(F)) gkv_store_attn_kernel
         *reinterpret_cast<float2*>(&s_o[warp][(d + 1) * 8 + h0]) = make_float2(acc[i][2], acc[i][3]);
     }
     __syncthreads();
-    if (threadIdx.x < 8) {
-        const int h = threadIdx.x;
+    if (threadIdx.x < 8 * NG) {                          // (every group works out the sums, the first leaves them)
+        const int h = threadIdx.x & 7, g = threadIdx.x >> 3;
         float m = -INFINITY, v = -INFINITY, l = 0.f;
-        for (int w = 0; w < kWarps; ++w) { m = fmaxf(m, s_m[w][h]); v = fmaxf(v, s_v[w][h]); }
+        for (int w = 0; w < kWarps; ++w) { m = fmaxf(m, s_m[w][h]); v = fmaxf(v, s_v[w][g][h]); }
         for (int w = 0; w < kWarps; ++w) {
             l += s_l[w][h] * fast_exp2(s_m[w][h] - finite_ref(m));
-            s_wgt[w][h] = fast_exp2(s_v[w][h] - finite_ref(v));
+            s_wgt[w][g][h] = fast_exp2(s_v[w][g][h] - finite_ref(v));
         }
-        s_fin[0][h] = m; s_fin[1][h] = l; s_fin[2][h] = v;
+        if (g == 0) { s_fin[0][h] = m; s_fin[1][h] = l; }
+        s_fin[2 + g][h] = v;
     }
     __syncthreads();
-    const int d = threadIdx.x;
+    const int d = threadIdx.x, dg = NG > 1 ? d / (kHeadDim / NG) : 0;
     float o[8];
 #pragma unroll
     for (int h = 0; h < 8; ++h) o[h] = 0.f;
 #pragma unroll
     for (int w = 0; w < kWarps; ++w) {
         const float4 a = *reinterpret_cast<const float4*>(&s_o[w][d * 8]), b = *reinterpret_cast<const float4*>(&s_o[w][d * 8 + 4]);
-        o[0] = fmaf(a.x, s_wgt[w][0], o[0]); o[1] = fmaf(a.y, s_wgt[w][1], o[1]); o[2] = fmaf(a.z, s_wgt[w][2], o[2]); o[3] = fmaf(a.w, s_wgt[w][3], o[3]);
-        o[4] = fmaf(b.x, s_wgt[w][4], o[4]); o[5] = fmaf(b.y, s_wgt[w][5], o[5]); o[6] = fmaf(b.z, s_wgt[w][6], o[6]); o[7] = fmaf(b.w, s_wgt[w][7], o[7]);
+        const float* f = s_wgt[w][dg];
+        o[0] = fmaf(a.x, f[0], o[0]); o[1] = fmaf(a.y, f[1], o[1]); o[2] = fmaf(a.z, f[2], o[2]); o[3] = fmaf(a.w, f[3], o[3]);
+        o[4] = fmaf(b.x, f[4], o[4]); o[5] = fmaf(b.y, f[5], o[5]); o[6] = fmaf(b.z, f[6], o[6]); o[7] = fmaf(b.w, f[7], o[7]);
     }
     if (MODE == kPart || MODE == kDealt) {
         float* rec = p.own_part + (size_t)blockIdx.x * kOwnRecFloats;
-        if (d < 8) { rec[d] = s_fin[0][d]; rec[8 + d] = s_fin[1][d]; rec[16 + d] = s_fin[2][d]; }
+        if (d < 16 + 8 * NG) rec[d] = s_fin[d >> 3][d & 7];
         // [dim / 4][head][4], by way of shared memory
         __syncthreads();                              // the warps' accumulators have been read
         float* mine = &s_o[0][0];
 #pragma unroll
         for (int h = 0; h < 8; ++h) mine[((d >> 2) * 8 + h) * 4 + (d & 3)] = o[h];
         __syncthreads();
-        float4* ro = reinterpret_cast<float4*>(rec + 32);
+        float4* ro = reinterpret_cast<float4*>(rec + kOwnRecHead);
 #pragma unroll
         for (int i = 0; i < 2; ++i) ro[i * kThreads + d] = *reinterpret_cast<const float4*>(mine + (i * kThreads + d) * 4);
         // The merge waits for this kernel only, so this kernel may not end before the prefixes' does.
@@ -660,34 +704,36 @@ __global__ void __launch_bounds__(kThreads, store_ctas(F)) gkv_store_attn_kernel
 #pragma unroll
         for (int h = 0; h < 8; ++h) mine[h * kHeadDim + d] = o[h];
         cluster_sync_all();
-        if (d < 8) {
+        if (d < 8 * NG) {
+            const int h = d & 7, g = d >> 3;
             float m = -INFINITY, v = -INFINITY, l = 0.f;
             float pm[kMaxCluster], pl[kMaxCluster], pv[kMaxCluster];
 #pragma unroll
             for (int r = 0; r < kMaxCluster; ++r) {
                 const bool in = r < p.splits;
-                const uint32_t at = cluster_map_shared(smem_u32(&s_fin[0][d]), in ? r : 0);
+                const uint32_t at = cluster_map_shared(smem_u32(&s_fin[0][h]), in ? r : 0);
                 pm[r] = in ? ld_cluster_f32(at) : -INFINITY;
                 pl[r] = in ? ld_cluster_f32(at + 32) : 0.f;
-                pv[r] = in ? ld_cluster_f32(at + 64) : -INFINITY;
+                pv[r] = in ? ld_cluster_f32(at + 64 + 32 * g) : -INFINITY;
                 m = fmaxf(m, pm[r]);
                 v = fmaxf(v, pv[r]);
             }
 #pragma unroll
             for (int r = 0; r < kMaxCluster; ++r) {
                 l += pl[r] * fast_exp2(pm[r] - finite_ref(m));
-                s_cl[r][d] = fast_exp2(pv[r] - finite_ref(v));
+                s_cl[r][g][h] = fast_exp2(pv[r] - finite_ref(v));
             }
-            s_norm[0][d] = m; s_norm[1][d] = l; s_norm[2][d] = v;
+            if (g == 0) { s_norm[0][h] = m; s_norm[1][h] = l; }
+            s_norm[2 + g][h] = v;
         }
         __syncthreads();
         for (int i = split * kThreads + d; i < p.g * kHeadDim; i += p.splits * kThreads) {
-            const int h = i / kHeadDim;
+            const int h = i / kHeadDim, g = NG > 1 ? i % kHeadDim / (kHeadDim / NG) : 0;
             float x = 0.f;
             for (int r = 0; r < p.splits; ++r)
-                x = fmaf(ld_cluster_f32(cluster_map_shared(smem_u32(&mine[i]), r)), s_cl[r][h], x);
+                x = fmaf(ld_cluster_f32(cluster_map_shared(smem_u32(&mine[i]), r)), s_cl[r][g][h], x);
             p.out[((size_t)seq * p.h_q + (size_t)head * p.g) * kHeadDim + i] =
-                __float2bfloat16_rn(final_value(x, s_norm[0][h], s_norm[1][h], s_norm[2][h], fits));
+                __float2bfloat16_rn(final_value(x, s_norm[0][h], s_norm[1][h], s_norm[2 + g][h], fits));
         }
         if (p.lse && split == 0 && d < p.g)
             p.lse[(size_t)seq * p.h_q + (size_t)head * p.g + d] = final_lse(s_norm[0][d], s_norm[1][d], fits);
@@ -697,19 +743,21 @@ __global__ void __launch_bounds__(kThreads, store_ctas(F)) gkv_store_attn_kernel
     __nv_bfloat16* orow = p.out + ((size_t)seq * p.h_q + (size_t)head * p.g) * kHeadDim + d;
 #pragma unroll
     for (int h = 0; h < 8; ++h)
-        if (h < p.g) orow[(size_t)h * kHeadDim] = __float2bfloat16_rn(final_value(o[h], s_fin[0][h], s_fin[1][h], s_fin[2][h], fits));
+        if (h < p.g) orow[(size_t)h * kHeadDim] = __float2bfloat16_rn(final_value(o[h], s_fin[0][h], s_fin[1][h], s_fin[2 + dg][h], fits));
     if (p.lse && d < p.g) p.lse[(size_t)seq * p.h_q + (size_t)head * p.g + d] = final_lse(s_fin[0][d], s_fin[1][d], fits);
 }
 
 // Joins the partial results of a unit: those of its own pieces and, with a prefix, those of the prefix items that hold its
 // query rows. 2^ds CTAs per unit, each with a share of the dimensions; thread t holds head t & 7 of four dimensions over every
 // (slices)th of the parts, so that 8 lanes read 128 contiguous bytes of a record. The statistics of all parts are loaded at once,
-// the values of 8 parts at a time: the kernel is a few trips to L2.
-template <bool DEALT>
+// the values of 8 parts at a time: the kernel is a few trips to L2. NG groups of dimensions have maxima v of their own.
+template <bool DEALT, int NG>
 __global__ void __launch_bounds__(1024) gkv_store_merge_kernel(const StoreAttnLaunch p, const int ds) {
-    extern __shared__ float s_part[];                // [parts][8] factors
+    // factors: own parts [part][group][8], then those of the prefix (with several groups: their maxima, a factor is worked out
+    // where it is used) [part][8]
+    extern __shared__ float s_part[];
     __shared__ __align__(16) float s_red[4 * 1024];
-    __shared__ float s_fin[3][8];
+    __shared__ float s_fin[2 + NG][8];
     const int unit = blockIdx.x >> ds, share = blockIdx.x & ((1 << ds) - 1), seq = unit / p.h_kv, head = unit - seq * p.h_kv;
     const int t = threadIdx.x, slices = blockDim.x >> (8 - ds), slice = t >> (8 - ds), h = t & 7;
     const int d4 = ((t >> 3) & ((32 >> ds) - 1)) + share * (32 >> ds);
@@ -748,51 +796,91 @@ __global__ void __launch_bounds__(1024) gkv_store_merge_kernel(const StoreAttnLa
         if (len < 0) return;
         fits = p.k_new ? len < p.capacity : len <= p.capacity;
     } else {
-        const float state = own[24];
+        const float state = own[kOwnRecState];
         if (state == kPieceLeftOut) return;
         fits = state == kPieceOk;
     }
 
     // ---- statistics: factors of all parts. Thread t has head t & 7 of parts t / 8, t / 8 + blockDim / 8, ...
     const int hops = (parts * 8 + (int)blockDim.x - 1) / (int)blockDim.x;
-    float m = -INFINITY, v = -INFINITY, l = 0.f, x[kMergeHops], y[kMergeHops], z[kMergeHops];
+    float m = -INFINITY, v[NG], l = 0.f, x[kMergeHops], y[kMergeHops][NG], z[kMergeHops];
+#pragma unroll
+    for (int g = 0; g < NG; ++g) v[g] = -INFINITY;
 #pragma unroll
     for (int k = 0; k < kMergeHops; ++k) {
-        x[k] = y[k] = -INFINITY;
+        x[k] = -INFINITY;
         z[k] = 0.f;
+#pragma unroll
+        for (int g = 0; g < NG; ++g) y[k][g] = -INFINITY;
         const int part = (t + k * (int)blockDim.x) >> 3;
         if (k < hops && part < parts) {
             if (part < n_own) {
                 const float* r = own + (size_t)part * kOwnRecFloats + hc;
-                x[k] = r[0]; z[k] = r[8]; y[k] = r[16];
+                x[k] = r[0]; z[k] = r[8];
+#pragma unroll
+                for (int g = 0; g < NG; ++g) y[k][g] = r[16 + 8 * g];
             } else {
                 const float* r = pre_stats(part - n_own) + hc;
-                x[k] = y[k] = r[0]; z[k] = r[kPrefixRows];
+                x[k] = r[0]; z[k] = r[kPrefixRows];
+#pragma unroll
+                for (int g = 0; g < NG; ++g) y[k][g] = x[k];
             }
         }
         m = fmaxf(m, x[k]);
-        v = fmaxf(v, y[k]);
-    }
 #pragma unroll
-    for (int o = 8; o < 32; o <<= 1) { m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o)); v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o)); }
-    if ((t & 31) < 8) { s_red[(t >> 5) * 16 + h] = m; s_red[(t >> 5) * 16 + 8 + h] = v; }
+        for (int g = 0; g < NG; ++g) v[g] = fmaxf(v[g], y[k][g]);
+    }
+    constexpr int kStats = 8 * (1 + NG);             // a warp's maxima
+#pragma unroll
+    for (int o = 8; o < 32; o <<= 1) {
+        m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+#pragma unroll
+        for (int g = 0; g < NG; ++g) v[g] = fmaxf(v[g], __shfl_xor_sync(0xffffffffu, v[g], o));
+    }
+    if ((t & 31) < 8) {
+        s_red[(t >> 5) * kStats + h] = m;
+#pragma unroll
+        for (int g = 0; g < NG; ++g) s_red[(t >> 5) * kStats + 8 + 8 * g + h] = v[g];
+    }
     __syncthreads();
-    for (int i = 0; i < warps; ++i) { m = fmaxf(m, s_red[i * 16 + h]); v = fmaxf(v, s_red[i * 16 + 8 + h]); }
-    const float mr = finite_ref(m), vr = finite_ref(v);
+    if constexpr (NG == 1) {
+        for (int i = 0; i < warps; ++i) { m = fmaxf(m, s_red[i * kStats + h]); v[0] = fmaxf(v[0], s_red[i * kStats + 8 + h]); }
+    } else {                                         // one thread a number
+        if (t < kStats) {
+            float a = -INFINITY;
+            for (int i = 0; i < warps; ++i) a = fmaxf(a, s_red[i * kStats + t]);
+            s_fin[t < 8 ? 0 : 1 + (t >> 3)][h] = a;
+        }
+        __syncthreads();
+        m = s_fin[0][h];
+#pragma unroll
+        for (int g = 0; g < NG; ++g) v[g] = s_fin[2 + g][h];
+    }
+    const float mr = finite_ref(m);
+    constexpr int kSums = 2048;                      // (the maxima take up to 32 kStats)
+    static_assert(32 * kStats <= kSums && kSums + 32 * 8 <= 4 * 1024, "scratch");
 #pragma unroll
     for (int k = 0; k < kMergeHops; ++k) {
-        const int i = t + k * (int)blockDim.x;
+        const int i = t + k * (int)blockDim.x, part = i >> 3;
         l += z[k] * fast_exp2(x[k] - mr);            // (a NaN sum comes with a maximum of -infinity)
-        if (k < hops && i < parts * 8) s_part[i] = x[k] == -INFINITY ? 0.f : fast_exp2(y[k] - vr);   // 0: no key, values may be missing
+        if (k < hops && part < parts) {              // 0: no key, values may be missing
+            if (NG == 1 || part < n_own) {
+#pragma unroll
+                for (int g = 0; g < NG; ++g) s_part[(part * NG + g) * 8 + h] = x[k] == -INFINITY ? 0.f : fast_exp2(y[k][g] - finite_ref(v[g]));
+            } else {
+                s_part[(n_own * (NG - 1) + part) * 8 + h] = x[k];
+            }
+        }
     }
 #pragma unroll
     for (int o = 8; o < 32; o <<= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
-    if ((t & 31) < 8) s_red[1024 + (t >> 5) * 8 + h] = l;
+    if ((t & 31) < 8) s_red[kSums + (t >> 5) * 8 + h] = l;
     __syncthreads();
     if (t < 8) {
         float sum = 0.f;
-        for (int i = 0; i < warps; ++i) sum += s_red[1024 + i * 8 + h];
-        s_fin[0][h] = m; s_fin[1][h] = sum; s_fin[2][h] = v;
+        for (int i = 0; i < warps; ++i) sum += s_red[kSums + i * 8 + h];
+        s_fin[1][h] = sum;
+        if (NG == 1) { s_fin[0][h] = m; s_fin[2][h] = v[0]; }
     }
 
     // ---- values
@@ -800,11 +888,13 @@ __global__ void __launch_bounds__(1024) gkv_store_merge_kernel(const StoreAttnLa
     auto add = [&](float w, const float4& a) {
         if (w != 0.f) { o.x = fmaf(a.x, w, o.x); o.y = fmaf(a.y, w, o.y); o.z = fmaf(a.z, w, o.z); o.w = fmaf(a.w, w, o.w); }
     };
-    const float4* ov = reinterpret_cast<const float4*>(own + 32) + d4 * 8 + h;
+    const int dg = NG > 1 ? d4 / (kHeadDim / 4 / NG) : 0;
+    const float vr = finite_ref(NG > 1 ? s_fin[2 + dg][h] : v[0]);
+    const float4* ov = reinterpret_cast<const float4*>(own + kOwnRecHead) + d4 * 8 + h;
 #pragma unroll 4
     for (int i = slice; i < n_own; i += slices) {
         const float4 a = ov[(size_t)i * (kOwnRecFloats / 4)];
-        add(s_part[i * 8 + h], a);
+        add(s_part[(i * NG + dg) * 8 + h], a);
     }
     const int n_pre = items << twice;
     for (int i0 = slice; i0 < n_pre; i0 += 8 * slices) {
@@ -813,7 +903,10 @@ __global__ void __launch_bounds__(1024) gkv_store_merge_kernel(const StoreAttnLa
         for (int k = 0; k < 8; ++k) a[k] = pre_values(min(i0 + k * slices, n_pre - 1))[d4 * kPrefixRows + hc];
 #pragma unroll
         for (int k = 0; k < 8; ++k)
-            if (i0 + k * slices < n_pre) add(s_part[(n_own + i0 + k * slices) * 8 + h], a[k]);
+            if (i0 + k * slices < n_pre) {
+                const float f = s_part[(n_own * NG + i0 + k * slices) * 8 + h];
+                add(NG == 1 ? f : f == -INFINITY ? 0.f : fast_exp2(f - vr), a[k]);
+            }
     }
     if (slices > 1) {
         __syncthreads();
@@ -828,7 +921,7 @@ __global__ void __launch_bounds__(1024) gkv_store_merge_kernel(const StoreAttnLa
         __syncthreads();
     }
     if (slice == 0 && h < p.g) {
-        const float fm = s_fin[0][h], fl = s_fin[1][h], fv = s_fin[2][h];
+        const float fm = s_fin[0][h], fl = s_fin[1][h], fv = s_fin[2 + dg][h];
         *reinterpret_cast<uint2*>(p.out + ((size_t)seq * p.h_q + (size_t)head * p.g + h) * kHeadDim + 4 * d4) =
             make_uint2(pack_bf16x2(final_value(o.x, fm, fl, fv, fits), final_value(o.y, fm, fl, fv, fits)),
                        pack_bf16x2(final_value(o.z, fm, fl, fv, fits), final_value(o.w, fm, fl, fv, fits)));
@@ -891,10 +984,12 @@ cudaError_t launch_store_merge(const StoreAttnLaunch& p, cudaStream_t s) {
     int longest = 0;
     for (int i = 0; i < p.n_prefix; ++i) longest = p.prefix_len[i] > longest ? p.prefix_len[i] : longest;
     const int items = p.prefix_part ? ((longest + 127) / 128 + p.chunk - 1) / p.chunk * (p.two_tiles ? 1 : 2) : 0;
-    const int parts = (p.dealt ? min(p.batch * p.splits, kMaxPieces) : p.splits) + items, units = p.batch * p.h_kv, ds = units <= 40 ? 2 : units <= 80 ? 1 : 0;
+    const int own = p.dealt ? min(p.batch * p.splits, kMaxPieces) : p.splits, parts = own + items, units = p.batch * p.h_kv;
+    const int ds = units <= 40 ? 2 : units <= 80 ? 1 : 0, ng = value_groups(p.format);
     const unsigned threads = p.dealt ? (units <= 148 ? 1024u : units <= 296 ? 512u : 256u) : parts <= 8 ? 256u : parts <= 16 ? 512u : 1024u;
-    return launch_ex(p.dealt ? gkv_store_merge_kernel<true> : gkv_store_merge_kernel<false>, (unsigned)units << ds, threads, (size_t)parts * 8 * sizeof(float), 1,
-                     true, s, p, ds);
+    const auto kernel = ng == 1 ? (p.dealt ? gkv_store_merge_kernel<true, 1> : gkv_store_merge_kernel<false, 1>)
+                                : (p.dealt ? gkv_store_merge_kernel<true, 4> : gkv_store_merge_kernel<false, 4>);
+    return launch_ex(kernel, (unsigned)units << ds, threads, (size_t)(own * ng + items) * 8 * sizeof(float), 1, true, s, p, ds);
 }
 
 }  // namespace gkv

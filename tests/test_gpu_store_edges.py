@@ -1,11 +1,12 @@
-"""Key/value stores at the ends of their documented range: tokens and rows at the ends of 32 bits."""
+"""Key/value stores at the ends of their documented range: tokens and rows at the ends of 32 bits, groups of a 4-bit row that differ by
+many powers of two."""
 import numpy as np
 import pytest
 import torch
 
 import paper_2512_00504_b200 as gkv
 import store_reference as ref
-from test_gpu_store import DEV, FORMATS, expect_codes, f64, gen, ints, randn, raw
+from test_gpu_store import DEV, FORMATS, dequantised, expect_codes, f64, gen, ints, randn, raw
 
 pytestmark = pytest.mark.gpu
 
@@ -58,3 +59,45 @@ def test_first_and_count_at_the_ends_of_32_bits(fmt):
         if fmt != "bf16":
             want = ref.round_bf16(ref.values(*ref.encode(want, fmt), fmt))
         assert (f64(out[i])[got] == want).all()
+
+
+# Groups of a 4-bit row differ by powers of two: the rest, one far below it, one far above, and one that differs from key to key.
+def rows_of_uneven_groups(g, shape, exponent):
+    x = randn(g, *shape)
+    x[..., 32:64] *= 2.0 ** -exponent
+    x[..., 64:96] *= 2.0 ** (exponent // 3)
+    x[..., 96:] *= torch.exp2(torch.randint(-exponent, 1, shape[:-1] + (1,), generator=g, device=DEV).float()).to(torch.bfloat16)
+    return x
+
+
+@pytest.mark.parametrize("append", [False, True])
+@pytest.mark.parametrize("exponent", [12, 30, 48, 96])
+@pytest.mark.parametrize("B,H,C,m", [(300, 2, 40, 0), (2, 1, 300, 0), (1, 1, 4000, 0), (3, 2, 9000, 0), (4, 1, 130, 200), (2, 1, 130, 0)],
+                         ids=["whole", "cluster", "pieces", "dealt", "prefix", "small"])
+def test_groups_of_very_different_size(B, H, C, m, exponent, append):
+    """Each group of 32 dimensions is as precise as if it were alone: the tolerance of a group counts that group's values only."""
+    g, rng = gen(17 + exponent), np.random.RandomState(exponent)
+    Hq = 4 * H
+    st = gkv.KVStore("int4", batch=B, h_q=Hq, h_kv=H, capacity=C, device=DEV, n_prefix=1 if m else 0, max_prefix=m)
+    lens = rng.randint(0, C, B)
+    lens[0], lens[-1] = C - 1, C - 1
+    st.write(randn(g, B, C, H, 128), rows_of_uneven_groups(g, (B, C, H, 128), exponent))
+    q, out, lse = randn(g, B, Hq, 128), torch.empty((B, Hq, 128), dtype=torch.bfloat16, device=DEV), torch.empty((B, Hq), device=DEV)
+    new = dict(k_new=randn(g, B, H, 128), v_new=rows_of_uneven_groups(g, (B, H, 128), exponent)) if append else {}
+    kp, vp = randn(g, 1, H, m, 128), rows_of_uneven_groups(g, (1, H, m, 128), exponent)
+    st.attn(ints(lens.tolist()), q, out, lse=lse, prefix=gkv.Prefix(kp, vp, [m]) if m else None, **new)
+    K, V = dequantised(st)
+    lens = lens + append
+    out, lse, q, kp, vp = f64(out), f64(lse), f64(q), f64(kp), f64(vp)
+    for b in range(B):
+        for h in range(H):
+            heads, n = slice(4 * h, 4 * h + 4), lens[b]
+            for i in range(4):
+                d = slice(32 * i, 32 * i + 32)
+                pre = (kp[0, h], vp[0, h, :, d]) if m else (None, None)
+                if n + m == 0:
+                    assert (out[b, heads] == 0).all() and (lse[b, heads] == -np.inf).all()
+                    continue
+                want, l, tol, ltol = ref.attend(q[b, heads], K[b, h, :n], V[b, h, :n, d], *pre)
+                assert (np.abs(out[b, heads, d] - want) <= tol).all(), (b, h, i, np.abs(out[b, heads, d] - want).max() / np.abs(want).max())
+                assert (np.abs(lse[b, heads] - l) <= ltol).all()
