@@ -389,7 +389,8 @@ gkv_status gkv_store_attn_workspace(const gkv_store* store, int32_t n_prefix, in
  *            len[i] and attended to as it stands there. The caller then counts len[i] up.
  *   prefix   NULL: none
  *   lse      device, fp32 [batch][n_q_heads], or NULL: the natural logarithm of the sum of exp(scaled logits)
- * A sequence with nothing to attend to gets out = 0 and lse = -infinity.
+ * A sequence with nothing to attend to gets out = 0 and lse = -infinity. (A bounded wait of the prefix kernel that expires cannot be
+ * polled through this entry point, which has no state: out and lse of its sequences are NaN then.)
  * Errors: as gkv_store_query_sizes; INVALID_ARG (NULL or misaligned pointer, only one of k_new and v_new, max_len outside
  * 0..capacity, n_prefix outside 1..64 or not a divisor of batch, a prefix length outside 0..rows, workspace_bytes too small),
  * UNSUPPORTED (2^31 prefix rows or more over all prefixes and heads), CUDA. */
@@ -400,10 +401,16 @@ gkv_status gkv_store_attn(const gkv_store* store, const int32_t* len, int32_t ma
 /* gkv_decode_attn of one layer with a shared prefix in front of the compressed cache: append, attention over the prefix and
  * the cache, len += 1. The prefix is not part of the cache and is never evicted. Window scores are not accumulated: a
  * compression is scored from q_window, over the cached keys alone. Workspace: gkv_store_attn_workspace of a GKV_STORE_BF16
- * store with this context's batch, heads and C as capacity (16-byte aligned, as there).
+ * store with this context's batch, heads and C as capacity (16-byte aligned, as there). A bounded wait that expires is latched for
+ * gkv_poll_device_status; out is NaN then.
  * Errors: as gkv_decode_attn and gkv_store_attn; INVALID_ARG (layer = -1, prefix == NULL), STATE (fuse_window_scores is on). */
 gkv_status gkv_decode_attn_prefix(gkv_ctx* ctx, int32_t layer, const void* q, const void* k_new, const void* v_new,
                                   const gkv_prefix* prefix, void* out, void* workspace, uint64_t workspace_bytes, void* stream);
+
+/* Self-test of that: the context's next gkv_decode_attn_prefix takes the waits of its prefix kernel for expired, so that
+ * it gives up, latches the status word and ends as it would then (nothing traps, faults or hangs; a prefix without rows has no
+ * such kernel). Errors: INVALID_ARG. */
+gkv_status gkv_selftest_prefix_wait(gkv_ctx* ctx);
 
 /* Memory model of the paper's appendix "Memory Analysis": bytes of the full KV cache at
  * seq_len tokens, of the compressed cache ((b + s) rows instead of seq_len), and of the score

@@ -175,8 +175,9 @@ def lib() -> ctypes.CDLL:
         L.gkv_store_attn_workspace.argtypes = [P(gkv_store), i32, i32, P(u64)]
         L.gkv_store_attn.argtypes = [P(gkv_store), vp, i32, vp, vp, vp, P(gkv_prefix), vp, vp, vp, u64, vp]
         L.gkv_decode_attn_prefix.argtypes = [vp, i32, vp, vp, vp, P(gkv_prefix), vp, vp, u64, vp]
+        L.gkv_selftest_prefix_wait.argtypes = [vp]
         for name in ("gkv_store_query_sizes", "gkv_store_write", "gkv_store_read", "gkv_store_attn_workspace",
-                     "gkv_store_attn", "gkv_decode_attn_prefix"):
+                     "gkv_store_attn", "gkv_decode_attn_prefix", "gkv_selftest_prefix_wait"):
             getattr(L, name).restype = ctypes.c_int
         L.gkv_strerror.argtypes = [ctypes.c_int]
         L.gkv_strerror.restype = ctypes.c_char_p
@@ -376,6 +377,10 @@ def gkv_decode_attn_prefix(ctx, layer, q, k_new, v_new, prefix, out, workspace):
     workspace: a uint8 tensor of gkv_store_attn_workspace bytes (GKVCache.prefix_workspace)."""
     _check(lib().gkv_decode_attn_prefix(ctx, layer, _ptr(q), _ptr(k_new), _ptr(v_new), ctypes.byref(prefix.desc), _ptr(out),
                                         _ptr(workspace), workspace.numel(), _stream()), "gkv_decode_attn_prefix")
+
+
+def gkv_selftest_prefix_wait(ctx):
+    _check(lib().gkv_selftest_prefix_wait(ctx), "gkv_selftest_prefix_wait")
 
 
 # ------------------------------------------------------------------ buffer holder

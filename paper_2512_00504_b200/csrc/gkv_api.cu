@@ -347,6 +347,7 @@ gkv_status gkv_init(gkv_ctx** out, const gkv_config* cfg, const gkv_buffers* b, 
     ctx->g = cfg->n_q_heads / cfg->n_kv_heads;
     ctx->units_per_layer = cfg->batch * cfg->n_kv_heads;
     ctx->launches = 0;
+    ctx->prefix_give_up = 0;
     ctx->evict_log = nullptr;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     bool ok = cudaGetDevice(&ctx->device) == cudaSuccess &&

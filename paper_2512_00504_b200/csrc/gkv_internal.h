@@ -162,6 +162,8 @@ struct StoreAttnLaunch {
     int dealt;               // the pieces are dealt out by the lengths instead: batch * splits per head over all sequences
     float scale_log2;
     // shared prefixes
+    int32_t* status;                // a context's status word, where an expired wait is latched; NULL: it shows as NaN alone
+    int give_up;                    // the prefix kernel takes its waits for expired (self-test)
     const __nv_bfloat16 *k_prefix, *v_prefix;
     int n_prefix, prefix_rows, seqs_per_prefix;
     int seqs_per_block, n_blocks;   // sequences of a row block; row blocks of a (prefix, KV head)
@@ -184,6 +186,7 @@ struct gkv_ctx {
     CUtensorMap tm_k128;          // 128-row boxes (the tensor-core scoring kernel's key tiles)
     std::vector<int32_t> len, n_hist, since_evict, sacc_valid, stage_next, cbar_valid;
     int64_t launches;
+    int prefix_give_up;   // the next prefix launch takes its waits for expired (self-test)
     int32_t* evict_log;  // caller's device buffer for the eviction log, or NULL
     gkv_sizes sizes;
 };

@@ -171,7 +171,7 @@ gkv_prefix_attn_kernel(const StoreAttnLaunch p, const __grid_constant__ CUtensor
         for (int s = 0; s < 2; ++s) mbar_init(smem_u32(&tail->s_full[s]), 1);
         for (int s = 0; s < 4; ++s) mbar_init(smem_u32(&tail->p_ready[s >> 1][s & 1]), kPxSoftmax / 2);
         mbar_init(smem_u32(&tail->o_full), 1);
-        tail->abort_flag = 0;
+        tail->abort_flag = p.give_up;
         tail->overflow = 0;
         tail->issued = 0;
         fence_mbar_init();
@@ -416,6 +416,10 @@ gkv_prefix_attn_kernel(const StoreAttnLaunch p, const __grid_constant__ CUtensor
     }
     __syncthreads();
     if (*(volatile int*)&tail->abort_flag && tid == 0) {
+        if (p.status && atomicCAS(p.status, 0, kStatusTimeout) == 0) {
+            p.status[1] = 50;
+            p.status[2] = blockIdx.x;
+        }
         // copies and products that are still in flight get a bounded time to end before the CTA does
         const int issued = *(volatile int*)&tail->issued;
         for (int pos = max(0, issued - kPxSlots); pos < issued; ++pos)

@@ -298,6 +298,12 @@ gkv_status gkv_store_attn(const gkv_store* store, const int32_t* len, int32_t ma
                     static_cast<cudaStream_t>(stream), &launches);
 }
 
+gkv_status gkv_selftest_prefix_wait(gkv_ctx* ctx) {
+    if (!ctx) return GKV_ERR_INVALID_ARG;
+    ctx->prefix_give_up = 1;
+    return GKV_OK;
+}
+
 gkv_status gkv_decode_attn_prefix(gkv_ctx* ctx, int32_t layer, const void* q, const void* k_new, const void* v_new,
                                   const gkv_prefix* prefix, void* out, void* workspace, uint64_t workspace_bytes, void* stream) {
     if (!ctx || layer < 0 || layer >= ctx->cfg.n_layers || !q || !k_new || !v_new || !out || !prefix) return GKV_ERR_INVALID_ARG;
@@ -319,6 +325,8 @@ gkv_status gkv_decode_attn_prefix(gkv_ctx* ctx, int32_t layer, const void* q, co
     p.q = static_cast<const __nv_bfloat16*>(q);
     p.k_new = static_cast<const __nv_bfloat16*>(k_new); p.v_new = static_cast<const __nv_bfloat16*>(v_new);
     p.out = static_cast<__nv_bfloat16*>(out);
+    p.status = reinterpret_cast<int32_t*>(static_cast<uint8_t*>(ctx->buf.workspace) + ctx->ws.status);
+    p.give_up = ctx->prefix_give_up;
     p.format = GKV_STORE_BF16; p.batch = c.batch; p.h_q = c.n_q_heads; p.h_kv = c.n_kv_heads; p.g = ctx->g; p.capacity = ctx->C;
     p.scale_log2 = (float)(1.4426950408889634 / sqrt((double)kHeadDim));
     int launches = 0;
@@ -326,6 +334,7 @@ gkv_status gkv_decode_attn_prefix(gkv_ctx* ctx, int32_t layer, const void* q, co
                                   static_cast<cudaStream_t>(stream), &launches);
     ctx->launches += launches;
     if (r != GKV_OK) return r;
+    ctx->prefix_give_up = 0;
     ctx->len[layer] += 1;
     ctx->since_evict[layer] += 1;
     ctx->stage_next[layer] = 0;

@@ -67,3 +67,8 @@ def test_lengths_of_a_prefix():
     assert list(gkv.Prefix(OnDevice(2, 2, 64, 128), OnDevice(2, 2, 64, 128), [3, torch.tensor(64)])._len) == [3, 64]
     with pytest.raises(ValueError, match="lengths"):
         gkv.Prefix(OnDevice(2, 2, 64, 128), OnDevice(2, 2, 64, 128), [3])
+
+
+def test_self_test_of_the_wait_needs_a_context():
+    gkv.build_library()
+    assert gkv.lib().gkv_selftest_prefix_wait(None) == gkv.GKV_ERR_INVALID_ARG
