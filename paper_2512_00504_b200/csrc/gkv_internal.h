@@ -147,6 +147,7 @@ struct StoreCopyLaunch {       // write / read
     int batch, h_kv, capacity, n_tokens, format;
 };
 
+// (448 bytes: with 464 a launch costs the host 0.5 us more, 4.9 -> 5.4. What the prefix kernel alone needs is passed to it beside this.)
 struct StoreAttnLaunch {
     uint8_t *k, *v;
     __nv_bfloat16 *k_scale, *v_scale;
@@ -162,8 +163,6 @@ struct StoreAttnLaunch {
     int dealt;               // the pieces are dealt out by the lengths instead: batch * splits per head over all sequences
     float scale_log2;
     // shared prefixes
-    int32_t* status;                // a context's status word, where an expired wait is latched; NULL: it shows as NaN alone
-    int give_up;                    // the prefix kernel takes its waits for expired (self-test)
     const __nv_bfloat16 *k_prefix, *v_prefix;
     int n_prefix, prefix_rows, seqs_per_prefix;
     int seqs_per_block, n_blocks;   // sequences of a row block; row blocks of a (prefix, KV head)
@@ -171,6 +170,11 @@ struct StoreAttnLaunch {
     int chunk;                      // 128-key tiles of a prefix item
     int prefix_items;
     int32_t prefix_len[kMaxPrefixes];
+};
+
+struct PrefixWatch {
+    int32_t* status;   // a context's status word, where an expired wait is latched; NULL: it shows as NaN alone
+    int give_up;       // take the waits for expired (self-test)
 };
 
 }  // namespace gkv
@@ -219,7 +223,7 @@ cudaError_t score_kernel_setup();
 cudaError_t launch_store_write(const StoreCopyLaunch& p, cudaStream_t s);
 cudaError_t launch_store_read(const StoreCopyLaunch& p, cudaStream_t s);
 cudaError_t launch_store_attn(const StoreAttnLaunch& p, cudaStream_t s);                    // a unit's own rows
-cudaError_t launch_prefix_attn(const StoreAttnLaunch& p, const CUtensorMap& tm_k, const CUtensorMap& tm_v, cudaStream_t s);
+cudaError_t launch_prefix_attn(const StoreAttnLaunch& p, const PrefixWatch& watch, const CUtensorMap& tm_k, const CUtensorMap& tm_v, cudaStream_t s);
 int store_attn_ctas_per_sm(int format);                                                      // of launch_store_attn
 bool store_needs_merge(const StoreAttnLaunch& p);                                           // partial results go through the workspace
 cudaError_t launch_store_merge(const StoreAttnLaunch& p, cudaStream_t s);

@@ -123,7 +123,7 @@ __device__ __forceinline__ void mask_block(float (&z)[32], int key0, int valid) 
 }
 
 __global__ void __maxnreg__(80)
-gkv_prefix_attn_kernel(const StoreAttnLaunch p, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v) {
+gkv_prefix_attn_kernel(const StoreAttnLaunch p, const PrefixWatch watch, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v) {
     grid_launch_dependents();   // the attention over own rows takes the SMs as they fall free
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -171,7 +171,7 @@ gkv_prefix_attn_kernel(const StoreAttnLaunch p, const __grid_constant__ CUtensor
         for (int s = 0; s < 2; ++s) mbar_init(smem_u32(&tail->s_full[s]), 1);
         for (int s = 0; s < 4; ++s) mbar_init(smem_u32(&tail->p_ready[s >> 1][s & 1]), kPxSoftmax / 2);
         mbar_init(smem_u32(&tail->o_full), 1);
-        tail->abort_flag = p.give_up;
+        tail->abort_flag = watch.give_up;
         tail->overflow = 0;
         tail->issued = 0;
         fence_mbar_init();
@@ -416,9 +416,9 @@ gkv_prefix_attn_kernel(const StoreAttnLaunch p, const __grid_constant__ CUtensor
     }
     __syncthreads();
     if (*(volatile int*)&tail->abort_flag && tid == 0) {
-        if (p.status && atomicCAS(p.status, 0, kStatusTimeout) == 0) {
-            p.status[1] = 50;
-            p.status[2] = blockIdx.x;
+        if (watch.status && atomicCAS(watch.status, 0, kStatusTimeout) == 0) {
+            watch.status[1] = 50;
+            watch.status[2] = blockIdx.x;
         }
         // copies and products that are still in flight get a bounded time to end before the CTA does
         const int issued = *(volatile int*)&tail->issued;
@@ -433,13 +433,13 @@ gkv_prefix_attn_kernel(const StoreAttnLaunch p, const __grid_constant__ CUtensor
     }
 }
 
-cudaError_t launch_prefix_attn(const StoreAttnLaunch& p, const CUtensorMap& tm_k, const CUtensorMap& tm_v, cudaStream_t s) {
+cudaError_t launch_prefix_attn(const StoreAttnLaunch& p, const PrefixWatch& watch, const CUtensorMap& tm_k, const CUtensorMap& tm_v, cudaStream_t s) {
     // a property of the function on the current device; setting it again costs less than finding out whether it is set
     // (All of the SM's memory as shared memory, so that CTAs of the next kernel find room beside this one's.)
     cudaError_t e = cudaFuncSetAttribute(gkv_prefix_attn_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kPxSmem);
     if (e == cudaSuccess) e = cudaFuncSetAttribute(gkv_prefix_attn_kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
     if (e != cudaSuccess) return e;
-    gkv_prefix_attn_kernel<<<(unsigned)p.prefix_items, kPxThreads, kPxSmem, s>>>(p, tm_k, tm_v);
+    gkv_prefix_attn_kernel<<<(unsigned)p.prefix_items, kPxThreads, kPxSmem, s>>>(p, watch, tm_k, tm_v);
     return cudaGetLastError();
 }
 

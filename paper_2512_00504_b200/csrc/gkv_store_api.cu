@@ -107,7 +107,7 @@ int device_sm_count() {
 }
 
 // Everything of an attention launch that is not a pointer, then the launches. `p` has its pointers and shape.
-gkv_status run_attn(StoreAttnLaunch& p, const gkv_store* shape, const gkv_prefix* prefix, int max_len, void* workspace,
+gkv_status run_attn(StoreAttnLaunch& p, const PrefixWatch& watch, const gkv_store* shape, const gkv_prefix* prefix, int max_len, void* workspace,
                     uint64_t workspace_bytes, int sm_count, cudaStream_t s, int* launches) {
     p.prefix_part = nullptr;
     p.n_prefix = 0;
@@ -136,7 +136,7 @@ gkv_status run_attn(StoreAttnLaunch& p, const gkv_store* shape, const gkv_prefix
         if (encode_map(&tm_k, const_cast<__nv_bfloat16*>(p.k_prefix), rows, 128) != GKV_OK ||
             encode_map(&tm_v, const_cast<__nv_bfloat16*>(p.v_prefix), rows, 128) != GKV_OK)
             return GKV_ERR_CUDA;
-        if (launch_prefix_attn(p, tm_k, tm_v, s) != cudaSuccess) { (void)cudaGetLastError(); return GKV_ERR_CUDA; }
+        if (launch_prefix_attn(p, watch, tm_k, tm_v, s) != cudaSuccess) { (void)cudaGetLastError(); return GKV_ERR_CUDA; }
         ++*launches;
     }
     if (launch_store_attn(p, s) != cudaSuccess) { (void)cudaGetLastError(); return GKV_ERR_CUDA; }
@@ -294,7 +294,7 @@ gkv_status gkv_store_attn(const gkv_store* store, const int32_t* len, int32_t ma
     p.g = store->n_q_heads / store->n_kv_heads; p.capacity = store->capacity;
     p.scale_log2 = (float)(1.4426950408889634 / sqrt((double)kHeadDim));
     int launches = 0;
-    return run_attn(p, store, prefix, max_len > 0 ? max_len : store->capacity, workspace, workspace_bytes, device_sm_count(),
+    return run_attn(p, PrefixWatch{nullptr, 0}, store, prefix, max_len > 0 ? max_len : store->capacity, workspace, workspace_bytes, device_sm_count(),
                     static_cast<cudaStream_t>(stream), &launches);
 }
 
@@ -325,12 +325,11 @@ gkv_status gkv_decode_attn_prefix(gkv_ctx* ctx, int32_t layer, const void* q, co
     p.q = static_cast<const __nv_bfloat16*>(q);
     p.k_new = static_cast<const __nv_bfloat16*>(k_new); p.v_new = static_cast<const __nv_bfloat16*>(v_new);
     p.out = static_cast<__nv_bfloat16*>(out);
-    p.status = reinterpret_cast<int32_t*>(static_cast<uint8_t*>(ctx->buf.workspace) + ctx->ws.status);
-    p.give_up = ctx->prefix_give_up;
+    const PrefixWatch watch = {reinterpret_cast<int32_t*>(static_cast<uint8_t*>(ctx->buf.workspace) + ctx->ws.status), ctx->prefix_give_up};
     p.format = GKV_STORE_BF16; p.batch = c.batch; p.h_q = c.n_q_heads; p.h_kv = c.n_kv_heads; p.g = ctx->g; p.capacity = ctx->C;
     p.scale_log2 = (float)(1.4426950408889634 / sqrt((double)kHeadDim));
     int launches = 0;
-    const gkv_status r = run_attn(p, &shape, prefix, ctx->len[layer], workspace, workspace_bytes, ctx->sm_count,
+    const gkv_status r = run_attn(p, watch, &shape, prefix, ctx->len[layer], workspace, workspace_bytes, ctx->sm_count,
                                   static_cast<cudaStream_t>(stream), &launches);
     ctx->launches += launches;
     if (r != GKV_OK) return r;
