@@ -516,7 +516,8 @@ class KVStore:
 
     fmt: "bf16", "e4m3", "int8" or "int4". The buffers are allocated here (uninitialised: rows are written before they are
     read) or given: (k, v, k_scale, v_scale), for bf16 (k, v). max_prefix and n_prefix: the longest prefix and the most
-    prefixes that attn will be given. Calls of one store must not overlap on the GPU (they share the workspace)."""
+    prefixes that attn will be given. Calls of one store must not overlap on the GPU (they share the workspace). What has been
+    allocated here may be dropped while streams still work on it (given buffers and a call's tensors are the caller's to keep)."""
 
     def __init__(self, fmt, *, batch, h_q, h_kv, capacity, device=None, buffers=None, max_prefix=0, n_prefix=0):
         import torch
@@ -527,6 +528,7 @@ class KVStore:
             _int32(n, what)
         self.desc = gkv_store(STORE_FORMATS[fmt], batch, h_q, h_kv, 128, capacity)
         self.sizes = gkv_store_query_sizes(self.desc)
+        given = buffers is not None
         code = {"bf16": torch.bfloat16, "e4m3": torch.float8_e4m3fn, "int8": torch.int8, "int4": torch.uint8}[fmt]
         scales = {"bf16": 0, "e4m3": 1, "int8": 1, "int4": 4}[fmt]
         shape, s_shape = torch.Size((batch, h_kv, capacity, 64 if fmt == "int4" else 128)), torch.Size((batch, h_kv, capacity, scales))
@@ -548,6 +550,8 @@ class KVStore:
         if self.device.type != "cuda":
             raise ValueError(f"the buffers are on {self.device}")
         self._call = _torch_binding()
+        # what has been allocated here, and on which stream
+        self._held = (torch.cuda.current_stream(self.device).cuda_stream, self.device.index, self.workspace) + (() if given else tuple(buffers))
         self._at = (ctypes.addressof(self.desc), self.device.index)
         self._ws = (self.workspace.data_ptr(), self.workspace.numel())
 
@@ -557,11 +561,13 @@ class KVStore:
         and all tokens)."""
         at, dev = self._at
         _check(self._call.copy(False, at, dev, k, v, first, count), "gkv_store_write")
+        self._call.in_use(self._held)
 
     def read(self, k, v, first=None, count=None):
         """Read the same rows back as bf16 into k and v, whose rows may not overlap; tokens from count[i] on are left as they were."""
         at, dev = self._at
         _check(self._call.copy(True, at, dev, k, v, first, count), "gkv_store_read")
+        self._call.in_use(self._held)
 
     def attn(self, length, q, out, k_new=None, v_new=None, prefix=None, lse=None, max_len=0):
         """Decode attention over rows 0 .. length[i] - 1 (int32 on the device), the new token (appended at row length[i]) and
@@ -573,3 +579,4 @@ class KVStore:
             _fitting(prefix, self.h_kv, self.device, "store")
             pre = prefix.at
         _check(self._call.attn(at, dev, length, max_len, q, k_new, v_new, pre, out, lse, ws, ws_bytes), "gkv_store_attn")
+        self._call.in_use(self._held)

@@ -3,6 +3,7 @@
 // most decode-sized kernels run; here they take well under one.) It holds no state but the addresses of the library's functions,
 // so that it serves every build of the library.
 #include <Python.h>
+#include <c10/cuda/CUDACachingAllocator.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -141,9 +142,33 @@ PyObject* attn(PyObject*, PyObject* const* a, Py_ssize_t n) try {
     return nullptr;
 }
 
+// in_use((stream, device, tensor, ...)): the tensors, allocated on that stream (its cudaStream_t), have been given to work on the
+// current stream. If that is another one, the allocator is told, so that it does not hand their memory out again before that work is done.
+PyObject* in_use(PyObject*, PyObject* held) try {
+    if (!PyTuple_Check(held) || PyTuple_GET_SIZE(held) < 2) {
+        PyErr_SetString(PyExc_TypeError, "in_use takes a tuple (stream, device, tensor, ...)");
+        return nullptr;
+    }
+    const void* home = address<const void>(PyTuple_GET_ITEM(held, 0));
+    const int device = (int)PyLong_AsLong(PyTuple_GET_ITEM(held, 1));
+    if (PyErr_Occurred()) return nullptr;
+    const c10::cuda::CUDAStream current = c10::cuda::getCurrentCUDAStream(device);
+    if (current.stream() != home)
+        for (Py_ssize_t i = 2; i < PyTuple_GET_SIZE(held); ++i) {
+            const at::Tensor* t = tensor(PyTuple_GET_ITEM(held, i), "in_use");
+            if (!t) return nullptr;
+            c10::cuda::CUDACachingAllocator::recordStream(t->storage().data_ptr(), current);
+        }
+    Py_RETURN_NONE;
+} catch (const std::exception& e) {
+    PyErr_SetString(PyExc_RuntimeError, e.what());
+    return nullptr;
+}
+
 PyMethodDef g_methods[] = {{"bind", (PyCFunction)(void (*)(void))bind, METH_FASTCALL, nullptr},
                            {"copy", (PyCFunction)(void (*)(void))copy, METH_FASTCALL, nullptr},
                            {"attn", (PyCFunction)(void (*)(void))attn, METH_FASTCALL, nullptr},
+                           {"in_use", (PyCFunction)in_use, METH_O, nullptr},
                            {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_gkv_torch", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
