@@ -110,18 +110,29 @@ def build_library(force: bool = False, verbose: bool = False, check_bounds: bool
     return out
 
 
+def _binding_built_for() -> str:
+    """The torch and Python that csrc/gkv_torch.cpp is compiled against: with others its layouts may not be theirs."""
+    import sysconfig
+
+    import torch
+    return f"gkv_torch for torch {torch.__version__}, {sysconfig.get_config_var('SOABI')}"
+
+
 def build_binding(force: bool = False) -> Path:
     """Compile csrc/gkv_torch.cpp (the Python module through which KVStore makes its calls) against this torch."""
     import sysconfig
 
     import torch
+    built_for = _binding_built_for()
     src, out = _PKG / "csrc" / "gkv_torch.cpp", _PKG / "_gkv_torch.so"
-    if not force and out.exists() and all(out.stat().st_mtime >= d.stat().st_mtime for d in (src, _ROOT / "include" / "gkv.h")):
+    if not force and out.exists() and all(out.stat().st_mtime >= d.stat().st_mtime for d in (src, _ROOT / "include" / "gkv.h")) \
+            and built_for.encode() + b"\0" in out.read_bytes():
         return out
     t = Path(torch.__file__).resolve().parent
     cuda = Path(os.environ.get("CUDA_HOME", "/usr/local/cuda"))
     tmp = out.with_suffix(f".so.tmp{os.getpid()}")
     subprocess.check_call(["g++", "-O2", "-std=c++17", "-shared", "-fPIC", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+                           f'-DGKV_BUILT_FOR="{built_for}"',
                            "-I", str(_ROOT / "include"), "-I", str(t / "include"), "-I", str(t / "include/torch/csrc/api/include"),
                            "-I", str(cuda / "include"), "-I", sysconfig.get_paths()["include"], "-o", str(tmp), str(src),
                            "-L", str(t / "lib"), "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_python"])
@@ -204,6 +215,8 @@ def _torch_binding():
         spec = importlib.util.spec_from_file_location("_gkv_torch", path)
         module = importlib.util.module_from_spec(spec)
         spec.loader.exec_module(module)
+        if module.built_for != _binding_built_for():
+            raise RuntimeError(f"{path} is a {module.built_for}, this is {_binding_built_for()}: run __graft_entry__.build() again")
         L = lib()
         module.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (L.gkv_store_write, L.gkv_store_read, L.gkv_store_attn)))
         _binding = module

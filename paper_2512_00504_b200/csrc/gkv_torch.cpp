@@ -174,4 +174,12 @@ PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_gkv_torch", nullptr, -1, g_meth
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__gkv_torch(void) { return PyModule_Create(&g_module); }
+#ifndef GKV_BUILT_FOR
+#define GKV_BUILT_FOR "unknown"
+#endif
+
+PyMODINIT_FUNC PyInit__gkv_torch(void) {
+    PyObject* m = PyModule_Create(&g_module);
+    if (m && PyModule_AddStringConstant(m, "built_for", GKV_BUILT_FOR) != 0) Py_CLEAR(m);
+    return m;
+}
