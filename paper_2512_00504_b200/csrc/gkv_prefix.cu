@@ -47,6 +47,7 @@ constexpr int kPxSlotBytes = 2 * kPxHalf;    // one K or V tile, or one row tile
 constexpr int kPxSlots = 3;
 constexpr float kPxLimit = 0x1p60f;          // a row's weights of half a tile may sum up to this
 constexpr float kPxCheck = 0x1p16f;          // from here on (in all) the row's values are looked at
+constexpr float kPxSum = 0x1p115f;           // and may be this large: the merge adds up to 320 of them
 
 struct __align__(16) PrefixTail {
     uint64_t q_full;
@@ -371,17 +372,17 @@ gkv_prefix_attn_kernel(const StoreAttnLaunch p, const PrefixWatch watch, const _
             if (pass == 1) m = top * p.scale_log2;
             if (!tc_wait(smem_u32(&tail->o_full), pass & 1, abort_flag)) ok = false;
             if (pass == 0 && __any_sync(0xffffffffu, l > kPxCheck)) {
-                // large weights of a row may have carried its values out of fp32's range
+                // large weights of a row may have carried its values out of fp32's range, or so near its end that the runs' sum leaves it
                 tmem_fence_after_sync();
-                float bad = 0.f;
+                bool bad = false;
                 for (int c = 0; c < 4; ++c) {
                     float o[32];
                     tmem_ld32_start(o_addr + 32 * c, o);
                     tmem_ld_wait(o);
 #pragma unroll
-                    for (int k = 0; k < 32; ++k) bad = fmaf(o[k], 0.f, bad);
+                    for (int k = 0; k < 32; ++k) bad |= !(fabsf(o[k]) <= kPxSum);
                 }
-                if (!(bad == 0.f)) *(volatile int*)&tail->overflow = 1;
+                if (bad) *(volatile int*)&tail->overflow = 1;
                 tmem_fence_before_sync();
             }
         }

@@ -101,3 +101,26 @@ def test_groups_of_very_different_size(B, H, C, m, exponent, append):
                 want, l, tol, ltol = ref.attend(q[b, heads], K[b, h, :n], V[b, h, :n, d], *pre)
                 assert (np.abs(out[b, heads, d] - want) <= tol).all(), (b, h, i, np.abs(out[b, heads, d] - want).max() / np.abs(want).max())
                 assert (np.abs(lse[b, heads] - l) <= ltol).all()
+
+
+@pytest.mark.parametrize("rise", [13, 14, 15, 16])           # in units of e: weights of 2^19 to 2^23 relative to the first tiles
+@pytest.mark.parametrize("period", [4, 5, 6, 7, 8, 9, 10, 11, 12, 13, 16, 22, 32])
+@pytest.mark.parametrize("seqs", [16, 32])
+def test_partial_results_of_large_values_add_up(seqs, period, rise):
+    """V of 2^96 and logits that are low in the first two of every `period` key tiles and high in the others: where that is how the
+    keys are cut into runs, every partial result comes near the end of fp32's range, each of them finite, and so has to be their sum."""
+    m, H = 8192, 16
+    g = gen(71)
+    high = (torch.arange(m // 128, device=DEV) % period >= 2).repeat_interleave(128)
+    q = randn(g, 1, 1, 128).expand(seqs, 8 * H, 128).contiguous()
+    unit = q[0, 0].float() / q[0, 0].float().square().sum() * 128 ** 0.5
+    k = (unit * (high * rise)[:, None]).to(torch.bfloat16).view(1, 1, m, 128).expand(1, H, m, 128).contiguous()
+    v = (torch.rand(1, H, m, 128, generator=g, device=DEV) * 2.0 ** 96).to(torch.bfloat16)
+    out, lse = torch.empty((seqs, 8 * H, 128), dtype=torch.bfloat16, device=DEV), torch.empty((seqs, 8 * H), device=DEV)
+    st = gkv.KVStore("bf16", batch=seqs, h_q=8 * H, h_kv=H, capacity=4, device=DEV, n_prefix=1, max_prefix=m)
+    st.attn(ints([0] * seqs), q, out, prefix=gkv.Prefix(k, v, [m]), lse=lse)
+    assert torch.isfinite(out).all()
+    for h in (0, H - 1):
+        hs = slice(8 * h, 8 * h + 8)
+        want, l, tol, ltol = ref.attend(f64(q[1, hs]), np.zeros((0, 128)), np.zeros((0, 128)), f64(k[0, h]), f64(v[0, h]), ref.U_BF16)
+        assert (np.abs(f64(out[1, hs]) - want) <= tol).all() and (np.abs(f64(lse[1, hs]) - l) <= ltol).all()
