@@ -51,3 +51,23 @@ def test_an_expired_wait_is_reported_once(B, m):
     step()                                             # and taken for expired once
     cache.poll()
     assert right()
+
+
+@pytest.mark.parametrize("rows", [0, 5])
+def test_a_context_with_a_prefix_without_rows_is_an_ordinary_step(rows):
+    B, Hq, H = 3, 8, 2
+    cache = gkv.GKVCache(gkv.make_config(n_layers=1, batch=B, h_q=Hq, h_kv=H, b=48, buffer=24, w=16, s=16, fuse_window_scores=False), DEV)
+    g = gen(52)
+    empty = torch.zeros((1, H, rows, 128), dtype=torch.bfloat16, device=DEV)
+    prefix, ws = gkv.Prefix(empty, empty, [0]), cache.prefix_workspace(1, 0)
+    out = torch.empty((B, Hq, 128), dtype=torch.bfloat16, device=DEV)
+    for t in range(20):
+        q, kn, vn = randn(g, B, Hq, 128), randn(g, B, H, 128), randn(g, B, H, 128)
+        cache.decode_attn_prefix(0, q, kn, vn, prefix, out, ws)
+        assert cache.len[0, 0].tolist() == [t + 1] * B and cache.state(0)[0] == t + 1
+        assert torch.equal(cache.k[0, :, :, t], kn) and torch.equal(cache.v[0, :, :, t], vn)
+        for h in range(H):
+            hs = slice(4 * h, 4 * h + 4)
+            want, _, tol, _ = ref.attend(f64(q[1, hs]), f64(cache.k[0, 1, h, :t + 1]), f64(cache.v[0, 1, h, :t + 1]), weight_unit=ref.U_BF16)
+            assert (np.abs(f64(out[1, hs]) - want) <= tol).all()
+    cache.poll()
