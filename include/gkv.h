@@ -323,7 +323,7 @@ gkv_status gkv_score_launch_plan(const gkv_config* cfg, int32_t n_layers_in_laun
  *   E4M3  8-bit floats (4 exponent, 3 mantissa bits); s = 2^e, the smallest e >= -126 with a / 2^e <= 448
  *   INT8  whole numbers -127..127, two's complement;  s = max(bf16(a / 127), 2^-126)
  *   INT4  whole numbers -7..7, stored + 8 in a nibble; s = max(bf16(a / 7), 2^-126)
- * and c = x / s rounded to nearest, ties to even. INT4 rows: elements 32g + 4q .. 32g + 4q + 3 are the nibbles, lowest first,
+ * and c = x / s rounded to nearest, ties to even (elements above 2^127.9 may read back as infinity: c * s rounds up to it). INT4 rows: elements 32g + 4q .. 32g + 4q + 3 are the nibbles, lowest first,
  * of the row's 16-bit word 4q + g (g = 0..3, q = 0..7). A group that holds a NaN or an infinity gets s = NaN: it reads back as
  * NaN and makes the attention over it NaN. */
 typedef enum { GKV_STORE_BF16 = 0, GKV_STORE_E4M3 = 1, GKV_STORE_INT8 = 2, GKV_STORE_INT4 = 3 } gkv_store_format;
@@ -383,12 +383,16 @@ gkv_status gkv_store_attn_workspace(const gkv_store* store, int32_t n_prefix, in
  *            is written to the store.
  *   max_len  the longest length, for spreading the work (0: capacity). Results do not depend on it beyond rounding. (How
  *            the work is spread, and with it the rounding of sums, may also depend on the other sequences' lengths; the same
- *            call gives the same bits.)
+ *            call gives the same bits.) The work of a single sequence, of a call with a prefix and of short rows is cut by
+ *            max_len alone: far above the lengths it leaves a part of the device idle.
  *   q, out   device, bf16 [batch][n_q_heads][128], 16-byte aligned
  *   k_new, v_new  device, bf16 [batch][n_kv_heads][128], 16-byte aligned, or both NULL. The new row is quantised into row
  *            len[i] and attended to as it stands there. The caller then counts len[i] up.
  *   prefix   NULL: none
  *   lse      device, fp32 [batch][n_q_heads], or NULL: the natural logarithm of the sum of exp(scaled logits)
+ * Precision: sums and statistics in 32 bits; weights of a V row as bf16 (bf16 rows and prefixes) or fp16 (the others); q, with
+ * 8- and 4-bit rows, as fp16 relative to the largest element of its head (elements below 2^-17 of that are off by up to 2^-25 of it).
+ * Values (V) up to 2^95 leave every sum finite at any length; far larger ones may not.
  * A sequence with nothing to attend to gets out = 0 and lse = -infinity. (A bounded wait of the prefix kernel that expires cannot be
  * polled through this entry point, which has no state: out and lse of its sequences are NaN then.)
  * Errors: as gkv_store_query_sizes; INVALID_ARG (NULL or misaligned pointer, only one of k_new and v_new, max_len outside

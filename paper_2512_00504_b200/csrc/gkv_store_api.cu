@@ -177,7 +177,9 @@ namespace gkv {
 // rows the pieces are dealt out by the lengths that the sequences really have (store_piece_tiles), by way of the workspace, which
 // costs a merge of 4 us when all are equally long and saves more the more they differ (32 sequences x 4 heads of 8192 keys in 8
 // bits: 49 us as clusters, 53 dealt out; of 256 to 8192 keys: 43, 36; one of 8192 and 31 of 512: 36, 20. 128 x 8 heads, one of
-// 65536 and 127 of 2048 keys: 963 us as whole units, 168; all of 8192 keys: 352, 378).
+// 65536 and 127 of 2048 keys: 963 us as whole units, 153; all of 8192 keys: 352, 369). A single sequence, launches with a prefix
+// and those of a context are not dealt out: their pieces go by max_len alone, and where that is far above the lengths the last
+// pieces have no keys.
 // Prefixes: the length of the runs that the prefixes' key tiles are cut into. An item occupies an SM for about 8 us + 1.05 us a
 // tile (2.1 with more than 128 query rows); the attention over own rows (at 5.5 TB/s, with sequences three quarters of the
 // longest on average) takes the SMs that are left and, in part, the same ones; every run leaves a partial result that is written

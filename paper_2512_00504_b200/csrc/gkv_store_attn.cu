@@ -11,7 +11,8 @@
 //
 // 8- and 4-bit codes become fp16 exactly (their scales stay outside the products), q becomes fp16 after division by a power
 // of two (an element is exact down to 2^-17 of its row's largest; below, the error is at most 2^-25 of the largest), weights
-// are rounded to fp16 (11 bits). The scale of a K row multiplies its logit. The scale s of a V row goes into the weight:
+// are rounded to fp16 (11 bits: outputs are off by 1.68e-3 instead of the 1.65e-3 that the output's own rounding to bf16 makes; it is
+// what the product takes, and codes times fp16 weights are exact in its sums). The scale of a K row multiplies its logit. The scale s of a V row goes into the weight:
 // w = p s c with p = exp2(z - m) as it enters the sum of the softmax, and c = exp2(m - v) with a running maximum v over
 // z + log2 s, so that the weights handed to the product lie in fp16's range whatever the scales are. A 4-bit row has a scale
 // for each 32 head dimensions, and every group of dimensions has its own v and c: groups of very different size do not share a
@@ -28,8 +29,9 @@
 // Bound by HBM for 8-bit rows in a large batch (128 sequences x 8 heads of about 2200 keys, 585 MB: 97 us, 6.0 TB/s). 4-bit rows
 // bring twice the elements per byte to unpack: 2 x 8 heads of about 120000 keys, 274 MB in 77 us, 3.6 TB/s, with the schedulers
 // issuing 6 cycles out of 10, the logic and fp32 pipes 4 to 5 (without the products and what feeds them the same loads take 55
-// us; one reference for all groups of a head instead of one for each: 75.7 against 76.8). A single sequence of 640 keys takes 6.7 us: the launch, three trips to memory (length, rows, the others' results), 3 tiles
-// per warp.
+// us; with one reference for all groups of a head, which is not precise enough, 75.7). bf16 rows: 128 sequences x 8 heads of 2200
+// keys, 1153 MB in 197 us, 5.9 TB/s. A single sequence of 640 keys takes 7.0 us: the launch, four trips to memory (length, q, rows,
+// the others' results) one after the other, 3 tiles per warp.
 #include "gkv_store_codes.cuh"
 
 namespace gkv {
@@ -120,7 +122,8 @@ __device__ __forceinline__ void unpack8(uint32_t w, uint32_t& lo, uint32_t& hi) 
     }
 }
 // Two bytes of nibbles under the exponent of 1024, x = 1024 + u0 + 16 u1 in both halves (u = c + 8) -> the fp16 pairs c0 and c1,
-// exactly: without its low nibble x is y = 1024 + 16 u1, so c1 = y / 16 - 72; without the high one it is 1024 + u0. Two
+// exactly. (Integers put into a mantissa under a fixed exponent instead of being converted: for 4-bit weights in fp16 published by
+// Kim et al. 2022, arXiv 2211.10017.) Without its low nibble x is y = 1024 + 16 u1, so c1 = y / 16 - 72; without the high one it is 1024 + u0. Two
 // instructions for the logic unit and two for the fp32 and half-precision pipe, which are about equally busy then (c0 as
 // (x - 16 c1) - 1160 puts three on the latter: 131071 keys take 80 us instead of 78). (Leaving the offset 8 in and taking it
 // off the sums would save the latter, but costs precision: as 1024 + u in the fp32 sums, as subnormals u 2^-24 where the
@@ -341,8 +344,8 @@ __device__ __forceinline__ float final_lse(float m, float l, bool fits) {
 }
 
 // Resident CTAs per SM. 8- and 4-bit rows: 128 registers, 16 warps (128 sequences x 8 heads of about 2200 keys in 8 bits: 97 us;
-// two tiles per step, 168 registers and 12 warps: 110 us. 2 x 8 heads of up to 131071 keys in 4 bits: 77 us; 12 warps: 78, with
-// two tiles per step 85). bf16 rows need twice the registers for a tile.
+// two tiles per step, 168 registers and 12 warps: 110 us. 2 x 8 heads of up to 131071 keys in 4 bits, with one reference a head: 76
+// us; 12 warps: 78, with two tiles per step 85). bf16 rows need twice the registers for a tile.
 __host__ __device__ constexpr int store_ctas(int format) { return format == GKV_STORE_BF16 ? 3 : 4; }
 int store_attn_ctas_per_sm(int format) { return store_ctas(format); }
 

@@ -22,7 +22,6 @@ template <> struct StoreFormat<GKV_STORE_INT4> { static constexpr int kRow = 64,
 
 __device__ __forceinline__ float bf16_lo(uint32_t x) { return __uint_as_float(x << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t x) { return __uint_as_float(x & 0xffff0000u); }
-__device__ __forceinline__ float bf16_float(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
 
 // The 8 bf16 elements lane l owns of a contiguous row (16-byte aligned).
 template <int F>
