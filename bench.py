@@ -813,6 +813,30 @@ def run_reference(args) -> dict | None:
             "gpu_launches": 0, "wall_s": wall, "wall_ms_per_step": 1e3 * wall / steps}
 
 
+def short(x):
+    """Numbers to 6 digits, and a list of records as a table: what the line says of the other configurations stays readable at a length
+    (about 10 KB instead of 23) that whoever keeps the end of the output keeps whole."""
+    if isinstance(x, float):
+        return int(x) if x.is_integer() and abs(x) < 2 ** 53 else float(f"{x:.6g}")
+    if isinstance(x, dict):
+        return {k: short(v) for k, v in x.items()}
+    if isinstance(x, list) and len(x) > 1 and all(isinstance(r, dict) for r in x):
+        flat = [flatten(short(r)) for r in x]
+        columns = list(flat[0])
+        if all(list(r) == columns for r in flat):
+            same = {c: flat[0][c] for c in columns if all(r[c] == flat[0][c] for r in flat)}
+            columns = [c for c in columns if c not in same]
+            return {"same": same, "columns": columns, "rows": [[r[c] for c in columns] for r in flat]}
+    return [short(v) for v in x] if isinstance(x, list) else x
+
+
+def flatten(record: dict, at: str = "") -> dict:
+    out = {}
+    for k, v in record.items():
+        out.update(flatten(v, f"{at}{k}.") if isinstance(v, dict) else {at + k: v})
+    return out
+
+
 def main():
     ap = argparse.ArgumentParser()
     ap.add_argument("--gpus", type=int, default=1)
@@ -849,6 +873,8 @@ def main():
     else:
         res = run_ours(args)
     if res is not None:
+        if "configs" in res:
+            res["configs"] = short(res["configs"])
         print(json.dumps(res))
 
 
