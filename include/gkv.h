@@ -323,7 +323,7 @@ gkv_status gkv_score_launch_plan(const gkv_config* cfg, int32_t n_layers_in_laun
  *   E4M3  8-bit floats (4 exponent, 3 mantissa bits); s = 2^e, the smallest e >= -126 with a / 2^e <= 448
  *   INT8  whole numbers -127..127, two's complement;  s = max(bf16(a / 127), 2^-126)
  *   INT4  whole numbers -7..7, stored + 8 in a nibble; s = max(bf16(a / 7), 2^-126)
- * and c = x / s rounded to nearest, ties to even (elements above 2^127.9 may read back as infinity: c * s rounds up to it). INT4 rows: elements 32g + 4q .. 32g + 4q + 3 are the nibbles, lowest first,
+ * and c = x / s rounded to nearest, ties to even. (Elements above 2^127.9 may read back as infinity: c * s rounds up to it.) INT4 rows: elements 32g + 4q .. 32g + 4q + 3 are the nibbles, lowest first,
  * of the row's 16-bit word 4q + g (g = 0..3, q = 0..7). A group that holds a NaN or an infinity gets s = NaN: it reads back as
  * NaN and makes the attention over it NaN. */
 typedef enum { GKV_STORE_BF16 = 0, GKV_STORE_E4M3 = 1, GKV_STORE_INT8 = 2, GKV_STORE_INT4 = 3 } gkv_store_format;
@@ -392,6 +392,8 @@ gkv_status gkv_store_attn_workspace(const gkv_store* store, int32_t n_prefix, in
  *   lse      device, fp32 [batch][n_q_heads], or NULL: the natural logarithm of the sum of exp(scaled logits)
  * Precision: sums and statistics in 32 bits; weights of a V row as bf16 (bf16 rows and prefixes) or fp16 (the others); q, with
  * 8- and 4-bit rows, as fp16 relative to the largest element of its head (elements below 2^-17 of that are off by up to 2^-25 of it).
+ * Weight times scale of an 8- or 4-bit V row loses bits below 2^-20 of the sequence's largest for the head (4 bits: for the head and
+ * the 32 dimensions of a scale), and is 0 from 2^-31 of it on.
  * Values (V) up to 2^95 leave every sum finite at any length; far larger ones may not.
  * A sequence with nothing to attend to gets out = 0 and lse = -infinity. (A bounded wait of the prefix kernel that expires cannot be
  * polled through this entry point, which has no state: out and lse of its sequences are NaN then.)

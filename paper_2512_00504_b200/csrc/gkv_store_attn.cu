@@ -11,13 +11,14 @@
 //
 // 8- and 4-bit codes become fp16 exactly (their scales stay outside the products), q becomes fp16 after division by a power
 // of two (an element is exact down to 2^-17 of its row's largest; below, the error is at most 2^-25 of the largest), weights
-// are rounded to fp16 (11 bits: outputs are off by 1.68e-3 instead of the 1.65e-3 that the output's own rounding to bf16 makes; it is
-// what the product takes, and codes times fp16 weights are exact in its sums). The scale of a K row multiplies its logit. The scale s of a V row goes into the weight:
-// w = p s c with p = exp2(z - m) as it enters the sum of the softmax, and c = exp2(m - v) with a running maximum v over
-// z + log2 s, so that the weights handed to the product lie in fp16's range whatever the scales are. A 4-bit row has a scale
-// for each 32 head dimensions, and every group of dimensions has its own v and c: groups of very different size do not share a
-// range. (v is kept at least at m - 112: c stays finite, and where all of a group's V is below 2^-112 its outputs are numbers of
-// that size.) Sums and accumulators are fp32.
+// are rounded to fp16 (11 bits: outputs are off by 1.68e-3 instead of the 1.65e-3 that the output's own rounding to bf16 makes;
+// it is what the product takes, and codes times fp16 weights are exact in its sums). The scale of a K row multiplies its logit.
+// The scale s of a V row goes into the weight: w = p s c with p = exp2(z - m) as it enters the sum of the softmax, and
+// c = exp2(m - v) with a running maximum v over z + log2 s, so that the largest of the weights handed to the product lie high in
+// fp16's range whatever the scales are (those 2^-20 below lose bits, and 2^-31 below they are 0). A 4-bit row has a scale for
+// each 32 head dimensions, and every group of dimensions has its own v and c: groups of very different size do not share a range.
+// (v is kept at least at m - 112: c stays finite, and where all of a group's V is below 2^-112 its outputs are numbers of that
+// size.) Sums and accumulators are fp32.
 //
 // The running maxima are allowed to lag: a step raises them (which costs a reduction over the warp and a rescaling of the
 // accumulators) only when its weights have grown large.
