@@ -323,8 +323,9 @@ gkv_status gkv_score_launch_plan(const gkv_config* cfg, int32_t n_layers_in_laun
  *   E4M3  8-bit floats (4 exponent, 3 mantissa bits); s = 2^e, the smallest e >= -126 with a / 2^e <= 448
  *   INT8  whole numbers -127..127, two's complement;  s = max(bf16(a / 127), 2^-126)
  *   INT4  whole numbers -7..7, stored + 8 in a nibble; s = max(bf16(a / 7), 2^-126)
- * and c = x / s rounded to nearest, ties to even. (Elements above 2^127.9 may read back as infinity: c * s rounds up to it.) INT4 rows: elements 32g + 4q .. 32g + 4q + 3 are the nibbles, lowest first,
- * of the row's 16-bit word 4q + g (g = 0..3, q = 0..7). A group that holds a NaN or an infinity gets s = NaN: it reads back as
+ * and c = x / s rounded to nearest, ties to even. (Elements above 2^127.9 may read back as infinity: c * s rounds up to it.)
+ * INT4 rows: elements 32g + 4q .. 32g + 4q + 3 are the nibbles, lowest first, of the row's 16-bit word 4q + g (g = 0..3,
+ * q = 0..7). A group that holds a NaN or an infinity gets s = NaN: it reads back as
  * NaN and makes the attention over it NaN. */
 typedef enum { GKV_STORE_BF16 = 0, GKV_STORE_E4M3 = 1, GKV_STORE_INT8 = 2, GKV_STORE_INT4 = 3 } gkv_store_format;
 typedef struct {
