@@ -419,6 +419,124 @@ gkv_status gkv_decode_attn_prefix(gkv_ctx* ctx, int32_t layer, const void* q, co
  * such kernel). Errors: INVALID_ARG. */
 gkv_status gkv_selftest_prefix_wait(gkv_ctx* ctx);
 
+/* ---- Rotary positions, and caches in pages -----------------------------------------------------------------------------
+ * (No counterpart in the paper, whose cache takes keys as they come and keeps one stretch of rows a sequence.) As with the stores,
+ * everything is a plain description of caller-owned buffers; the calls keep no state, allocate nothing, change no lengths or
+ * tables, and run on the caller's stream and the current device, so that one can be captured and replayed while both grow.
+ *
+ * Rotation of a head's first rot_dim elements, taken as rot_dim / 2 pairs (a, b): (i, i + rot_dim / 2) or, interleaved, (2i, 2i + 1).
+ * Pair i of a token at position p turns by p f_i and is multiplied by `factor`:
+ *   a' = factor (a cos(p f_i) - b sin(p f_i)),  b' = factor (b cos(p f_i) + a sin(p f_i))
+ * The elements behind them stay as they are. Frequencies are kept as fractions of a turn in units of 2^-64, so that p f_i is reduced to
+ * one turn by the wrap of a 64-bit product, exactly, at any position. */
+typedef enum { GKV_TYPE_BF16 = 0, GKV_TYPE_FP16 = 1, GKV_TYPE_FP32 = 2 } gkv_type;
+typedef enum { GKV_ROTARY_PLAIN = 0, GKV_ROTARY_LINEAR = 1, GKV_ROTARY_NTK = 2, GKV_ROTARY_WAVELENGTH = 3, GKV_ROTARY_YARN = 4 } gkv_rotary_scaling;
+
+typedef struct {
+    int32_t head_dim;      /* even, 2..512                                                                   */
+    int32_t rot_dim;       /* even, 2..head_dim                                                              */
+    int32_t interleaved;   /* 0: pairs (i, i + rot_dim / 2), 1: (2i, 2i + 1)                                 */
+    float factor;          /* 1 unless the frequencies ask for another                                       */
+    const uint64_t* turns; /* device, [rot_dim / 2], 8-byte aligned: from gkv_rotary_turns                   */
+} gkv_rotary;
+
+/* Rows to rotate: element (i, t, h, e) of x at i * x_stride[0] + t * x_stride[1] + h * x_stride[2] + e, and y likewise (strides in
+ * elements; aligned to their type). y is x itself (with the same strides) or does not overlap it. */
+typedef struct {
+    const void* x;
+    void* y;
+    int64_t x_stride[3], y_stride[3];
+    int32_t n_heads;
+} gkv_rotary_rows;
+
+/* Frequencies of the pairs in radians a position (radians[rot_dim / 2], host) and the factor that belongs to them (may be NULL: 1 but
+ * for YARN), with base frequencies f_i = theta^(-2i / rot_dim) and r = rot_dim:
+ *   PLAIN       f_i
+ *   LINEAR      f_i / scale                                   (positions are interpolated)
+ *   NTK         those of the base theta * scale^(r / (r - 2)) (rot_dim 2: PLAIN)
+ *   WAVELENGTH  with x = original f_i / 2pi turns in the original context: f_i from `high` turns on, f_i / scale up to `low`, between them
+ *               f_i (s + (1 - s) / scale), s = (x - low) / (high - low)
+ *   YARN        (arXiv 2309.00071) f_i (1 - s) + (f_i / scale) s, s = (i - a) / (b - a) within 0..1, a and b the pair numbers (a rounded
+ *               down and at least 0, b rounded up and at most r - 1, at least 0.001 apart) at which a pair makes `high` and `low` turns in the
+ *               original context; factor 0.1 ln(scale) + 1
+ * Host arithmetic. Errors: INVALID_ARG (radians NULL, rot_dim odd or outside 2..512, unknown scaling, theta <= 1 or not finite; but for
+ * PLAIN scale < 1 or not finite; for the last two original < 1, low <= 0, high <= low, or not finite). */
+gkv_status gkv_rotary_frequencies(double theta, int32_t rot_dim, int32_t scaling, double scale, double original, double low, double high,
+                                  double* radians, float* factor);
+/* Host: radians[n] -> turns[n], rounded to the nearest 2^-64 of a turn. Errors: INVALID_ARG (NULL, n < 0, a value that is not finite or
+ * above 2^20 in magnitude). */
+gkv_status gkv_rotary_turns(const double* radians, int32_t n, uint64_t* turns);
+
+/* Rotate tokens 0..count[i] - 1 of sequence i in q and, if there is one, k (NULL: none), both [batch][n_tokens][their heads][head_dim] of
+ * `type`, in one launch. pos: device int32, position of token t of sequence i at i * pos_seq_stride + t * pos_token_stride; any 32-bit
+ * number, also below 0. count: device int32[batch], or NULL = n_tokens (above it counts as n_tokens, below 0 as 0). Tokens from count[i] on
+ * are not looked at, and their y stays as it was. transpose != 0 turns the other way, which is the gradient: with y = rotated x and dy
+ * the gradient of y, the transposed rotation of dy is that of x (`factor` included). Computed in 32 bits, rounded once.
+ * Errors: INVALID_ARG (NULL or misaligned pointer, sizes <= 0 but n_tokens = 0, which does nothing, unknown type, rot_dim odd or outside
+ * 2..head_dim, head_dim odd or above 512, factor not finite, a negative stride, a y whose rows overlap or interleave (in rising order, strides of
+ * sizes of 1 left out, the first must be >= head_dim and each other one >= the one before times its size), x = y with different strides, one
+ * y for both), UNSUPPORTED (batch > 65535, n_tokens * all heads >= 2^30), CUDA. */
+gkv_status gkv_rotary_apply(const gkv_rotary* rotary, int32_t type, int32_t batch, int32_t n_tokens, const int32_t* pos,
+                            int64_t pos_seq_stride, int64_t pos_token_stride, const int32_t* count, const gkv_rotary_rows* q,
+                            const gkv_rotary_rows* k, int32_t transpose, void* stream);
+
+/* A cache in pages: the rows of one layer in n_pages pages of page_size rows a head, in the row formats of the stores.
+ *   k, v             [n_pages][n_kv_heads][page_size][row], token_major: [n_pages][page_size][n_kv_heads][row]
+ *   k_scale, v_scale the same with [scales]
+ * Row r of sequence i is row r % page_size of page page[i * stride + r / page_size]. A page may be in several places of the table (shared
+ * rows); a call must not write a row twice. Places that no row of a call needs are not looked at. */
+typedef struct {
+    int32_t format;                        /* gkv_store_format                                        */
+    int32_t n_q_heads, n_kv_heads, head_dim;   /* head_dim 128; n_q_heads / n_kv_heads <= 8           */
+    int32_t n_pages, page_size;            /* page_size 1..65536                                      */
+    int32_t token_major;
+    void *k, *v;                           /* 16-byte aligned                                         */
+    void *k_scale, *v_scale;               /* 8-byte aligned; NULL for GKV_STORE_BF16                 */
+} gkv_pages;
+typedef struct {
+    const int32_t* page;                   /* device                                                  */
+    int64_t stride;                        /* places from a sequence to the next                      */
+    int32_t batch, width;                  /* sequences, places of each                               */
+} gkv_page_table;
+
+/* Bytes of the four buffers (pointers are not looked at).
+ * Errors: INVALID_ARG (NULL, sizes <= 0, unknown format, n_q_heads not a multiple of n_kv_heads), UNSUPPORTED (head_dim != 128, more than
+ * 8 query heads per KV head, page_size > 65536, 2^31 rows or more over all pages and heads). */
+gkv_status gkv_pages_query_sizes(const gkv_pages* pages, gkv_store_sizes* out);
+
+/* gkv_store_write into pages: row first[i] + t of every head of sequence i becomes token t of k and v, for t < count[i]. With `rotary`
+ * (head_dim 128; NULL: none) keys are rotated on the way, at position pos (device int32, i * pos_seq_stride + t * pos_token_stride;
+ * NULL: first[i] + t), and rounded to bf16 as gkv_rotary_apply would leave them before they are quantised; values are not. Rows outside
+ * 0..width * page_size - 1 and rows whose place in the table holds no page (outside 0..n_pages - 1) are not written.
+ * Errors: as gkv_store_write and gkv_pages_query_sizes; INVALID_ARG (page NULL or misaligned, batch or width <= 0, stride < 0, or a
+ * rotary that gkv_rotary_apply would refuse or of another head_dim), UNSUPPORTED (batch > 65535, width * page_size > 2^24). */
+gkv_status gkv_pages_append(const gkv_pages* pages, const gkv_page_table* table, const void* k, const void* v, int64_t seq_stride,
+                            int64_t token_stride, int64_t head_stride, const int32_t* first, const int32_t* count, int32_t n_tokens,
+                            const gkv_rotary* rotary, const int32_t* pos, int64_t pos_seq_stride, int64_t pos_token_stride, void* stream);
+
+/* Read back, as gkv_store_read: tokens whose row is outside the table or on no page are left as they were. Keys come as they are kept,
+ * rotated. Errors: as gkv_pages_append and gkv_store_read. */
+gkv_status gkv_pages_read(const gkv_pages* pages, const gkv_page_table* table, void* k, void* v, int64_t seq_stride, int64_t token_stride,
+                          int64_t head_stride, const int32_t* first, const int32_t* count, int32_t n_tokens, void* stream);
+
+/* Bytes of workspace that gkv_pages_attn needs for up to `batch` sequences, at any lengths. As with the stores it needs no initial contents
+ * and holds nothing between calls; calls that share one must not overlap on the GPU.
+ * Errors: as gkv_pages_query_sizes; INVALID_ARG (batch <= 0), UNSUPPORTED (batch > 65535, batch * n_q_heads >= 2^30). */
+gkv_status gkv_pages_attn_workspace(const gkv_pages* pages, int32_t batch, uint64_t* bytes);
+
+/* Decode attention over pages: gkv_store_attn (without a prefix) with rows found through the table.
+ *   q             device, bf16, element (i, h, e) at i * q_stride + h * 128 + e (q_stride a multiple of 8, >= 0), 16-byte aligned
+ *   k_new, v_new  the same with kv_stride, or both NULL. The new row is quantised into row len[i] and attended to as it stands there.
+ *   rotary        NULL, or q and k_new are rotated on the way (each rounded to bf16 as gkv_rotary_apply would leave it), at position pos[i]
+ *                 (device int32[batch]; NULL: the last row's number, which is len[i] with a new row and len[i] - 1 without)
+ *   out, lse, len, max_len and precision as in gkv_store_attn; a length that does not fit width * page_size gives NaN and nothing is
+ *   written. A row whose place in the table holds no page makes the sequence's out and lse NaN (for the new row: it is not written either);
+ *   nothing outside the buffers is touched.
+ * Errors: as gkv_pages_append and gkv_store_attn; INVALID_ARG (workspace_bytes too small for table->batch). */
+gkv_status gkv_pages_attn(const gkv_pages* pages, const gkv_page_table* table, const int32_t* len, int32_t max_len, const void* q,
+                          int64_t q_stride, const void* k_new, const void* v_new, int64_t kv_stride, const gkv_rotary* rotary,
+                          const int32_t* pos, void* out, float* lse, void* workspace, uint64_t workspace_bytes, void* stream);
+
 /* Memory model of the paper's appendix "Memory Analysis": bytes of the full KV cache at
  * seq_len tokens, of the compressed cache ((b + s) rows instead of seq_len), and of the score
  * cache F (b - w entries per head), for `elem_bytes`-wide elements, over all layers and the

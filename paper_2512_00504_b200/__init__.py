@@ -22,7 +22,8 @@ _ROOT = _PKG.parent
 _CHECKED = os.environ.get("GKV_LIB_VARIANT", "") == "check"
 LIB_PATH = _PKG / ("libgkv_check.so" if _CHECKED else "libgkv.so")
 _SOURCES = ["gkv_api.cu", "gkv_decode.cu", "gkv_evict.cu", "gkv_score.cu", "gkv_score_tc.cu", "gkv_redundancy.cu",
-            "gkv_static_scratch.cu", "gkv_store.cu", "gkv_store_attn.cu", "gkv_prefix.cu", "gkv_store_api.cu"]
+            "gkv_static_scratch.cu", "gkv_store.cu", "gkv_store_attn.cu", "gkv_prefix.cu", "gkv_store_api.cu", "gkv_rotary.cu", "gkv_pages.cu", "gkv_pages_attn.cu",
+            "gkv_pages_api.cu"]
 
 GKV_OK, GKV_ERR_INVALID_ARG, GKV_ERR_STATE, GKV_ERR_CAPACITY, GKV_ERR_CUDA, GKV_ERR_TIMEOUT, GKV_ERR_UNSUPPORTED, \
     GKV_ERR_SCRATCH_LIMIT, GKV_ERR_INTERNAL = range(9)
@@ -30,6 +31,10 @@ GKV_MODE_MAX, GKV_MODE_MEAN, GKV_MODE_SUM, GKV_MODE_LOCAL = range(4)
 GKV_STAGE_SCORE, GKV_STAGE_MERGE, GKV_STAGE_SELECT, GKV_STAGE_COMPACT, GKV_STAGE_REDUNDANCY = range(5)
 GKV_POLICY_SCORE, GKV_POLICY_STREAMING = range(2)
 GKV_STORE_BF16, GKV_STORE_E4M3, GKV_STORE_INT8, GKV_STORE_INT4 = range(4)
+GKV_TYPE_BF16, GKV_TYPE_FP16, GKV_TYPE_FP32 = range(3)
+GKV_ROTARY_PLAIN, GKV_ROTARY_LINEAR, GKV_ROTARY_NTK, GKV_ROTARY_WAVELENGTH, GKV_ROTARY_YARN = range(5)
+ROTARY_SCALINGS = {"plain": GKV_ROTARY_PLAIN, "linear": GKV_ROTARY_LINEAR, "ntk": GKV_ROTARY_NTK, "wavelength": GKV_ROTARY_WAVELENGTH,
+                   "yarn": GKV_ROTARY_YARN}
 STORE_FORMATS = {"bf16": GKV_STORE_BF16, "e4m3": GKV_STORE_E4M3, "int8": GKV_STORE_INT8, "int4": GKV_STORE_INT4}
 
 
@@ -85,6 +90,25 @@ class gkv_prefix(ctypes.Structure):
                 ("k", ctypes.c_void_p), ("v", ctypes.c_void_p)]
 
 
+class gkv_rotary(ctypes.Structure):
+    _fields_ = [("head_dim", ctypes.c_int32), ("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("factor", ctypes.c_float),
+                ("turns", ctypes.c_void_p)]
+
+
+class gkv_rotary_rows(ctypes.Structure):
+    _fields_ = [("x", ctypes.c_void_p), ("y", ctypes.c_void_p), ("x_stride", ctypes.c_int64 * 3), ("y_stride", ctypes.c_int64 * 3),
+                ("n_heads", ctypes.c_int32)]
+
+
+class gkv_pages(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("format", "n_q_heads", "n_kv_heads", "head_dim", "n_pages", "page_size", "token_major")] + \
+               [(n, ctypes.c_void_p) for n in ("k", "v", "k_scale", "v_scale")]
+
+
+class gkv_page_table(ctypes.Structure):
+    _fields_ = [("page", ctypes.c_void_p), ("stride", ctypes.c_int64), ("batch", ctypes.c_int32), ("width", ctypes.c_int32)]
+
+
 class gkv_memory_model_t(ctypes.Structure):
     _fields_ = [(n, ctypes.c_uint64) for n in ("full_kv", "compressed_kv", "score_cache")]
 
@@ -99,7 +123,7 @@ def build_library(force: bool = False, verbose: bool = False, check_bounds: bool
     if not force and out.exists() and all(out.stat().st_mtime >= d.stat().st_mtime for d in deps):
         return out
     tmp = out.with_suffix(f".so.tmp{os.getpid()}")
-    cmd = ["nvcc", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17", "-shared",
+    cmd = ["nvcc", "-t", "0", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17", "-shared",
            "-Xcompiler", "-fPIC", "-I", str(_ROOT / "include"), "-o", str(tmp)] + [str(s) for s in srcs]
     if check:
         cmd.insert(1, "-DGKV_CHECK_BOUNDS")
@@ -187,6 +211,18 @@ def lib() -> ctypes.CDLL:
         L.gkv_store_attn.argtypes = [P(gkv_store), vp, i32, vp, vp, vp, P(gkv_prefix), vp, vp, vp, u64, vp]
         L.gkv_decode_attn_prefix.argtypes = [vp, i32, vp, vp, vp, P(gkv_prefix), vp, vp, u64, vp]
         L.gkv_selftest_prefix_wait.argtypes = [vp]
+        f64 = ctypes.c_double
+        L.gkv_rotary_frequencies.argtypes = [f64, i32, i32, f64, f64, f64, f64, P(f64), P(ctypes.c_float)]
+        L.gkv_rotary_turns.argtypes = [P(f64), i32, P(u64)]
+        L.gkv_rotary_apply.argtypes = [P(gkv_rotary), i32, i32, i32, vp, i64, i64, vp, P(gkv_rotary_rows), P(gkv_rotary_rows), i32, vp]
+        L.gkv_pages_query_sizes.argtypes = [P(gkv_pages), P(gkv_store_sizes)]
+        L.gkv_pages_append.argtypes = [P(gkv_pages), P(gkv_page_table), vp, vp, i64, i64, i64, vp, vp, i32, P(gkv_rotary), vp, i64, i64, vp]
+        L.gkv_pages_read.argtypes = [P(gkv_pages), P(gkv_page_table), vp, vp, i64, i64, i64, vp, vp, i32, vp]
+        L.gkv_pages_attn_workspace.argtypes = [P(gkv_pages), i32, P(u64)]
+        L.gkv_pages_attn.argtypes = [P(gkv_pages), P(gkv_page_table), vp, i32, vp, i64, vp, vp, i64, P(gkv_rotary), vp, vp, vp, vp, u64, vp]
+        for name in ("gkv_rotary_frequencies", "gkv_rotary_turns", "gkv_rotary_apply", "gkv_pages_query_sizes", "gkv_pages_append",
+                     "gkv_pages_read", "gkv_pages_attn_workspace", "gkv_pages_attn"):
+            getattr(L, name).restype = ctypes.c_int
         for name in ("gkv_store_query_sizes", "gkv_store_write", "gkv_store_read", "gkv_store_attn_workspace",
                      "gkv_store_attn", "gkv_decode_attn_prefix", "gkv_selftest_prefix_wait"):
             getattr(L, name).restype = ctypes.c_int
@@ -218,7 +254,8 @@ def _torch_binding():
         if module.built_for != _binding_built_for():
             raise RuntimeError(f"{path} is a {module.built_for}, this is {_binding_built_for()}: run __graft_entry__.build() again")
         L = lib()
-        module.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (L.gkv_store_write, L.gkv_store_read, L.gkv_store_attn)))
+        module.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
+            L.gkv_store_write, L.gkv_store_read, L.gkv_store_attn, L.gkv_pages_append, L.gkv_pages_read, L.gkv_pages_attn, L.gkv_rotary_apply)))
         _binding = module
     return _binding
 
@@ -394,6 +431,35 @@ def gkv_decode_attn_prefix(ctx, layer, q, k_new, v_new, prefix, out, workspace):
 
 def gkv_selftest_prefix_wait(ctx):
     _check(lib().gkv_selftest_prefix_wait(ctx), "gkv_selftest_prefix_wait")
+
+
+# The calls that rotate tensors and take pages are made by Rotary and PagedStore (below), through csrc/gkv_torch.cpp.
+def gkv_rotary_frequencies(theta, rot_dim, scaling=GKV_ROTARY_PLAIN, scale=1.0, original=0.0, low=0.0, high=0.0):
+    """(radians a position of the rot_dim / 2 pairs, factor); the scalings' formulas are in gkv.h."""
+    out, factor = (ctypes.c_double * max(1, int(rot_dim) // 2))(), ctypes.c_float()
+    _check(lib().gkv_rotary_frequencies(float(theta), _int32(rot_dim, "rot_dim"), int(scaling), float(scale), float(original), float(low),
+                                        float(high), out, ctypes.byref(factor)), "gkv_rotary_frequencies")
+    return list(out), factor.value
+
+
+def gkv_rotary_turns(radians):
+    """Frequencies in radians a position as units of 2^-64 turns."""
+    radians = [float(f) for f in radians]
+    out = (ctypes.c_uint64 * max(1, len(radians)))()
+    _check(lib().gkv_rotary_turns((ctypes.c_double * max(1, len(radians)))(*radians), len(radians), out), "gkv_rotary_turns")
+    return list(out[:len(radians)])
+
+
+def gkv_pages_query_sizes(pages: gkv_pages) -> gkv_store_sizes:
+    out = gkv_store_sizes()
+    _check(lib().gkv_pages_query_sizes(ctypes.byref(pages), ctypes.byref(out)), "gkv_pages_query_sizes")
+    return out
+
+
+def gkv_pages_attn_workspace(pages: gkv_pages, batch: int) -> int:
+    out = ctypes.c_uint64()
+    _check(lib().gkv_pages_attn_workspace(ctypes.byref(pages), _int32(batch, "batch"), ctypes.byref(out)), "gkv_pages_attn_workspace")
+    return out.value
 
 
 # ------------------------------------------------------------------ buffer holder
@@ -593,3 +659,130 @@ class KVStore:
             pre = prefix.at
         _check(self._call.attn(at, dev, length, max_len, q, k_new, v_new, pre, out, lse, ws, ws_bytes), "gkv_store_attn")
         self._call.in_use(self._held)
+
+
+class Rotary:
+    """Rotary positions: the frequencies of the pairs of a head's first 2 len(frequencies) elements, in radians a position, and how the
+    pairs lie (formulas in gkv.h). Rotary.scaled makes the usual ones."""
+
+    def __init__(self, frequencies, *, head_dim=128, interleaved=False, factor=1.0, device=None):
+        import numpy as np
+        import torch
+        turns = np.array(gkv_rotary_turns(frequencies), np.uint64)
+        head_dim, rot_dim = _int32(head_dim, "head_dim"), 2 * len(turns)
+        if not 2 <= rot_dim <= head_dim or head_dim % 2 or head_dim > 512 or not abs(float(factor)) < float("inf"):
+            raise ValueError(f"{len(turns)} frequencies, factor {factor}: 1 to head_dim / 2 of them and a finite factor are needed, with an even "
+                             f"head_dim of 2 to 512 ({head_dim})")
+        device = torch.device(device or "cuda")
+        if device.type != "cuda":
+            raise ValueError(f"the frequencies would be on {device}")
+        self.turns = torch.from_numpy(turns.view(np.int64)).to(device)
+        self.device, self.head_dim, self.rot_dim = self.turns.device, head_dim, rot_dim
+        self.desc = gkv_rotary(head_dim, rot_dim, int(bool(interleaved)), float(factor), self.turns.data_ptr())
+        self.at = ctypes.addressof(self.desc)
+        self._call = _torch_binding()
+        self._held = (torch.cuda.current_stream(self.device).cuda_stream, self.device.index, self.turns)
+
+    @classmethod
+    def scaled(cls, theta, rot_dim=128, *, scaling="plain", scale=1.0, original=0.0, low=1.0, high=None, head_dim=128, interleaved=False,
+               device=None):
+        """Base frequencies theta^(-2i / rot_dim), for a context `scale` times the original one by one of ROTARY_SCALINGS. low, high: the
+        turns in the original context between which "wavelength" (high: 4 by default) and "yarn" (32) blend."""
+        if scaling not in ROTARY_SCALINGS:
+            raise ValueError(f"scaling {scaling!r}: one of {sorted(ROTARY_SCALINGS)} is needed")
+        high = (4.0 if scaling == "wavelength" else 32.0) if high is None else high
+        frequencies, factor = gkv_rotary_frequencies(theta, rot_dim, ROTARY_SCALINGS[scaling], scale, original, low, high)
+        return cls(frequencies, head_dim=head_dim, interleaved=interleaved, factor=factor, device=device)
+
+    def apply(self, pos, q, k=None, *, q_out=None, k_out=None, count=None, transpose=False):
+        """Rotate q and k in one launch, in place or into q_out, k_out. q, k: [batch][tokens][their heads][head_dim] in bf16, fp16 or fp32, any
+        strides whose last one is 1; pos: int32 [batch][tokens] on the device; count: int32 [batch], tokens from count[i] on are left as
+        they were. transpose turns the other way: given the gradients of what was rotated, it leaves those of q and k."""
+        _check(self._call.rotary(self.at, self.device.index, pos, q, k, q_out, k_out, count, transpose), "gkv_rotary_apply")
+        self._call.in_use(self._held)
+
+
+class PagedStore:
+    """K and V rows of one layer in pages (layouts in gkv.h), with the workspace of their attention for up to max_batch sequences.
+
+    fmt: "bf16", "e4m3", "int8" or "int4". The pages are allocated here (uninitialised) or given as buffers: (k, v, k_scale, v_scale),
+    for bf16 (k, v), each [pages][h_kv][page_size][...] or, token_major, [pages][page_size][h_kv][...]. Every call takes the table of its
+    sequences, int32 [batch][places] on the device: row r of sequence i is row r % page_size of page table[i][r // page_size]. Calls of
+    one store must not overlap on the GPU (they share the workspace). What has been allocated here may be dropped while streams still work on it
+    (given buffers and a call's tensors are the caller's to keep)."""
+
+    def __init__(self, fmt, *, pages, page_size, h_q, h_kv, max_batch, token_major=False, device=None, buffers=None):
+        import torch
+        if fmt not in STORE_FORMATS:
+            raise ValueError(f"format {fmt!r}: one of {sorted(STORE_FORMATS)} is needed")
+        pages, page_size, h_q, h_kv, max_batch = (_int32(n, what) for n, what in (
+            (pages, "pages"), (page_size, "page_size"), (h_q, "h_q"), (h_kv, "h_kv"), (max_batch, "max_batch")))
+        self.fmt, self.pages, self.page_size, self.h_q, self.h_kv, self.max_batch = fmt, pages, page_size, h_q, h_kv, max_batch
+        self.token_major = bool(token_major)
+        self.desc = gkv_pages(STORE_FORMATS[fmt], h_q, h_kv, 128, pages, page_size, int(self.token_major))
+        self.sizes = gkv_pages_query_sizes(self.desc)
+        given = buffers is not None
+        code = {"bf16": torch.bfloat16, "e4m3": torch.float8_e4m3fn, "int8": torch.int8, "int4": torch.uint8}[fmt]
+        scales = {"bf16": 0, "e4m3": 1, "int8": 1, "int4": 4}[fmt]
+        rows = (pages, page_size, h_kv) if self.token_major else (pages, h_kv, page_size)
+        shape, s_shape = torch.Size((*rows, 64 if fmt == "int4" else 128)), torch.Size((*rows, scales))
+        ws_bytes = gkv_pages_attn_workspace(self.desc, max_batch)
+        if buffers is None:
+            device = torch.device(device or "cuda")
+            buffers = [torch.empty(shape, dtype=code, device=device) for _ in range(2)]
+            if scales:
+                buffers += [torch.empty(s_shape, dtype=torch.bfloat16, device=device) for _ in range(2)]
+        if len(buffers) != (4 if scales else 2):
+            raise ValueError(f"{len(buffers)} buffers for format {fmt}")
+        self.device = buffers[0].device
+        for t, n in zip(buffers, ("k", "v")):
+            setattr(self.desc, n, _tensor(t, n, code, shape, self.device))
+        for t, n in zip(buffers[2:], ("k_scale", "v_scale")):
+            setattr(self.desc, n, _tensor(t, n, torch.bfloat16, s_shape, self.device))
+        self.k, self.v = buffers[0], buffers[1]
+        self.k_scale, self.v_scale = (buffers[2], buffers[3]) if scales else (None, None)
+        if self.device.type != "cuda":
+            raise ValueError(f"the buffers are on {self.device}")
+        self.workspace = torch.empty(ws_bytes, dtype=torch.uint8, device=self.device)
+        self._call = _torch_binding()
+        # what has been allocated here, and on which stream
+        self._held = (torch.cuda.current_stream(self.device).cuda_stream, self.device.index, self.workspace) + (() if given else tuple(buffers))
+        self._at = (ctypes.addressof(self.desc), self.device.index, max_batch)
+        self._ws = (self.workspace.data_ptr(), self.workspace.numel())
+
+    def _rotary(self, rotary):
+        if rotary is None:
+            return 0
+        if rotary.head_dim != 128 or rotary.device != self.device:
+            raise ValueError(f"the rotary is for heads of {rotary.head_dim} on {rotary.device}, the pages hold 128 on {self.device}")
+        return rotary.at
+
+    def _used(self, rotary):
+        self._call.in_use(self._held)
+        if rotary is not None:
+            self._call.in_use(rotary._held)
+
+    def append(self, table, k, v, first=None, count=None, rotary=None, pos=None):
+        """Quantise tokens into rows first[i] .. first[i] + count[i] - 1 of every sequence i, keys rotated on the way if there is a rotary, at
+        positions pos (int32 [batch][tokens] on the device; None: the rows' numbers). k, v: bf16 [batch][tokens][kv heads][128] with any
+        strides whose last one is 1, the same ones for both; first, count: int32 on the device (None: 0 and all tokens)."""
+        at, dev, _ = self._at
+        _check(self._call.pages_copy(False, at, dev, table, k, v, first, count, self._rotary(rotary), pos), "gkv_pages_append")
+        self._used(rotary)
+
+    def read(self, table, k, v, first=None, count=None):
+        """Read the same rows back as bf16 into k and v, whose rows may not overlap; tokens from count[i] on are left as they were."""
+        at, dev, _ = self._at
+        _check(self._call.pages_copy(True, at, dev, table, k, v, first, count, 0, None), "gkv_pages_read")
+        self._used(None)
+
+    def attn(self, table, length, q, out, k_new=None, v_new=None, rotary=None, pos=None, lse=None, max_len=0):
+        """Decode attention over rows 0 .. length[i] - 1 (int32 on the device) and the new token, which is appended at row length[i]. With a
+        rotary, q and k_new are rotated on the way, at pos[i] (int32 on the device; None: the number of the last row). q, k_new, v_new:
+        bf16 [batch][their heads][128], slices of one projection's output if need be. The caller counts length up. max_len: the longest
+        length (0: what the table can hold)."""
+        at, dev, most = self._at
+        ws, ws_bytes = self._ws
+        _check(self._call.pages_attn(at, dev, most, table, length, max_len, q, k_new, v_new, self._rotary(rotary), pos, out, lse, ws, ws_bytes),
+               "gkv_pages_attn")
+        self._used(rotary)

@@ -177,6 +177,59 @@ struct PrefixWatch {
     int give_up;       // take the waits for expired (self-test)
 };
 
+// ---- rotary positions and pages
+struct RotaryView {            // a gkv_rotary as the kernels take it
+    const uint64_t* turns;     // NULL: nothing is rotated
+    int half, interleaved;     // pairs; how they lie
+    float factor;
+};
+struct RotaryRows { const void* x; void* y; int64_t xs[3], ys[3]; };
+struct RotaryLaunch {
+    RotaryView rotary;
+    float sign;                // -1: the other way
+    const int32_t *pos, *count;
+    int64_t pos_seq_stride, pos_token_stride;
+    RotaryRows rows[2];
+    int heads0, heads;         // of the first tensor, of both
+    int batch, n_tokens;
+    int tokens_per_cta, pair_runs, runs;   // runs of pairs of a row, and with those that are copied (launch_rotary)
+};
+
+struct PagesView {             // pages and the table through which their rows are found
+    uint8_t* data[2];
+    __nv_bfloat16* scale[2];
+    const int32_t* table;
+    int64_t table_stride;
+    uint64_t inv_page;         // ceil(2^40 / page_size): r * inv_page >> 40 = r / page_size for r < 2^24, page_size <= 2^16
+    int n_pages, page_size;
+    uint32_t page_rows, head_rows, token_rows;   // rows from one page, head, token to the next
+};
+struct PagesCopyLaunch {       // append / read
+    PagesView pages;
+    RotaryView rotary;
+    const int32_t* pos;        // may be NULL: the row's number
+    int64_t pos_seq_stride, pos_token_stride;
+    __nv_bfloat16* x[2];
+    int64_t seq_stride, token_stride, head_stride;
+    const int32_t *first, *count;   // may be NULL
+    int batch, h_kv, capacity, n_tokens, format;
+};
+// (The names that it shares with StoreAttnLaunch are those of the code that both kinds of attention have in common. It is a
+// struct of its own because the host pays for the length of what a launch carries.)
+struct PagesAttnLaunch {
+    PagesView pages;
+    RotaryView rotary;
+    const int32_t *pos, *len;
+    const __nv_bfloat16 *q, *k_new, *v_new;
+    int64_t q_stride, kv_stride;
+    __nv_bfloat16* out;
+    float* lse;
+    float* own_part;
+    int batch, h_q, h_kv, g, capacity;
+    int splits, split_tiles;
+    float scale_log2;
+};
+
 }  // namespace gkv
 
 struct gkv_ctx {
@@ -228,6 +281,14 @@ int store_attn_ctas_per_sm(int format);                                         
 bool store_needs_merge(const StoreAttnLaunch& p);                                           // partial results go through the workspace
 cudaError_t launch_store_merge(const StoreAttnLaunch& p, cudaStream_t s);
 void store_plan(StoreAttnLaunch* p, int max_len, int sm_count);                             // splits, row blocks, chunk, items
+cudaError_t launch_rotary(RotaryLaunch& p, int type, int head_dim, int sm_count, cudaStream_t s);
+cudaError_t launch_pages_append(const PagesCopyLaunch& p, cudaStream_t s);
+cudaError_t launch_pages_read(const PagesCopyLaunch& p, cudaStream_t s);
+cudaError_t launch_pages_attn(const PagesAttnLaunch& p, int format, int mode, cudaStream_t s);
+enum { kPagesWhole = 0, kPagesCluster = 1, kPagesDealt = 2 };                              // mode: how a unit's pieces are joined
+int device_sm_count();                                                                      // of the current device
+uint64_t own_part_bytes(const gkv_store* s, bool merged);                                   // partial results of own rows, at any lengths
+bool rows_overlap(int64_t width, const int64_t (&n)[3], const int64_t (&s)[3]);             // of an array of rows
 gkv_status encode_map(CUtensorMap* map, void* base, uint64_t rows, uint32_t box_rows);      // [rows][128] bf16, 64-element boxes
 
 }  // namespace gkv

@@ -63,23 +63,7 @@ __global__ void __launch_bounds__(kCopyThreads) gkv_store_copy_kernel(const Stor
     } else {
         float inv0 = 1.f, inv1 = 1.f;
         if (Fm::kScales != 0) {
-            // Maxima of the 8 tokens, reduced and handed out at once: a lane gives away half of what it holds at every step
-            // (7 exchanges for 8 tokens instead of 3 or 4 for each), until it has the token of its scale.
-            uint32_t a[kRun];
-#pragma unroll
-            for (int i = 0; i < kRun; ++i) a[i] = store_lane_max<F>(v[i]);
-#pragma unroll
-            for (int o = 8, n = kRun / 2; o >= 2; o >>= 1, n >>= 1) {
-                const bool upper = (l & o) != 0;
-#pragma unroll
-                for (int i = 0; i < kRun / 2; ++i)
-                    if (i < n) {
-                        const uint32_t keep = upper ? a[i + n] : a[i], give = upper ? a[i] : a[i + n];
-                        a[i] = __vmaxu2(keep, __shfl_xor_sync(0xffffffffu, give, o));
-                    }
-            }
-            if (F != GKV_STORE_INT4) a[0] = __vmaxu2(a[0], __shfl_xor_sync(0xffffffffu, a[0], 1));
-            const uint32_t sc = store_scale<F>(a[0], &inv0, &inv1);
+            const uint32_t sc = store_run_scales<F>(v, l, &inv0, &inv1);
             if (has_scale) {
                 if (F == GKV_STORE_INT4) *scale4 = sc;
                 else *scale2 = (uint16_t)sc;

@@ -55,13 +55,6 @@ int64_t prefix_items(const StoreAttnLaunch& p, int chunk) {
     return items * p.h_kv * p.n_blocks;
 }
 
-// Upper bounds over all lengths, without a device. Partial results of own rows: of every unit when they are merged with
-// something else, and of the pieces of cut units.
-uint64_t own_part_bytes(const gkv_store* s, bool merged) {
-    const uint64_t units = (uint64_t)s->batch * s->n_kv_heads;
-    const uint64_t pieces = units * kMaxPieces < (uint64_t)kSplitUnits ? units * kMaxPieces : (uint64_t)kSplitUnits;
-    return align_up((pieces > units || !merged ? pieces : units) * kOwnRecFloats * 4);
-}
 uint64_t prefix_part_bytes(const gkv_store* s, int n_prefix, int rows) {
     if (n_prefix == 0 || rows == 0) return 0;
     int per_block, blocks, two;
@@ -82,28 +75,6 @@ gkv_status check_prefix(const gkv_prefix* x, int batch, int h_kv) {
     // row coordinates of the tensor maps are signed 32-bit numbers, and a tile may reach past the end
     if ((int64_t)x->n_prefix * h_kv * x->rows >= (1ll << 31) - 256) return GKV_ERR_UNSUPPORTED;
     return GKV_OK;
-}
-
-// Whether elements of an array of rows of 128 share an address (or may, with strides that no slice of an array has).
-bool rows_overlap(int64_t n0, int64_t s0, int64_t n1, int64_t s1, int64_t n2, int64_t s2) {
-    int64_t n[3] = {n0, n1, n2}, s[3] = {s0, s1, s2};
-    int64_t least = kHeadDim;                  // the next larger stride has to step over what the smaller ones span
-    for (int k = 0; k < 3; ++k) {
-        int next = -1;
-        for (int i = 0; i < 3; ++i)
-            if (n[i] > 1 && (next < 0 || s[i] < s[next])) next = i;
-        if (next < 0) break;
-        if (s[next] < least || s[next] > INT64_MAX / n[next]) return true;
-        least = s[next] * n[next];
-        n[next] = 1;
-    }
-    return false;
-}
-
-int device_sm_count() {
-    int dev = 0, sm = 0;
-    if (cudaGetDevice(&dev) == cudaSuccess) cudaDeviceGetAttribute(&sm, cudaDevAttrMultiProcessorCount, dev);
-    return sm > 0 ? sm : 148;
 }
 
 // Everything of an attention launch that is not a pointer, then the launches. `p` has its pointers and shape.
@@ -157,7 +128,7 @@ gkv_status copy_args(const gkv_store* store, const void* k, const void* v, int64
     if (seq_stride < 0 || token_stride < 0 || head_stride < 0 || ((seq_stride | token_stride | head_stride) & 7) != 0) return GKV_ERR_INVALID_ARG;
     if ((int64_t)n_tokens * store->n_kv_heads >= (1ll << 30)) return GKV_ERR_UNSUPPORTED;
     if (read && n_tokens > 0 && k == v) return GKV_ERR_INVALID_ARG;
-    if (read && n_tokens > 0 && rows_overlap(store->batch, seq_stride, n_tokens, token_stride, store->n_kv_heads, head_stride)) return GKV_ERR_INVALID_ARG;
+    if (read && n_tokens > 0 && rows_overlap(kHeadDim, {store->batch, n_tokens, store->n_kv_heads}, {seq_stride, token_stride, head_stride})) return GKV_ERR_INVALID_ARG;
     p->data[0] = static_cast<uint8_t*>(store->k); p->data[1] = static_cast<uint8_t*>(store->v);
     p->scale[0] = static_cast<__nv_bfloat16*>(store->k_scale); p->scale[1] = static_cast<__nv_bfloat16*>(store->v_scale);
     p->x[0] = static_cast<__nv_bfloat16*>(const_cast<void*>(k)); p->x[1] = static_cast<__nv_bfloat16*>(const_cast<void*>(v));
@@ -170,6 +141,35 @@ gkv_status copy_args(const gkv_store* store, const void* k, const void* v, int64
 }  // namespace
 
 namespace gkv {
+
+// Upper bounds over all lengths, without a device. Partial results of own rows: of every unit when they are merged with
+// something else, and of the pieces of cut units.
+uint64_t own_part_bytes(const gkv_store* s, bool merged) {
+    const uint64_t units = (uint64_t)s->batch * s->n_kv_heads;
+    const uint64_t pieces = units * kMaxPieces < (uint64_t)kSplitUnits ? units * kMaxPieces : (uint64_t)kSplitUnits;
+    return align_up((pieces > units || !merged ? pieces : units) * kOwnRecFloats * 4);
+}
+// Whether elements of an array of rows of `width` share an address (or may, with strides that no slice of an array has).
+bool rows_overlap(int64_t width, const int64_t (&sizes)[3], const int64_t (&s)[3]) {
+    int64_t n[3] = {sizes[0], sizes[1], sizes[2]};
+    int64_t least = width;                  // the next larger stride has to step over what the smaller ones span
+    for (int k = 0; k < 3; ++k) {
+        int next = -1;
+        for (int i = 0; i < 3; ++i)
+            if (n[i] > 1 && (next < 0 || s[i] < s[next])) next = i;
+        if (next < 0) break;
+        if (s[next] < least || s[next] > INT64_MAX / n[next]) return true;
+        least = s[next] * n[next];
+        n[next] = 1;
+    }
+    return false;
+}
+
+int device_sm_count() {
+    int dev = 0, sm = 0;
+    if (cudaGetDevice(&dev) == cudaSuccess) cudaDeviceGetAttribute(&sm, cudaDevAttrMultiProcessorCount, dev);
+    return sm > 0 ? sm : 148;
+}
 
 // Own rows: as many pieces per unit as fill the places of resident CTAs, none below 8 tiles (two turns of the four warps). (With
 // more units than half the places units go whole: cutting 1024 units into thirds, to fill the last round of CTAs better, took 157

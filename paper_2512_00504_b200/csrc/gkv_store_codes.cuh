@@ -11,6 +11,7 @@
 
 #include "gkv_common.cuh"
 #include "gkv_internal.h"
+#include "gkv_store_rows.h"
 
 namespace gkv {
 
@@ -153,6 +154,29 @@ __device__ __forceinline__ void store_put_row(uint8_t* row, __nv_bfloat16* scale
         else if (l == 0) *reinterpret_cast<uint16_t*>(scale) = (uint16_t)s;
     }
     store_put_codes<F>(row, l, store_codes<F>(x, inv0, inv1));
+}
+
+// Scales of a run of kRun rows (half a warp, lane l of 16 with 8 elements of each): what store_scale gives for token l >> 1, in 4 bits
+// for groups 2j and 2j + 1 with j = l & 1.
+template <int F>
+__device__ __forceinline__ uint32_t store_run_scales(const uint4 (&v)[kRun], int l, float* inv0, float* inv1) {
+    // Maxima of the 8 tokens, reduced and handed out at once: a lane gives away half of what it holds at every step
+    // (7 exchanges for 8 tokens instead of 3 or 4 for each), until it has the token of its scale.
+    uint32_t a[kRun];
+#pragma unroll
+    for (int i = 0; i < kRun; ++i) a[i] = store_lane_max<F>(v[i]);
+#pragma unroll
+    for (int o = 8, n = kRun / 2; o >= 2; o >>= 1, n >>= 1) {
+        const bool upper = (l & o) != 0;
+#pragma unroll
+        for (int i = 0; i < kRun / 2; ++i)
+            if (i < n) {
+                const uint32_t keep = upper ? a[i + n] : a[i], give = upper ? a[i] : a[i + n];
+                a[i] = __vmaxu2(keep, __shfl_xor_sync(0xffffffffu, give, o));
+            }
+    }
+    if (F != GKV_STORE_INT4) a[0] = __vmaxu2(a[0], __shfl_xor_sync(0xffffffffu, a[0], 1));
+    return store_scale<F>(a[0], inv0, inv1);
 }
 
 template <int F>
