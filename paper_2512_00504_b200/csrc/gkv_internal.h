@@ -213,6 +213,7 @@ struct PagesCopyLaunch {       // append / read
     int64_t seq_stride, token_stride, head_stride;
     const int32_t *first, *count;   // may be NULL
     int batch, h_kv, capacity, n_tokens, format;
+    int head_blocks, heads_per_cta, tokens_per_half;   // how an append is cut (launch_pages_append)
 };
 // (The names that it shares with StoreAttnLaunch are those of the code that both kinds of attention have in common. It is a
 // struct of its own because the host pays for the length of what a launch carries.)

@@ -1,11 +1,21 @@
 // Appending rows to a cache in pages, with keys rotated on the way, and reading them back.
 //
-// As the copies of a store (half a warp takes kRun tokens of a head, all loads first), bound by HBM, with two things more. A token's row
-// is found through the table: eight lanes look up the eight tokens of the run while its loads are on their way, and hand the rows
-// round. And keys are rotated: cos and sin depend on the token and the pair alone, so a CTA works them out once for the tokens
-// of its runs, in shared memory, for all heads that it has of them. Pairs (i, i + rot_dim / 2) lie in two lanes; the partner's elements are
-// loaded a second time, which the L1 answers, and each lane turns its own side. What is rotated is rounded to bf16 and goes on from
-// there as if it had been read, so that a fused append leaves the bits that rotating first would.
+// Bound by HBM, as the copies of a store, with two things more: a token's row is found through the table, and keys are rotated. cos
+// and sin depend on the token and the pair alone, and cost more than all else that is done to a pair. So a half warp that appends has the
+// heads of one token (up to kRun rows, all of whose loads start first) and holds the cos and sin of its lanes' elements in registers; the
+// CTA works them out once for its tokens, through shared memory. (With kRun tokens of one head instead, as the store's copies go, every row
+// reads its own cos and sin from shared memory: 4 x 32768 tokens x 8 heads in bf16 302 us.) K and V take turns in the grid, so that K's
+// arithmetic runs while V moves. A lane has 8 neighbouring elements, those on the other side of their pairs come from another lane. What
+// is rotated is rounded to bf16 and goes on from there as if it had been read, so that a fused append leaves the bits that rotating first would.
+// Scales of one head's rows lie next to one another in a page while a half warp has different heads: the CTA gathers them in shared memory and
+// writes those of its tokens together.
+//
+// Reading back takes kRun tokens of a head, so that scales come with one access.
+//
+// Measured (bytes of both sides): 4 x 32768 tokens x 8 heads in bf16, rotated, 1.07 GB in 161 us, 6.7 TB/s; 8 prompts of 129 to 4097 tokens x 4
+// heads, 70 MB in bf16 in 18.7 us (16.2 without the rotation), 52 MB in 8 bits in 21.4 (14.4), in 4 bits 24.2 (14.8): a few rounds of CTAs,
+// each a chain of count, rows, arithmetic; back in 13.5 to 16.1. One token of 32 sequences x 4 heads: 3.5 us in bf16, 4.6 in 8 bits (1.9 and
+// 2.9 without the rotation).
 #include "gkv_pages.cuh"
 #include "gkv_rotary.cuh"
 #include "gkv_store_rows.h"
@@ -15,185 +25,304 @@ namespace gkv {
 constexpr int kPageCopyThreads = 128;
 constexpr int kPageCopyItems = kPageCopyThreads / 16;
 
-// What a copy does to K: moves it out, in as it is, or in with the rotation of pairs that are neighbours, that lie half of rot_dim apart (a
-// multiple of 4 elements), or the same by single elements.
-enum { kRead = 0, kWrite = 1, kWriteNeighbours = 2, kWriteHalves = 3, kWriteAny = 4 };
-
-// First element of a lane's first and last four.
-template <int F> __device__ __forceinline__ int lane_dim(int l, int which) {
-    return F == GKV_STORE_INT4 ? 64 * (l & 1) + 4 * (l >> 1) + 32 * which : 8 * l + 4 * which;
+// The 8 elements of a row that lane l has, neighbours or those of format F. These loads stay where they are written: all of them ahead of
+// what they are to overlap with. (Left to the compiler, they were put off to the rows' turn where registers were short: an append of
+// ragged prompts in 8 bits took 31 us instead of 21.)
+template <int F>
+__device__ __forceinline__ uint4 load_row(const __nv_bfloat16* row, int l, bool neighbours) {
+    uint4 r;
+    if (F != GKV_STORE_INT4 || neighbours) {
+        asm volatile("ld.global.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "l"(row + 8 * l) : "memory");
+    } else {
+        const __nv_bfloat16* x = row + 64 * (l & 1) + 4 * (l >> 1);
+        asm volatile("ld.global.v2.u32 {%0, %1}, [%2];" : "=r"(r.x), "=r"(r.y) : "l"(x) : "memory");
+        asm volatile("ld.global.v2.u32 {%0, %1}, [%2];" : "=r"(r.z), "=r"(r.w) : "l"(x + 32) : "memory");
+    }
+    return r;
 }
 
-// Four elements of a row (elements e .. e + 3, two packed words) turned. partner: the other sides of their pairs, where those are not
-// among them; c, s: cos and sin of the token's pairs.
+// How keys are turned: not at all; pairs that are neighbours, rot_dim a multiple of a lane's 8 elements; pairs a multiple of 8 elements apart;
+// any others.
+enum { kStraight = 0, kNeighbours = 1, kLanes = 2, kAny = 3 };
+
+// cos and sin of what a lane has of a token: of the pairs of its 8 elements, or (neighbours) of its 4 pairs.
 template <int OP>
-__device__ __forceinline__ uint2 rotate_four(uint2 x, uint2 partner, int e, int half, const float* c, const float* s) {
-    float v[4] = {bf16_lo(x.x), bf16_hi(x.x), bf16_lo(x.y), bf16_hi(x.y)};
-    if (OP == kWriteNeighbours) {
+struct LaneTurn {
+    static constexpr int N = OP == kNeighbours ? 1 : 2;
+    float4 c[N], s[N];
+    __device__ __forceinline__ void load(int l, int half, const float* cos, const float* sin) {
+        const int at = OP == kNeighbours ? 4 * l : 8 * l < half ? 8 * l : 8 * l - half;      // (lanes behind the pairs: not used)
+        if (OP == kNeighbours ? at < half : 8 * l < 2 * half)
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int pair = (e >> 1) + i;
-            if (pair < half) {
-                const float2 r = rotary_turn(v[2 * i], v[2 * i + 1], c[pair], s[pair]);
-                v[2 * i] = r.x; v[2 * i + 1] = r.y;
+            for (int i = 0; i < N; ++i) {
+                c[i] = reinterpret_cast<const float4*>(cos + at)[i];
+                s[i] = reinterpret_cast<const float4*>(sin + at)[i];
             }
-        }
-    } else {
-        const float w[4] = {bf16_lo(partner.x), bf16_hi(partner.x), bf16_lo(partner.y), bf16_hi(partner.y)};
+    }
+};
+// A lane's 8 elements of a row, turned: x c + y s with y the other sides of their pairs, negated where x is the first side, and both products
+// in the order of rotary_turn.
+template <int OP>
+__device__ __forceinline__ uint4 turn_lane(const LaneTurn<OP>& r, uint4 v, int l, int half) {
+    const uint32_t x[4] = {v.x, v.y, v.z, v.w};
+    const bool first = 8 * l < half;
+    const int from = first ? l + half / 8 : l - half / 8;
+    const uint32_t minus = OP == kNeighbours ? 0x00008000u : first ? 0x80008000u : 0u;
+    uint32_t y[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int d = e + i;                       // (halves a multiple of 4 apart: all four are on the same side)
-            if (d < half) v[i] = rotary_turn(v[i], w[i], c[d], s[d]).x;
-            else if (d < 2 * half) v[i] = rotary_turn(w[i], v[i], c[d - half], s[d - half]).y;
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t o = (OP == kNeighbours ? __byte_perm(x[i], 0u, 0x1032) : __shfl_sync(0xffffffffu, x[i], from, 16)) ^ minus;
+        const float4 c4 = r.c[OP == kNeighbours ? 0 : i >> 1], s4 = r.s[OP == kNeighbours ? 0 : i >> 1];
+        auto pick = [](const float4& f, int k) { return k == 0 ? f.x : k == 1 ? f.y : k == 2 ? f.z : f.w; };
+        const int ka = OP == kNeighbours ? i : 2 * (i & 1), kb = OP == kNeighbours ? i : ka + 1;
+        y[i] = pack_bf16x2(__fmaf_rn(bf16_lo(x[i]), pick(c4, ka), __fmul_rn(bf16_lo(o), pick(s4, ka))),
+                           __fmaf_rn(bf16_hi(x[i]), pick(c4, kb), __fmul_rn(bf16_hi(o), pick(s4, kb))));
+    }
+    return 8 * l < 2 * half ? make_uint4(y[0], y[1], y[2], y[3]) : v;
+}
+// The same element by element, for any rot_dim and either order of pairs, with cos and sin from shared memory.
+__device__ __forceinline__ uint4 turn_any(uint4 v, int l, const RotaryView& r, const __nv_bfloat16* row, const float* cos, const float* sin) {
+    uint32_t x[4] = {v.x, v.y, v.z, v.w};
+    const uint16_t* e = reinterpret_cast<const uint16_t*>(row);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int d = 8 * l + i;
+        if (row && d < 2 * r.half) {
+            const bool first = r.interleaved ? i % 2 == 0 : d < r.half;
+            const int pair = r.interleaved ? d >> 1 : first ? d : d - r.half;
+            const int o = r.interleaved ? d ^ 1 : first ? d + r.half : d - r.half;
+            const float a = i & 1 ? bf16_hi(x[i >> 1]) : bf16_lo(x[i >> 1]), b = __uint_as_float((uint32_t)e[o] << 16);
+            const float y = __fmaf_rn(a, cos[pair], __fmul_rn(first ? -b : b, sin[pair]));
+            const uint32_t w = pack_bf16x2(y, y);
+            x[i >> 1] = i & 1 ? __byte_perm(x[i >> 1], w, 0x5410) : __byte_perm(x[i >> 1], w, 0x3254);
         }
     }
-    return make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+    return make_uint4(x[0], x[1], x[2], x[3]);
 }
-// The partners of elements e .. e + 3 of a row.
-template <int OP>
-__device__ __forceinline__ uint2 load_partner(const __nv_bfloat16* row, int e, int half) {
-    if constexpr (OP == kWriteHalves) {
-        if (e >= 2 * half) return make_uint2(0u, 0u);
-        return *reinterpret_cast<const uint2*>(row + (e < half ? e + half : e - half));
-    } else {
-        uint32_t w[4];
+// A row whose lanes have 8 neighbouring elements each -> the elements that lane l has in format F.
+template <int F>
+__device__ __forceinline__ uint4 as_format(uint4 v, int l) {
+    if constexpr (F != GKV_STORE_INT4) return v;
+    const int q = l >> 1, from = 8 * (l & 1) + (q >> 1);
+    uint32_t w[2][4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int d = e + i;
-            w[i] = d < 2 * half ? reinterpret_cast<const uint16_t*>(row)[d < half ? d + half : d - half] : 0u;
+    for (int k = 0; k < 2; ++k) {
+        w[k][0] = __shfl_sync(0xffffffffu, v.x, from + 4 * k, 16);
+        w[k][1] = __shfl_sync(0xffffffffu, v.y, from + 4 * k, 16);
+        w[k][2] = __shfl_sync(0xffffffffu, v.z, from + 4 * k, 16);
+        w[k][3] = __shfl_sync(0xffffffffu, v.w, from + 4 * k, 16);
+    }
+    return q & 1 ? make_uint4(w[0][2], w[0][3], w[1][2], w[1][3]) : make_uint4(w[0][0], w[0][1], w[1][0], w[1][1]);
+}
+
+// CTA: K or V, heads_per_cta heads, 8 * tokens_per_half tokens of sequence blockIdx.y. Half warp w: tokens_per_half tokens from w *
+// tokens_per_half on, all those heads of each (at most kRun rows).
+template <int F, int OP>
+__global__ void __launch_bounds__(kPageCopyThreads) gkv_pages_append_kernel(const PagesCopyLaunch p) {
+    using Fm = StoreFormat<F>;
+    extern __shared__ __align__(16) float s_table[];     // cos and sin of the CTA's tokens: [token][half] each
+    __shared__ uint32_t s_row[kPageCopyItems * kRun];    // [token]: number of head 0's row
+    __shared__ uint2 s_scale[kPageCopyItems * kRun];     // [head][token]
+    const int b = blockIdx.y, l = threadIdx.x & 15, w = threadIdx.x >> 4;
+    const bool is_v = blockIdx.x & 1;
+    const int block = blockIdx.x >> 1, head_block = block % p.head_blocks;
+    const int tokens = kPageCopyItems * p.tokens_per_half, t0 = block / p.head_blocks * tokens;
+    const int head0 = head_block * p.heads_per_cta, heads = min(p.heads_per_cta, p.h_kv - head0);
+    const int half = p.rotary.half;
+    const bool turns = OP != kStraight && !is_v;
+    // This thread's pairs are those of its number and, blockDim by blockDim, on through the tokens: where a token's pairs divide the threads
+    // (the usual case) always the same one, whose frequency is on its way while the count is.
+    int token = 0, pair = 0;
+    uint64_t frequency = 0;
+    if (turns) {
+        token = threadIdx.x / half;
+        pair = threadIdx.x - token * half;
+        frequency = p.rotary.turns[pair];
+    }
+    const int32_t first = p.first ? p.first[b] : 0, count = p.count ? p.count[b] : p.n_tokens;
+    const int n = min(count, p.n_tokens);
+    if (t0 >= n) return;
+    const int t_half = t0 + w * p.tokens_per_half;       // the half warp's first token
+
+    // lane l's token of the half warp, as far as there is one, and what the table has for its row
+    const int mine = t_half + l;
+    const RunRows one = run_rows(first, n, p.n_tokens, p.capacity, mine);
+    const bool there = l < p.tokens_per_half && mine < n && one.lo == 0 && one.hi > 0;
+    const int32_t entry = there ? page_entry(p.pages, p.pages.table + b * p.pages.table_stride, first + mine) : 0;
+    // Row k is head k % heads_per_cta of token k / heads_per_cta.
+    const int rows = p.tokens_per_half * p.heads_per_cta;
+    const __nv_bfloat16* const x = (is_v ? p.x[1] : p.x[0]) + ((int64_t)b * p.seq_stride + (int64_t)t_half * p.token_stride + (int64_t)head0 * p.head_stride);
+    const int64_t next_token = p.token_stride - (p.heads_per_cta - 1) * p.head_stride;
+    uint4 v[kRun];
+    {
+        const __nv_bfloat16* src = x;
+        int t = t_half, h = 0;
+#pragma unroll
+        for (int k = 0; k < kRun; ++k) {
+            v[k] = make_uint4(0u, 0u, 0u, 0u);
+            if (k < rows && h < heads && t < n) v[k] = load_row<F>(src, l, turns);
+            if (++h == p.heads_per_cta) { h = 0; ++t; src += next_token; }
+            else src += p.head_stride;
         }
-        return make_uint2(w[0] | w[1] << 16, w[2] | w[3] << 16);
+    }
+    const uint32_t row = there ? page_row(p.pages, entry, (uint32_t)head0 * p.pages.head_rows, first + mine) : kNoRow;
+    if (OP != kStraight && turns) {
+        float* s_sin = s_table + tokens * half;
+        const int dk = kPageCopyThreads / half, dp = kPageCopyThreads - dk * half, end = min(n - t0, tokens) * half;
+        for (int i = threadIdx.x; i < end; i += kPageCopyThreads) {
+            const int t = t0 + token;
+            const int32_t pos = p.pos ? p.pos[(int64_t)b * p.pos_seq_stride + (int64_t)t * p.pos_token_stride]
+                                      : (int32_t)((uint32_t)first + (uint32_t)t);
+            const float2 cs = rotary_cos_sin(frequency, pos, p.rotary.factor, 1.f);
+            s_table[i] = cs.x;
+            s_sin[i] = cs.y;
+            token += dk;
+            if (dp) {
+                pair += dp;
+                if (pair >= half) { pair -= half; ++token; }
+                frequency = p.rotary.turns[pair];
+            }
+        }
+        __syncthreads();
+        int k0 = w * p.tokens_per_half, h = 0;           // token within the CTA, head
+        if constexpr (OP == kAny) {
+            const __nv_bfloat16* src = x;
+#pragma unroll
+            for (int k = 0; k < kRun; ++k) {
+                if (k < rows)
+                    v[k] = as_format<F>(turn_any(v[k], l, p.rotary, h < heads && t0 + k0 < n ? src : nullptr, s_table + k0 * half, s_sin + k0 * half), l);
+                if (++h == p.heads_per_cta) { h = 0; ++k0; src += next_token; }
+                else src += p.head_stride;
+            }
+        } else {
+            LaneTurn<OP> r;
+#pragma unroll
+            for (int k = 0; k < kRun; ++k) {
+                if (k < rows) {
+                    if (h == 0) r.load(l, half, s_table + k0 * half, s_sin + k0 * half);
+                    v[k] = as_format<F>(turn_lane<OP>(r, v[k], l, half), l);
+                }
+                if (++h == p.heads_per_cta) { h = 0; ++k0; }
+            }
+        }
+    }
+
+    uint8_t* data = is_v ? p.pages.data[1] : p.pages.data[0];
+    if (Fm::kScales != 0 && l < p.tokens_per_half) s_row[w * p.tokens_per_half + l] = row;
+    float inv0 = 1.f, inv1 = 1.f;
+    if (Fm::kScales != 0) {
+        const uint32_t sc = store_run_scales<F>(v, l, &inv0, &inv1);       // lanes 2k, 2k + 1: row k's
+        const int k = l >> 1, i = k / p.heads_per_cta, h = k - i * p.heads_per_cta;
+        if (k < rows && (F == GKV_STORE_INT4 || (l & 1) == 0))
+            reinterpret_cast<uint32_t*>(s_scale + h * tokens + w * p.tokens_per_half + i)[F == GKV_STORE_INT4 ? l & 1 : 0] = sc;
+    }
+    {
+        const size_t head_bytes = (size_t)p.pages.head_rows * Fm::kRow;
+        uint32_t at = __shfl_sync(0xffffffffu, row, 0, 16);
+        uint8_t* dst = data + (size_t)at * Fm::kRow;
+        int i = 0, h = 0;
+#pragma unroll
+        for (int k = 0; k < kRun; ++k) {
+            const int from = 2 * k + (F == GKV_STORE_INT4 ? l & 1 : 0);
+            float f0 = 1.f, f1 = 1.f;
+            if (Fm::kScales != 0) f0 = f1 = __shfl_sync(0xffffffffu, inv0, from, 16);
+            if (F == GKV_STORE_INT4) f1 = __shfl_sync(0xffffffffu, inv1, from, 16);
+            if (k < rows && h < heads && at < kNoPage) store_put_codes<F>(dst, l, store_codes<F>(v[k], f0, f1));
+            dst += head_bytes;
+            if (++h == p.heads_per_cta) {
+                h = 0;
+                at = __shfl_sync(0xffffffffu, row, ++i, 16);
+                dst = data + (size_t)at * Fm::kRow;
+            }
+        }
+    }
+    if (Fm::kScales != 0) {
+        __syncthreads();
+        __nv_bfloat16* scale = is_v ? p.pages.scale[1] : p.pages.scale[0];
+        const int h = threadIdx.x / tokens, t = threadIdx.x - h * tokens;
+        if (h < heads) {
+            const uint32_t at = s_row[t];
+            if (at < kNoPage) {
+                __nv_bfloat16* dst = scale + (size_t)(at + h * p.pages.head_rows) * Fm::kScales;
+                if (F == GKV_STORE_INT4) *reinterpret_cast<uint2*>(dst) = s_scale[threadIdx.x];
+                else *reinterpret_cast<uint16_t*>(dst) = (uint16_t)s_scale[threadIdx.x].x;
+            }
+        }
     }
 }
 
 // Work item i of sequence blockIdx.y: head i % h_kv, tokens kRun * (i / h_kv) and on; blockIdx.z = K or V.
-template <int F, int OP>
-__global__ void __launch_bounds__(kPageCopyThreads) gkv_pages_copy_kernel(const PagesCopyLaunch p) {
+template <int F>
+__global__ void __launch_bounds__(kPageCopyThreads) gkv_pages_read_kernel(const PagesCopyLaunch p) {
     using Fm = StoreFormat<F>;
-    extern __shared__ __align__(16) float s_table[];   // cos and sin of the CTA's tokens: [token][half] each
     const int b = blockIdx.y, l = threadIdx.x & 15;
     const bool is_v = blockIdx.z != 0;
-    const int item0 = blockIdx.x * kPageCopyItems, item = item0 + (threadIdx.x >> 4);
+    const int item = blockIdx.x * kPageCopyItems + (threadIdx.x >> 4);
     const int h = item % p.h_kv, t0 = item / p.h_kv * kRun;
-    const int32_t first = p.first ? p.first[b] : 0, count = p.count ? p.count[b] : p.n_tokens;
+    const int32_t first = p.first ? p.first[b] : 0;
     // the whole warp stays for the shuffles, whatever the run has
-    const RunRows rows = run_rows(first, count, p.n_tokens, p.capacity, t0);
-    const int lo = rows.lo, hi = rows.hi;
-    const int half = p.rotary.half;
-    const bool rotates = OP >= kWriteNeighbours && !is_v;
+    const RunRows rows = run_rows(first, p.count ? p.count[b] : p.n_tokens, p.n_tokens, p.capacity, t0);
     __nv_bfloat16* x = (is_v ? p.x[1] : p.x[0]) + (int64_t)b * p.seq_stride + (int64_t)t0 * p.token_stride + (int64_t)h * p.head_stride;
-
+    const uint8_t* data = is_v ? p.pages.data[1] : p.pages.data[0];
+    const __nv_bfloat16* scale = is_v ? p.pages.scale[1] : p.pages.scale[0];
     // lane l's row: that of token l & 7 of the run
     const int mine = l & (kRun - 1);
     uint32_t row = kNoRow;
-    if (mine >= lo && mine < hi) {
+    if (mine >= rows.lo && mine < rows.hi) {
         const int r = first + t0 + mine;               // (within 0 .. capacity - 1)
         row = page_row(p.pages, page_entry(p.pages, p.pages.table + b * p.pages.table_stride, r), (uint32_t)h * p.pages.head_rows, r);
     }
     uint4 v[kRun];
-    uint2 w[kRun][2];                                  // partners
+    uint32_t at[kRun];
 #pragma unroll
     for (int i = 0; i < kRun; ++i) {
-        v[i] = make_uint4(0u, 0u, 0u, 0u);
-        if (OP != kRead && i >= lo && i < hi) {
-            const __nv_bfloat16* src = x + (int64_t)i * p.token_stride;
-            v[i] = store_load_source<F>(src, l);
-            if (OP >= kWriteHalves && rotates)
-#pragma unroll
-                for (int k = 0; k < 2; ++k) w[i][k] = load_partner<OP>(src, lane_dim<F>(l, k), half);
-        }
+        at[i] = __shfl_sync(0xffffffffu, row, i, 16);
+        v[i] = at[i] < kNoPage ? store_get_codes<F>(data + (size_t)at[i] * Fm::kRow, l) : make_uint4(0u, 0u, 0u, 0u);
     }
-    const int run0 = item0 / p.h_kv;                   // of the CTA's first item
-    if (OP >= kWriteNeighbours && rotates) {
-        const int last = min((item0 + kPageCopyItems - 1) / p.h_kv, (p.n_tokens - 1) / kRun);
-        const int tokens = (last - run0 + 1) * kRun;
-        const int n = count < p.n_tokens ? count : p.n_tokens;
-        float* s_sin = s_table + tokens * half;
-        for (int i = threadIdx.x; i < tokens * half; i += kPageCopyThreads) {
-            const int k = i / half, pair = i - k * half, t = run0 * kRun + k;
-            if (t < n) {
-                const int32_t pos = p.pos ? p.pos[(int64_t)b * p.pos_seq_stride + (int64_t)t * p.pos_token_stride]
-                                          : (int32_t)((uint32_t)first + (uint32_t)t);
-                const float2 cs = rotary_cos_sin(p.rotary.turns[pair], pos, p.rotary.factor, 1.f);
-                s_table[i] = cs.x;
-                s_sin[i] = cs.y;
-            }
-        }
-        __syncthreads();
-        const float* c = s_table + (t0 - run0 * kRun) * half;
-        const float* s = s_sin + (t0 - run0 * kRun) * half;
-#pragma unroll
-        for (int i = 0; i < kRun; ++i)
-            if (i >= lo && i < hi) {
-                const uint2 a = rotate_four<OP>(make_uint2(v[i].x, v[i].y), w[i][0], lane_dim<F>(l, 0), half, c + i * half, s + i * half);
-                const uint2 z = rotate_four<OP>(make_uint2(v[i].z, v[i].w), w[i][1], lane_dim<F>(l, 1), half, c + i * half, s + i * half);
-                v[i] = make_uint4(a.x, a.y, z.x, z.y);
-            }
-    }
-
-    uint8_t* data = is_v ? p.pages.data[1] : p.pages.data[0];
-    __nv_bfloat16* scale = is_v ? p.pages.scale[1] : p.pages.scale[0];
-    // Scales are held and moved by lane 2i + j: in 4 bits those of groups 2j, 2j + 1 of token i, in 8 bits that of token i (the
-    // odd lane has a copy).
+    // Scales are held by lane 2i + j: in 4 bits those of groups 2j, 2j + 1 of token i, in 8 bits that of token i.
     const uint32_t scale_row = __shfl_sync(0xffffffffu, row, l >> 1, 16);
-    const bool has_scale = Fm::kScales != 0 && scale_row < kNoPage && (F == GKV_STORE_INT4 || (l & 1) == 0);
-    uint32_t* scale4 = reinterpret_cast<uint32_t*>(scale) + (size_t)scale_row * 2 + (l & 1);
-    uint16_t* scale2 = reinterpret_cast<uint16_t*>(scale) + scale_row;
-    if (OP == kRead) {
-        uint32_t at[kRun];
-#pragma unroll
-        for (int i = 0; i < kRun; ++i) {
-            at[i] = __shfl_sync(0xffffffffu, row, i, 16);
-            if (at[i] < kNoPage) v[i] = store_get_codes<F>(data + (size_t)at[i] * Fm::kRow, l);
-        }
-        uint32_t sc = 0u;
-        if (has_scale) sc = F == GKV_STORE_INT4 ? *scale4 : *scale2;
-#pragma unroll
-        for (int i = 0; i < kRun; ++i) {
-            const uint32_t s = __shfl_sync(0xffffffffu, sc, 2 * i + (F == GKV_STORE_INT4 ? l & 1 : 0), 16);
-            if (at[i] < kNoPage) store_put_target<F>(x + (int64_t)i * p.token_stride, l, store_decode<F>(v[i], s));
-        }
-        return;
-    }
-    float inv0 = 1.f, inv1 = 1.f;
-    if (Fm::kScales != 0) {
-        const uint32_t sc = store_run_scales<F>(v, l, &inv0, &inv1);
-        if (has_scale) {
-            if (F == GKV_STORE_INT4) *scale4 = sc;
-            else *scale2 = (uint16_t)sc;
-        }
-    }
+    uint32_t sc = 0u;
+    if (Fm::kScales != 0 && scale_row < kNoPage)
+        sc = F == GKV_STORE_INT4 ? *(reinterpret_cast<const uint32_t*>(scale) + (size_t)scale_row * 2 + (l & 1))
+                                 : *(reinterpret_cast<const uint16_t*>(scale) + scale_row);
 #pragma unroll
     for (int i = 0; i < kRun; ++i) {
-        const int from = 2 * i + (F == GKV_STORE_INT4 ? l & 1 : 0);
-        float f0 = 1.f, f1 = 1.f;
-        if (Fm::kScales != 0) f0 = f1 = __shfl_sync(0xffffffffu, inv0, from, 16);
-        if (F == GKV_STORE_INT4) f1 = __shfl_sync(0xffffffffu, inv1, from, 16);
-        const uint32_t at = __shfl_sync(0xffffffffu, row, i, 16);
-        if (at < kNoPage) store_put_codes<F>(data + (size_t)at * Fm::kRow, l, store_codes<F>(v[i], f0, f1));
+        const uint32_t s = __shfl_sync(0xffffffffu, sc, 2 * i + (F == GKV_STORE_INT4 ? l & 1 : 0), 16);
+        if (at[i] < kNoPage) store_put_target<F>(x + (int64_t)i * p.token_stride, l, store_decode<F>(v[i], s));
     }
 }
 
 template <int OP>
-static cudaError_t launch_copy(const PagesCopyLaunch& p, cudaStream_t s) {
-    const int items = (p.n_tokens + kRun - 1) / kRun * p.h_kv;
-    const dim3 grid((unsigned)((items + kPageCopyItems - 1) / kPageCopyItems), (unsigned)p.batch, 2);
-    // runs that a CTA's items touch: h_kv items each, and the first may start inside one
-    const int runs = kPageCopyItems % p.h_kv == 0 ? kPageCopyItems / p.h_kv : (kPageCopyItems - 2) / p.h_kv + 2;
-    const size_t smem = OP >= kWriteNeighbours ? (size_t)runs * kRun * p.rotary.half * 2 * sizeof(float) : 0;
+static cudaError_t launch_append(PagesCopyLaunch p, cudaStream_t s) {
+    p.head_blocks = (p.h_kv + kRun - 1) / kRun;
+    p.heads_per_cta = (p.h_kv + p.head_blocks - 1) / p.head_blocks;
+    p.tokens_per_half = kRun / p.heads_per_cta;
+    const int tokens = kPageCopyItems * p.tokens_per_half;
+    const dim3 grid((unsigned)((p.n_tokens + tokens - 1) / tokens) * p.head_blocks * 2, (unsigned)p.batch);
+    const size_t smem = OP != kStraight ? (size_t)tokens * p.rotary.half * 2 * sizeof(float) : 0;
     switch (p.format) {
-        case GKV_STORE_BF16: gkv_pages_copy_kernel<GKV_STORE_BF16, OP><<<grid, kPageCopyThreads, smem, s>>>(p); break;
-        case GKV_STORE_E4M3: gkv_pages_copy_kernel<GKV_STORE_E4M3, OP><<<grid, kPageCopyThreads, smem, s>>>(p); break;
-        case GKV_STORE_INT8: gkv_pages_copy_kernel<GKV_STORE_INT8, OP><<<grid, kPageCopyThreads, smem, s>>>(p); break;
-        default:             gkv_pages_copy_kernel<GKV_STORE_INT4, OP><<<grid, kPageCopyThreads, smem, s>>>(p); break;
+        case GKV_STORE_BF16: gkv_pages_append_kernel<GKV_STORE_BF16, OP><<<grid, kPageCopyThreads, smem, s>>>(p); break;
+        case GKV_STORE_E4M3: gkv_pages_append_kernel<GKV_STORE_E4M3, OP><<<grid, kPageCopyThreads, smem, s>>>(p); break;
+        case GKV_STORE_INT8: gkv_pages_append_kernel<GKV_STORE_INT8, OP><<<grid, kPageCopyThreads, smem, s>>>(p); break;
+        default:             gkv_pages_append_kernel<GKV_STORE_INT4, OP><<<grid, kPageCopyThreads, smem, s>>>(p); break;
     }
     return cudaGetLastError();
 }
 cudaError_t launch_pages_append(const PagesCopyLaunch& p, cudaStream_t s) {
-    if (!p.rotary.turns) return launch_copy<kWrite>(p, s);
-    if (p.rotary.interleaved) return launch_copy<kWriteNeighbours>(p, s);
-    return p.rotary.half % 4 == 0 ? launch_copy<kWriteHalves>(p, s) : launch_copy<kWriteAny>(p, s);
+    if (!p.rotary.turns) return launch_append<kStraight>(p, s);
+    if (p.rotary.interleaved) return p.rotary.half % 4 == 0 ? launch_append<kNeighbours>(p, s) : launch_append<kAny>(p, s);
+    return p.rotary.half % 8 == 0 ? launch_append<kLanes>(p, s) : launch_append<kAny>(p, s);
 }
-cudaError_t launch_pages_read(const PagesCopyLaunch& p, cudaStream_t s) { return launch_copy<kRead>(p, s); }
+cudaError_t launch_pages_read(const PagesCopyLaunch& p, cudaStream_t s) {
+    const int items = (p.n_tokens + kRun - 1) / kRun * p.h_kv;
+    const dim3 grid((unsigned)((items + kPageCopyItems - 1) / kPageCopyItems), (unsigned)p.batch, 2);
+    switch (p.format) {
+        case GKV_STORE_BF16: gkv_pages_read_kernel<GKV_STORE_BF16><<<grid, kPageCopyThreads, 0, s>>>(p); break;
+        case GKV_STORE_E4M3: gkv_pages_read_kernel<GKV_STORE_E4M3><<<grid, kPageCopyThreads, 0, s>>>(p); break;
+        case GKV_STORE_INT8: gkv_pages_read_kernel<GKV_STORE_INT8><<<grid, kPageCopyThreads, 0, s>>>(p); break;
+        default:             gkv_pages_read_kernel<GKV_STORE_INT4><<<grid, kPageCopyThreads, 0, s>>>(p); break;
+    }
+    return cudaGetLastError();
+}
 
 }  // namespace gkv

@@ -35,8 +35,8 @@ def rotate(x, angle, interleaved, factor=1.0, transpose=False):
 
 def rotation_tolerance(y, mag, dtype):
     """What the kernels may be off. In units of u = 2^-24, relative to (|a| + |b|) factor: the angle (at most pi/4, relative u: below 1, and
-    the whole multiple of 2^-64 turns it stands for is the test's own), cos and sin (one step of a value below 1: below 1; CUDA's stated
-    bound for sincospif), the factor's product 1, the product's rounding 1: 4 in all; u |y| for the last one; then the type's."""
+    the whole multiple of 2^-64 turns it stands for is the test's own) and cos and sin of it (a series with one rounding of a value below
+    1 that matters: below 1), the factor's product 1, the product's rounding 1: 4 in all; u |y| for the last one; then the type's."""
     wide = 4 * U_F32 * mag + U_F32 * np.abs(y)
     fixed = np.where(mag > 0, wide * (1 + 2 * UNIT[dtype]), 0)
     return fixed + np.where(mag > 0, (0 if dtype == "fp32" else UNIT[dtype]) * np.abs(y) + LEAST[dtype], 0)
