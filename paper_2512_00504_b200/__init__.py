@@ -22,7 +22,7 @@ _ROOT = _PKG.parent
 _CHECKED = os.environ.get("GKV_LIB_VARIANT", "") == "check"
 LIB_PATH = _PKG / ("libgkv_check.so" if _CHECKED else "libgkv.so")
 _SOURCES = ["gkv_api.cu", "gkv_decode.cu", "gkv_evict.cu", "gkv_score.cu", "gkv_score_tc.cu", "gkv_redundancy.cu",
-            "gkv_static_scratch.cu", "gkv_store.cu", "gkv_store_attn.cu", "gkv_prefix.cu", "gkv_store_api.cu", "gkv_rotary.cu", "gkv_pages.cu", "gkv_pages_attn.cu",
+            "gkv_static_scratch.cu", "gkv_store.cu", "gkv_store_attn.cu", "gkv_prefix.cu", "gkv_store_api.cu", "gkv_rotary.cu", "gkv_pages.cu", "gkv_pages_attn.cu", "gkv_pages_stream.cu",
             "gkv_pages_api.cu"]
 
 GKV_OK, GKV_ERR_INVALID_ARG, GKV_ERR_STATE, GKV_ERR_CAPACITY, GKV_ERR_CUDA, GKV_ERR_TIMEOUT, GKV_ERR_UNSUPPORTED, \

@@ -215,6 +215,11 @@ struct PagesCopyLaunch {       // append / read
     int batch, h_kv, capacity, n_tokens, format;
     int head_blocks, heads_per_cta, tokens_per_half;   // how an append is cut (launch_pages_append)
 };
+// Partial result of a warp's part of a unit, two a warp: M[8], L[8], Mv[groups][8], O[8][32 lanes][4] as the lanes hold them. A warp takes
+// at least kStreamLeast tiles.
+constexpr int kStreamRecHead = 48, kStreamRecFloats = kStreamRecHead + kHeadDimHost * 8;
+constexpr int kStreamLeast = 4;
+constexpr int kStreamMaxCtas = 640;       // of four warps
 // (The names that it shares with StoreAttnLaunch are those of the code that both kinds of attention have in common. It is a
 // struct of its own because the host pays for the length of what a launch carries.)
 struct PagesAttnLaunch {
@@ -285,10 +290,11 @@ void store_plan(StoreAttnLaunch* p, int max_len, int sm_count);                 
 cudaError_t launch_rotary(RotaryLaunch& p, int type, int head_dim, int sm_count, cudaStream_t s);
 cudaError_t launch_pages_append(const PagesCopyLaunch& p, cudaStream_t s);
 cudaError_t launch_pages_read(const PagesCopyLaunch& p, cudaStream_t s);
-cudaError_t launch_pages_attn(const PagesAttnLaunch& p, int format, int mode, cudaStream_t s);
-enum { kPagesWhole = 0, kPagesCluster = 1, kPagesDealt = 2 };                              // mode: how a unit's pieces are joined
+cudaError_t launch_pages_attn(const PagesAttnLaunch& p, int format, cudaStream_t s);        // a cluster (or one CTA) a unit
+cudaError_t launch_pages_stream(const PagesAttnLaunch& p, int format, int ctas, cudaStream_t s);   // equal shares for all warps, then the merge
+int pages_attn_ctas_per_sm(int format);
+int pages_stream_ctas_per_sm(int format);
 int device_sm_count();                                                                      // of the current device
-uint64_t own_part_bytes(const gkv_store* s, bool merged);                                   // partial results of own rows, at any lengths
 bool rows_overlap(int64_t width, const int64_t (&n)[3], const int64_t (&s)[3]);             // of an array of rows
 gkv_status encode_map(CUtensorMap* map, void* base, uint64_t rows, uint32_t box_rows);      // [rows][128] bf16, 64-element boxes
 

@@ -17,4 +17,15 @@ __device__ __forceinline__ uint32_t page_row(const PagesView& g, int32_t entry, 
     return (uint32_t)entry * g.page_rows + head0 + (uint32_t)(row - page_of(g, row) * g.page_size) * g.token_rows;
 }
 
+__device__ __forceinline__ uint4 lds16(uint32_t a) {
+    uint4 r;
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "r"(a) : "memory");
+    return r;
+}
+__device__ __forceinline__ uint2 lds8(uint32_t a) {
+    uint2 r;
+    asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(r.x), "=r"(r.y) : "r"(a) : "memory");
+    return r;
+}
+
 }  // namespace gkv

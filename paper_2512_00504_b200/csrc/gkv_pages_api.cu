@@ -64,11 +64,26 @@ PagesView view(const gkv_pages* g, const gkv_page_table* t) {
     v.token_rows = g->token_major ? (uint32_t)g->n_kv_heads : 1u;
     return v;
 }
-// The workspace is that of a store with as many sequences.
-gkv_store as_store(const gkv_pages* g, int batch, int capacity) {
-    gkv_store s = {};
-    s.format = g->format; s.batch = batch; s.n_q_heads = g->n_q_heads; s.n_kv_heads = g->n_kv_heads; s.head_dim = kHeadDim; s.capacity = capacity;
-    return s;
+// Room for the partial results of the form that deals out equal shares.
+constexpr uint64_t kStreamBytes = (uint64_t)kStreamMaxCtas * 4 * 2 * kStreamRecFloats * sizeof(float);
+constexpr int kStreamMaxUnits = 16384, kStreamMaxBatch = 2048;      // its merge has a CTA a unit, which adds up all lengths
+constexpr int kStreamFrom = 6;
+
+// A cluster of up to kMaxCluster CTAs a unit, if that leaves a warp no more than kStreamFrom tiles (or there are more units than the merge of the
+// other form is made for); else equal shares for all warps. Returns the CTAs of the latter, 0 for the former.
+int pages_plan(PagesAttnLaunch* p, int format, int max_len, int sm_count) {
+    const int64_t units = (int64_t)p->batch * p->h_kv;
+    const int tiles = (max_len + (p->k_new ? 1 : 0) + 15) / 16;
+    int64_t splits = (int64_t)pages_attn_ctas_per_sm(format) * sm_count / units;
+    const int64_t most = (tiles + 7) / 8;                      // two turns of the four warps
+    if (splits > most) splits = most;
+    if (splits > kMaxCluster) splits = kMaxCluster;
+    if (splits < 1) splits = 1;
+    p->split_tiles = tiles > 0 ? (int)((tiles + splits - 1) / splits) : 1;
+    p->splits = tiles > 0 ? (tiles + p->split_tiles - 1) / p->split_tiles : 1;
+    if (p->split_tiles <= 4 * kStreamFrom || units > kStreamMaxUnits || p->batch > kStreamMaxBatch) return 0;
+    const int ctas = pages_stream_ctas_per_sm(format) * sm_count;
+    return ctas < kStreamMaxCtas ? ctas : kStreamMaxCtas;
 }
 
 gkv_status copy_args(const gkv_pages* g, const gkv_page_table* t, const void* k, const void* v, int64_t seq_stride, int64_t token_stride,
@@ -231,8 +246,7 @@ gkv_status gkv_pages_attn_workspace(const gkv_pages* pages, int32_t batch, uint6
     if (st != GKV_OK) return st;
     if (batch <= 0) return GKV_ERR_INVALID_ARG;
     if (batch > kMaxPagedBatch || (int64_t)batch * pages->n_q_heads >= (1ll << 30)) return GKV_ERR_UNSUPPORTED;
-    const gkv_store s = as_store(pages, batch, 1);
-    *bytes = own_part_bytes(&s, false);
+    *bytes = kStreamBytes;
     return GKV_OK;
 }
 
@@ -252,38 +266,22 @@ gkv_status gkv_pages_attn(const gkv_pages* pages, const gkv_page_table* table, c
         if (st != GKV_OK) return st;
         if (rotary->head_dim != kHeadDim) return GKV_ERR_INVALID_ARG;
     }
-    const gkv_store shape = as_store(pages, table->batch, capacity);
-    if (!workspace || misaligned(workspace, 16) || workspace_bytes < own_part_bytes(&shape, false)) return GKV_ERR_INVALID_ARG;
-
-    // the plan, and what a merge goes by, are those of a store
-    StoreAttnLaunch m = {};
-    m.len = len;
-    m.q = static_cast<const __nv_bfloat16*>(q);
-    m.k_new = static_cast<const __nv_bfloat16*>(k_new); m.v_new = static_cast<const __nv_bfloat16*>(v_new);
-    m.out = static_cast<__nv_bfloat16*>(out);
-    m.lse = lse;
-    m.own_part = static_cast<float*>(workspace);
-    m.format = pages->format; m.batch = table->batch; m.h_q = pages->n_q_heads; m.h_kv = pages->n_kv_heads;
-    m.g = pages->n_q_heads / pages->n_kv_heads; m.capacity = capacity;
-    store_plan(&m, max_len > 0 ? max_len : capacity, device_sm_count());
-    if (!m.dealt && m.splits > kMaxCluster) {      // one long sequence: its pieces meet in the workspace, too
-        m.dealt = 1;
-    }
+    if (!workspace || misaligned(workspace, 16) || workspace_bytes < kStreamBytes) return GKV_ERR_INVALID_ARG;
 
     PagesAttnLaunch p = {};
     p.pages = view(pages, table);
     p.rotary = view(rotary);
     p.pos = pos; p.len = len;
-    p.q = m.q; p.k_new = m.k_new; p.v_new = m.v_new;
+    p.q = static_cast<const __nv_bfloat16*>(q);
+    p.k_new = static_cast<const __nv_bfloat16*>(k_new); p.v_new = static_cast<const __nv_bfloat16*>(v_new);
     p.q_stride = q_stride; p.kv_stride = kv_stride;
-    p.out = m.out; p.lse = lse; p.own_part = m.own_part;
-    p.batch = m.batch; p.h_q = m.h_q; p.h_kv = m.h_kv; p.g = m.g; p.capacity = capacity;
-    p.splits = m.splits; p.split_tiles = m.split_tiles;
+    p.out = static_cast<__nv_bfloat16*>(out); p.lse = lse; p.own_part = static_cast<float*>(workspace);
+    p.batch = table->batch; p.h_q = pages->n_q_heads; p.h_kv = pages->n_kv_heads; p.g = p.h_q / p.h_kv; p.capacity = capacity;
     p.scale_log2 = (float)(1.4426950408889634 / sqrt((double)kHeadDim));
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
-    const int mode = m.dealt ? kPagesDealt : m.splits > 1 ? kPagesCluster : kPagesWhole;
-    if (launch_pages_attn(p, m.format, mode, s) != cudaSuccess) { (void)cudaGetLastError(); return GKV_ERR_CUDA; }
-    if (m.dealt && launch_store_merge(m, s) != cudaSuccess) { (void)cudaGetLastError(); return GKV_ERR_CUDA; }
+    const int stream_ctas = pages_plan(&p, pages->format, max_len > 0 ? max_len : capacity, device_sm_count());
+    const cudaError_t e = stream_ctas ? launch_pages_stream(p, pages->format, stream_ctas, s) : launch_pages_attn(p, pages->format, s);
+    if (e != cudaSuccess) { (void)cudaGetLastError(); return GKV_ERR_CUDA; }
     return GKV_OK;
 }
 

@@ -1,5 +1,5 @@
 // Decode attention over a cache in pages: one query token per sequence, rows found through the sequence's table, q and the new key
-// rotated on the way.
+// rotated on the way. This form is for short calls: a CTA, or a cluster of up to eight, per unit, all in one launch.
 //
 // The mathematics and the layout of the products are those of the attention over a store (gkv_store_rows.cuh): a unit is (sequence, KV
 // head), a tile 16 keys, the tiles of a piece go round the CTA's four warps, and a warp works on its own. What differs is how rows come.
@@ -34,16 +34,6 @@ struct PageRing {
 
 __device__ __forceinline__ void cp_async_8(uint32_t dst, const void* src) {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst), "l"(src) : "memory");
-}
-__device__ __forceinline__ uint4 lds16(uint32_t a) {
-    uint4 r;
-    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "r"(a) : "memory");
-    return r;
-}
-__device__ __forceinline__ uint2 lds8(uint32_t a) {
-    uint2 r;
-    asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(r.x), "=r"(r.y) : "r"(a) : "memory");
-    return r;
 }
 __device__ __forceinline__ void sts16(uint32_t a, uint4 v) {
     asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(a), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
@@ -169,7 +159,7 @@ __device__ __forceinline__ void patch_v(TileV<F>& t, const NewRow<F>& n, int at,
     }
 }
 
-// Grid as in the attention over a store: units x splits, split fastest; dealt out: a head's places, head slowest.
+// Grid: units x splits, split fastest.
 template <int F, int MODE>
 __global__ void __launch_bounds__(kThreads, pages_ctas(F)) gkv_pages_attn_kernel(const PagesAttnLaunch p) {
     using Ring = PageRing<F>;
@@ -179,12 +169,8 @@ __global__ void __launch_bounds__(kThreads, pages_ctas(F)) gkv_pages_attn_kernel
     __shared__ NewRow<F> s_new;
     extern __shared__ __align__(128) uint8_t s_ring[];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    int unit = blockIdx.x / p.splits, split = blockIdx.x - unit * p.splits, splits = p.splits, split_tiles = p.split_tiles;
-    int seq = unit / p.h_kv, head = unit - seq * p.h_kv;
-    if (MODE == kDealt) {
-        grid_launch_dependents();
-        if (!dealt_place(p, lane, &seq, &head, &split, &splits, &split_tiles)) return;   // a place that nobody needs
-    }
+    const int unit = blockIdx.x / p.splits, split = blockIdx.x - unit * p.splits, splits = p.splits, split_tiles = p.split_tiles;
+    const int seq = unit / p.h_kv, head = unit - seq * p.h_kv;
     const int len = p.len[seq];
     if (len < 0) return;
     const bool append = p.k_new != nullptr;
@@ -348,17 +334,15 @@ static cudaError_t launch_mode(const PagesAttnLaunch& p, int cluster, cudaStream
     return cudaLaunchKernelEx(&cfg, kernel, p);
 }
 template <int F>
-static cudaError_t launch_format(const PagesAttnLaunch& p, int mode, cudaStream_t s) {
-    if (mode == kPagesDealt) return launch_mode<F, kDealt>(p, 1, s);
-    if (mode == kPagesCluster) return launch_mode<F, kCluster>(p, p.splits, s);
-    return launch_mode<F, kWhole>(p, 1, s);
+static cudaError_t launch_format(const PagesAttnLaunch& p, cudaStream_t s) {
+    return p.splits > 1 ? launch_mode<F, kCluster>(p, p.splits, s) : launch_mode<F, kWhole>(p, 1, s);
 }
-cudaError_t launch_pages_attn(const PagesAttnLaunch& p, int format, int mode, cudaStream_t s) {
+cudaError_t launch_pages_attn(const PagesAttnLaunch& p, int format, cudaStream_t s) {
     switch (format) {
-        case GKV_STORE_BF16: return launch_format<GKV_STORE_BF16>(p, mode, s);
-        case GKV_STORE_E4M3: return launch_format<GKV_STORE_E4M3>(p, mode, s);
-        case GKV_STORE_INT8: return launch_format<GKV_STORE_INT8>(p, mode, s);
-        default:             return launch_format<GKV_STORE_INT4>(p, mode, s);
+        case GKV_STORE_BF16: return launch_format<GKV_STORE_BF16>(p, s);
+        case GKV_STORE_E4M3: return launch_format<GKV_STORE_E4M3>(p, s);
+        case GKV_STORE_INT8: return launch_format<GKV_STORE_INT8>(p, s);
+        default:             return launch_format<GKV_STORE_INT4>(p, s);
     }
 }
 

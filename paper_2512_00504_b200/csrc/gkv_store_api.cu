@@ -55,6 +55,13 @@ int64_t prefix_items(const StoreAttnLaunch& p, int chunk) {
     return items * p.h_kv * p.n_blocks;
 }
 
+// Upper bounds over all lengths, without a device. Partial results of own rows: of every unit when they are merged with
+// something else, and of the pieces of cut units.
+uint64_t own_part_bytes(const gkv_store* s, bool merged) {
+    const uint64_t units = (uint64_t)s->batch * s->n_kv_heads;
+    const uint64_t pieces = units * kMaxPieces < (uint64_t)kSplitUnits ? units * kMaxPieces : (uint64_t)kSplitUnits;
+    return align_up((pieces > units || !merged ? pieces : units) * kOwnRecFloats * 4);
+}
 uint64_t prefix_part_bytes(const gkv_store* s, int n_prefix, int rows) {
     if (n_prefix == 0 || rows == 0) return 0;
     int per_block, blocks, two;
@@ -142,13 +149,6 @@ gkv_status copy_args(const gkv_store* store, const void* k, const void* v, int64
 
 namespace gkv {
 
-// Upper bounds over all lengths, without a device. Partial results of own rows: of every unit when they are merged with
-// something else, and of the pieces of cut units.
-uint64_t own_part_bytes(const gkv_store* s, bool merged) {
-    const uint64_t units = (uint64_t)s->batch * s->n_kv_heads;
-    const uint64_t pieces = units * kMaxPieces < (uint64_t)kSplitUnits ? units * kMaxPieces : (uint64_t)kSplitUnits;
-    return align_up((pieces > units || !merged ? pieces : units) * kOwnRecFloats * 4);
-}
 // Whether elements of an array of rows of `width` share an address (or may, with strides that no slice of an array has).
 bool rows_overlap(int64_t width, const int64_t (&sizes)[3], const int64_t (&s)[3]) {
     int64_t n[3] = {sizes[0], sizes[1], sizes[2]};

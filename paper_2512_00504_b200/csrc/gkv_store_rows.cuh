@@ -303,19 +303,15 @@ __device__ __forceinline__ void load_query(const __nv_bfloat16* row, int ks, int
 }
 __device__ __forceinline__ uint32_t bf16x2_to_f16x2(uint32_t x, float f) { return pack_f16x2(bf16_lo(x) * f, bf16_hi(x) * f); }
 
-// The heads of a unit as the B operand of the first product, lane (head lane / 4, j = lane & 3), from the head's row; with 8- and 4-bit
-// rows as fp16 relative to a power of two, which goes into the factors f0, f1 of heads 2j, 2j + 1.
+// Heads as the B operand of the first product, lane (head lane / 4, j = lane & 3), as they were loaded: with 8- and 4-bit rows they
+// become fp16 relative to a power of two, which goes into the factors f0, f1 of heads 2j, 2j + 1.
 template <int F>
-__device__ __forceinline__ void load_queries(const __nv_bfloat16* row, int lane, uint32_t (&qf)[8][2], float& f0, float& f1) {
-    constexpr bool kScaled = F != GKV_STORE_BF16;
-    const int j = lane & 3;
-    uint32_t a = 0;
+__device__ __forceinline__ void scale_queries(int lane, uint32_t (&qf)[8][2], float& f0, float& f1) {
+    if constexpr (F != GKV_STORE_BF16) {
+        const int j = lane & 3;
+        uint32_t a = 0;
 #pragma unroll
-    for (int ks = 0; ks < 8; ++ks) {
-        load_query<F>(row, ks, j, qf[ks][0], qf[ks][1]);
-        if (kScaled) a = max(a, bf16_absmax(qf[ks][0], qf[ks][1]));
-    }
-    if (kScaled) {
+        for (int ks = 0; ks < 8; ++ks) a = max(a, bf16_absmax(qf[ks][0], qf[ks][1]));
         a = max(a, __shfl_xor_sync(0xffffffffu, a, 1));
         a = max(a, __shfl_xor_sync(0xffffffffu, a, 2));
         const int e = min(max((int)(a >> 7) - 127, -126), 126);        // exponent of the row's largest element
@@ -328,6 +324,13 @@ __device__ __forceinline__ void load_queries(const __nv_bfloat16* row, int lane,
         f0 *= __shfl_sync(0xffffffffu, up, 8 * j);
         f1 *= __shfl_sync(0xffffffffu, up, 8 * j + 4);
     }
+}
+// The same from the rows of a unit's heads (this lane's).
+template <int F>
+__device__ __forceinline__ void load_queries(const __nv_bfloat16* row, int lane, uint32_t (&qf)[8][2], float& f0, float& f1) {
+#pragma unroll
+    for (int ks = 0; ks < 8; ++ks) load_query<F>(row, ks, lane & 3, qf[ks][0], qf[ks][1]);
+    scale_queries<F>(lane, qf, f0, f1);
 }
 
 __device__ __forceinline__ float finite_ref(float m) { return m == -INFINITY ? 0.f : m; }
