@@ -491,7 +491,7 @@ typedef struct {
     int32_t n_pages, page_size;            /* page_size 1..65536                                      */
     int32_t token_major;
     void *k, *v;                           /* 16-byte aligned                                         */
-    void *k_scale, *v_scale;               /* 8-byte aligned; NULL for GKV_STORE_BF16                 */
+    void *k_scale, *v_scale;               /* 16-byte aligned; NULL for GKV_STORE_BF16                */
 } gkv_pages;
 typedef struct {
     const int32_t* page;                   /* device                                                  */

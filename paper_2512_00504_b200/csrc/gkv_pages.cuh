@@ -27,5 +27,10 @@ __device__ __forceinline__ uint2 lds8(uint32_t a) {
     asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(r.x), "=r"(r.y) : "r"(a) : "memory");
     return r;
 }
+__device__ __forceinline__ uint32_t lds2(uint32_t a) {
+    uint16_t r;
+    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(r) : "r"(a) : "memory");
+    return r;
+}
 
 }  // namespace gkv

@@ -44,7 +44,7 @@ gkv_status check_pages(const gkv_pages* g, const gkv_page_table* t) {
     const gkv_status st = check_shape(g);
     if (st != GKV_OK) return st;
     if (!g->k || !g->v || misaligned(g->k, 16) || misaligned(g->v, 16)) return GKV_ERR_INVALID_ARG;
-    if (g->format != GKV_STORE_BF16 && (!g->k_scale || !g->v_scale || misaligned(g->k_scale, 8) || misaligned(g->v_scale, 8)))
+    if (g->format != GKV_STORE_BF16 && (!g->k_scale || !g->v_scale || misaligned(g->k_scale, 16) || misaligned(g->v_scale, 16)))
         return GKV_ERR_INVALID_ARG;
     if (!t || !t->page || misaligned(t->page, 4) || t->batch <= 0 || t->width <= 0 || t->stride < 0) return GKV_ERR_INVALID_ARG;
     if (t->batch > kMaxPagedBatch || (int64_t)t->batch * g->n_q_heads >= (1ll << 30)) return GKV_ERR_UNSUPPORTED;
@@ -68,6 +68,7 @@ PagesView view(const gkv_pages* g, const gkv_page_table* t) {
 constexpr uint64_t kStreamBytes = (uint64_t)kStreamMaxCtas * 4 * 2 * kStreamRecFloats * sizeof(float);
 constexpr int kStreamMaxUnits = 16384, kStreamMaxBatch = 2048;      // its merge has a CTA a unit, which adds up all lengths
 constexpr int kStreamFrom = 6;
+constexpr int kStreamRounds = 1;
 
 // A cluster of up to kMaxCluster CTAs a unit, if that leaves a warp no more than kStreamFrom tiles (or there are more units than the merge of the
 // other form is made for); else equal shares for all warps. Returns the CTAs of the latter, 0 for the former.
@@ -82,7 +83,7 @@ int pages_plan(PagesAttnLaunch* p, int format, int max_len, int sm_count) {
     p->split_tiles = tiles > 0 ? (int)((tiles + splits - 1) / splits) : 1;
     p->splits = tiles > 0 ? (tiles + p->split_tiles - 1) / p->split_tiles : 1;
     if (p->split_tiles <= 4 * kStreamFrom || units > kStreamMaxUnits || p->batch > kStreamMaxBatch) return 0;
-    const int ctas = pages_stream_ctas_per_sm(format) * sm_count;
+    const int ctas = pages_stream_ctas_per_sm() * sm_count * kStreamRounds;
     return ctas < kStreamMaxCtas ? ctas : kStreamMaxCtas;
 }
 

@@ -7,8 +7,8 @@
 // warp has to itself is finished by it; of the others (a warp's first or last one) it leaves a partial result, and the merge joins them.
 //
 // Rows come by bulk copies into a ring of the warp's own, issued by its lanes and completed on a barrier of the warp's own: with pages whose
-// size is a multiple of the tile and that hold a head's rows together, one copy for a tile of K and four for V; with any others, one for
-// each row. (By cp.async, 16 bytes a lane, a tile costs the warp 100 more instructions: 128 sequences x 8 heads of about 2200 keys in bf16
+// size is a multiple of the tile and that hold a head's rows together, one copy for a tile of K and four for V (and two for their scales); with
+// any others, one for each row. (By cp.async, 16 bytes a lane, a tile costs the warp 100 more instructions: 128 sequences x 8 heads of about 2200 keys in bf16
 // 225 us, 2 x 8 of up to 131071 in 4 bits 108.) V is taken in four groups of four rows, 32 bytes further apart than the rows, and row r of
 // the first product (lanes' group q = r % 8) is key 4 (q / 2) + q % 2 + 2 (r / 8): lane j then finds its four keys of V in its own group, at
 // banks of its own.
@@ -21,45 +21,59 @@
 
 namespace gkv {
 
-__host__ __device__ constexpr int stream_ctas(int format) { return format == GKV_STORE_E4M3 || format == GKV_STORE_INT8 ? 4 : 3; }
-int pages_stream_ctas_per_sm(int format) { return stream_ctas(format); }
+constexpr int kStreamCtas = 3;                             // of an SM: 12 warps, 168 registers a thread
+int pages_stream_ctas_per_sm() { return kStreamCtas; }
+
+// 16-key tiles of a step: what is done once a step (waiting, finding rows, issuing copies) then counts for two of them. bf16 rows are so
+// long that one is enough, and two would leave a ring without stages.
+__host__ __device__ constexpr int stream_tiles(int format) { return format == GKV_STORE_BF16 ? 1 : 2; }
 
 template <int F>
 struct __align__(16) StreamWarp {
-    static constexpr int kRow = StoreFormat<F>::kRow;
-    static constexpr int kStages = F == GKV_STORE_BF16 ? 2 : F == GKV_STORE_INT4 ? 6 : 3;
+    static constexpr int kRow = StoreFormat<F>::kRow, kScales = StoreFormat<F>::kScales;
+    static constexpr int kTiles = stream_tiles(F), kKeys = kTiles * kTile;
+    static constexpr int kStages = F == GKV_STORE_INT4 ? 3 : 2;
     static constexpr int kGroup = 4 * kRow + 32;           // bytes from one group of V rows to the next
-    static constexpr int kK = kTile * kRow, kStage = kK + 4 * kGroup;
-    uint8_t ring[kStages][kStage];
+    static constexpr int kK = kTile * kRow, kV = 4 * kGroup, kS = kTile * kScales * 2;      // a tile's K, V, and scales of either
+    static constexpr int kBytes = kK + kV + 2 * kS;
+    uint8_t ring[kStages][kTiles][kBytes];
     __nv_bfloat16 row[kHeadDim];                           // a head, or the new key, as it is turned
     uint8_t code[2][kRow];                                 // the new row as it stands in the cache
     __nv_bfloat16 scale[2][4];
     float v[value_groups(F)][8];
-    uint32_t rows[kStages][kTile];                         // numbers of the tiles' rows
+    uint32_t rows[kStages][kKeys];                         // numbers of the rows, where they do not lie together
     uint64_t full[kStages];
 };
 
-// A place in the line of tiles.
+// A place in the line of steps: every unit has as many as its rows take, KEYS each.
+template <int KEYS>
+__device__ __forceinline__ int stream_steps(const PagesAttnLaunch& p, int seq) {
+    if (seq >= p.batch) return 0;
+    const int len = p.len[seq], n = p.k_new ? 1 : 0;
+    return len < 0 || len > p.capacity - n ? 0 : (len + n + KEYS - 1) / KEYS;
+}
 struct StreamPlace {
-    int seq, head, tile, tiles, len;
+    int seq, head, tile, tiles, len;                       // tile of so many, KEYS keys each; rows of the sequence in the cache
 };
 // On to the next one: there is one, as long as nobody changes the lengths meanwhile; if somebody does, this ends all the same.
+template <int KEYS>
 __device__ __forceinline__ void stream_next(const PagesAttnLaunch& p, StreamPlace& c) {
     if (++c.tile < c.tiles) return;
     c.tile = 0;
     if (++c.head < p.h_kv) return;
     c.head = 0;
     while (c.seq < p.batch - 1) {
-        c.tiles = own_tiles_of(p, ++c.seq);
+        c.tiles = stream_steps<KEYS>(p, ++c.seq);
         if (c.tiles > 0) break;
     }
     c.len = p.len[c.seq];
 }
-// Tiles of all units, and of those of the sequences before `seq`.
+// Steps of all units, and of those of the sequences before `seq`.
+template <int KEYS>
 __device__ __forceinline__ int64_t stream_total(const PagesAttnLaunch& p, int seq, int lane, int64_t* before) {
     int64_t all = 0, part = 0;
     for (int b = lane; b < p.batch; b += 32) {
-        const int t = own_tiles_of(p, b);
+        const int t = stream_steps<KEYS>(p, b);
         all += t;
         if (b < seq) part += t;
     }
@@ -72,32 +86,32 @@ __device__ __forceinline__ int64_t stream_total(const PagesAttnLaunch& p, int se
     return all * p.h_kv;
 }
 __device__ __forceinline__ int64_t stream_share(int64_t all, int warps) {
-    const int64_t per = (all + warps - 1) / warps;
+    const int64_t per = all < 1ll << 30 ? (int64_t)(((uint32_t)all + (uint32_t)warps - 1) / (uint32_t)warps) : (all + warps - 1) / warps;
     return per < kStreamLeast ? kStreamLeast : per;
 }
 
 template <int F, bool TOGETHER>
-__global__ void __launch_bounds__(kThreads, stream_ctas(F)) gkv_pages_stream_kernel(const PagesAttnLaunch p) {
+__global__ void __launch_bounds__(kThreads, kStreamCtas) gkv_pages_stream_kernel(const PagesAttnLaunch p) {
     using Warp = StreamWarp<F>;
-    constexpr int NG = value_groups(F), S = Warp::kStages, kRow = Warp::kRow, kScales = StoreFormat<F>::kScales;
+    constexpr int NG = value_groups(F), S = Warp::kStages, TILES = Warp::kTiles, KEYS = Warp::kKeys, kRow = Warp::kRow, kScales = Warp::kScales;
     constexpr bool kScaled = F != GKV_STORE_BF16;
     extern __shared__ __align__(128) uint8_t s_raw[];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     Warp& sw = reinterpret_cast<Warp*>(s_raw)[warp];
     grid_launch_dependents();
 
-    // ---- this warp's tiles
+    // ---- this warp's steps
     const int w = blockIdx.x * kWarps + warp;
     int64_t none;
-    const int64_t all = stream_total(p, 0, lane, &none), per = stream_share(all, (int)gridDim.x * kWarps), begin = w * per;
+    const int64_t all = stream_total<KEYS>(p, 0, lane, &none), per = stream_share(all, (int)gridDim.x * kWarps), begin = w * per;
     if (begin >= all) return;
     const int steps = (int)(all - begin < per ? all - begin : per);
-    StreamPlace fetch;
+    StreamPlace ahead;
     {
-        int64_t left = begin;                              // tiles between sequence b's first and ours
+        int64_t left = begin;                              // steps between sequence b's first and ours
         bool found = false;
         for (int b = 0; b < p.batch; b += 32) {
-            const int t = own_tiles_of(p, b + lane);
+            const int t = stream_steps<KEYS>(p, b + lane);
             int64_t upto = (int64_t)t * p.h_kv;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
@@ -107,20 +121,20 @@ __global__ void __launch_bounds__(kThreads, stream_ctas(F)) gkv_pages_stream_ker
             const unsigned past = __ballot_sync(0xffffffffu, upto > left);
             if (past) {
                 const int at = __ffs(past) - 1;
-                fetch.seq = b + at;
-                fetch.tiles = __shfl_sync(0xffffffffu, t, at);
-                left -= __shfl_sync(0xffffffffu, upto, at) - (int64_t)fetch.tiles * p.h_kv;
+                ahead.seq = b + at;
+                ahead.tiles = __shfl_sync(0xffffffffu, t, at);
+                left -= __shfl_sync(0xffffffffu, upto, at) - (int64_t)ahead.tiles * p.h_kv;
                 found = true;
                 break;
             }
             left -= __shfl_sync(0xffffffffu, upto, 31);
         }
         if (!found) return;                                // (somebody has changed the lengths)
-        fetch.head = (int)(left / fetch.tiles);
-        fetch.tile = (int)(left - (int64_t)fetch.head * fetch.tiles);
-        fetch.len = p.len[fetch.seq];
+        ahead.head = (int)(left < 1ll << 31 ? (uint32_t)left / (uint32_t)ahead.tiles : left / ahead.tiles);
+        ahead.tile = (int)(left - (int64_t)ahead.head * ahead.tiles);
+        ahead.len = p.len[ahead.seq];
     }
-    StreamPlace at = fetch;
+    StreamPlace at = ahead;
     const int added = p.k_new ? 1 : 0;
 
     if (lane == 0) {
@@ -130,44 +144,58 @@ __global__ void __launch_bounds__(kThreads, stream_ctas(F)) gkv_pages_stream_ker
     }
     __syncwarp();
 
-    // ---- tiles on their way: the table's entries one tile ahead of the copies. Lane l & 15 has key l & 15.
-    const uint8_t *kb = p.pages.data[0], *vb = p.pages.data[1];
-    auto entry = [&]() {
-        const int key = fetch.tile * kTile + (TOGETHER ? 0 : lane & 15);
-        return key < fetch.len + added ? page_entry(p.pages, p.pages.table + fetch.seq * p.pages.table_stride, key) : 0;
+    // ---- rows on their way: the table's entries a step ahead of the copies. A lane looks up its key's, or (rows together) its tile's first one's.
+    const int mine = TOGETHER ? (lane >> 4) * kTile : lane;      // that key within the step
+    auto lookup = [&](int& slot) {
+        const int key = ahead.tile * KEYS + mine;
+        if (mine >= KEYS || key >= ahead.len + added) return 0;            // no such key
+        const int page = page_of(p.pages, key);
+        slot = key - page * p.pages.page_size;
+        return p.pages.table[ahead.seq * p.pages.table_stride + page];
     };
-    int issued = 0;
-    int32_t next = entry();
+    int issued = 0, next_slot = 0, next = lookup(next_slot);
+    uint32_t lost = 0;                                     // stages with a row on no page
     auto issue = [&](int stage) {
-        const int key0 = fetch.tile * kTile, key = key0 + (lane & 15), here = fetch.len - key0;      // rows in the cache from key0 on
-        const uint32_t first = TOGETHER ? page_row(p.pages, next, (uint32_t)fetch.head * p.pages.head_rows, key0) : 0u;
-        uint32_t row = kNoRow;
-        if (key < fetch.len + added) {
-            if (TOGETHER) row = first == kNoPage ? kNoPage : first + (lane & 15);
-            else row = page_row(p.pages, next, (uint32_t)fetch.head * p.pages.head_rows, key);
-        }
-        const bool fine = __all_sync(0xffffffffu, row != kNoPage);
-        if (lane < kTile) sw.rows[stage][lane] = row;
-        const uint32_t bar = smem_u32(&sw.full[stage]), k = smem_u32(sw.ring[stage]), v = k + Warp::kK;
-        const int n = fine ? min(max(here, 0), kTile) : 0;                                           // rows to be copied
-        if (lane == 0) mbar_arrive_expect_tx(bar, (uint32_t)(2 * n * kRow));
-        if (TOGETHER) {
-            const size_t src = (size_t)first * kRow;
-            if (lane < 4) {
-                const int rows = min(n - 4 * lane, 4);
-                if (rows > 0) bulk_load(v + lane * Warp::kGroup, vb + src + lane * 4 * kRow, (uint32_t)(rows * kRow), bar);
-            } else if (lane == 4 && n > 0) {
-                bulk_load(k, kb + src, (uint32_t)(n * kRow), bar);
+        const int key0 = ahead.tile * KEYS, here = ahead.len - key0;       // rows in the cache from key0 on
+        const bool page = (uint32_t)next < (uint32_t)p.pages.n_pages;
+        const uint32_t row = (uint32_t)next * p.pages.page_rows + (uint32_t)ahead.head * p.pages.head_rows + (uint32_t)next_slot * p.pages.token_rows;
+        const bool fine = __all_sync(0xffffffffu, page || mine >= KEYS || key0 + mine >= ahead.len + added);
+        lost = fine ? lost & ~(1u << stage) : lost | 1u << stage;
+        const uint32_t bar = smem_u32(&sw.full[stage]), to = smem_u32(sw.ring[stage]);
+        const int n = fine ? min(max(here, 0), KEYS) : 0;                  // rows to be copied
+        if constexpr (TOGETHER) {
+            const int tile = lane >> 4, l = lane & 15, rows = min(n - tile * kTile, kTile);      // (tile 1 of 1: none)
+            const int scaled = kScaled ? (n + kTile - 1) / kTile * 2 * Warp::kS : 0;
+            if (lane == 0) mbar_arrive_expect_tx(bar, (uint32_t)(2 * n * kRow + scaled));
+            if (rows > 0 && tile < TILES && l < (kScaled ? 7 : 5)) {
+                const uint32_t k = to + tile * Warp::kBytes;
+                if (l < 4) {
+                    const int part = min(rows - 4 * l, 4);
+                    if (part > 0) bulk_load(k + Warp::kK + l * Warp::kGroup, p.pages.data[1] + (size_t)(row + 4 * l) * kRow, (uint32_t)(part * kRow), bar);
+                } else if (l == 4) {
+                    bulk_load(k, p.pages.data[0] + (size_t)row * kRow, (uint32_t)(rows * kRow), bar);
+                } else if (kScaled) {                      // those of all of the tile's rows: 16 bytes are the least
+                    bulk_load(k + Warp::kK + Warp::kV + (l - 5) * Warp::kS, p.pages.scale[l - 5] + (size_t)row * kScales, Warp::kS, bar);
+                }
             }
-        } else if ((lane & 15) < n) {
-            const size_t src = (size_t)row * kRow;
-            const int r = lane & 15;
-            if (lane < 16) bulk_load(k + r * kRow, kb + src, kRow, bar);
-            else bulk_load(v + (r >> 2) * Warp::kGroup + (r & 3) * kRow, vb + src, kRow, bar);
+        } else {
+            if (lane < KEYS) sw.rows[stage][lane] = key0 + lane >= ahead.len + added ? kNoRow : page ? row : kNoPage;
+            if (lane == 0) mbar_arrive_expect_tx(bar, (uint32_t)(2 * n * kRow));
+            if (lane < n) {
+                const uint32_t k = to + (lane >> 4) * Warp::kBytes;
+                const int r = lane & 15;
+                bulk_load(k + r * kRow, p.pages.data[0] + (size_t)row * kRow, kRow, bar);
+                bulk_load(k + Warp::kK + (r >> 2) * Warp::kGroup + (r & 3) * kRow, p.pages.data[1] + (size_t)row * kRow, kRow, bar);
+            }
         }
         if (++issued < steps) {
-            stream_next(p, fetch);
-            next = entry();
+            stream_next<KEYS>(p, ahead);
+            next = lookup(next_slot);
+            if (ahead.tile == 0) {                         // a unit begins: what it will ask for comes closer
+                const __nv_bfloat16* x = p.q + ((int64_t)ahead.seq * p.q_stride + (int64_t)ahead.head * p.g * kHeadDim) + lane * 64;
+                if (lane >= 2 * p.g) x = (lane & 2 ? p.v_new : p.k_new) + ((int64_t)ahead.seq * p.kv_stride + (int64_t)ahead.head * kHeadDim) + (lane & 1) * 64;
+                if (lane < 2 * p.g || (added && lane < 2 * p.g + 4)) asm volatile("prefetch.global.L2 [%0];" ::"l"(x));
+            }
         }
     };
 #pragma unroll
@@ -178,14 +206,20 @@ __global__ void __launch_bounds__(kThreads, stream_ctas(F)) gkv_pages_stream_ker
     const int key_a = 4 * (q >> 1) + (q & 1);              // this lane's keys of a tile: key_a and two on
     TileK<F> tk;
     TileV<F> tv;
-    auto fetch_scales = [&](auto& t, const __nv_bfloat16* scale, int stage) {
+    auto take_scales = [&](auto& t, int which, int stage, int tile) {
         if constexpr (kScaled) {
 #pragma unroll
             for (int hf = 0; hf < 2; ++hf) {
-                const uint32_t r = sw.rows[stage][key_a + 2 * hf];
-                const __nv_bfloat16* s = scale + (size_t)r * kScales;
-                if constexpr (F == GKV_STORE_INT4) t.s[hf] = r < kNoPage ? ld8(s) : make_uint2(0u, 0u);
-                else t.s[hf] = r < kNoPage ? ld2(s) : 0u;
+                if constexpr (TOGETHER) {
+                    const uint32_t a = smem_u32(sw.ring[stage][tile]) + Warp::kK + Warp::kV + which * Warp::kS + (key_a + 2 * hf) * 2 * kScales;
+                    if constexpr (F == GKV_STORE_INT4) t.s[hf] = lds8(a);
+                    else t.s[hf] = lds2(a);
+                } else {
+                    const uint32_t r = sw.rows[stage][tile * kTile + key_a + 2 * hf];
+                    const __nv_bfloat16* s = p.pages.scale[which] + (size_t)r * kScales;
+                    if constexpr (F == GKV_STORE_INT4) t.s[hf] = r < kNoPage ? ld8(s) : make_uint2(0u, 0u);
+                    else t.s[hf] = r < kNoPage ? ld2(s) : 0u;
+                }
             }
         }
     };
@@ -208,41 +242,40 @@ __global__ void __launch_bounds__(kThreads, stream_ctas(F)) gkv_pages_stream_ker
     float f0 = 0.f, f1 = 0.f;
     RunningRows<F> r;
     bool begins = true, whole = false, ok = true;          // a unit begins; it is ours from its first tile on; no wait has run out
-    int stage = 0;
     bool first_unit = true;
+    int stage = 0;
     uint32_t parity = 0;
     __syncwarp();
-    fetch_scales(tk, p.pages.scale[0], 0);
-    fetch_scales(tv, p.pages.scale[1], 0);
+    if (!TOGETHER) {                                       // scales by ordinary loads: a tile ahead
+        take_scales(tk, 0, 0, 0);
+        take_scales(tv, 1, 0, 0);
+    }
     for (int step = 0; step < steps; ++step) {
         if (begins) {
             // ---- a unit's heads
             const __nv_bfloat16* x = p.q + ((int64_t)at.seq * p.q_stride + (int64_t)at.head * p.g * kHeadDim);
             if (rotates) {
-                const float2 cs0 = cos_sin(lane), cs1 = cos_sin(lane + 32);
-#pragma unroll 1
-                for (int h4 = 0; h4 < p.g; h4 += 4) {                  // four heads' loads at a time
-                    __nv_bfloat16 e[4][4];
+                __nv_bfloat16 e[kMaxGroup][4];
 #pragma unroll
-                    for (int h = 0; h < 4; ++h)
-                        if (h4 + h < p.g)
+                for (int h = 0; h < kMaxGroup; ++h)
+                    if (h < p.g)
 #pragma unroll
-                            for (int k = 0; k < 2; ++k) {
-                                e[h][2 * k] = x[(h4 + h) * kHeadDim + first_of(lane + 32 * k)];
-                                e[h][2 * k + 1] = x[(h4 + h) * kHeadDim + second_of(lane + 32 * k)];
-                            }
-#pragma unroll
-                    for (int h = 0; h < 4; ++h)
-                        if (h4 + h < p.g) {
-                            turn_into(lane, e[h][0], e[h][1], cs0);
-                            turn_into(lane + 32, e[h][2], e[h][3], cs1);
-                            __syncwarp();
-                            if (min(q, p.g - 1) == h4 + h)
-#pragma unroll
-                                for (int ks = 0; ks < 8; ++ks) load_query<F>(sw.row, ks, j, qf[ks][0], qf[ks][1]);
-                            __syncwarp();
+                        for (int k = 0; k < 2; ++k) {
+                            e[h][2 * k] = x[h * kHeadDim + first_of(lane + 32 * k)];
+                            e[h][2 * k + 1] = x[h * kHeadDim + second_of(lane + 32 * k)];
                         }
-                }
+                const float2 cs0 = cos_sin(lane), cs1 = cos_sin(lane + 32);
+#pragma unroll
+                for (int h = 0; h < kMaxGroup; ++h)
+                    if (h < p.g) {
+                        turn_into(lane, e[h][0], e[h][1], cs0);
+                        turn_into(lane + 32, e[h][2], e[h][3], cs1);
+                        __syncwarp();
+                        if (min(q, p.g - 1) == h)
+#pragma unroll
+                            for (int ks = 0; ks < 8; ++ks) load_query<F>(sw.row, ks, j, qf[ks][0], qf[ks][1]);
+                        __syncwarp();
+                    }
             } else {
 #pragma unroll
                 for (int ks = 0; ks < 8; ++ks) load_query<F>(x + min(q, p.g - 1) * kHeadDim, ks, j, qf[ks][0], qf[ks][1]);
@@ -253,23 +286,28 @@ __global__ void __launch_bounds__(kThreads, stream_ctas(F)) gkv_pages_stream_ker
             whole = at.tile == 0;
             begins = false;
         }
-        // ---- a tile
+        // ---- a step
         if (ok) ok = __all_sync(0xffffffffu, mbar_wait_bounded(smem_u32(&sw.full[stage]), parity));
-        const uint32_t k = smem_u32(sw.ring[stage]), v = k + Warp::kK;
-        const int left = at.len + added - at.tile * kTile;                       // keys from this tile's first on
-        const bool last = at.tile == at.tiles - 1;
-        const bool bad = !ok || __any_sync(0xffffffffu, sw.rows[stage][lane & 15] == kNoPage);
+        const int left = at.len + added - at.tile * KEYS;                        // keys from this step's first on
+        const bool last = at.tile == at.tiles - 1, bad = !ok || (lost >> stage & 1u);
         if (last) {
-            // What V has behind the end, whatever it is, becomes zeros.
-            for (int i = lane; i < (kTile - left) * (kRow / 16); i += 32) {
-                const int key = left + i / (kRow / 16);
-                *reinterpret_cast<uint4*>(sw.ring[stage] + Warp::kK + (key >> 2) * Warp::kGroup + (key & 3) * kRow + i % (kRow / 16) * 16) =
-                    make_uint4(0u, 0u, 0u, 0u);
+            // What V and its scales have behind the end, whatever it is, becomes zeros.
+            constexpr int kPer = kRow / 16;
+            for (int i = lane; i < (KEYS - left) * kPer; i += 32) {
+                const int key = left + i / kPer, k = key & (kTile - 1);
+                uint8_t* t = sw.ring[stage][key / kTile] + Warp::kK;
+                *reinterpret_cast<uint4*>(t + (k >> 2) * Warp::kGroup + (k & 3) * kRow + i % kPer * 16) = make_uint4(0u, 0u, 0u, 0u);
+                if (kScaled && TOGETHER && i % kPer == 0) {
+                    uint8_t* z = t + Warp::kV + Warp::kS + k * 2 * kScales;
+                    if (F == GKV_STORE_INT4) *reinterpret_cast<uint2*>(z) = make_uint2(0u, 0u);
+                    else *reinterpret_cast<uint16_t*>(z) = 0;
+                }
             }
             if (added) {
                 // The new row, its last key: turned, quantised, into its page and into the tile.
                 const int64_t new_row = (int64_t)at.seq * p.kv_stride + (int64_t)at.head * kHeadDim;
                 const __nv_bfloat16 *kn = p.k_new + new_row, *vn = p.v_new + new_row;
+                const int32_t e = page_entry(p.pages, p.pages.table + at.seq * p.pages.table_stride, at.len);
                 if (rotates) {
                     turn_into(lane, kn[first_of(lane)], kn[second_of(lane)], cos_sin(lane));
                     turn_into(lane + 32, kn[first_of(lane + 32)], kn[second_of(lane + 32)], cos_sin(lane + 32));
@@ -277,64 +315,80 @@ __global__ void __launch_bounds__(kThreads, stream_ctas(F)) gkv_pages_stream_ker
                     kn = sw.row;
                 }
                 const uint4 x = store_load_source<F>(lane < 16 ? kn : vn, lane & 15);
-                const int key = left - 1;
-                const uint32_t to = sw.rows[stage][key];
+                const uint32_t to = page_row(p.pages, e, (uint32_t)at.head * p.pages.head_rows, at.len);
                 store_put_row<F>(sw.code[lane >> 4], sw.scale[lane >> 4], lane & 15, x);
                 if (to < kNoPage)
                     store_put_row<F>(p.pages.data[lane >> 4] + (size_t)to * kRow, p.pages.scale[lane >> 4] + (size_t)to * kScales, lane & 15, x);
                 __syncwarp();
-                uint8_t* dst = lane < 16 ? sw.ring[stage] + key * kRow : sw.ring[stage] + Warp::kK + (key >> 2) * Warp::kGroup + (key & 3) * kRow;
-                if ((lane & 15) < kRow / 16)
-                    reinterpret_cast<uint4*>(dst)[lane & 15] = reinterpret_cast<const uint4*>(sw.code[lane >> 4])[lane & 15];
-                if constexpr (kScaled) {
-#pragma unroll
-                    for (int hf = 0; hf < 2; ++hf)
-                        if (key_a + 2 * hf == key) {
-                            if constexpr (F == GKV_STORE_INT4) {
-                                tk.s[hf] = *reinterpret_cast<const uint2*>(sw.scale[0]);
-                                tv.s[hf] = *reinterpret_cast<const uint2*>(sw.scale[1]);
-                            } else {
-                                tk.s[hf] = *reinterpret_cast<const uint16_t*>(sw.scale[0]);
-                                tv.s[hf] = *reinterpret_cast<const uint16_t*>(sw.scale[1]);
-                            }
-                        }
-                }
+                const int key = left - 1, k = key & (kTile - 1);
+                uint8_t* t = sw.ring[stage][key / kTile];
+                uint8_t* dst = lane < 16 ? t + k * kRow : t + Warp::kK + (k >> 2) * Warp::kGroup + (k & 3) * kRow;
+                if ((lane & 15) < kPer) reinterpret_cast<uint4*>(dst)[lane & 15] = reinterpret_cast<const uint4*>(sw.code[lane >> 4])[lane & 15];
+                if (kScaled && TOGETHER && lane < 2 * kScales)         // (the others take them below)
+                    reinterpret_cast<__nv_bfloat16*>(t + Warp::kK + Warp::kV + lane / max(kScales, 1) * Warp::kS)[k * kScales + lane % max(kScales, 1)] =
+                        sw.scale[lane / max(kScales, 1)][lane % max(kScales, 1)];
             }
             fence_proxy_async_smem();                      // before the ring's next copies
             __syncwarp();
         }
+#pragma unroll 1
+        for (int tile = 0; tile < TILES; ++tile) {
+            const int keys = left - tile * kTile;          // of this tile and on
+            if (keys <= 0) break;
+            const uint32_t k = smem_u32(sw.ring[stage][tile]), v = k + Warp::kK;
+            if (TOGETHER) {
+                take_scales(tk, 0, stage, tile);
+                take_scales(tv, 1, stage, tile);
+            } else if (kScaled && last && added) {         // the new row's
 #pragma unroll
-        for (int hf = 0; hf < 2; ++hf)
-#pragma unroll
-            for (int c = 0; c < (F == GKV_STORE_BF16 ? 4 : F == GKV_STORE_INT4 ? 1 : 2); ++c)
-                tk.d[hf][c] = lds16(k + (key_a + 2 * hf) * kRow + j * 16 + c * 64);
-        float z[4];
-        tile_logits<F>(tk, qf, f0, f1, z);
-        if (left < kTile) {
+                for (int hf = 0; hf < 2; ++hf)
+                    if (key_a + 2 * hf == keys - 1) {
+                        if constexpr (F == GKV_STORE_INT4) {
+                            tk.s[hf] = *reinterpret_cast<const uint2*>(sw.scale[0]);
+                            tv.s[hf] = *reinterpret_cast<const uint2*>(sw.scale[1]);
+                        } else if constexpr (kScaled) {
+                            tk.s[hf] = *reinterpret_cast<const uint16_t*>(sw.scale[0]);
+                            tv.s[hf] = *reinterpret_cast<const uint16_t*>(sw.scale[1]);
+                        }
+                    }
+            }
 #pragma unroll
             for (int hf = 0; hf < 2; ++hf)
-                if (key_a + 2 * hf >= left) z[2 * hf] = z[2 * hf + 1] = -INFINITY;
-        }
-        if (bad) z[0] = z[1] = z[2] = z[3] = NAN;
-        uint32_t b[NG][2];
-        r.weigh_tile(z, tv, sw.v, lane, b);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint32_t a = v + j * Warp::kGroup + i * kRow + q * (F == GKV_STORE_INT4 ? 8 : 16);
-            if constexpr (F == GKV_STORE_INT4) tv.d[i] = lds8(a);
-            else if constexpr (F == GKV_STORE_BF16) {
-                tv.d[i][0] = lds16(a);
-                tv.d[i][1] = lds16(a + 128);
-            } else tv.d[i] = lds16(a);
+                for (int c = 0; c < (F == GKV_STORE_BF16 ? 4 : F == GKV_STORE_INT4 ? 1 : 2); ++c)
+                    tk.d[hf][c] = lds16(k + (key_a + 2 * hf) * kRow + j * 16 + c * 64);
+            float z[4];
+            tile_logits<F>(tk, qf, f0, f1, z);
+            if (keys < kTile) {
+#pragma unroll
+                for (int hf = 0; hf < 2; ++hf)
+                    if (key_a + 2 * hf >= keys) z[2 * hf] = z[2 * hf + 1] = -INFINITY;
+            }
+            if (bad) z[0] = z[1] = z[2] = z[3] = NAN;
+            uint32_t b[NG][2];
+            r.weigh_tile(z, tv, sw.v, lane, b);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t a = v + j * Warp::kGroup + i * kRow + q * (F == GKV_STORE_INT4 ? 8 : 16);
+                if constexpr (F == GKV_STORE_INT4) tv.d[i] = lds8(a);
+                else if constexpr (F == GKV_STORE_BF16) {
+                    tv.d[i][0] = lds16(a);
+                    tv.d[i][1] = lds16(a + 128);
+                } else tv.d[i] = lds16(a);
+            }
+            tile_values<F, NG>(tv, b, r.acc);
+            if (!TOGETHER && tile + 1 < TILES && keys > kTile) {
+                take_scales(tk, 0, stage, tile + 1);
+                take_scales(tv, 1, stage, tile + 1);
+            }
         }
-        tile_values<F, NG>(tv, b, r.acc);
         __syncwarp();                                      // the slot has been read
         if (issued < steps && ok) issue(stage);
         if (++stage == S) { stage = 0; parity ^= 1; }
-        if (step + 1 < steps) {
-            __syncwarp();                                  // (S = 1 aside, the next tile's rows have been there for long)
-            fetch_scales(tk, p.pages.scale[0], stage);
-            fetch_scales(tv, p.pages.scale[1], stage);
+        if (!TOGETHER && step + 1 < steps) {
+            __syncwarp();
+            take_scales(tk, 0, stage, 0);
+            take_scales(tv, 1, stage, 0);
         }
         // ---- the end of the unit, or of this warp's part of it
         if (last || step + 1 == steps) {
@@ -381,34 +435,35 @@ __global__ void __launch_bounds__(kThreads, stream_ctas(F)) gkv_pages_stream_ker
             first_unit = false;
             __syncwarp();
         }
-        if (step + 1 < steps) stream_next(p, at);
+        if (step + 1 < steps) stream_next<KEYS>(p, at);
     }
     if (!ok)                                               // what is still on its way gets a bounded time to arrive
         for (int s = 0; s < S; ++s) mbar_wait_bounded(smem_u32(&sw.full[s]), s < stage ? parity ^ 1 : parity);
 }
 
-// Joins the partial results of a unit. `apart`: 8 CTAs a unit, each with two dimensions of every lane's, their threads 32 lanes x 8 shares of
-// the records; else one CTA a unit, whose warps have two dimensions each.
-template <int F>
-__global__ void __launch_bounds__(256) gkv_pages_stream_merge_kernel(const PagesAttnLaunch p, const int warps, const int apart) {
-    constexpr int NG = value_groups(F);
-    __shared__ float s_max[8][1 + NG][8], s_sum[8][8], s_fin[2 + NG][8];
-    __shared__ float4 s_o[8][32];
-    const int unit = apart ? blockIdx.x >> 3 : blockIdx.x, seq = unit / p.h_kv, head = unit - seq * p.h_kv;
+// Joins the partial results of a unit: a running softmax over them, kJoin at a time, all of whose loads are under way before the first is
+// looked at. APART (few units, with many parts): 8 CTAs a unit, each with two dimensions of every lane's, its warps with a share of the parts
+// each; else one CTA a unit, whose warps have two dimensions each.
+template <int F, bool APART>
+__global__ void __launch_bounds__(256, APART ? 2 : 6) gkv_pages_stream_merge_kernel(const PagesAttnLaunch p, const int warps) {
+    constexpr int NG = value_groups(F), KEYS = StreamWarp<F>::kKeys, kJoin = APART ? 8 : 2;
+    __shared__ float4 s_o[8][32], s_mv[8][32];
+    __shared__ float2 s_l[8][32];
+    const int unit = APART ? blockIdx.x >> 3 : blockIdx.x, seq = unit / p.h_kv, head = unit - seq * p.h_kv;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     int64_t before;
-    const int64_t all = stream_total(p, seq, lane, &before), per = stream_share(all, warps);
-    const int len = p.len[seq], tiles = own_tiles_of(p, seq);
+    const int64_t all = stream_total<KEYS>(p, seq, lane, &before), per = stream_share(all, warps);
+    const int len = p.len[seq], tiles = stream_steps<KEYS>(p, seq);
     const int64_t first = before + (int64_t)head * tiles;
     const int w0 = (int)(first / per), n = tiles ? (int)((first + tiles - 1) / per) - w0 + 1 : 0;
     const size_t out = ((size_t)seq * p.h_q + (size_t)head * p.g) * kHeadDim;
-    const int slice = apart ? blockIdx.x & 7 : warp;       // the two dimensions
+    const int slice = APART ? blockIdx.x & 7 : warp;       // the two dimensions
     const int q = lane >> 2, h0 = 2 * (lane & 3), d = out_dim<F>(slice, q), dg = slice / (8 / NG);
     grid_wait_previous();                                  // (nobody leaves before: what comes next waits for this kernel alone)
     if (len < 0 || n == 1) return;                         // left out, or finished by the warp that had it
     if (n == 0) {
         const bool fits = p.k_new ? len < p.capacity : len <= p.capacity;
-        if (apart && warp != 0) return;
+        if (APART && warp != 0) return;
         const uint32_t x = fits ? 0u : 0x7fff7fffu;        // bf16 NaN
 #pragma unroll
         for (int h = 0; h < 2; ++h)
@@ -418,77 +473,73 @@ __global__ void __launch_bounds__(256) gkv_pages_stream_merge_kernel(const Pages
     }
     // Part i is warp w0 + i's: the first of its two, but where the unit begins inside a warp's share its last one.
     const bool inside = first != w0 * per;
-    auto record = [&](int i) { return p.own_part + (size_t)(2 * (w0 + i) + (i == 0 && inside ? 1 : 0)) * kStreamRecFloats; };
-    // ---- maxima and the sum of weights: thread t has head t & 7 of every 32nd record
-    const int h = threadIdx.x & 7;
-    float m = -INFINITY, v[NG], l = 0.f;
-#pragma unroll
-    for (int g = 0; g < NG; ++g) v[g] = -INFINITY;
-    for (int i = threadIdx.x >> 3; i < n; i += 32) {
-        const float* a = record(i) + h;
-        m = fmaxf(m, a[0]);
-#pragma unroll
-        for (int g = 0; g < NG; ++g) v[g] = fmaxf(v[g], a[16 + 8 * g]);
-    }
-#pragma unroll
-    for (int o = 8; o < 32; o <<= 1) {
-        m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-#pragma unroll
-        for (int g = 0; g < NG; ++g) v[g] = fmaxf(v[g], __shfl_xor_sync(0xffffffffu, v[g], o));
-    }
-    if (lane < 8) {
-        s_max[warp][0][h] = m;
-#pragma unroll
-        for (int g = 0; g < NG; ++g) s_max[warp][1 + g][h] = v[g];
-    }
-    __syncthreads();
-    if (threadIdx.x < 8 * (1 + NG)) {
-        float a = -INFINITY;
-        for (int i = 0; i < 8; ++i) a = fmaxf(a, s_max[i][threadIdx.x >> 3][h]);
-        s_fin[threadIdx.x < 8 ? 0 : 1 + (threadIdx.x >> 3)][h] = a;
-    }
-    __syncthreads();
-    const float mr = finite_ref(s_fin[0][h]);
-    for (int i = threadIdx.x >> 3; i < n; i += 32) {
-        const float* a = record(i) + h;
-        l += a[8] * fast_exp2(a[0] - mr);                  // (a NaN sum may come with a maximum of -infinity)
-    }
-#pragma unroll
-    for (int o = 8; o < 32; o <<= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
-    if (lane < 8) s_sum[warp][h] = l;
-    __syncthreads();
-    if (threadIdx.x < 8) {
-        float a = 0.f;
-        for (int i = 0; i < 8; ++i) a += s_sum[i][h];
-        s_fin[1][h] = a;
-    }
-    // ---- values
-    const float v0 = finite_ref(s_fin[2 + dg][h0]), v1 = finite_ref(s_fin[2 + dg][h0 + 1]);
-    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-    for (int i = apart ? warp : 0; i < n; i += apart ? 8 : 1) {
-        const float* a = record(i);
-        const float4 x = reinterpret_cast<const float4*>(a + kStreamRecHead)[32 * slice + lane];
-        const float2 am = *reinterpret_cast<const float2*>(a + h0), av = *reinterpret_cast<const float2*>(a + 16 + 8 * dg + h0);
-        const float e0 = am.x == -INFINITY ? 0.f : fast_exp2(av.x - v0), e1 = am.y == -INFINITY ? 0.f : fast_exp2(av.y - v1);
-        if (e0 != 0.f) { o.x = fmaf(x.x, e0, o.x); o.z = fmaf(x.z, e0, o.z); }      // (no key: values may be missing)
+    float2 m = make_float2(-INFINITY, -INFINITY), v = m, l = make_float2(0.f, 0.f);
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);            // dimension d of heads h0 and h0 + 1, then d + 1
+    // Takes in another result (am, av, al, x): relative to 2^av, weights to 2^am; am = -infinity: no key, its values may be missing.
+    auto raise = [&](float2 am, float2 av) {
+        const float2 nm = make_float2(fmaxf(m.x, am.x), fmaxf(m.y, am.y)), nv = make_float2(fmaxf(v.x, av.x), fmaxf(v.y, av.y));
+        l.x *= fast_exp2(m.x - finite_ref(nm.x)); l.y *= fast_exp2(m.y - finite_ref(nm.y));
+        const float e0 = fast_exp2(v.x - finite_ref(nv.x)), e1 = fast_exp2(v.y - finite_ref(nv.y));
+        o.x *= e0; o.z *= e0; o.y *= e1; o.w *= e1;
+        m = nm; v = nv;
+    };
+    auto add = [&](float2 am, float2 av, float2 al, float4 x) {
+        l.x += al.x * fast_exp2(am.x - finite_ref(m.x));   // (a NaN sum may come with a maximum of -infinity)
+        l.y += al.y * fast_exp2(am.y - finite_ref(m.y));
+        const float e0 = am.x == -INFINITY ? 0.f : fast_exp2(av.x - finite_ref(v.x)), e1 = am.y == -INFINITY ? 0.f : fast_exp2(av.y - finite_ref(v.y));
+        if (e0 != 0.f) { o.x = fmaf(x.x, e0, o.x); o.z = fmaf(x.z, e0, o.z); }
         if (e1 != 0.f) { o.y = fmaf(x.y, e1, o.y); o.w = fmaf(x.w, e1, o.w); }
+    };
+    const int step = APART ? 8 : 1;
+    for (int i0 = APART ? warp : 0; i0 < n; i0 += kJoin * step) {
+        float2 am[kJoin], av[kJoin], al[kJoin];
+        float4 x[kJoin];
+#pragma unroll
+        for (int k = 0; k < kJoin; ++k) {
+            const int i = i0 + k * step;
+            am[k] = av[k] = make_float2(-INFINITY, -INFINITY);
+            al[k] = make_float2(0.f, 0.f);
+            x[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (i < n) {
+                const float* a = p.own_part + (size_t)(2 * (w0 + i) + (i == 0 && inside ? 1 : 0)) * kStreamRecFloats;
+                am[k] = *reinterpret_cast<const float2*>(a + h0);
+                al[k] = *reinterpret_cast<const float2*>(a + 8 + h0);
+                av[k] = *reinterpret_cast<const float2*>(a + 16 + 8 * dg + h0);
+                x[k] = reinterpret_cast<const float4*>(a + kStreamRecHead)[32 * slice + lane];
+            }
+        }
+        float2 tm = am[0], tv = av[0];
+#pragma unroll
+        for (int k = 1; k < kJoin; ++k) {
+            tm.x = fmaxf(tm.x, am[k].x); tm.y = fmaxf(tm.y, am[k].y);
+            tv.x = fmaxf(tv.x, av[k].x); tv.y = fmaxf(tv.y, av[k].y);
+        }
+        raise(tm, tv);
+#pragma unroll
+        for (int k = 0; k < kJoin; ++k) add(am[k], av[k], al[k], x[k]);
     }
-    if (apart) s_o[warp][lane] = o;
-    __syncthreads();
-    if (apart) {
+    if (APART) {                                           // the warps' shares
+        s_o[warp][lane] = o;
+        s_mv[warp][lane] = make_float4(m.x, m.y, v.x, v.y);
+        s_l[warp][lane] = l;
+        __syncthreads();
         if (warp != 0) return;
-        for (int i = 1; i < 8; ++i) {
-            const float4 x = s_o[i][lane];
-            o.x += x.x; o.y += x.y; o.z += x.z; o.w += x.w;
+        const int parts = min(n, 8);
+        for (int i = 1; i < parts; ++i) {
+            const float4 a = s_mv[i][lane];
+            raise(make_float2(a.x, a.y), make_float2(a.z, a.w));
+            add(make_float2(a.x, a.y), make_float2(a.z, a.w), s_l[i][lane], s_o[i][lane]);
         }
     }
-    const float m0 = s_fin[0][h0], m1 = s_fin[0][h0 + 1], l0 = s_fin[1][h0], l1 = s_fin[1][h0 + 1];
-    const float t0 = s_fin[2 + dg][h0], t1 = s_fin[2 + dg][h0 + 1];
-    if (h0 < p.g) *reinterpret_cast<uint32_t*>(p.out + out + h0 * kHeadDim + d) = pack_bf16x2(final_value(o.x, m0, l0, t0, true), final_value(o.z, m0, l0, t0, true));
+    if (h0 < p.g)
+        *reinterpret_cast<uint32_t*>(p.out + out + h0 * kHeadDim + d) = pack_bf16x2(final_value(o.x, m.x, l.x, v.x, true), final_value(o.z, m.x, l.x, v.x, true));
     if (h0 + 1 < p.g)
-        *reinterpret_cast<uint32_t*>(p.out + out + (h0 + 1) * kHeadDim + d) = pack_bf16x2(final_value(o.y, m1, l1, t1, true), final_value(o.w, m1, l1, t1, true));
-    if (p.lse && slice == 0 && lane < p.g) p.lse[(size_t)seq * p.h_q + (size_t)head * p.g + lane] = final_lse(s_fin[0][lane], s_fin[1][lane], true);
+        *reinterpret_cast<uint32_t*>(p.out + out + (h0 + 1) * kHeadDim + d) = pack_bf16x2(final_value(o.y, m.y, l.y, v.y, true), final_value(o.w, m.y, l.y, v.y, true));
+    if (p.lse && slice == 0 && q == 0) {
+        float* lse = p.lse + (size_t)seq * p.h_q + (size_t)head * p.g + h0;
+        if (h0 < p.g) lse[0] = final_lse(m.x, l.x, true);
+        if (h0 + 1 < p.g) lse[1] = final_lse(m.y, l.y, true);
+    }
 }
 
 template <int F, bool TOGETHER>
@@ -501,7 +552,8 @@ static cudaError_t launch_stream(const PagesAttnLaunch& p, int ctas, cudaStream_
     kernel<<<(unsigned)ctas, kThreads, kSmem, s>>>(p);
     e = cudaGetLastError();
     if (e != cudaSuccess) return e;
-    const int units = p.batch * p.h_kv, apart = units <= 128;
+    const int units = p.batch * p.h_kv;
+    const bool apart = units <= 128;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)units << (apart ? 3 : 0));
     cfg.blockDim = dim3(256);
@@ -511,7 +563,7 @@ static cudaError_t launch_stream(const PagesAttnLaunch& p, int ctas, cudaStream_
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, gkv_pages_stream_merge_kernel<F>, p, ctas * kWarps, apart);
+    return cudaLaunchKernelEx(&cfg, apart ? gkv_pages_stream_merge_kernel<F, true> : gkv_pages_stream_merge_kernel<F, false>, p, ctas * kWarps);
 }
 cudaError_t launch_pages_stream(const PagesAttnLaunch& p, int format, int ctas, cudaStream_t s) {
     const bool together = p.pages.token_rows == 1 && p.pages.page_size % kTile == 0;
