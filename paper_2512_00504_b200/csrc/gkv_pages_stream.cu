@@ -6,12 +6,12 @@
 // all warps have the same work, none waits for another, and the stream of rows from HBM does not stop at the end of a unit. A unit that one
 // warp has to itself is finished by it; of the others (a warp's first or last one) it leaves a partial result, and the merge joins them.
 //
-// Rows come by bulk copies into a ring of the warp's own, issued by its lanes and completed on a barrier of the warp's own: with pages whose
-// size is a multiple of the tile and that hold a head's rows together, one copy for a tile of K and four for V (and two for their scales); with
-// any others, one for each row. (By cp.async, 16 bytes a lane, a tile costs the warp 100 more instructions: 128 sequences x 8 heads of about 2200 keys in bf16
-// 225 us, 2 x 8 of up to 131071 in 4 bits 108.) V is taken in four groups of four rows, 32 bytes further apart than the rows, and row r of
-// the first product (lanes' group q = r % 8) is key 4 (q / 2) + q % 2 + 2 (r / 8): lane j then finds its four keys of V in its own group, at
-// banks of its own.
+// Rows come by bulk copies into a ring of the warp's own, completed on a barrier of its own: with pages whose size is a multiple of the tile and
+// that hold a head's rows together, one copy for a tile of K, one for each four rows of V (4-bit rows: one for all), and two for their
+// scales; with any others, one for each row. (By cp.async, 16 bytes a lane, a tile costs the warp 100 more instructions: 128
+// sequences x 8 heads of about 2200 keys in bf16 225 us, 2 x 8 of up to 131071 in 4 bits 108.) Which key is which row of the products is
+// free as long as the two agree, and chosen such that lanes that read V at once find their rows at banks of their own, groups of four rows
+// being 32 bytes further apart than the rows.
 //
 // Products and softmax are those of the attention over a store (gkv_store_rows.cuh). A row that lies on no page makes its unit NaN.
 // A wait that runs out (never, but every wait ends) makes the warp's units NaN, too.
@@ -21,8 +21,8 @@
 
 namespace gkv {
 
-constexpr int kStreamCtas = 3;                             // of an SM: 12 warps, 168 registers a thread
-int pages_stream_ctas_per_sm() { return kStreamCtas; }
+constexpr int kStreamWarps = 12;                           // of an SM, a CTA each: 168 registers a thread
+int pages_stream_warps_per_sm() { return kStreamWarps; }
 
 // 16-key tiles of a step: what is done once a step (waiting, finding rows, issuing copies) then counts for two of them. bf16 rows are so
 // long that one is enough, and two would leave a ring without stages.
@@ -33,16 +33,27 @@ struct __align__(16) StreamWarp {
     static constexpr int kRow = StoreFormat<F>::kRow, kScales = StoreFormat<F>::kScales;
     static constexpr int kTiles = stream_tiles(F), kKeys = kTiles * kTile;
     static constexpr int kStages = F == GKV_STORE_INT4 ? 3 : 2;
-    static constexpr int kGroup = 4 * kRow + 32;           // bytes from one group of V rows to the next
-    static constexpr int kK = kTile * kRow, kV = 4 * kGroup, kS = kTile * kScales * 2;      // a tile's K, V, and scales of either
-    static constexpr int kBytes = kK + kV + 2 * kS;
-    uint8_t ring[kStages][kTiles][kBytes];
+    // Of V, rows of a group, bytes from one group to the next. 4-bit rows are so short that a copy for each group costs more than what
+    // the banks' conflicts do.
+    static constexpr int kGroupRows = F == GKV_STORE_INT4 ? kKeys : 4, kGroup = kGroupRows * kRow + (F == GKV_STORE_INT4 ? 0 : 32);
+    static constexpr int kV = kKeys * kRow, kKS = kV + kKeys / kGroupRows * kGroup, kVS = kKS + kKeys * kScales * 2;   // where V and scales begin
+    static constexpr int kBytes = kVS + kKeys * kScales * 2;
+    uint8_t ring[kStages][kBytes];
     __nv_bfloat16 row[kHeadDim];                           // a head, or the new key, as it is turned
     uint8_t code[2][kRow];                                 // the new row as it stands in the cache
     __nv_bfloat16 scale[2][4];
     float v[value_groups(F)][8];
     uint32_t rows[kStages][kKeys];                         // numbers of the rows, where they do not lie together
     uint64_t full[kStages];
+
+    static __device__ __forceinline__ int k_at(int key) { return key * kRow; }
+    static __device__ __forceinline__ int v_at(int key) { return kV + key / kGroupRows * kGroup + key % kGroupRows * kRow; }
+    // The keys of a tile behind row r = q + 8 hf of the first product, and (i = 0 .. 3) behind the four that lane j has in the second,
+    // k = 2j, 2j + 1, 2j + 8, 2j + 9: the two agree.
+    static __device__ __forceinline__ int key_of(int q, int hf) {
+        return F == GKV_STORE_INT4 ? (q >> 1) + 4 * (q & 1) + 8 * hf : 4 * (q >> 1) + (q & 1) + 2 * hf;
+    }
+    static __device__ __forceinline__ int key_of_value(int j, int i) { return F == GKV_STORE_INT4 ? j + 4 * i : 4 * j + i; }
 };
 
 // A place in the line of steps: every unit has as many as its rows take, KEYS each.
@@ -85,27 +96,41 @@ __device__ __forceinline__ int64_t stream_total(const PagesAttnLaunch& p, int se
     *before = part * p.h_kv;
     return all * p.h_kv;
 }
-__device__ __forceinline__ int64_t stream_share(int64_t all, int warps) {
-    const int64_t per = all < 1ll << 30 ? (int64_t)(((uint32_t)all + (uint32_t)warps - 1) / (uint32_t)warps) : (all + warps - 1) / warps;
-    return per < kStreamLeast ? kStreamLeast : per;
-}
+// The shares: the first `large` warps take a steps each, the others b.
+struct StreamShares {
+    int large;
+    int64_t a, b;
+    __device__ __forceinline__ StreamShares(int64_t all, int large_, int small) : large(large_) {
+        const int parts = kStreamRatio * large + small;
+        b = all < 1ll << 30 ? (int64_t)(((uint32_t)all + (uint32_t)parts - 1) / (uint32_t)parts) : (all + parts - 1) / parts;
+        a = kStreamRatio * b;
+        if (b < kStreamLeast) {                            // little work: as many warps as it takes
+            a = b = all <= (int64_t)kStreamLeast * large ? kStreamLeast : (all + large - 1) / large;
+        }
+    }
+    __device__ __forceinline__ int64_t begin(int w) const { return w < large ? w * a : large * a + (w - large) * b; }
+    __device__ __forceinline__ int64_t size(int w) const { return w < large ? a : b; }
+    __device__ __forceinline__ int owner(int64_t step) const { return step < large * a ? (int)(step / a) : large + (int)((step - large * a) / b); }
+};
 
 template <int F, bool TOGETHER>
-__global__ void __launch_bounds__(kThreads, kStreamCtas) gkv_pages_stream_kernel(const PagesAttnLaunch p) {
+__global__ void __launch_bounds__(32, kStreamWarps) gkv_pages_stream_kernel(const PagesAttnLaunch p) {
     using Warp = StreamWarp<F>;
     constexpr int NG = value_groups(F), S = Warp::kStages, TILES = Warp::kTiles, KEYS = Warp::kKeys, kRow = Warp::kRow, kScales = Warp::kScales;
     constexpr bool kScaled = F != GKV_STORE_BF16;
     extern __shared__ __align__(128) uint8_t s_raw[];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    Warp& sw = reinterpret_cast<Warp*>(s_raw)[warp];
+    const int lane = threadIdx.x;
+    Warp& sw = *reinterpret_cast<Warp*>(s_raw);
     grid_launch_dependents();
 
     // ---- this warp's steps
-    const int w = blockIdx.x * kWarps + warp;
+    const int w = blockIdx.x;
     int64_t none;
-    const int64_t all = stream_total<KEYS>(p, 0, lane, &none), per = stream_share(all, (int)gridDim.x * kWarps), begin = w * per;
+    const int64_t all = stream_total<KEYS>(p, 0, lane, &none);
+    const StreamShares shares(all, p.splits, (int)gridDim.x - p.splits);
+    const int64_t begin = shares.begin(w);
     if (begin >= all) return;
-    const int steps = (int)(all - begin < per ? all - begin : per);
+    const int steps = (int)(all - begin < shares.size(w) ? all - begin : shares.size(w));
     StreamPlace ahead;
     {
         int64_t left = begin;                              // steps between sequence b's first and ours
@@ -153,6 +178,7 @@ __global__ void __launch_bounds__(kThreads, kStreamCtas) gkv_pages_stream_kernel
         slot = key - page * p.pages.page_size;
         return p.pages.table[ahead.seq * p.pages.table_stride + page];
     };
+    const bool on_one_page = p.pages.page_size % KEYS == 0;      // all rows of a step (rows together)
     int issued = 0, next_slot = 0, next = lookup(next_slot);
     uint32_t lost = 0;                                     // stages with a row on no page
     auto issue = [&](int stage) {
@@ -164,28 +190,41 @@ __global__ void __launch_bounds__(kThreads, kStreamCtas) gkv_pages_stream_kernel
         const uint32_t bar = smem_u32(&sw.full[stage]), to = smem_u32(sw.ring[stage]);
         const int n = fine ? min(max(here, 0), KEYS) : 0;                  // rows to be copied
         if constexpr (TOGETHER) {
-            const int tile = lane >> 4, l = lane & 15, rows = min(n - tile * kTile, kTile);      // (tile 1 of 1: none)
-            const int scaled = kScaled ? (n + kTile - 1) / kTile * 2 * Warp::kS : 0;
-            if (lane == 0) mbar_arrive_expect_tx(bar, (uint32_t)(2 * n * kRow + scaled));
-            if (rows > 0 && tile < TILES && l < (kScaled ? 7 : 5)) {
-                const uint32_t k = to + tile * Warp::kBytes;
-                if (l < 4) {
-                    const int part = min(rows - 4 * l, 4);
-                    if (part > 0) bulk_load(k + Warp::kK + l * Warp::kGroup, p.pages.data[1] + (size_t)(row + 4 * l) * kRow, (uint32_t)(part * kRow), bar);
-                } else if (l == 4) {
-                    bulk_load(k, p.pages.data[0] + (size_t)row * kRow, (uint32_t)(rows * kRow), bar);
-                } else if (kScaled) {                      // those of all of the tile's rows: 16 bytes are the least
-                    bulk_load(k + Warp::kK + Warp::kV + (l - 5) * Warp::kS, p.pages.scale[l - 5] + (size_t)row * kScales, Warp::kS, bar);
+            // One lane issues them all, with numbers that are the same for the warp: a copy takes a few instructions then, and many where every lane
+            // has its own.
+            const bool joined = TILES == 1 || on_one_page;
+            const uint32_t first[2] = {__shfl_sync(0xffffffffu, row, 0), __shfl_sync(0xffffffffu, row, 16)};
+            const int part = joined ? KEYS : kTile;
+            if (elect_one()) {
+                const int scaled = kScaled ? (n + kTile - 1) / kTile * kTile * kScales * 4 : 0;
+                mbar_arrive_expect_tx(bar, (uint32_t)(2 * n * kRow + scaled));
+#pragma unroll
+                for (int t = 0; t < TILES; ++t) {
+                    const int rows = min(n - t * kTile, part), key = t * kTile;
+                    if (rows <= 0 || (t > 0 && joined)) break;
+                    const uint8_t *ks = p.pages.data[0] + (size_t)first[t] * kRow, *vs = p.pages.data[1] + (size_t)first[t] * kRow;
+                    bulk_load(to + Warp::k_at(key), ks, (uint32_t)(rows * kRow), bar);
+                    if constexpr (F == GKV_STORE_INT4) {
+                        bulk_load(to + Warp::v_at(key), vs, (uint32_t)(rows * kRow), bar);
+                    } else {
+#pragma unroll
+                        for (int g = 0; g < KEYS / 4; ++g)
+                            if (rows > 4 * g) bulk_load(to + Warp::v_at(key + 4 * g), vs + 4 * g * kRow, (uint32_t)(min(rows - 4 * g, 4) * kRow), bar);
+                    }
+                    if constexpr (kScaled) {               // those of whole tiles: 16 bytes are the least
+                        const uint32_t bytes = (uint32_t)((rows + kTile - 1) / kTile * kTile * kScales * 2);
+                        bulk_load(to + Warp::kKS + key * kScales * 2, p.pages.scale[0] + (size_t)first[t] * kScales, bytes, bar);
+                        bulk_load(to + Warp::kVS + key * kScales * 2, p.pages.scale[1] + (size_t)first[t] * kScales, bytes, bar);
+                    }
                 }
             }
+            __syncwarp();
         } else {
             if (lane < KEYS) sw.rows[stage][lane] = key0 + lane >= ahead.len + added ? kNoRow : page ? row : kNoPage;
             if (lane == 0) mbar_arrive_expect_tx(bar, (uint32_t)(2 * n * kRow));
             if (lane < n) {
-                const uint32_t k = to + (lane >> 4) * Warp::kBytes;
-                const int r = lane & 15;
-                bulk_load(k + r * kRow, p.pages.data[0] + (size_t)row * kRow, kRow, bar);
-                bulk_load(k + Warp::kK + (r >> 2) * Warp::kGroup + (r & 3) * kRow, p.pages.data[1] + (size_t)row * kRow, kRow, bar);
+                bulk_load(to + Warp::k_at(lane), p.pages.data[0] + (size_t)row * kRow, kRow, bar);
+                bulk_load(to + Warp::v_at(lane), p.pages.data[1] + (size_t)row * kRow, kRow, bar);
             }
         }
         if (++issued < steps) {
@@ -203,7 +242,7 @@ __global__ void __launch_bounds__(kThreads, kStreamCtas) gkv_pages_stream_kernel
         if (issued < steps) issue(s);
 
     const int q = lane >> 2, j = lane & 3, h0 = 2 * j;
-    const int key_a = 4 * (q >> 1) + (q & 1);              // this lane's keys of a tile: key_a and two on
+    const int key[2] = {Warp::key_of(q, 0), Warp::key_of(q, 1)};       // this lane's keys of a tile, for the logits
     TileK<F> tk;
     TileV<F> tv;
     auto take_scales = [&](auto& t, int which, int stage, int tile) {
@@ -211,11 +250,11 @@ __global__ void __launch_bounds__(kThreads, kStreamCtas) gkv_pages_stream_kernel
 #pragma unroll
             for (int hf = 0; hf < 2; ++hf) {
                 if constexpr (TOGETHER) {
-                    const uint32_t a = smem_u32(sw.ring[stage][tile]) + Warp::kK + Warp::kV + which * Warp::kS + (key_a + 2 * hf) * 2 * kScales;
+                    const uint32_t a = smem_u32(sw.ring[stage]) + (which ? Warp::kVS : Warp::kKS) + (tile * kTile + key[hf]) * 2 * kScales;
                     if constexpr (F == GKV_STORE_INT4) t.s[hf] = lds8(a);
                     else t.s[hf] = lds2(a);
                 } else {
-                    const uint32_t r = sw.rows[stage][tile * kTile + key_a + 2 * hf];
+                    const uint32_t r = sw.rows[stage][tile * kTile + key[hf]];
                     const __nv_bfloat16* s = p.pages.scale[which] + (size_t)r * kScales;
                     if constexpr (F == GKV_STORE_INT4) t.s[hf] = r < kNoPage ? ld8(s) : make_uint2(0u, 0u);
                     else t.s[hf] = r < kNoPage ? ld2(s) : 0u;
@@ -294,11 +333,10 @@ __global__ void __launch_bounds__(kThreads, kStreamCtas) gkv_pages_stream_kernel
             // What V and its scales have behind the end, whatever it is, becomes zeros.
             constexpr int kPer = kRow / 16;
             for (int i = lane; i < (KEYS - left) * kPer; i += 32) {
-                const int key = left + i / kPer, k = key & (kTile - 1);
-                uint8_t* t = sw.ring[stage][key / kTile] + Warp::kK;
-                *reinterpret_cast<uint4*>(t + (k >> 2) * Warp::kGroup + (k & 3) * kRow + i % kPer * 16) = make_uint4(0u, 0u, 0u, 0u);
+                const int gone = left + i / kPer;
+                *reinterpret_cast<uint4*>(sw.ring[stage] + Warp::v_at(gone) + i % kPer * 16) = make_uint4(0u, 0u, 0u, 0u);
                 if (kScaled && TOGETHER && i % kPer == 0) {
-                    uint8_t* z = t + Warp::kV + Warp::kS + k * 2 * kScales;
+                    uint8_t* z = sw.ring[stage] + Warp::kVS + gone * 2 * kScales;
                     if (F == GKV_STORE_INT4) *reinterpret_cast<uint2*>(z) = make_uint2(0u, 0u);
                     else *reinterpret_cast<uint16_t*>(z) = 0;
                 }
@@ -320,13 +358,13 @@ __global__ void __launch_bounds__(kThreads, kStreamCtas) gkv_pages_stream_kernel
                 if (to < kNoPage)
                     store_put_row<F>(p.pages.data[lane >> 4] + (size_t)to * kRow, p.pages.scale[lane >> 4] + (size_t)to * kScales, lane & 15, x);
                 __syncwarp();
-                const int key = left - 1, k = key & (kTile - 1);
-                uint8_t* t = sw.ring[stage][key / kTile];
-                uint8_t* dst = lane < 16 ? t + k * kRow : t + Warp::kK + (k >> 2) * Warp::kGroup + (k & 3) * kRow;
+                uint8_t* dst = sw.ring[stage] + (lane < 16 ? Warp::k_at(left - 1) : Warp::v_at(left - 1));
                 if ((lane & 15) < kPer) reinterpret_cast<uint4*>(dst)[lane & 15] = reinterpret_cast<const uint4*>(sw.code[lane >> 4])[lane & 15];
-                if (kScaled && TOGETHER && lane < 2 * kScales)         // (the others take them below)
-                    reinterpret_cast<__nv_bfloat16*>(t + Warp::kK + Warp::kV + lane / max(kScales, 1) * Warp::kS)[k * kScales + lane % max(kScales, 1)] =
-                        sw.scale[lane / max(kScales, 1)][lane % max(kScales, 1)];
+                if (kScaled && TOGETHER && lane < 2 * kScales) {       // (the others take them below)
+                    constexpr int kDiv = kScales > 0 ? kScales : 1;
+                    __nv_bfloat16* z = reinterpret_cast<__nv_bfloat16*>(sw.ring[stage] + (lane < kDiv ? Warp::kKS : Warp::kVS)) + (left - 1) * kScales;
+                    z[lane % kDiv] = sw.scale[lane / kDiv][lane % kDiv];
+                }
             }
             fence_proxy_async_smem();                      // before the ring's next copies
             __syncwarp();
@@ -335,14 +373,14 @@ __global__ void __launch_bounds__(kThreads, kStreamCtas) gkv_pages_stream_kernel
         for (int tile = 0; tile < TILES; ++tile) {
             const int keys = left - tile * kTile;          // of this tile and on
             if (keys <= 0) break;
-            const uint32_t k = smem_u32(sw.ring[stage][tile]), v = k + Warp::kK;
+            const uint32_t base = smem_u32(sw.ring[stage]);
             if (TOGETHER) {
                 take_scales(tk, 0, stage, tile);
                 take_scales(tv, 1, stage, tile);
             } else if (kScaled && last && added) {         // the new row's
 #pragma unroll
                 for (int hf = 0; hf < 2; ++hf)
-                    if (key_a + 2 * hf == keys - 1) {
+                    if (key[hf] == keys - 1) {
                         if constexpr (F == GKV_STORE_INT4) {
                             tk.s[hf] = *reinterpret_cast<const uint2*>(sw.scale[0]);
                             tv.s[hf] = *reinterpret_cast<const uint2*>(sw.scale[1]);
@@ -356,20 +394,20 @@ __global__ void __launch_bounds__(kThreads, kStreamCtas) gkv_pages_stream_kernel
             for (int hf = 0; hf < 2; ++hf)
 #pragma unroll
                 for (int c = 0; c < (F == GKV_STORE_BF16 ? 4 : F == GKV_STORE_INT4 ? 1 : 2); ++c)
-                    tk.d[hf][c] = lds16(k + (key_a + 2 * hf) * kRow + j * 16 + c * 64);
+                    tk.d[hf][c] = lds16(base + Warp::k_at(tile * kTile + key[hf]) + j * 16 + c * 64);
             float z[4];
             tile_logits<F>(tk, qf, f0, f1, z);
             if (keys < kTile) {
 #pragma unroll
                 for (int hf = 0; hf < 2; ++hf)
-                    if (key_a + 2 * hf >= keys) z[2 * hf] = z[2 * hf + 1] = -INFINITY;
+                    if (key[hf] >= keys) z[2 * hf] = z[2 * hf + 1] = -INFINITY;
             }
             if (bad) z[0] = z[1] = z[2] = z[3] = NAN;
             uint32_t b[NG][2];
             r.weigh_tile(z, tv, sw.v, lane, b);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const uint32_t a = v + j * Warp::kGroup + i * kRow + q * (F == GKV_STORE_INT4 ? 8 : 16);
+                const uint32_t a = base + Warp::v_at(tile * kTile + Warp::key_of_value(j, i)) + q * (F == GKV_STORE_INT4 ? 8 : 16);
                 if constexpr (F == GKV_STORE_INT4) tv.d[i] = lds8(a);
                 else if constexpr (F == GKV_STORE_BF16) {
                     tv.d[i][0] = lds16(a);
@@ -452,10 +490,11 @@ __global__ void __launch_bounds__(256, APART ? 2 : 6) gkv_pages_stream_merge_ker
     const int unit = APART ? blockIdx.x >> 3 : blockIdx.x, seq = unit / p.h_kv, head = unit - seq * p.h_kv;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     int64_t before;
-    const int64_t all = stream_total<KEYS>(p, seq, lane, &before), per = stream_share(all, warps);
+    const int64_t all = stream_total<KEYS>(p, seq, lane, &before);
+    const StreamShares shares(all, p.splits, warps - p.splits);
     const int len = p.len[seq], tiles = stream_steps<KEYS>(p, seq);
     const int64_t first = before + (int64_t)head * tiles;
-    const int w0 = (int)(first / per), n = tiles ? (int)((first + tiles - 1) / per) - w0 + 1 : 0;
+    const int w0 = shares.owner(first), n = tiles ? shares.owner(first + tiles - 1) - w0 + 1 : 0;
     const size_t out = ((size_t)seq * p.h_q + (size_t)head * p.g) * kHeadDim;
     const int slice = APART ? blockIdx.x & 7 : warp;       // the two dimensions
     const int q = lane >> 2, h0 = 2 * (lane & 3), d = out_dim<F>(slice, q), dg = slice / (8 / NG);
@@ -472,7 +511,7 @@ __global__ void __launch_bounds__(256, APART ? 2 : 6) gkv_pages_stream_merge_ker
         return;
     }
     // Part i is warp w0 + i's: the first of its two, but where the unit begins inside a warp's share its last one.
-    const bool inside = first != w0 * per;
+    const bool inside = first != shares.begin(w0);
     float2 m = make_float2(-INFINITY, -INFINITY), v = m, l = make_float2(0.f, 0.f);
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);            // dimension d of heads h0 and h0 + 1, then d + 1
     // Takes in another result (am, av, al, x): relative to 2^av, weights to 2^am; am = -infinity: no key, its values may be missing.
@@ -544,12 +583,13 @@ __global__ void __launch_bounds__(256, APART ? 2 : 6) gkv_pages_stream_merge_ker
 
 template <int F, bool TOGETHER>
 static cudaError_t launch_stream(const PagesAttnLaunch& p, int ctas, cudaStream_t s) {
-    constexpr int kSmem = kWarps * (int)sizeof(StreamWarp<F>);
+    constexpr int kSmem = (int)sizeof(StreamWarp<F>);
+    static_assert(kSmem + 1024 <= 228 * 1024 / kStreamWarps, "room for all warps of an SM");
     const auto kernel = gkv_pages_stream_kernel<F, TOGETHER>;
     // a property of the function on the current device; setting it again costs less than finding out whether it is set
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
     if (e != cudaSuccess) return e;
-    kernel<<<(unsigned)ctas, kThreads, kSmem, s>>>(p);
+    kernel<<<(unsigned)ctas, 32, kSmem, s>>>(p);
     e = cudaGetLastError();
     if (e != cudaSuccess) return e;
     const int units = p.batch * p.h_kv;
@@ -563,7 +603,7 @@ static cudaError_t launch_stream(const PagesAttnLaunch& p, int ctas, cudaStream_
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, apart ? gkv_pages_stream_merge_kernel<F, true> : gkv_pages_stream_merge_kernel<F, false>, p, ctas * kWarps);
+    return cudaLaunchKernelEx(&cfg, apart ? gkv_pages_stream_merge_kernel<F, true> : gkv_pages_stream_merge_kernel<F, false>, p, ctas);
 }
 cudaError_t launch_pages_stream(const PagesAttnLaunch& p, int format, int ctas, cudaStream_t s) {
     const bool together = p.pages.token_rows == 1 && p.pages.page_size % kTile == 0;

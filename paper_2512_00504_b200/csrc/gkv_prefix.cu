@@ -63,14 +63,6 @@ struct __align__(16) PrefixTail {
 constexpr size_t kPxSmem = 1024 + 2 * kPxSlotBytes + kPxSlots * kPxSlotBytes + sizeof(PrefixTail);
 static_assert(kPxSmem <= 227 * 1024, "shared memory of a CTA");
 
-// One lane of the warp, chosen by the hardware: the branch that it takes leaves the rest of the code uniform for the warp, which
-// keeps descriptors in uniform registers. (The same products issued under `lane == 0` took 1580 cycles for a P V and a Q K^T of
-// half a tile, more than the tensor cores need.)
-__device__ __forceinline__ bool elect_one() {
-    uint32_t r;
-    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
-    return r != 0;
-}
 // A operand in tensor memory (lane = row, one 32-bit column = two bf16 of the inner index), B in shared memory.
 __device__ __forceinline__ void umma_bf16_ta(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
     asm volatile(
