@@ -7,10 +7,10 @@
 // warp has to itself is finished by it; of the others (a warp's first or last one) it leaves a partial result, and the merge joins them.
 //
 // Rows come by bulk copies into a ring of the warp's own, completed on a barrier of its own: with pages whose size is a multiple of the tile and
-// that hold a head's rows together, one copy for a tile of K, one for each four rows of V (4-bit rows: one for all), and two for their
-// scales; with any others, one for each row. (By cp.async, 16 bytes a lane, a tile costs the warp 100 more instructions: 128
+// that hold a head's rows together, one copy for a tile of K, one for each group of rows of V (four, with 8 bits eight, with 4 bits all), and
+// two for their scales; with any others, one for each row. (By cp.async, 16 bytes a lane, a tile costs the warp 100 more instructions: 128
 // sequences x 8 heads of about 2200 keys in bf16 225 us, 2 x 8 of up to 131071 in 4 bits 108.) Which key is which row of the products is
-// free as long as the two agree, and chosen such that lanes that read V at once find their rows at banks of their own, groups of four rows
+// free as long as the two agree, and chosen such that lanes that read V at once find their rows at banks of their own (4 bits: of two), groups
 // being 32 bytes further apart than the rows.
 //
 // Products and softmax are those of the attention over a store (gkv_store_rows.cuh). A row that lies on no page makes its unit NaN.
@@ -33,14 +33,14 @@ struct __align__(16) StreamWarp {
     static constexpr int kRow = StoreFormat<F>::kRow, kScales = StoreFormat<F>::kScales;
     static constexpr int kTiles = stream_tiles(F), kKeys = kTiles * kTile;
     static constexpr int kStages = F == GKV_STORE_INT4 ? 3 : 2;
-    // Of V, rows of a group, bytes from one group to the next. 4-bit rows are so short that a copy for each group costs more than what
+    // Of V, rows of a group, bytes from one group to the next. The shorter the rows, the more a copy for each group costs against what
     // the banks' conflicts do.
-    static constexpr int kGroupRows = F == GKV_STORE_INT4 ? kKeys : 4, kGroup = kGroupRows * kRow + (F == GKV_STORE_INT4 ? 0 : 32);
+    static constexpr int kGroupRows = F == GKV_STORE_INT4 ? kKeys : F == GKV_STORE_BF16 ? 4 : 8;
+    static constexpr int kGroup = kGroupRows * kRow + (F == GKV_STORE_INT4 ? 0 : 32);
     static constexpr int kV = kKeys * kRow, kKS = kV + kKeys / kGroupRows * kGroup, kVS = kKS + kKeys * kScales * 2;   // where V and scales begin
     static constexpr int kBytes = kVS + kKeys * kScales * 2;
     uint8_t ring[kStages][kBytes];
-    __nv_bfloat16 row[kHeadDim];                           // a head, or the new key, as it is turned
-    uint8_t code[2][kRow];                                 // the new row as it stands in the cache
+    __nv_bfloat16 row[4][kHeadDim];                        // heads as they are turned; the new key (0), and its and its value's codes (2, 3)
     __nv_bfloat16 scale[2][4];
     float v[value_groups(F)][8];
     uint32_t rows[kStages][kKeys];                         // numbers of the rows, where they do not lie together
@@ -79,11 +79,19 @@ __device__ __forceinline__ void stream_next(const PagesAttnLaunch& p, StreamPlac
     }
     c.len = p.len[c.seq];
 }
-// Steps of all units, and of those of the sequences before `seq`.
+// Steps of all units, and of those of the sequences before `seq`. The first 128 sequences' are kept: lane l's of sequences 32 k + l.
+constexpr int kKept = 4;
 template <int KEYS>
-__device__ __forceinline__ int64_t stream_total(const PagesAttnLaunch& p, int seq, int lane, int64_t* before) {
+__device__ __forceinline__ int64_t stream_total(const PagesAttnLaunch& p, int seq, int lane, int (&kept)[kKept], int64_t* before) {
     int64_t all = 0, part = 0;
-    for (int b = lane; b < p.batch; b += 32) {
+#pragma unroll
+    for (int k = 0; k < kKept; ++k) kept[k] = stream_steps<KEYS>(p, 32 * k + lane);
+#pragma unroll
+    for (int k = 0; k < kKept; ++k) {
+        all += kept[k];
+        if (32 * k + lane < seq) part += kept[k];
+    }
+    for (int b = 32 * kKept + lane; b < p.batch; b += 32) {
         const int t = stream_steps<KEYS>(p, b);
         all += t;
         if (b < seq) part += t;
@@ -126,7 +134,8 @@ __global__ void __launch_bounds__(32, kStreamWarps) gkv_pages_stream_kernel(cons
     // ---- this warp's steps
     const int w = blockIdx.x;
     int64_t none;
-    const int64_t all = stream_total<KEYS>(p, 0, lane, &none);
+    int kept[kKept];
+    const int64_t all = stream_total<KEYS>(p, 0, lane, kept, &none);
     const StreamShares shares(all, p.splits, (int)gridDim.x - p.splits);
     const int64_t begin = shares.begin(w);
     if (begin >= all) return;
@@ -135,8 +144,9 @@ __global__ void __launch_bounds__(32, kStreamWarps) gkv_pages_stream_kernel(cons
     {
         int64_t left = begin;                              // steps between sequence b's first and ours
         bool found = false;
+#pragma unroll 1
         for (int b = 0; b < p.batch; b += 32) {
-            const int t = stream_steps<KEYS>(p, b + lane);
+            const int t = b == 0 ? kept[0] : b == 32 ? kept[1] : b == 64 ? kept[2] : b == 96 ? kept[3] : stream_steps<KEYS>(p, b + lane);
             int64_t upto = (int64_t)t * p.h_kv;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
@@ -161,6 +171,94 @@ __global__ void __launch_bounds__(32, kStreamWarps) gkv_pages_stream_kernel(cons
     }
     StreamPlace at = ahead;
     const int added = p.k_new ? 1 : 0;
+
+    const int q = lane >> 2, j = lane & 3, h0 = 2 * j;
+    // Heads' rows are turned word by word (two elements), lane l those of words `word_a` and `word_b`: the two sides of two pairs each, or
+    // (neighbours, and behind the pairs) words l and l + 32 on their own. rot_dim / 2 odd: the sides of a pair are in other halves of their words, and
+    // single elements are turned.
+    const bool rotates = p.rotary.turns != nullptr;
+    const int half = p.rotary.half;
+    const bool words = p.rotary.interleaved || half % 2 == 0, sides = !p.rotary.interleaved && 2 * lane < half;
+    // (halves: words 0 .. half / 2 - 1 are first sides; the words behind the pairs go to the lanes that have none)
+    const int word_a = p.rotary.interleaved ? lane : sides ? lane : 2 * lane;
+    const int word_b = p.rotary.interleaved ? lane + 32 : sides ? lane + half / 2 : 2 * lane + 1;
+    // The two pairs and their frequencies, which stay the same.
+    const bool by_word = words && !p.rotary.interleaved;
+    const int pair_a = by_word ? (sides ? 2 * lane : half) : lane, pair_b = by_word ? (sides ? 2 * lane + 1 : half) : lane + 32;
+    const uint64_t turns_a = rotates && pair_a < half ? p.rotary.turns[pair_a] : 0, turns_b = rotates && pair_b < half ? p.rotary.turns[pair_b] : 0;
+    struct Angles { float2 a, b; };
+    auto angles = [&]() {
+        const int32_t pos = p.pos ? p.pos[at.seq] : added ? at.len : at.len - 1;
+        return Angles{rotary_cos_sin(turns_a, pos, p.rotary.factor, 1.f), rotary_cos_sin(turns_b, pos, p.rotary.factor, 1.f)};
+    };
+    auto first_of = [&](int i) { return i < half ? i : 2 * i; };             // (single elements: pair i, or what lies behind the pairs)
+    auto second_of = [&](int i) { return i < half ? i + half : 2 * i + 1; };
+    struct Two { uint32_t a, b; };
+    auto load_two = [&](const __nv_bfloat16* x) {          // 4 elements of a head
+        if (words) return Two{reinterpret_cast<const uint32_t*>(x)[word_a], reinterpret_cast<const uint32_t*>(x)[word_b]};
+        const uint16_t* e = reinterpret_cast<const uint16_t*>(x);
+        return Two{(uint32_t)e[first_of(lane)] | (uint32_t)e[second_of(lane)] << 16, (uint32_t)e[first_of(lane + 32)] | (uint32_t)e[second_of(lane + 32)] << 16};
+    };
+    auto neighbours = [&](uint32_t w, float2 cs, bool turns) {       // one pair in a word
+        const float2 r = rotary_turn(bf16_lo(w), bf16_hi(w), cs.x, cs.y);
+        return turns ? pack_bf16x2(r.x, r.y) : w;
+    };
+    auto turn_into = [&](__nv_bfloat16* y, Two x, const Angles& g) {
+        if (words && !p.rotary.interleaved) {
+            const float2 r = rotary_turn(bf16_lo(x.a), bf16_lo(x.b), g.a.x, g.a.y), t = rotary_turn(bf16_hi(x.a), bf16_hi(x.b), g.b.x, g.b.y);
+            reinterpret_cast<uint32_t*>(y)[word_a] = sides ? pack_bf16x2(r.x, t.x) : x.a;
+            reinterpret_cast<uint32_t*>(y)[word_b] = sides ? pack_bf16x2(r.y, t.y) : x.b;
+            return;
+        }
+        const uint32_t a = neighbours(x.a, g.a, lane < half), b = neighbours(x.b, g.b, lane + 32 < half);
+        if (words) {
+            reinterpret_cast<uint32_t*>(y)[word_a] = a;
+            reinterpret_cast<uint32_t*>(y)[word_b] = b;
+        } else {
+            uint16_t* e = reinterpret_cast<uint16_t*>(y);
+            e[first_of(lane)] = (uint16_t)a;
+            e[second_of(lane)] = (uint16_t)(a >> 16);
+            e[first_of(lane + 32)] = (uint16_t)b;
+            e[second_of(lane + 32)] = (uint16_t)(b >> 16);
+        }
+    };
+
+    // A unit's heads: their elements, and the operand made of them.
+    uint32_t qf[8][2];
+    float f0 = 0.f, f1 = 0.f;
+    Two e[kMaxGroup];
+    auto load_heads = [&]() {
+        const __nv_bfloat16* x = p.q + ((int64_t)at.seq * p.q_stride + (int64_t)at.head * p.g * kHeadDim);
+        if (rotates) {
+#pragma unroll
+            for (int h = 0; h < kMaxGroup; ++h)
+                if (h < p.g) e[h] = load_two(x + h * kHeadDim);
+        } else {
+#pragma unroll
+            for (int ks = 0; ks < 8; ++ks) load_query<F>(x + min(q, p.g - 1) * kHeadDim, ks, j, qf[ks][0], qf[ks][1]);
+        }
+    };
+    auto make_heads = [&]() {
+        if (rotates) {
+            const Angles g = angles();
+#pragma unroll
+            for (int h4 = 0; h4 < kMaxGroup; h4 += 4)
+                if (h4 < p.g) {
+#pragma unroll
+                    for (int h = 0; h < 4; ++h)
+                        if (h4 + h < p.g) turn_into(sw.row[h], e[h4 + h], g);
+                    __syncwarp();
+                    const int mine = min(q, p.g - 1) - h4;
+                    if (mine >= 0 && mine < 4)
+#pragma unroll
+                        for (int ks = 0; ks < 8; ++ks) load_query<F>(sw.row[mine], ks, j, qf[ks][0], qf[ks][1]);
+                    __syncwarp();
+                }
+        }
+        f0 = f1 = p.scale_log2;
+        scale_queries<F>(lane, qf, f0, f1);
+    };
+    load_heads();                                          // the first unit's, ahead of the ring's many bytes
 
     if (lane == 0) {
 #pragma unroll
@@ -208,8 +306,8 @@ __global__ void __launch_bounds__(32, kStreamWarps) gkv_pages_stream_kernel(cons
                         bulk_load(to + Warp::v_at(key), vs, (uint32_t)(rows * kRow), bar);
                     } else {
 #pragma unroll
-                        for (int g = 0; g < KEYS / 4; ++g)
-                            if (rows > 4 * g) bulk_load(to + Warp::v_at(key + 4 * g), vs + 4 * g * kRow, (uint32_t)(min(rows - 4 * g, 4) * kRow), bar);
+                        for (int g = 0; g < KEYS; g += Warp::kGroupRows)
+                            if (rows > g) bulk_load(to + Warp::v_at(key + g), vs + g * kRow, (uint32_t)(min(rows - g, Warp::kGroupRows) * kRow), bar);
                     }
                     if constexpr (kScaled) {               // those of whole tiles: 16 bytes are the least
                         const uint32_t bytes = (uint32_t)((rows + kTile - 1) / kTile * kTile * kScales * 2);
@@ -241,7 +339,6 @@ __global__ void __launch_bounds__(32, kStreamWarps) gkv_pages_stream_kernel(cons
     for (int s = 0; s < S; ++s)
         if (issued < steps) issue(s);
 
-    const int q = lane >> 2, j = lane & 3, h0 = 2 * j;
     const int key[2] = {Warp::key_of(q, 0), Warp::key_of(q, 1)};       // this lane's keys of a tile, for the logits
     TileK<F> tk;
     TileV<F> tv;
@@ -262,25 +359,8 @@ __global__ void __launch_bounds__(32, kStreamWarps) gkv_pages_stream_kernel(cons
             }
         }
     };
-    // Two elements of a head's row that are turned together (or, behind the pairs, copied): those of pair number i.
-    const bool rotates = p.rotary.turns != nullptr;
-    auto first_of = [&](int i) { return i < p.rotary.half && !p.rotary.interleaved ? i : 2 * i; };
-    auto second_of = [&](int i) { return i < p.rotary.half && !p.rotary.interleaved ? i + p.rotary.half : 2 * i + 1; };
-    auto cos_sin = [&](int i) {
-        if (i >= p.rotary.half) return make_float2(1.f, 0.f);
-        return rotary_cos_sin(p.rotary.turns[i], p.pos ? p.pos[at.seq] : added ? at.len : at.len - 1, p.rotary.factor, 1.f);
-    };
-    auto turn_into = [&](int i, __nv_bfloat16 a, __nv_bfloat16 b, float2 cs) {
-        const float2 r = rotary_turn(__bfloat162float(a), __bfloat162float(b), cs.x, cs.y);
-        const bool turns = i < p.rotary.half;
-        sw.row[first_of(i)] = turns ? __float2bfloat16_rn(r.x) : a;
-        sw.row[second_of(i)] = turns ? __float2bfloat16_rn(r.y) : b;
-    };
-
-    uint32_t qf[8][2];
-    float f0 = 0.f, f1 = 0.f;
     RunningRows<F> r;
-    bool begins = true, whole = false, ok = true;          // a unit begins; it is ours from its first tile on; no wait has run out
+    bool whole = at.tile == 0, ok = true;                  // the unit is ours from its first tile on; no wait has run out
     bool first_unit = true;
     int stage = 0;
     uint32_t parity = 0;
@@ -289,42 +369,9 @@ __global__ void __launch_bounds__(32, kStreamWarps) gkv_pages_stream_kernel(cons
         take_scales(tk, 0, 0, 0);
         take_scales(tv, 1, 0, 0);
     }
+    make_heads();
+    r.start(sw.v, lane);
     for (int step = 0; step < steps; ++step) {
-        if (begins) {
-            // ---- a unit's heads
-            const __nv_bfloat16* x = p.q + ((int64_t)at.seq * p.q_stride + (int64_t)at.head * p.g * kHeadDim);
-            if (rotates) {
-                __nv_bfloat16 e[kMaxGroup][4];
-#pragma unroll
-                for (int h = 0; h < kMaxGroup; ++h)
-                    if (h < p.g)
-#pragma unroll
-                        for (int k = 0; k < 2; ++k) {
-                            e[h][2 * k] = x[h * kHeadDim + first_of(lane + 32 * k)];
-                            e[h][2 * k + 1] = x[h * kHeadDim + second_of(lane + 32 * k)];
-                        }
-                const float2 cs0 = cos_sin(lane), cs1 = cos_sin(lane + 32);
-#pragma unroll
-                for (int h = 0; h < kMaxGroup; ++h)
-                    if (h < p.g) {
-                        turn_into(lane, e[h][0], e[h][1], cs0);
-                        turn_into(lane + 32, e[h][2], e[h][3], cs1);
-                        __syncwarp();
-                        if (min(q, p.g - 1) == h)
-#pragma unroll
-                            for (int ks = 0; ks < 8; ++ks) load_query<F>(sw.row, ks, j, qf[ks][0], qf[ks][1]);
-                        __syncwarp();
-                    }
-            } else {
-#pragma unroll
-                for (int ks = 0; ks < 8; ++ks) load_query<F>(x + min(q, p.g - 1) * kHeadDim, ks, j, qf[ks][0], qf[ks][1]);
-            }
-            f0 = f1 = p.scale_log2;
-            scale_queries<F>(lane, qf, f0, f1);
-            r.start(sw.v, lane);
-            whole = at.tile == 0;
-            begins = false;
-        }
         // ---- a step
         if (ok) ok = __all_sync(0xffffffffu, mbar_wait_bounded(smem_u32(&sw.full[stage]), parity));
         const int left = at.len + added - at.tile * KEYS;                        // keys from this step's first on
@@ -347,19 +394,18 @@ __global__ void __launch_bounds__(32, kStreamWarps) gkv_pages_stream_kernel(cons
                 const __nv_bfloat16 *kn = p.k_new + new_row, *vn = p.v_new + new_row;
                 const int32_t e = page_entry(p.pages, p.pages.table + at.seq * p.pages.table_stride, at.len);
                 if (rotates) {
-                    turn_into(lane, kn[first_of(lane)], kn[second_of(lane)], cos_sin(lane));
-                    turn_into(lane + 32, kn[first_of(lane + 32)], kn[second_of(lane + 32)], cos_sin(lane + 32));
+                    turn_into(sw.row[0], load_two(kn), angles());
                     __syncwarp();
-                    kn = sw.row;
+                    kn = sw.row[0];
                 }
                 const uint4 x = store_load_source<F>(lane < 16 ? kn : vn, lane & 15);
                 const uint32_t to = page_row(p.pages, e, (uint32_t)at.head * p.pages.head_rows, at.len);
-                store_put_row<F>(sw.code[lane >> 4], sw.scale[lane >> 4], lane & 15, x);
+                store_put_row<F>(reinterpret_cast<uint8_t*>(sw.row[2 + (lane >> 4)]), sw.scale[lane >> 4], lane & 15, x);
                 if (to < kNoPage)
                     store_put_row<F>(p.pages.data[lane >> 4] + (size_t)to * kRow, p.pages.scale[lane >> 4] + (size_t)to * kScales, lane & 15, x);
                 __syncwarp();
                 uint8_t* dst = sw.ring[stage] + (lane < 16 ? Warp::k_at(left - 1) : Warp::v_at(left - 1));
-                if ((lane & 15) < kPer) reinterpret_cast<uint4*>(dst)[lane & 15] = reinterpret_cast<const uint4*>(sw.code[lane >> 4])[lane & 15];
+                if ((lane & 15) < kPer) reinterpret_cast<uint4*>(dst)[lane & 15] = reinterpret_cast<const uint4*>(sw.row[2 + (lane >> 4)])[lane & 15];
                 if (kScaled && TOGETHER && lane < 2 * kScales) {       // (the others take them below)
                     constexpr int kDiv = kScales > 0 ? kScales : 1;
                     __nv_bfloat16* z = reinterpret_cast<__nv_bfloat16*>(sw.ring[stage] + (lane < kDiv ? Warp::kKS : Warp::kVS)) + (left - 1) * kScales;
@@ -469,11 +515,17 @@ __global__ void __launch_bounds__(32, kStreamWarps) gkv_pages_stream_kernel(cons
 #pragma unroll
                 for (int i = 0; i < 8; ++i) o[32 * i] = make_float4(r.acc[i][0], r.acc[i][1], r.acc[i][2], r.acc[i][3]);
             }
-            begins = true;
             first_unit = false;
+            if (step + 1 == steps) break;
             __syncwarp();
+            stream_next<KEYS>(p, at);
+            whole = true;
+            load_heads();
+            make_heads();
+            r.start(sw.v, lane);
+        } else {
+            stream_next<KEYS>(p, at);
         }
-        if (step + 1 < steps) stream_next<KEYS>(p, at);
     }
     if (!ok)                                               // what is still on its way gets a bounded time to arrive
         for (int s = 0; s < S; ++s) mbar_wait_bounded(smem_u32(&sw.full[s]), s < stage ? parity ^ 1 : parity);
@@ -490,7 +542,8 @@ __global__ void __launch_bounds__(256, APART ? 2 : 6) gkv_pages_stream_merge_ker
     const int unit = APART ? blockIdx.x >> 3 : blockIdx.x, seq = unit / p.h_kv, head = unit - seq * p.h_kv;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     int64_t before;
-    const int64_t all = stream_total<KEYS>(p, seq, lane, &before);
+    int kept[kKept];
+    const int64_t all = stream_total<KEYS>(p, seq, lane, kept, &before);
     const StreamShares shares(all, p.splits, warps - p.splits);
     const int len = p.len[seq], tiles = stream_steps<KEYS>(p, seq);
     const int64_t first = before + (int64_t)head * tiles;
