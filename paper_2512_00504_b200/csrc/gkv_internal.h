@@ -219,8 +219,7 @@ struct PagesCopyLaunch {       // append / read
 // at least kStreamLeast tiles.
 constexpr int kStreamRecHead = 48, kStreamRecFloats = kStreamRecHead + kHeadDimHost * 8;
 constexpr int kStreamLeast = 4;
-constexpr int kStreamMaxWarps = 8192;
-constexpr int kStreamRatio = 1;
+constexpr int kStreamMaxWarps = 2560;
 // (The names that it shares with StoreAttnLaunch are those of the code that both kinds of attention have in common. It is a
 // struct of its own because the host pays for the length of what a launch carries.)
 struct PagesAttnLaunch {
@@ -294,7 +293,7 @@ cudaError_t launch_pages_read(const PagesCopyLaunch& p, cudaStream_t s);
 cudaError_t launch_pages_attn(const PagesAttnLaunch& p, int format, cudaStream_t s);        // a cluster (or one CTA) a unit
 cudaError_t launch_pages_stream(const PagesAttnLaunch& p, int format, int ctas, cudaStream_t s);   // equal shares for all warps, then the merge
 int pages_attn_ctas_per_sm(int format);
-int pages_stream_warps_per_sm();
+int pages_stream_warps_per_sm(const PagesAttnLaunch& p, int format);
 int device_sm_count();                                                                      // of the current device
 bool rows_overlap(int64_t width, const int64_t (&n)[3], const int64_t (&s)[3]);             // of an array of rows
 gkv_status encode_map(CUtensorMap* map, void* base, uint64_t rows, uint32_t box_rows);      // [rows][128] bf16, 64-element boxes

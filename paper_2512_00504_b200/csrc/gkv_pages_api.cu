@@ -68,7 +68,6 @@ PagesView view(const gkv_pages* g, const gkv_page_table* t) {
 constexpr uint64_t kStreamBytes = (uint64_t)kStreamMaxWarps * 2 * kStreamRecFloats * sizeof(float);
 constexpr int kStreamMaxUnits = 16384, kStreamMaxBatch = 2048;      // its merge has a CTA a unit, which adds up all lengths
 constexpr int kStreamFrom = 6;
-constexpr int kStreamRounds = 0;
 
 // A cluster of up to kMaxCluster CTAs a unit, if that leaves a warp no more than kStreamFrom tiles (or there are more units than the merge of the
 // other form is made for); else equal shares for all warps. Returns the CTAs of the latter, 0 for the former.
@@ -83,8 +82,7 @@ int pages_plan(PagesAttnLaunch* p, int format, int max_len, int sm_count) {
     p->split_tiles = tiles > 0 ? (int)((tiles + splits - 1) / splits) : 1;
     p->splits = tiles > 0 ? (tiles + p->split_tiles - 1) / p->split_tiles : 1;
     if (p->split_tiles <= 4 * kStreamFrom || units > kStreamMaxUnits || p->batch > kStreamMaxBatch) return 0;
-    p->splits = pages_stream_warps_per_sm() * sm_count;
-    const int warps = p->splits * (1 + kStreamRounds);
+    const int warps = pages_stream_warps_per_sm(*p, format) * sm_count;
     return warps < kStreamMaxWarps ? warps : kStreamMaxWarps;
 }
 

@@ -8,7 +8,8 @@
 //
 // Rows come by bulk copies into a ring of the warp's own, completed on a barrier of its own: with pages whose size is a multiple of the tile and
 // that hold a head's rows together, one copy for a tile of K, one for each group of rows of V (four, with 8 bits eight, with 4 bits all), and
-// two for their scales; with any others, one for each row. (By cp.async, 16 bytes a lane, a tile costs the warp 100 more instructions: 128
+// two for their scales; with any others, one for each bf16 row, and 16 bytes a lane at a time for shorter ones (a copy of its own for each takes
+// 13 cycles: 128 x 8 heads of about 2200 keys in 8 bits in pages of 5 rows 216 us instead of REPLACE). (By cp.async, 16 bytes a lane, a tile costs the warp 100 more instructions: 128
 // sequences x 8 heads of about 2200 keys in bf16 225 us, 2 x 8 of up to 131071 in 4 bits 108.) Which key is which row of the products is
 // free as long as the two agree, and chosen such that lanes that read V at once find their rows at banks of their own (4 bits: of two), groups
 // being 32 bytes further apart than the rows.
@@ -21,8 +22,10 @@
 
 namespace gkv {
 
-constexpr int kStreamWarps = 12;                           // of an SM, a CTA each: 168 registers a thread
-int pages_stream_warps_per_sm() { return kStreamWarps; }
+// Warps of an SM, a CTA each: as many as shared memory has room for, three for each scheduler. (bf16 rows that lie together come in copies so
+// large that two are enough: 128 sequences x 8 heads of about 2200 keys in pages of 16 191 us, with 12 warps 199. Apart, 16 x 4 heads: 218
+// with 12, 296 with 8. 4 bits, 2 x 8 of up to 131071: 89, 99; 14 or 16 leave too few registers.)
+__host__ __device__ constexpr int stream_warps(int format, bool together) { return format == GKV_STORE_BF16 && together ? 8 : 12; }
 
 // 16-key tiles of a step: what is done once a step (waiting, finding rows, issuing copies) then counts for two of them. bf16 rows are so
 // long that one is enough, and two would leave a ring without stages.
@@ -104,25 +107,17 @@ __device__ __forceinline__ int64_t stream_total(const PagesAttnLaunch& p, int se
     *before = part * p.h_kv;
     return all * p.h_kv;
 }
-// The shares: the first `large` warps take a steps each, the others b.
-struct StreamShares {
-    int large;
-    int64_t a, b;
-    __device__ __forceinline__ StreamShares(int64_t all, int large_, int small) : large(large_) {
-        const int parts = kStreamRatio * large + small;
-        b = all < 1ll << 30 ? (int64_t)(((uint32_t)all + (uint32_t)parts - 1) / (uint32_t)parts) : (all + parts - 1) / parts;
-        a = kStreamRatio * b;
-        if (b < kStreamLeast) {                            // little work: as many warps as it takes
-            a = b = all <= (int64_t)kStreamLeast * large ? kStreamLeast : (all + large - 1) / large;
-        }
-    }
-    __device__ __forceinline__ int64_t begin(int w) const { return w < large ? w * a : large * a + (w - large) * b; }
-    __device__ __forceinline__ int64_t size(int w) const { return w < large ? a : b; }
-    __device__ __forceinline__ int owner(int64_t step) const { return step < large * a ? (int)(step / a) : large + (int)((step - large * a) / b); }
-};
+// A warp's share of the steps.
+__device__ __forceinline__ int64_t stream_share(int64_t all, int warps) {
+    const int64_t per = all < 1ll << 30 ? (int64_t)(((uint32_t)all + (uint32_t)warps - 1) / (uint32_t)warps) : (all + warps - 1) / warps;
+    return per < kStreamLeast ? kStreamLeast : per;
+}
+__device__ __forceinline__ int stream_owner(int64_t step, int64_t per) {
+    return step < 1ll << 30 && per < 1ll << 30 ? (int)((uint32_t)step / (uint32_t)per) : (int)(step / per);
+}
 
 template <int F, bool TOGETHER>
-__global__ void __launch_bounds__(32, kStreamWarps) gkv_pages_stream_kernel(const PagesAttnLaunch p) {
+__global__ void __launch_bounds__(32, stream_warps(F, TOGETHER)) gkv_pages_stream_kernel(const PagesAttnLaunch p) {
     using Warp = StreamWarp<F>;
     constexpr int NG = value_groups(F), S = Warp::kStages, TILES = Warp::kTiles, KEYS = Warp::kKeys, kRow = Warp::kRow, kScales = Warp::kScales;
     constexpr bool kScaled = F != GKV_STORE_BF16;
@@ -136,10 +131,9 @@ __global__ void __launch_bounds__(32, kStreamWarps) gkv_pages_stream_kernel(cons
     int64_t none;
     int kept[kKept];
     const int64_t all = stream_total<KEYS>(p, 0, lane, kept, &none);
-    const StreamShares shares(all, p.splits, (int)gridDim.x - p.splits);
-    const int64_t begin = shares.begin(w);
+    const int64_t per = stream_share(all, (int)gridDim.x), begin = w * per;
     if (begin >= all) return;
-    const int steps = (int)(all - begin < shares.size(w) ? all - begin : shares.size(w));
+    const int steps = (int)(all - begin < per ? all - begin : per);
     StreamPlace ahead;
     {
         int64_t left = begin;                              // steps between sequence b's first and ours
@@ -262,7 +256,7 @@ __global__ void __launch_bounds__(32, kStreamWarps) gkv_pages_stream_kernel(cons
 
     if (lane == 0) {
 #pragma unroll
-        for (int s = 0; s < S; ++s) mbar_init(smem_u32(&sw.full[s]), 1);
+        for (int s = 0; s < S; ++s) mbar_init(smem_u32(&sw.full[s]), kScaled && !TOGETHER ? 32 : 1);
         fence_mbar_init();
     }
     __syncwarp();
@@ -319,10 +313,24 @@ __global__ void __launch_bounds__(32, kStreamWarps) gkv_pages_stream_kernel(cons
             __syncwarp();
         } else {
             if (lane < KEYS) sw.rows[stage][lane] = key0 + lane >= ahead.len + added ? kNoRow : page ? row : kNoPage;
-            if (lane == 0) mbar_arrive_expect_tx(bar, (uint32_t)(2 * n * kRow));
-            if (lane < n) {
-                bulk_load(to + Warp::k_at(lane), p.pages.data[0] + (size_t)row * kRow, kRow, bar);
-                bulk_load(to + Warp::v_at(lane), p.pages.data[1] + (size_t)row * kRow, kRow, bar);
+            if constexpr (kScaled) {
+                constexpr int kPer = kRow / 16;            // pieces of a row
+#pragma unroll
+                for (int i = 0; i < KEYS * kPer / 32; ++i) {
+                    const int key = i * (32 / kPer) + lane / kPer, piece = lane % kPer * 16;
+                    const size_t src = (size_t)__shfl_sync(0xffffffffu, row, key) * kRow + piece;
+                    if (key < n) {
+                        cp_async_16(to + Warp::k_at(key) + piece, p.pages.data[0] + src);
+                        cp_async_16(to + Warp::v_at(key) + piece, p.pages.data[1] + src);
+                    }
+                }
+                asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
+            } else {
+                if (lane == 0) mbar_arrive_expect_tx(bar, (uint32_t)(2 * n * kRow));
+                if (lane < n) {
+                    bulk_load(to + Warp::k_at(lane), p.pages.data[0] + (size_t)row * kRow, kRow, bar);
+                    bulk_load(to + Warp::v_at(lane), p.pages.data[1] + (size_t)row * kRow, kRow, bar);
+                }
             }
         }
         if (++issued < steps) {
@@ -544,10 +552,10 @@ __global__ void __launch_bounds__(256, APART ? 2 : 6) gkv_pages_stream_merge_ker
     int64_t before;
     int kept[kKept];
     const int64_t all = stream_total<KEYS>(p, seq, lane, kept, &before);
-    const StreamShares shares(all, p.splits, warps - p.splits);
+    const int64_t per = stream_share(all, warps);
     const int len = p.len[seq], tiles = stream_steps<KEYS>(p, seq);
     const int64_t first = before + (int64_t)head * tiles;
-    const int w0 = shares.owner(first), n = tiles ? shares.owner(first + tiles - 1) - w0 + 1 : 0;
+    const int w0 = stream_owner(first, per), n = tiles ? stream_owner(first + tiles - 1, per) - w0 + 1 : 0;
     const size_t out = ((size_t)seq * p.h_q + (size_t)head * p.g) * kHeadDim;
     const int slice = APART ? blockIdx.x & 7 : warp;       // the two dimensions
     const int q = lane >> 2, h0 = 2 * (lane & 3), d = out_dim<F>(slice, q), dg = slice / (8 / NG);
@@ -564,7 +572,7 @@ __global__ void __launch_bounds__(256, APART ? 2 : 6) gkv_pages_stream_merge_ker
         return;
     }
     // Part i is warp w0 + i's: the first of its two, but where the unit begins inside a warp's share its last one.
-    const bool inside = first != shares.begin(w0);
+    const bool inside = first != w0 * per;
     float2 m = make_float2(-INFINITY, -INFINITY), v = m, l = make_float2(0.f, 0.f);
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);            // dimension d of heads h0 and h0 + 1, then d + 1
     // Takes in another result (am, av, al, x): relative to 2^av, weights to 2^am; am = -infinity: no key, its values may be missing.
@@ -637,7 +645,7 @@ __global__ void __launch_bounds__(256, APART ? 2 : 6) gkv_pages_stream_merge_ker
 template <int F, bool TOGETHER>
 static cudaError_t launch_stream(const PagesAttnLaunch& p, int ctas, cudaStream_t s) {
     constexpr int kSmem = (int)sizeof(StreamWarp<F>);
-    static_assert(kSmem + 1024 <= 228 * 1024 / kStreamWarps, "room for all warps of an SM");
+    static_assert(kSmem + 1024 <= 228 * 1024 / stream_warps(F, TOGETHER), "room for all warps of an SM");
     const auto kernel = gkv_pages_stream_kernel<F, TOGETHER>;
     // a property of the function on the current device; setting it again costs less than finding out whether it is set
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
@@ -658,8 +666,10 @@ static cudaError_t launch_stream(const PagesAttnLaunch& p, int ctas, cudaStream_
     cfg.numAttrs = 1;
     return cudaLaunchKernelEx(&cfg, apart ? gkv_pages_stream_merge_kernel<F, true> : gkv_pages_stream_merge_kernel<F, false>, p, ctas);
 }
+static bool rows_together(const PagesAttnLaunch& p) { return p.pages.token_rows == 1 && p.pages.page_size % kTile == 0; }
+int pages_stream_warps_per_sm(const PagesAttnLaunch& p, int format) { return stream_warps(format, rows_together(p)); }
 cudaError_t launch_pages_stream(const PagesAttnLaunch& p, int format, int ctas, cudaStream_t s) {
-    const bool together = p.pages.token_rows == 1 && p.pages.page_size % kTile == 0;
+    const bool together = rows_together(p);
     switch (format) {
         case GKV_STORE_BF16: return together ? launch_stream<GKV_STORE_BF16, true>(p, ctas, s) : launch_stream<GKV_STORE_BF16, false>(p, ctas, s);
         case GKV_STORE_E4M3: return together ? launch_stream<GKV_STORE_E4M3, true>(p, ctas, s) : launch_stream<GKV_STORE_E4M3, false>(p, ctas, s);
