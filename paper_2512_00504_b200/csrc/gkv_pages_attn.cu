@@ -171,9 +171,29 @@ __global__ void __launch_bounds__(kThreads, pages_ctas(F)) gkv_pages_attn_kernel
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int unit = blockIdx.x / p.splits, split = blockIdx.x - unit * p.splits, splits = p.splits, split_tiles = p.split_tiles;
     const int seq = unit / p.h_kv, head = unit - seq * p.h_kv;
+    // ---- everything that can be loaded before the length is known: the heads (those of this warp), the new row, and what the table has for the
+    // first tiles, were they all there
+    const bool append = p.k_new != nullptr;
+    const HeadTurn turn(p.rotary, lane);
+    const __nv_bfloat16* q = p.q + ((int64_t)seq * p.q_stride + (int64_t)head * p.g * kHeadDim);
+    const __nv_bfloat16* k_new = append ? p.k_new + ((int64_t)seq * p.kv_stride + (int64_t)head * kHeadDim) : q;
+    const __nv_bfloat16* v_new = append ? p.v_new + ((int64_t)seq * p.kv_stride + (int64_t)head * kHeadDim) : q;
+    HeadTurn::Words heads[2], key_words;
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+        if (warp + k * kWarps < p.g) heads[k] = turn.load(q + (warp + k * kWarps) * kHeadDim);
+    key_words = turn.load(k_new);
+    const uint4 value = store_load_source<F>(v_new, lane & 15);
+    const int32_t given = p.pos ? p.pos[seq] : 0;
+    const int32_t* table = p.pages.table + seq * p.pages.table_stride;
+    constexpr int kStep = kWarps * kTile;
+    const int guess0 = (split * split_tiles + warp) * kTile + (lane & 15);
+    int32_t e[S + 1];
+#pragma unroll
+    for (int s = 0; s <= S; ++s) e[s] = guess0 + s * kStep < p.capacity ? page_entry(p.pages, table, guess0 + s * kStep) : 0;
+
     const int len = p.len[seq];
     if (len < 0) return;
-    const bool append = p.k_new != nullptr;
     const bool fits = append ? len < p.capacity : len <= p.capacity;
     const int old = fits ? len : 0, n = old + (fits && append ? 1 : 0);      // rows in the pages, rows to attend to
     const int tiles = (n + kTile - 1) / kTile;
@@ -183,12 +203,10 @@ __global__ void __launch_bounds__(kThreads, pages_ctas(F)) gkv_pages_attn_kernel
     const bool writes = append && fits && own_tiles > 0 && t_end == tiles;
 
     // ---- the first tiles set out. Tile s of this warp begins with key `key0` + s * kWarps * kTile.
-    const int32_t* table = p.pages.table + seq * p.pages.table_stride;
     const uint32_t head0 = (uint32_t)head * p.pages.head_rows;
-    const int key0 = (t_begin + warp) * kTile;
+    const int key0 = (t_begin + warp) * kTile;           // (the guess, wherever there is a tile)
     const int mine = own_tiles > warp ? (own_tiles - warp + kWarps - 1) / kWarps : 0;
     const int last_old = min(old, t_end * kTile);        // (a piece's tiles are whole but for the unit's last)
-    constexpr int kStep = kWarps * kTile;
     auto entry = [&](int s) {
         const int key = key0 + s * kStep + (lane & 15);
         return key < last_old ? page_entry(p.pages, table, key) : 0;
@@ -200,9 +218,6 @@ __global__ void __launch_bounds__(kThreads, pages_ctas(F)) gkv_pages_attn_kernel
     const uint8_t *kb = p.pages.data[0], *vb = p.pages.data[1];
     const __nv_bfloat16 *ksb = p.pages.scale[0], *vsb = p.pages.scale[1];
     const uint32_t ring = smem_u32(s_ring) + warp * Ring::kWarp;
-    int32_t e[S + 1];
-#pragma unroll
-    for (int s = 0; s <= S; ++s) e[s] = entry(s);
     uint32_t rows[S];                                    // of tiles s + 1 .. s + S
     TileK<F> tk;
     TileV<F> tv;
@@ -225,43 +240,21 @@ __global__ void __launch_bounds__(kThreads, pages_ctas(F)) gkv_pages_attn_kernel
 
     // ---- q and the new row
     const int hq = lane >> 2;
-    const __nv_bfloat16* q = p.q + (int64_t)seq * p.q_stride + (int64_t)head * p.g * kHeadDim;
-    const __nv_bfloat16* k_new = append ? p.k_new + (int64_t)seq * p.kv_stride + (int64_t)head * kHeadDim : nullptr;
-    const __nv_bfloat16* v_new = append ? p.v_new + (int64_t)seq * p.kv_stride + (int64_t)head * kHeadDim : nullptr;
-    if (p.rotary.turns) {
-        // thread t: pair t & 63 (those behind the pairs that turn are copied), every other row
-        const int half = p.rotary.half, i = threadIdx.x & 63;
-        const bool turns = i < half;
-        const int a = turns && !p.rotary.interleaved ? i : 2 * i, b = turns && !p.rotary.interleaved ? i + half : 2 * i + 1;
-        float2 cs = make_float2(1.f, 0.f);
-        if (turns) cs = rotary_cos_sin(p.rotary.turns[i], p.pos ? p.pos[seq] : append ? len : len - 1, p.rotary.factor, 1.f);
-        const int n_rows = p.g + (writes ? 1 : 0);
-        for (int h = threadIdx.x >> 6; h < n_rows; h += kThreads / 64) {
-            const __nv_bfloat16* x = h < p.g ? q + h * kHeadDim : k_new;
-            __nv_bfloat16* y = s_q[h < p.g ? h : kMaxGroup];
-            const __nv_bfloat16 xa = x[a], xb = x[b];
-            if (turns) {
-                const float2 r = rotary_turn(__bfloat162float(xa), __bfloat162float(xb), cs.x, cs.y);
-                y[a] = __float2bfloat16_rn(r.x);
-                y[b] = __float2bfloat16_rn(r.y);
-            } else {
-                y[a] = xa;
-                y[b] = xb;
-            }
-        }
-        __syncthreads();
-        q = s_q[0];
-        k_new = s_q[kMaxGroup];
-    }
+    const HeadTurn::Angles angles = turn.angles(p.pos ? given : append ? len : len - 1);
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+        if (warp + k * kWarps < p.g) turn.put(s_q[warp + k * kWarps], heads[k], angles);
+    const int new_step = writes && warp == (own_tiles - 1) % kWarps ? mine - 1 : -1;     // the tile that has the new row
+    if (new_step >= 0) turn.put(s_q[kMaxGroup], key_words, angles);
+    __syncthreads();
     uint32_t qf[8][2];
     float f0 = p.scale_log2, f1 = p.scale_log2;
-    load_queries<F>(q + min(hq, p.g - 1) * kHeadDim, lane, qf, f0, f1);
+    load_queries<F>(s_q[min(hq, p.g - 1)], lane, qf, f0, f1);
     bool new_page = true;
-    const int new_step = writes && warp == (own_tiles - 1) % kWarps ? mine - 1 : -1;     // the tile that has the new row
     if (new_step >= 0) {
         const uint32_t r = page_row(p.pages, page_entry(p.pages, table, len), head0, len);
         new_page = r < kNoPage;
-        const uint4 x = store_load_source<F>(lane < 16 ? k_new : v_new, lane & 15);
+        const uint4 x = lane < 16 ? store_load_source<F>(s_q[kMaxGroup], lane) : value;
         store_put_row<F>(s_new.code[lane >> 4], s_new.scale[lane >> 4], lane & 15, x);
         if (new_page)
             store_put_row<F>(p.pages.data[lane >> 4] + (size_t)r * StoreFormat<F>::kRow,

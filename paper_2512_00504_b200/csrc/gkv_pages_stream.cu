@@ -167,88 +167,33 @@ __global__ void __launch_bounds__(32, stream_warps(F, TOGETHER)) gkv_pages_strea
     const int added = p.k_new ? 1 : 0;
 
     const int q = lane >> 2, j = lane & 3, h0 = 2 * j;
-    // Heads' rows are turned word by word (two elements), lane l those of words `word_a` and `word_b`: the two sides of two pairs each, or
-    // (neighbours, and behind the pairs) words l and l + 32 on their own. rot_dim / 2 odd: the sides of a pair are in other halves of their words, and
-    // single elements are turned.
-    const bool rotates = p.rotary.turns != nullptr;
-    const int half = p.rotary.half;
-    const bool words = p.rotary.interleaved || half % 2 == 0, sides = !p.rotary.interleaved && 2 * lane < half;
-    // (halves: words 0 .. half / 2 - 1 are first sides; the words behind the pairs go to the lanes that have none)
-    const int word_a = p.rotary.interleaved ? lane : sides ? lane : 2 * lane;
-    const int word_b = p.rotary.interleaved ? lane + 32 : sides ? lane + half / 2 : 2 * lane + 1;
-    // The two pairs and their frequencies, which stay the same.
-    const bool by_word = words && !p.rotary.interleaved;
-    const int pair_a = by_word ? (sides ? 2 * lane : half) : lane, pair_b = by_word ? (sides ? 2 * lane + 1 : half) : lane + 32;
-    const uint64_t turns_a = rotates && pair_a < half ? p.rotary.turns[pair_a] : 0, turns_b = rotates && pair_b < half ? p.rotary.turns[pair_b] : 0;
-    struct Angles { float2 a, b; };
-    auto angles = [&]() {
-        const int32_t pos = p.pos ? p.pos[at.seq] : added ? at.len : at.len - 1;
-        return Angles{rotary_cos_sin(turns_a, pos, p.rotary.factor, 1.f), rotary_cos_sin(turns_b, pos, p.rotary.factor, 1.f)};
-    };
-    auto first_of = [&](int i) { return i < half ? i : 2 * i; };             // (single elements: pair i, or what lies behind the pairs)
-    auto second_of = [&](int i) { return i < half ? i + half : 2 * i + 1; };
-    struct Two { uint32_t a, b; };
-    auto load_two = [&](const __nv_bfloat16* x) {          // 4 elements of a head
-        if (words) return Two{reinterpret_cast<const uint32_t*>(x)[word_a], reinterpret_cast<const uint32_t*>(x)[word_b]};
-        const uint16_t* e = reinterpret_cast<const uint16_t*>(x);
-        return Two{(uint32_t)e[first_of(lane)] | (uint32_t)e[second_of(lane)] << 16, (uint32_t)e[first_of(lane + 32)] | (uint32_t)e[second_of(lane + 32)] << 16};
-    };
-    auto neighbours = [&](uint32_t w, float2 cs, bool turns) {       // one pair in a word
-        const float2 r = rotary_turn(bf16_lo(w), bf16_hi(w), cs.x, cs.y);
-        return turns ? pack_bf16x2(r.x, r.y) : w;
-    };
-    auto turn_into = [&](__nv_bfloat16* y, Two x, const Angles& g) {
-        if (words && !p.rotary.interleaved) {
-            const float2 r = rotary_turn(bf16_lo(x.a), bf16_lo(x.b), g.a.x, g.a.y), t = rotary_turn(bf16_hi(x.a), bf16_hi(x.b), g.b.x, g.b.y);
-            reinterpret_cast<uint32_t*>(y)[word_a] = sides ? pack_bf16x2(r.x, t.x) : x.a;
-            reinterpret_cast<uint32_t*>(y)[word_b] = sides ? pack_bf16x2(r.y, t.y) : x.b;
-            return;
-        }
-        const uint32_t a = neighbours(x.a, g.a, lane < half), b = neighbours(x.b, g.b, lane + 32 < half);
-        if (words) {
-            reinterpret_cast<uint32_t*>(y)[word_a] = a;
-            reinterpret_cast<uint32_t*>(y)[word_b] = b;
-        } else {
-            uint16_t* e = reinterpret_cast<uint16_t*>(y);
-            e[first_of(lane)] = (uint16_t)a;
-            e[second_of(lane)] = (uint16_t)(a >> 16);
-            e[first_of(lane + 32)] = (uint16_t)b;
-            e[second_of(lane + 32)] = (uint16_t)(b >> 16);
-        }
-    };
-
+    const HeadTurn turn(p.rotary, lane);
     // A unit's heads: their elements, and the operand made of them.
     uint32_t qf[8][2];
     float f0 = 0.f, f1 = 0.f;
-    Two e[kMaxGroup];
+    HeadTurn::Words e[kMaxGroup];
+    auto position = [&]() { return p.pos ? p.pos[at.seq] : added ? at.len : at.len - 1; };
     auto load_heads = [&]() {
         const __nv_bfloat16* x = p.q + ((int64_t)at.seq * p.q_stride + (int64_t)at.head * p.g * kHeadDim);
-        if (rotates) {
 #pragma unroll
-            for (int h = 0; h < kMaxGroup; ++h)
-                if (h < p.g) e[h] = load_two(x + h * kHeadDim);
-        } else {
-#pragma unroll
-            for (int ks = 0; ks < 8; ++ks) load_query<F>(x + min(q, p.g - 1) * kHeadDim, ks, j, qf[ks][0], qf[ks][1]);
-        }
+        for (int h = 0; h < kMaxGroup; ++h)
+            if (h < p.g) e[h] = turn.load(x + h * kHeadDim);
     };
     auto make_heads = [&]() {
-        if (rotates) {
-            const Angles g = angles();
+        const HeadTurn::Angles g = turn.angles(position());
 #pragma unroll
-            for (int h4 = 0; h4 < kMaxGroup; h4 += 4)
-                if (h4 < p.g) {
+        for (int h4 = 0; h4 < kMaxGroup; h4 += 4)
+            if (h4 < p.g) {
 #pragma unroll
-                    for (int h = 0; h < 4; ++h)
-                        if (h4 + h < p.g) turn_into(sw.row[h], e[h4 + h], g);
-                    __syncwarp();
-                    const int mine = min(q, p.g - 1) - h4;
-                    if (mine >= 0 && mine < 4)
+                for (int h = 0; h < 4; ++h)
+                    if (h4 + h < p.g) turn.put(sw.row[h], e[h4 + h], g);
+                __syncwarp();
+                const int mine = min(q, p.g - 1) - h4;
+                if (mine >= 0 && mine < 4)
 #pragma unroll
-                        for (int ks = 0; ks < 8; ++ks) load_query<F>(sw.row[mine], ks, j, qf[ks][0], qf[ks][1]);
-                    __syncwarp();
-                }
-        }
+                    for (int ks = 0; ks < 8; ++ks) load_query<F>(sw.row[mine], ks, j, qf[ks][0], qf[ks][1]);
+                __syncwarp();
+            }
         f0 = f1 = p.scale_log2;
         scale_queries<F>(lane, qf, f0, f1);
     };
@@ -401,11 +346,9 @@ __global__ void __launch_bounds__(32, stream_warps(F, TOGETHER)) gkv_pages_strea
                 const int64_t new_row = (int64_t)at.seq * p.kv_stride + (int64_t)at.head * kHeadDim;
                 const __nv_bfloat16 *kn = p.k_new + new_row, *vn = p.v_new + new_row;
                 const int32_t e = page_entry(p.pages, p.pages.table + at.seq * p.pages.table_stride, at.len);
-                if (rotates) {
-                    turn_into(sw.row[0], load_two(kn), angles());
-                    __syncwarp();
-                    kn = sw.row[0];
-                }
+                turn.put(sw.row[0], turn.load(kn), turn.angles(position()));
+                __syncwarp();
+                kn = sw.row[0];
                 const uint4 x = store_load_source<F>(lane < 16 ? kn : vn, lane & 15);
                 const uint32_t to = page_row(p.pages, e, (uint32_t)at.head * p.pages.head_rows, at.len);
                 store_put_row<F>(reinterpret_cast<uint8_t*>(sw.row[2 + (lane >> 4)]), sw.scale[lane >> 4], lane & 15, x);
