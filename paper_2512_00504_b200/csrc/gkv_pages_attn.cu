@@ -197,20 +197,23 @@ __global__ void __launch_bounds__(kThreads, pages_ctas(F)) gkv_pages_attn_kernel
     const bool fits = append ? len < p.capacity : len <= p.capacity;
     const int old = fits ? len : 0, n = old + (fits && append ? 1 : 0);      // rows in the pages, rows to attend to
     const int tiles = (n + kTile - 1) / kTile;
-    const int t_begin = min(split * split_tiles, tiles);
-    const int t_end = split == splits - 1 ? tiles : min(t_begin + split_tiles, tiles);
+    const int cut = (tiles + splits - 1) / splits;       // pieces go by the length that the sequence has
+    const int t_begin = min(split * cut, tiles), t_end = min(t_begin + cut, tiles);
     const int own_tiles = t_end - t_begin;               // tile i of the piece is warp i % kWarps'
     const bool writes = append && fits && own_tiles > 0 && t_end == tiles;
 
     // ---- the first tiles set out. Tile s of this warp begins with key `key0` + s * kWarps * kTile.
     const uint32_t head0 = (uint32_t)head * p.pages.head_rows;
-    const int key0 = (t_begin + warp) * kTile;           // (the guess, wherever there is a tile)
+    const int key0 = (t_begin + warp) * kTile;
     const int mine = own_tiles > warp ? (own_tiles - warp + kWarps - 1) / kWarps : 0;
     const int last_old = min(old, t_end * kTile);        // (a piece's tiles are whole but for the unit's last)
     auto entry = [&](int s) {
         const int key = key0 + s * kStep + (lane & 15);
         return key < last_old ? page_entry(p.pages, table, key) : 0;
     };
+    if (cut != split_tiles)                              // (the guess went by the longest length)
+#pragma unroll
+        for (int s = 0; s <= S; ++s) e[s] = entry(s);
     auto row_of = [&](int32_t e, int s) {
         const int key = key0 + s * kStep + (lane & 15);
         return key < last_old ? page_row(p.pages, e, head0, key) : kNoRow;

@@ -483,15 +483,16 @@ __global__ void __launch_bounds__(32, stream_warps(F, TOGETHER)) gkv_pages_strea
 }
 
 // Joins the partial results of a unit: a running softmax over them, kJoin at a time, all of whose loads are under way before the first is
-// looked at. APART (few units, with many parts): 8 CTAs a unit, each with two dimensions of every lane's, its warps with a share of the parts
-// each; else one CTA a unit, whose warps have two dimensions each.
-template <int F, bool APART>
-__global__ void __launch_bounds__(256, APART ? 2 : 6) gkv_pages_stream_merge_kernel(const PagesAttnLaunch p, const int warps) {
-    constexpr int NG = value_groups(F), KEYS = StreamWarp<F>::kKeys, kJoin = APART ? 8 : 2;
+// looked at. 2^split CTAs a unit; a warp has two dimensions of every lane's, those of its CTA's 2^-split of all, and every 2^split-th of the parts.
+// kJoin = 8 takes 128 registers, two CTAs an SM, kJoin = 2 leaves room for five.
+template <int F, int kJoin>
+__global__ void __launch_bounds__(256, kJoin == 8 ? 2 : 5) gkv_pages_stream_merge_kernel(const PagesAttnLaunch p, const int warps, const int split) {
+    constexpr int NG = value_groups(F), KEYS = StreamWarp<F>::kKeys;
     __shared__ float4 s_o[8][32], s_mv[8][32];
     __shared__ float2 s_l[8][32];
-    const int unit = APART ? blockIdx.x >> 3 : blockIdx.x, seq = unit / p.h_kv, head = unit - seq * p.h_kv;
+    const int unit = blockIdx.x >> split, seq = unit / p.h_kv, head = unit - seq * p.h_kv;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int slices = 8 >> split, share = warp / slices;          // of a CTA; of the parts
     int64_t before;
     int kept[kKept];
     const int64_t all = stream_total<KEYS>(p, seq, lane, kept, &before);
@@ -500,13 +501,13 @@ __global__ void __launch_bounds__(256, APART ? 2 : 6) gkv_pages_stream_merge_ker
     const int64_t first = before + (int64_t)head * tiles;
     const int w0 = stream_owner(first, per), n = tiles ? stream_owner(first + tiles - 1, per) - w0 + 1 : 0;
     const size_t out = ((size_t)seq * p.h_q + (size_t)head * p.g) * kHeadDim;
-    const int slice = APART ? blockIdx.x & 7 : warp;       // the two dimensions
+    const int slice = (blockIdx.x & ((1 << split) - 1)) * slices + warp % slices;      // the two dimensions
     const int q = lane >> 2, h0 = 2 * (lane & 3), d = out_dim<F>(slice, q), dg = slice / (8 / NG);
     grid_wait_previous();                                  // (nobody leaves before: what comes next waits for this kernel alone)
     if (len < 0 || n == 1) return;                         // left out, or finished by the warp that had it
     if (n == 0) {
         const bool fits = p.k_new ? len < p.capacity : len <= p.capacity;
-        if (APART && warp != 0) return;
+        if (share != 0) return;
         const uint32_t x = fits ? 0u : 0x7fff7fffu;        // bf16 NaN
 #pragma unroll
         for (int h = 0; h < 2; ++h)
@@ -533,8 +534,8 @@ __global__ void __launch_bounds__(256, APART ? 2 : 6) gkv_pages_stream_merge_ker
         if (e0 != 0.f) { o.x = fmaf(x.x, e0, o.x); o.z = fmaf(x.z, e0, o.z); }
         if (e1 != 0.f) { o.y = fmaf(x.y, e1, o.y); o.w = fmaf(x.w, e1, o.w); }
     };
-    const int step = APART ? 8 : 1;
-    for (int i0 = APART ? warp : 0; i0 < n; i0 += kJoin * step) {
+    const int step = 1 << split;
+    for (int i0 = share; i0 < n; i0 += kJoin * step) {
         float2 am[kJoin], av[kJoin], al[kJoin];
         float4 x[kJoin];
 #pragma unroll
@@ -561,17 +562,18 @@ __global__ void __launch_bounds__(256, APART ? 2 : 6) gkv_pages_stream_merge_ker
 #pragma unroll
         for (int k = 0; k < kJoin; ++k) add(am[k], av[k], al[k], x[k]);
     }
-    if (APART) {                                           // the warps' shares
+    if (split > 0) {                                       // the shares of the same dimensions
         s_o[warp][lane] = o;
         s_mv[warp][lane] = make_float4(m.x, m.y, v.x, v.y);
         s_l[warp][lane] = l;
         __syncthreads();
-        if (warp != 0) return;
-        const int parts = min(n, 8);
-        for (int i = 1; i < parts; ++i) {
-            const float4 a = s_mv[i][lane];
+        if (share != 0) return;
+        const int shares = min(n, step);
+        for (int i = 1; i < shares; ++i) {
+            const int other = warp + i * slices;
+            const float4 a = s_mv[other][lane];
             raise(make_float2(a.x, a.y), make_float2(a.z, a.w));
-            add(make_float2(a.x, a.y), make_float2(a.z, a.w), s_l[i][lane], s_o[i][lane]);
+            add(make_float2(a.x, a.y), make_float2(a.z, a.w), s_l[other][lane], s_o[other][lane]);
         }
     }
     if (h0 < p.g)
@@ -597,9 +599,13 @@ static cudaError_t launch_stream(const PagesAttnLaunch& p, int ctas, cudaStream_
     e = cudaGetLastError();
     if (e != cudaSuccess) return e;
     const int units = p.batch * p.h_kv;
-    const bool apart = units <= 128;
+    // CTAs a unit, and warps that share its parts: few units have many parts, and all the CTAs fit the device at once (148 SMs).
+    int split = 0;
+    const bool many = units <= 2 * 148 / 8;
+    while (!many && split < 2 && (ctas >> split) > 2 * units && (units << (split + 1)) <= 5 * 148) ++split;
+    if (many) split = 3;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)units << (apart ? 3 : 0));
+    cfg.gridDim = dim3((unsigned)units << split);
     cfg.blockDim = dim3(256);
     cfg.stream = s;
     cudaLaunchAttribute attr[1];
@@ -607,7 +613,7 @@ static cudaError_t launch_stream(const PagesAttnLaunch& p, int ctas, cudaStream_
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, apart ? gkv_pages_stream_merge_kernel<F, true> : gkv_pages_stream_merge_kernel<F, false>, p, ctas);
+    return cudaLaunchKernelEx(&cfg, many ? gkv_pages_stream_merge_kernel<F, 8> : gkv_pages_stream_merge_kernel<F, 2>, p, ctas, split);
 }
 static bool rows_together(const PagesAttnLaunch& p) { return p.pages.token_rows == 1 && p.pages.page_size % kTile == 0; }
 int pages_stream_warps_per_sm(const PagesAttnLaunch& p, int format) { return stream_warps(format, rows_together(p)); }

@@ -669,9 +669,14 @@ __device__ __forceinline__ void finish_rows(const P& p, RunningRows<F>& r, RowsS
         __syncthreads();
         for (int i = split * kThreads + d; i < p.g * kHeadDim; i += p.splits * kThreads) {
             const int h = i / kHeadDim, g = NG > 1 ? i % kHeadDim / (kHeadDim / NG) : 0;
+            float part[kMaxCluster];                  // all under way at once
+#pragma unroll
+            for (int c = 0; c < kMaxCluster; ++c)
+                if (c < p.splits) part[c] = ld_cluster_f32(cluster_map_shared(smem_u32(&mine[i]), c));
             float x = 0.f;
-            for (int c = 0; c < p.splits; ++c)
-                x = fmaf(ld_cluster_f32(cluster_map_shared(smem_u32(&mine[i]), c)), sh.cl[c][g][h], x);
+#pragma unroll
+            for (int c = 0; c < kMaxCluster; ++c)
+                if (c < p.splits) x = fmaf(part[c], sh.cl[c][g][h], x);
             p.out[((size_t)seq * p.h_q + (size_t)head * p.g) * kHeadDim + i] =
                 __float2bfloat16_rn(final_value(x, sh.norm[0][h], sh.norm[1][h], sh.norm[2 + g][h], fits));
         }
