@@ -708,10 +708,11 @@ class PagedStore:
     fmt: "bf16", "e4m3", "int8" or "int4". The pages are allocated here (uninitialised) or given as buffers: (k, v, k_scale, v_scale),
     for bf16 (k, v), each [pages][h_kv][page_size][...] or, token_major, [pages][page_size][h_kv][...]. Every call takes the table of its
     sequences, int32 [batch][places] on the device: row r of sequence i is row r % page_size of page table[i][r // page_size]. Calls of
-    one store must not overlap on the GPU (they share the workspace). What has been allocated here may be dropped while streams still work on it
-    (given buffers and a call's tensors are the caller's to keep)."""
+    one store must not overlap on the GPU (they share the workspace); the stores of a model's layers may share one (workspace: another
+    store's, 22 MB) if theirs do not either. What has been allocated here may be dropped while streams still work on it (given buffers, a given
+    workspace and a call's tensors are the caller's to keep)."""
 
-    def __init__(self, fmt, *, pages, page_size, h_q, h_kv, max_batch, token_major=False, device=None, buffers=None):
+    def __init__(self, fmt, *, pages, page_size, h_q, h_kv, max_batch, token_major=False, device=None, buffers=None, workspace=None):
         import torch
         if fmt not in STORE_FORMATS:
             raise ValueError(f"format {fmt!r}: one of {sorted(STORE_FORMATS)} is needed")
@@ -743,10 +744,14 @@ class PagedStore:
         self.k_scale, self.v_scale = (buffers[2], buffers[3]) if scales else (None, None)
         if self.device.type != "cuda":
             raise ValueError(f"the buffers are on {self.device}")
-        self.workspace = torch.empty(ws_bytes, dtype=torch.uint8, device=self.device)
+        if workspace is not None and (workspace.dtype != torch.uint8 or workspace.device != self.device or not workspace.is_contiguous()
+                                      or workspace.numel() < ws_bytes):
+            raise ValueError(f"workspace: {ws_bytes} contiguous bytes (uint8) on {self.device} are needed")
+        self.workspace = torch.empty(ws_bytes, dtype=torch.uint8, device=self.device) if workspace is None else workspace
         self._call = _torch_binding()
         # what has been allocated here, and on which stream
-        self._held = (torch.cuda.current_stream(self.device).cuda_stream, self.device.index, self.workspace) + (() if given else tuple(buffers))
+        self._held = (torch.cuda.current_stream(self.device).cuda_stream, self.device.index) + (() if given else tuple(buffers)) + \
+            ((self.workspace,) if workspace is None else ())
         self._at = (ctypes.addressof(self.desc), self.device.index, max_batch)
         self._ws = (self.workspace.data_ptr(), self.workspace.numel())
 

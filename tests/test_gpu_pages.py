@@ -303,6 +303,78 @@ def test_work_spread_over_the_length(fmt, lens, h_q, h_kv):
 
 
 @pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("kind", [("halves", 20), ("halves", 6), ("halves", 96), ("neighbours", 44), ("neighbours", 2), ("halves", 126)])
+@pytest.mark.parametrize("lens", [[70, 0, 33], [6000, 17, 2100]])
+def test_parts_of_a_head(fmt, kind, lens):
+    """Every way in which words and single elements are turned, in the short form and the one of equal shares; at the rows' numbers."""
+    st, table, g = filled(fmt, 40, lens, 16, 7, 1)
+    q, k_new, v_new = randn(g, 3, 7, 128), randn(g, 3, 1, 128), randn(g, 3, 1, 128)
+    rot = rotary(kind)
+    out, lse = run(st, table, lens, q, k_new, v_new, rot)
+    at = ints(lens)[:, None]
+    for (codes, scale), (wc, ws) in zip(stored(st), [expect_codes(turned(rot, at, k_new[:, None])[:, 0], fmt), expect_codes(v_new, fmt)]):
+        for b, n in enumerate(lens):
+            p, s = table[b, n // 16], n % 16
+            assert (codes[p, s] == wc[b]).all() and (scale is None or (scale[p, s] == ws[b]).all())
+    eo, el, to, tl = expect(st, table, lens, turned(rot, at, q[:, None])[:, 0], [n + 1 for n in lens])
+    close(f64(out), eo, to)
+    close(f64(lse), el, tl)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("page,token_major,h_kv", [(16, False, 2), (32, False, 1), (48, False, 2), (64, True, 2), (1, False, 1), (7, True, 2)])
+@pytest.mark.parametrize("append", [False, True])
+def test_equal_shares(fmt, page, token_major, h_kv, append):
+    """Long calls: units that several warps share, that one has to itself and that have no rows; ends of a page, a tile, a step and a share; left out,
+    empty and unfitting sequences among them; everything behind the ends NaN."""
+    lens = [4095, -1, 0, 1, 31, 32, 33, 2047, 2 ** 31 - 1, 900, 16, 4096, 15, 5000]
+    have = [n if n < 10000 else 0 for n in lens]
+    st, table, g = filled(fmt, 41, have, page, 4 * h_kv, h_kv, token_major)
+    B = len(lens)
+    qkv = randn(g, B, 6 * h_kv, 128)
+    q, k_new, v_new = qkv[:, :4 * h_kv], qkv[:, 4 * h_kv:5 * h_kv], qkv[:, 5 * h_kv:]
+    before = stored(st)
+    out, lse = run(st, table, lens, q, k_new if append else None, v_new if append else None)
+    written = np.zeros((st.pages, page), bool)
+    want = [expect_codes(x.contiguous(), fmt) for x in (k_new, v_new)]
+    after = stored(st)
+    for b, n in enumerate(lens):
+        if append and 0 <= n < 10000:
+            p, s = table[b, n // page], n % page
+            written[p, s] = True
+            for (codes, scale), (wc, ws) in zip(after, want):
+                assert (codes[p, s] == wc[b]).all() and (scale is None or (scale[p, s] == ws[b]).all())
+    for (c0, s0), (c1, s1) in zip(before, after):
+        assert (c0[~written] == c1[~written]).all() and (s0 is None or np.array_equal(s0[~written], s1[~written], equal_nan=True))
+    eo, el, to, tl = expect(st, table, lens, q, [n + append if 0 <= n < 10000 else 0 for n in lens])
+    for b, n in enumerate(lens):
+        if n < 0:
+            assert (out[b] == 9).all() and (lse[b] == 9).all()
+        elif n > 10000:
+            assert torch.isnan(out[b]).all() and torch.isnan(lse[b]).all()
+        else:
+            close(f64(out[b]), eo[b], to[b])
+            close(f64(lse[b]), el[b], tl[b])
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("batch,h_kv,longest", [(200, 8, 200), (1100, 1, 130), (2049, 1, 300), (40, 4, 1500), (300, 8, 500)])
+def test_many_sequences(fmt, batch, h_kv, longest):
+    """More sequences than a warp keeps lengths of, than the merge is made for, and units far more than warps; the results of a few."""
+    rng = np.random.RandomState(batch)
+    lens = rng.randint(0, longest + 1, batch)
+    lens[rng.randint(batch)] = longest
+    st, table, g = filled(fmt, 42, lens.tolist(), 16, 2 * h_kv, h_kv)
+    q, k_new, v_new = randn(g, batch, 2 * h_kv, 128), randn(g, batch, h_kv, 128), randn(g, batch, h_kv, 128)
+    out, lse = run(st, table, lens, q, k_new, v_new, max_len=longest)
+    picked = sorted({0, 31, 32, 127, 128, batch // 2, batch - 1} & set(range(batch)))
+    eo, el, to, tl = expect(st, table[picked], None, q[picked], [lens[b] + 1 for b in picked])
+    close(f64(out[picked]), eo, to)
+    close(f64(lse[picked]), el, tl)
+    assert torch.isfinite(out).all() and torch.isfinite(lse).all()
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
 def test_a_table_far_wider_than_the_lengths(fmt):
     """As in a captured step that leaves max_len to the table: most CTAs have nothing to do."""
     lens = [40, 0, 1000]
@@ -520,6 +592,41 @@ def test_a_captured_step_replayed_while_lengths_and_tables_grow():
     assert torch.equal(st.k.view(torch.uint8)[table[table >= 0].long()][:, :, 0], two.k.view(torch.uint8)[table[table >= 0].long()][:, :, 0])
 
 
+@pytest.mark.parametrize("fmt", ["bf16", "int4"])
+def test_long_captured_steps_that_share_a_workspace(fmt):
+    """Two stores, each with a captured long step, in one workspace: replayed in turn while their lengths change, from a few rows to many."""
+    B, h_q, h_kv = 2, 8, 2
+    rot = rotary(("halves", 128))
+    g = gen(50)
+    stores, graphs, calls = [], [], []
+    for i in range(2):
+        st, table, _ = filled(fmt, 51 + i, [5000, 5000], 16, h_q, h_kv)
+        if i:
+            st = gkv.PagedStore(fmt, pages=st.pages, page_size=16, h_q=h_q, h_kv=h_kv, max_batch=B, buffers=[t for t in (st.k, st.v, st.k_scale, st.v_scale) if t is not None],
+                                workspace=stores[0].workspace)
+            assert st.workspace is stores[0].workspace
+        stores.append(st)
+        q, k1, v1, length = randn(g, B, h_q, 128), randn(g, B, h_kv, 128), randn(g, B, h_kv, 128), ints([5000, 4000])
+        out, lse, tab = torch.zeros_like(q), torch.zeros(B, h_q, device=DEV), ints(table)
+        st.attn(tab, length, q, out, k_new=k1, v_new=v1, rotary=rot, lse=lse)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            st.attn(tab, length, q, out, k_new=k1, v_new=v1, rotary=rot, lse=lse)
+        graphs.append(graph)
+        calls.append((tab, length, q, out, k1, v1, lse, table))
+    for lens in ([4999, 20], [0, 0], [1, 4096], [-1, 3000], [300, 4000]):
+        for st, graph, (tab, length, q, out, k1, v1, lse, table) in zip(stores, graphs, calls):
+            length.copy_(ints(lens))
+            q.copy_(randn(g, B, h_q, 128))
+            graph.replay()
+            at = length[:, None]
+            eo, el, to, tl = expect(st, table, lens, turned(rot, at, q[:, None])[:, 0], [n + 1 for n in lens])
+            for b, n in enumerate(lens):
+                if n >= 0:
+                    close(f64(out[b]), eo[b], to[b])
+                    close(f64(lse[b]), el[b], tl[b])
+
+
 def test_two_stores_on_two_streams():
     g = gen(32)
     made = [filled("bf16", 33 + i, [3000, 20, 700], 16, 8, 2) for i in range(2)]
@@ -557,6 +664,9 @@ def test_tensors_that_are_refused():
                                                                torch.zeros(3, 4, 128, dtype=torch.bfloat16, device=DEV)), {})):
         with pytest.raises(ValueError):
             st.attn(*args, **kw)
+    for ws in (torch.zeros(100, dtype=torch.uint8, device=DEV), st.workspace[::2], st.workspace.cpu(), st.workspace.to(torch.int8)):
+        with pytest.raises(ValueError):
+            gkv.PagedStore("bf16", pages=4, page_size=16, h_q=4, h_kv=2, max_batch=2, buffers=(st.k, st.v), workspace=ws)
     for args, kw in (((tab, n, q, out), dict(k_new=k1)), ((tab, n, q, out), dict(v_new=k1)), ((tab, n, q, out), dict(max_len=33)), ((tab, n, q, out), dict(max_len=-1)),
                      ((tab[:, :0], n, q, out), {})):
         with pytest.raises(gkv.GKVError):
