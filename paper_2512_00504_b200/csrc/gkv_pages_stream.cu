@@ -1,21 +1,28 @@
 // Decode attention over a cache in pages, for more work than a few clusters: every warp of a grid that fills the device takes an equal
-// share of all tiles.
+// share of all steps.
 //
-// The units (sequence, KV head) lie one after the other, each as many 16-key tiles long as its sequence, and warp w of W takes tiles
+// The units (sequence, KV head) lie one after the other, each as many steps of 16 or 32 keys long as its sequence, and warp w of W takes steps
 // w * per .. (w + 1) * per - 1 of that line, per = ceil(all / W): it may begin and end inside a unit and pass through several. Whatever the lengths are,
-// all warps have the same work, none waits for another, and the stream of rows from HBM does not stop at the end of a unit. A unit that one
-// warp has to itself is finished by it; of the others (a warp's first or last one) it leaves a partial result, and the merge joins them.
+// all warps have the same work, none waits for another, and the stream of rows from HBM does not stop at the end of a unit. A warp is a CTA, so
+// that an SM's registers and shared memory hold as many as they can. A unit that one warp has to itself is finished by it; of the others (a warp's
+// first or last one) it leaves a partial result, and the merge joins them. (Handing out smaller shares as warps become free, to make up for the
+// parts of the device that are up to 15% slower: 196 to 214 us instead of 193 in the first case below, since there is more to merge.)
 //
 // Rows come by bulk copies into a ring of the warp's own, completed on a barrier of its own: with pages whose size is a multiple of the tile and
 // that hold a head's rows together, one copy for a tile of K, one for each group of rows of V (four, with 8 bits eight, with 4 bits all), and
-// two for their scales; with any others, one for each bf16 row, and 16 bytes a lane at a time for shorter ones (a copy of its own for each takes
-// 13 cycles: 128 x 8 heads of about 2200 keys in 8 bits in pages of 5 rows 216 us instead of REPLACE). (By cp.async, 16 bytes a lane, a tile costs the warp 100 more instructions: 128
-// sequences x 8 heads of about 2200 keys in bf16 225 us, 2 x 8 of up to 131071 in 4 bits 108.) Which key is which row of the products is
-// free as long as the two agree, and chosen such that lanes that read V at once find their rows at banks of their own (4 bits: of two), groups
+// two for their scales, all issued by one lane; with any others, one for each bf16 row, and 16 bytes a lane at a time for shorter ones (a copy
+// of its own for each takes 13 cycles: in pages of 5 rows in 8 bits 216 us instead of 156. By cp.async where rows lie together, 16 bytes a lane, a
+// tile costs the warp 100 more instructions: in bf16 225 us, 131071 keys in 4 bits 108). Which key is which row of the products is free
+// as long as the two agree, and chosen such that lanes that read V at once find their rows at banks of their own (4 bits: of two), groups
 // being 32 bytes further apart than the rows.
 //
 // Products and softmax are those of the attention over a store (gkv_store_rows.cuh). A row that lies on no page makes its unit NaN.
 // A wait that runs out (never, but every wait ends) makes the warp's units NaN, too.
+//
+// Measured (with the merge; the time that the rows' bytes take at 6.46 TB/s): 128 sequences x 8 heads of about 2200 keys in bf16 in pages of 64
+// 188 to 193 us (177), of 16 190 to 194, of 5 197 to 199; in 8 bits in pages of 64 112 (92), of 5 156; in 4 bits 110 (51) and 170. 16 x 4 heads of 300
+// to 65535 keys in bf16 217 to 219 (206). 2 x 8 heads of up to 131071 in 4 bits 89 (42). 16-bit rows are bound by HBM. With 4-bit rows the warps
+// issue in 61% of all cycles, 480 instructions a tile, of which 170 unpack codes: instructions and what they wait for bound it.
 #include "gkv_pages.cuh"
 #include "gkv_rotary.cuh"
 #include "gkv_store_rows.cuh"
