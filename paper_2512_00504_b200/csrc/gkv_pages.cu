@@ -24,6 +24,7 @@ namespace gkv {
 
 constexpr int kPageCopyThreads = 128;
 constexpr int kPageCopyItems = kPageCopyThreads / 16;
+constexpr int64_t kFewRows = 16384;
 
 // The 8 elements of a row that lane l has, neighbours or those of format F. These loads stay where they are written: all of them ahead of
 // what they are to overlap with. (Left to the compiler, they were put off to the rows' turn where registers were short: an append of
@@ -45,7 +46,8 @@ __device__ __forceinline__ uint4 load_row(const __nv_bfloat16* row, int l, bool 
 // any others.
 enum { kStraight = 0, kNeighbours = 1, kLanes = 2, kAny = 3 };
 
-// cos and sin of what a lane has of a token: of the pairs of its 8 elements, or (neighbours) of its 4 pairs.
+// cos and sin of what a lane has of a token: of the pairs of its 8 elements, sin negated where it has the first sides, or (neighbours) of its 4
+// pairs.
 template <int OP>
 struct LaneTurn {
     static constexpr int N = OP == kNeighbours ? 1 : 2;
@@ -56,28 +58,34 @@ struct LaneTurn {
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 c[i] = reinterpret_cast<const float4*>(cos + at)[i];
-                s[i] = reinterpret_cast<const float4*>(sin + at)[i];
+                const float4 x = reinterpret_cast<const float4*>(sin + at)[i];
+                s[i] = OP == kLanes && 8 * l < half ? make_float4(-x.x, -x.y, -x.z, -x.w) : x;
             }
     }
 };
-// A lane's 8 elements of a row, turned: x c + y s with y the other sides of their pairs, negated where x is the first side, and both products
-// in the order of rotary_turn.
+// A lane's 8 elements of a row, turned: x c + y s with y the other sides of their pairs, the products in the order of rotary_turn.
 template <int OP>
 __device__ __forceinline__ uint4 turn_lane(const LaneTurn<OP>& r, uint4 v, int l, int half) {
     const uint32_t x[4] = {v.x, v.y, v.z, v.w};
-    const bool first = 8 * l < half;
-    const int from = first ? l + half / 8 : l - half / 8;
-    const uint32_t minus = OP == kNeighbours ? 0x00008000u : first ? 0x80008000u : 0u;
+    const int from = 8 * l < half ? l + half / 8 : l - half / 8;
     uint32_t y[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const uint32_t o = (OP == kNeighbours ? __byte_perm(x[i], 0u, 0x1032) : __shfl_sync(0xffffffffu, x[i], from, 16)) ^ minus;
-        const float4 c4 = r.c[OP == kNeighbours ? 0 : i >> 1], s4 = r.s[OP == kNeighbours ? 0 : i >> 1];
-        auto pick = [](const float4& f, int k) { return k == 0 ? f.x : k == 1 ? f.y : k == 2 ? f.z : f.w; };
-        const int ka = OP == kNeighbours ? i : 2 * (i & 1), kb = OP == kNeighbours ? i : ka + 1;
-        y[i] = pack_bf16x2(__fmaf_rn(bf16_lo(x[i]), pick(c4, ka), __fmul_rn(bf16_lo(o), pick(s4, ka))),
-                           __fmaf_rn(bf16_hi(x[i]), pick(c4, kb), __fmul_rn(bf16_hi(o), pick(s4, kb))));
+        const float2 a = make_float2(bf16_lo(x[i]), bf16_hi(x[i]));
+        float2 t;
+        if constexpr (OP == kNeighbours) {
+            const float c = i == 0 ? r.c[0].x : i == 1 ? r.c[0].y : i == 2 ? r.c[0].z : r.c[0].w;
+            const float s = i == 0 ? r.s[0].x : i == 1 ? r.s[0].y : i == 2 ? r.s[0].z : r.s[0].w;
+            t = fma2(a, make_float2(c, c), mul2(make_float2(-a.y, a.x), make_float2(s, s)));
+        } else {
+            const uint32_t o = __shfl_sync(0xffffffffu, x[i], from, 16);
+            const float4 c4 = r.c[i >> 1], s4 = r.s[i >> 1];
+            const float2 c = i & 1 ? make_float2(c4.z, c4.w) : make_float2(c4.x, c4.y), s = i & 1 ? make_float2(s4.z, s4.w) : make_float2(s4.x, s4.y);
+            t = fma2(a, c, mul2(make_float2(bf16_lo(o), bf16_hi(o)), s));
+        }
+        y[i] = pack_bf16x2(t.x, t.y);
     }
+    if (half == 64) return make_uint4(y[0], y[1], y[2], y[3]);
     return 8 * l < 2 * half ? make_uint4(y[0], y[1], y[2], y[3]) : v;
 }
 // The same element by element, for any rot_dim and either order of pairs, with cos and sin from shared memory.
@@ -116,18 +124,20 @@ __device__ __forceinline__ uint4 as_format(uint4 v, int l) {
 }
 
 // CTA: K or V, heads_per_cta heads, 8 * tokens_per_half tokens of sequence blockIdx.y. Half warp w: tokens_per_half tokens from w *
-// tokens_per_half on, all those heads of each (at most kRun rows).
-template <int F, int OP>
+// tokens_per_half on, all those heads of each (at most R rows).
+template <int F, int OP, int R, int H>
 __global__ void __launch_bounds__(kPageCopyThreads) gkv_pages_append_kernel(const PagesCopyLaunch p) {
     using Fm = StoreFormat<F>;
+    constexpr int kLanesOfRow = 16 / R;                  // that have its scales
     extern __shared__ __align__(16) float s_table[];     // cos and sin of the CTA's tokens: [token][half] each
-    __shared__ uint32_t s_row[kPageCopyItems * kRun];    // [token]: number of head 0's row
-    __shared__ uint2 s_scale[kPageCopyItems * kRun];     // [head][token]
+    __shared__ uint32_t s_row[kPageCopyItems * R];    // [token]: number of head 0's row
+    __shared__ uint2 s_scale[kPageCopyItems * R];     // [head][token]
+    const int heads_per_cta = H ? H : p.heads_per_cta, tokens_per_half = H ? R / H : p.tokens_per_half;
     const int b = blockIdx.y, l = threadIdx.x & 15, w = threadIdx.x >> 4;
     const bool is_v = blockIdx.x & 1;
     const int block = blockIdx.x >> 1, head_block = block % p.head_blocks;
-    const int tokens = kPageCopyItems * p.tokens_per_half, t0 = block / p.head_blocks * tokens;
-    const int head0 = head_block * p.heads_per_cta, heads = min(p.heads_per_cta, p.h_kv - head0);
+    const int tokens = kPageCopyItems * tokens_per_half, t0 = block / p.head_blocks * tokens;
+    const int head0 = head_block * heads_per_cta, heads = H ? H : min(heads_per_cta, p.h_kv - head0);
     const int half = p.rotary.half;
     const bool turns = OP != kStraight && !is_v;
     // This thread's pairs are those of its number and, blockDim by blockDim, on through the tokens: where a token's pairs divide the threads
@@ -142,26 +152,26 @@ __global__ void __launch_bounds__(kPageCopyThreads) gkv_pages_append_kernel(cons
     const int32_t first = p.first ? p.first[b] : 0, count = p.count ? p.count[b] : p.n_tokens;
     const int n = min(count, p.n_tokens);
     if (t0 >= n) return;
-    const int t_half = t0 + w * p.tokens_per_half;       // the half warp's first token
+    const int t_half = t0 + w * tokens_per_half;       // the half warp's first token
 
     // lane l's token of the half warp, as far as there is one, and what the table has for its row
     const int mine = t_half + l;
     const RunRows one = run_rows(first, n, p.n_tokens, p.capacity, mine);
-    const bool there = l < p.tokens_per_half && mine < n && one.lo == 0 && one.hi > 0;
+    const bool there = l < tokens_per_half && mine < n && one.lo == 0 && one.hi > 0;
     const int32_t entry = there ? page_entry(p.pages, p.pages.table + b * p.pages.table_stride, first + mine) : 0;
     // Row k is head k % heads_per_cta of token k / heads_per_cta.
-    const int rows = p.tokens_per_half * p.heads_per_cta;
+    const int rows = tokens_per_half * heads_per_cta;
     const __nv_bfloat16* const x = (is_v ? p.x[1] : p.x[0]) + ((int64_t)b * p.seq_stride + (int64_t)t_half * p.token_stride + (int64_t)head0 * p.head_stride);
-    const int64_t next_token = p.token_stride - (p.heads_per_cta - 1) * p.head_stride;
-    uint4 v[kRun];
+    const int64_t next_token = p.token_stride - (heads_per_cta - 1) * p.head_stride;
+    uint4 v[R];
     {
         const __nv_bfloat16* src = x;
         int t = t_half, h = 0;
 #pragma unroll
-        for (int k = 0; k < kRun; ++k) {
+        for (int k = 0; k < R; ++k) {
             v[k] = make_uint4(0u, 0u, 0u, 0u);
             if (k < rows && h < heads && t < n) v[k] = load_row<F>(src, l, turns);
-            if (++h == p.heads_per_cta) { h = 0; ++t; src += next_token; }
+            if (++h == heads_per_cta) { h = 0; ++t; src += next_token; }
             else src += p.head_stride;
         }
     }
@@ -184,37 +194,37 @@ __global__ void __launch_bounds__(kPageCopyThreads) gkv_pages_append_kernel(cons
             }
         }
         __syncthreads();
-        int k0 = w * p.tokens_per_half, h = 0;           // token within the CTA, head
+        int k0 = w * tokens_per_half, h = 0;           // token within the CTA, head
         if constexpr (OP == kAny) {
             const __nv_bfloat16* src = x;
 #pragma unroll
-            for (int k = 0; k < kRun; ++k) {
+            for (int k = 0; k < R; ++k) {
                 if (k < rows)
                     v[k] = as_format<F>(turn_any(v[k], l, p.rotary, h < heads && t0 + k0 < n ? src : nullptr, s_table + k0 * half, s_sin + k0 * half), l);
-                if (++h == p.heads_per_cta) { h = 0; ++k0; src += next_token; }
+                if (++h == heads_per_cta) { h = 0; ++k0; src += next_token; }
                 else src += p.head_stride;
             }
         } else {
             LaneTurn<OP> r;
 #pragma unroll
-            for (int k = 0; k < kRun; ++k) {
+            for (int k = 0; k < R; ++k) {
                 if (k < rows) {
                     if (h == 0) r.load(l, half, s_table + k0 * half, s_sin + k0 * half);
                     v[k] = as_format<F>(turn_lane<OP>(r, v[k], l, half), l);
                 }
-                if (++h == p.heads_per_cta) { h = 0; ++k0; }
+                if (++h == heads_per_cta) { h = 0; ++k0; }
             }
         }
     }
 
     uint8_t* data = is_v ? p.pages.data[1] : p.pages.data[0];
-    if (Fm::kScales != 0 && l < p.tokens_per_half) s_row[w * p.tokens_per_half + l] = row;
+    if (Fm::kScales != 0 && l < tokens_per_half) s_row[w * tokens_per_half + l] = row;
     float inv0 = 1.f, inv1 = 1.f;
     if (Fm::kScales != 0) {
-        const uint32_t sc = store_run_scales<F>(v, l, &inv0, &inv1);       // lanes 2k, 2k + 1: row k's
-        const int k = l >> 1, i = k / p.heads_per_cta, h = k - i * p.heads_per_cta;
-        if (k < rows && (F == GKV_STORE_INT4 || (l & 1) == 0))
-            reinterpret_cast<uint32_t*>(s_scale + h * tokens + w * p.tokens_per_half + i)[F == GKV_STORE_INT4 ? l & 1 : 0] = sc;
+        const uint32_t sc = store_run_scales<F>(v, l, &inv0, &inv1);
+        const int k = l / kLanesOfRow, i = k / heads_per_cta, h = k - i * heads_per_cta;
+        if (k < rows && l % kLanesOfRow < (F == GKV_STORE_INT4 ? 2 : 1))
+            reinterpret_cast<uint32_t*>(s_scale + h * tokens + w * tokens_per_half + i)[F == GKV_STORE_INT4 ? l & 1 : 0] = sc;
     }
     {
         const size_t head_bytes = (size_t)p.pages.head_rows * Fm::kRow;
@@ -222,14 +232,14 @@ __global__ void __launch_bounds__(kPageCopyThreads) gkv_pages_append_kernel(cons
         uint8_t* dst = data + (size_t)at * Fm::kRow;
         int i = 0, h = 0;
 #pragma unroll
-        for (int k = 0; k < kRun; ++k) {
-            const int from = 2 * k + (F == GKV_STORE_INT4 ? l & 1 : 0);
+        for (int k = 0; k < R; ++k) {
+            const int from = k * kLanesOfRow + (F == GKV_STORE_INT4 ? l & 1 : 0);
             float f0 = 1.f, f1 = 1.f;
             if (Fm::kScales != 0) f0 = f1 = __shfl_sync(0xffffffffu, inv0, from, 16);
             if (F == GKV_STORE_INT4) f1 = __shfl_sync(0xffffffffu, inv1, from, 16);
             if (k < rows && h < heads && at < kNoPage) store_put_codes<F>(dst, l, store_codes<F>(v[k], f0, f1));
             dst += head_bytes;
-            if (++h == p.heads_per_cta) {
+            if (++h == heads_per_cta) {
                 h = 0;
                 at = __shfl_sync(0xffffffffu, row, ++i, 16);
                 dst = data + (size_t)at * Fm::kRow;
@@ -292,21 +302,31 @@ __global__ void __launch_bounds__(kPageCopyThreads) gkv_pages_read_kernel(const 
     }
 }
 
-template <int OP>
-static cudaError_t launch_append(PagesCopyLaunch p, cudaStream_t s) {
-    p.head_blocks = (p.h_kv + kRun - 1) / kRun;
-    p.heads_per_cta = (p.h_kv + p.head_blocks - 1) / p.head_blocks;
-    p.tokens_per_half = kRun / p.heads_per_cta;
+template <int OP, int R, int H>
+static cudaError_t launch_append_rows(const PagesCopyLaunch& p, cudaStream_t s) {
     const int tokens = kPageCopyItems * p.tokens_per_half;
     const dim3 grid((unsigned)((p.n_tokens + tokens - 1) / tokens) * p.head_blocks * 2, (unsigned)p.batch);
     const size_t smem = OP != kStraight ? (size_t)tokens * p.rotary.half * 2 * sizeof(float) : 0;
     switch (p.format) {
-        case GKV_STORE_BF16: gkv_pages_append_kernel<GKV_STORE_BF16, OP><<<grid, kPageCopyThreads, smem, s>>>(p); break;
-        case GKV_STORE_E4M3: gkv_pages_append_kernel<GKV_STORE_E4M3, OP><<<grid, kPageCopyThreads, smem, s>>>(p); break;
-        case GKV_STORE_INT8: gkv_pages_append_kernel<GKV_STORE_INT8, OP><<<grid, kPageCopyThreads, smem, s>>>(p); break;
-        default:             gkv_pages_append_kernel<GKV_STORE_INT4, OP><<<grid, kPageCopyThreads, smem, s>>>(p); break;
+        case GKV_STORE_BF16: gkv_pages_append_kernel<GKV_STORE_BF16, OP, R, H><<<grid, kPageCopyThreads, smem, s>>>(p); break;
+        case GKV_STORE_E4M3: gkv_pages_append_kernel<GKV_STORE_E4M3, OP, R, H><<<grid, kPageCopyThreads, smem, s>>>(p); break;
+        case GKV_STORE_INT8: gkv_pages_append_kernel<GKV_STORE_INT8, OP, R, H><<<grid, kPageCopyThreads, smem, s>>>(p); break;
+        default:             gkv_pages_append_kernel<GKV_STORE_INT4, OP, R, H><<<grid, kPageCopyThreads, smem, s>>>(p); break;
     }
     return cudaGetLastError();
+}
+template <int OP>
+static cudaError_t launch_append(PagesCopyLaunch p, cudaStream_t s) {
+    const int rows = (int64_t)p.batch * p.n_tokens * p.h_kv <= kFewRows ? 2 : kRun;
+    p.head_blocks = (p.h_kv + rows - 1) / rows;
+    p.heads_per_cta = (p.h_kv + p.head_blocks - 1) / p.head_blocks;
+    p.tokens_per_half = rows / p.heads_per_cta;
+    if (rows == 2) return launch_append_rows<OP, 2, 0>(p, s);
+    if (OP != kAny && p.heads_per_cta * p.head_blocks == p.h_kv) {
+        if (p.heads_per_cta == 8) return launch_append_rows<OP, kRun, 8>(p, s);
+        if (p.heads_per_cta == 4) return launch_append_rows<OP, kRun, 4>(p, s);
+    }
+    return launch_append_rows<OP, kRun, 0>(p, s);
 }
 cudaError_t launch_pages_append(const PagesCopyLaunch& p, cudaStream_t s) {
     if (!p.rotary.turns) return launch_append<kStraight>(p, s);

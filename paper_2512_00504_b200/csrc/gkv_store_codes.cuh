@@ -74,8 +74,10 @@ __device__ __forceinline__ uint32_t int_scale(uint32_t a, float one_over_levels,
 // least 2^-10 away from half-way, and x * (1 / s) is within 2^-16 of the quotient. Adding 1.5 * 2^10 rounds it to a multiple of
 // 2^-13, which puts the half-way cases exactly on half-way and moves none of the others across; going on to 1.5 * 2^23 rounds
 // that to a whole number.
-__device__ __forceinline__ uint32_t round_quotient(float x, float inv, float add) {
-    return __float_as_uint(__fadd_rn(__fmaf_rn(x, inv, 1536.f), 12582912.f - 1536.f + add));
+__device__ __forceinline__ uint2 round_quotients(float2 x, float inv, float add) {
+    const float up = 12582912.f - 1536.f + add;
+    const float2 r = add2(fma2(x, make_float2(inv, inv), make_float2(1536.f, 1536.f)), make_float2(up, up));
+    return make_uint2(__float_as_uint(r.x), __float_as_uint(r.y));
 }
 
 __device__ __forceinline__ uint32_t e4m3_pack4(float a, float b, float c, float d) {
@@ -90,15 +92,20 @@ __device__ __forceinline__ uint32_t e4m3x2_to_f16x2(uint16_t x) {
     return d;
 }
 
+// Of two pairs of bf16 numbers the larger magnitudes, with some sign; NaN if one of them is.
+__device__ __forceinline__ uint32_t bf16_larger(uint32_t a, uint32_t b) {
+    uint32_t d;
+    asm("max.NaN.xorsign.abs.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
 // The largest magnitudes among a lane's 8 elements, two 16-bit numbers still to be reduced: in 4 bits those of groups 2p (low)
 // and 2p + 1 over the lanes of the same p, else two of the row over all lanes.
 template <int F>
 __device__ __forceinline__ uint32_t store_lane_max(uint4 x) {
-    const uint32_t m = 0x7fff7fffu;
-    const uint32_t a = __vmaxu2(x.x & m, x.y & m), b = __vmaxu2(x.z & m, x.w & m);
+    const uint32_t m = 0x7fff7fffu, a = bf16_larger(x.x, x.y), b = bf16_larger(x.z, x.w);
     if (F == GKV_STORE_INT4)   // low: groups 2p of both halves, high: 2p + 1
-        return __vmaxu2(__byte_perm(a, b, 0x5410), __byte_perm(a, b, 0x7632));
-    return __vmaxu2(a, b);
+        return bf16_larger(__byte_perm(a, b, 0x5410), __byte_perm(a, b, 0x7632)) & m;
+    return bf16_larger(a, b) & m;
 }
 // bf16 bits of the scale(s) for reduced maxima (both groups' in 4 bits), and the factors of the lane's first and last 4 elements.
 template <int F>
@@ -116,15 +123,22 @@ __device__ __forceinline__ uint32_t store_scale(uint32_t a, float* inv0, float* 
 template <int F>
 __device__ __forceinline__ uint4 store_codes(uint4 x, float inv0, float inv1) {
     if constexpr (F == GKV_STORE_BF16) return x;
-    const float v[8] = {bf16_lo(x.x), bf16_hi(x.x), bf16_lo(x.y), bf16_hi(x.y), bf16_lo(x.z), bf16_hi(x.z), bf16_lo(x.w), bf16_hi(x.w)};
+    const float2 v[4] = {{bf16_lo(x.x), bf16_hi(x.x)}, {bf16_lo(x.y), bf16_hi(x.y)}, {bf16_lo(x.z), bf16_hi(x.z)}, {bf16_lo(x.w), bf16_hi(x.w)}};
     uint4 c = make_uint4(0u, 0u, 0u, 0u);
     if constexpr (F == GKV_STORE_E4M3) {
-        c.x = e4m3_pack4(v[0] * inv0, v[1] * inv0, v[2] * inv0, v[3] * inv0);
-        c.y = e4m3_pack4(v[4] * inv0, v[5] * inv0, v[6] * inv0, v[7] * inv0);
+        float2 y[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i] = mul2(v[i], make_float2(inv0, inv0));
+        c.x = e4m3_pack4(y[0].x, y[0].y, y[1].x, y[1].y);
+        c.y = e4m3_pack4(y[2].x, y[2].y, y[3].x, y[3].y);
     } else {
         uint32_t b[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) b[i] = round_quotient(v[i], i < 4 ? inv0 : inv1, F == GKV_STORE_INT4 ? 8.f : 0.f);
+        for (int i = 0; i < 4; ++i) {
+            const uint2 r = round_quotients(v[i], i < 2 ? inv0 : inv1, F == GKV_STORE_INT4 ? 8.f : 0.f);
+            b[2 * i] = r.x;
+            b[2 * i + 1] = r.y;
+        }
         if constexpr (F == GKV_STORE_INT4) {   // the low 20 bits of the numbers are the codes alone
 #pragma unroll
             for (int i = 0; i < 4; ++i) b[i] = b[2 * i] + (b[2 * i + 1] << 4);
@@ -156,20 +170,21 @@ __device__ __forceinline__ void store_put_row(uint8_t* row, __nv_bfloat16* scale
     store_put_codes<F>(row, l, store_codes<F>(x, inv0, inv1));
 }
 
-// Scales of a run of kRun rows (half a warp, lane l of 16 with 8 elements of each): what store_scale gives for token l >> 1, in 4 bits
-// for groups 2j and 2j + 1 with j = l & 1.
-template <int F>
-__device__ __forceinline__ uint32_t store_run_scales(const uint4 (&v)[kRun], int l, float* inv0, float* inv1) {
-    // Maxima of the 8 tokens, reduced and handed out at once: a lane gives away half of what it holds at every step
-    // (7 exchanges for 8 tokens instead of 3 or 4 for each), until it has the token of its scale.
-    uint32_t a[kRun];
+// Scales of a run of R rows (1, 2, 4 or 8; half a warp, lane l of 16 with 8 elements of each): what store_scale gives for row l / (16 / R), in
+// 4 bits for groups 2j and 2j + 1 with j = l & 1.
+template <int F, int R>
+__device__ __forceinline__ uint32_t store_run_scales(const uint4 (&v)[R], int l, float* inv0, float* inv1) {
+    // Maxima of the rows, reduced and handed out at once: a lane gives away half of what it holds at every step
+    // (7 exchanges for 8 rows instead of 3 or 4 for each), until it has the row of its scale.
+    uint32_t a[R];
 #pragma unroll
-    for (int i = 0; i < kRun; ++i) a[i] = store_lane_max<F>(v[i]);
+    for (int i = 0; i < R; ++i) a[i] = store_lane_max<F>(v[i]);
 #pragma unroll
-    for (int o = 8, n = kRun / 2; o >= 2; o >>= 1, n >>= 1) {
+    for (int o = 8, n = R / 2; o >= 2; o >>= 1, n >>= 1) {
         const bool upper = (l & o) != 0;
+        if (n == 0) a[0] = __vmaxu2(a[0], __shfl_xor_sync(0xffffffffu, a[0], o));
 #pragma unroll
-        for (int i = 0; i < kRun / 2; ++i)
+        for (int i = 0; i < R / 2; ++i)
             if (i < n) {
                 const uint32_t keep = upper ? a[i + n] : a[i], give = upper ? a[i] : a[i + n];
                 a[i] = __vmaxu2(keep, __shfl_xor_sync(0xffffffffu, give, o));
