@@ -42,32 +42,50 @@ __device__ __forceinline__ uint4 load_row(const __nv_bfloat16* row, int l, bool 
     return r;
 }
 
-// How keys are turned: not at all; pairs that are neighbours, rot_dim a multiple of a lane's 8 elements; pairs a multiple of 8 elements apart;
-// any others.
-enum { kStraight = 0, kNeighbours = 1, kLanes = 2, kAny = 3 };
+// How keys are turned: not at all; pairs that are neighbours, rot_dim a multiple of a lane's 8 elements; pairs half a head apart; pairs another
+// multiple of 8 elements apart; any others.
+enum { kStraight = 0, kNeighbours = 1, kWhole = 2, kLanes = 3, kAny = 4 };
+// Where a row's lanes hold its elements in the order of 4-bit codes from the start: elements 4i .. 4i + 3 with i = l / 2 + 16 (l % 2), and
+// 32 further on. The other sides of pairs half a head apart are then lane l ^ 1's, those of neighbours its own.
+template <int F, int OP> constexpr bool kCodeOrder = F == GKV_STORE_INT4 && OP <= kWhole;
 
 // cos and sin of what a lane has of a token: of the pairs of its 8 elements, sin negated where it has the first sides, or (neighbours) of its 4
 // pairs.
-template <int OP>
+template <int F, int OP>
 struct LaneTurn {
     static constexpr int N = OP == kNeighbours ? 1 : 2;
     float4 c[N], s[N];
     __device__ __forceinline__ void load(int l, int half, const float* cos, const float* sin) {
-        const int at = OP == kNeighbours ? 4 * l : 8 * l < half ? 8 * l : 8 * l - half;      // (lanes behind the pairs: not used)
-        if (OP == kNeighbours ? at < half : 8 * l < 2 * half)
+        if constexpr (OP == kNeighbours && kCodeOrder<F, OP>) {
+            const int at = 2 * (l >> 1) + 32 * (l & 1);
+            float2 x[2] = {}, y[2] = {};
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                c[i] = reinterpret_cast<const float4*>(cos + at)[i];
-                const float4 x = reinterpret_cast<const float4*>(sin + at)[i];
-                s[i] = OP == kLanes && 8 * l < half ? make_float4(-x.x, -x.y, -x.z, -x.w) : x;
-            }
+            for (int i = 0; i < 2; ++i)
+                if (at + 16 * i < half) {
+                    x[i] = *reinterpret_cast<const float2*>(cos + at + 16 * i);
+                    y[i] = *reinterpret_cast<const float2*>(sin + at + 16 * i);
+                }
+            c[0] = make_float4(x[0].x, x[0].y, x[1].x, x[1].y);
+            s[0] = make_float4(y[0].x, y[0].y, y[1].x, y[1].y);
+        } else {
+            const int first = OP == kWhole && kCodeOrder<F, OP> ? 4 * (l >> 1) : 8 * l, next = OP == kWhole && kCodeOrder<F, OP> ? 32 : 4;
+            const bool negate = OP == kWhole && kCodeOrder<F, OP> ? (l & 1) == 0 : OP != kNeighbours && 8 * l < half;
+            const int at = OP == kNeighbours ? 4 * l : first < half ? first : first - half;      // (lanes behind the pairs: not used)
+            if (OP == kWhole || (OP == kNeighbours ? at < half : 8 * l < 2 * half))
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    c[i] = *reinterpret_cast<const float4*>(cos + at + next * i);
+                    const float4 x = *reinterpret_cast<const float4*>(sin + at + next * i);
+                    s[i] = negate ? make_float4(-x.x, -x.y, -x.z, -x.w) : x;
+                }
+        }
     }
 };
 // A lane's 8 elements of a row, turned: x c + y s with y the other sides of their pairs, the products in the order of rotary_turn.
-template <int OP>
-__device__ __forceinline__ uint4 turn_lane(const LaneTurn<OP>& r, uint4 v, int l, int half) {
+template <int F, int OP>
+__device__ __forceinline__ uint4 turn_lane(const LaneTurn<F, OP>& r, uint4 v, int l, int half) {
     const uint32_t x[4] = {v.x, v.y, v.z, v.w};
-    const int from = 8 * l < half ? l + half / 8 : l - half / 8;
+    const int from = OP == kWhole ? (kCodeOrder<F, OP> ? l ^ 1 : l ^ 8) : 8 * l < half ? l + half / 8 : l - half / 8;
     uint32_t y[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -85,7 +103,12 @@ __device__ __forceinline__ uint4 turn_lane(const LaneTurn<OP>& r, uint4 v, int l
         }
         y[i] = pack_bf16x2(t.x, t.y);
     }
-    if (half == 64) return make_uint4(y[0], y[1], y[2], y[3]);
+    if (OP == kWhole || half == 64) return make_uint4(y[0], y[1], y[2], y[3]);
+    if constexpr (kCodeOrder<F, OP>) {
+        const int at = 4 * (l >> 1) + 64 * (l & 1);
+        const bool p = at < 2 * half, q = at + 32 < 2 * half;
+        return make_uint4(p ? y[0] : v.x, p ? y[1] : v.y, q ? y[2] : v.z, q ? y[3] : v.w);
+    }
     return 8 * l < 2 * half ? make_uint4(y[0], y[1], y[2], y[3]) : v;
 }
 // The same element by element, for any rot_dim and either order of pairs, with cos and sin from shared memory.
@@ -170,7 +193,7 @@ __global__ void __launch_bounds__(kPageCopyThreads) gkv_pages_append_kernel(cons
 #pragma unroll
         for (int k = 0; k < R; ++k) {
             v[k] = make_uint4(0u, 0u, 0u, 0u);
-            if (k < rows && h < heads && t < n) v[k] = load_row<F>(src, l, turns);
+            if (k < rows && h < heads && t < n) v[k] = load_row<F>(src, l, turns && !kCodeOrder<F, OP>);
             if (++h == heads_per_cta) { h = 0; ++t; src += next_token; }
             else src += p.head_stride;
         }
@@ -205,12 +228,13 @@ __global__ void __launch_bounds__(kPageCopyThreads) gkv_pages_append_kernel(cons
                 else src += p.head_stride;
             }
         } else {
-            LaneTurn<OP> r;
+            LaneTurn<F, OP> r;
 #pragma unroll
             for (int k = 0; k < R; ++k) {
                 if (k < rows) {
                     if (h == 0) r.load(l, half, s_table + k0 * half, s_sin + k0 * half);
-                    v[k] = as_format<F>(turn_lane<OP>(r, v[k], l, half), l);
+                    v[k] = turn_lane<F, OP>(r, v[k], l, half);
+                    if constexpr (!kCodeOrder<F, OP>) v[k] = as_format<F>(v[k], l);
                 }
                 if (++h == heads_per_cta) { h = 0; ++k0; }
             }
@@ -322,14 +346,16 @@ static cudaError_t launch_append(PagesCopyLaunch p, cudaStream_t s) {
     p.heads_per_cta = (p.h_kv + p.head_blocks - 1) / p.head_blocks;
     p.tokens_per_half = rows / p.heads_per_cta;
     if (rows == 2) return launch_append_rows<OP, 2, 0>(p, s);
-    if (OP != kAny && p.heads_per_cta * p.head_blocks == p.h_kv) {
-        if (p.heads_per_cta == 8) return launch_append_rows<OP, kRun, 8>(p, s);
-        if (p.heads_per_cta == 4) return launch_append_rows<OP, kRun, 4>(p, s);
+    if constexpr (OP <= kWhole) {
+        const bool even = p.heads_per_cta * p.head_blocks == p.h_kv;
+        if (even && p.heads_per_cta == 8) return launch_append_rows<OP, kRun, 8>(p, s);
+        if (even && p.heads_per_cta == 4) return launch_append_rows<OP, kRun, 4>(p, s);
     }
     return launch_append_rows<OP, kRun, 0>(p, s);
 }
 cudaError_t launch_pages_append(const PagesCopyLaunch& p, cudaStream_t s) {
     if (!p.rotary.turns) return launch_append<kStraight>(p, s);
+    if (!p.rotary.interleaved && p.rotary.half == 64) return launch_append<kWhole>(p, s);
     if (p.rotary.interleaved) return p.rotary.half % 4 == 0 ? launch_append<kNeighbours>(p, s) : launch_append<kAny>(p, s);
     return p.rotary.half % 8 == 0 ? launch_append<kLanes>(p, s) : launch_append<kAny>(p, s);
 }
