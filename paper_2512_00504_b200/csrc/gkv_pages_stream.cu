@@ -123,11 +123,14 @@ __device__ __forceinline__ int stream_owner(int64_t step, int64_t per) {
     return step < 1ll << 30 && per < 1ll << 30 ? (int)((uint32_t)step / (uint32_t)per) : (int)(step / per);
 }
 
-template <int F, bool TOGETHER>
-__global__ void __launch_bounds__(32, stream_warps(F, TOGETHER)) gkv_pages_stream_kernel(const PagesAttnLaunch p) {
+// How rows lie: anyhow; those of a tile, or of a whole step, next to one another in one page.
+enum { kApart = 0, kTiles = 1, kSteps = 2 };
+
+template <int F, int LIE>
+__global__ void __launch_bounds__(32, stream_warps(F, LIE != kApart)) gkv_pages_stream_kernel(const PagesAttnLaunch p) {
     using Warp = StreamWarp<F>;
     constexpr int NG = value_groups(F), S = Warp::kStages, TILES = Warp::kTiles, KEYS = Warp::kKeys, kRow = Warp::kRow, kScales = Warp::kScales;
-    constexpr bool kScaled = F != GKV_STORE_BF16;
+    constexpr bool kScaled = F != GKV_STORE_BF16, TOGETHER = LIE != kApart;
     extern __shared__ __align__(128) uint8_t s_raw[];
     const int lane = threadIdx.x;
     Warp& sw = *reinterpret_cast<Warp*>(s_raw);
@@ -174,19 +177,20 @@ __global__ void __launch_bounds__(32, stream_warps(F, TOGETHER)) gkv_pages_strea
     const int added = p.k_new ? 1 : 0;
 
     const int q = lane >> 2, j = lane & 3, h0 = 2 * j;
-    const HeadTurn turn(p.rotary, lane);
     // A unit's heads: their elements, and the operand made of them.
     uint32_t qf[8][2];
     float f0 = 0.f, f1 = 0.f;
     HeadTurn::Words e[kMaxGroup];
     auto position = [&]() { return p.pos ? p.pos[at.seq] : added ? at.len : at.len - 1; };
     auto load_heads = [&]() {
+        const HeadTurn turn(p.rotary, lane);
         const __nv_bfloat16* x = p.q + ((int64_t)at.seq * p.q_stride + (int64_t)at.head * p.g * kHeadDim);
 #pragma unroll
         for (int h = 0; h < kMaxGroup; ++h)
             if (h < p.g) e[h] = turn.load(x + h * kHeadDim);
     };
     auto make_heads = [&]() {
+        const HeadTurn turn(p.rotary, lane);
         const HeadTurn::Angles g = turn.angles(position());
 #pragma unroll
         for (int h4 = 0; h4 < kMaxGroup; h4 += 4)
@@ -213,32 +217,39 @@ __global__ void __launch_bounds__(32, stream_warps(F, TOGETHER)) gkv_pages_strea
     }
     __syncwarp();
 
-    // ---- rows on their way: the table's entries a step ahead of the copies. A lane looks up its key's, or (rows together) its tile's first one's.
-    const int mine = TOGETHER ? (lane >> 4) * kTile : lane;      // that key within the step
-    auto lookup = [&](int& slot) {
+    // ---- rows on their way: the table's entries a step ahead of the copies. A lane looks up its key's, its tile's first one's, or all of them their
+    // step's first one's, and that only where a page begins.
+    const int mine = LIE == kSteps ? 0 : TOGETHER ? (lane >> 4) * kTile : lane;      // that key within the step
+    auto lookup = [&](int& slot, int32_t& entry) {
+        if (LIE == kSteps && ahead.tile > 0 && slot + KEYS < p.pages.page_size) {
+            slot += KEYS;
+            return;
+        }
         const int key = ahead.tile * KEYS + mine;
-        if (mine >= KEYS || key >= ahead.len + added) return 0;            // no such key
+        entry = 0;
+        if (LIE != kSteps && (mine >= KEYS || key >= ahead.len + added)) return;      // no such key
         const int page = page_of(p.pages, key);
         slot = key - page * p.pages.page_size;
-        return p.pages.table[ahead.seq * p.pages.table_stride + page];
+        entry = p.pages.table[ahead.seq * p.pages.table_stride + page];
     };
-    const bool on_one_page = p.pages.page_size % KEYS == 0;      // all rows of a step (rows together)
-    int issued = 0, next_slot = 0, next = lookup(next_slot);
+    int issued = 0, next_slot = p.pages.page_size;         // (no page has been looked up yet)
+    int32_t next;
+    lookup(next_slot, next);
     uint32_t lost = 0;                                     // stages with a row on no page
     auto issue = [&](int stage) {
         const int key0 = ahead.tile * KEYS, here = ahead.len - key0;       // rows in the cache from key0 on
         const bool page = (uint32_t)next < (uint32_t)p.pages.n_pages;
         const uint32_t row = (uint32_t)next * p.pages.page_rows + (uint32_t)ahead.head * p.pages.head_rows + (uint32_t)next_slot * p.pages.token_rows;
-        const bool fine = __all_sync(0xffffffffu, page || mine >= KEYS || key0 + mine >= ahead.len + added);
+        const bool fine = LIE == kSteps ? page : __all_sync(0xffffffffu, page || mine >= KEYS || key0 + mine >= ahead.len + added);
         lost = fine ? lost & ~(1u << stage) : lost | 1u << stage;
         const uint32_t bar = smem_u32(&sw.full[stage]), to = smem_u32(sw.ring[stage]);
         const int n = fine ? min(max(here, 0), KEYS) : 0;                  // rows to be copied
         if constexpr (TOGETHER) {
             // One lane issues them all, with numbers that are the same for the warp: a copy takes a few instructions then, and many where every lane
             // has its own.
-            const bool joined = TILES == 1 || on_one_page;
-            const uint32_t first[2] = {__shfl_sync(0xffffffffu, row, 0), __shfl_sync(0xffffffffu, row, 16)};
-            const int part = joined ? KEYS : kTile;
+            constexpr bool joined = LIE == kSteps;
+            constexpr int part = joined ? KEYS : kTile;
+            const uint32_t first[2] = {__shfl_sync(0xffffffffu, row, 0), joined ? 0u : __shfl_sync(0xffffffffu, row, 16)};
             if (elect_one()) {
                 const int scaled = kScaled ? (n + kTile - 1) / kTile * kTile * kScales * 4 : 0;
                 mbar_arrive_expect_tx(bar, (uint32_t)(2 * n * kRow + scaled));
@@ -287,7 +298,7 @@ __global__ void __launch_bounds__(32, stream_warps(F, TOGETHER)) gkv_pages_strea
         }
         if (++issued < steps) {
             stream_next<KEYS>(p, ahead);
-            next = lookup(next_slot);
+            lookup(next_slot, next);
             if (ahead.tile == 0) {                         // a unit begins: what it will ask for comes closer
                 const __nv_bfloat16* x = p.q + ((int64_t)ahead.seq * p.q_stride + (int64_t)ahead.head * p.g * kHeadDim) + lane * 64;
                 if (lane >= 2 * p.g) x = (lane & 2 ? p.v_new : p.k_new) + ((int64_t)ahead.seq * p.kv_stride + (int64_t)ahead.head * kHeadDim) + (lane & 1) * 64;
@@ -352,6 +363,7 @@ __global__ void __launch_bounds__(32, stream_warps(F, TOGETHER)) gkv_pages_strea
                 // The new row, its last key: turned, quantised, into its page and into the tile.
                 const int64_t new_row = (int64_t)at.seq * p.kv_stride + (int64_t)at.head * kHeadDim;
                 const __nv_bfloat16 *kn = p.k_new + new_row, *vn = p.v_new + new_row;
+                const HeadTurn turn(p.rotary, lane);
                 const int32_t e = page_entry(p.pages, p.pages.table + at.seq * p.pages.table_stride, at.len);
                 turn.put(sw.row[0], turn.load(kn), turn.angles(position()));
                 __syncwarp();
@@ -594,11 +606,11 @@ __global__ void __launch_bounds__(256, kJoin == 8 ? 2 : 5) gkv_pages_stream_merg
     }
 }
 
-template <int F, bool TOGETHER>
+template <int F, int LIE>
 static cudaError_t launch_stream(const PagesAttnLaunch& p, int ctas, cudaStream_t s) {
     constexpr int kSmem = (int)sizeof(StreamWarp<F>);
-    static_assert(kSmem + 1024 <= 228 * 1024 / stream_warps(F, TOGETHER), "room for all warps of an SM");
-    const auto kernel = gkv_pages_stream_kernel<F, TOGETHER>;
+    static_assert(kSmem + 1024 <= 228 * 1024 / stream_warps(F, LIE != kApart), "room for all warps of an SM");
+    const auto kernel = gkv_pages_stream_kernel<F, LIE>;
     // a property of the function on the current device; setting it again costs less than finding out whether it is set
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
     if (e != cudaSuccess) return e;
@@ -624,13 +636,19 @@ static cudaError_t launch_stream(const PagesAttnLaunch& p, int ctas, cudaStream_
 }
 static bool rows_together(const PagesAttnLaunch& p) { return p.pages.token_rows == 1 && p.pages.page_size % kTile == 0; }
 int pages_stream_warps_per_sm(const PagesAttnLaunch& p, int format) { return stream_warps(format, rows_together(p)); }
+template <int F>
+static cudaError_t launch_format(const PagesAttnLaunch& p, int ctas, cudaStream_t s) {
+    if (!rows_together(p)) return launch_stream<F, kApart>(p, ctas, s);
+    if constexpr (stream_tiles(F) > 1)
+        if (p.pages.page_size % StreamWarp<F>::kKeys != 0) return launch_stream<F, kTiles>(p, ctas, s);
+    return launch_stream<F, kSteps>(p, ctas, s);
+}
 cudaError_t launch_pages_stream(const PagesAttnLaunch& p, int format, int ctas, cudaStream_t s) {
-    const bool together = rows_together(p);
     switch (format) {
-        case GKV_STORE_BF16: return together ? launch_stream<GKV_STORE_BF16, true>(p, ctas, s) : launch_stream<GKV_STORE_BF16, false>(p, ctas, s);
-        case GKV_STORE_E4M3: return together ? launch_stream<GKV_STORE_E4M3, true>(p, ctas, s) : launch_stream<GKV_STORE_E4M3, false>(p, ctas, s);
-        case GKV_STORE_INT8: return together ? launch_stream<GKV_STORE_INT8, true>(p, ctas, s) : launch_stream<GKV_STORE_INT8, false>(p, ctas, s);
-        default:             return together ? launch_stream<GKV_STORE_INT4, true>(p, ctas, s) : launch_stream<GKV_STORE_INT4, false>(p, ctas, s);
+        case GKV_STORE_BF16: return launch_format<GKV_STORE_BF16>(p, ctas, s);
+        case GKV_STORE_E4M3: return launch_format<GKV_STORE_E4M3>(p, ctas, s);
+        case GKV_STORE_INT8: return launch_format<GKV_STORE_INT8>(p, ctas, s);
+        default:             return launch_format<GKV_STORE_INT4>(p, ctas, s);
     }
 }
 

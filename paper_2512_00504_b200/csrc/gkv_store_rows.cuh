@@ -189,6 +189,7 @@ __device__ __forceinline__ void load_tile_v(TileV<F>& t, const TilePtrs<F>& p, i
 template <int F>
 __device__ __forceinline__ void tile_logits(const TileK<F>& t, const uint32_t (&qf)[8][2], float f0, float f1, float (&z)[4]) {
     if constexpr (F == GKV_STORE_INT4) {
+        float2 y0, y1;
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
             float acc[4];
@@ -206,10 +207,13 @@ __device__ __forceinline__ void tile_logits(const TileK<F>& t, const uint32_t (&
             }
             const uint32_t w0 = g < 2 ? t.s[0].x : t.s[0].y, w1 = g < 2 ? t.s[1].x : t.s[1].y;
             const float s0 = (g & 1) ? bf16_hi(w0) : bf16_lo(w0), s1 = (g & 1) ? bf16_hi(w1) : bf16_lo(w1);
-            z[0] = g == 0 ? acc[0] * s0 : fmaf(acc[0], s0, z[0]); z[1] = g == 0 ? acc[1] * s0 : fmaf(acc[1], s0, z[1]);
-            z[2] = g == 0 ? acc[2] * s1 : fmaf(acc[2], s1, z[2]); z[3] = g == 0 ? acc[3] * s1 : fmaf(acc[3], s1, z[3]);
+            const float2 a0 = make_float2(acc[0], acc[1]), a1 = make_float2(acc[2], acc[3]), s00 = make_float2(s0, s0), s11 = make_float2(s1, s1);
+            y0 = g == 0 ? mul2(a0, s00) : fma2(a0, s00, y0);
+            y1 = g == 0 ? mul2(a1, s11) : fma2(a1, s11, y1);
         }
-        z[0] *= f0; z[1] *= f1; z[2] *= f0; z[3] *= f1;
+        y0 = mul2(y0, make_float2(f0, f1));
+        y1 = mul2(y1, make_float2(f0, f1));
+        z[0] = y0.x; z[1] = y0.y; z[2] = y1.x; z[3] = y1.y;
     } else {
         float sa[4], sb[4];   // two accumulators: half the dependent chain
 #pragma unroll
@@ -399,20 +403,21 @@ struct RunningRows {
         // (at most the limit then), infinite or NaN, also at the first step, where m is -infinity.
         float total = 0.f;
         auto weigh = [&]() {
-            e[0] = fast_exp2(z[0] - n0); e[1] = fast_exp2(z[1] - n1);
-            e[2] = fast_exp2(z[2] - n0); e[3] = fast_exp2(z[3] - n1);
+            const float2 n = make_float2(-n0, -n1), d0 = add2(make_float2(z[0], z[1]), n), d1 = add2(make_float2(z[2], z[3]), n);
+            e[0] = fast_exp2(d0.x); e[1] = fast_exp2(d0.y);
+            e[2] = fast_exp2(d1.x); e[3] = fast_exp2(d1.y);
             total += (e[0] + e[2]) + (e[1] + e[3]);
             if constexpr (NG > 1) {
-                float sum = 0.f;
+                float2 sum = make_float2(0.f, 0.f);
 #pragma unroll
                 for (int g = 0; g < NG; ++g)
 #pragma unroll
                     for (int hf = 0; hf < 2; ++hf) {      // (e c is finite, c s need not be)
-                        const float x = e[2 * hf] * c0[g] * sc[hf][g], y = e[2 * hf + 1] * c1[g] * sc[hf][g];
-                        sum += x + y;
-                        b[g][hf] = pack_weights<F>(x, y);
+                        const float2 x = mul2(mul2(make_float2(e[2 * hf], e[2 * hf + 1]), make_float2(c0[g], c1[g])), make_float2(sc[hf][g], sc[hf][g]));
+                        sum = add2(sum, x);
+                        b[g][hf] = pack_weights<F>(x.x, x.y);
                     }
-                total += sum * (1.f / kLiftFactor);
+                total += (sum.x + sum.y) * (1.f / kLiftFactor);
             } else if constexpr (kScaled) {
                 total += ((e[0] * c0[0] + e[1] * c1[0]) * sc[0][0] + (e[2] * c0[0] + e[3] * c1[0]) * sc[1][0]) * (1.f / kLiftFactor);
             }
