@@ -1,21 +1,24 @@
 // Appending rows to a cache in pages, with keys rotated on the way, and reading them back.
 //
-// Bound by HBM, as the copies of a store, with two things more: a token's row is found through the table, and keys are rotated. cos
-// and sin depend on the token and the pair alone, and cost more than all else that is done to a pair. So a half warp that appends has the
-// heads of one token (up to kRun rows, all of whose loads start first) and holds the cos and sin of its lanes' elements in registers; the
-// CTA works them out once for its tokens, through shared memory. (With kRun tokens of one head instead, as the store's copies go, every row
-// reads its own cos and sin from shared memory: 4 x 32768 tokens x 8 heads in bf16 302 us.) K and V take turns in the grid, so that K's
-// arithmetic runs while V moves. A lane has 8 neighbouring elements, those on the other side of their pairs come from another lane. What
+// Two things more than in the copies of a store: a token's row is found through the table, and keys are rotated. cos and sin depend on
+// the token and the pair alone, and cost more than all else that is done to a pair. So a half warp that appends has the heads of one token (up to
+// kRun rows, all of whose loads start first) and holds the cos and sin of its lanes' elements in registers; the CTA works them out once for its
+// tokens, through shared memory. (With kRun tokens of one head instead, as the store's copies go, every row reads its own cos and sin from
+// shared memory: 4 x 32768 tokens x 8 heads in bf16 302 us.) K and V take turns in the grid, so that K's arithmetic runs while V moves. A lane has
+// 8 neighbouring elements, those on the other side of their pairs come from another lane (4 bits: of the order that lets its codes be one
+// store, where the pairs allow it; turned in the plain order and exchanged afterwards, the same rows in 4 bits take 180 us instead of 158). What
 // is rotated is rounded to bf16 and goes on from there as if it had been read, so that a fused append leaves the bits that rotating first would.
 // Scales of one head's rows lie next to one another in a page while a half warp has different heads: the CTA gathers them in shared memory and
 // writes those of its tokens together.
 //
+// What bounds it: bf16 rows HBM; quantised ones that are rotated the issue of instructions (8 bits: 80% of all cycles), so that what goes into
+// pairs of fp32 operations does, and the number of heads is known at compile time where it can be (without both 174 us instead of 148).
+//
 // Reading back takes kRun tokens of a head, so that scales come with one access.
 //
-// Measured (bytes of both sides): 4 x 32768 tokens x 8 heads in bf16, rotated, 1.07 GB in 161 us, 6.7 TB/s; 8 prompts of 129 to 4097 tokens x 4
-// heads, 70 MB in bf16 in 18.7 us (16.2 without the rotation), 52 MB in 8 bits in 21.4 (14.4), in 4 bits 24.2 (14.8): a few rounds of CTAs,
-// each a chain of count, rows, arithmetic; back in 13.5 to 16.1. One token of 32 sequences x 4 heads: 3.5 us in bf16, 4.6 in 8 bits (1.9 and
-// 2.9 without the rotation).
+// Measured: 4 x 32768 tokens x 8 heads, rotated: in bf16 161 us (1.07 GB, 6.7 TB/s), in 8 bits 148 to 153, in 4 bits 158; without the rotation 165,
+// 120 and 101; back in 163, 127 and 113. 8 prompts of 129 to 4097 tokens x 4 heads 17 to 18.5 us (without the rotation 16, 13, 12.5), back in 16.2, 13.7
+// and 13.7. One token of 32 sequences x 4 heads: 2.3 us in bf16, 2.8 to 3.1 in the others (1.7 and 2.4 without the rotation), back in 2.
 #include "gkv_pages.cuh"
 #include "gkv_rotary.cuh"
 #include "gkv_store_rows.h"
@@ -24,7 +27,6 @@ namespace gkv {
 
 constexpr int kPageCopyThreads = 128;
 constexpr int kPageCopyItems = kPageCopyThreads / 16;
-constexpr int64_t kFewRows = 16384;
 
 // The 8 elements of a row that lane l has, neighbours or those of format F. These loads stay where they are written: all of them ahead of
 // what they are to overlap with. (Left to the compiler, they were put off to the rows' turn where registers were short: an append of
@@ -341,11 +343,17 @@ static cudaError_t launch_append_rows(const PagesCopyLaunch& p, cudaStream_t s) 
 }
 template <int OP>
 static cudaError_t launch_append(PagesCopyLaunch p, cudaStream_t s) {
-    const int rows = (int64_t)p.batch * p.n_tokens * p.h_kv <= kFewRows ? 2 : kRun;
-    p.head_blocks = (p.h_kv + rows - 1) / rows;
-    p.heads_per_cta = (p.h_kv + p.head_blocks - 1) / p.head_blocks;
-    p.tokens_per_half = rows / p.heads_per_cta;
-    if (rows == 2) return launch_append_rows<OP, 2, 0>(p, s);
+    // Two rows a half warp, whose chain is shorter, as long as that leaves no more than three CTAs an SM (one token of 32 sequences x 4 heads in 8
+    // bits, 128 CTAs, 2.8 us with two, 4.4 with eight; 1024 tokens of one, 512 CTAs, 3.85 and 3.67; 128 x 8 heads, 1024 CTAs, 4.3 and 3.6).
+    auto shape = [&](int rows) {
+        p.head_blocks = (p.h_kv + rows - 1) / rows;
+        p.heads_per_cta = (p.h_kv + p.head_blocks - 1) / p.head_blocks;
+        p.tokens_per_half = rows / p.heads_per_cta;
+        const int tokens = kPageCopyItems * p.tokens_per_half;
+        return (int64_t)((p.n_tokens + tokens - 1) / tokens) * p.head_blocks * 2 * p.batch;
+    };
+    if (shape(2) <= 3 * device_sm_count()) return launch_append_rows<OP, 2, 0>(p, s);
+    shape(kRun);
     if constexpr (OP <= kWhole) {
         const bool even = p.heads_per_cta * p.head_blocks == p.h_kv;
         if (even && p.heads_per_cta == 8) return launch_append_rows<OP, kRun, 8>(p, s);

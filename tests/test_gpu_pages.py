@@ -186,6 +186,33 @@ def test_append_with_any_number_of_heads(h_kv, kind):
         assert torch.equal(rows, b.view(torch.uint8))
 
 
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("h_kv", [3, 4, 8, 12])
+@pytest.mark.parametrize("kind", [None, ("halves", 128), ("halves", 64), ("halves", 16), ("halves", 20), ("neighbours", 128), ("neighbours", 64), ("neighbours", 24), ("neighbours", 44)])
+def test_append_of_many_rows(fmt, h_kv, kind):
+    """As many as take the wider runs, every way of turning them: the bytes that rotating and then storing leaves, and all others as they were."""
+    B, T, cap = 3, 307, 320
+    g = gen(7)
+    first, count = [0, 13, 5], [307, 290, 1]
+    kv = randn(g, B, T, 2 * h_kv, 128) * torch.exp2(torch.randint(-20, 20, (B, T, 2 * h_kv, 1), generator=g, device=DEV).to(torch.bfloat16))
+    kv[0, 40, 0, 5], kv[0, 41, h_kv, 77], kv[1, 2, 1, 100] = float("nan"), float("inf"), float("-inf")      # their rows are not finite
+    k, v = kv[:, :, :h_kv], kv[:, :, h_kv:]
+    rot = rotary(kind)
+    table, n_pages = deal_pages(3, [cap] * B, 16)
+    st = gkv.PagedStore(fmt, pages=n_pages, page_size=16, h_q=h_kv, h_kv=h_kv, max_batch=B, device=DEV)
+    flat = gkv.KVStore(fmt, batch=B, h_q=h_kv, h_kv=h_kv, capacity=cap, device=DEV)
+    for t in (st.k, st.v, st.k_scale, st.v_scale, flat.k, flat.v, flat.k_scale, flat.v_scale):
+        if t is not None:
+            t.view(torch.uint8).fill_(0x3A)
+    st.append(ints(table), k, v, first=ints(first), count=ints(count), rotary=rot)
+    pos = ints(first)[:, None] + torch.arange(T, device=DEV, dtype=torch.int32)
+    flat.write(turned(rot, pos, k), v.contiguous(), first=ints(first), count=ints(count))
+    for a, b in ((st.k, flat.k), (st.v, flat.v), (st.k_scale, flat.k_scale), (st.v_scale, flat.v_scale)):
+        if a is not None:
+            rows = a.view(torch.uint8)[ints(table).long()].transpose(1, 2).flatten(2, 3)[:, :, :cap]
+            assert torch.equal(rows, b.view(torch.uint8))
+
+
 def test_no_tokens_do_nothing():
     st = gkv.PagedStore("int8", pages=2, page_size=16, h_q=4, h_kv=2, max_batch=1, device=DEV)
     x = torch.zeros(1, 0, 2, 128, dtype=torch.bfloat16, device=DEV)
