@@ -6,17 +6,18 @@
 // tokens, through shared memory. (With kRun tokens of one head instead, as the store's copies go, every row reads its own cos and sin from
 // shared memory: 4 x 32768 tokens x 8 heads in bf16 302 us.) K and V take turns in the grid, so that K's arithmetic runs while V moves. A lane has
 // 8 neighbouring elements, those on the other side of their pairs come from another lane (4 bits: of the order that lets its codes be one
-// store, where the pairs allow it; turned in the plain order and exchanged afterwards, the same rows in 4 bits take 180 us instead of 158). What
+// store, where the pairs allow it; turned in the plain order and exchanged afterwards, the same rows in 4 bits took 180 us instead of 158). What
 // is rotated is rounded to bf16 and goes on from there as if it had been read, so that a fused append leaves the bits that rotating first would.
 // Scales of one head's rows lie next to one another in a page while a half warp has different heads: the CTA gathers them in shared memory and
 // writes those of its tokens together.
 //
-// What bounds it: bf16 rows HBM; quantised ones that are rotated the issue of instructions (8 bits: 80% of all cycles), so that what goes into
-// pairs of fp32 operations does, and the number of heads is known at compile time where it can be (without both 174 us instead of 148).
+// What bounds it: bf16 rows HBM; quantised ones that are rotated the issue of instructions. So fp32 operations go in pairs, the number of heads is
+// known at compile time where it can be, pairs half a head apart have a way of their own, and registers are held to eight CTAs an SM (8 bits: 174 us
+// without all of it, 155 with the first two, 148 with three, 132 with all).
 //
 // Reading back takes kRun tokens of a head, so that scales come with one access.
 //
-// Measured: 4 x 32768 tokens x 8 heads, rotated: in bf16 161 us (1.07 GB, 6.7 TB/s), in 8 bits 148 to 153, in 4 bits 158; without the rotation 165,
+// Measured: 4 x 32768 tokens x 8 heads, rotated: in bf16 160 us (1.07 GB, 6.7 TB/s), in 8 bits 132 to 137, in 4 bits 145; without the rotation 165,
 // 120 and 101; back in 163, 127 and 113. 8 prompts of 129 to 4097 tokens x 4 heads 17 to 18.5 us (without the rotation 16, 13, 12.5), back in 16.2, 13.7
 // and 13.7. One token of 32 sequences x 4 heads: 2.3 us in bf16, 2.8 to 3.1 in the others (1.7 and 2.4 without the rotation), back in 2.
 #include "gkv_pages.cuh"
@@ -150,8 +151,14 @@ __device__ __forceinline__ uint4 as_format(uint4 v, int l) {
 
 // CTA: K or V, heads_per_cta heads, 8 * tokens_per_half tokens of sequence blockIdx.y. Half warp w: tokens_per_half tokens from w *
 // tokens_per_half on, all those heads of each (at most R rows).
+// CTAs an SM that a kernel's registers are held to (0: as the compiler would have it). Rows that are rotated and quantised do better with eight,
+// which hides their arithmetic, although a few registers are spilled (in 8 bits 132 us instead of 147 with six; nine 140); the others wait for memory, and
+// do better with all loads under way (bf16 160 us, with eight 173; in 8 bits without a rotation 120 and 148).
+__host__ __device__ constexpr int append_ctas(int format, int op, int rows) {
+    return rows != kRun || op == kStraight || op == kAny ? 0 : format == GKV_STORE_BF16 ? 1 : 8;
+}
 template <int F, int OP, int R, int H>
-__global__ void __launch_bounds__(kPageCopyThreads) gkv_pages_append_kernel(const PagesCopyLaunch p) {
+__global__ void __launch_bounds__(kPageCopyThreads, append_ctas(F, OP, R)) gkv_pages_append_kernel(const PagesCopyLaunch p) {
     using Fm = StoreFormat<F>;
     constexpr int kLanesOfRow = 16 / R;                  // that have its scales
     extern __shared__ __align__(16) float s_table[];     // cos and sin of the CTA's tokens: [token][half] each
