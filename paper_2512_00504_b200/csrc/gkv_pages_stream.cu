@@ -620,9 +620,8 @@ static cudaError_t launch_stream(const PagesAttnLaunch& p, int ctas, cudaStream_
     const int units = p.batch * p.h_kv;
     // CTAs a unit, and warps that share its parts: few units have many parts, and all the CTAs fit the device at once (148 SMs).
     int split = 0;
-    const bool many = units <= 2 * 148 / 8;
-    while (!many && split < 2 && (ctas >> split) > 2 * units && (units << (split + 1)) <= 5 * 148) ++split;
-    if (many) split = 3;
+    const bool many = units <= 2 * 148;
+    while (many && split < 3 && (units << (split + 1)) <= 2 * 148) ++split;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)units << split);
     cfg.blockDim = dim3(256);
