@@ -20,9 +20,9 @@
 // A wait that runs out (never, but every wait ends) makes the warp's units NaN, too.
 //
 // Measured (with the merge; the time that the rows' bytes take at 6.46 TB/s): 128 sequences x 8 heads of about 2200 keys in bf16 in pages of 64
-// 188 to 193 us (177), of 16 190 to 194, of 5 197 to 199; in 8 bits in pages of 64 112 (92), of 5 156; in 4 bits 110 (51) and 170. 16 x 4 heads of 300
-// to 65535 keys in bf16 217 to 219 (206). 2 x 8 heads of up to 131071 in 4 bits 89 (42). 16-bit rows are bound by HBM. With 4-bit rows the warps
-// issue in 61% of all cycles, 480 instructions a tile, of which 170 unpack codes: instructions and what they wait for bound it.
+// 187 to 190 us (177), of 16 188 to 190, of 5 197 to 199; in 8 bits in pages of 64 110 (90), of 5 155; in 4 bits 106 (50) and 166. 16 x 4 heads of 300
+// to 65535 keys in bf16 216 (206). 2 x 8 heads of up to 131071 in 4 bits 88 (42). 16-bit rows are bound by HBM. With 4-bit rows the warps
+// issue in 63% of all cycles, 450 instructions a tile, of which 170 unpack codes: instructions and what they wait for bound it.
 #include "gkv_pages.cuh"
 #include "gkv_rotary.cuh"
 #include "gkv_store_rows.cuh"
@@ -502,16 +502,16 @@ __global__ void __launch_bounds__(32, stream_warps(F, LIE != kApart)) gkv_pages_
 }
 
 // Joins the partial results of a unit: a running softmax over them, kJoin at a time, all of whose loads are under way before the first is
-// looked at. 2^split CTAs a unit; a warp has two dimensions of every lane's, those of its CTA's 2^-split of all, and every 2^split-th of the parts.
-// kJoin = 8 takes 128 registers, two CTAs an SM, kJoin = 2 leaves room for five.
-template <int F, int kJoin>
-__global__ void __launch_bounds__(256, kJoin == 8 ? 2 : 5) gkv_pages_stream_merge_kernel(const PagesAttnLaunch p, const int warps, const int split) {
+// looked at. A warp has two dimensions of every lane's (a slice), or kSlices times that; 2^split CTAs a unit, each with its slices, and 2^split shares of
+// the parts. It takes 5 to 8 us behind the stream, trips to memory one after the other. Up to 296 units: kJoin = 8, 128 registers, two CTAs of 256
+// threads an SM (16 x 4 heads of 300 to 65535 keys, 100 parts of the longest: 2 at a time 219 us, 8 216). More of them: kJoin = 2, CTAs of 128 threads, so
+// that those of 1184 units fit the device at once (128 x 8 heads in 8 bits 110 us; with 256 threads, 740 at once, 112).
+template <int F, int kJoin, int kSlices>
+__global__ void __launch_bounds__(256 / kSlices, kSlices == 2 ? 8 : 2) gkv_pages_stream_merge_kernel(const PagesAttnLaunch p, const int warps, const int split) {
     constexpr int NG = value_groups(F), KEYS = StreamWarp<F>::kKeys;
-    __shared__ float4 s_o[8][32], s_mv[8][32];
-    __shared__ float2 s_l[8][32];
     const int unit = blockIdx.x >> split, seq = unit / p.h_kv, head = unit - seq * p.h_kv;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int slices = 8 >> split, share = warp / slices;          // of a CTA; of the parts
+    const int slices = (8 >> split) / kSlices, share = warp / slices;          // warps that share a part; which of the parts
     int64_t before;
     int kept[kKept];
     const int64_t all = stream_total<KEYS>(p, seq, lane, kept, &before);
@@ -520,8 +520,8 @@ __global__ void __launch_bounds__(256, kJoin == 8 ? 2 : 5) gkv_pages_stream_merg
     const int64_t first = before + (int64_t)head * tiles;
     const int w0 = stream_owner(first, per), n = tiles ? stream_owner(first + tiles - 1, per) - w0 + 1 : 0;
     const size_t out = ((size_t)seq * p.h_q + (size_t)head * p.g) * kHeadDim;
-    const int slice = (blockIdx.x & ((1 << split) - 1)) * slices + warp % slices;      // the two dimensions
-    const int q = lane >> 2, h0 = 2 * (lane & 3), d = out_dim<F>(slice, q), dg = slice / (8 / NG);
+    const int slice0 = (blockIdx.x & ((1 << split) - 1)) * slices * kSlices + warp % slices;      // two dimensions each: slice0, slice0 + slices ..
+    const int q = lane >> 2, h0 = 2 * (lane & 3);
     grid_wait_previous();                                  // (nobody leaves before: what comes next waits for this kernel alone)
     if (len < 0 || n == 1) return;                         // left out, or finished by the warp that had it
     if (n == 0) {
@@ -529,77 +529,116 @@ __global__ void __launch_bounds__(256, kJoin == 8 ? 2 : 5) gkv_pages_stream_merg
         if (share != 0) return;
         const uint32_t x = fits ? 0u : 0x7fff7fffu;        // bf16 NaN
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
-            if (h0 + h < p.g) *reinterpret_cast<uint32_t*>(p.out + out + (h0 + h) * kHeadDim + d) = x;
-        if (p.lse && slice == 0 && lane < p.g) p.lse[(size_t)seq * p.h_q + (size_t)head * p.g + lane] = fits ? -INFINITY : NAN;
+        for (int k = 0; k < kSlices; ++k)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                if (h0 + h < p.g) *reinterpret_cast<uint32_t*>(p.out + out + (h0 + h) * kHeadDim + out_dim<F>(slice0 + k * slices, q)) = x;
+        if (p.lse && slice0 == 0 && lane < p.g) p.lse[(size_t)seq * p.h_q + (size_t)head * p.g + lane] = fits ? -INFINITY : NAN;
         return;
     }
     // Part i is warp w0 + i's: the first of its two, but where the unit begins inside a warp's share its last one.
     const bool inside = first != w0 * per;
-    float2 m = make_float2(-INFINITY, -INFINITY), v = m, l = make_float2(0.f, 0.f);
-    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);            // dimension d of heads h0 and h0 + 1, then d + 1
-    // Takes in another result (am, av, al, x): relative to 2^av, weights to 2^am; am = -infinity: no key, its values may be missing.
-    auto raise = [&](float2 am, float2 av) {
-        const float2 nm = make_float2(fmaxf(m.x, am.x), fmaxf(m.y, am.y)), nv = make_float2(fmaxf(v.x, av.x), fmaxf(v.y, av.y));
+    struct Values { float2 v; float4 o; };                 // relative to 2^v; dimension d of heads h0 and h0 + 1, then d + 1
+    float2 m = make_float2(-INFINITY, -INFINITY), l = make_float2(0.f, 0.f);
+    Values r[kSlices];
+#pragma unroll
+    for (int k = 0; k < kSlices; ++k) r[k] = Values{m, make_float4(0.f, 0.f, 0.f, 0.f)};
+    // Takes in another result: weights al relative to 2^am, and by slice its values; am = -infinity: no key, its values may be missing.
+    auto raise = [&](float2 am) {
+        const float2 nm = make_float2(fmaxf(m.x, am.x), fmaxf(m.y, am.y));
         l.x *= fast_exp2(m.x - finite_ref(nm.x)); l.y *= fast_exp2(m.y - finite_ref(nm.y));
-        const float e0 = fast_exp2(v.x - finite_ref(nv.x)), e1 = fast_exp2(v.y - finite_ref(nv.y));
-        o.x *= e0; o.z *= e0; o.y *= e1; o.w *= e1;
-        m = nm; v = nv;
+        m = nm;
     };
-    auto add = [&](float2 am, float2 av, float2 al, float4 x) {
+    auto raise_values = [&](Values& r, float2 av) {
+        const float2 nv = make_float2(fmaxf(r.v.x, av.x), fmaxf(r.v.y, av.y));
+        const float e0 = fast_exp2(r.v.x - finite_ref(nv.x)), e1 = fast_exp2(r.v.y - finite_ref(nv.y));
+        r.o.x *= e0; r.o.z *= e0; r.o.y *= e1; r.o.w *= e1;
+        r.v = nv;
+    };
+    auto add = [&](float2 am, float2 al) {
         l.x += al.x * fast_exp2(am.x - finite_ref(m.x));   // (a NaN sum may come with a maximum of -infinity)
         l.y += al.y * fast_exp2(am.y - finite_ref(m.y));
-        const float e0 = am.x == -INFINITY ? 0.f : fast_exp2(av.x - finite_ref(v.x)), e1 = am.y == -INFINITY ? 0.f : fast_exp2(av.y - finite_ref(v.y));
-        if (e0 != 0.f) { o.x = fmaf(x.x, e0, o.x); o.z = fmaf(x.z, e0, o.z); }
-        if (e1 != 0.f) { o.y = fmaf(x.y, e1, o.y); o.w = fmaf(x.w, e1, o.w); }
+    };
+    auto add_values = [&](Values& r, float2 am, const Values& a) {
+        const float e0 = am.x == -INFINITY ? 0.f : fast_exp2(a.v.x - finite_ref(r.v.x)), e1 = am.y == -INFINITY ? 0.f : fast_exp2(a.v.y - finite_ref(r.v.y));
+        if (e0 != 0.f) { r.o.x = fmaf(a.o.x, e0, r.o.x); r.o.z = fmaf(a.o.z, e0, r.o.z); }
+        if (e1 != 0.f) { r.o.y = fmaf(a.o.y, e1, r.o.y); r.o.w = fmaf(a.o.w, e1, r.o.w); }
     };
     const int step = 1 << split;
     for (int i0 = share; i0 < n; i0 += kJoin * step) {
-        float2 am[kJoin], av[kJoin], al[kJoin];
-        float4 x[kJoin];
+        float2 am[kJoin], al[kJoin];
+        Values x[kJoin][kSlices];
 #pragma unroll
-        for (int k = 0; k < kJoin; ++k) {
-            const int i = i0 + k * step;
-            am[k] = av[k] = make_float2(-INFINITY, -INFINITY);
-            al[k] = make_float2(0.f, 0.f);
-            x[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (i < n) {
-                const float* a = p.own_part + (size_t)(2 * (w0 + i) + (i == 0 && inside ? 1 : 0)) * kStreamRecFloats;
-                am[k] = *reinterpret_cast<const float2*>(a + h0);
-                al[k] = *reinterpret_cast<const float2*>(a + 8 + h0);
-                av[k] = *reinterpret_cast<const float2*>(a + 16 + 8 * dg + h0);
-                x[k] = reinterpret_cast<const float4*>(a + kStreamRecHead)[32 * slice + lane];
+        for (int i = 0; i < kJoin; ++i) {
+            const int part = i0 + i * step;
+            am[i] = make_float2(-INFINITY, -INFINITY);
+            al[i] = make_float2(0.f, 0.f);
+#pragma unroll
+            for (int k = 0; k < kSlices; ++k) x[i][k] = Values{am[i], make_float4(0.f, 0.f, 0.f, 0.f)};
+            if (part < n) {
+                const float* a = p.own_part + (size_t)(2 * (w0 + part) + (part == 0 && inside ? 1 : 0)) * kStreamRecFloats;
+                am[i] = *reinterpret_cast<const float2*>(a + h0);
+                al[i] = *reinterpret_cast<const float2*>(a + 8 + h0);
+#pragma unroll
+                for (int k = 0; k < kSlices; ++k) {
+                    const int slice = slice0 + k * slices;
+                    x[i][k].v = *reinterpret_cast<const float2*>(a + 16 + 8 * (slice / (8 / NG)) + h0);
+                    x[i][k].o = reinterpret_cast<const float4*>(a + kStreamRecHead)[32 * slice + lane];
+                }
             }
         }
-        float2 tm = am[0], tv = av[0];
+        float2 top = am[0];
 #pragma unroll
-        for (int k = 1; k < kJoin; ++k) {
-            tm.x = fmaxf(tm.x, am[k].x); tm.y = fmaxf(tm.y, am[k].y);
-            tv.x = fmaxf(tv.x, av[k].x); tv.y = fmaxf(tv.y, av[k].y);
+        for (int i = 1; i < kJoin; ++i) { top.x = fmaxf(top.x, am[i].x); top.y = fmaxf(top.y, am[i].y); }
+        raise(top);
+#pragma unroll
+        for (int i = 0; i < kJoin; ++i) add(am[i], al[i]);
+#pragma unroll
+        for (int k = 0; k < kSlices; ++k) {
+            top = x[0][k].v;
+#pragma unroll
+            for (int i = 1; i < kJoin; ++i) { top.x = fmaxf(top.x, x[i][k].v.x); top.y = fmaxf(top.y, x[i][k].v.y); }
+            raise_values(r[k], top);
+#pragma unroll
+            for (int i = 0; i < kJoin; ++i) add_values(r[k], am[i], x[i][k]);
         }
-        raise(tm, tv);
-#pragma unroll
-        for (int k = 0; k < kJoin; ++k) add(am[k], av[k], al[k], x[k]);
     }
     if (split > 0) {                                       // the shares of the same dimensions
-        s_o[warp][lane] = o;
-        s_mv[warp][lane] = make_float4(m.x, m.y, v.x, v.y);
+        __shared__ float4 s_o[kSlices][8 / kSlices][32];
+        __shared__ float2 s_m[8 / kSlices][32], s_l[8 / kSlices][32], s_v[kSlices][8 / kSlices][32];
+        s_m[warp][lane] = m;
         s_l[warp][lane] = l;
+#pragma unroll
+        for (int k = 0; k < kSlices; ++k) {
+            s_o[k][warp][lane] = r[k].o;
+            s_v[k][warp][lane] = r[k].v;
+        }
         __syncthreads();
         if (share != 0) return;
         const int shares = min(n, step);
         for (int i = 1; i < shares; ++i) {
             const int other = warp + i * slices;
-            const float4 a = s_mv[other][lane];
-            raise(make_float2(a.x, a.y), make_float2(a.z, a.w));
-            add(make_float2(a.x, a.y), make_float2(a.z, a.w), s_l[other][lane], s_o[other][lane]);
+            const float2 am = s_m[other][lane];
+            raise(am);
+            add(am, s_l[other][lane]);
+#pragma unroll
+            for (int k = 0; k < kSlices; ++k) {
+                const Values a = {s_v[k][other][lane], s_o[k][other][lane]};
+                raise_values(r[k], a.v);
+                add_values(r[k], am, a);
+            }
         }
     }
-    if (h0 < p.g)
-        *reinterpret_cast<uint32_t*>(p.out + out + h0 * kHeadDim + d) = pack_bf16x2(final_value(o.x, m.x, l.x, v.x, true), final_value(o.z, m.x, l.x, v.x, true));
-    if (h0 + 1 < p.g)
-        *reinterpret_cast<uint32_t*>(p.out + out + (h0 + 1) * kHeadDim + d) = pack_bf16x2(final_value(o.y, m.y, l.y, v.y, true), final_value(o.w, m.y, l.y, v.y, true));
-    if (p.lse && slice == 0 && q == 0) {
+#pragma unroll
+    for (int k = 0; k < kSlices; ++k) {
+        const float4 o = r[k].o;
+        const float2 v = r[k].v;
+        __nv_bfloat16* to = p.out + out + h0 * kHeadDim + out_dim<F>(slice0 + k * slices, q);
+        if (h0 < p.g) *reinterpret_cast<uint32_t*>(to) = pack_bf16x2(final_value(o.x, m.x, l.x, v.x, true), final_value(o.z, m.x, l.x, v.x, true));
+        if (h0 + 1 < p.g)
+            *reinterpret_cast<uint32_t*>(to + kHeadDim) = pack_bf16x2(final_value(o.y, m.y, l.y, v.y, true), final_value(o.w, m.y, l.y, v.y, true));
+    }
+    if (p.lse && slice0 == 0 && q == 0) {
         float* lse = p.lse + (size_t)seq * p.h_q + (size_t)head * p.g + h0;
         if (h0 < p.g) lse[0] = final_lse(m.x, l.x, true);
         if (h0 + 1 < p.g) lse[1] = final_lse(m.y, l.y, true);
@@ -621,17 +660,17 @@ static cudaError_t launch_stream(const PagesAttnLaunch& p, int ctas, cudaStream_
     // CTAs a unit, and warps that share its parts: few units have many parts, and all the CTAs fit the device at once (148 SMs).
     int split = 0;
     const bool many = units <= 2 * 148;
-    while (many && split < 3 && (units << (split + 1)) <= 2 * 148) ++split;
+    while (split < (many ? 3 : 2) && (units << (split + 1)) <= (many ? 2 : 8) * 148) ++split;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)units << split);
-    cfg.blockDim = dim3(256);
+    cfg.blockDim = dim3(many ? 256 : 128);
     cfg.stream = s;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, many ? gkv_pages_stream_merge_kernel<F, 8> : gkv_pages_stream_merge_kernel<F, 2>, p, ctas, split);
+    return cudaLaunchKernelEx(&cfg, many ? gkv_pages_stream_merge_kernel<F, 8, 1> : gkv_pages_stream_merge_kernel<F, 2, 2>, p, ctas, split);
 }
 static bool rows_together(const PagesAttnLaunch& p) { return p.pages.token_rows == 1 && p.pages.page_size % kTile == 0; }
 int pages_stream_warps_per_sm(const PagesAttnLaunch& p, int format) { return stream_warps(format, rows_together(p)); }
