@@ -20,8 +20,8 @@
 // A wait that runs out (never, but every wait ends) makes the warp's units NaN, too.
 //
 // Measured (with the merge; the time that the rows' bytes take at 6.46 TB/s): 128 sequences x 8 heads of about 2200 keys in bf16 in pages of 64
-// 187 to 190 us (177), of 16 188 to 190, of 5 197 to 199; in 8 bits in pages of 64 110 (90), of 5 155; in 4 bits 106 (50) and 166. 16 x 4 heads of 300
-// to 65535 keys in bf16 216 (206). 2 x 8 heads of up to 131071 in 4 bits 88 (42). 16-bit rows are bound by HBM. With 4-bit rows the warps
+// 187 to 190 us (177), of 16 188 to 190, of 5 197 to 199; in 8 bits in pages of 64 109 (90), of 5 150; in 4 bits 102 (50) and 159. 16 x 4 heads of 300
+// to 65535 keys in bf16 216 (206). 2 x 8 heads of up to 131071 in 4 bits 83 (42). 16-bit rows are bound by HBM. With 4-bit rows the warps
 // issue in 63% of all cycles, 450 instructions a tile, of which 170 unpack codes: instructions and what they wait for bound it.
 #include "gkv_pages.cuh"
 #include "gkv_rotary.cuh"
@@ -385,33 +385,14 @@ __global__ void __launch_bounds__(32, stream_warps(F, LIE != kApart)) gkv_pages_
             fence_proxy_async_smem();                      // before the ring's next copies
             __syncwarp();
         }
-#pragma unroll 1
-        for (int tile = 0; tile < TILES; ++tile) {
+        const uint32_t base = smem_u32(sw.ring[stage]);
+        auto logits = [&](int tile, float (&z)[4]) {
             const int keys = left - tile * kTile;          // of this tile and on
-            if (keys <= 0) break;
-            const uint32_t base = smem_u32(sw.ring[stage]);
-            if (TOGETHER) {
-                take_scales(tk, 0, stage, tile);
-                take_scales(tv, 1, stage, tile);
-            } else if (kScaled && last && added) {         // the new row's
-#pragma unroll
-                for (int hf = 0; hf < 2; ++hf)
-                    if (key[hf] == keys - 1) {
-                        if constexpr (F == GKV_STORE_INT4) {
-                            tk.s[hf] = *reinterpret_cast<const uint2*>(sw.scale[0]);
-                            tv.s[hf] = *reinterpret_cast<const uint2*>(sw.scale[1]);
-                        } else if constexpr (kScaled) {
-                            tk.s[hf] = *reinterpret_cast<const uint16_t*>(sw.scale[0]);
-                            tv.s[hf] = *reinterpret_cast<const uint16_t*>(sw.scale[1]);
-                        }
-                    }
-            }
 #pragma unroll
             for (int hf = 0; hf < 2; ++hf)
 #pragma unroll
                 for (int c = 0; c < (F == GKV_STORE_BF16 ? 4 : F == GKV_STORE_INT4 ? 1 : 2); ++c)
                     tk.d[hf][c] = lds16(base + Warp::k_at(tile * kTile + key[hf]) + j * 16 + c * 64);
-            float z[4];
             tile_logits<F>(tk, qf, f0, f1, z);
             if (keys < kTile) {
 #pragma unroll
@@ -419,6 +400,8 @@ __global__ void __launch_bounds__(32, stream_warps(F, LIE != kApart)) gkv_pages_
                     if (key[hf] >= keys) z[2 * hf] = z[2 * hf + 1] = -INFINITY;
             }
             if (bad) z[0] = z[1] = z[2] = z[3] = NAN;
+        };
+        auto values = [&](int tile, const float (&z)[4]) {
             uint32_t b[NG][2];
             r.weigh_tile(z, tv, sw.v, lane, b);
 #pragma unroll
@@ -431,9 +414,49 @@ __global__ void __launch_bounds__(32, stream_warps(F, LIE != kApart)) gkv_pages_
                 } else tv.d[i] = lds16(a);
             }
             tile_values<F, NG>(tv, b, r.acc);
-            if (!TOGETHER && tile + 1 < TILES && keys > kTile) {
-                take_scales(tk, 0, stage, tile + 1);
-                take_scales(tv, 1, stage, tile + 1);
+        };
+        if constexpr (TOGETHER && TILES > 1) {
+            // The logits of both tiles, then the rest of both: more at a time that does not wait for one another (tile by tile 131071 keys in 4 bits
+            // 84 us instead of 83; as a loop that is not unrolled 88). A tile behind the end has no weights, and zeros for V.
+            float z[TILES][4];
+#pragma unroll
+            for (int tile = 0; tile < TILES; ++tile) {
+                take_scales(tk, 0, stage, tile);
+                logits(tile, z[tile]);
+            }
+#pragma unroll
+            for (int tile = 0; tile < TILES; ++tile) {
+                take_scales(tv, 1, stage, tile);
+                values(tile, z[tile]);
+            }
+        } else {
+#pragma unroll
+            for (int tile = 0; tile < TILES; ++tile) {
+                const int keys = left - tile * kTile;
+                if (keys <= 0) break;
+                if (TOGETHER) {
+                    take_scales(tk, 0, stage, tile);
+                    take_scales(tv, 1, stage, tile);
+                } else if (kScaled && last && added) {     // the new row's
+#pragma unroll
+                    for (int hf = 0; hf < 2; ++hf)
+                        if (key[hf] == keys - 1) {
+                            if constexpr (F == GKV_STORE_INT4) {
+                                tk.s[hf] = *reinterpret_cast<const uint2*>(sw.scale[0]);
+                                tv.s[hf] = *reinterpret_cast<const uint2*>(sw.scale[1]);
+                            } else if constexpr (kScaled) {
+                                tk.s[hf] = *reinterpret_cast<const uint16_t*>(sw.scale[0]);
+                                tv.s[hf] = *reinterpret_cast<const uint16_t*>(sw.scale[1]);
+                            }
+                        }
+                }
+                float z[4];
+                logits(tile, z);
+                values(tile, z);
+                if (!TOGETHER && tile + 1 < TILES && keys > kTile) {
+                    take_scales(tk, 0, stage, tile + 1);
+                    take_scales(tv, 1, stage, tile + 1);
+                }
             }
         }
         __syncwarp();                                      // the slot has been read
