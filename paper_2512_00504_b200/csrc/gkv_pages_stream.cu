@@ -20,7 +20,7 @@
 // A wait that runs out (never, but every wait ends) makes the warp's units NaN, too.
 //
 // Measured (with the merge; the time that the rows' bytes take at 6.46 TB/s): 128 sequences x 8 heads of about 2200 keys in bf16 in pages of 64
-// 187 to 190 us (177), of 16 188 to 190, of 5 197 to 199; in 8 bits in pages of 64 109 (90), of 5 150; in 4 bits 102 (50) and 159. 16 x 4 heads of 300
+// 187 to 190 us (177), of 16 188 to 190, of 5 197 to 199; in 8 bits in pages of 64 109 (90), of 5 149; in 4 bits 102 (50) and 159. 16 x 4 heads of 300
 // to 65535 keys in bf16 216 (206). 2 x 8 heads of up to 131071 in 4 bits 83 (42). 16-bit rows are bound by HBM. With 4-bit rows the warps
 // issue in 63% of all cycles, 450 instructions a tile, of which 170 unpack codes: instructions and what they wait for bound it.
 #include "gkv_pages.cuh"
@@ -31,7 +31,7 @@ namespace gkv {
 
 // Warps of an SM, a CTA each: as many as shared memory has room for, three for each scheduler. (bf16 rows that lie together come in copies so
 // large that two are enough: 128 sequences x 8 heads of about 2200 keys in pages of 16 191 us, with 12 warps 199. Apart, 16 x 4 heads: 218
-// with 12, 296 with 8. 4 bits, 2 x 8 of up to 131071: 89, 99; 14 or 16 leave too few registers.)
+// with 12, 296 with 8. 4 bits, 2 x 8 of up to 131071, before later steps: 89, 99; 14 or 16 leave too few registers.)
 __host__ __device__ constexpr int stream_warps(int format, bool together) { return format == GKV_STORE_BF16 && together ? 8 : 12; }
 
 // 16-key tiles of a step: what is done once a step (waiting, finding rows, issuing copies) then counts for two of them. bf16 rows are so
