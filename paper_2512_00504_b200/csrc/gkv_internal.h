@@ -192,7 +192,7 @@ struct RotaryLaunch {
     RotaryRows rows[2];
     int heads0, heads;         // of the first tensor, of both
     int batch, n_tokens;
-    int tokens_per_cta, pair_runs, runs;   // runs of pairs of a row, and with those that are copied (launch_rotary)
+    int tokens_per_cta, pair_runs, runs, parts;   // runs of pairs of a row, and with those that are copied; CTAs that share a token (launch_rotary)
 };
 
 struct PagesView {             // pages and the table through which their rows are found

@@ -7,7 +7,7 @@
 // in bf16 264 us. With loads that the compiler may put off, and elements of 16 bits converted one by one: 180.)
 //
 // Measured (bytes read and written): 8 x 8192 tokens x 32 heads in bf16, 1.07 GB in 166 us, 6.5 TB/s; 4 x 4096 x 40 in fp32, half of each head
-// turned, 0.67 GB in 105 us, 6.4 TB/s; 4097 tokens x 72 heads, 151 MB in 27 us; 32 tokens x 32 heads 2.6 us, which is a launch.
+// turned, 0.67 GB in 105 us, 6.4 TB/s; 4097 tokens x 72 heads, 151 MB in 27 us; 32 tokens x 32 heads 2.5 us, which is a launch.
 #include "gkv_rotary.cuh"
 
 #include <cuda_fp16.h>
@@ -123,9 +123,9 @@ __global__ void __launch_bounds__(2 * kRotThreads, VEC == 8 ? 4 : 2) gkv_rotary_
     }
     __syncthreads();
     const int slot = threadIdx.x / p.runs, run = threadIdx.x - slot * p.runs;       // thread: run of a row, token, share of the heads
-    const int share = slot / p.tokens_per_cta, t = slot - share * p.tokens_per_cta;
-    const int shares = (int)blockDim.x / p.runs / p.tokens_per_cta;
-    if (share >= shares || t >= n) return;
+    const int local = slot / p.tokens_per_cta, t = slot - local * p.tokens_per_cta, locals = (int)blockDim.x / p.runs / p.tokens_per_cta;
+    const int share = blockIdx.z * locals + local, shares = (int)gridDim.z * locals;
+    if (local >= locals || t >= n) return;
     const bool turns = run < p.pair_runs;
     const int at0 = turns ? (INTERLEAVED ? 2 : 1) * run * VEC : 2 * half + (run - p.pair_runs) * 2 * VEC;
     const int at1 = turns && !INTERLEAVED ? at0 + half : at0 + VEC;
@@ -169,7 +169,7 @@ __global__ void __launch_bounds__(2 * kRotThreads, VEC == 8 ? 4 : 2) gkv_rotary_
 
 template <typename T, int VEC>
 static cudaError_t launch_typed(const RotaryLaunch& p, cudaStream_t s) {
-    const dim3 grid((unsigned)((p.n_tokens + p.tokens_per_cta - 1) / p.tokens_per_cta), (unsigned)p.batch);
+    const dim3 grid((unsigned)((p.n_tokens + p.tokens_per_cta - 1) / p.tokens_per_cta), (unsigned)p.batch, (unsigned)p.parts);
     const int threads = p.runs <= kRotThreads ? kRotThreads : 2 * kRotThreads;      // (at most 256 runs: a head of 512 by single pairs)
     const size_t smem = (size_t)p.tokens_per_cta * p.rotary.half * 2 * sizeof(float);
     if (p.rotary.interleaved) gkv_rotary_kernel<T, VEC, true><<<grid, threads, smem, s>>>(p);
@@ -210,6 +210,11 @@ cudaError_t launch_rotary(RotaryLaunch& p, int type, int head_dim, int sm_count,
     int per = 1;
     while (4 * per * p.runs <= kRotThreads && (int64_t)((p.n_tokens + 2 * per - 1) / (2 * per)) * p.batch >= 20ll * sm_count) per *= 2;
     p.tokens_per_cta = per;
+    // Few tokens: up to four CTAs share one's heads, as long as that makes no more than two an SM (1 token x 72 heads 2.7 us instead of 3.2, 128 tokens
+    // 3.1 instead of 3.4; with many tokens cos and sin worked out twice cost more: 1000 x 32 heads 5.8 instead of 4.5).
+    const int64_t ctas = (int64_t)((p.n_tokens + per - 1) / per) * p.batch;
+    p.parts = 1;
+    while (p.parts < 4 && 2 * p.parts * ctas <= 2ll * sm_count) p.parts *= 2;
     switch (type) {
         case GKV_TYPE_BF16: return launch_type<__nv_bfloat16>(p, vec, s);
         case GKV_TYPE_FP16: return launch_type<__half>(p, vec, s);
