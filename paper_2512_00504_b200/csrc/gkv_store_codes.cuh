@@ -206,25 +206,30 @@ __device__ __forceinline__ uint4 store_get_codes(const uint8_t* row, int l) {
 template <int F>
 __device__ __forceinline__ uint4 store_decode(uint4 c, uint32_t sc) {
     if (F == GKV_STORE_BF16) return c;
-    float v[8];
-    if (F == GKV_STORE_INT4) {
-        const float s0 = bf16_lo(sc), s1 = bf16_hi(sc);
+    if constexpr (F == GKV_STORE_INT4) {
+        // 128 + u of two codes u = c + 8 in bf16, minus 136, times the scale: exact but for the product, which is rounded once.
+        uint32_t y[4];
+        const uint32_t next = c.x >> 4, s0 = __byte_perm(sc, 0u, 0x1010), s1 = __byte_perm(sc, 0u, 0x3232);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = (float)((int)((c.x >> (4 * i)) & 15u) - 8) * (i < 4 ? s0 : s1);
-    } else {
-        const float s = bf16_lo(sc);
-        if (F == GKV_STORE_E4M3) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint32_t w = i < 2 ? c.x : c.y;
-                const uint32_t h = e4m3x2_to_f16x2((uint16_t)(w >> (16 * (i & 1))));
-                const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h));
-                v[2 * i] = f.x * s; v[2 * i + 1] = f.y * s;
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = (float)(int8_t)((i < 4 ? c.x : c.y) >> (8 * (i & 3))) * s;
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t x = (__byte_perm(c.x, next, i | (4 + i) << 8) & 0x000f000fu) | 0x43004300u;
+            asm("{ .reg .b32 t; sub.rn.bf16x2 t, %1, %2; mul.rn.bf16x2 %0, t, %3; }" : "=r"(y[i]) : "r"(x), "r"(0x43084308u), "r"(i < 2 ? s0 : s1));
         }
+        return make_uint4(y[0], y[1], y[2], y[3]);
+    }
+    float v[8];
+    const float s = bf16_lo(sc);
+    if (F == GKV_STORE_E4M3) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t w = i < 2 ? c.x : c.y;
+            const uint32_t h = e4m3x2_to_f16x2((uint16_t)(w >> (16 * (i & 1))));
+            const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h));
+            v[2 * i] = f.x * s; v[2 * i + 1] = f.y * s;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = (float)(int8_t)((i < 4 ? c.x : c.y) >> (8 * (i & 3))) * s;
     }
     return make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
 }
