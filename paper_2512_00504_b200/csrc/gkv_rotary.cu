@@ -9,6 +9,7 @@
 // Measured (bytes read and written): 8 x 8192 tokens x 32 heads in bf16, 1.07 GB in 166 us, 6.5 TB/s; 4 x 4096 x 40 in fp32, half of each head
 // turned, 0.67 GB in 105 us, 6.4 TB/s; 4097 tokens x 72 heads, 151 MB in 27 us; 32 tokens x 32 heads 2.5 us, which is a launch.
 #include "gkv_rotary.cuh"
+#include "gkv_store_rows.h"
 
 #include <cuda_fp16.h>
 #include <string.h>
@@ -110,9 +111,8 @@ template <typename T, int VEC, bool INTERLEAVED>
 __global__ void __launch_bounds__(2 * kRotThreads, VEC == 8 ? 4 : 2) gkv_rotary_kernel(const RotaryLaunch p) {
     extern __shared__ __align__(16) float s_table[];
     const int b = blockIdx.y, t0 = blockIdx.x * p.tokens_per_cta, half = p.rotary.half;
-    int n = p.count ? min(p.count[b], p.n_tokens) : p.n_tokens;
-    n = min(n - t0, p.tokens_per_cta);
-    if (n <= 0) return;
+    const int n = tokens_here(p.count ? p.count[b] : p.n_tokens, p.n_tokens, t0, p.tokens_per_cta);
+    if (n == 0) return;
     float *s_cos = s_table, *s_sin = s_table + p.tokens_per_cta * half;
     for (int i = threadIdx.x; i < n * half; i += blockDim.x) {
         const int t = i / half, pair = i - t * half;

@@ -1,4 +1,5 @@
-// Which tokens of a run a store copy moves. Plain C++, so that a host compiler can check the arithmetic over its whole range.
+// Which tokens of a run a store copy moves, and which of a block's the rotation turns. Plain C++, so that a host compiler can check the
+// arithmetic over its whole range.
 #pragma once
 
 #include <stdint.h>
@@ -24,6 +25,13 @@ GKV_HOST_DEVICE RunRows run_rows(int32_t first, int32_t count, int n_tokens, int
     const int row0 = (first > capacity ? capacity : first < -(1 << 30) ? -(1 << 30) : first) + t0;
     const int left = n - t0, room = capacity - row0, hi = left < room ? left : room, lo = -row0;
     return {lo < 0 ? 0 : lo > kRun ? kRun : lo, hi < 0 ? 0 : hi > kRun ? kRun : hi};
+}
+
+// How many of the tokens t0 .. t0 + per - 1 are below a sequence's count (below 0 as 0, above n_tokens as n_tokens), whatever the
+// caller's array holds.
+GKV_HOST_DEVICE int tokens_here(int32_t count, int n_tokens, int t0, int per) {
+    const int left = (count < 0 ? 0 : count < n_tokens ? count : n_tokens) - t0;
+    return left < 0 ? 0 : left < per ? left : per;
 }
 
 }  // namespace gkv
