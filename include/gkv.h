@@ -531,11 +531,20 @@ gkv_status gkv_pages_attn_workspace(const gkv_pages* pages, int32_t batch, uint6
  *                 (device int32[batch]; NULL: the last row's number, which is len[i] with a new row and len[i] - 1 without)
  *   out, lse, len, max_len and precision as in gkv_store_attn; a length that does not fit width * page_size gives NaN and nothing is
  *   written. A row whose place in the table holds no page makes the sequence's out and lse NaN (for the new row: it is not written either);
- *   nothing outside the buffers is touched.
+ *   nothing outside the buffers is touched. A wait that expires (none should) makes NaN of what was waited for.
  * Errors: as gkv_pages_append and gkv_store_attn; INVALID_ARG (workspace_bytes too small for table->batch). */
 gkv_status gkv_pages_attn(const gkv_pages* pages, const gkv_page_table* table, const int32_t* len, int32_t max_len, const void* q,
                           int64_t q_stride, const void* k_new, const void* v_new, int64_t kv_stride, const gkv_rotary* rotary,
                           const int32_t* pos, void* out, float* lse, void* workspace, uint64_t workspace_bytes, void* stream);
+
+/* Fault handling check: gkv_pages_attn, whose warps take every wait from their step `step` on (counted from 0; a step is 16 or 32 keys) for
+ * expired, which takes that path for real: what they attend to from there on becomes NaN, and they end once the copies under way have
+ * arrived. New rows are appended all the same. Errors: as gkv_pages_attn; INVALID_ARG (step < 0 or 2^31 - 1), UNSUPPORTED (a call so short
+ * that it is made without such waits). */
+gkv_status gkv_selftest_pages_wait(int32_t step, const gkv_pages* pages, const gkv_page_table* table, const int32_t* len, int32_t max_len,
+                                   const void* q, int64_t q_stride, const void* k_new, const void* v_new, int64_t kv_stride,
+                                   const gkv_rotary* rotary, const int32_t* pos, void* out, float* lse, void* workspace,
+                                   uint64_t workspace_bytes, void* stream);
 
 /* Memory model of the paper's appendix "Memory Analysis": bytes of the full KV cache at
  * seq_len tokens, of the compressed cache ((b + s) rows instead of seq_len), and of the score

@@ -220,8 +220,9 @@ def lib() -> ctypes.CDLL:
         L.gkv_pages_read.argtypes = [P(gkv_pages), P(gkv_page_table), vp, vp, i64, i64, i64, vp, vp, i32, vp]
         L.gkv_pages_attn_workspace.argtypes = [P(gkv_pages), i32, P(u64)]
         L.gkv_pages_attn.argtypes = [P(gkv_pages), P(gkv_page_table), vp, i32, vp, i64, vp, vp, i64, P(gkv_rotary), vp, vp, vp, vp, u64, vp]
+        L.gkv_selftest_pages_wait.argtypes = [i32] + L.gkv_pages_attn.argtypes
         for name in ("gkv_rotary_frequencies", "gkv_rotary_turns", "gkv_rotary_apply", "gkv_pages_query_sizes", "gkv_pages_append",
-                     "gkv_pages_read", "gkv_pages_attn_workspace", "gkv_pages_attn"):
+                     "gkv_pages_read", "gkv_pages_attn_workspace", "gkv_pages_attn", "gkv_selftest_pages_wait"):
             getattr(L, name).restype = ctypes.c_int
         for name in ("gkv_store_query_sizes", "gkv_store_write", "gkv_store_read", "gkv_store_attn_workspace",
                      "gkv_store_attn", "gkv_decode_attn_prefix", "gkv_selftest_prefix_wait"):
@@ -460,6 +461,19 @@ def gkv_pages_attn_workspace(pages: gkv_pages, batch: int) -> int:
     out = ctypes.c_uint64()
     _check(lib().gkv_pages_attn_workspace(ctypes.byref(pages), _int32(batch, "batch"), ctypes.byref(out)), "gkv_pages_attn_workspace")
     return out.value
+
+
+def gkv_selftest_pages_wait(store: "PagedStore", step, table, length, q, out, k_new=None, v_new=None, lse=None, max_len=0):
+    """PagedStore.attn without a rotation, whose warps take every wait from their step `step` on for expired. All tensors contiguous."""
+    import torch
+    dev, batch, bf16 = store.device, table.shape[0], torch.bfloat16
+    t = gkv_page_table(_tensor(table, "table", torch.int32, table.shape, dev), table.shape[1], batch, table.shape[1])
+    new = [None if x is None else _tensor(x, n, bf16, (batch, store.h_kv, 128), dev) for x, n in ((k_new, "k_new"), (v_new, "v_new"))]
+    _check(lib().gkv_selftest_pages_wait(
+        _int32(step, "step"), ctypes.byref(store.desc), ctypes.byref(t), _tensor(length, "length", torch.int32, (batch,), dev),
+        _int32(max_len, "max_len"), _tensor(q, "q", bf16, (batch, store.h_q, 128), dev), store.h_q * 128, *new, store.h_kv * 128, None, None,
+        _tensor(out, "out", bf16, (batch, store.h_q, 128), dev), None if lse is None else _tensor(lse, "lse", torch.float32, (batch, store.h_q), dev),
+        *store._ws, torch.cuda.current_stream(dev).cuda_stream), "gkv_selftest_pages_wait")
 
 
 # ------------------------------------------------------------------ buffer holder

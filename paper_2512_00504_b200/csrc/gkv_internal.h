@@ -220,6 +220,7 @@ struct PagesCopyLaunch {       // append / read
 constexpr int kStreamRecHead = 48, kStreamRecFloats = kStreamRecHead + kHeadDimHost * 8;
 constexpr int kStreamLeast = 4;
 constexpr int kStreamMaxWarps = 2560;
+constexpr int kNeverExpire = 0x7fffffff;
 // (The names that it shares with StoreAttnLaunch are those of the code that both kinds of attention have in common. It is a
 // struct of its own because the host pays for the length of what a launch carries.)
 struct PagesAttnLaunch {
@@ -291,7 +292,7 @@ cudaError_t launch_rotary(RotaryLaunch& p, int type, int head_dim, int sm_count,
 cudaError_t launch_pages_append(const PagesCopyLaunch& p, cudaStream_t s);
 cudaError_t launch_pages_read(const PagesCopyLaunch& p, cudaStream_t s);
 cudaError_t launch_pages_attn(const PagesAttnLaunch& p, int format, cudaStream_t s);        // a cluster (or one CTA) a unit
-cudaError_t launch_pages_stream(const PagesAttnLaunch& p, int format, int ctas, cudaStream_t s);   // equal shares for all warps, then the merge
+cudaError_t launch_pages_stream(const PagesAttnLaunch& p, int format, int ctas, int expire, cudaStream_t s);   // equal shares for all warps, then the merge
 int pages_attn_ctas_per_sm(int format);
 int pages_stream_warps_per_sm(const PagesAttnLaunch& p, int format);
 int device_sm_count();                                                                      // of the current device

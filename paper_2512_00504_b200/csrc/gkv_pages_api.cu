@@ -117,6 +117,43 @@ gkv_status copy_args(const gkv_pages* g, const gkv_page_table* t, const void* k,
     return GKV_OK;
 }
 
+// gkv_pages_attn; expire: the step of every warp from which on its waits are taken for expired.
+gkv_status run_attn(const gkv_pages* pages, const gkv_page_table* table, const int32_t* len, int32_t max_len, const void* q,
+                    int64_t q_stride, const void* k_new, const void* v_new, int64_t kv_stride, const gkv_rotary* rotary,
+                    const int32_t* pos, void* out, float* lse, void* workspace, uint64_t workspace_bytes, int expire, void* stream) {
+    gkv_status st = check_pages(pages, table);
+    if (st != GKV_OK) return st;
+    if (!len || !q || !out || misaligned(len, 4) || misaligned(q, 16) || misaligned(out, 16) || misaligned(lse, 4) || misaligned(pos, 4))
+        return GKV_ERR_INVALID_ARG;
+    if ((k_new == nullptr) != (v_new == nullptr) || misaligned(k_new, 16) || misaligned(v_new, 16)) return GKV_ERR_INVALID_ARG;
+    if (q_stride < 0 || q_stride % 8 != 0 || (k_new && (kv_stride < 0 || kv_stride % 8 != 0))) return GKV_ERR_INVALID_ARG;
+    const int capacity = table->width * pages->page_size;
+    if (max_len < 0 || max_len > capacity) return GKV_ERR_INVALID_ARG;
+    if (rotary) {
+        st = check_rotary(rotary);
+        if (st != GKV_OK) return st;
+        if (rotary->head_dim != kHeadDim) return GKV_ERR_INVALID_ARG;
+    }
+    if (!workspace || misaligned(workspace, 16) || workspace_bytes < kStreamBytes) return GKV_ERR_INVALID_ARG;
+
+    PagesAttnLaunch p = {};
+    p.pages = view(pages, table);
+    p.rotary = view(rotary);
+    p.pos = pos; p.len = len;
+    p.q = static_cast<const __nv_bfloat16*>(q);
+    p.k_new = static_cast<const __nv_bfloat16*>(k_new); p.v_new = static_cast<const __nv_bfloat16*>(v_new);
+    p.q_stride = q_stride; p.kv_stride = kv_stride;
+    p.out = static_cast<__nv_bfloat16*>(out); p.lse = lse; p.own_part = static_cast<float*>(workspace);
+    p.batch = table->batch; p.h_q = pages->n_q_heads; p.h_kv = pages->n_kv_heads; p.g = p.h_q / p.h_kv; p.capacity = capacity;
+    p.scale_log2 = (float)(1.4426950408889634 / sqrt((double)kHeadDim));
+    const cudaStream_t s = static_cast<cudaStream_t>(stream);
+    const int stream_ctas = pages_plan(&p, pages->format, max_len > 0 ? max_len : capacity, device_sm_count());
+    if (expire != kNeverExpire && !stream_ctas) return GKV_ERR_UNSUPPORTED;
+    const cudaError_t e = stream_ctas ? launch_pages_stream(p, pages->format, stream_ctas, expire, s) : launch_pages_attn(p, pages->format, s);
+    if (e != cudaSuccess) { (void)cudaGetLastError(); return GKV_ERR_CUDA; }
+    return GKV_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -255,36 +292,17 @@ gkv_status gkv_pages_attn_workspace(const gkv_pages* pages, int32_t batch, uint6
 gkv_status gkv_pages_attn(const gkv_pages* pages, const gkv_page_table* table, const int32_t* len, int32_t max_len, const void* q,
                           int64_t q_stride, const void* k_new, const void* v_new, int64_t kv_stride, const gkv_rotary* rotary,
                           const int32_t* pos, void* out, float* lse, void* workspace, uint64_t workspace_bytes, void* stream) {
-    gkv_status st = check_pages(pages, table);
-    if (st != GKV_OK) return st;
-    if (!len || !q || !out || misaligned(len, 4) || misaligned(q, 16) || misaligned(out, 16) || misaligned(lse, 4) || misaligned(pos, 4))
-        return GKV_ERR_INVALID_ARG;
-    if ((k_new == nullptr) != (v_new == nullptr) || misaligned(k_new, 16) || misaligned(v_new, 16)) return GKV_ERR_INVALID_ARG;
-    if (q_stride < 0 || q_stride % 8 != 0 || (k_new && (kv_stride < 0 || kv_stride % 8 != 0))) return GKV_ERR_INVALID_ARG;
-    const int capacity = table->width * pages->page_size;
-    if (max_len < 0 || max_len > capacity) return GKV_ERR_INVALID_ARG;
-    if (rotary) {
-        st = check_rotary(rotary);
-        if (st != GKV_OK) return st;
-        if (rotary->head_dim != kHeadDim) return GKV_ERR_INVALID_ARG;
-    }
-    if (!workspace || misaligned(workspace, 16) || workspace_bytes < kStreamBytes) return GKV_ERR_INVALID_ARG;
+    return run_attn(pages, table, len, max_len, q, q_stride, k_new, v_new, kv_stride, rotary, pos, out, lse, workspace, workspace_bytes,
+                    kNeverExpire, stream);
+}
 
-    PagesAttnLaunch p = {};
-    p.pages = view(pages, table);
-    p.rotary = view(rotary);
-    p.pos = pos; p.len = len;
-    p.q = static_cast<const __nv_bfloat16*>(q);
-    p.k_new = static_cast<const __nv_bfloat16*>(k_new); p.v_new = static_cast<const __nv_bfloat16*>(v_new);
-    p.q_stride = q_stride; p.kv_stride = kv_stride;
-    p.out = static_cast<__nv_bfloat16*>(out); p.lse = lse; p.own_part = static_cast<float*>(workspace);
-    p.batch = table->batch; p.h_q = pages->n_q_heads; p.h_kv = pages->n_kv_heads; p.g = p.h_q / p.h_kv; p.capacity = capacity;
-    p.scale_log2 = (float)(1.4426950408889634 / sqrt((double)kHeadDim));
-    const cudaStream_t s = static_cast<cudaStream_t>(stream);
-    const int stream_ctas = pages_plan(&p, pages->format, max_len > 0 ? max_len : capacity, device_sm_count());
-    const cudaError_t e = stream_ctas ? launch_pages_stream(p, pages->format, stream_ctas, s) : launch_pages_attn(p, pages->format, s);
-    if (e != cudaSuccess) { (void)cudaGetLastError(); return GKV_ERR_CUDA; }
-    return GKV_OK;
+gkv_status gkv_selftest_pages_wait(int32_t step, const gkv_pages* pages, const gkv_page_table* table, const int32_t* len, int32_t max_len,
+                                   const void* q, int64_t q_stride, const void* k_new, const void* v_new, int64_t kv_stride,
+                                   const gkv_rotary* rotary, const int32_t* pos, void* out, float* lse, void* workspace,
+                                   uint64_t workspace_bytes, void* stream) {
+    if (step < 0 || step == kNeverExpire) return GKV_ERR_INVALID_ARG;
+    return run_attn(pages, table, len, max_len, q, q_stride, k_new, v_new, kv_stride, rotary, pos, out, lse, workspace, workspace_bytes, step,
+                    stream);
 }
 
 }  // extern "C"

@@ -24,6 +24,7 @@
 // to 65535 keys in bf16 216 (206). 2 x 8 heads of up to 131071 in 4 bits 83 (42). 16-bit rows are bound by HBM. With 4-bit rows the warps
 // issue in 60% of all cycles, 420 instructions a tile, of which 170 unpack codes: instructions and what they wait for bound it.
 #include "gkv_pages.cuh"
+#include "gkv_pages_steps.h"
 #include "gkv_rotary.cuh"
 #include "gkv_store_rows.cuh"
 
@@ -126,8 +127,9 @@ __device__ __forceinline__ int stream_owner(int64_t step, int64_t per) {
 // How rows lie: anyhow; those of a tile, or of a whole step, next to one another in one page.
 enum { kApart = 0, kTiles = 1, kSteps = 2 };
 
+// expire: the step of every warp from which on waits are taken for expired (self-test; kNeverExpire otherwise).
 template <int F, int LIE>
-__global__ void __launch_bounds__(32, stream_warps(F, LIE != kApart)) gkv_pages_stream_kernel(const PagesAttnLaunch p) {
+__global__ void __launch_bounds__(32, stream_warps(F, LIE != kApart)) gkv_pages_stream_kernel(const PagesAttnLaunch p, const int expire) {
     using Warp = StreamWarp<F>;
     constexpr int NG = value_groups(F), S = Warp::kStages, TILES = Warp::kTiles, KEYS = Warp::kKeys, kRow = Warp::kRow, kScales = Warp::kScales;
     constexpr bool kScaled = F != GKV_STORE_BF16, TOGETHER = LIE != kApart;
@@ -333,8 +335,7 @@ __global__ void __launch_bounds__(32, stream_warps(F, LIE != kApart)) gkv_pages_
     RunningRows<F> r;
     bool whole = at.tile == 0, ok = true;                  // the unit is ours from its first tile on; no wait has run out
     bool first_unit = true;
-    int stage = 0;
-    uint32_t parity = 0;
+    RingPlace<S> place;                                    // of the step that is waited for; stays where a wait has run out
     __syncwarp();
     if (!TOGETHER) {                                       // scales by ordinary loads: a tile ahead
         take_scales(tk, 0, 0, 0);
@@ -344,7 +345,11 @@ __global__ void __launch_bounds__(32, stream_warps(F, LIE != kApart)) gkv_pages_
     r.start(sw.v, lane);
     for (int step = 0; step < steps; ++step) {
         // ---- a step
-        if (ok) ok = __all_sync(0xffffffffu, mbar_wait_bounded(smem_u32(&sw.full[stage]), parity));
+        const int stage = place.stage;
+        if (ok && (step >= expire || !__all_sync(0xffffffffu, mbar_wait_bounded(smem_u32(&sw.full[stage]), place.parity)))) {
+            ok = false;
+            issued -= step;                                // what is under way: this step's copies and those behind it
+        }
         const int left = at.len + added - at.tile * KEYS;                        // keys from this step's first on
         const bool last = at.tile == at.tiles - 1, bad = !ok || (lost >> stage & 1u);
         if (last) {
@@ -461,11 +466,11 @@ __global__ void __launch_bounds__(32, stream_warps(F, LIE != kApart)) gkv_pages_
         }
         __syncwarp();                                      // the slot has been read
         if (issued < steps && ok) issue(stage);
-        if (++stage == S) { stage = 0; parity ^= 1; }
+        if (ok) place.next();
         if (!TOGETHER && step + 1 < steps) {
             __syncwarp();
-            take_scales(tk, 0, stage, 0);
-            take_scales(tv, 1, stage, 0);
+            take_scales(tk, 0, place.stage, 0);
+            take_scales(tv, 1, place.stage, 0);
         }
         // ---- the end of the unit, or of this warp's part of it
         if (last || step + 1 == steps) {
@@ -520,8 +525,8 @@ __global__ void __launch_bounds__(32, stream_warps(F, LIE != kApart)) gkv_pages_
             stream_next<KEYS>(p, at);
         }
     }
-    if (!ok)                                               // what is still on its way gets a bounded time to arrive
-        for (int s = 0; s < S; ++s) mbar_wait_bounded(smem_u32(&sw.full[s]), s < stage ? parity ^ 1 : parity);
+    // What is still on its way gets a bounded time to arrive, before this shared memory is another's.
+    if (!ok) drain_ring(place, issued, [&](int s, uint32_t parity) { mbar_wait_bounded(smem_u32(&sw.full[s]), parity); });
 }
 
 // Joins the partial results of a unit: a running softmax over them, kJoin at a time, all of whose loads are under way before the first is
@@ -669,14 +674,14 @@ __global__ void __launch_bounds__(256 / kSlices, kSlices == 2 ? 8 : 2) gkv_pages
 }
 
 template <int F, int LIE>
-static cudaError_t launch_stream(const PagesAttnLaunch& p, int ctas, cudaStream_t s) {
+static cudaError_t launch_stream(const PagesAttnLaunch& p, int ctas, int expire, cudaStream_t s) {
     constexpr int kSmem = (int)sizeof(StreamWarp<F>);
     static_assert(kSmem + 1024 <= 228 * 1024 / stream_warps(F, LIE != kApart), "room for all warps of an SM");
     const auto kernel = gkv_pages_stream_kernel<F, LIE>;
     // a property of the function on the current device; setting it again costs less than finding out whether it is set
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
     if (e != cudaSuccess) return e;
-    kernel<<<(unsigned)ctas, 32, kSmem, s>>>(p);
+    kernel<<<(unsigned)ctas, 32, kSmem, s>>>(p, expire);
     e = cudaGetLastError();
     if (e != cudaSuccess) return e;
     const int units = p.batch * p.h_kv;
@@ -698,18 +703,18 @@ static cudaError_t launch_stream(const PagesAttnLaunch& p, int ctas, cudaStream_
 static bool rows_together(const PagesAttnLaunch& p) { return p.pages.token_rows == 1 && p.pages.page_size % kTile == 0; }
 int pages_stream_warps_per_sm(const PagesAttnLaunch& p, int format) { return stream_warps(format, rows_together(p)); }
 template <int F>
-static cudaError_t launch_format(const PagesAttnLaunch& p, int ctas, cudaStream_t s) {
-    if (!rows_together(p)) return launch_stream<F, kApart>(p, ctas, s);
+static cudaError_t launch_format(const PagesAttnLaunch& p, int ctas, int expire, cudaStream_t s) {
+    if (!rows_together(p)) return launch_stream<F, kApart>(p, ctas, expire, s);
     if constexpr (stream_tiles(F) > 1)
-        if (p.pages.page_size % StreamWarp<F>::kKeys != 0) return launch_stream<F, kTiles>(p, ctas, s);
-    return launch_stream<F, kSteps>(p, ctas, s);
+        if (p.pages.page_size % StreamWarp<F>::kKeys != 0) return launch_stream<F, kTiles>(p, ctas, expire, s);
+    return launch_stream<F, kSteps>(p, ctas, expire, s);
 }
-cudaError_t launch_pages_stream(const PagesAttnLaunch& p, int format, int ctas, cudaStream_t s) {
+cudaError_t launch_pages_stream(const PagesAttnLaunch& p, int format, int ctas, int expire, cudaStream_t s) {
     switch (format) {
-        case GKV_STORE_BF16: return launch_format<GKV_STORE_BF16>(p, ctas, s);
-        case GKV_STORE_E4M3: return launch_format<GKV_STORE_E4M3>(p, ctas, s);
-        case GKV_STORE_INT8: return launch_format<GKV_STORE_INT8>(p, ctas, s);
-        default:             return launch_format<GKV_STORE_INT4>(p, ctas, s);
+        case GKV_STORE_BF16: return launch_format<GKV_STORE_BF16>(p, ctas, expire, s);
+        case GKV_STORE_E4M3: return launch_format<GKV_STORE_E4M3>(p, ctas, expire, s);
+        case GKV_STORE_INT8: return launch_format<GKV_STORE_INT8>(p, ctas, expire, s);
+        default:             return launch_format<GKV_STORE_INT4>(p, ctas, expire, s);
     }
 }
 

@@ -4,6 +4,7 @@ import pytest
 import torch
 
 import paper_2512_00504_b200 as gkv
+from test_gpu_pages import deal_pages, randn as rows
 from test_gpu_rotary import DEV, check, gen, ints, plain, randn
 
 pytestmark = pytest.mark.gpu
@@ -33,3 +34,44 @@ def test_counts_at_the_lower_end_of_their_range(batch, tokens, heads):
     y[~turned] = 0
     q[~turned] = 0
     check(rot, "bf16", pos, q, y)
+
+
+# ---------------------------------------------------------------------------------------------- attention
+def cache(fmt, seed, lens, page, h_q, h_kv, token_major=False):
+    """Pages full of rows, some of them of sequences of these lengths (and one row more), and their table."""
+    table, n_pages = deal_pages(seed, [max(n, 0) + 1 for n in lens], page)
+    st = gkv.PagedStore(fmt, pages=n_pages, page_size=page, h_q=h_q, h_kv=h_kv, max_batch=len(lens), token_major=token_major, device=DEV)
+    g = gen(seed)
+    every = torch.arange(n_pages, dtype=torch.int32, device=DEV)[:, None]
+    st.append(every, rows(g, n_pages, page, h_kv, 128), rows(g, n_pages, page, h_kv, 128))
+    return st, table, g
+
+
+@pytest.mark.parametrize("fmt,page,token_major", [("bf16", 16, False), ("bf16", 5, False), ("e4m3", 64, False), ("e4m3", 16, True), ("int8", 16, False),
+                                                  ("int4", 32, False), ("int4", 48, False), ("int4", 7, False)])
+def test_waits_that_are_taken_for_expired(fmt, page, token_major):
+    """Every warp gives up at its first, second .. step: no number comes out where one is missing, new rows are appended as ever, and the call
+    after that is right. (Here a warp has four steps, so that none is left to a step of five.)"""
+    lens, h_q, h_kv = [5000, 3001], 8, 2
+    st, table, g = cache(fmt, 61, lens, page, h_q, h_kv, token_major)
+    tab, n = ints(table), ints(lens)
+    q, k1, v1 = rows(g, 2, h_q, 128), rows(g, 2, h_kv, 128), rows(g, 2, h_kv, 128)
+    buffers = [t for t in (st.k, st.v, st.k_scale, st.v_scale) if t is not None]
+    before = [t.view(torch.uint8).clone() for t in buffers]
+    out, lse = torch.zeros_like(q), torch.zeros(2, h_q, device=DEV)
+    st.attn(tab, n, q, out, k_new=k1, v_new=v1, lse=lse)
+    after = [t.view(torch.uint8).clone() for t in buffers]
+    assert torch.isfinite(out).all()
+    for step in (0, 1, 2, 3, 4, 3, 0):
+        for t, b in zip(buffers, before):
+            t.view(torch.uint8).copy_(b)
+        o, l = torch.zeros_like(out), torch.zeros_like(lse)
+        gkv.gkv_selftest_pages_wait(st, step, tab, n, q, o, k_new=k1, v_new=v1, lse=l)
+        if step < 4:
+            assert torch.isnan(o).all() and torch.isnan(l).all()
+        else:
+            assert torch.equal(o, out) and torch.equal(l, lse)
+        assert all(torch.equal(t.view(torch.uint8), a) for t, a in zip(buffers, after))
+        o, l = torch.zeros_like(out), torch.zeros_like(lse)
+        st.attn(tab, n, q, o, k_new=k1, v_new=v1, lse=l)
+        assert torch.equal(o, out) and torch.equal(l, lse)
