@@ -58,6 +58,12 @@ bool current_stream(int device, void** stream) {
     *stream = c10::cuda::getCurrentCUDAStream(device).stream();
     return true;
 }
+// A tensor that a call has written counts as changed, so that a backward pass that has kept it says so instead of using what it holds now.
+void changed(PyObject* o) {
+    if (o == Py_None) return;
+    const at::Tensor& t = THPVariable_Unpack(o);
+    if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
 bool arguments(Py_ssize_t n, Py_ssize_t want, const char* what) {
     if (n != want) PyErr_Format(PyExc_TypeError, "%s takes %zd arguments, got %zd", what, want, n);
     return n == want;
@@ -132,6 +138,10 @@ PyObject* copy(PyObject*, PyObject* const* a, Py_ssize_t n) try {
                                         (const int32_t*)count, tokens, stream)
                                : g_write(s, k->data_ptr(), v->data_ptr(), strides[0], strides[1], strides[2], (const int32_t*)first,
                                          (const int32_t*)count, tokens, stream);
+    if (read && st == GKV_OK) {
+        changed(a[3]);
+        changed(a[4]);
+    }
     return PyLong_FromLong(st);
 } catch (const std::exception& e) {
     PyErr_SetString(PyExc_RuntimeError, e.what());
@@ -157,7 +167,12 @@ PyObject* attn(PyObject*, PyObject* const* a, Py_ssize_t n) try {
         !pointer(a[8], "out", at::kBFloat16, qs, device, false, &out) || !pointer(a[9], "lse", at::kFloat, ls, device, true, &lse) ||
         !current_stream(device, &stream))
         return nullptr;
-    return PyLong_FromLong(g_attn(s, (const int32_t*)length, (int32_t)max_len, q, k_new, v_new, prefix, out, (float*)lse, ws, ws_bytes, stream));
+    const gkv_status st = g_attn(s, (const int32_t*)length, (int32_t)max_len, q, k_new, v_new, prefix, out, (float*)lse, ws, ws_bytes, stream);
+    if (st == GKV_OK) {
+        changed(a[8]);
+        changed(a[9]);
+    }
+    return PyLong_FromLong(st);
 } catch (const std::exception& e) {
     PyErr_SetString(PyExc_RuntimeError, e.what());
     return nullptr;
@@ -244,6 +259,10 @@ PyObject* pages_copy(PyObject*, PyObject* const* a, Py_ssize_t n) try {
                             tokens, stream)
              : g_pages_append(s, &table, k->data_ptr(), v->data_ptr(), strides[0], strides[1], strides[2], (const int32_t*)first,
                               (const int32_t*)count, tokens, rotary, pos, ps[0], ps[1], stream);
+    if (read && st == GKV_OK) {
+        changed(a[4]);
+        changed(a[5]);
+    }
     return PyLong_FromLong(st);
 } catch (const std::exception& e) {
     PyErr_SetString(PyExc_RuntimeError, e.what());
@@ -282,8 +301,13 @@ PyObject* pages_attn(PyObject*, PyObject* const* a, Py_ssize_t n) try {
                      (long long)v_stride);
         return nullptr;
     }
-    return PyLong_FromLong(g_pages_attn(s, &table, (const int32_t*)length, (int32_t)max_len, q, q_stride, k_new, v_new, k_stride, rotary,
-                                        (const int32_t*)pos, out, (float*)lse, ws, ws_bytes, stream));
+    const gkv_status st = g_pages_attn(s, &table, (const int32_t*)length, (int32_t)max_len, q, q_stride, k_new, v_new, k_stride, rotary,
+                                       (const int32_t*)pos, out, (float*)lse, ws, ws_bytes, stream);
+    if (st == GKV_OK) {
+        changed(a[11]);
+        changed(a[12]);
+    }
+    return PyLong_FromLong(st);
 } catch (const std::exception& e) {
     PyErr_SetString(PyExc_RuntimeError, e.what());
     return nullptr;
@@ -342,8 +366,13 @@ PyObject* rotary(PyObject*, PyObject* const* a, Py_ssize_t n) try {
         return nullptr;
     if (t.size(0) > INT32_MAX || t.size(1) > INT32_MAX) return PyLong_FromLong(GKV_ERR_UNSUPPORTED);
     const int type = t.scalar_type() == at::kFloat ? GKV_TYPE_FP32 : t.scalar_type() == at::kHalf ? GKV_TYPE_FP16 : GKV_TYPE_BF16;
-    return PyLong_FromLong(g_rotary(r, type, (int32_t)t.size(0), (int32_t)t.size(1), pos, ps[0], ps[1], (const int32_t*)count, &q, two ? &k : nullptr,
-                                    transpose, stream));
+    const gkv_status st = g_rotary(r, type, (int32_t)t.size(0), (int32_t)t.size(1), pos, ps[0], ps[1], (const int32_t*)count, &q, two ? &k : nullptr,
+                                   transpose, stream);
+    if (st == GKV_OK) {
+        changed(a[5] != Py_None ? a[5] : a[3]);
+        if (two) changed(a[6] != Py_None ? a[6] : a[4]);
+    }
+    return PyLong_FromLong(st);
 } catch (const std::exception& e) {
     PyErr_SetString(PyExc_RuntimeError, e.what());
     return nullptr;

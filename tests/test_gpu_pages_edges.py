@@ -75,3 +75,41 @@ def test_waits_that_are_taken_for_expired(fmt, page, token_major):
         o, l = torch.zeros_like(out), torch.zeros_like(lse)
         st.attn(tab, n, q, o, k_new=k1, v_new=v1, lse=l)
         assert torch.equal(o, out) and torch.equal(l, lse)
+
+
+# ---------------------------------------------------------------------------------------------- next to a backward pass
+def test_written_tensors_count_as_changed():
+    """Every tensor that a call writes: a backward pass that has kept one refuses it, as after torch's own writes. Those that are only read, and
+    those of a refused call, do not."""
+    g = gen(64)
+    rot = gkv.Rotary(plain(128), device=DEV)
+    pos, n, tab = torch.zeros(1, 4, dtype=torch.int32, device=DEV), ints([3]), ints([[0]])
+    x, y, z, u = (rows(g, 1, 4, 2, 128) for _ in range(4))
+    q, out, lse, k1 = rows(g, 1, 2, 128), rows(g, 1, 2, 128), torch.zeros(1, 2, device=DEV), rows(g, 1, 2, 128)
+    paged = gkv.PagedStore("int8", pages=1, page_size=16, h_q=2, h_kv=2, max_batch=1, device=DEV)
+    flat = gkv.KVStore("int8", batch=1, h_q=2, h_kv=2, capacity=16, device=DEV)
+    read = (pos, n, tab, q, k1, x, y)
+    for call, written in (
+            (lambda: rot.apply(pos, z), [z]), (lambda: rot.apply(pos, z, u), [z, u]), (lambda: rot.apply(pos, x, q_out=z), [z]),
+            (lambda: rot.apply(pos, x, z, q_out=u), [u, z]), (lambda: paged.append(tab, x, y), []), (lambda: paged.read(tab, z, u), [z, u]),
+            (lambda: paged.attn(tab, n, q, out, k_new=k1, v_new=k1), [out]), (lambda: paged.attn(tab, n, q, out, lse=lse), [out, lse]),
+            (lambda: flat.write(x, y), []), (lambda: flat.read(z, u), [z, u]), (lambda: flat.attn(n, q, out, lse=lse), [out, lse])):
+        before = {id(t): t._version for t in (*read, z, u, out, lse)}
+        call()
+        for t in (*read, z, u, out, lse):
+            assert (t._version > before[id(t)]) == any(t is w for w in written)
+    before = x._version
+    with pytest.raises(gkv.GKVError):
+        rot.apply(pos, x, y, q_out=x, k_out=x)
+    assert x._version == before
+    leaf = torch.ones(1, 4, 2, 128, device=DEV, requires_grad=True)
+    h = leaf * 2
+    loss = (h * h).sum()
+    with torch.no_grad():
+        rot.apply(pos + 5, h)
+    with pytest.raises(RuntimeError, match="inplace"):
+        loss.backward()
+    with torch.inference_mode():
+        i = torch.ones(1, 4, 2, 128, device=DEV)
+    rot.apply(pos + 5, i)                                      # has no count of changes
+    assert not (i == 1).all()
