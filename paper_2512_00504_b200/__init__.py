@@ -711,7 +711,9 @@ class Rotary:
     def apply(self, pos, q, k=None, *, q_out=None, k_out=None, count=None, transpose=False):
         """Rotate q and k in one launch, in place or into q_out, k_out. q, k: [batch][tokens][their heads][head_dim] in bf16, fp16 or fp32, any
         strides whose last one is 1; pos: int32 [batch][tokens] on the device; count: int32 [batch], tokens from count[i] on are left as
-        they were. transpose turns the other way: given the gradients of what was rotated, it leaves those of q and k."""
+        they were. transpose turns the other way: given the gradients of what was rotated, it leaves those of q and k. Nothing is recorded for a
+        backward pass: tensors that require grad are refused unless gradients are off (torch.no_grad(), or within a torch.autograd.Function,
+        whose backward is the same call with transpose)."""
         _check(self._call.rotary(self.at, self.device.index, pos, q, k, q_out, k_out, count, transpose), "gkv_rotary_apply")
         self._call.in_use(self._held)
 

@@ -3,6 +3,7 @@
 // most decode-sized kernels run; here they take well under one.) It holds no state but the addresses of the library's functions,
 // so that it serves every build of the library.
 #include <Python.h>
+#include <c10/core/GradMode.h>
 #include <c10/cuda/CUDACachingAllocator.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -63,6 +64,14 @@ void changed(PyObject* o) {
     if (o == Py_None) return;
     const at::Tensor& t = THPVariable_Unpack(o);
     if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+// The calls record nothing for a backward pass. What needs a gradient is refused where one is being recorded, as torch refuses it of its
+// own functions that write to given tensors.
+bool outside_autograd(PyObject* o, const char* what) {
+    if (o == Py_None || !c10::GradMode::is_enabled() || !THPVariable_Unpack(o).requires_grad()) return true;
+    PyErr_Format(PyExc_ValueError, "%s requires grad, and this call records nothing for a backward pass: make it under torch.no_grad() (in "
+                 "a torch.autograd.Function, say), and turn the gradients with transpose=True", what);
+    return false;
 }
 bool arguments(Py_ssize_t n, Py_ssize_t want, const char* what) {
     if (n != want) PyErr_Format(PyExc_TypeError, "%s takes %zd arguments, got %zd", what, want, n);
@@ -357,6 +366,8 @@ PyObject* rotary(PyObject*, PyObject* const* a, Py_ssize_t n) try {
         PyErr_SetString(PyExc_ValueError, "k_out without k");
         return nullptr;
     }
+    if (!outside_autograd(a[3], "q") || !outside_autograd(a[4], "k") || !outside_autograd(a[5], "q_out") || !outside_autograd(a[6], "k_out"))
+        return nullptr;
     const int32_t* pos;
     int64_t ps[2];
     void *count, *stream;

@@ -3,6 +3,7 @@ import numpy as np
 import pytest
 import torch
 
+import pages_reference as pref
 import paper_2512_00504_b200 as gkv
 from test_gpu_pages import deal_pages, randn as rows
 from test_gpu_rotary import DEV, check, gen, ints, plain, randn
@@ -78,6 +79,64 @@ def test_waits_that_are_taken_for_expired(fmt, page, token_major):
 
 
 # ---------------------------------------------------------------------------------------------- next to a backward pass
+class Turn(torch.autograd.Function):
+    """The rotation in a model that is trained."""
+
+    @staticmethod
+    def forward(ctx, rot, pos, q, k):
+        ctx.rot = rot
+        ctx.save_for_backward(pos)
+        qo, ko = torch.empty_like(q), torch.empty_like(k)
+        rot.apply(pos, q, k, q_out=qo, k_out=ko)
+        return qo, ko
+
+    @staticmethod
+    def backward(ctx, dq, dk):
+        (pos,) = ctx.saved_tensors
+        dq, dk = dq.clone(), dk.clone()
+        ctx.rot.apply(pos, dq, dk, transpose=True)
+        return None, None, dq, dk
+
+
+def test_a_rotation_within_a_backward_pass():
+    """Gradients of a sum of products of turned q and k, against the same in fp64 by torch. Of q and k that are turned by rounded cos and sin the
+    product is off by what the tolerance of a rotation says of its factors; a gradient is one of them, times the weight, turned once more."""
+    g = gen(63)
+    q, k = (randn(g, "fp32", 2, 9, 3, 80).requires_grad_() for _ in range(2))
+    w = randn(g, "fp32", 2, 9, 3, 80)
+    pos = torch.randint(0, 3000, (2, 9), generator=g, device=DEV, dtype=torch.int32)
+    rot = gkv.Rotary(plain(40), head_dim=80, device=DEV)
+    qo, ko = Turn.apply(rot, pos, q, k)
+    (qo * ko * w).sum().backward()
+    angle = torch.from_numpy(pref.angles(rot.turns.cpu().numpy().view(np.uint64), pos.cpu().numpy())).to(DEV)[:, :, None]
+    c, s = torch.cos(angle), torch.sin(angle)
+
+    def turn(x):
+        a, b = x[..., :20], x[..., 20:40]
+        return torch.cat((a * c - b * s, b * c + a * s, x[..., 40:]), -1)
+
+    q64, k64 = (x.detach().double().requires_grad_() for x in (q, k))
+    (turn(q64) * turn(k64) * w.double()).sum().backward()
+    # numbers below 6, so a pair's magnitudes add up to less than 12 and a turned one to less than 9: 4 u 12 + u 9 for it, times w below 6, and
+    # the product's rounding u 54: 400 u; turned, two of them and 4 u 2 54 + u 77 of its own: 1310 u
+    assert all(float(x.detach().abs().max()) < 6 for x in (q, k, w))
+    for x, y in ((q, q64), (k, k64)):
+        assert (x.grad.double() - y.grad).abs().max() < 1310 * 2.0 ** -24
+
+
+@pytest.mark.parametrize("which", ["q", "k", "q_out", "k_out"])
+def test_a_rotation_that_a_backward_pass_would_not_see_is_refused(which):
+    rot = gkv.Rotary(plain(128), device=DEV)
+    pos = torch.zeros(1, 2, dtype=torch.int32, device=DEV)
+    given = {n: torch.ones(1, 2, 1, 128, device=DEV) for n in ("q", "k", "q_out", "k_out")}
+    given[which].requires_grad_()
+    with pytest.raises(ValueError, match=f"{which} requires grad"):
+        rot.apply(pos, given["q"], given["k"], q_out=given["q_out"], k_out=given["k_out"])
+    with torch.no_grad():
+        rot.apply(pos, given["q"], given["k"], q_out=given["q_out"], k_out=given["k_out"])
+    assert (given["q_out"] == 1).all() and (given["k_out"] == 1).all()
+
+
 def test_written_tensors_count_as_changed():
     """Every tensor that a call writes: a backward pass that has kept one refuses it, as after torch's own writes. Those that are only read, and
     those of a refused call, do not."""
