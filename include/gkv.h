@@ -484,7 +484,8 @@ gkv_status gkv_rotary_apply(const gkv_rotary* rotary, int32_t type, int32_t batc
  *   k, v             [n_pages][n_kv_heads][page_size][row], token_major: [n_pages][page_size][n_kv_heads][row]
  *   k_scale, v_scale the same with [scales]
  * Row r of sequence i is row r % page_size of page page[i * stride + r / page_size]. A page may be in several places of the table (shared
- * rows); a call must not write a row twice. Places that no row of a call needs are not looked at. */
+ * rows); a call must not write a row twice. All batch x width places have to be readable memory (an attention fetches some before it knows the
+ * lengths); what stands in those that no row of a call needs does not matter. */
 typedef struct {
     int32_t format;                        /* gkv_store_format                                        */
     int32_t n_q_heads, n_kv_heads, head_dim;   /* head_dim 128; n_q_heads / n_kv_heads <= 8           */

@@ -78,6 +78,33 @@ def test_waits_that_are_taken_for_expired(fmt, page, token_major):
         assert torch.equal(o, out) and torch.equal(l, lse)
 
 
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3", "int8", "int4"])
+@pytest.mark.parametrize("page,width,append", [(16, 9, True), (16, 9, False), (5, 26, True), (24, 400, True), (5, 2000, False), (64, 200, True)])
+def test_what_stands_in_places_that_nobody_needs(fmt, page, width, append):
+    """Short and long calls, sequences that are left out and such without rows: numbers of no page, of pages full of NaN or of other sequences'
+    pages in the places behind a sequence's rows are as good as -1."""
+    lens, h_q, h_kv = [100, -1, 0, page, 17, -5, 127], 8, 2
+    st, table, g = cache(fmt, 65, lens, page, h_q, h_kv)
+    need = [0 if n < 0 else -(-(n + append) // page) for n in lens]
+    at = np.arange(width)[None, :] < np.array(need)[:, None]
+    table = np.where(at, np.pad(table, ((0, 0), (0, max(0, width - table.shape[1]))))[:, :width], -1)
+    nan = next(i for i in range(st.pages) if i not in table)
+    x = torch.full((1, page, h_kv, 128), float("nan"), device=DEV, dtype=torch.bfloat16)
+    st.append(ints([[nan]]), x, x)
+    q, k1, v1 = rows(g, 7, h_q, 128), rows(g, 7, h_kv, 128), rows(g, 7, h_kv, 128)
+    kw = dict(k_new=k1, v_new=v1) if append else {}
+    got = []
+    for odd in (None, [-2 ** 31, 2 ** 31 - 1, st.pages, nan], [nan, int(table[0, 0])]):
+        t = table if odd is None else np.where(at, table, np.array(odd)[np.arange(7 * width).reshape(7, width) % len(odd)])
+        out, lse = torch.full_like(q, 7), torch.full((7, h_q), 7.0, device=DEV)
+        st.attn(ints(t), ints(lens), q, out, lse=lse, **kw)
+        got.append((out, lse, *(x.view(torch.uint8).clone() for x in (st.k, st.v, st.k_scale, st.v_scale) if x is not None)))
+    out, lse = got[0][:2]
+    assert torch.isfinite(out).all() and (out[[1, 5]] == 7).all() and (lse[[1, 5]] == 7).all() and not (out[[0, 3, 4, 6]] == 7).all(-1).any()
+    for other in got[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(got[0], other))
+
+
 # ---------------------------------------------------------------------------------------------- next to a backward pass
 class Turn(torch.autograd.Function):
     """The rotation in a model that is trained."""
