@@ -292,7 +292,7 @@ cudaError_t launch_rotary(RotaryLaunch& p, int type, int head_dim, int sm_count,
 cudaError_t launch_pages_append(const PagesCopyLaunch& p, cudaStream_t s);
 cudaError_t launch_pages_read(const PagesCopyLaunch& p, cudaStream_t s);
 cudaError_t launch_pages_attn(const PagesAttnLaunch& p, int format, cudaStream_t s);        // a cluster (or one CTA) a unit
-cudaError_t launch_pages_stream(const PagesAttnLaunch& p, int format, int ctas, int expire, cudaStream_t s);   // equal shares for all warps, then the merge
+cudaError_t launch_pages_stream(const PagesAttnLaunch& p, int format, int ctas, int expire, int sms, cudaStream_t s);   // equal shares for all warps, then the merge
 int pages_attn_ctas_per_sm(int format);
 int pages_stream_warps_per_sm(const PagesAttnLaunch& p, int format);
 int device_sm_count();                                                                      // of the current device

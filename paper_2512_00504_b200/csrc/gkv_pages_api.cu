@@ -147,9 +147,9 @@ gkv_status run_attn(const gkv_pages* pages, const gkv_page_table* table, const i
     p.batch = table->batch; p.h_q = pages->n_q_heads; p.h_kv = pages->n_kv_heads; p.g = p.h_q / p.h_kv; p.capacity = capacity;
     p.scale_log2 = (float)(1.4426950408889634 / sqrt((double)kHeadDim));
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
-    const int stream_ctas = pages_plan(&p, pages->format, max_len > 0 ? max_len : capacity, device_sm_count());
+    const int sms = device_sm_count(), stream_ctas = pages_plan(&p, pages->format, max_len > 0 ? max_len : capacity, sms);
     if (expire != kNeverExpire && !stream_ctas) return GKV_ERR_UNSUPPORTED;
-    const cudaError_t e = stream_ctas ? launch_pages_stream(p, pages->format, stream_ctas, expire, s) : launch_pages_attn(p, pages->format, s);
+    const cudaError_t e = stream_ctas ? launch_pages_stream(p, pages->format, stream_ctas, expire, sms, s) : launch_pages_attn(p, pages->format, s);
     if (e != cudaSuccess) { (void)cudaGetLastError(); return GKV_ERR_CUDA; }
     return GKV_OK;
 }

@@ -1,4 +1,5 @@
-// Where a warp of the paged attention is in its ring of copies. Plain C++, so that a host compiler can check it.
+// Where a warp of the paged attention is in its ring of copies, and the shape of the merge behind it. Plain C++, so that a host compiler
+// can check it.
 #pragma once
 
 #include <stdint.h>
@@ -28,6 +29,18 @@ struct RingPlace {
 template <int S, class Wait>
 GKV_HOST_DEVICE void drain_ring(RingPlace<S> at, int copies, Wait wait) {
     for (; copies > 0; --copies, at.next()) wait(at.stage, at.parity);
+}
+
+// The merge of `units` units on a device of `sms` SMs: 2^split CTAs a unit, which with few units are CTAs of 256 threads, two an SM, else
+// of 128, eight an SM, as many as fit the device at once.
+struct MergeShape {
+    bool few;
+    int split;
+};
+GKV_HOST_DEVICE MergeShape merge_shape(int64_t units, int sms) {
+    MergeShape m = {units <= 2ll * sms, 0};
+    while (m.split < (m.few ? 3 : 2) && (units << (m.split + 1)) <= (m.few ? 2ll : 8ll) * sms) ++m.split;
+    return m;
 }
 
 }  // namespace gkv

@@ -531,7 +531,7 @@ __global__ void __launch_bounds__(32, stream_warps(F, LIE != kApart)) gkv_pages_
 
 // Joins the partial results of a unit: a running softmax over them, kJoin at a time, all of whose loads are under way before the first is
 // looked at. A warp has two dimensions of every lane's (a slice), or kSlices times that; 2^split CTAs a unit, each with its slices, and 2^split shares of
-// the parts. It takes 5 to 8 us behind the stream, trips to memory one after the other. Up to 296 units: kJoin = 8, 128 registers, two CTAs of 256
+// the parts. It takes 5 to 8 us behind the stream, trips to memory one after the other. Up to two units an SM (296): kJoin = 8, 128 registers, two CTAs of 256
 // threads an SM (16 x 4 heads of 300 to 65535 keys, 100 parts of the longest: 2 at a time 219 us, 8 216). More of them: kJoin = 2, CTAs of 128 threads, so
 // that those of 1184 units fit the device at once (128 x 8 heads in 8 bits 110 us; with 256 threads, 740 at once, 112).
 template <int F, int kJoin, int kSlices>
@@ -674,7 +674,7 @@ __global__ void __launch_bounds__(256 / kSlices, kSlices == 2 ? 8 : 2) gkv_pages
 }
 
 template <int F, int LIE>
-static cudaError_t launch_stream(const PagesAttnLaunch& p, int ctas, int expire, cudaStream_t s) {
+static cudaError_t launch_stream(const PagesAttnLaunch& p, int ctas, int expire, int sms, cudaStream_t s) {
     constexpr int kSmem = (int)sizeof(StreamWarp<F>);
     static_assert(kSmem + 1024 <= 228 * 1024 / stream_warps(F, LIE != kApart), "room for all warps of an SM");
     const auto kernel = gkv_pages_stream_kernel<F, LIE>;
@@ -685,36 +685,34 @@ static cudaError_t launch_stream(const PagesAttnLaunch& p, int ctas, int expire,
     e = cudaGetLastError();
     if (e != cudaSuccess) return e;
     const int units = p.batch * p.h_kv;
-    // CTAs a unit, and warps that share its parts: few units have many parts, and all the CTAs fit the device at once (148 SMs).
-    int split = 0;
-    const bool many = units <= 2 * 148;
-    while (split < (many ? 3 : 2) && (units << (split + 1)) <= (many ? 2 : 8) * 148) ++split;
+    // CTAs a unit, and warps that share its parts: few units have many parts
+    const MergeShape shape = merge_shape(units, sms);
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)units << split);
-    cfg.blockDim = dim3(many ? 256 : 128);
+    cfg.gridDim = dim3((unsigned)units << shape.split);
+    cfg.blockDim = dim3(shape.few ? 256 : 128);
     cfg.stream = s;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, many ? gkv_pages_stream_merge_kernel<F, 8, 1> : gkv_pages_stream_merge_kernel<F, 2, 2>, p, ctas, split);
+    return cudaLaunchKernelEx(&cfg, shape.few ? gkv_pages_stream_merge_kernel<F, 8, 1> : gkv_pages_stream_merge_kernel<F, 2, 2>, p, ctas, shape.split);
 }
 static bool rows_together(const PagesAttnLaunch& p) { return p.pages.token_rows == 1 && p.pages.page_size % kTile == 0; }
 int pages_stream_warps_per_sm(const PagesAttnLaunch& p, int format) { return stream_warps(format, rows_together(p)); }
 template <int F>
-static cudaError_t launch_format(const PagesAttnLaunch& p, int ctas, int expire, cudaStream_t s) {
-    if (!rows_together(p)) return launch_stream<F, kApart>(p, ctas, expire, s);
+static cudaError_t launch_format(const PagesAttnLaunch& p, int ctas, int expire, int sms, cudaStream_t s) {
+    if (!rows_together(p)) return launch_stream<F, kApart>(p, ctas, expire, sms, s);
     if constexpr (stream_tiles(F) > 1)
-        if (p.pages.page_size % StreamWarp<F>::kKeys != 0) return launch_stream<F, kTiles>(p, ctas, expire, s);
-    return launch_stream<F, kSteps>(p, ctas, expire, s);
+        if (p.pages.page_size % StreamWarp<F>::kKeys != 0) return launch_stream<F, kTiles>(p, ctas, expire, sms, s);
+    return launch_stream<F, kSteps>(p, ctas, expire, sms, s);
 }
-cudaError_t launch_pages_stream(const PagesAttnLaunch& p, int format, int ctas, int expire, cudaStream_t s) {
+cudaError_t launch_pages_stream(const PagesAttnLaunch& p, int format, int ctas, int expire, int sms, cudaStream_t s) {
     switch (format) {
-        case GKV_STORE_BF16: return launch_format<GKV_STORE_BF16>(p, ctas, expire, s);
-        case GKV_STORE_E4M3: return launch_format<GKV_STORE_E4M3>(p, ctas, expire, s);
-        case GKV_STORE_INT8: return launch_format<GKV_STORE_INT8>(p, ctas, expire, s);
-        default:             return launch_format<GKV_STORE_INT4>(p, ctas, expire, s);
+        case GKV_STORE_BF16: return launch_format<GKV_STORE_BF16>(p, ctas, expire, sms, s);
+        case GKV_STORE_E4M3: return launch_format<GKV_STORE_E4M3>(p, ctas, expire, sms, s);
+        case GKV_STORE_INT8: return launch_format<GKV_STORE_INT8>(p, ctas, expire, sms, s);
+        default:             return launch_format<GKV_STORE_INT4>(p, ctas, expire, sms, s);
     }
 }
 

@@ -1,5 +1,6 @@
-"""A warp's ring of copies in the paged attention (csrc/gkv_pages_steps.h), compiled for the host: a warp that gives up waits for exactly the
-copies that are under way, whichever step it gives up at; and the arguments of the self-test that takes this path."""
+"""A warp's ring of copies in the paged attention and the shape of its merge (csrc/gkv_pages_steps.h), compiled for the host: a warp that
+gives up waits for exactly the copies that are under way, whichever step it gives up at; the merge fits the device that it is for; and the
+arguments of the self-test that takes the first path."""
 import ctypes
 import subprocess
 from pathlib import Path
@@ -48,13 +49,39 @@ int main() {
 """
 
 
-def test_copies_under_way_where_a_warp_gives_up(tmp_path):
-    (tmp_path / "ring.cc").write_text(PROGRAM)
-    exe = tmp_path / "ring"
+MERGE = r"""
+#include <stdio.h>
+#include "gkv_pages_steps.h"
+int main() {
+    for (int sms : {1, 16, 74, 132, 148, 160})
+        for (int64_t units = 1; units <= 16384; ++units) {
+            const gkv::MergeShape m = gkv::merge_shape(units, sms);
+            const int64_t room = (m.few ? 2 : 8) * sms;      // CTAs that the device holds
+            const int most = m.few ? 3 : 2;
+            if (m.few != (units <= 2 * sms) || m.split < 0 || m.split > most) return printf("%d %ld\n", sms, (long)units);
+            if (m.split > 0 && (units << m.split) > room) return printf("%d %ld: more than fit\n", sms, (long)units);
+            if (m.split < most && (units << (m.split + 1)) <= room) return printf("%d %ld: room left\n", sms, (long)units);
+        }
+    return 0;
+}
+"""
+
+
+def run(tmp_path, program):
+    (tmp_path / "steps.cc").write_text("#include <initializer_list>\n" + program)
+    exe = tmp_path / "steps"
     subprocess.check_call(["g++", "-O1", "-std=c++17", "-fsanitize=undefined", "-fno-sanitize-recover=all", "-I",
-                           str(ROOT / "paper_2512_00504_b200" / "csrc"), "-o", str(exe), str(tmp_path / "ring.cc")])
+                           str(ROOT / "paper_2512_00504_b200" / "csrc"), "-o", str(exe), str(tmp_path / "steps.cc")])
     r = subprocess.run([str(exe)], capture_output=True, text=True, timeout=300)
     assert r.returncode == 0, r.stdout + r.stderr
+
+
+def test_copies_under_way_where_a_warp_gives_up(tmp_path):
+    run(tmp_path, PROGRAM)
+
+
+def test_the_merge_fits_the_device(tmp_path):
+    run(tmp_path, MERGE)
 
 
 def test_selftest_arguments():
