@@ -105,6 +105,59 @@ def test_what_stands_in_places_that_nobody_needs(fmt, page, width, append):
         assert all(torch.equal(a, b) for a, b in zip(got[0], other))
 
 
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3", "int8", "int4"])
+@pytest.mark.parametrize("page,places,interleaved", [(16, 12, False), (5, 36, True), (16, 520, True)])      # short calls, and long ones
+def test_every_byte_that_a_captured_step_leaves(fmt, page, places, interleaved):
+    """A captured step that rotates, appends and attends, replayed while lengths and tables grow, next to the same calls one by one: all bytes of
+    rows and scales of K and V are the same, those that the steps wrote and all others, which are as they were."""
+    B, h_q, h_kv, n_pages = 3, 8, 2, 120
+    g = gen(66)
+    rot = gkv.Rotary(plain(64), interleaved=interleaved, device=DEV)
+    st, two = (gkv.PagedStore(fmt, pages=n_pages, page_size=page, h_q=h_q, h_kv=h_kv, max_batch=B, device=DEV) for _ in range(2))
+    every = torch.arange(n_pages, dtype=torch.int32, device=DEV)[:, None]
+    x = rows(g, 2, n_pages, page, h_kv, 128)
+    for s in (st, two):
+        s.append(every, x[0], x[1])
+    buffers = [[t.view(torch.uint8) for t in (s.k, s.v, s.k_scale, s.v_scale) if t is not None] for s in (st, two)]
+    order = np.random.RandomState(4).permutation(n_pages)
+    table, length, used = torch.full((B, places), -1, dtype=torch.int32, device=DEV), ints([0, 14, 31]), 0
+
+    def grow():
+        nonlocal used
+        for b, n in enumerate(length.tolist()):
+            for p in range(n // page + 1):
+                if table[b, p] < 0:
+                    table[b, p] = int(order[used])
+                    used += 1
+
+    grow()
+    q, k1, v1 = rows(g, B, h_q, 128), rows(g, B, h_kv, 128), rows(g, B, h_kv, 128)
+    out, lse = torch.zeros_like(q), torch.zeros(B, h_q, device=DEV)
+    for s in (st, two):                                    # not captured: modules are loaded
+        s.attn(table, length, q, out, k_new=k1, v_new=v1, rotary=rot, lse=lse)
+    start = [b.clone() for b in buffers[1]]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        st.attn(table, length, q, out, k_new=k1, v_new=v1, rotary=rot, lse=lse)
+    written = torch.zeros(n_pages, page, dtype=torch.bool, device=DEV)
+    for _ in range(40):
+        q.copy_(rows(g, B, h_q, 128)), k1.copy_(rows(g, B, h_kv, 128)), v1.copy_(rows(g, B, h_kv, 128))
+        graph.replay()
+        o2, l2 = torch.empty_like(out), torch.empty_like(lse)
+        turned = torch.empty_like(k1)
+        rot.apply(length[:, None], k1[:, None], q_out=turned[:, None])
+        two.append(table, turned[:, None], v1[:, None], first=length)
+        two.attn(table, length + 1, q, o2, rotary=rot, lse=l2)
+        assert torch.equal(out, o2) and torch.equal(lse, l2)
+        for b, n in enumerate(length.tolist()):
+            written[int(table[b, n // page]), n % page] = True
+        length += 1
+        grow()
+    for a, b, c in zip(*buffers, start):
+        assert torch.equal(a, b)
+        assert torch.equal(a.transpose(1, 2)[~written], c.transpose(1, 2)[~written])
+
+
 # ---------------------------------------------------------------------------------------------- next to a backward pass
 class Turn(torch.autograd.Function):
     """The rotation in a model that is trained."""
