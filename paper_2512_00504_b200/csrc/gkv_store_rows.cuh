@@ -403,9 +403,14 @@ struct RunningRows {
         // (at most the limit then), infinite or NaN, also at the first step, where m is -infinity.
         float total = 0.f;
         auto weigh = [&]() {
-            const float2 n = make_float2(-n0, -n1), d0 = add2(make_float2(z[0], z[1]), n), d1 = add2(make_float2(z[2], z[3]), n);
-            e[0] = fast_exp2(d0.x); e[1] = fast_exp2(d0.y);
-            e[2] = fast_exp2(d1.x); e[3] = fast_exp2(d1.y);
+            if constexpr (NG == 1) {    // (in pairs: 128 x 8 heads of 2200 keys in 8 bits 96.5 us instead of 96.2, with shared documents 145.7 and 144.4)
+                e[0] = fast_exp2(z[0] - n0); e[1] = fast_exp2(z[1] - n1);
+                e[2] = fast_exp2(z[2] - n0); e[3] = fast_exp2(z[3] - n1);
+            } else {
+                const float2 n = make_float2(-n0, -n1), d0 = add2(make_float2(z[0], z[1]), n), d1 = add2(make_float2(z[2], z[3]), n);
+                e[0] = fast_exp2(d0.x); e[1] = fast_exp2(d0.y);
+                e[2] = fast_exp2(d1.x); e[3] = fast_exp2(d1.y);
+            }
             total += (e[0] + e[2]) + (e[1] + e[3]);
             if constexpr (NG > 1) {
                 float2 sum = make_float2(0.f, 0.f);
