@@ -216,7 +216,7 @@ struct PagesCopyLaunch {       // append / read
     int head_blocks, heads_per_cta, tokens_per_half;   // how an append is cut (launch_pages_append)
 };
 // Partial result of a warp's part of a unit, two a warp: M[8], L[8], Mv[groups][8], O[8][32 lanes][4] as the lanes hold them. A warp takes
-// at least kStreamLeast tiles.
+// at least kStreamLeast steps (of one tile with bf16 rows, two with scaled ones).
 constexpr int kStreamRecHead = 48, kStreamRecFloats = kStreamRecHead + kHeadDimHost * 8;
 constexpr int kStreamLeast = 4;
 constexpr int kStreamMaxWarps = 2560;
