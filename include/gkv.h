@@ -441,7 +441,7 @@ typedef struct {
 } gkv_rotary;
 
 /* Rows to rotate: element (i, t, h, e) of x at i * x_stride[0] + t * x_stride[1] + h * x_stride[2] + e, and y likewise (strides in
- * elements; aligned to their type). y is x itself (with the same strides) or does not overlap it. */
+ * elements; aligned to their type). y is x itself (with the same strides) or does not overlap it; nor does it the other tensor of a call. */
 typedef struct {
     const void* x;
     void* y;
@@ -463,8 +463,8 @@ typedef struct {
  * PLAIN scale < 1 or not finite; for the last two original < 1, low <= 0, high <= low, or not finite). */
 gkv_status gkv_rotary_frequencies(double theta, int32_t rot_dim, int32_t scaling, double scale, double original, double low, double high,
                                   double* radians, float* factor);
-/* Host: radians[n] -> turns[n], rounded to the nearest 2^-64 of a turn. Errors: INVALID_ARG (NULL, n < 0, a value that is not finite or
- * above 2^20 in magnitude). */
+/* Host: radians[n] -> turns[n], whole numbers of 2^-64 of a turn: below one radian the nearest or the one beside it, above within
+ * 2 (1 + |radians| / 2 pi) of it. Errors: INVALID_ARG (NULL, n < 0, a value that is not finite or above 2^20 in magnitude). */
 gkv_status gkv_rotary_turns(const double* radians, int32_t n, uint64_t* turns);
 
 /* Rotate tokens 0..count[i] - 1 of sequence i in q and, if there is one, k (NULL: none), both [batch][n_tokens][their heads][head_dim] of

@@ -17,9 +17,9 @@
 //
 // Reading back takes kRun tokens of a head, so that scales come with one access.
 //
-// Measured: 4 x 32768 tokens x 8 heads, rotated: in bf16 160 us (1.07 GB, 6.7 TB/s), in 8 bits 132 to 138, in 4 bits 141 to 145; without the rotation 165,
-// 120 and 102; back in 163, 127 and 109. 8 prompts of 129 to 4097 tokens x 4 heads 17 to 18.5 us (without the rotation 16, 13, 12.5), back in 16.2, 13.7
-// and 12.2. One token of 32 sequences x 4 heads: 2.3 us in bf16, 2.8 to 3.1 in the others (1.7 and 2.4 without the rotation), back in 2.
+// Measured: 4 x 32768 tokens x 8 heads, rotated: in bf16 160 us (1.07 GB, 6.7 TB/s), in 8 bits 132 to 140, in 4 bits 141 to 150; without the rotation 164,
+// 120 and 102 to 105; back in 162, 127 and 109. 8 prompts of 129 to 4097 tokens x 4 heads 17 to 18 us (without the rotation 16, 13.3, 12.5), back in 16.1,
+// 13.6 and 12.1. One token of 32 sequences x 4 heads: 2.3 us in bf16, 2.8 to 3.1 in the others (1.7 and 2.4 without the rotation), back in 2.
 #include "gkv_pages.cuh"
 #include "gkv_rotary.cuh"
 #include "gkv_store_rows.h"

@@ -71,7 +71,7 @@ constexpr int kStreamFrom = 6;
 
 // A cluster of up to kMaxCluster CTAs a unit, if that leaves a warp no more than kStreamFrom tiles (or there are more units than the merge of the
 // other form is made for); else equal shares for all warps. Returns the CTAs of the latter, 0 for the former. Both sides, measured: 32 x 4 heads of
-// up to 1151 keys in 8 bits, 5 to 6 tiles a warp, 15 us in clusters, 30 in equal shares, which have the merge to pay; 1 x 4 heads of 4096 keys in
+// up to 1151 keys in 8 bits, 5 to 6 tiles a warp, 15 us in clusters, 22 in equal shares, which have the merge to pay; 1 x 4 heads of 4096 keys in
 // bf16, 8 tiles a warp, 14.3 and 12.8.
 int pages_plan(PagesAttnLaunch* p, int format, int max_len, int sm_count) {
     const int64_t units = (int64_t)p->batch * p->h_kv;

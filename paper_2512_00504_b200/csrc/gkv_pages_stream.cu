@@ -20,8 +20,8 @@
 // A wait that runs out (never, but every wait ends) makes the warp's units NaN, too.
 //
 // Measured (with the merge; the time that the rows' bytes take at 6.46 TB/s): 128 sequences x 8 heads of about 2200 keys in bf16 in pages of 64
-// 187 to 190 us (177), of 16 188 to 190, of 5 197 to 199; in 8 bits in pages of 64 109 (90), of 5 149; in 4 bits 102 (50) and 159. 16 x 4 heads of 300
-// to 65535 keys in bf16 216 (206). 2 x 8 heads of up to 131071 in 4 bits 83 (42). 16-bit rows are bound by HBM. With 4-bit rows the warps
+// 187 to 190 us (177), of 16 187 to 190, of 5 196 to 199; in 8 bits in pages of 64 109 to 112 (90), of 5 149; in 4 bits 101 (50) and 160. 16 x 4 heads of 300
+// to 65535 keys in bf16 216 (206). 2 x 8 heads of up to 131071 in 4 bits 82 to 83 (42). 16-bit rows are bound by HBM. With 4-bit rows the warps
 // issue in 60% of all cycles, 420 instructions a tile, of which 170 unpack codes: instructions and what they wait for bound it.
 #include "gkv_pages.cuh"
 #include "gkv_pages_steps.h"

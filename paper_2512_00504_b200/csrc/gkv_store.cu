@@ -7,8 +7,8 @@
 // gathered in the lanes and go with one access (2 bytes at a time they cost a 32-byte sector each). Neighbouring half warps
 // have the neighbouring heads of the same tokens, which lie next to each other on the bf16 side.
 //
-// Measured (bytes of both sides): 4 x 32768 tokens x 8 heads into 4 bits, 688 MB in 111 us: 6.2 TB/s, and back in 106; into 8 bits,
-// 809 MB in 143 to 147 us: 5.6 TB/s, and back in 123; bf16, 1074 MB in 160 us either way: 6.7 TB/s; 64 x about 1900 tokens x 8 heads
+// Measured (bytes of both sides): 4 x 32768 tokens x 8 heads into 4 bits, 688 MB in 113 us: 6.1 TB/s, and back in 108; into 8 bits,
+// 809 MB in 133 to 139 us: 6 TB/s, and back in 123; bf16, 1074 MB in 160 us either way: 6.7 TB/s; 64 x about 1900 tokens x 8 heads
 // back from e4m3, 738 MB in 113 us: 6.5 TB/s; one token of 32 sequences x 4 heads: 2 us, which is a launch.
 #include "gkv_store_codes.cuh"
 #include "gkv_store_rows.h"

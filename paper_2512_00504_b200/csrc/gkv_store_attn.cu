@@ -28,10 +28,10 @@
 // that one long sequence among short ones gets the places that they do not need.
 //
 // Bound by HBM for 8-bit rows in a large batch (128 sequences x 8 heads of about 2200 keys, 585 MB: 97 us, 6.0 TB/s). 4-bit rows
-// bring twice the elements per byte to unpack: 2 x 8 heads of about 120000 keys, 274 MB in 77 us, 3.6 TB/s, with the schedulers
+// bring twice the elements per byte to unpack: 2 x 8 heads of about 120000 keys, 274 MB in 73 us, 3.7 TB/s (before fp32 operations went in pairs 77), with the schedulers
 // issuing 6 cycles out of 10, the logic and fp32 pipes 4 to 5 (without the products and what feeds them the same loads take 55
 // us; with one reference for all groups of a head, which is not precise enough, 75.7). bf16 rows: 128 sequences x 8 heads of 2200
-// keys, 1153 MB in 197 us, 5.9 TB/s. A single sequence of 640 keys takes 7.0 us: the launch, four trips to memory (length, q, rows,
+// keys, 1153 MB in 197 us, 5.9 TB/s. A single sequence of 640 keys takes 6.4 us: the launch, four trips to memory (length, q, rows,
 // the others' results) one after the other, 3 tiles per warp.
 #include "gkv_store_rows.cuh"
 
